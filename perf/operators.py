@@ -1,11 +1,12 @@
-"""Cases of the operators on the tokens of a window: route counts, the router with its balance loss, its gradient, and the rotation
-of queries and keys in packed rows with its gradient.
+"""Cases of the operators on the tokens of a window: route counts, the router with its balance loss, the rotation of queries and keys in
+packed rows and the attention inside their samples, with their gradients.
 
 ``own`` says which side ``run`` computes: the plain form (elementary torch operations in 32 bits, angles in 64) or the calls of this
 framework's entry points.  Sizes of experts, layers and choices per token are those of the framework's windows; samples' lengths are
 lognormal as theirs; head counts and widths are generic.
 """
 import math
+import random
 
 import torch
 
@@ -20,29 +21,30 @@ EPS = 1e-6
 
 def listed():
     return [
-        # the record of a small window: a few short samples, four layers
-        {"name": "counts small", "op": "counts", "tokens": 5003, "samples": 16, "layers": 4, "experts": 16, "k": 2, "type": "i32", "order": "token"},
+        # the record of a small window: a few short samples, four layers, kept layer after layer by a trainer
+        {"name": "counts small", "op": "counts", "tokens": 5003, "samples": 16, "layers": 4, "experts": 16, "k": 2, "type": "i32", "order": "layer"},
         # the record of a step's window, kept in bytes per token as a serving engine hands it over
         {"name": "counts step", "op": "counts", "tokens": 900001, "samples": 640, "layers": 32, "experts": 128, "k": 8, "type": "u8", "order": "token"},
-        # the same kept layer after layer by a trainer, 256 experts
-        {"name": "counts by layer", "op": "counts", "tokens": 260017, "samples": 301, "layers": 48, "experts": 256, "k": 8, "type": "i16", "order": "layer"},
         # one decoding step of a few sequences
         {"name": "route decode", "op": "route", "tokens": 16, "groups": 1, "experts": 256, "k": 8, "type": "bf16", "score": "sigmoid", "replay": False},
         # a cell of 32768 tokens, loss for each sample, routes chosen
         {"name": "route samples", "op": "route", "tokens": 32768, "groups": 41, "experts": 64, "k": 4, "type": "f32", "score": "softmax", "replay": False},
-        # the largest cell of the widest window, routes replayed as reinforcement learning does
-        {"name": "route replay", "op": "route", "tokens": 131072, "groups": 33, "experts": 256, "k": 8, "type": "bf16", "score": "softmax", "replay": True},
-        # the same with the routes chosen and one group
+        # the largest cell of the widest window, the loss over the whole of it
         {"name": "route wide", "op": "route", "tokens": 131072, "groups": 1, "experts": 256, "k": 8, "type": "bf16", "score": "sigmoid", "replay": False},
-        # backward passes: an odd small cell, and the largest
-        {"name": "route grad small", "op": "route_grad", "tokens": 4099, "groups": 7, "experts": 128, "k": 8, "type": "bf16", "score": "softmax", "replay": False},
-        {"name": "route grad wide", "op": "route_grad", "tokens": 131072, "groups": 33, "experts": 256, "k": 8, "type": "bf16", "score": "sigmoid", "replay": True},
+        # its backward pass, routes replayed as reinforcement learning does, loss for each sample
+        {"name": "route grad wide", "op": "route_grad", "tokens": 131072, "groups": 33, "experts": 256, "k": 8, "type": "bf16", "score": "softmax", "replay": True},
         # decoding: one token of each sequence, far into its context
         {"name": "rotate decode", "op": "rotate", "tokens": 64, "samples": 64, "q": 32, "k": 8, "dim": 128, "rotary": 128, "layout": "half", "norm": True, "type": "bf16", "far": 400000},
         # a packed row in training
         {"name": "rotate row", "op": "rotate", "tokens": 32768, "samples": 29, "q": 32, "k": 8, "dim": 128, "rotary": 128, "layout": "half", "norm": True, "type": "bf16", "far": 0},
         # the backward pass of a row, a part of each head rotated, neighbours paired
         {"name": "rotate grad row", "op": "rotate_grad", "tokens": 16411, "samples": 37, "q": 32, "k": 8, "dim": 128, "rotary": 64, "layout": "interleaved", "norm": True, "type": "bf16", "far": 0},
+        # a row of many short samples
+        {"name": "attend ragged", "op": "attend", "tokens": 4096, "samples": 23, "q": 16, "k": 16, "dim": 64, "causal": True, "type": "f16"},
+        # a row of a few long ones, four query heads to a key head
+        {"name": "attend long", "op": "attend", "tokens": 12289, "samples": 2, "q": 16, "k": 4, "dim": 128, "causal": True, "type": "bf16"},
+        # the backward pass
+        {"name": "attend grad", "op": "attend_grad", "tokens": 8192, "samples": 3, "q": 16, "k": 4, "dim": 128, "causal": True, "type": "bf16"},
     ]
 
 
@@ -51,7 +53,11 @@ def spread(rng, low, high):
 
 
 def draw(rng):
-    op = rng.choice(["counts", "route", "route_grad", "rotate", "rotate_grad"])
+    op = rng.choice(["counts", "route", "route_grad", "rotate", "rotate_grad", "attend", "attend_grad"])
+    if op in ("attend", "attend_grad"):
+        q, k = rng.choice([(16, 4), (16, 16), (8, 2), (12, 4), (5, 1)])
+        return {"op": op, "tokens": spread(rng, 1, 12289 if op == "attend" else 8192), "samples": rng.choice([1, 1, 2, 5, 17, 60]), "q": q, "k": k,
+                "dim": rng.choice([64, 128]), "causal": rng.random() < 0.8, "type": rng.choice(["bf16", "f16"])}
     if op == "counts":
         experts, k = rng.choice([(16, 2), (64, 4), (128, 8), (256, 8)])
         layers = rng.choice([4, 16, 23, 32, 48])
@@ -81,6 +87,18 @@ def cut(gen, tokens, parts):
     start = torch.zeros(parts + 1, dtype=torch.int64, device="cuda")
     start[1:] = inner + torch.arange(1, parts + 1, device="cuda")
     start[parts] = tokens
+    return start
+
+
+def sample_starts(case):
+    """Starts of a row's samples, the same for every seed: lengths of a lognormal law, none of no token where the tokens suffice."""
+    rng = random.Random(case["tokens"])
+    weight = [math.exp(rng.gauss(0.0, 0.8)) for _ in range(case["samples"])]
+    spare, start, done = max(0, case["tokens"] - case["samples"]), [0], 0.0
+    for i, w in enumerate(weight):
+        done += w
+        start.append(min(case["tokens"], int(spare * done / sum(weight)) + i + 1))
+    start[-1] = case["tokens"]
     return start
 
 
@@ -121,8 +139,17 @@ def prepare(case, seed):
             group = torch.searchsorted(st["start"], torch.arange(T, device="cuda"), right=True) - 1
             st["counts"] = torch.bincount((group[:, None] * E + st["routes"]).reshape(-1), minlength=case["groups"] * E).view(-1, E).to(torch.int32)
         return st
-    d, r = case["dim"], case["rotary"]
+    d = case["dim"]
     kind = TYPES[case["type"]]
+    if case["op"] in ("attend", "attend_grad"):
+        st["start"] = torch.tensor(sample_starts(case), device="cuda")
+        for name, heads in (("q", case["q"]), ("k", case["k"]), ("v", case["k"])):
+            st[name] = torch.randn(T, heads, d, generator=gen, device="cuda").to(kind)
+        if case["op"] == "attend_grad":
+            st["grad"] = torch.randn(T, case["q"], d, generator=gen, device="cuda").to(kind)
+            st["out"], st["lse"] = plain_attend(st)
+        return st
+    r = case["rotary"]
     st["start"] = cut(gen, T, case["samples"])
     st["first"] = torch.randint(0, case["far"], (case["samples"],), generator=gen, device="cuda") if case["far"] else None
     scale = torch.exp(torch.randn(T, 1, 1, generator=gen, device="cuda") * 0.5)
@@ -244,7 +271,44 @@ def plain_rotate_grad(st):
     return dq, dk, dwq, dwk
 
 
-PLAIN = {"counts": plain_counts, "route": plain_route, "route_grad": plain_route_grad, "rotate": plain_rotate, "rotate_grad": plain_rotate_grad}
+def plain_weights(st):
+    """Attention weights [heads, T, T] inside the samples, the log of each row's sum, and keys' and values' heads for each query head."""
+    c = st["case"]
+    T, share = c["tokens"], c["q"] // c["k"]
+    q = st["q"].float().transpose(0, 1)
+    k, v = (st[n].float().transpose(0, 1).repeat_interleave(share, 0) for n in ("k", "v"))
+    sample = owner(st["start"], T)
+    seen = sample[:, None] == sample
+    if c["causal"]:
+        seen &= torch.ones(T, T, dtype=torch.bool, device="cuda").tril_()
+    s = torch.matmul(q, k.transpose(1, 2)).mul_(c["dim"] ** -0.5).masked_fill_(~seen, -math.inf)
+    top = s.amax(2, keepdim=True)
+    p = s.sub_(top).exp_()
+    total = p.sum(2, keepdim=True)
+    return p.div_(total), (top + torch.log(total)).squeeze(2), q, k, v
+
+
+def plain_attend(st):
+    p, lse, _, _, v = plain_weights(st)
+    return torch.matmul(p, v).transpose(0, 1).to(st["q"].dtype).contiguous(), lse.transpose(0, 1).contiguous()
+
+
+def plain_attend_grad(st):
+    c = st["case"]
+    p, _, q, k, v = plain_weights(st)
+    do = st["grad"].float().transpose(0, 1)
+    dv = torch.matmul(p.transpose(1, 2), do)
+    ds = torch.matmul(do, v.transpose(1, 2)).sub_((do * torch.matmul(p, v)).sum(2, keepdim=True)).mul_(p)
+    dq = torch.matmul(ds, k) * c["dim"] ** -0.5
+    dk = torch.matmul(ds.transpose(1, 2), q) * c["dim"] ** -0.5
+
+    def shared(x):
+        return x.view(c["k"], -1, c["tokens"], c["dim"]).sum(1).transpose(0, 1)
+
+    return tuple(x.to(st["q"].dtype).contiguous() for x in (dq.transpose(0, 1), shared(dk), shared(dv)))
+
+
+PLAIN = {"attend": plain_attend, "attend_grad": plain_attend_grad, "counts": plain_counts, "route": plain_route, "route_grad": plain_route_grad, "rotate": plain_rotate, "rotate_grad": plain_rotate_grad}
 
 
 def run(state):
@@ -261,6 +325,10 @@ def run(state):
     if c["op"] == "route_grad":
         return rp.rp_route_grad(state["logits"], state["routes"], state["start"], state["counts"], gates_grad=state["gates_grad"],
                                 loss_grad=state["loss_grad"], score=c["score"], normalise=True, loss_coef=COEF)
+    if c["op"] == "attend":
+        return rp.rp_attend(state["q"], state["k"], state["v"], state["start"], causal=c["causal"])
+    if c["op"] == "attend_grad":
+        return rp.rp_attend_grad(state["grad"], state["q"], state["k"], state["v"], state["out"], state["lse"], state["start"], causal=c["causal"])
     if c["op"] == "rotate":
         return rp.rp_rotate(state["q"], state["k"], state["inv_freq"], state["start"], first_position=state["first"],
                             q_weight=state["q_weight"], k_weight=state["k_weight"], eps=EPS, layout=c["layout"])
@@ -278,6 +346,13 @@ def work(case):
         if case["op"] == "route":
             return {"bytes": T * E * size + T * k * 8 + G * (E * 4 + 8), "flops": T * E * 5}
         return {"bytes": 2 * T * E * size + T * k * 8 + G * (E * 4 + 8), "flops": T * E * 8}
+    if case["op"] in ("attend", "attend_grad"):
+        start = sample_starts(case)
+        pairs = sum((hi - lo) * ((hi - lo + 1) / 2 if case["causal"] else hi - lo) for lo, hi in zip(start, start[1:]))
+        q, kv, lse = T * case["q"] * case["dim"] * size, T * case["k"] * case["dim"] * size, T * case["q"] * 4
+        if case["op"] == "attend":
+            return {"bytes": 2 * q + 2 * kv + lse, "flops": 4 * pairs * case["q"] * case["dim"]}
+        return {"bytes": 4 * q + 4 * kv + lse, "flops": 10 * pairs * case["q"] * case["dim"]}
     heads = T * (case["q"] + case["k"]) * case["dim"]
     n = 2 if case["op"] == "rotate" else 3
     return {"bytes": n * heads * size + case["samples"] * 8, "flops": heads * (6 if n == 2 else 14)}
@@ -313,6 +388,8 @@ def exact(case, seed):
             f = st["counts"][i].double() * E / (k * (hi - lo))
             value = value + st["loss_grad"].double()[0] * COEF / G * (f * p[lo:hi].mean(0)).sum()
         return torch.autograd.grad(value, x)[0]
+    if case["op"] in ("attend", "attend_grad"):
+        return exact_attention(case, st, start)
     r = case["rotary"]
     position = torch.cat([torch.arange(hi - lo, device="cuda") for lo, hi in zip(start, start[1:])]).double()
     if st["first"] is not None:
@@ -337,3 +414,28 @@ def exact(case, seed):
         dx.append(got[0])
         dw.append(None if w is None else got[1])
     return dx[0], dx[1], dw[0], dw[1]
+
+
+def exact_attention(case, st, start):
+    share, scale = case["q"] // case["k"], 1 / math.sqrt(case["dim"])
+    back = case["op"] == "attend_grad"
+    x = {n: st[n].double() for n in (("q", "k", "v", "grad") if back else ("q", "k", "v"))}
+    out, lse = torch.empty_like(x["q"]), torch.empty(case["tokens"], case["q"], device="cuda", dtype=torch.float64)
+    dq, dk, dv = torch.zeros_like(x["q"]), torch.zeros_like(x["k"]), torch.zeros_like(x["v"])
+    for lo, hi in zip(start, start[1:]):
+        for h in range(case["q"]):
+            q, k, v = x["q"][lo:hi, h], x["k"][lo:hi, h // share], x["v"][lo:hi, h // share]
+            s = q @ k.T * scale
+            if case["causal"]:
+                s += torch.full_like(s, -math.inf).triu(1)
+            lse[lo:hi, h] = torch.logsumexp(s, 1)
+            p = torch.softmax(s, 1)
+            out[lo:hi, h] = p @ v
+            if back:
+                do = x["grad"][lo:hi, h]
+                dp = do @ v.T
+                ds = p * (dp - (p * dp).sum(1, keepdim=True))
+                dq[lo:hi, h] = ds @ k * scale
+                dk[lo:hi, h // share] += ds.T @ q * scale
+                dv[lo:hi, h // share] += p.T @ do
+    return (dq, dk, dv) if back else (out, lse)
