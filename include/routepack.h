@@ -259,6 +259,39 @@ typedef struct {
 } rp_diag;
 int rp_diagnostics(rp_ctx *ctx, const int32_t *layout, rp_diag *out);
 
+/* ---- operators on the tokens of a window ------------------------------------------------
+ * What a trainer runs on the rows of a plan, and what its routers record for the next one.  They need no context.
+ *
+ * Conventions of this section (where it differs from the above):
+ *  - Every array is in DEVICE memory of one GPU (managed memory counts); a host pointer, or arrays of two GPUs, give
+ *    RP_ERR_ARG before anything is launched.  The GPU need not be the current one; the stream has to be one of that GPU.
+ *  - Calls queue their kernels on the stream and return: no synchronisation, no allocation, nothing kept between calls.
+ *    They may be captured into a CUDA graph.  Two calls that may run at once need workspaces of their own.
+ *  - Results do not depend on the order in which the GPU runs its threads: a call with the same arguments on the same kind
+ *    of GPU gives the same bits.
+ *  - Samples (or groups) are given by `start` [n+1] int64, not decreasing: sample i holds the tokens start[i] .. start[i+1]-1
+ *    (as far as they are in 0 .. n_tokens-1).  Samples may be empty.  A token that no sample holds gets zeros in every output
+ *    (routes: -1, which one byte holds as 255) and adds to no sum, whatever its inputs hold.  Rows of outputs behind n_tokens
+ *    are not touched.
+ *  - Strides count elements and may be negative or 0 for inputs; the last dimension is contiguous. */
+typedef enum { RP_F32 = 0, RP_F16 = 1, RP_BF16 = 2 } rp_type;
+
+/* Per-expert counts of recorded routes: demand[i][l][e] = how often the tokens of sample i chose expert e in layer l.
+ *   routes: element (t, l, j) at t * token_stride + l * layer_stride + j, j < top_k; route_bytes = 1 (unsigned), 2, 4 or 8 (signed).
+ *     Values outside [0, n_experts) (places left empty) are not counted.
+ *   demand [n_samples][n_layers][n_experts] int32, written whole: the input of rp_window_load.
+ * Limits: n_experts <= 1024, top_k <= 1024, n_layers * n_experts < 2^31. */
+int rp_count_routes(const void *routes, int32_t route_bytes, int64_t n_tokens, int32_t n_layers, int32_t top_k, int32_t n_experts,
+                    int64_t token_stride, int64_t layer_stride, const int64_t *start, int32_t n_samples, int32_t *demand,
+                    void *cuda_stream);
+
+/* rp_window_load from the record itself: sample i's tokens are the lengths[i] ones behind those of the samples before it, and the
+ * demand tensor is counted (as by rp_count_routes) into memory of the context.  lengths: host or device; routes: DEVICE memory
+ * of the current GPU, free again when the call returns.  RP_ERR_CONSERVATION when the lengths add up to more than n_tokens, a
+ * value is outside [0, n_experts), or a check of rp_window_load fails.  Conventions of the planner's calls (the call synchronises). */
+int rp_window_load_routes(rp_ctx **out, const rp_config *cfg, const int32_t *lengths, const void *routes, int32_t route_bytes,
+                          int64_t n_tokens, int64_t token_stride, int64_t layer_stride, void *cuda_stream);
+
 /* Frees the context.  Its device memory goes back to a per-device cache inside the library
  * (so that the next window does not pay for allocation); rp_release_cached_memory() returns
  * that cache to the driver. */

@@ -26,7 +26,8 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_best", "rp_destroy", "rp_release_cached_memory", "rp_strerror", "rp_last_cuda_error", "rp_debug_dump",
            "rp_debug_set_trace", "rp_debug_set_knob", "rp_debug_set_stage_timing", "rp_debug_stage_times",
            "rp_debug_nl2", "rp_debug_exp2neg", "rp_debug_philox", "rp_debug_launch_count", "rp_debug_l2_read_rate",
-           "rp_debug_chain_kernel", "rp_debug_chain_form")
+           "rp_debug_chain_kernel", "rp_debug_chain_form",
+           "rp_count_routes", "rp_window_load_routes")
 
 
 class RpError(RuntimeError):
@@ -103,6 +104,9 @@ def lib():
         L.rp_debug_l2_read_rate.argtypes = [C.c_int64, C.c_int32, C.POINTER(C.c_double)]
         L.rp_debug_chain_kernel.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
         L.rp_debug_chain_form.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
+        V, I, Q = C.c_void_p, C.c_int32, C.c_int64
+        L.rp_count_routes.argtypes = [V, I, Q, I, I, I, Q, Q, V, I, V, V]
+        L.rp_window_load_routes.argtypes = [C.POINTER(C.c_void_p), C.POINTER(rp_config), V, V, I, Q, Q, Q, V]
         _lib = L
     return _lib
 
@@ -157,20 +161,42 @@ class Context:
             pass
 
 
-def rp_window_load(lengths, demand, *, top_k: int, token_cap: int, dp_width: int, ep_width: int,
-                   pop_size: int, edp_of_dp: Optional[Sequence[int]] = None,
-                   alpha: Sequence[float] = (1.0, 1.0), beta: Sequence[float] = (0.0, 1.0),
-                   min_rows: int = 0, seed: int = 0, stream=None) -> Context:
-    n, l, e = tuple(demand.shape)
+def _window_config(n, l, e, top_k, token_cap, dp_width, ep_width, pop_size, edp_of_dp, alpha, beta, min_rows, seed):
+    """rp_config and the arrays it points to."""
     al = np.ascontiguousarray(alpha, dtype=np.float64)
     be = np.ascontiguousarray(beta, dtype=np.float64)
     edp = None if edp_of_dp is None else np.ascontiguousarray(edp_of_dp, dtype=np.int32)
     cfg = rp_config(n, l, e, top_k, token_cap, dp_width, ep_width, _ptr(edp), len(al), _ptr(al), _ptr(be),
                     pop_size, min_rows, seed)
+    return cfg, al, be, edp
+
+
+def rp_window_load(lengths, demand, *, top_k: int, token_cap: int, dp_width: int, ep_width: int,
+                   pop_size: int, edp_of_dp: Optional[Sequence[int]] = None,
+                   alpha: Sequence[float] = (1.0, 1.0), beta: Sequence[float] = (0.0, 1.0),
+                   min_rows: int = 0, seed: int = 0, stream=None) -> Context:
+    n, l, e = tuple(demand.shape)
+    cfg, al, be, edp = _window_config(n, l, e, top_k, token_cap, dp_width, ep_width, pop_size, edp_of_dp, alpha, beta, min_rows, seed)
     out = C.c_void_p(None)
     st = lib().rp_window_load(C.byref(out), C.byref(cfg), _ptr(lengths), _ptr(demand), _stream_handle(stream))
     _check(st, "rp_window_load")
     ctx = Context(out.value, cfg, (lengths, demand, al, be, edp))
+    ctx.n_shards = dp_width if edp is None else int(edp.max()) + 1
+    return ctx
+
+
+def rp_window_load_routes(lengths, routes, n_experts: int, *, token_cap: int, dp_width: int, ep_width: int, pop_size: int,
+                          edp_of_dp: Optional[Sequence[int]] = None, alpha: Sequence[float] = (1.0, 1.0),
+                          beta: Sequence[float] = (0.0, 1.0), min_rows: int = 0, seed: int = 0, stream=None) -> Context:
+    """A window from recorded routes (CUDA tensor [n_tokens, n_layers, top_k] of integers, any strides with the choices side by side)."""
+    T, l, k = routes.shape
+    size, ts, ls = _route_layout(routes)
+    cfg, al, be, edp = _window_config(int(lengths.shape[0]), l, n_experts, k, token_cap, dp_width, ep_width, pop_size, edp_of_dp, alpha, beta,
+                                      min_rows, seed)
+    out = C.c_void_p(None)
+    st = lib().rp_window_load_routes(C.byref(out), C.byref(cfg), _ptr(lengths), routes.data_ptr(), size, T, ts, ls, _stream_handle(stream))
+    _check(st, "rp_window_load_routes")
+    ctx = Context(out.value, cfg, (lengths, al, be, edp))
     ctx.n_shards = dp_width if edp is None else int(edp.max()) + 1
     return ctx
 
@@ -279,6 +305,91 @@ def rp_destroy(ctx: Context):
 
 def rp_release_cached_memory():
     _check(lib().rp_release_cached_memory(), "rp_release_cached_memory")
+
+
+# ---- operators on the tokens of a window ------------------------------------------------
+# Arrays are CUDA tensors of one GPU; calls queue on ``stream`` (default: torch's current stream of that GPU) and return.
+# Outputs that the caller does not pass are allocated on that stream.
+_TYPES = {}
+
+
+def _torch():
+    import torch
+    if not _TYPES:
+        _TYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    return torch
+
+
+class _Queue:
+    """Stream of a call: its handle, and as a context the stream that new tensors belong to."""
+    __slots__ = ("handle", "scope")
+
+    def __init__(self, torch, tensor, stream):
+        self.scope = None
+        if stream is None:
+            self.handle = torch.cuda.current_stream(tensor.device).cuda_stream
+            return
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=tensor.device)
+        self.handle = stream.cuda_stream
+        self.scope = torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.scope is not None:
+            self.scope.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dense(t, dtype, shape, what: str):
+    """Address of a contiguous CUDA tensor of a type and shape; None stays NULL."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: contiguous CUDA tensor {tuple(shape)} of {dtype} wanted, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _starts(torch, start):
+    """(address, number of samples) of a tensor of starts."""
+    if start.dim() != 1 or start.shape[0] < 2:
+        raise ValueError("start: [n + 1] wanted")
+    return _dense(start, torch.int64, start.shape, "start"), start.shape[0] - 1
+
+
+_ROUTE_TYPES = ("torch.uint8", "torch.int16", "torch.int32", "torch.int64")
+
+
+def _route_layout(routes):
+    """(bytes of a route, strides of all dimensions but the last) of recorded routes."""
+    if str(routes.dtype) not in _ROUTE_TYPES or not routes.is_cuda:
+        raise ValueError(f"routes: a CUDA tensor of uint8, int16, int32 or int64 wanted, got {routes.dtype} on {routes.device}")
+    if routes.shape[-1] != 1 and routes.stride(-1) != 1:
+        raise ValueError("routes: a token's choices have to lie side by side")
+    return (routes.element_size(), *routes.stride()[:-1])
+
+
+def rp_count_routes(routes, start, n_experts: int, demand=None, stream=None):
+    """Per-expert counts [n_samples, n_layers, n_experts] int32 of recorded routes [n_tokens, n_layers, top_k]."""
+    torch = _torch()
+    _need(routes.dim() == 3, "routes: [n_tokens, n_layers, top_k] wanted")
+    T, L, k = routes.shape
+    size, ts, ls = _route_layout(routes)
+    at, n = _starts(torch, start)
+    with _Queue(torch, routes, stream) as queue:
+        if demand is None:
+            demand = torch.empty((n, L, n_experts), dtype=torch.int32, device=routes.device)
+        _check(lib().rp_count_routes(routes.data_ptr() or at, size, T, L, k, n_experts, ts, ls, at, n,
+                                     _dense(demand, torch.int32, (n, L, n_experts), "demand"), queue.handle), "rp_count_routes")
+    return demand
 
 
 # ---- inspection hooks -------------------------------------------------------------------

@@ -7,6 +7,7 @@
 #include <new>
 
 #include "rp_common.cuh"
+#include "rp_ops.cuh"
 
 thread_local int g_rp_last_cuda_error = 0;
 long long g_rp_launches = 0;      // kernels launched by this library in this process
@@ -219,7 +220,10 @@ static int reset_status(rp_ctx *c)
     return RP_OK;
 }
 
-static int window_load_impl(rp_ctx *c, const rp_config *cfg, const int32_t *lengths, const int32_t *demand)
+// A record of routes in place of the demand tensor (rp_window_load_routes); starts: where its samples begin, freed by the caller.
+struct RpRecord { const void *routes; int bytes; i64 tokens, token_stride, layer_stride; i64 *starts; };
+
+static int window_load_impl(rp_ctx *c, const rp_config *cfg, const int32_t *lengths, const int32_t *demand, RpRecord *rec)
 {
     RpDims &dm = c->dm;
     const int N = cfg->n_samples, L = cfg->n_layers, E = cfg->n_experts, D = cfg->dp_width, P = cfg->ep_width;
@@ -272,7 +276,13 @@ static int window_load_impl(rp_ctx *c, const rp_config *cfg, const int32_t *leng
             if (const cudaError_t e = cudaMemcpyAsync(c->own_t, lengths, sizeof(int) * N, cudaMemcpyHostToDevice, c->stream)) { st = rp_fail(e); break; }
             c->d_t = c->own_t;
         }
-        if (rp_is_device_ptr(demand)) c->d_a = demand;
+        if (rec) {
+            if ((st = dev_alloc(c, &c->own_a, n_a)) != RP_OK || (st = dev_alloc(c, &rec->starts, (size_t)N + 1)) != RP_OK) break;
+            if ((st = rp_launch_starts(c->d_t, N, rec->starts, c->stream)) != RP_OK) break;
+            if ((st = rp_launch_count(c->device, rec->routes, rec->bytes, rec->tokens, L, dm.k, E, rec->token_stride, rec->layer_stride,
+                                      rec->starts, N, c->own_a, c->stream)) != RP_OK) break;
+            c->d_a = c->own_a;
+        } else if (rp_is_device_ptr(demand)) c->d_a = demand;
         else {
             if ((st = dev_alloc(c, &c->own_a, n_a)) != RP_OK) break;
             if (const cudaError_t e = cudaMemcpyAsync(c->own_a, demand, sizeof(int) * n_a, cudaMemcpyHostToDevice, c->stream)) { st = rp_fail(e); break; }
@@ -366,12 +376,11 @@ static int window_load_impl(rp_ctx *c, const rp_config *cfg, const int32_t *leng
     return RP_OK;
 }
 
-extern "C" int rp_window_load(rp_ctx **out, const rp_config *cfg, const int32_t *lengths,
-                              const int32_t *demand, void *cuda_stream)
+static int window_load(rp_ctx **out, const rp_config *cfg, const int32_t *lengths, const int32_t *demand, RpRecord *rec, void *cuda_stream)
 {
     if (!out) return RP_ERR_ARG;
     *out = nullptr;
-    if (!cfg || !lengths || !demand) return RP_ERR_ARG;
+    if (!cfg || !lengths || !(demand || rec)) return RP_ERR_ARG;
     if (cfg->n_samples < 1 || cfg->n_layers < 1 || cfg->n_experts < 1 || cfg->top_k < 1 || cfg->token_cap < 1 ||
         cfg->dp_width < 1 || cfg->ep_width < 1 || cfg->pop_size < 1 || cfg->min_rows < 0)
         return RP_ERR_ARG;
@@ -382,6 +391,15 @@ extern "C" int rp_window_load(rp_ctx **out, const rp_config *cfg, const int32_t 
     if (cfg->ep_width > RP_MAX_EP || cfg->dp_width > 4096 || cfg->n_experts > 1024) return RP_ERR_RANGE;
     if (cfg->token_cap > (1 << 24) || cfg->n_samples > (1 << 20) || cfg->pop_size > (1 << 20)) return RP_ERR_RANGE;
     if ((long long)cfg->n_layers * cfg->ep_width > (1 << 20)) return RP_ERR_RANGE;
+
+    if (rec) {
+        RP_TRY(rp_count_args(rec->routes, rec->bytes, rec->tokens, cfg->n_layers, cfg->top_k, cfg->n_experts));
+        int device = -1;
+        RP_CUDA(cudaGetDevice(&device));
+        RpOpDevice dev;                                  // (only asked where the record is)
+        RP_TRY(dev.hold(rec->routes));
+        if (dev.device >= 0 && dev.device != device) return RP_ERR_ARG;
+    }
 
     rp_ctx *c = (rp_ctx *)calloc(1, sizeof(rp_ctx));
     if (!c) return RP_ERR_ARG;
@@ -399,11 +417,25 @@ extern "C" int rp_window_load(rp_ctx **out, const rp_config *cfg, const int32_t 
     if (g_stage_timing)
         for (int x = 0; x < RP_STAGE_EVENTS; ++x)
             if (cudaEventCreate(&c->ev_stage[x]) != cudaSuccess) { cudaGetLastError(); c->ev_stage[0] = nullptr; break; }
-    int st = window_load_impl(c, cfg, lengths, demand);
+    int st = window_load_impl(c, cfg, lengths, demand, rec);
+    if (rec) dev_free(c, rec->starts);
     if (st != RP_OK) { rp_destroy(c); return st; }
     c->stage = 1;
     *out = c;
     return RP_OK;
+}
+
+extern "C" int rp_window_load(rp_ctx **out, const rp_config *cfg, const int32_t *lengths,
+                              const int32_t *demand, void *cuda_stream)
+{
+    return window_load(out, cfg, lengths, demand, nullptr, cuda_stream);
+}
+
+extern "C" int rp_window_load_routes(rp_ctx **out, const rp_config *cfg, const int32_t *lengths, const void *routes, int32_t route_bytes,
+                                     int64_t n_tokens, int64_t token_stride, int64_t layer_stride, void *cuda_stream)
+{
+    RpRecord rec = { routes, route_bytes, n_tokens, token_stride, layer_stride, nullptr };
+    return window_load(out, cfg, lengths, nullptr, &rec, cuda_stream);
 }
 
 extern "C" int rp_place_experts(rp_ctx *c, int32_t *pi, int64_t *rank_load)
