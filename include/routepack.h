@@ -292,6 +292,42 @@ int rp_count_routes(const void *routes, int32_t route_bytes, int64_t n_tokens, i
 int rp_window_load_routes(rp_ctx **out, const rp_config *cfg, const int32_t *lengths, const void *routes, int32_t route_bytes,
                           int64_t n_tokens, int64_t token_stride, int64_t layer_stride, void *cuda_stream);
 
+typedef enum { RP_SCORE_SOFTMAX = 0, RP_SCORE_SIGMOID = 1 } rp_score;
+typedef struct {
+    int32_t n_experts;          /* E <= 1024                                                  */
+    int32_t top_k;              /* k <= min(E, 32)                                            */
+    int32_t type;               /* rp_type of the logits and their gradient                  */
+    int32_t score;              /* rp_score: s = softmax(x) over the experts, or sigmoid(x)  */
+    int32_t normalise;          /* 1: gates are divided by the sum of the token's k scores   */
+    float scale;                /* factor of the gates                                       */
+    float loss_coef;            /* factor of the balance loss                                */
+} rp_router;
+
+/* Router of one MoE layer with its balance loss.
+ *   logits [n_tokens][E], row_stride apart.  -inf takes an expert out (score 0).
+ *   replay = 0: the k experts with the largest logits are chosen, in falling order, ties to the lower index (NaN counts as largest); with
+ *     choice_bias [E] float (nullable) those with the largest s + bias.  routes is written.
+ *   replay = 1: routes is read, as a record of an earlier pass has it; values outside [0, E) are empty places (gate 0, not counted), and
+ *     an expert may be there twice.
+ *   routes [n_tokens] rows of k, route_stride apart, of route_bytes = 1 (unsigned), 2, 4 or 8.
+ *   gates [n_tokens][k] float: scale * s_j, or scale * s_j / sum_i s_i (0 where that sum is 0).
+ *   counts [n_groups][E] int32 (nullable): how often each group's tokens have each expert.
+ *   loss [1] float (nullable; needs counts): loss_coef / n_groups * sum_g E / (k T_g^2) * sum_e counts[g][e] * P[g][e], P[g][e] = sum over the
+ *     group's T_g tokens of s[t][e] / sum_e s[t][e].  Empty groups add nothing.
+ *   workspace: rp_route_workspace(r, n_groups) bytes, 16-byte aligned (nullable without loss); contents need not be set.
+ * Limits: n_tokens <= 2^26, n_tokens * k < 2^31, n_groups * E < 2^31. */
+int64_t rp_route_workspace(const rp_router *r, int32_t n_groups);
+int rp_route(const rp_router *r, const void *logits, int64_t row_stride, int64_t n_tokens, const float *choice_bias,
+             const int64_t *start, int32_t n_groups, int32_t replay, void *routes, int32_t route_bytes, int64_t route_stride,
+             float *gates, int32_t *counts, float *loss, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* Gradient for the logits of what rp_route computes: of the gates (gates_grad [n_tokens][k] float, nullable) and of the balance loss
+ * (loss_grad [1] float, nullable; counts as rp_route wrote them or as added up over several ranks, held fixed: a count has no gradient).
+ *   logits_grad [n_tokens][E] of r->type, grad_stride apart; may not overlap the logits. */
+int rp_route_grad(const rp_router *r, const void *logits, int64_t row_stride, int64_t n_tokens, const void *routes, int32_t route_bytes,
+                  int64_t route_stride, const float *gates_grad, const float *loss_grad, const int64_t *start, int32_t n_groups,
+                  const int32_t *counts, void *logits_grad, int64_t grad_stride, void *cuda_stream);
+
 /* Frees the context.  Its device memory goes back to a per-device cache inside the library
  * (so that the next window does not pay for allocation); rp_release_cached_memory() returns
  * that cache to the driver. */

@@ -8,6 +8,7 @@ library cannot be loaded, every call raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -27,7 +28,7 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_debug_set_trace", "rp_debug_set_knob", "rp_debug_set_stage_timing", "rp_debug_stage_times",
            "rp_debug_nl2", "rp_debug_exp2neg", "rp_debug_philox", "rp_debug_launch_count", "rp_debug_l2_read_rate",
            "rp_debug_chain_kernel", "rp_debug_chain_form",
-           "rp_count_routes", "rp_window_load_routes")
+           "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad")
 
 
 class RpError(RuntimeError):
@@ -56,6 +57,11 @@ class rp_anneal_stats(C.Structure):
                 ("improved", C.c_int64), ("ms_chains", C.c_double),
                 ("move_bytes", C.c_int64), ("gather_bytes", C.c_int64), ("staging_bytes", C.c_int64),
                 ("kernel_launches", C.c_int64)]
+
+
+class rp_router(C.Structure):
+    _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("type", C.c_int32), ("score", C.c_int32), ("normalise", C.c_int32),
+                ("scale", C.c_float), ("loss_coef", C.c_float)]
 
 
 class rp_diag(C.Structure):
@@ -107,6 +113,10 @@ def lib():
         V, I, Q = C.c_void_p, C.c_int32, C.c_int64
         L.rp_count_routes.argtypes = [V, I, Q, I, I, I, Q, Q, V, I, V, V]
         L.rp_window_load_routes.argtypes = [C.POINTER(C.c_void_p), C.POINTER(rp_config), V, V, I, Q, Q, Q, V]
+        L.rp_route_workspace.restype = Q
+        L.rp_route_workspace.argtypes = [C.POINTER(rp_router), I]
+        L.rp_route.argtypes = [C.POINTER(rp_router), V, Q, Q, V, V, I, I, V, I, Q, V, V, V, V, Q, V]
+        L.rp_route_grad.argtypes = [C.POINTER(rp_router), V, Q, Q, V, I, Q, V, V, V, I, V, V, Q, V]
         _lib = L
     return _lib
 
@@ -390,6 +400,91 @@ def rp_count_routes(routes, start, n_experts: int, demand=None, stream=None):
         _check(lib().rp_count_routes(routes.data_ptr() or at, size, T, L, k, n_experts, ts, ls, at, n,
                                      _dense(demand, torch.int32, (n, L, n_experts), "demand"), queue.handle), "rp_count_routes")
     return demand
+
+
+SCORES = dict(softmax=0, sigmoid=1)
+
+
+@functools.lru_cache(maxsize=256)
+def _router(n_experts, top_k, kind, score, normalise, scale, loss_coef):
+    r = rp_router(n_experts, top_k, kind, SCORES[score], int(normalise), scale, loss_coef)
+    return r, C.byref(r)
+
+
+def _rows(x, what: str):
+    """Stride of the rows of a matrix."""
+    if x.dim() != 2 or not x.is_cuda or (x.shape[1] != 1 and x.stride(1) != 1):
+        raise ValueError(f"{what}: a CUDA tensor [n_tokens, n] with its last dimension side by side wanted")
+    return x.stride(0)
+
+
+def _kind(x, what: str):
+    kind = _TYPES.get(x.dtype)
+    if kind is None:
+        raise ValueError(f"{what}: float32, float16 or bfloat16 wanted, got {x.dtype}")
+    return kind
+
+
+def rp_route(logits, top_k: int, start, *, score: str = "softmax", normalise: bool = True, scale: float = 1.0, loss_coef: float = 0.0,
+             choice_bias=None, replay=None, routes=None, gates=None, counts=None, loss=None, stream=None):
+    """Router of one layer: (routes [T, k], gates [T, k] float32, counts [n_groups, E] int32, loss [1] float32).
+
+    ``replay``: routes of an earlier pass to be taken in place of the largest logits (returned as they are).  ``routes``: where the chosen
+    ones go (any integer type, rows with a stride: a slice of a record); int32 by default.
+    """
+    torch = _torch()
+    row = _rows(logits, "logits")
+    T, E = logits.shape
+    at, n = _starts(torch, start)
+    r, ref = _router(E, top_k, _kind(logits, "logits"), score, normalise, scale, loss_coef)
+    dev = logits.device
+    with _Queue(torch, logits, stream) as queue:
+        if replay is not None:
+            routes = replay
+        elif routes is None:
+            routes = torch.empty((T, top_k), dtype=torch.int32, device=dev)
+        if routes.shape != (T, top_k):
+            raise ValueError(f"routes: {(T, top_k)} wanted, got {tuple(routes.shape)}")
+        size, step = _route_layout(routes)
+        if gates is None:
+            gates = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+        if counts is None:
+            counts = torch.empty((n, E), dtype=torch.int32, device=dev)
+        if loss is None:
+            loss = torch.empty(1, dtype=torch.float32, device=dev)
+        nbytes = lib().rp_route_workspace(ref, n)
+        space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        # (an empty tensor has no address: any will do)
+        _check(lib().rp_route(ref, logits.data_ptr() or at, row, T, _dense(choice_bias, torch.float32, (E,), "choice_bias"), at, n,
+                              int(replay is not None), routes.data_ptr() or at, size, step,
+                              _dense(gates, torch.float32, (T, top_k), "gates") or at, _dense(counts, torch.int32, (n, E), "counts"),
+                              _dense(loss, torch.float32, (1,), "loss"), space.data_ptr(), nbytes, queue.handle), "rp_route")
+    return routes, gates, counts, loss
+
+
+def rp_route_grad(logits, routes, start, counts, *, gates_grad=None, loss_grad=None, score: str = "softmax", normalise: bool = True,
+                  scale: float = 1.0, loss_coef: float = 0.0, logits_grad=None, stream=None):
+    """Gradient for the logits of the gates (``gates_grad`` [T, k] float32) and the balance loss (``loss_grad`` [1] float32) of rp_route."""
+    torch = _torch()
+    row = _rows(logits, "logits")
+    T, E = logits.shape
+    if routes.dim() != 2 or routes.shape[0] != T:
+        raise ValueError("routes: [n_tokens, top_k] wanted")
+    k = routes.shape[1]
+    size, step = _route_layout(routes)
+    at, n = _starts(torch, start)
+    r, ref = _router(E, k, _kind(logits, "logits"), score, normalise, scale, loss_coef)
+    with _Queue(torch, logits, stream) as queue:
+        if logits_grad is None:
+            logits_grad = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+        if logits_grad.shape != logits.shape or logits_grad.dtype != logits.dtype:
+            raise ValueError("logits_grad: shape and type of the logits wanted")
+        if T:
+            _check(lib().rp_route_grad(ref, logits.data_ptr(), row, T, routes.data_ptr(), size, step,
+                                       _dense(gates_grad, torch.float32, (T, k), "gates_grad"), _dense(loss_grad, torch.float32, (1,), "loss_grad"),
+                                       at, n, _dense(counts, torch.int32, (n, E), "counts"), logits_grad.data_ptr(),
+                                       _rows(logits_grad, "logits_grad"), queue.handle), "rp_route_grad")
+    return logits_grad
 
 
 # ---- inspection hooks -------------------------------------------------------------------

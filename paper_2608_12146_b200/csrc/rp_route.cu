@@ -1,0 +1,570 @@
+// Router of one MoE layer with its balance loss, and its gradient.
+//
+//   s = softmax(x) or sigmoid(x) over the E experts, p = s / sum s
+//   gates: scale * s at the k chosen or replayed experts (over their sum)
+//   loss = coef / G * sum_g E / (k T_g^2) * sum_e counts[g][e] * sum_{t in g} p[t][e]
+//
+// One pass over the logits each way: T * E elements read (and written by the gradient), T * k routes and gates beside them.
+// A token belongs to SUB neighbouring lanes of a warp, VPL experts to a lane, so that its row is read with one or two 16-byte loads a lane and all
+// sums over experts are shuffles.  Every such group of lanes owns a run of neighbouring tokens and carries the sums of p of the run's
+// present group of tokens in registers, its counts in shared memory; what a CTA's last runs hold meets in shared memory before it goes out.
+// Sums of p leave a CTA in fixed point (2^-36): additions of whole numbers, so their order does not matter.
+#include <algorithm>
+
+#include "rp_ops.cuh"
+
+#define ROUTE_WARPS 8
+#define ROUTE_THREADS (32 * ROUTE_WARPS)
+#define ROUTE_MAX_K 32
+#define ROUTE_FIX 68719476736.0f            // 2^36: up to 2^26 tokens of p <= 1 add up to less than 2^63
+#define ROUTE_LOSS_CTAS 128
+
+struct RouteSpace {                         // workspace of rp_route; sums [G][E] behind it
+    u32 ticket, loss_ticket, odd, pad;      // odd: some p was not a number
+    double part[ROUTE_LOSS_CTAS];
+};
+
+struct RouteArgs {
+    const void *x;
+    i64 row, T, run;                        // run: tokens of a group of lanes
+    int E, k, score, normalise, replay, G;
+    float scale, coef;
+    const float *bias;
+    const i64 *start;
+    void *routes;
+    int route_bytes;
+    i64 route_row;
+    float *gates;
+    int *counts;
+    u64 *sums;
+    RouteSpace *space;
+    float *loss;
+    int wide;                               // rows can be read 16 bytes at a time
+    int finish;                             // 0: one CTA does it all, 1: the last CTA works out the loss, 2: another launch does
+    // gradient
+    const float *gates_grad, *loss_grad;
+    const int *counts_in;
+    void *dx;
+    i64 dx_row;
+};
+
+template <int SUB> __device__ __forceinline__ float sub_sum(float v)
+{
+#pragma unroll
+    for (int o = 1; o < SUB; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <int SUB> __device__ __forceinline__ float sub_max(float v)      // of numbers; NaN loses against any
+{
+#pragma unroll
+    for (int o = 1; o < SUB; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+template <int SUB> __device__ __forceinline__ u32 sub_max(u32 v)
+{
+    if constexpr (SUB == 32) v = __reduce_max_sync(0xffffffffu, v);
+    else {
+#pragma unroll
+        for (int o = 1; o < SUB; o <<= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+    }
+    return v;
+}
+
+// A row's VPL elements of a lane; experts from E on do not exist.
+template <typename X, int VPL>
+__device__ __forceinline__ void load_row(const RouteArgs &A, i64 t, int e0, float *x)
+{
+    const X *row = (const X *)A.x + t * A.row;
+    if (A.wide) {
+#pragma unroll
+        for (int c = 0; c < VPL; c += 8)
+            if (e0 + c < A.E) rp_open8(rp_load8(row + e0 + c), x + c);
+    } else {
+#pragma unroll
+        for (int c = 0; c < VPL; ++c)
+            if (e0 + c < A.E) x[c] = rp_float(row[e0 + c]);
+    }
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return __frcp_rn(1.0f + rp_exp2(-x * RP_LOG2E)); }
+
+// Scores of one token from its logits: softmax: e^(x - max) and 1 / their sum; sigmoid: s, and 1 / their sum.
+// `top` is what the largest logit is taken for: 0 where it is -inf (all scores are 0 then, and so is the inverse).
+template <int VPL, int SUB>
+__device__ __forceinline__ void scores(const RouteArgs &A, const float *x, int e0, float *s, float &top, float &inv)
+{
+    float sum = 0.0f;
+    if (A.score == RP_SCORE_SOFTMAX) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            if (e0 + i < A.E) m = fmaxf(m, x[i]);
+        m = sub_max<SUB>(m);
+        top = m == -INFINITY ? 0.0f : m;
+        const float shift = -top * RP_LOG2E;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            s[i] = e0 + i < A.E ? rp_exp2(fmaf(x[i], RP_LOG2E, shift)) : 0.0f;
+            sum += s[i];
+        }
+    } else {
+        top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            s[i] = e0 + i < A.E ? sigmoid(x[i]) : 0.0f;
+            sum += s[i];
+        }
+    }
+    sum = sub_sum<SUB>(sum);
+    inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+}
+// Score of one expert as the gates use it.
+__device__ __forceinline__ float score_of(const RouteArgs &A, float x, float top, float inv)
+{
+    return A.score == RP_SCORE_SOFTMAX ? rp_exp2(fmaf(x, RP_LOG2E, -top * RP_LOG2E)) * inv : sigmoid(x);
+}
+
+// Floats as unsigned numbers in the same order; -0 as 0, NaN above all.
+__device__ __forceinline__ u32 order_of(float x)
+{
+    const u32 b = __float_as_uint(x + 0.0f);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+    return (b >> 31) ? ~b : b | 0x80000000u;
+}
+
+// One group's part of the loss, by one warp.
+__device__ double group_loss(const RouteArgs &A, int g, int lane)
+{
+    i64 lo = A.start[g], hi = A.start[g + 1];
+    lo = lo < 0 ? 0 : lo; hi = hi > A.T ? A.T : hi;
+    if (hi <= lo) return 0.0;
+    double sum = 0.0;
+    for (int e = lane; e < A.E; e += 32)
+        sum += (double)__ldcg(A.counts + (i64)g * A.E + e) * ((double)__ldcg(A.sums + (i64)g * A.E + e) * (1.0 / 68719476736.0));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const double n = (double)(hi - lo);
+    return sum * ((double)A.coef / A.G * A.E / A.k / (n * n));
+}
+// The groups first, first + step, ... of each warp, added up in a fixed order by all threads of a CTA.
+__device__ double groups_loss(const RouteArgs &A, int first, int step, double *part)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    double sum = 0.0;
+    for (i64 g = first + warp; g < A.G; g += step) sum += group_loss(A, (int)g, lane);
+    if (lane == 0) part[warp] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < ROUTE_WARPS; ++w) sum += part[w];
+    return sum;
+}
+
+template <int VPL>
+__device__ __forceinline__ void add_sums(const RouteArgs &A, int g, int e0, const float *acc)
+{
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        if (e0 + i >= A.E) continue;
+        if (!(acc[i] >= 0.0f && acc[i] < 1.0e8f)) { odd = true; continue; }
+        const u64 v = __float2ull_rn(acc[i] * ROUTE_FIX);
+        if (v) atomicAdd(&A.sums[(i64)g * A.E + e0 + i], v);
+    }
+    if (odd) atomicExch(&A.space->odd, 1u);
+}
+
+template <typename X, int VPL, int SUB>
+__global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
+{
+    constexpr int NSUB = ROUTE_THREADS / SUB, EP = VPL * SUB;             // groups of lanes, experts they hold
+    __shared__ int cnt[NSUB][EP];
+    __shared__ u32 pick[NSUB][ROUTE_MAX_K];                               // chosen experts of the present token
+    __shared__ int last[NSUB];                                           // group of tokens that a run ends in
+    __shared__ double part[ROUTE_WARPS];
+    __shared__ u32 turn;
+    const int sub = threadIdx.x / SUB, sl = threadIdx.x % SUB, e0 = sl * VPL;
+    const int first_lane = threadIdx.x & 31 & ~(SUB - 1);
+    const bool want_loss = A.loss != nullptr, want_counts = A.counts != nullptr;
+    if (A.finish == 0 && want_counts) {
+        // the only CTA: nobody has cleared its sums
+        for (i64 x = threadIdx.x; x < (i64)A.G * A.E; x += ROUTE_THREADS) { A.counts[x] = 0; if (want_loss) A.sums[x] = 0; }
+        if (want_loss && threadIdx.x == 0) A.space->odd = 0;
+        __threadfence();
+    }
+    for (int x = threadIdx.x; x < NSUB * EP; x += ROUTE_THREADS) (&cnt[0][0])[x] = 0;
+    __syncthreads();
+
+    const i64 t0 = ((i64)blockIdx.x * NSUB + sub) * A.run;
+    int g = rp_sample_of(A.start, A.G, t0);
+    i64 next = g < A.G ? A.start[g + 1] : INT64_MAX;                      // where the next group begins
+    float acc[VPL], x[VPL], s[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) acc[i] = 0.0f;
+    for (i64 step = 0; step < A.run; ++step) {
+        const i64 t = t0 + step;
+        const bool there = t < A.T;
+        if (there && t >= next) {
+            // another group: what the run has of the one before goes out
+            if (g >= 0 && g < A.G) {
+                if (want_loss) add_sums<VPL>(A, g, e0, acc);
+                if (want_counts)
+                    for (int i = 0; i < VPL; ++i) {
+                        const int c = cnt[sub][e0 + i];
+                        if (c) { atomicAdd(&A.counts[(i64)g * A.E + e0 + i], c); cnt[sub][e0 + i] = 0; }
+                    }
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) acc[i] = 0.0f;
+            }
+            g = rp_sample_of(A.start, A.G, t);
+            next = g < A.G ? A.start[g + 1] : INT64_MAX;
+        }
+        const bool held = there && g >= 0 && g < A.G;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
+        if (held) load_row<X, VPL>(A, t, e0, x);
+        float top, inv;
+        scores<VPL, SUB>(A, x, e0, s, top, inv);
+        if (want_loss && held) {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) acc[i] = fmaf(s[i], inv, acc[i]);
+        }
+        if (!A.replay) {
+            // The k largest, one after the other.  16-bit logits leave their last 13 bits as floats free for the expert; others need a second look
+            // for the lowest expert that has the number.
+            u32 key[VPL];
+            if (sizeof(X) == 2 && !A.bias) {
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) key[i] = e0 + i < A.E ? (order_of(x[i]) & ~0x1fffu) | (u32)(1023 - e0 - i) | 0x400u : 0u;
+                for (int j = 0; j < A.k; ++j) {
+                    u32 best = 0;
+#pragma unroll
+                    for (int i = 0; i < VPL; ++i) best = max(best, key[i]);
+                    best = sub_max<SUB>(best);
+#pragma unroll
+                    for (int i = 0; i < VPL; ++i) key[i] = key[i] == best ? 0u : key[i];
+                    if (sl == 0) pick[sub][j] = 1023u - (best & 0x3ffu);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) {
+                    const float v = !A.bias ? x[i] : (A.score == RP_SCORE_SOFTMAX ? s[i] * inv : s[i]) + (e0 + i < A.E ? A.bias[e0 + i] : 0.0f);
+                    key[i] = e0 + i < A.E ? max(order_of(v), 1u) : 0u;
+                }
+                for (int j = 0; j < A.k; ++j) {
+                    u32 mine = 0;
+#pragma unroll
+                    for (int i = 0; i < VPL; ++i) mine = max(mine, key[i]);
+                    const u32 best = sub_max<SUB>(mine);
+                    u32 who = __ballot_sync(0xffffffffu, mine == best) >> first_lane;
+                    if (SUB < 32) who &= (1u << (SUB & 31)) - 1u;
+                    if (sl == __ffs((int)who) - 1) {
+                        bool gone = false;
+#pragma unroll
+                        for (int i = 0; i < VPL; ++i)
+                            if (!gone && key[i] == best) { gone = true; key[i] = 0; pick[sub][j] = (u32)(e0 + i); }
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        float total = 0.0f;
+        for (int j = sl; j < A.k; j += SUB) {
+            i64 e = -1;
+            if (held) e = A.replay ? rp_load_route(A.routes, A.route_bytes, t * A.route_row + j) : (i64)pick[sub][j];
+            const bool valid = e >= 0 && e < A.E;
+            float v = 0.0f;
+            if (valid) {
+                v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv);
+                if (want_counts) atomicAdd(&cnt[sub][(int)e], 1);
+            }
+            total += v;
+        }
+        if (A.normalise) {
+            total = sub_sum<SUB>(total);
+            total = total == 0.0f ? 0.0f : 1.0f / total;
+        } else
+            total = 1.0f;
+        for (int j = sl; j < A.k; j += SUB) {
+            i64 e = -1;
+            if (held) e = A.replay ? rp_load_route(A.routes, A.route_bytes, t * A.route_row + j) : (i64)pick[sub][j];
+            const bool valid = e >= 0 && e < A.E;
+            float v = 0.0f;
+            if (valid) v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv) * total * A.scale;
+            if (there) {
+                A.gates[t * A.k + j] = v;
+                if (!A.replay) rp_store_route(A.routes, A.route_bytes, t * A.route_row + j, (int)e);
+            }
+        }
+        __syncwarp();
+    }
+    // Runs that end in the same group meet here: their counts, then in the same place their sums of p.
+    if (!want_counts) return;
+    if (sl == 0) last[sub] = g >= 0 && g < A.G ? g : -1;
+    __syncthreads();
+    for (int e = threadIdx.x; e < A.E; e += ROUTE_THREADS)
+        for (int u = 0; u < NSUB;) {
+            const int gu = last[u];
+            int c = 0;
+            for (; u < NSUB && last[u] == gu; ++u) c += cnt[u][e];
+            if (gu >= 0 && c) atomicAdd(&A.counts[(i64)gu * A.E + e], c);
+        }
+    if (!want_loss) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) cnt[sub][e0 + i] = __float_as_int(acc[i]);
+    __syncthreads();
+    for (int e = threadIdx.x; e < A.E; e += ROUTE_THREADS)
+        for (int u = 0; u < NSUB;) {
+            const int gu = last[u];
+            float f = 0.0f;
+            for (; u < NSUB && last[u] == gu; ++u) f += __int_as_float(cnt[u][e]);
+            if (gu >= 0) add_sums<1>(A, gu, e, &f);
+        }
+    if (A.finish == 2) return;
+    __threadfence();
+    __syncthreads();
+    if (A.finish == 1) {
+        if (threadIdx.x == 0) turn = atomicAdd(&A.space->ticket, 1u);
+        __syncthreads();
+        if (turn != gridDim.x - 1) return;
+        __threadfence();
+    }
+    const double loss = groups_loss(A, 0, ROUTE_WARPS, part);
+    if (threadIdx.x == 0) *A.loss = __ldcg(&A.space->odd) ? NAN : (float)loss;
+}
+
+// The loss where there are many groups: CTAs add up groups of their own, the last one adds up the CTAs.
+__global__ void __launch_bounds__(ROUTE_THREADS) k_route_loss(RouteArgs A)
+{
+    __shared__ double part[ROUTE_WARPS];
+    const double mine = groups_loss(A, blockIdx.x * ROUTE_WARPS, gridDim.x * ROUTE_WARPS, part);
+    if (threadIdx.x) return;
+    A.space->part[blockIdx.x] = mine;
+    __threadfence();
+    if (atomicAdd(&A.space->loss_ticket, 1u) != gridDim.x - 1) return;
+    __threadfence();
+    double sum = 0.0;
+    for (int b = 0; b < (int)gridDim.x; ++b) sum += __ldcg(&A.space->part[b]);
+    *A.loss = __ldcg(&A.space->odd) ? NAN : (float)sum;
+}
+
+// Gradient for the logits.  With b[e] = loss_grad * coef / G * E * counts[g][e] / (k T_g^2), a_j = scale * gates_grad_j and y_j = s_j / sum of the chosen:
+//   softmax: dx = p (b - sum p b) + at the chosen: y_j (a_j - sum y a), or, not normalised, p (b - sum p b - sum_j p_j a_j) + p_j a_j
+//   sigmoid: ds = (b - sum p b) / sum s + at the chosen: (a_j - sum y a) / sum of the chosen, or a_j;  dx = s (1 - s) ds
+// The token's row is put together in shared memory, where the parts of its chosen experts are added one after the other.
+template <typename X, int VPL, int SUB>
+__global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
+{
+    constexpr int NSUB = ROUTE_THREADS / SUB, EP = VPL * SUB;
+    __shared__ __align__(16) float rows[NSUB][EP];
+    __shared__ int pick[NSUB][ROUTE_MAX_K];
+    __shared__ float add[NSUB][ROUTE_MAX_K];
+    const int sub = threadIdx.x / SUB, sl = threadIdx.x % SUB, e0 = sl * VPL;
+    const bool soft = A.score == RP_SCORE_SOFTMAX;
+    const float loss_grad = A.loss_grad ? *A.loss_grad : 0.0f;
+    const i64 t0 = ((i64)blockIdx.x * NSUB + sub) * A.run;
+    int g = -2;
+    i64 next = INT64_MIN;
+    float b[VPL], x[VPL], s[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) b[i] = 0.0f;
+    for (i64 step = 0; step < A.run; ++step) {
+        const i64 t = t0 + step;
+        const bool there = t < A.T;
+        if (there && t >= next) {
+            g = rp_sample_of(A.start, A.G, t);
+            next = g < A.G ? A.start[g + 1] : INT64_MAX;
+            if (A.loss_grad && g >= 0 && g < A.G) {
+                const i64 lo = max(A.start[g], (i64)0), hi = min(A.start[g + 1], A.T);
+                const float n = (float)(hi - lo), f = loss_grad * (A.coef / A.G) * A.E / A.k / n / n;
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) b[i] = e0 + i < A.E ? f * (float)A.counts_in[(i64)g * A.E + e0 + i] : 0.0f;
+            }
+        }
+        const bool held = there && g >= 0 && g < A.G;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
+        if (held) load_row<X, VPL>(A, t, e0, x);
+        float top, inv;
+        scores<VPL, SUB>(A, x, e0, s, top, inv);
+        float pb = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) pb = fmaf(s[i], b[i], pb);
+        pb = sub_sum<SUB>(pb) * inv;
+        if (A.gates_grad) {
+            float z = 0.0f, za = 0.0f;
+            for (int j = sl; j < A.k; j += SUB) {
+                i64 e = -1;
+                float a = 0.0f, v = 0.0f;
+                if (held) { e = rp_load_route(A.routes, A.route_bytes, t * A.route_row + j); a = A.scale * A.gates_grad[t * A.k + j]; }
+                const bool valid = e >= 0 && e < A.E;
+                if (valid) v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv);
+                pick[sub][j] = valid ? (int)e : -1;
+                z += v;
+                za += valid ? v * a : 0.0f;
+            }
+            z = sub_sum<SUB>(z);
+            za = sub_sum<SUB>(za);
+            const float zi = z == 0.0f ? 0.0f : 1.0f / z;
+            for (int j = sl; j < A.k; j += SUB) {
+                const int e = pick[sub][j];
+                if (e < 0) continue;
+                const float a = A.scale * A.gates_grad[t * A.k + j];
+                const float v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv);
+                const float ds = A.normalise ? (a - za * zi) * zi : a;
+                add[sub][j] = ds * (soft ? v : v * (1.0f - v));
+            }
+            if (soft && !A.normalise) pb += za;
+        }
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            const float p = s[i] * inv;
+            rows[sub][e0 + i] = (b[i] - pb) * (soft ? p : p * (1.0f - s[i]));
+        }
+        __syncwarp();
+        if (A.gates_grad && sl == 0 && held)
+            for (int j = 0; j < A.k; ++j)
+                if (pick[sub][j] >= 0) rows[sub][pick[sub][j]] += add[sub][j];
+        __syncwarp();
+        if (there) {
+            X *out = (X *)A.dx + t * A.dx_row;
+            if (A.wide) {
+#pragma unroll
+                for (int c = 0; c < VPL; c += 8)
+                    if (e0 + c < A.E) {
+                        float f[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = held ? rows[sub][e0 + c + i] : 0.0f;
+                        rp_store8(out + e0 + c, rp_close8<X>(f));
+                    }
+            } else
+                for (int i = 0; i < VPL; ++i)
+                    if (e0 + i < A.E) out[e0 + i] = rp_round<X>(held ? rows[sub][e0 + i] : 0.0f);
+        }
+        __syncwarp();
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------------------
+// A lane holds 8 experts (more where a row of E needs more than a warp), so SUB lanes a token.
+template <typename X, int VPL, int SUB>
+static int launch(RouteArgs &A, bool grad, int sms, cudaStream_t stream)
+{
+    constexpr int NSUB = ROUTE_THREADS / SUB;
+    if (grad) {
+        const i64 subs = std::min((A.T + 1) / 2, (i64)sms * 4 * NSUB);
+        A.run = (A.T + subs - 1) / subs;
+        k_route_grad<X, VPL, SUB><<<(unsigned)((A.T + A.run * NSUB - 1) / (A.run * NSUB)), ROUTE_THREADS, 0, stream>>>(A);
+        return rp_op_launched();
+    }
+    const i64 cells = (i64)A.G * A.E;
+    if (A.T <= (i64)NSUB * 4 && cells <= 4096) {         // up to four tokens a group of lanes: one CTA, one launch
+        A.finish = 0;
+        A.run = (A.T + NSUB - 1) / NSUB;
+    } else {
+        const i64 subs = std::min((A.T + 3) / 4, (i64)sms * 4 * NSUB);
+        A.finish = cells <= 16384 ? 1 : 2;
+        A.run = (A.T + subs - 1) / subs;
+        if (A.counts) RP_CUDA(cudaMemsetAsync(A.counts, 0, sizeof(int) * (size_t)cells, stream));
+        if (A.loss) RP_CUDA(cudaMemsetAsync(A.space, 0, sizeof(RouteSpace) + sizeof(u64) * (size_t)cells, stream));
+    }
+    k_route<X, VPL, SUB><<<(unsigned)((A.T + A.run * NSUB - 1) / (A.run * NSUB)), ROUTE_THREADS, 0, stream>>>(A);
+    RP_TRY(rp_op_launched());
+    if (A.loss && A.finish == 2) {
+        k_route_loss<<<std::min(ROUTE_LOSS_CTAS, (A.G + ROUTE_WARPS - 1) / ROUTE_WARPS), ROUTE_THREADS, 0, stream>>>(A);
+        RP_TRY(rp_op_launched());
+    }
+    return RP_OK;
+}
+template <typename X>
+static int launch_for(RouteArgs &A, bool grad, int sms, cudaStream_t stream)
+{
+    if (A.E <= 16) return launch<X, 8, 2>(A, grad, sms, stream);
+    if (A.E <= 32) return launch<X, 8, 4>(A, grad, sms, stream);
+    if (A.E <= 64) return launch<X, 8, 8>(A, grad, sms, stream);
+    if (A.E <= 128) return launch<X, 8, 16>(A, grad, sms, stream);
+    if (A.E <= 256) return launch<X, 8, 32>(A, grad, sms, stream);
+    if (A.E <= 512) return launch<X, 16, 32>(A, grad, sms, stream);
+    return launch<X, 32, 32>(A, grad, sms, stream);
+}
+
+static int check_router(const rp_router *r, const void *logits, i64 T, const void *start, int G, int route_bytes)
+{
+    if (!r || !logits || !start || T < 0 || G < 1) return RP_ERR_ARG;
+    if (r->n_experts < 1 || r->top_k < 1 || r->top_k > r->n_experts || r->type < RP_F32 || r->type > RP_BF16 ||
+        r->score < RP_SCORE_SOFTMAX || r->score > RP_SCORE_SIGMOID || r->normalise < 0 || r->normalise > 1)
+        return RP_ERR_ARG;
+    if (route_bytes != 1 && route_bytes != 2 && route_bytes != 4 && route_bytes != 8) return RP_ERR_ARG;
+    if (r->n_experts > 1024 || r->top_k > ROUTE_MAX_K || T > (1ll << 26) || T * r->top_k >= (1ll << 31) || (i64)G * r->n_experts >= (1ll << 31))
+        return RP_ERR_RANGE;
+    if (!rp_aligned(logits, rp_type_bytes(r->type)) || !rp_aligned(start, 8)) return RP_ERR_ARG;
+    return RP_OK;
+}
+static bool wide_rows(const void *p, i64 row, int E, int bytes) { return E % 8 == 0 && rp_aligned(p, 16) && row * bytes % 16 == 0; }
+
+extern "C" int64_t rp_route_workspace(const rp_router *r, int32_t n_groups)
+{
+    if (!r || r->n_experts < 1 || n_groups < 1) return 0;
+    return (int64_t)sizeof(RouteSpace) + (int64_t)sizeof(u64) * n_groups * r->n_experts;
+}
+
+static RouteArgs router_args(const rp_router *r, const void *logits, i64 row, i64 T, const int64_t *start, int G, const void *routes, int bytes, i64 route_row)
+{
+    RouteArgs A = {};
+    A.x = logits; A.row = row; A.T = T; A.E = r->n_experts; A.k = r->top_k; A.score = r->score; A.normalise = r->normalise;
+    A.G = G; A.scale = r->scale; A.coef = r->loss_coef; A.start = (const i64 *)start;
+    A.routes = (void *)routes; A.route_bytes = bytes; A.route_row = route_row;
+    A.wide = wide_rows(logits, row, r->n_experts, rp_type_bytes(r->type));
+    return A;
+}
+
+extern "C" int rp_route(const rp_router *r, const void *logits, int64_t row_stride, int64_t n_tokens, const float *choice_bias,
+                        const int64_t *start, int32_t n_groups, int32_t replay, void *routes, int32_t route_bytes, int64_t route_stride,
+                        float *gates, int32_t *counts, float *loss, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    RP_TRY(check_router(r, logits, n_tokens, start, n_groups, route_bytes));
+    if (!routes || !gates || (loss && (!counts || !workspace)) || replay < 0 || replay > 1) return RP_ERR_ARG;
+    if (loss && (workspace_bytes < rp_route_workspace(r, n_groups) || !rp_aligned(workspace, 16))) return RP_ERR_ARG;
+    if (!rp_aligned(routes, route_bytes) || !rp_aligned(gates, 4) || !rp_aligned(counts, 4) || !rp_aligned(loss, 4) || !rp_aligned(choice_bias, 4))
+        return RP_ERR_ARG;
+    if (!replay && route_stride < r->top_k && n_tokens > 1) return RP_ERR_ARG;         // rows would write over one another
+    if (!replay && route_bytes == 1 && r->n_experts > 256) return RP_ERR_RANGE;
+    RpOpDevice dev;
+    RP_TRY(rp_op_enter(dev, logits, choice_bias, start, routes, gates, counts, loss, workspace));
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    RouteArgs A = router_args(r, logits, row_stride, n_tokens, start, n_groups, routes, route_bytes, route_stride);
+    A.replay = replay; A.bias = choice_bias; A.gates = gates; A.counts = counts;
+    A.space = (RouteSpace *)workspace; A.sums = loss ? (u64 *)(A.space + 1) : nullptr; A.loss = loss;
+    if (n_tokens == 0) {
+        if (counts) RP_CUDA(cudaMemsetAsync(counts, 0, sizeof(int) * (size_t)n_groups * r->n_experts, stream));
+        if (loss) RP_CUDA(cudaMemsetAsync(loss, 0, sizeof(float), stream));
+        return RP_OK;
+    }
+    int st = RP_OK;
+    RP_FOR_TYPE(r->type, st = launch_for<X>(A, false, rp_op_sms(dev.device), stream));
+    return st;
+}
+
+extern "C" int rp_route_grad(const rp_router *r, const void *logits, int64_t row_stride, int64_t n_tokens, const void *routes, int32_t route_bytes,
+                             int64_t route_stride, const float *gates_grad, const float *loss_grad, const int64_t *start, int32_t n_groups,
+                             const int32_t *counts, void *logits_grad, int64_t grad_stride, void *cuda_stream)
+{
+    RP_TRY(check_router(r, logits, n_tokens, start, n_groups, route_bytes));
+    if (!logits_grad || (gates_grad && !routes) || (loss_grad && !counts) || logits_grad == logits) return RP_ERR_ARG;
+    if (!rp_aligned(routes, route_bytes) || !rp_aligned(gates_grad, 4) || !rp_aligned(loss_grad, 4) || !rp_aligned(counts, 4) ||
+        !rp_aligned(logits_grad, rp_type_bytes(r->type)))
+        return RP_ERR_ARG;
+    if (grad_stride < r->n_experts && n_tokens > 1) return RP_ERR_ARG;
+    RpOpDevice dev;
+    RP_TRY(rp_op_enter(dev, logits, routes, gates_grad, loss_grad, start, counts, logits_grad));
+    if (n_tokens == 0) return RP_OK;
+    RouteArgs A = router_args(r, logits, row_stride, n_tokens, start, n_groups, routes, route_bytes, route_stride);
+    A.gates_grad = gates_grad; A.loss_grad = loss_grad; A.counts_in = counts; A.dx = logits_grad; A.dx_row = grad_stride;
+    A.wide = A.wide && wide_rows(logits_grad, grad_stride, r->n_experts, rp_type_bytes(r->type));
+    int st = RP_OK;
+    RP_FOR_TYPE(r->type, st = launch_for<X>(A, true, rp_op_sms(dev.device), (cudaStream_t)cuda_stream));
+    return st;
+}
