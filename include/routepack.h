@@ -328,6 +328,42 @@ int rp_route_grad(const rp_router *r, const void *logits, int64_t row_stride, in
                   int64_t route_stride, const float *gates_grad, const float *loss_grad, const int64_t *start, int32_t n_groups,
                   const int32_t *counts, void *logits_grad, int64_t grad_stride, void *cuda_stream);
 
+/* Norm of each head and rotation by position, for queries and keys of packed rows in one launch.
+ *   position of token t of sample i = t - start[i] + first_position[i] (int64, nullable = 0): it starts again with every sample; decoding has one
+ *   token a sample, and its place in the context as first_position.
+ *   y = x * rsqrt(mean(x^2) + eps) * weight over each head (weight NULL: y = x); then for the pairs p < rotary_dim / 2 of the head's
+ *   first rotary_dim elements, with angle a = position * inv_freq[p]:  (y1, y2) -> mscale * (y1 cos a - y2 sin a, y1 sin a + y2 cos a).
+ *   RP_ROTARY_HALF pairs elements p and p + rotary_dim / 2, RP_ROTARY_INTERLEAVED 2p and 2p + 1.  Elements from rotary_dim on are not turned.
+ *   inv_freq [rotary_dim/2] double, radians per position, as scaled for a long context by the caller; angles are worked out in 64 bits.
+ *   Limits: head_dim <= 1024, rotary_dim even and <= head_dim (0: norm alone). */
+typedef enum { RP_ROTARY_HALF = 0, RP_ROTARY_INTERLEAVED = 1 } rp_rotary_layout;
+typedef struct {
+    int32_t head_dim, rotary_dim;
+    int32_t layout;             /* rp_rotary_layout                                          */
+    int32_t type;               /* rp_type of x, y and their gradients                       */
+    int32_t weight_type;        /* rp_type of the weights: RP_F32 or `type`                  */
+    float eps, mscale;
+} rp_rotary;
+typedef struct {                /* one tensor of heads; n_heads = 0: none                    */
+    int32_t n_heads;
+    const void *x;              /* [n_tokens][n_heads][head_dim]                             */
+    int64_t x_token, x_head;    /* strides                                                   */
+    void *y;                    /* output; may be x itself with the same strides             */
+    int64_t y_token, y_head;
+    const void *weight;         /* [head_dim], NULL: no norm                                 */
+    const void *y_grad;         /* rp_rotate_grad: gradient of the output                    */
+    int64_t g_token, g_head;
+    float *weight_grad;         /* rp_rotate_grad: [head_dim] out, nullable                  */
+} rp_heads;
+int rp_rotate(const rp_rotary *r, int64_t n_tokens, const double *inv_freq, const int64_t *start, int32_t n_samples,
+              const int64_t *first_position, const rp_heads *q, const rp_heads *k, void *cuda_stream);
+/* Gradient of rp_rotate: x as in the forward call (not read without weight), y_grad in, y receives the gradient of x (may be y_grad itself
+ * with the same strides).  workspace: rp_rotate_workspace(r) bytes, 16-byte aligned (nullable when no weight_grad is asked for). */
+int64_t rp_rotate_workspace(const rp_rotary *r);
+int rp_rotate_grad(const rp_rotary *r, int64_t n_tokens, const double *inv_freq, const int64_t *start, int32_t n_samples,
+                   const int64_t *first_position, const rp_heads *q, const rp_heads *k, void *workspace, int64_t workspace_bytes,
+                   void *cuda_stream);
+
 /* Frees the context.  Its device memory goes back to a per-device cache inside the library
  * (so that the next window does not pay for allocation); rp_release_cached_memory() returns
  * that cache to the driver. */

@@ -28,7 +28,8 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_debug_set_trace", "rp_debug_set_knob", "rp_debug_set_stage_timing", "rp_debug_stage_times",
            "rp_debug_nl2", "rp_debug_exp2neg", "rp_debug_philox", "rp_debug_launch_count", "rp_debug_l2_read_rate",
            "rp_debug_chain_kernel", "rp_debug_chain_form",
-           "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad")
+           "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad",
+           "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad")
 
 
 class RpError(RuntimeError):
@@ -62,6 +63,17 @@ class rp_anneal_stats(C.Structure):
 class rp_router(C.Structure):
     _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("type", C.c_int32), ("score", C.c_int32), ("normalise", C.c_int32),
                 ("scale", C.c_float), ("loss_coef", C.c_float)]
+
+
+class rp_rotary(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("type", C.c_int32), ("weight_type", C.c_int32),
+                ("eps", C.c_float), ("mscale", C.c_float)]
+
+
+class rp_heads(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("x", C.c_void_p), ("x_token", C.c_int64), ("x_head", C.c_int64),
+                ("y", C.c_void_p), ("y_token", C.c_int64), ("y_head", C.c_int64), ("weight", C.c_void_p),
+                ("y_grad", C.c_void_p), ("g_token", C.c_int64), ("g_head", C.c_int64), ("weight_grad", C.c_void_p)]
 
 
 class rp_diag(C.Structure):
@@ -117,6 +129,11 @@ def lib():
         L.rp_route_workspace.argtypes = [C.POINTER(rp_router), I]
         L.rp_route.argtypes = [C.POINTER(rp_router), V, Q, Q, V, V, I, I, V, I, Q, V, V, V, V, Q, V]
         L.rp_route_grad.argtypes = [C.POINTER(rp_router), V, Q, Q, V, I, Q, V, V, V, I, V, V, Q, V]
+        H = C.POINTER(rp_heads)
+        L.rp_rotate.argtypes = [C.POINTER(rp_rotary), Q, V, V, I, V, H, H, V]
+        L.rp_rotate_workspace.restype = Q
+        L.rp_rotate_workspace.argtypes = [C.POINTER(rp_rotary)]
+        L.rp_rotate_grad.argtypes = [C.POINTER(rp_rotary), Q, V, V, I, V, H, H, V, Q, V]
         _lib = L
     return _lib
 
@@ -485,6 +502,87 @@ def rp_route_grad(logits, routes, start, counts, *, gates_grad=None, loss_grad=N
                                        at, n, _dense(counts, torch.int32, (n, E), "counts"), logits_grad.data_ptr(),
                                        _rows(logits_grad, "logits_grad"), queue.handle), "rp_route_grad")
     return logits_grad
+
+
+LAYOUTS = dict(half=0, interleaved=1)
+
+
+@functools.lru_cache(maxsize=256)
+def _rotary(head_dim, rotary_dim, layout, kind, weight_kind, eps, mscale):
+    r = rp_rotary(head_dim, rotary_dim, LAYOUTS[layout], kind, weight_kind, eps, mscale)
+    return r, C.byref(r)
+
+
+def _head_strides(x, like, what: str):
+    """Strides of tokens and heads of a tensor of the shape and type of `like`."""
+    if x.shape != like.shape or x.dtype != like.dtype or not x.is_cuda or (x.shape[2] != 1 and x.stride(2) != 1):
+        raise ValueError(f"{what}: CUDA tensor {tuple(like.shape)} of {like.dtype} with its last dimension side by side wanted, "
+                         f"got {tuple(x.shape)} of {x.dtype}")
+    return x.stride(0), x.stride(1)
+
+
+def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale, outs, grads, stream):
+    torch = _torch()
+    _need(q.dim() == 3 and (k is None or (k.dim() == 3 and k.dtype == q.dtype and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2])),
+          "q and k: [n_tokens, n_heads, head_dim] of one type, as many tokens and one head size wanted")
+    T, _, d = q.shape
+    kind = _kind(q, "q")
+    at, n = _starts(torch, start)
+    w_type = next((w.dtype for w in weights if w is not None), q.dtype)
+    _need(w_type == q.dtype or w_type == torch.float32, "weights: float32 or the type of q wanted")
+    back = grads[0] is not None
+    with _Queue(torch, q, stream) as queue:
+        sides, results, dws = [None, None], [None, None], [None, None]
+        for i, (x, w, out, g) in enumerate(zip((q, k), weights, outs, grads)):
+            if x is None:
+                continue
+            if out is None:
+                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            results[i] = out
+            side = rp_heads(x.shape[1], x.data_ptr(), *_head_strides(x, x, "input"), out.data_ptr(), *_head_strides(out, x, "output"),
+                            _dense(w, w_type, (d,), "weight"))
+            if back:
+                side.y_grad = g.data_ptr()
+                side.g_token, side.g_head = _head_strides(g, x, "gradient")
+                if w is not None:
+                    dws[i] = torch.empty(d, dtype=torch.float32, device=x.device)
+                    side.weight_grad = dws[i].data_ptr()
+            sides[i] = C.byref(side)
+        freq = None if inv_freq is None else _dense(inv_freq, torch.float64, inv_freq.shape, "inv_freq")
+        r, ref = _rotary(d, 0 if inv_freq is None else 2 * inv_freq.numel(), layout, kind, _TYPES[w_type], eps, mscale)
+        args = (ref, T, freq, at, n, _dense(first_position, torch.int64, (n,), "first_position"), *sides)
+        if not T:
+            for dw in dws:
+                if dw is not None:
+                    dw.zero_()
+        elif not back:
+            _check(lib().rp_rotate(*args, queue.handle), "rp_rotate")
+        else:
+            space, nbytes = None, 0
+            if dws[0] is not None or dws[1] is not None:
+                nbytes = lib().rp_rotate_workspace(ref)
+                space = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+            _check(lib().rp_rotate_grad(*args, None if space is None else space.data_ptr(), nbytes, queue.handle), "rp_rotate_grad")
+    return results, dws
+
+
+def rp_rotate(q, k, inv_freq, start, *, first_position=None, q_weight=None, k_weight=None, eps: float = 1e-6, layout: str = "half",
+              mscale: float = 1.0, q_out=None, k_out=None, stream=None):
+    """Norm of each head (where there is a weight) and rotation by the position in the sample: (q, k) of [n_tokens, n_heads, head_dim].
+
+    ``inv_freq`` float64 [rotary_dim / 2] on the GPU, radians per position (None: no rotation); ``k`` may be None; outputs may be the inputs.
+    """
+    results, _ = _rotate(q, k, inv_freq, start, first_position, (q_weight, k_weight), eps, layout, mscale, (q_out, k_out), (None, None), stream)
+    return tuple(results)
+
+
+def rp_rotate_grad(q_out_grad, k_out_grad, q, k, inv_freq, start, *, first_position=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                   layout: str = "half", mscale: float = 1.0, q_grad=None, k_grad=None, stream=None):
+    """Gradients of rp_rotate: (q_grad, k_grad, q_weight_grad, k_weight_grad), the weights' in float32, None where there is no weight."""
+    _need(q_out_grad is not None and (k is None) == (k_out_grad is None), "a gradient for each of q and k wanted")
+    results, dws = _rotate(q, k, inv_freq, start, first_position, (q_weight, k_weight), eps, layout, mscale, (q_grad, k_grad),
+                           (q_out_grad, k_out_grad), stream)
+    return (*results, *dws)
 
 
 # ---- inspection hooks -------------------------------------------------------------------
