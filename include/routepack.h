@@ -364,6 +364,26 @@ int rp_rotate_grad(const rp_rotary *r, int64_t n_tokens, const double *inv_freq,
                    const int64_t *first_position, const rp_heads *q, const rp_heads *k, void *workspace, int64_t workspace_bytes,
                    void *cuda_stream);
 
+/* Attention of the tokens of a packed row inside their samples: token t sees the tokens s of its sample (causal: s <= t).
+ *   o[t][h] = sum_s softmax_s(scale * q[t][h] . k[s][h']) v[s][h'],  h' = h / (q_heads / kv_heads);  lse[t][h] = log sum_s exp(scale * q . k).
+ *   Weights are rounded to `type` before their product with v (the sums they are divided by are not); sums are held in 32 bits.
+ *   What tokens of other samples hold, infinities and NaN too, does not matter.
+ *   Strides and addresses of q, k, v, out and their gradients have to be multiples of 16 bytes, strides positive.
+ *   lse [n_tokens][q_heads] float, strides as given; nullable in rp_attend.
+ *   workspace: rp_attend_workspace(a, n_tokens, n_samples) bytes, 16-byte aligned.  Its first int32 is 0 when the kernels are done, or RP_ERR_TIMEOUT if one of their
+ *     waits (two seconds each) ran out: outputs that had not been worked out are NaN then.
+ * Limits: head_dim <= 128 and a multiple of 8, q_heads a multiple of kv_heads, type RP_F16 or RP_BF16, scale > 0, n_tokens < 2^31 - 512, n_samples <= 2^24. */
+typedef struct {
+    int32_t q_heads, kv_heads, head_dim;
+    int32_t type;               /* rp_type of all tensors but lse                            */
+    int32_t causal;
+    float scale;
+} rp_attend_config;
+typedef struct { void *x; int64_t token, head; } rp_view;      /* [n_tokens][heads][head_dim] (lse: [n_tokens][heads]) and its strides */
+int64_t rp_attend_workspace(const rp_attend_config *a, int64_t n_tokens, int32_t n_samples);
+int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const int64_t *start,
+              int32_t n_samples, const rp_view *out, const rp_view *lse, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
 /* Frees the context.  Its device memory goes back to a per-device cache inside the library
  * (so that the next window does not pay for allocation); rp_release_cached_memory() returns
  * that cache to the driver. */

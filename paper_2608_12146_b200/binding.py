@@ -29,7 +29,7 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_debug_nl2", "rp_debug_exp2neg", "rp_debug_philox", "rp_debug_launch_count", "rp_debug_l2_read_rate",
            "rp_debug_chain_kernel", "rp_debug_chain_form",
            "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad",
-           "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad")
+           "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad", "rp_attend_workspace", "rp_attend")
 
 
 class RpError(RuntimeError):
@@ -74,6 +74,15 @@ class rp_heads(C.Structure):
     _fields_ = [("n_heads", C.c_int32), ("x", C.c_void_p), ("x_token", C.c_int64), ("x_head", C.c_int64),
                 ("y", C.c_void_p), ("y_token", C.c_int64), ("y_head", C.c_int64), ("weight", C.c_void_p),
                 ("y_grad", C.c_void_p), ("g_token", C.c_int64), ("g_head", C.c_int64), ("weight_grad", C.c_void_p)]
+
+
+class rp_attend_config(C.Structure):
+    _fields_ = [("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("type", C.c_int32), ("causal", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class rp_view(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("token", C.c_int64), ("head", C.c_int64)]
 
 
 class rp_diag(C.Structure):
@@ -134,6 +143,10 @@ def lib():
         L.rp_rotate_workspace.restype = Q
         L.rp_rotate_workspace.argtypes = [C.POINTER(rp_rotary)]
         L.rp_rotate_grad.argtypes = [C.POINTER(rp_rotary), Q, V, V, I, V, H, H, V, Q, V]
+        W = C.POINTER(rp_view)
+        L.rp_attend_workspace.restype = Q
+        L.rp_attend_workspace.argtypes = [C.POINTER(rp_attend_config), Q, I]
+        L.rp_attend.argtypes = [C.POINTER(rp_attend_config), Q, W, W, W, V, I, W, W, V, Q, V]
         _lib = L
     return _lib
 
@@ -583,6 +596,51 @@ def rp_rotate_grad(q_out_grad, k_out_grad, q, k, inv_freq, start, *, first_posit
     results, dws = _rotate(q, k, inv_freq, start, first_position, (q_weight, k_weight), eps, layout, mscale, (q_grad, k_grad),
                            (q_out_grad, k_out_grad), stream)
     return (*results, *dws)
+
+
+@functools.lru_cache(maxsize=256)
+def _attention(q_heads, kv_heads, head_dim, kind, causal, scale):
+    a = rp_attend_config(q_heads, kv_heads, head_dim, kind, int(causal), head_dim ** -0.5 if scale is None else scale)
+    return a, C.byref(a)
+
+
+def _view(x, like, what: str):
+    token, head = _head_strides(x, like, what)
+    return C.byref(rp_view(x.data_ptr(), token, head))
+
+
+def _lse_view(x, T, H, torch):
+    if x.shape != (T, H) or x.dtype != torch.float32 or not x.is_cuda:
+        raise ValueError(f"lse: CUDA tensor {(T, H)} of float32 wanted, got {tuple(x.shape)} of {x.dtype}")
+    return C.byref(rp_view(x.data_ptr(), x.stride(0), x.stride(1)))
+
+
+def _attend_args(torch, q, k, v, start, causal, scale):
+    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.dtype == q.dtype and v.dtype == q.dtype and k.shape[0] == q.shape[0]
+          and k.shape[2] == q.shape[2], "q, k and v: [n_tokens, n_heads, head_dim] of one type, as many tokens and one head size wanted")
+    at, n = _starts(torch, start)
+    return _attention(q.shape[1], k.shape[1], q.shape[2], _kind(q, "q"), causal, scale)[1], at, n
+
+
+def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = None, out=None, lse=None, stream=None):
+    """Attention inside the samples of a packed row: (out [n_tokens, q_heads, head_dim], lse [n_tokens, q_heads] float32).
+
+    ``q`` [n_tokens, q_heads, head_dim], ``k`` and ``v`` [n_tokens, kv_heads, head_dim] of float16 or bfloat16; ``scale`` is head_dim ** -0.5 by default.
+    """
+    torch = _torch()
+    ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
+    T, H, _ = q.shape
+    with _Queue(torch, q, stream) as queue:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((H, T), dtype=torch.float32, device=q.device).t()      # a head's rows side by side: what the backward pass reads fastest
+        nbytes = lib().rp_attend_workspace(ref, T, n)
+        space = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+        if T:
+            _check(lib().rp_attend(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _view(out, q, "out"), _lse_view(lse, T, H, torch),
+                                   space.data_ptr(), nbytes, queue.handle), "rp_attend")
+    return out, lse
 
 
 # ---- inspection hooks -------------------------------------------------------------------

@@ -1,0 +1,418 @@
+// Attention inside the samples of a packed row, forward.
+//
+//   s = scale q k^T over the tokens of a sample, p = exp(s - m), o = p v / sum p, lse = m + log sum p, m a running maximum
+//
+// Bound by the tensor cores and the special function unit alike: a tile of 128 queries and 128 keys is 2 * 128 * 128 * head_dim multiply-adds (1024
+// cycles of an SM's tensor cores at head_dim 128) and 128 * 128 exponentials (1024 cycles of its special function units).
+// A CTA takes 256 queries of a head as two tiles of 128, each with four warps of its own for the softmax (a thread has a row, so a row's maximum and sum
+// need no exchange); while one tile's weights are worked out, the tensor cores work on the other's.  One warp copies keys and values into a ring of
+// shared memory, one issues the products.  Scores and outputs live in tensor memory (2 x 128 + 2 x head_dim columns), the weights take the
+// scores' place as the operand of the second product.  Outputs are scaled again only when a row's maximum has grown by more than 2^8.
+// CTAs stay resident and take blocks of queries in the order of falling work.
+#include <algorithm>
+
+#include "rp_attend.cuh"
+
+// ---------------------------------------------------------------------------------------
+// what is to be done
+// ---------------------------------------------------------------------------------------
+// CTA 0 lists the blocks of `rows` tokens of all samples, those with the most tiles of others first; the other CTAs clear the rows that no sample holds.
+#define PLAN_BUCKETS 1024
+__global__ void __launch_bounds__(1024) k_attend_plan(AttendPlan A)
+{
+    if (blockIdx.x) {
+        i64 head = A.start[0], tail = A.start[A.N];
+        head = min(max(head, (i64)0), A.T); tail = min(max(tail, head), A.T);
+        const i64 gone = head + A.T - tail;
+        for (int o = 0; o < A.n_clear; ++o) {
+            const AttendClear &C = A.clear[o];
+            const i64 width = (i64)C.heads * C.d;
+            for (i64 x = (i64)(blockIdx.x - 1) * 1024 + threadIdx.x; x < gone * width; x += (i64)(gridDim.x - 1) * 1024) {
+                i64 t = x / width;
+                const i64 h = x % width / C.d, i = x % C.d;
+                t = t < head ? t : tail + t - head;
+                const i64 at = t * C.token + h * C.head + i;
+                if (C.bytes == 2) ((unsigned short *)C.x)[at] = 0; else ((float *)C.x)[at] = 0.0f;
+            }
+        }
+        return;
+    }
+    __shared__ int count[PLAN_BUCKETS];
+    __shared__ int from[PLAN_BUCKETS];
+    for (int x = threadIdx.x; x < PLAN_BUCKETS; x += 1024) count[x] = 0;
+    __syncthreads();
+    // work of a block: queries (by_key 0) see the keys up to them, keys (by_key 1) are seen by the queries from them on
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int i = threadIdx.x >> 5; i < A.N; i += 32) {
+            const i64 lo = max(A.start[i], (i64)0), hi = min(A.start[i + 1], A.T);
+            const int blocks = hi > lo ? (int)((hi - lo + A.rows - 1) / A.rows) : 0;
+            for (int b = threadIdx.x & 31; b < blocks; b += 32) {
+                const int work = !A.causal ? blocks : A.by_key ? blocks - b : b + 1;
+                const int bucket = PLAN_BUCKETS - 1 - min(work - 1, PLAN_BUCKETS - 1);
+                if (pass == 0) atomicAdd(&count[bucket], 1);
+                else {
+                    const int at = atomicAdd(&from[bucket], 1);
+                    if (at < A.most) A.items[at] = make_int2(i, b);
+                }
+            }
+        }
+        __syncthreads();
+        if (pass == 0 && threadIdx.x < 32) {
+            int sum = 0;
+            for (int base = 0; base < PLAN_BUCKETS; base += 32) {
+                int c = count[base + threadIdx.x], x = c;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, x, o);
+                    if ((int)threadIdx.x >= o) x += y;
+                }
+                from[base + threadIdx.x] = sum + x - c;
+                sum += __shfl_sync(0xffffffffu, x, 31);
+            }
+            if (threadIdx.x == 0) { A.head->count = min(sum, A.most); A.head->status = 0; }
+        }
+        __syncthreads();
+    }
+}
+
+int rp_launch_attend_plan(const AttendPlan &A, cudaStream_t stream)
+{
+    k_attend_plan<<<1 + 32, 1024, 0, stream>>>(A);
+    return rp_op_launched();
+}
+
+// ---------------------------------------------------------------------------------------
+// the kernel
+// ---------------------------------------------------------------------------------------
+struct AttendArgs {
+    const AttendHead *head;
+    const int2 *items;
+    const i64 *start;
+    i64 T;
+    int N, Hq, share, d, causal;            // share: query heads to a key head
+    float scale;
+    void *out;
+    i64 o_token, o_head;
+    float *lse;
+    i64 l_token, l_head;
+    int *status;
+};
+
+template <int D> struct FwdSmem {
+    static constexpr int TILE = 128 * D * 2, STAGES = D == 128 ? 4 : 6;
+    alignas(1024) unsigned char q[2][TILE];
+    alignas(1024) unsigned char kv[STAGES][TILE];
+    u64 q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_full[2], o_full[2], done;
+    u32 tmem;
+    volatile int gave_up;
+};
+
+#define FWD_THREADS 320
+
+template <typename X, int D>
+__global__ void __launch_bounds__(FWD_THREADS, 1)
+k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttendArgs A)
+{
+    typedef FwdSmem<D> Smem;
+    constexpr int STAGES = Smem::STAGES, PANELS = D / 64, PANEL = 128 * 128;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    Smem &sm = *(Smem *)(raw + ((1024 - (rp_smem(raw) & 1023)) & 1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        bar_init(rp_smem(&sm.q_full), 1); bar_init(rp_smem(&sm.q_empty), 1);
+        for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.kv_full[s]), 1); bar_init(rp_smem(&sm.kv_empty[s]), 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.p_full[i]), 128); bar_init(rp_smem(&sm.o_full[i]), 1); }
+        bar_init(rp_smem(&sm.done), 1);
+        sm.gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) tmem_alloc(rp_smem(&sm.tmem), 512);
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    const u32 tm = sm.tmem;
+    const int total = A.head->count * A.Hq;
+    volatile int *gave_up = &sm.gave_up;
+
+    if (warp == 8) {
+        // copies
+        if (lane == 0) {
+            tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v);
+            int n = 0;
+            u32 fill = 0;                               // copies into the ring so far
+            bool ok = true;
+            for (int round = 0; ok; ++round, ++n) {
+                const int at = rp_attend_item(round, total);
+                if (at < 0) break;
+                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
+                const int h = at % A.Hq, hk = h / A.share;
+                if (n && !(ok = bar_wait(rp_smem(&sm.q_empty), (n - 1) & 1, gave_up))) break;
+                const int tiles = t.row0 + 128 < t.len ? 2 : 1;
+                bar_expect(rp_smem(&sm.q_full), tiles * Smem::TILE);
+                for (int i = 0; i < tiles; ++i)
+                    for (int p = 0; p < PANELS; ++p)
+                        tma_load3(rp_smem(sm.q[i]) + p * PANEL, &map_q, p * 64, h, (int)t.base + t.row0 + 128 * i, rp_smem(&sm.q_full));
+                const int nk = rp_attend_tiles(t, tiles - 1, A.causal);
+                for (int j = 0; j < 2 * nk; ++j, ++fill) {
+                    const u32 s = fill % STAGES, turn = fill / STAGES;
+                    if (turn && !(ok = bar_wait(rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, gave_up))) break;
+                    bar_expect(rp_smem(&sm.kv_full[s]), Smem::TILE);
+                    for (int p = 0; p < PANELS; ++p)
+                        tma_load3(rp_smem(sm.kv[s]) + p * PANEL, j & 1 ? &map_v : &map_k, p * 64, hk, (int)t.base + (j >> 1) * 128, rp_smem(&sm.kv_full[s]));
+                }
+            }
+            if (!ok) {
+                // nobody may leave while copies are under way
+                for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1);
+                if (n) rp_drain(rp_smem(&sm.q_full), (n - 1) & 1);
+                rp_drain(rp_smem(&sm.q_full), n & 1);
+            }
+        }
+    } else if (warp == 9) {
+        // products
+        const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
+        u32 used = 0, ps[2] = { 0, 0 };                 // copies taken from the ring; weights taken of each tile
+        bool ok = true;
+        auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
+            if (lane == 0) {
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    const u32 off = (x / 4) * PANEL + (x % 4) * 32;
+                    mma_ss(tm + i * 128, mma_operand(rp_smem(sm.q[i]) + off, true, 0), mma_operand(rp_smem(sm.kv[stage]) + off, true, 0), shape_s, x > 0);
+                }
+                mma_commit(rp_smem(&sm.s_full[i]));
+            }
+        };
+        for (int round = 0; ok; ++round) {
+            const int at = rp_attend_item(round, total);
+            if (at < 0) break;
+            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
+            const int tiles = t.row0 + 128 < t.len ? 2 : 1, n0 = rp_attend_tiles(t, 0, A.causal), n1 = tiles == 2 ? rp_attend_tiles(t, 1, A.causal) : 0;
+            const int nk = max(n0, n1);
+            if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), round & 1, gave_up))) break;
+            if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up))) break;
+            for (int i = 0; i < tiles; ++i) scores(i, used % STAGES);
+            if (lane == 0) { mma_commit(rp_smem(&sm.kv_empty[used % STAGES])); if (nk == 1) mma_commit(rp_smem(&sm.q_empty)); }
+            ++used;
+            for (int j = 0; ok && j < nk; ++j) {
+                const u32 sv = used % STAGES, sk = (used + 1) % STAGES;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[sv]), (used / STAGES) & 1, gave_up))) break;
+                // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
+                if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.kv[sv], t.len - j * 128, 128, lane);
+                bool keys = false;                      // the next keys have come
+                for (int i = 0; i < tiles; ++i) {
+                    const int ni = i ? n1 : n0;
+                    if (j >= ni) continue;
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[i]), ps[i] & 1, gave_up))) break;
+                    ++ps[i];
+                    tmem_after();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            mma_ts(tm + 256 + i * D, tm + i * 128 + x * 8, mma_operand(rp_smem(sm.kv[sv]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
+                        if (j == ni - 1) mma_commit(rp_smem(&sm.o_full[i]));
+                    }
+                    if (j + 1 < ni) {
+                        if (!keys && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;
+                        keys = true;
+                        scores(i, sk);
+                    }
+                }
+                if (!ok) break;
+                if (lane == 0) {
+                    mma_commit(rp_smem(&sm.kv_empty[sv]));
+                    if (j + 1 < nk) mma_commit(rp_smem(&sm.kv_empty[sk]));
+                    if (j + 2 == nk) mma_commit(rp_smem(&sm.q_empty));
+                }
+                used += j + 1 < nk ? 2 : 1;
+            }
+        }
+        // nobody may leave while products are under way
+        if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
+    } else {
+        // softmax of a tile
+        const int i = warp >> 2, row = threadIdx.x & 127;
+        const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + i * 128, to = tm + lanes + 256 + i * D;
+        const float sl = A.scale * RP_LOG2E;
+        u32 ss = 0, os = 0;
+        for (int round = 0;; ++round) {
+            const int at = rp_attend_item(round, total);
+            if (at < 0) break;
+            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
+            const int h = at % A.Hq, r0 = t.row0 + 128 * i, r = r0 + row;
+            if (r0 >= t.len) continue;
+            const int nk = rp_attend_tiles(t, i, A.causal);
+            float m = -INFINITY, l = 0.0f;
+            bool ok = true;
+            for (int j = 0; j < nk; ++j) {
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[i]), ss & 1, gave_up))) break;
+                ++ss;
+                tmem_after();
+                u32 s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_load32(ts + 32 * c, s + 32 * c);
+                tmem_loaded();
+                if (j * 128 + 128 > t.len || (A.causal && j * 128 + 127 > r0)) {
+                    const int lim = (A.causal ? min(t.len, r + 1) : t.len) - j * 128;
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : 0xff800000u;
+                }
+                float top = __uint_as_float(s[0]);
+#pragma unroll
+                for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(s[c]));
+                if (j == 0) m = top == -INFINITY ? 0.0f : top;
+                else {
+                    // (a maximum that grows by less than 2^8 stays: weights up to 256 and their sums lose nothing)
+                    const float grown = (top - m) * sl;
+                    if (__any_sync(0xffffffffu, grown > 8.0f)) {
+                        const float up = fmaxf(top, m), f = rp_exp2((m - up) * sl);
+                        m = up;
+                        l *= f;
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            u32 o[32];
+                            tmem_load32(to + c, o);
+                            tmem_loaded();
+#pragma unroll
+                            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                            tmem_store32(to + c, o);
+                        }
+                    }
+                }
+                const float shift = -m * sl;
+                float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+                for (int c = 0; c < 128; c += 2) {
+                    const float a = rp_exp2(fmaf(__uint_as_float(s[c]), sl, shift)), b = rp_exp2(fmaf(__uint_as_float(s[c + 1]), sl, shift));
+                    sum0 += a; sum1 += b;
+                    s[c / 2] = rp_pair(a, b, X());
+                }
+                l += sum0 + sum1;
+                tmem_store32(ts, s);
+                tmem_store32(ts + 32, s + 32);
+                tmem_stored();
+                tmem_before();
+                bar_arrive(rp_smem(&sm.p_full[i]));
+            }
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.o_full[i]), os & 1, gave_up);
+            ++os;
+            tmem_after();
+            const float f = ok ? 1.0f / l : NAN;
+            X *out = (X *)A.out + (t.base + r) * A.o_token + h * A.o_head;
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                u32 o[32];
+                tmem_load32(to + c, o);
+                tmem_loaded();
+                float v[32];
+#pragma unroll
+                for (int x = 0; x < 32; ++x) v[x] = __uint_as_float(o[x]) * f;
+#pragma unroll
+                for (int x = 0; x < 32; x += 8)
+                    if (r < t.len && c + x < A.d) rp_store8(out + c + x, rp_close8<X>(v + x));
+                __syncwarp();
+            }
+            if (r < t.len && A.lse) A.lse[(t.base + r) * A.l_token + h * A.l_head] = ok ? fmaf(m, A.scale, logf(l)) : NAN;
+            __syncwarp();
+            tmem_before();
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
+    if (warp == 8) tmem_free(tm, 512);
+}
+
+// ---------------------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------------------
+int rp_tensor_map(CUtensorMap *map, int type, const void *x, i64 tokens, int heads, int dim, i64 token_stride, i64 head_stride, int rows)
+{
+    typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                               const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static Encode encode = nullptr;                      // the same value from every thread that fills it in
+    if (!encode) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult how;
+        RP_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &how));
+        if (!fn || how != cudaDriverEntryPointSuccess) return RP_ERR_CUDA;
+        encode = (Encode)fn;
+    }
+    if (heads == 1) head_stride = 8;                     // (not used)
+    if (tokens == 1) token_stride = 8;
+    const cuuint64_t size[3] = { (cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)tokens };
+    const cuuint64_t stride[2] = { (cuuint64_t)head_stride * 2, (cuuint64_t)token_stride * 2 };
+    const cuuint32_t box[3] = { 64, 1, (cuuint32_t)rows }, one[3] = { 1, 1, 1 };
+    const CUresult e = encode(map, type == RP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (void *)x, size, stride, box, one,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return e == CUDA_SUCCESS ? RP_OK : RP_ERR_ARG;
+}
+
+int rp_attend_check(const rp_attend_config *a, i64 T, int N)
+{
+    if (!a || T < 0 || N < 1 || a->q_heads < 1 || a->kv_heads < 1 || a->head_dim < 1 || (a->type != RP_F16 && a->type != RP_BF16) || a->causal < 0 || a->causal > 1 ||
+        !(a->scale > 0.0f) || !(a->scale < INFINITY))
+        return RP_ERR_ARG;
+    if (a->q_heads % a->kv_heads || a->head_dim % 8) return RP_ERR_SHAPE;
+    if (a->head_dim > 128 || a->q_heads > 65536 || T >= (1ll << 31) - 512 || N > (1 << 24)) return RP_ERR_RANGE;
+    if ((T / 64 + N) * a->q_heads >= (1ll << 31)) return RP_ERR_RANGE;
+    return RP_OK;
+}
+int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev)
+{
+    if (!v || !v->x || !rp_aligned(v->x, 16)) return RP_ERR_ARG;
+    if ((T > 1 && (v->token < 1 || v->token % 8 || v->token >= (1ll << 39))) || (heads > 1 && (v->head < 1 || v->head % 8 || v->head >= (1ll << 39)))) return RP_ERR_ARG;
+    return dev.hold(v->x);
+}
+static i64 plan_bytes(i64 T, int N, int rows) { return (i64)sizeof(AttendHead) + 8 * (T / rows + N); }
+
+extern "C" int64_t rp_attend_workspace(const rp_attend_config *a, int64_t n_tokens, int32_t n_samples)
+{
+    if (rp_attend_check(a, n_tokens, n_samples) != RP_OK) return 0;
+    return plan_bytes(n_tokens, n_samples, 256);
+}
+
+template <typename X, int D>
+static int launch(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const AttendArgs &A, int ctas, cudaStream_t stream)
+{
+    const size_t smem = sizeof(FwdSmem<D>) + 1024;
+    RP_CUDA(cudaFuncSetAttribute(k_attend<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    k_attend<X, D><<<ctas, FWD_THREADS, smem, stream>>>(q, k, v, A);
+    return rp_op_launched();
+}
+
+extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const int64_t *start,
+                         int32_t n_samples, const rp_view *out, const rp_view *lse, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    RP_TRY(rp_attend_check(a, n_tokens, n_samples));
+    if (!start || !rp_aligned(start, 8) || !workspace || !rp_aligned(workspace, 16) || workspace_bytes < rp_attend_workspace(a, n_tokens, n_samples)) return RP_ERR_ARG;
+    if (n_tokens == 0) return RP_OK;
+    RpOpDevice dev;
+    RP_TRY(rp_attend_view(q, n_tokens, a->q_heads, dev));
+    RP_TRY(rp_attend_view(k, n_tokens, a->kv_heads, dev));
+    RP_TRY(rp_attend_view(v, n_tokens, a->kv_heads, dev));
+    RP_TRY(rp_attend_view(out, n_tokens, a->q_heads, dev));
+    if (lse && lse->x && !rp_aligned(lse->x, 4)) return RP_ERR_ARG;
+    RP_TRY(rp_op_enter(dev, start, workspace, lse ? lse->x : nullptr));
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    AttendHead *head = (AttendHead *)workspace;
+    int2 *items = (int2 *)(head + 1);
+    AttendPlan P = {};
+    P.start = (const i64 *)start; P.T = n_tokens; P.N = n_samples; P.rows = 256; P.causal = a->causal; P.by_key = 0; P.most = (int)(n_tokens / 256 + n_samples);
+    P.head = head; P.items = items; P.n_clear = 1;
+    P.clear[0] = { out->x, out->token, out->head, a->q_heads, a->head_dim, 2 };
+    if (lse && lse->x) P.clear[P.n_clear++] = { lse->x, lse->token, lse->head, a->q_heads, 1, 4 };
+    CUtensorMap mq, mk, mv;
+    RP_TRY(rp_tensor_map(&mq, a->type, q->x, n_tokens, a->q_heads, a->head_dim, q->token, q->head, 128));
+    RP_TRY(rp_tensor_map(&mk, a->type, k->x, n_tokens, a->kv_heads, a->head_dim, k->token, k->head, 128));
+    RP_TRY(rp_tensor_map(&mv, a->type, v->x, n_tokens, a->kv_heads, a->head_dim, v->token, v->head, 128));
+    RP_TRY(rp_launch_attend_plan(P, stream));
+    AttendArgs A = {};
+    A.head = head; A.items = items; A.start = (const i64 *)start; A.T = n_tokens; A.N = n_samples; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads;
+    A.d = a->head_dim; A.causal = a->causal; A.scale = a->scale; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
+    if (lse && lse->x) { A.lse = (float *)lse->x; A.l_token = lse->token; A.l_head = lse->head; }
+    A.status = &head->status;
+    const int ctas = (int)std::min((i64)rp_op_sms(dev.device), (i64)P.most * a->q_heads);
+    if (a->type == RP_F16) return a->head_dim <= 64 ? launch<__half, 64>(mq, mk, mv, A, ctas, stream) : launch<__half, 128>(mq, mk, mv, A, ctas, stream);
+    return a->head_dim <= 64 ? launch<bf16, 64>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128>(mq, mk, mv, A, ctas, stream);
+}

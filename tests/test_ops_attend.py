@@ -1,0 +1,153 @@
+"""Attention inside the samples of a packed row, and its gradient, against the formulas in 64 bits."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import paper_2608_12146_b200.binding as rp
+
+
+def weights(q, k, scale, causal):
+    """Softmax weights [n, n] of one sample and one head, and the log of each row's sum, in 64 bits."""
+    import torch
+    s = q @ k.T * scale
+    if causal:
+        s = s.masked_fill(torch.ones_like(s, dtype=torch.bool).triu(1), -math.inf)
+    return torch.softmax(s, 1), torch.logsumexp(s, 1)
+
+
+def samples(start, T):
+    for lo, hi in zip(start, start[1:]):
+        lo, hi = max(lo, 0), min(hi, T)
+        if hi > lo:
+            yield lo, hi
+
+
+def test_refusals():
+    lib = rp.lib()
+    buf = np.zeros(4096, np.float64)
+    p = (buf.ctypes.data + 15) // 16 * 16
+
+    def a(hq=2, hk=1, d=64, kind=2, causal=1, scale=0.1):
+        return C.byref(rp.rp_attend_config(hq, hk, d, kind, causal, scale))
+
+    def view(x=p, token=128, head=64):
+        return C.byref(rp.rp_view(x, token, head))
+
+    def fwd(cfg=a(), T=2, q=view(), k=view(), v=view(), start=p, N=1, out=view(), lse=None, space=p, nbytes=1 << 14):
+        return lib.rp_attend(cfg, T, q, k, v, start, N, out, lse, space, nbytes, None)
+
+    assert fwd() == -1                                   # host arrays
+    for bad in (dict(cfg=None), dict(T=-1), dict(N=0), dict(start=None), dict(start=p + 4), dict(space=None), dict(space=p + 8), dict(nbytes=8), dict(q=None),
+                dict(k=view(x=None)), dict(v=view(x=p + 8)), dict(out=view(token=0)), dict(q=view(head=-64)), dict(k=view(token=100)), dict(cfg=a(hq=0)),
+                dict(cfg=a(kind=0)), dict(cfg=a(causal=2)), dict(cfg=a(scale=0.0)), dict(cfg=a(scale=-1.0)), dict(cfg=a(scale=math.inf)),
+                dict(cfg=a(scale=math.nan))):
+        assert fwd(**bad) == -1, bad
+    assert fwd(cfg=a(hq=3, hk=2)) == -2 and fwd(cfg=a(d=60)) == -2 and fwd(cfg=a(d=136)) == -5 and fwd(T=(1 << 31) - 512) == -5
+    assert lib.rp_attend_workspace(None, 1, 1) == 0 and lib.rp_attend_workspace(a(), 1, 0) == 0 and lib.rp_attend_workspace(a(), 1000, 3) > 0
+
+
+SHAPES = [
+    # tokens, query heads, key heads, head size, starts
+    (1, 1, 1, 64, [0, 1]), (1, 4, 2, 128, [0, 1]), (64, 2, 2, 64, list(range(65))), (127, 2, 1, 128, [0, 127]), (128, 1, 1, 64, [0, 128]),
+    (129, 1, 1, 128, [0, 129]), (257, 3, 1, 64, [0, 256, 257]), (300, 2, 1, 128, [0, 0, 5, 133, 133, 300]), (500, 4, 4, 64, [17, 200, 444]),
+    (384, 2, 1, 96, [0, 100, 384]), (640, 2, 2, 80, [-7, 300, 700]), (700, 2, 1, 8, [0, 700]), (1000, 5, 1, 128, [0, 1, 2, 130, 600, 1000]),
+    (2049, 2, 1, 64, [0, 2049]), (1500, 6, 2, 120, [0, 700, 1500]), (4096, 1, 1, 128, [0, 1024, 4096]), (777, 16, 4, 128, [0, 777]),
+]
+
+
+def inputs(shape, kind, extra=0):
+    """q, k, v as slices of one tensor, as a projection of all three leaves them."""
+    import torch
+    T, hq, hk, d, start = shape
+    g = torch.Generator().manual_seed(T + d)
+    wide = torch.randn(T, hq + 2 * hk, d + extra, generator=g).to(getattr(torch, kind)).cuda()
+    return wide[:, :hq, :d], wide[:, hq:hq + hk, :d], wide[:, hq + hk:, :d], g
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind,extra", [("bfloat16", 0), ("float16", 8)])
+@pytest.mark.parametrize("shape", SHAPES, ids=[str(s[:4]) for s in SHAPES])
+def test_forward(shape, kind, extra, causal):
+    import torch
+    T, hq, hk, d, start = shape
+    q, k, v, _ = inputs(shape, kind, extra)
+    out, lse = rp.rp_attend(q, k, v, torch.tensor(start, device="cuda"), causal=causal, scale=0.2)
+    half = torch.finfo(q.dtype).eps / 2
+    seen = torch.zeros(T, dtype=torch.bool)
+    for lo, hi in samples(start, T):
+        seen[lo:hi] = True
+        for h in range(hq):
+            p, w_lse = weights(q[lo:hi, h].double(), k[lo:hi, h // (hq // hk)].double(), 0.2, causal)
+            v64 = v[lo:hi, h // (hq // hk)].double()
+            want, size = p @ v64, p @ v64.abs()
+            # every weight and the output rounded once; scores in 32 bits (|s| <= 20: 1e-5 of a weight); values under the 16-bit types' normal range
+            assert ((out[lo:hi, h].double() - want).abs() <= half * (size + want.abs()) + 1e-5 * size + 1e-7).all()
+            assert ((lse[lo:hi, h].double() - w_lse).abs() <= 4e-6 * (1 + w_lse.abs())).all()
+    assert (out[~seen.cuda()] == 0).all() and (lse[~seen.cuda()] == 0).all()
+
+
+@pytest.mark.gpu
+def test_other_samples_do_not_matter():
+    """Infinities and NaN in the tokens of other samples and in the row's padding; the rows behind the outputs stay."""
+    import torch
+    shape = (400, 2, 1, 128, [0, 70, 211, 330])
+    start = torch.tensor(shape[4], device="cuda")
+    q, k, v, g = inputs(shape, "bfloat16")
+    want = rp.rp_attend(q, k, v, start)
+    bad = [x.clone() for x in (q, k, v)]
+    for x in bad:
+        x[:70] = float("nan")
+        x[211:300] = float("inf")
+        x[330:] = float("nan")
+    big = torch.full((405, 2, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((405, 2), 3.0, device="cuda")
+    rp.rp_attend(*bad, start, out=big[:400], lse=lse[:400])
+    assert (big[70:211] == want[0][70:211]).all() and (lse[70:211] == want[1][70:211]).all()
+    assert (big[330:400] == 0).all() and (big[400:] == 3).all() and (lse[400:] == 3).all()
+
+
+@pytest.mark.gpu
+def test_scores_far_apart():
+    """Rows whose maximum grows by much from tile to tile, and rows that one key takes whole."""
+    import torch
+    T = 1024
+    q, k, v, g = inputs((T, 1, 1, 64, [0, T]), "bfloat16")
+    k = (k * torch.linspace(0.1, 30, T, device="cuda")[:, None, None]).bfloat16()
+    out, lse = rp.rp_attend(q, k, v, torch.tensor([0, T], device="cuda"), causal=True, scale=0.125)
+    p, w_lse = weights(q[:, 0].double(), k[:, 0].double(), 0.125, True)
+    size = p @ v[:, 0].double().abs()
+    # (scores to 250: 32 bits leave them 2e-5, so 3e-5 of a weight)
+    assert ((out[:, 0].double() - p @ v[:, 0].double()).abs() <= 2.0 ** -8 * (size + (p @ v[:, 0].double()).abs()) + 6e-5 * size).all()
+    assert ((lse[:, 0].double() - w_lse).abs() <= 4e-6 * (1 + w_lse.abs())).all()
+
+
+@pytest.mark.gpu
+def test_repeated_streamed_and_captured_calls_agree_bit_for_bit():
+    import torch
+    shape = (3000, 8, 2, 128, [0, 500, 501, 3000])
+    q, k, v, _ = inputs(shape, "bfloat16")
+    start = torch.tensor(shape[4], device="cuda")
+    want = rp.rp_attend(q, k, v, start)
+    torch.cuda.synchronize()
+    results = [rp.rp_attend(q, k, v, start, stream=s) for s in [torch.cuda.Stream() for _ in range(4)] for _ in range(3)]
+    torch.cuda.synchronize()
+    for got in results:
+        assert all((a == b).all() for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = rp.rp_attend(q, k, v, start)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all((a == b).all() for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_no_tokens():
+    import torch
+    q = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    out, lse = rp.rp_attend(q, q, q, torch.tensor([0, 0], device="cuda"))
+    assert out.shape == (0, 2, 64) and lse.shape == (0, 2)
