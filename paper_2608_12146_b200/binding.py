@@ -29,7 +29,8 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_debug_nl2", "rp_debug_exp2neg", "rp_debug_philox", "rp_debug_launch_count", "rp_debug_l2_read_rate",
            "rp_debug_chain_kernel", "rp_debug_chain_form",
            "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad",
-           "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad", "rp_attend_workspace", "rp_attend")
+           "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad", "rp_attend_workspace", "rp_attend",
+           "rp_attend_grad_workspace", "rp_attend_grad")
 
 
 class RpError(RuntimeError):
@@ -147,6 +148,9 @@ def lib():
         L.rp_attend_workspace.restype = Q
         L.rp_attend_workspace.argtypes = [C.POINTER(rp_attend_config), Q, I]
         L.rp_attend.argtypes = [C.POINTER(rp_attend_config), Q, W, W, W, V, I, W, W, V, Q, V]
+        L.rp_attend_grad_workspace.restype = Q
+        L.rp_attend_grad_workspace.argtypes = [C.POINTER(rp_attend_config), Q, I]
+        L.rp_attend_grad.argtypes = [C.POINTER(rp_attend_config), Q, W, W, W, W, W, W, V, I, W, W, W, V, Q, V]
         _lib = L
     return _lib
 
@@ -641,6 +645,25 @@ def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = N
             _check(lib().rp_attend(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _view(out, q, "out"), _lse_view(lse, T, H, torch),
                                    space.data_ptr(), nbytes, queue.handle), "rp_attend")
     return out, lse
+
+
+def rp_attend_grad(out_grad, q, k, v, out, lse, start, *, causal: bool = True, scale: Optional[float] = None, q_grad=None, k_grad=None, v_grad=None,
+                   stream=None):
+    """Gradients (q_grad, k_grad, v_grad) of rp_attend from that of its output, its inputs, ``out`` and ``lse``."""
+    torch = _torch()
+    ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
+    T, H, _ = q.shape
+    with _Queue(torch, q, stream) as queue:
+        q_grad = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_grad is None else q_grad
+        k_grad = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_grad is None else k_grad
+        v_grad = torch.empty(v.shape, dtype=v.dtype, device=v.device) if v_grad is None else v_grad
+        nbytes = lib().rp_attend_grad_workspace(ref, T, n)
+        space = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+        if T:
+            _check(lib().rp_attend_grad(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), _view(out, q, "out"), _lse_view(lse, T, H, torch),
+                                        _view(out_grad, q, "out_grad"), at, n, _view(q_grad, q, "q_grad"), _view(k_grad, k, "k_grad"),
+                                        _view(v_grad, v, "v_grad"), space.data_ptr(), nbytes, queue.handle), "rp_attend_grad")
+    return q_grad, k_grad, v_grad
 
 
 # ---- inspection hooks -------------------------------------------------------------------

@@ -107,10 +107,8 @@ template <int D> struct FwdSmem {
     volatile int gave_up;
 };
 
-#define FWD_THREADS 320
-
 template <typename X, int D>
-__global__ void __launch_bounds__(FWD_THREADS, 1)
+__global__ void __launch_bounds__(ATTEND_THREADS, 1)
 k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttendArgs A)
 {
     typedef FwdSmem<D> Smem;
@@ -126,7 +124,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) tmem_alloc(rp_smem(&sm.tmem), 512);
+    if (warp == ATTEND_COPY_WARP) tmem_alloc(rp_smem(&sm.tmem), 512);
     tmem_before();
     __syncthreads();
     tmem_after();
@@ -134,9 +132,9 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     const int total = A.head->count * A.Hq;
     volatile int *gave_up = &sm.gave_up;
 
-    if (warp == 8) {
-        // copies
-        if (lane == 0) {
+    if (warp >= 8) {
+        rp_few_registers();
+        if (warp == ATTEND_COPY_WARP && lane == 0) {
             tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v);
             int n = 0;
             u32 fill = 0;                               // copies into the ring so far
@@ -168,69 +166,69 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 rp_drain(rp_smem(&sm.q_full), n & 1);
             }
         }
-    } else if (warp == 9) {
-        // products
-        const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
-        u32 used = 0, ps[2] = { 0, 0 };                 // copies taken from the ring; weights taken of each tile
-        bool ok = true;
-        auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
-            if (lane == 0) {
-#pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const u32 off = (x / 4) * PANEL + (x % 4) * 32;
-                    mma_ss(tm + i * 128, mma_operand(rp_smem(sm.q[i]) + off, true, 0), mma_operand(rp_smem(sm.kv[stage]) + off, true, 0), shape_s, x > 0);
-                }
-                mma_commit(rp_smem(&sm.s_full[i]));
-            }
-        };
-        for (int round = 0; ok; ++round) {
-            const int at = rp_attend_item(round, total);
-            if (at < 0) break;
-            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
-            const int tiles = t.row0 + 128 < t.len ? 2 : 1, n0 = rp_attend_tiles(t, 0, A.causal), n1 = tiles == 2 ? rp_attend_tiles(t, 1, A.causal) : 0;
-            const int nk = max(n0, n1);
-            if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), round & 1, gave_up))) break;
-            if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up))) break;
-            for (int i = 0; i < tiles; ++i) scores(i, used % STAGES);
-            if (lane == 0) { mma_commit(rp_smem(&sm.kv_empty[used % STAGES])); if (nk == 1) mma_commit(rp_smem(&sm.q_empty)); }
-            ++used;
-            for (int j = 0; ok && j < nk; ++j) {
-                const u32 sv = used % STAGES, sk = (used + 1) % STAGES;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[sv]), (used / STAGES) & 1, gave_up))) break;
-                // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
-                if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.kv[sv], t.len - j * 128, 128, lane);
-                bool keys = false;                      // the next keys have come
-                for (int i = 0; i < tiles; ++i) {
-                    const int ni = i ? n1 : n0;
-                    if (j >= ni) continue;
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[i]), ps[i] & 1, gave_up))) break;
-                    ++ps[i];
-                    tmem_after();
-                    if (lane == 0) {
-#pragma unroll
-                        for (int x = 0; x < 8; ++x)
-                            mma_ts(tm + 256 + i * D, tm + i * 128 + x * 8, mma_operand(rp_smem(sm.kv[sv]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
-                        if (j == ni - 1) mma_commit(rp_smem(&sm.o_full[i]));
-                    }
-                    if (j + 1 < ni) {
-                        if (!keys && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;
-                        keys = true;
-                        scores(i, sk);
-                    }
-                }
-                if (!ok) break;
+        if (warp == ATTEND_MMA_WARP) {
+            const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
+            u32 used = 0, ps[2] = { 0, 0 };                 // copies taken from the ring; weights taken of each tile
+            bool ok = true;
+            auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
                 if (lane == 0) {
-                    mma_commit(rp_smem(&sm.kv_empty[sv]));
-                    if (j + 1 < nk) mma_commit(rp_smem(&sm.kv_empty[sk]));
-                    if (j + 2 == nk) mma_commit(rp_smem(&sm.q_empty));
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x) {
+                        const u32 off = (x / 4) * PANEL + (x % 4) * 32;
+                        mma_ss(tm + i * 128, mma_operand(rp_smem(sm.q[i]) + off, true, 0), mma_operand(rp_smem(sm.kv[stage]) + off, true, 0), shape_s, x > 0);
+                    }
+                    mma_commit(rp_smem(&sm.s_full[i]));
                 }
-                used += j + 1 < nk ? 2 : 1;
+            };
+            for (int round = 0; ok; ++round) {
+                const int at = rp_attend_item(round, total);
+                if (at < 0) break;
+                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
+                const int tiles = t.row0 + 128 < t.len ? 2 : 1, n0 = rp_attend_tiles(t, 0, A.causal), n1 = tiles == 2 ? rp_attend_tiles(t, 1, A.causal) : 0;
+                const int nk = max(n0, n1);
+                if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), round & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up))) break;
+                for (int i = 0; i < tiles; ++i) scores(i, used % STAGES);
+                if (lane == 0) { mma_commit(rp_smem(&sm.kv_empty[used % STAGES])); if (nk == 1) mma_commit(rp_smem(&sm.q_empty)); }
+                ++used;
+                for (int j = 0; ok && j < nk; ++j) {
+                    const u32 sv = used % STAGES, sk = (used + 1) % STAGES;
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[sv]), (used / STAGES) & 1, gave_up))) break;
+                    // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
+                    if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.kv[sv], t.len - j * 128, 128, lane);
+                    bool keys = false;                      // the next keys have come
+                    for (int i = 0; i < tiles; ++i) {
+                        const int ni = i ? n1 : n0;
+                        if (j >= ni) continue;
+                        if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[i]), ps[i] & 1, gave_up))) break;
+                        ++ps[i];
+                        tmem_after();
+                        if (lane == 0) {
+#pragma unroll
+                            for (int x = 0; x < 8; ++x)
+                                mma_ts(tm + 256 + i * D, tm + i * 128 + x * 8, mma_operand(rp_smem(sm.kv[sv]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
+                            if (j == ni - 1) mma_commit(rp_smem(&sm.o_full[i]));
+                        }
+                        if (j + 1 < ni) {
+                            if (!keys && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;
+                            keys = true;
+                            scores(i, sk);
+                        }
+                    }
+                    if (!ok) break;
+                    if (lane == 0) {
+                        mma_commit(rp_smem(&sm.kv_empty[sv]));
+                        if (j + 1 < nk) mma_commit(rp_smem(&sm.kv_empty[sk]));
+                        if (j + 2 == nk) mma_commit(rp_smem(&sm.q_empty));
+                    }
+                    used += j + 1 < nk ? 2 : 1;
+                }
             }
+            // nobody may leave while products are under way
+            if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
         }
-        // nobody may leave while products are under way
-        if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
     } else {
-        // softmax of a tile
+        rp_many_registers();
         const int i = warp >> 2, row = threadIdx.x & 127;
         const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + i * 128, to = tm + lanes + 256 + i * D;
         const float sl = A.scale * RP_LOG2E;
@@ -320,7 +318,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     __syncwarp();
     __syncthreads();
     if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
-    if (warp == 8) tmem_free(tm, 512);
+    if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -377,7 +375,7 @@ static int launch(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap 
 {
     const size_t smem = sizeof(FwdSmem<D>) + 1024;
     RP_CUDA(cudaFuncSetAttribute(k_attend<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    k_attend<X, D><<<ctas, FWD_THREADS, smem, stream>>>(q, k, v, A);
+    k_attend<X, D><<<ctas, ATTEND_THREADS, smem, stream>>>(q, k, v, A);
     return rp_op_launched();
 }
 

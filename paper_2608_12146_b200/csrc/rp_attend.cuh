@@ -18,6 +18,14 @@ int rp_launch_attend_plan(const AttendPlan &A, cudaStream_t stream);
 int rp_attend_check(const rp_attend_config *a, i64 T, int N);
 int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev);
 
+// The attention kernels have twelve warps: eight for the softmax, in two groups of four (a warp reaches the 32 rows of tensor memory that go by its number), one that
+// copies, one that issues the products, two that wait.  The latter four give registers to the former eight: 4 * 32 * 72 + 8 * 32 * 216 = 12 * 32 * 168.
+#define ATTEND_THREADS 384
+#define ATTEND_COPY_WARP 8
+#define ATTEND_MMA_WARP 9
+__device__ __forceinline__ void rp_many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
+__device__ __forceinline__ void rp_few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
+
 // The CTA's item of a round, -1 when there is none: rounds go through the list forwards and backwards in turn, so that who gets the largest of one
 // round gets the smallest of the next.
 __device__ __forceinline__ int rp_attend_item(int round, int total)

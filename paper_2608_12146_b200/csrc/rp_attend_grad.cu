@@ -1,0 +1,578 @@
+// Gradient of the attention inside the samples of a packed row.
+//
+//   p = exp(scale q k^T - lse), ds = p (do v^T - delta), delta = sum_d do o;   dv = p^T do, dk = scale ds^T q, dq = scale ds k
+//
+// Two kernels: one takes 128 keys and goes through the queries that see them (dk, dv), one takes 128 queries and goes through the keys that they see
+// (dq).  Each output is summed by one CTA in a fixed order: no additions from several CTAs to one place, whose order would change the last bits.  The price is
+// that scores and do v^T are worked out twice, 14 multiply-adds a pair and element in place of 10.  Bound by the tensor cores.
+#include <algorithm>
+
+#include "rp_attend.cuh"
+
+struct GradArgs {
+    const int2 *items;
+    const AttendHead *head;
+    const i64 *start;
+    i64 T;
+    int Hq, Hk, share, d, causal;
+    float scale;
+    const float2 *stats;                     // [Hq][T]: lse / ln 2, delta
+    void *x[2];                              // dv, dk, or dq
+    i64 token[2], hd[2];
+    int *status;
+};
+
+// lse / ln 2 and delta of every token and query head: 16 lanes a head, 16 bytes of do and o a lane.
+template <typename X>
+__global__ void __launch_bounds__(256) k_attend_stats(i64 T, int H, int d, const X *o, i64 o_token, i64 o_head, const X *g, i64 g_token, i64 g_head, const float *lse, i64 l_token,
+                                                      i64 l_head, float2 *stats)
+{
+    const int lane = threadIdx.x & 15;
+    for (i64 x = ((i64)blockIdx.x * 256 + threadIdx.x) >> 4; x - (threadIdx.x >> 4 & 1) < T * H; x += (i64)gridDim.x * 16) {
+        const i64 t = x / H;
+        const int h = (int)(x % H);
+        float sum = 0.0f;
+        if (x < T * H && lane * 8 < d) {
+            float a[8], b[8];
+            rp_open8(rp_load8(o + t * o_token + h * o_head + lane * 8), a);
+            rp_open8(rp_load8(g + t * g_token + h * g_head + lane * 8), b);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(a[i], b[i], sum);
+        }
+#pragma unroll
+        for (int o2 = 1; o2 < 16; o2 <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o2);
+        if (x < T * H && lane == 0) stats[(i64)h * T + t] = make_float2(lse[t * l_token + h * l_head] * RP_LOG2E, sum);
+    }
+}
+
+// One row of an accumulator in tensor memory, D columns, goes out.
+template <typename X, int D>
+__device__ __forceinline__ void store_row(u32 at, X *out, int d, bool there, float f)
+{
+#pragma unroll
+    for (int c = 0; c < D; c += 32) {
+        u32 o[32];
+        tmem_load32(at + c, o);
+        tmem_loaded();
+        float v[32];
+#pragma unroll
+        for (int x = 0; x < 32; ++x) v[x] = __uint_as_float(o[x]) * f;
+#pragma unroll
+        for (int x = 0; x < 32; x += 8)
+            if (there && c + x < d) rp_store8(out + c + x, rp_close8<X>(v + x));
+        __syncwarp();
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// keys: dk and dv
+// ---------------------------------------------------------------------------------------
+// The tiles are 64 queries wide, so that scores and do v^T of two of them fit beside the two sums (2 * 64 + 2 * 64 + 2 * head_dim columns): while one tile's weights
+// are worked out, by four warps of its own, the tensor cores work on the other.
+template <int D> struct KeySmem {
+    static constexpr int TILE = 128 * D * 2, HALF = 64 * D * 2, STAGES = 4;
+    alignas(1024) unsigned char k[TILE];
+    alignas(1024) unsigned char v[TILE];
+    alignas(1024) unsigned char q[STAGES][HALF];
+    alignas(1024) unsigned char g[STAGES][HALF];
+    float2 stats[2][2][64];
+    u64 kv_full, kv_empty, q_full[STAGES], q_empty[STAGES], s_full[2], dp_full[2], p_full[2], ds_full[2], st_full[2], acc_full, acc_empty, done;
+    u32 tmem;
+    volatile int gave_up;
+};
+
+template <typename X, int D>
+__global__ void __launch_bounds__(ATTEND_THREADS, 1)
+k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+              const __grid_constant__ CUtensorMap map_g, const GradArgs A)
+{
+    typedef KeySmem<D> Smem;
+    constexpr int STAGES = Smem::STAGES, PANELS = D / 64, PANEL = 128 * 128, HALF = 64 * 128;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    Smem &sm = *(Smem *)(raw + ((1024 - (rp_smem(raw) & 1023)) & 1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        bar_init(rp_smem(&sm.kv_full), 1); bar_init(rp_smem(&sm.kv_empty), 1);
+        for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.q_full[s]), 1); bar_init(rp_smem(&sm.q_empty[s]), 1); }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.dp_full[i]), 1);
+            bar_init(rp_smem(&sm.p_full[i]), 128); bar_init(rp_smem(&sm.ds_full[i]), 128); bar_init(rp_smem(&sm.st_full[i]), 128);
+        }
+        bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 256); bar_init(rp_smem(&sm.done), 1);
+        sm.gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == ATTEND_COPY_WARP) tmem_alloc(rp_smem(&sm.tmem), 512);
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    const u32 tm = sm.tmem;
+    const int total = A.head->count * A.Hk;
+    volatile int *gave_up = &sm.gave_up;
+
+    if (warp >= 8) {
+        rp_few_registers();
+        if (warp == ATTEND_COPY_WARP && lane == 0) {
+            tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v); tma_prefetch(&map_g);
+            int n = 0;
+            u32 fill = 0;
+            bool ok = true;
+            for (; ok; ++n) {
+                const int at = rp_attend_item(n, total);
+                if (at < 0) break;
+                const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
+                const int hk = at % A.Hk, first = A.causal ? t.row0 >> 6 : 0, per = ((t.len + 63) >> 6) - first;
+                if (n && !(ok = bar_wait(rp_smem(&sm.kv_empty), (n - 1) & 1, gave_up))) break;
+                bar_expect(rp_smem(&sm.kv_full), 2 * Smem::TILE);
+                for (int p = 0; p < PANELS; ++p) {
+                    tma_load3(rp_smem(sm.k) + p * PANEL, &map_k, p * 64, hk, (int)t.base + t.row0, rp_smem(&sm.kv_full));
+                    tma_load3(rp_smem(sm.v) + p * PANEL, &map_v, p * 64, hk, (int)t.base + t.row0, rp_smem(&sm.kv_full));
+                }
+                for (int h = hk * A.share; ok && h < (hk + 1) * A.share; ++h)
+                    for (int j = 0; j < per; ++j, ++fill) {
+                        const u32 s = fill % STAGES, turn = fill / STAGES;
+                        if (turn && !(ok = bar_wait(rp_smem(&sm.q_empty[s]), (turn - 1) & 1, gave_up))) break;
+                        bar_expect(rp_smem(&sm.q_full[s]), 2 * Smem::HALF);
+                        for (int p = 0; p < PANELS; ++p) {
+                            tma_load3(rp_smem(sm.q[s]) + p * HALF, &map_q, p * 64, h, (int)t.base + (first + j) * 64, rp_smem(&sm.q_full[s]));
+                            tma_load3(rp_smem(sm.g[s]) + p * HALF, &map_g, p * 64, h, (int)t.base + (first + j) * 64, rp_smem(&sm.q_full[s]));
+                        }
+                    }
+            }
+            if (!ok) {
+                // nobody may leave while copies are under way
+                for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.q_full[f % STAGES]), (f / STAGES) & 1);
+                if (n) rp_drain(rp_smem(&sm.kv_full), (n - 1) & 1);
+                rp_drain(rp_smem(&sm.kv_full), n & 1);
+            }
+        }
+        if (warp == ATTEND_MMA_WARP) {
+            const u32 shape_s = mma_shape<X>(64, false), shape_o = mma_shape<X>(D, true);
+            u32 base = 0, uses[2] = { 0, 0 };               // tiles of the items before; weights taken of each half
+            bool ok = true;
+            for (int n = 0; ok; ++n) {
+                const int at = rp_attend_item(n, total);
+                if (at < 0) break;
+                const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
+                const int first = A.causal ? t.row0 >> 6 : 0, per = ((t.len + 63) >> 6) - first, nt = per * A.share;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full), n & 1, gave_up))) break;
+                auto scores = [&](int j) -> bool {          // scores and do v^T of a tile
+                    const u32 f = base + j, s = f % STAGES;
+                    const int b = j & 1, left = t.len - (first + j % per) * 64;
+                    if (!bar_wait_warp(rp_smem(&sm.q_full[s]), (f / STAGES) & 1, gave_up)) return false;
+                    // queries behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
+                    if (left < 64) { rp_clear_rows<D, 64>(sm.q[s], left, 64, lane); rp_clear_rows<D, 64>(sm.g[s], left, 64, lane); }
+                    if (lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const u32 oa = (x / 4) * PANEL + (x % 4) * 32, ob = (x / 4) * HALF + (x % 4) * 32;
+                            mma_ss(tm + b * 64, mma_operand(rp_smem(sm.k) + oa, true, 0), mma_operand(rp_smem(sm.q[s]) + ob, true, 0), shape_s, x > 0);
+                        }
+                        mma_commit(rp_smem(&sm.s_full[b]));
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const u32 oa = (x / 4) * PANEL + (x % 4) * 32, ob = (x / 4) * HALF + (x % 4) * 32;
+                            mma_ss(tm + 128 + b * 64, mma_operand(rp_smem(sm.v) + oa, true, 0), mma_operand(rp_smem(sm.g[s]) + ob, true, 0), shape_s, x > 0);
+                        }
+                        mma_commit(rp_smem(&sm.dp_full[b]));
+                        if (j == nt - 1) mma_commit(rp_smem(&sm.kv_empty));
+                    }
+                    return true;
+                };
+                if (!(ok = scores(0))) break;
+                if (nt > 1 && !(ok = scores(1))) break;
+                if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
+                for (int j = 0; j < nt; ++j) {
+                    const int b = j & 1;
+                    const u32 s = (base + j) % STAGES;
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[b]), uses[b] & 1, gave_up))) break;
+                    tmem_after();
+                    if (lane == 0)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            mma_ts(tm + 256, tm + b * 64 + x * 8, mma_operand(rp_smem(sm.g[s]) + x * 2048, false, HALF), shape_o, j > 0 || x > 0);
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full[b]), uses[b] & 1, gave_up))) break;
+                    ++uses[b];
+                    tmem_after();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            mma_ts(tm + 256 + D, tm + 128 + b * 64 + x * 8, mma_operand(rp_smem(sm.q[s]) + x * 2048, false, HALF), shape_o, j > 0 || x > 0);
+                        mma_commit(rp_smem(&sm.q_empty[s]));
+                        if (j == nt - 1) mma_commit(rp_smem(&sm.acc_full));
+                    }
+                    if (j + 2 < nt && !(ok = scores(j + 2))) break;
+                }
+                base += nt;
+            }
+            // nobody may leave while products are under way
+            if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
+        }
+    } else {
+        rp_many_registers();
+        const int b = warp >> 2, row = threadIdx.x & 127;
+        const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + b * 64, td = tm + lanes + 128 + b * 64;
+        const float sl = A.scale * RP_LOG2E;
+        u32 uses = 0;
+        for (int n = 0;; ++n) {
+            const int at = rp_attend_item(n, total);
+            if (at < 0) break;
+            const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
+            const int hk = at % A.Hk, first = A.causal ? t.row0 >> 6 : 0, per = ((t.len + 63) >> 6) - first, nt = per * A.share, r = t.row0 + row;
+            bool ok = true;
+            for (int j = b; j < nt; j += 2) {
+                const int h = hk * A.share + j / per, q0 = (first + j % per) * 64;
+                // (two places in turn: who has come to a tile's barrier has read the tile before)
+                float2 *st = sm.stats[b][uses & 1];
+                if (row < 64) st[row] = q0 + row < t.len ? A.stats[(i64)h * A.T + t.base + q0 + row] : make_float2(0.0f, 0.0f);
+                bar_arrive(rp_smem(&sm.st_full[b]));
+                if (!(ok = bar_wait_warp(rp_smem(&sm.st_full[b]), uses & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[b]), uses & 1, gave_up))) break;
+                tmem_after();
+                u32 s[64];
+                float p[64];
+                tmem_load32(ts, s);
+                tmem_load32(ts + 32, s + 32);
+                tmem_loaded();
+#pragma unroll
+                for (int c = 0; c < 64; ++c) p[c] = rp_exp2(fmaf(__uint_as_float(s[c]), sl, -st[c].x));
+                if (q0 + 64 > t.len || (A.causal && q0 < t.row0 + 128)) {
+                    const int lo = A.causal ? r - q0 : 0, hi = t.len - q0;
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) p[c] = c >= lo && c < hi ? p[c] : 0.0f;
+                }
+#pragma unroll
+                for (int c = 0; c < 32; ++c) s[c] = rp_pair(p[2 * c], p[2 * c + 1], X());
+                tmem_store32(ts, s);
+                tmem_stored();
+                tmem_before();
+                bar_arrive(rp_smem(&sm.p_full[b]));
+                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full[b]), uses & 1, gave_up))) break;
+                ++uses;
+                tmem_after();
+                tmem_load32(td, s);
+                tmem_load32(td + 32, s + 32);
+                tmem_loaded();
+#pragma unroll
+                for (int c = 0; c < 32; ++c)
+                    s[c] = rp_pair(p[2 * c] * (__uint_as_float(s[2 * c]) - st[2 * c].y), p[2 * c + 1] * (__uint_as_float(s[2 * c + 1]) - st[2 * c + 1].y), X());
+                tmem_store32(td, s);
+                tmem_stored();
+                tmem_before();
+                bar_arrive(rp_smem(&sm.ds_full[b]));
+            }
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
+            tmem_after();
+            // the first group hands over dv, the second dk
+            X *out = b ? (X *)A.x[1] + (t.base + r) * A.token[1] + hk * A.hd[1] : (X *)A.x[0] + (t.base + r) * A.token[0] + hk * A.hd[0];
+            store_row<X, D>(tm + lanes + 256 + b * D, out, A.d, r < t.len, !ok ? NAN : b ? A.scale : 1.0f);
+            tmem_before();
+            bar_arrive(rp_smem(&sm.acc_empty));
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
+    if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);
+}
+
+// ---------------------------------------------------------------------------------------
+// queries: dq
+// ---------------------------------------------------------------------------------------
+// Tiles of 128 keys; the scores of the next tile are there when a tile's are worked on (two groups of four warps take tiles in turn), do v^T of the next one comes as
+// soon as it has been read.  The gradients of the scores take the scores' place as operand.  Columns: 2 * 128 + 128 + head_dim.
+template <int D> struct QuerySmem {
+    static constexpr int TILE = 128 * D * 2, KS = 3, VS = 2;
+    alignas(1024) unsigned char q[TILE];
+    alignas(1024) unsigned char g[TILE];
+    alignas(1024) unsigned char k[KS][TILE];
+    alignas(1024) unsigned char v[VS][TILE];
+    u64 q_full, q_empty, k_full[KS], k_empty[KS], v_full[VS], v_empty[VS], s_full[2], dp_full[2], dp_empty, ds_full[2], acc_full, acc_empty, done;
+    u32 tmem;
+    volatile int gave_up;
+};
+
+template <typename X, int D>
+__global__ void __launch_bounds__(ATTEND_THREADS, 1)
+k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                 const __grid_constant__ CUtensorMap map_g, const GradArgs A)
+{
+    typedef QuerySmem<D> Smem;
+    constexpr int KS = Smem::KS, VS = Smem::VS, PANELS = D / 64, PANEL = 128 * 128;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    Smem &sm = *(Smem *)(raw + ((1024 - (rp_smem(raw) & 1023)) & 1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        bar_init(rp_smem(&sm.q_full), 1); bar_init(rp_smem(&sm.q_empty), 1);
+        for (int s = 0; s < KS; ++s) { bar_init(rp_smem(&sm.k_full[s]), 1); bar_init(rp_smem(&sm.k_empty[s]), 1); }
+        for (int s = 0; s < VS; ++s) { bar_init(rp_smem(&sm.v_full[s]), 1); bar_init(rp_smem(&sm.v_empty[s]), 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.dp_full[i]), 1); bar_init(rp_smem(&sm.ds_full[i]), 128); }
+        bar_init(rp_smem(&sm.dp_empty), 128);
+        bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 256); bar_init(rp_smem(&sm.done), 1);
+        sm.gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == ATTEND_COPY_WARP) tmem_alloc(rp_smem(&sm.tmem), 512);
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    const u32 tm = sm.tmem;
+    const int total = A.head->count * A.Hq;
+    volatile int *gave_up = &sm.gave_up;
+
+    if (warp >= 8) {
+        rp_few_registers();
+        if (warp == ATTEND_COPY_WARP && lane == 0) {
+            tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v); tma_prefetch(&map_g);
+            int n = 0;
+            u32 fill = 0;
+            bool ok = true;
+            for (; ok; ++n) {
+                const int at = rp_attend_item(n, total);
+                if (at < 0) break;
+                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
+                const int h = at % A.Hq, hk = h / A.share, nk = rp_attend_tiles(t, 0, A.causal);
+                if (n && !(ok = bar_wait(rp_smem(&sm.q_empty), (n - 1) & 1, gave_up))) break;
+                bar_expect(rp_smem(&sm.q_full), 2 * Smem::TILE);
+                for (int p = 0; p < PANELS; ++p) {
+                    tma_load3(rp_smem(sm.q) + p * PANEL, &map_q, p * 64, h, (int)t.base + t.row0, rp_smem(&sm.q_full));
+                    tma_load3(rp_smem(sm.g) + p * PANEL, &map_g, p * 64, h, (int)t.base + t.row0, rp_smem(&sm.q_full));
+                }
+                for (int j = 0; j < nk; ++j, ++fill) {
+                    const u32 ks = fill % KS, kt = fill / KS, vs = fill % VS, vt = fill / VS;
+                    if (kt && !(ok = bar_wait(rp_smem(&sm.k_empty[ks]), (kt - 1) & 1, gave_up))) break;
+                    if (vt && !(ok = bar_wait(rp_smem(&sm.v_empty[vs]), (vt - 1) & 1, gave_up))) break;
+                    bar_expect(rp_smem(&sm.k_full[ks]), Smem::TILE);
+                    for (int p = 0; p < PANELS; ++p) tma_load3(rp_smem(sm.k[ks]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.k_full[ks]));
+                    bar_expect(rp_smem(&sm.v_full[vs]), Smem::TILE);
+                    for (int p = 0; p < PANELS; ++p) tma_load3(rp_smem(sm.v[vs]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.v_full[vs]));
+                }
+            }
+            if (!ok) {
+                // nobody may leave while copies are under way
+                for (u32 f = fill > (u32)KS ? fill - KS : 0; f < fill; ++f) rp_drain(rp_smem(&sm.k_full[f % KS]), (f / KS) & 1);
+                for (u32 f = fill > (u32)VS ? fill - VS : 0; f < fill; ++f) rp_drain(rp_smem(&sm.v_full[f % VS]), (f / VS) & 1);
+                if (n) rp_drain(rp_smem(&sm.q_full), (n - 1) & 1);
+                rp_drain(rp_smem(&sm.q_full), n & 1);
+            }
+        }
+        if (warp == ATTEND_MMA_WARP) {
+            const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
+            u32 base = 0, ds[2] = { 0, 0 };                 // tiles of the items before; tiles taken of each group
+            bool ok = true;
+            for (int n = 0; ok; ++n) {
+                const int at = rp_attend_item(n, total);
+                if (at < 0) break;
+                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
+                const int nk = rp_attend_tiles(t, 0, A.causal);
+                if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), n & 1, gave_up))) break;
+                auto scores = [&](int j) -> bool {
+                    const u32 f = base + j, s = f % KS;
+                    const int b = j & 1;
+                    if (!bar_wait_warp(rp_smem(&sm.k_full[s]), (f / KS) & 1, gave_up)) return false;
+                    // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
+                    if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.k[s], t.len - j * 128, 128, lane);
+                    if (lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const u32 off = (x / 4) * PANEL + (x % 4) * 32;
+                            mma_ss(tm + b * 128, mma_operand(rp_smem(sm.q) + off, true, 0), mma_operand(rp_smem(sm.k[s]) + off, true, 0), shape_s, x > 0);
+                        }
+                        mma_commit(rp_smem(&sm.s_full[b]));
+                    }
+                    return true;
+                };
+                auto products = [&](int j) -> bool {        // do v^T
+                    const u32 f = base + j, s = f % VS;
+                    if (!bar_wait_warp(rp_smem(&sm.v_full[s]), (f / VS) & 1, gave_up)) return false;
+                    if (lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const u32 off = (x / 4) * PANEL + (x % 4) * 32;
+                            mma_ss(tm + 256, mma_operand(rp_smem(sm.g) + off, true, 0), mma_operand(rp_smem(sm.v[s]) + off, true, 0), shape_s, x > 0);
+                        }
+                        mma_commit(rp_smem(&sm.dp_full[j & 1]));
+                        mma_commit(rp_smem(&sm.v_empty[s]));
+                        if (j == nk - 1) mma_commit(rp_smem(&sm.q_empty));
+                    }
+                    return true;
+                };
+                // (the last tile's do v^T is issued behind its scores: when q_empty is arrived at, both are done with q and do)
+                if (!(ok = scores(0))) break;
+                if (nk > 1 && !(ok = scores(1))) break;
+                if (!(ok = products(0))) break;
+                if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
+                for (int j = 0; j < nk; ++j) {
+                    const int b = j & 1;
+                    const u32 f = base + j;
+                    if (j + 1 < nk) {
+                        if (!(ok = bar_wait_warp(rp_smem(&sm.dp_empty), f & 1, gave_up))) break;
+                        tmem_after();
+                        if (!(ok = products(j + 1))) break;
+                    }
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full[b]), ds[b] & 1, gave_up))) break;
+                    ++ds[b];
+                    tmem_after();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            mma_ts(tm + 384, tm + b * 128 + x * 8, mma_operand(rp_smem(sm.k[f % KS]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
+                        mma_commit(rp_smem(&sm.k_empty[f % KS]));
+                        if (j == nk - 1) mma_commit(rp_smem(&sm.acc_full));
+                    }
+                    if (j + 2 < nk && !(ok = scores(j + 2))) break;
+                }
+                base += nk;
+            }
+            // nobody may leave while products are under way
+            if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
+        }
+    } else {
+        rp_many_registers();
+        const int b = warp >> 2, row = threadIdx.x & 127;
+        const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + b * 128, td = tm + lanes + 256;
+        const float sl = A.scale * RP_LOG2E;
+        u32 uses = 0;
+        for (int n = 0;; ++n) {
+            const int at = rp_attend_item(n, total);
+            if (at < 0) break;
+            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
+            const int h = at % A.Hq, nk = rp_attend_tiles(t, 0, A.causal), r = t.row0 + row;
+            const float2 st = r < t.len ? A.stats[(i64)h * A.T + t.base + r] : make_float2(0.0f, 0.0f);
+            bool ok = true;
+            for (int j = b; j < nk; j += 2) {
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[b]), uses & 1, gave_up))) break;
+                tmem_after();
+                u32 s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_load32(ts + 32 * c, s + 32 * c);
+                tmem_loaded();
+#pragma unroll
+                for (int c = 0; c < 128; ++c) s[c] = __float_as_uint(rp_exp2(fmaf(__uint_as_float(s[c]), sl, -st.x)));
+                const bool edge = j * 128 + 128 > t.len || (A.causal && j * 128 + 127 > t.row0);
+                const int lim = (A.causal ? min(t.len, r + 1) : t.len) - j * 128;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full[b]), uses & 1, gave_up))) break;
+                ++uses;
+                tmem_after();
+#pragma unroll
+                for (int c = 0; c < 128; c += 32) {
+                    u32 dp[32];
+                    tmem_load32(td + c, dp);
+                    tmem_loaded();
+                    float ds[32];
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) ds[x] = __uint_as_float(s[c + x]) * (__uint_as_float(dp[x]) - st.y);
+                    if (edge) {
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) ds[x] = c + x < lim ? ds[x] : 0.0f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[c / 2 + x] = rp_pair(ds[2 * x], ds[2 * x + 1], X());
+                }
+                tmem_before();
+                bar_arrive(rp_smem(&sm.dp_empty));
+                tmem_store32(ts, s);
+                tmem_store32(ts + 32, s + 32);
+                tmem_stored();
+                tmem_before();
+                bar_arrive(rp_smem(&sm.ds_full[b]));
+            }
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
+            tmem_after();
+            // each group hands over one half of the columns
+            X *out = (X *)A.x[0] + (t.base + r) * A.token[0] + h * A.hd[0] + b * (D / 2);
+            store_row<X, D / 2>(tm + lanes + 384 + b * (D / 2), out, A.d - b * (D / 2), r < t.len, ok ? A.scale : NAN);
+            tmem_before();
+            bar_arrive(rp_smem(&sm.acc_empty));
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
+    if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);
+}
+
+// ---------------------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------------------
+// Workspace: front and items of the keys' kernel, the same of the queries', statistics.
+static i64 plan_bytes(i64 T, int N) { return ((i64)sizeof(AttendHead) + 8 * (T / 128 + N) + 15) / 16 * 16; }
+
+extern "C" int64_t rp_attend_grad_workspace(const rp_attend_config *a, int64_t n_tokens, int32_t n_samples)
+{
+    if (rp_attend_check(a, n_tokens, n_samples) != RP_OK) return 0;
+    return 2 * plan_bytes(n_tokens, n_samples) + 8 * n_tokens * a->q_heads;
+}
+
+struct GradMaps { CUtensorMap q64, q, k, v, g64, g; };
+
+template <typename X, int D>
+static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most, int sms, cudaStream_t stream)
+{
+    const size_t sk = sizeof(KeySmem<D>) + 1024, sq = sizeof(QuerySmem<D>) + 1024;
+    RP_CUDA(cudaFuncSetAttribute(k_attend_keys<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sk));
+    RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
+    k_attend_keys<X, D><<<(int)std::min((i64)sms, most * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q64, M.k, M.v, M.g64, keys);
+    RP_TRY(rp_op_launched());
+    k_attend_queries<X, D><<<(int)std::min((i64)sms, most * keys.Hq), ATTEND_THREADS, sq, stream>>>(M.q, M.k, M.v, M.g, queries);
+    return rp_op_launched();
+}
+
+extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const rp_view *out,
+                              const rp_view *lse, const rp_view *out_grad, const int64_t *start, int32_t n_samples, const rp_view *q_grad,
+                              const rp_view *k_grad, const rp_view *v_grad, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    RP_TRY(rp_attend_check(a, n_tokens, n_samples));
+    if (!start || !rp_aligned(start, 8) || !workspace || !rp_aligned(workspace, 16) || workspace_bytes < rp_attend_grad_workspace(a, n_tokens, n_samples)) return RP_ERR_ARG;
+    if (!lse || !lse->x || !rp_aligned(lse->x, 4)) return RP_ERR_ARG;
+    if (n_tokens == 0) return RP_OK;
+    RpOpDevice dev;
+    const rp_view *by_q[4] = { q, out, out_grad, q_grad }, *by_k[4] = { k, v, k_grad, v_grad };
+    for (int i = 0; i < 4; ++i) {
+        RP_TRY(rp_attend_view(by_q[i], n_tokens, a->q_heads, dev));
+        RP_TRY(rp_attend_view(by_k[i], n_tokens, a->kv_heads, dev));
+    }
+    RP_TRY(rp_op_enter(dev, start, workspace, lse->x));
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    const i64 T = n_tokens, plan = plan_bytes(T, n_samples);
+    AttendHead *head[2] = { (AttendHead *)workspace, (AttendHead *)((char *)workspace + plan) };
+    float2 *stats = (float2 *)((char *)workspace + 2 * plan);
+    const int d = a->head_dim, Hq = a->q_heads, Hk = a->kv_heads;
+    GradMaps M;
+    RP_TRY(rp_tensor_map(&M.q64, a->type, q->x, T, Hq, d, q->token, q->head, 64));
+    RP_TRY(rp_tensor_map(&M.q, a->type, q->x, T, Hq, d, q->token, q->head, 128));
+    RP_TRY(rp_tensor_map(&M.k, a->type, k->x, T, Hk, d, k->token, k->head, 128));
+    RP_TRY(rp_tensor_map(&M.v, a->type, v->x, T, Hk, d, v->token, v->head, 128));
+    RP_TRY(rp_tensor_map(&M.g64, a->type, out_grad->x, T, Hq, d, out_grad->token, out_grad->head, 64));
+    RP_TRY(rp_tensor_map(&M.g, a->type, out_grad->x, T, Hq, d, out_grad->token, out_grad->head, 128));
+    AttendPlan P = {};
+    P.start = (const i64 *)start; P.T = T; P.N = n_samples; P.rows = 128; P.causal = a->causal; P.most = (int)(T / 128 + n_samples);
+    GradArgs G[2];
+    for (int w = 0; w < 2; ++w) {
+        P.by_key = w == 0; P.head = head[w]; P.items = (int2 *)(head[w] + 1); P.n_clear = 0;
+        if (w == 0) {
+            P.clear[P.n_clear++] = { k_grad->x, k_grad->token, k_grad->head, Hk, d, 2 };
+            P.clear[P.n_clear++] = { v_grad->x, v_grad->token, v_grad->head, Hk, d, 2 };
+        } else
+            P.clear[P.n_clear++] = { q_grad->x, q_grad->token, q_grad->head, Hq, d, 2 };
+        RP_TRY(rp_launch_attend_plan(P, stream));
+        GradArgs &A = G[w];
+        A = GradArgs();
+        A.items = P.items; A.head = head[w]; A.start = (const i64 *)start; A.T = T; A.Hq = Hq; A.Hk = Hk; A.share = Hq / Hk; A.d = d; A.causal = a->causal;
+        A.scale = a->scale; A.stats = stats; A.status = &head[0]->status;
+    }
+    G[0].x[0] = v_grad->x; G[0].token[0] = v_grad->token; G[0].hd[0] = v_grad->head;
+    G[0].x[1] = k_grad->x; G[0].token[1] = k_grad->token; G[0].hd[1] = k_grad->head;
+    G[1].x[0] = q_grad->x; G[1].token[0] = q_grad->token; G[1].hd[0] = q_grad->head;
+    const int sms = rp_op_sms(dev.device);
+    const int ctas = (int)std::min((T * Hq + 15) / 16, (i64)sms * 8);
+    if (a->type == RP_F16)
+        k_attend_stats<__half><<<ctas, 256, 0, stream>>>(T, Hq, d, (const __half *)out->x, out->token, out->head, (const __half *)out_grad->x, out_grad->token, out_grad->head,
+                                                         (const float *)lse->x, lse->token, lse->head, stats);
+    else
+        k_attend_stats<bf16><<<ctas, 256, 0, stream>>>(T, Hq, d, (const bf16 *)out->x, out->token, out->head, (const bf16 *)out_grad->x, out_grad->token, out_grad->head,
+                                                       (const float *)lse->x, lse->token, lse->head, stats);
+    RP_TRY(rp_op_launched());
+    if (a->type == RP_F16) return d <= 64 ? launch<__half, 64>(M, G[0], G[1], P.most, sms, stream) : launch<__half, 128>(M, G[0], G[1], P.most, sms, stream);
+    return d <= 64 ? launch<bf16, 64>(M, G[0], G[1], P.most, sms, stream) : launch<bf16, 128>(M, G[0], G[1], P.most, sms, stream);
+}

@@ -30,7 +30,7 @@ __device__ __forceinline__ u64 rp_nanoseconds()
 }
 // Waits for the end of a barrier's phase, two seconds at most (a step of these kernels takes microseconds): false when they ran out.  `gave_up` is the CTA's
 // word for it: whoever waits longer than that sets it, and all others stop waiting when they see it.
-__device__ __noinline__ bool bar_wait_long(u32 bar, u32 parity, volatile int *gave_up)
+__device__ __forceinline__ bool bar_wait_long(u32 bar, u32 parity, volatile int *gave_up)
 {
     const u64 since = rp_nanoseconds();
     for (u32 n = 0;; ++n) {

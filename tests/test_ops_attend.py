@@ -151,3 +151,137 @@ def test_no_tokens():
     q = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
     out, lse = rp.rp_attend(q, q, q, torch.tensor([0, 0], device="cuda"))
     assert out.shape == (0, 2, 64) and lse.shape == (0, 2)
+
+
+# ---- gradient ---------------------------------------------------------------------------
+def gradients(q, k, v, do, scale, causal):
+    """Gradients of one sample and head in 64 bits, and the sums of magnitudes that their roundings go by."""
+    p, _ = weights(q, k, scale, causal)
+    o = p @ v
+    dp = do @ v.T
+    delta = (do * o).sum(1, keepdim=True)
+    ds = p * (dp - delta)
+    # ds is off by its own rounding, and by what o's rounding does to delta
+    slip = p * (do * o).abs().sum(1, keepdim=True)
+    return (ds @ k * scale, ds.T @ q * scale, p.T @ do), (ds.abs() @ k.abs() * scale, ds.abs().T @ q.abs() * scale, p.T @ do.abs()), \
+        (slip @ k.abs() * scale, slip.T @ q.abs() * scale, 0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind,extra", [("bfloat16", 0), ("float16", 8)])
+@pytest.mark.parametrize("shape", SHAPES, ids=[str(s[:4]) for s in SHAPES])
+def test_gradient(shape, kind, extra, causal):
+    import torch
+    T, hq, hk, d, start = shape
+    q, k, v, g = inputs(shape, kind, extra)
+    st, scale, share = torch.tensor(start, device="cuda"), 0.2, hq // hk
+    do = torch.randn(hq, T, d + 8, generator=g).to(q.dtype).cuda()[:, :, :d].transpose(0, 1)
+    out, lse = rp.rp_attend(q, k, v, st, causal=causal, scale=scale)
+    got = rp.rp_attend_grad(do, q, k, v, out, lse, st, causal=causal, scale=scale)
+    half = torch.finfo(q.dtype).eps / 2
+    seen = torch.zeros(T, dtype=torch.bool)
+    for lo, hi in samples(start, T):
+        seen[lo:hi] = True
+        want, size, slip = [[torch.zeros(hi - lo, n, d, dtype=torch.float64, device="cuda") for n in (hq, hk, hk)] for _ in range(3)]
+        for h in range(hq):
+            a = [x[lo:hi, h // n].double() for x, n in ((q, 1), (k, share), (v, share), (do, 1))]
+            for to, parts in zip((want, size, slip), gradients(*a, scale, causal)):
+                for i, n in enumerate((1, share, share)):
+                    to[i][:, h // n] += parts[i]
+        for x, w, s, e in zip(got, want, size, slip):
+            # each weight (or gradient of a score) and the result rounded once, delta by the rounding of o; 32 bits: 1e-5 of the weights;
+            # float16 numbers of less than 2^-14 are off by 2^-25 at most, in up to T terms of |x| <= 6
+            tol = half * (s + w.abs() + e) + 2e-5 * (s + e) + (1e-7 + 2.0 ** -25 * 6 * (hi - lo) * share * (kind == "float16"))
+            assert ((x[lo:hi].double() - w).abs() <= tol).all()
+    for x in got:
+        assert x.dtype == q.dtype and (x[~seen.cuda()] == 0).all()
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences():
+    import torch
+    T, start = 10, [0, 4, 10]
+    g = torch.Generator().manual_seed(8)
+    q, k, v, do = [(torch.randn(T, 2 if i in (0, 3) else 1, 16, generator=g) * 0.5).half() for i in range(4)]
+    st = torch.tensor(start, device="cuda")
+    dev = [x.cuda() for x in (q, k, v)]
+    out, lse = rp.rp_attend(*dev, st)
+    got = rp.rp_attend_grad(do.cuda(), *dev, out, lse, st)
+
+    def value(q, k, v):
+        total = 0.0
+        for lo, hi in samples(start, T):
+            for h in range(2):
+                p, _ = weights(q[lo:hi, h], k[lo:hi, 0], 0.25, True)
+                total += (p @ v[lo:hi, 0] * do[lo:hi, h].double()).sum().item()
+        return total
+    leaves = [x.double() for x in (q, k, v)]
+    for i, x in enumerate(leaves):
+        for at in [(0, 0, 0), (3, 0, 5), (4, 0, 15), (9, 0, 7)] + ([(9, 1, 2)] if i == 0 else []):
+            up, down = [y.clone() for y in leaves], [y.clone() for y in leaves]
+            up[i][at] += 1e-4
+            down[i][at] -= 1e-4
+            # (roundings of float16, 2^-11 each of sums of a few terms below 2)
+            assert abs((value(*up) - value(*down)) / 2e-4 - got[i][at].item()) < 4e-3
+
+
+@pytest.mark.gpu
+def test_gradients_of_other_samples_do_not_matter():
+    import torch
+    shape = (400, 4, 2, 64, [0, 70, 211, 330])
+    st = torch.tensor(shape[4], device="cuda")
+    q, k, v, g = inputs(shape, "bfloat16")
+    do = torch.randn(400, 4, 64, generator=g).bfloat16().cuda()
+    out, lse = rp.rp_attend(q, k, v, st)
+    want = rp.rp_attend_grad(do, q, k, v, out, lse, st)
+    bad = [x.clone() for x in (do, q, k, v, out, lse)]
+    for x in bad:
+        x[:70] = float("nan")
+        x[211:300] = float("inf")
+        x[330:] = float("nan")
+    big = [torch.full((405, n, 64), 3.0, dtype=torch.bfloat16, device="cuda") for n in (4, 2, 2)]
+    rp.rp_attend_grad(*bad, st, q_grad=big[0][:400], k_grad=big[1][:400], v_grad=big[2][:400])
+    for x, w in zip(big, want):
+        assert (x[70:211] == w[70:211]).all() and (x[330:400] == 0).all() and (x[400:] == 3).all()
+
+
+@pytest.mark.gpu
+def test_repeated_streamed_and_captured_gradients_agree_bit_for_bit():
+    import torch
+    shape = (3000, 8, 2, 128, [0, 500, 501, 3000])
+    q, k, v, g = inputs(shape, "bfloat16")
+    st = torch.tensor(shape[4], device="cuda")
+    do = torch.randn(3000, 8, 128, generator=g).bfloat16().cuda()
+    out, lse = rp.rp_attend(q, k, v, st)
+    want = rp.rp_attend_grad(do, q, k, v, out, lse, st)
+    torch.cuda.synchronize()
+    results = [rp.rp_attend_grad(do, q, k, v, out, lse, st, stream=s) for s in [torch.cuda.Stream() for _ in range(4)] for _ in range(3)]
+    torch.cuda.synchronize()
+    for got in results:
+        assert all((a == b).all() for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, l = rp.rp_attend(q, k, v, st)
+        got = rp.rp_attend_grad(do, q, k, v, o, l, st)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all((a == b).all() for a, b in zip(got, want))
+
+
+def test_refusals_of_the_gradient():
+    lib = rp.lib()
+    buf = np.zeros(4096, np.float64)
+    p = (buf.ctypes.data + 15) // 16 * 16
+    cfg = rp.rp_attend_config(2, 1, 64, 2, 1, 0.1)
+    ok, bad = C.byref(rp.rp_view(p, 128, 64)), C.byref(rp.rp_view(p, 100, 64))
+
+    def call(at=None, lse=ok, nbytes=1 << 14, space=p):
+        views = [ok] * 8
+        if at is not None:
+            views[at] = bad
+        q, k, v, o, g, dq, dk, dv = views
+        return lib.rp_attend_grad(C.byref(cfg), 2, q, k, v, o, lse, g, p, 1, dq, dk, dv, space, nbytes, None)
+    assert call() == -1 and all(call(at=i) == -1 for i in range(8)) and call(lse=None) == -1 and call(nbytes=16) == -1 and call(space=None) == -1
+    assert lib.rp_attend_grad_workspace(None, 1, 1) == 0 and lib.rp_attend_grad_workspace(C.byref(cfg), 100, 1) >= 100 * 2 * 8
