@@ -64,6 +64,18 @@ template <typename X> __device__ __forceinline__ float weight_at(const RotArgs &
     return A.w32 ? ((const float *)w)[i] : rp_float(((const X *)w)[i]);
 }
 
+// Turns the pairs of a lane's two pieces, or turns them back: (a[p], b[p]), or neighbours in a and then in b.
+template <bool INTERLEAVED, bool BACK> __device__ __forceinline__ void turn(float *a, float *b, const float *c, const float *s)
+{
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        float &x = !INTERLEAVED ? a[p] : p < 4 ? a[2 * p] : b[2 * p - 8], &y = !INTERLEAVED ? b[p] : p < 4 ? a[2 * p + 1] : b[2 * p - 7];
+        const float sn = BACK ? -s[p] : s[p], was = x;
+        x = was * c[p] - y * sn;
+        y = was * sn + y * c[p];
+    }
+}
+
 // Any head size and alignment: a warp takes one head after the other, a lane the pairs lane, lane + 32, .. and then the elements behind them.
 // GRAD: y receives the gradient of x.
 template <typename X, bool GRAD>
@@ -164,6 +176,157 @@ __global__ void __launch_bounds__(ROT_THREADS) k_rotate_any(RotArgs A)
     }
 }
 
+// Heads of whole 16-byte pieces.  A head belongs to TPH neighbouring lanes of a warp with two pieces of eight elements each: those that are turned into one another
+// (half layout) or neighbours, so that a lane has all pairs that it needs and the mean of squares is a few shuffles.  A warp takes ROT_CHUNK tokens at a time:
+// their sines and cosines go to shared memory once, for all heads; then it goes through the heads of the queries, then of the keys, with the weights (and the sums for
+// their gradients) in registers.  STEPS heads' loads are issued before any is worked on.
+#define ROT_CHUNK 4
+template <typename X, int TPH, bool INTERLEAVED, bool GRAD>
+__global__ void __launch_bounds__(ROT_THREADS, GRAD ? 2 : 3) k_rotate_rows(RotArgs A)
+{
+    constexpr int NG = 32 / TPH, STEPS = 2;              // heads of a warp at a time; how many of them in flight
+    extern __shared__ float2 table[];                    // [warps][ROT_CHUNK][r / 2], then (GRAD) the CTA's weight gradients [warps][2][d]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pairs = A.r / 2, j = lane % TPH, group = lane / TPH;
+    float2 *cs = table + warp * ROT_CHUNK * pairs;
+    float *dw = (float *)(table + ROT_WARPS * ROT_CHUNK * pairs) + warp * 2 * A.d;
+    if (GRAD && A.part)
+        for (int i = lane; i < 2 * A.d; i += 32) dw[i] = 0.0f;
+    __syncwarp();
+    const bool mine = 16 * j < A.d;
+    const int turned = A.r / 16;                         // half layout: pieces of a half
+    const int pa = INTERLEAVED ? 16 * j : j < turned ? 8 * j : A.r + 16 * (j - turned);          // first elements of the lane's pieces
+    const int pb = INTERLEAVED || j >= turned ? pa + 8 : pa + A.r / 2;
+    const i64 unit = (i64)blockIdx.x * ROT_WARPS + warp;
+    const i64 t0 = unit / A.parts * A.run, t1 = min(A.T, t0 + A.run);
+    const int share = (int)(unit % A.parts);
+    Place at;
+    at.next = INT64_MIN;
+    for (i64 c0 = t0; c0 < t1; c0 += ROT_CHUNK) {
+        const int n = (int)min((i64)ROT_CHUNK, t1 - c0);
+        u32 held = 0;
+        __syncwarp();
+        for (int i = 0; i < n; ++i) {
+            if (c0 + i >= at.next) at.find(A, c0 + i);
+            held |= (at.held ? 1u : 0u) << i;
+            for (int p = lane; p < pairs; p += 32) cs[i * pairs + p] = turn_of(A, c0 + i + at.base, p);
+        }
+        __syncwarp();
+        int before = 0;                                  // steps of the tensor before
+        for (int which = 0; which < 2; ++which) {
+            const RotTensor &H = A.h[which];
+            const int steps = (H.heads + NG - 1) / NG;
+            const bool norm = H.w != nullptr;
+            float wa[8], wb[8], da[8], db[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                wa[i] = norm && mine ? weight_at<X>(A, H.w, pa + i) : 1.0f;
+                wb[i] = norm && mine ? weight_at<X>(A, H.w, pb + i) : 1.0f;
+                if (GRAD) { da[i] = 0.0f; db[i] = 0.0f; }
+            }
+            // a step's warps go by its number in both tensors
+            const int first = A.parts == 1 ? 0 : ((share - before) % A.parts + A.parts) % A.parts;
+            before += steps;
+            for (int i = 0; i < n; ++i) {
+                const i64 t = c0 + i;
+                float c[8], s[8];
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                    float2 v = make_float2(1.0f, 0.0f);
+                    if (8 * j + p < pairs) v = cs[i * pairs + 8 * j + p];
+                    c[p] = v.x; s[p] = v.y;
+                }
+                const bool there = held >> i & 1;
+                for (int st = first; st < steps; st += A.parts * STEPS) {
+                    Pack8<X> xa[STEPS], xb[STEPS], ga[STEPS], gb[STEPS];
+                    bool ok[STEPS];
+#pragma unroll
+                    for (int u = 0; u < STEPS; ++u) {
+                        const int head = (st + u * A.parts) * NG + group;
+                        ok[u] = mine && st + u * A.parts < steps && head < H.heads;
+                        xa[u] = Pack8<X>(); xb[u] = Pack8<X>(); ga[u] = Pack8<X>(); gb[u] = Pack8<X>();
+                        if (ok[u] && there) {
+                            if (!GRAD || norm) {
+                                const X *x = (const X *)H.x + t * H.x_token + head * H.x_head;
+                                xa[u] = rp_load8(x + pa); xb[u] = rp_load8(x + pb);
+                            }
+                            if (GRAD) {
+                                const X *g = (const X *)H.dy + t * H.g_token + head * H.g_head;
+                                ga[u] = rp_load8(g + pa); gb[u] = rp_load8(g + pb);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < STEPS; ++u) {
+                        float a[8], b[8];
+                        rp_open8(xa[u], a); rp_open8(xb[u], b);
+                        float r = 1.0f;
+                        if (norm) {
+                            float sum = 0.0f;
+#pragma unroll
+                            for (int p = 0; p < 8; ++p) sum = fmaf(a[p], a[p], fmaf(b[p], b[p], sum));
+#pragma unroll
+                            for (int o = 1; o < TPH; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                            r = rsqrtf(sum / A.d + A.eps);
+                        }
+                        if (!GRAD) {
+#pragma unroll
+                            for (int p = 0; p < 8; ++p) { a[p] *= r * wa[p]; b[p] *= r * wb[p]; }
+                        } else {
+                            float g[8], h[8];
+                            rp_open8(ga[u], g); rp_open8(gb[u], h);
+                            turn<INTERLEAVED, true>(g, h, c, s);
+                            if (norm) {
+                                float dot = 0.0f;
+#pragma unroll
+                                for (int p = 0; p < 8; ++p) {
+                                    a[p] *= r; b[p] *= r;
+                                    da[p] = fmaf(g[p], a[p], da[p]); db[p] = fmaf(h[p], b[p], db[p]);
+                                    g[p] *= wa[p]; h[p] *= wb[p];
+                                    dot = fmaf(g[p], a[p], fmaf(h[p], b[p], dot));
+                                }
+#pragma unroll
+                                for (int o = 1; o < TPH; o <<= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                                dot /= A.d;
+#pragma unroll
+                                for (int p = 0; p < 8; ++p) { g[p] = r * (g[p] - a[p] * dot); h[p] = r * (h[p] - b[p] * dot); }
+                            }
+#pragma unroll
+                            for (int p = 0; p < 8; ++p) { a[p] = g[p]; b[p] = h[p]; }
+                        }
+                        if (!GRAD) turn<INTERLEAVED, false>(a, b, c, s);
+                        if (ok[u]) {
+                            X *y = (X *)H.y + t * H.y_token + ((st + u * A.parts) * NG + group) * H.y_head;
+                            if (!there) {
+#pragma unroll
+                                for (int p = 0; p < 8; ++p) { a[p] = 0.0f; b[p] = 0.0f; }
+                            }
+                            rp_store8(y + pa, rp_close8<X>(a));
+                            rp_store8(y + pb, rp_close8<X>(b));
+                        }
+                    }
+                }
+            }
+            if (GRAD && norm && A.part) {
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+#pragma unroll
+                    for (int o = TPH; o < 32; o <<= 1) { da[p] += __shfl_xor_sync(0xffffffffu, da[p], o); db[p] += __shfl_xor_sync(0xffffffffu, db[p], o); }
+                    if (group == 0 && mine) { dw[which * A.d + pa + p] += da[p]; dw[which * A.d + pb + p] += db[p]; }
+                }
+            }
+        }
+    }
+    if (GRAD && A.part) {
+        __syncthreads();
+        const float *from = (const float *)(table + ROT_WARPS * ROT_CHUNK * pairs);
+        for (int i = threadIdx.x; i < 2 * A.d; i += ROT_THREADS) {
+            float sum = 0.0f;
+            for (int w = 0; w < ROT_WARPS; ++w) sum += from[w * 2 * A.d + i];
+            A.part[(i64)blockIdx.x * 2 * A.d + i] = sum;
+        }
+    }
+}
+
 // Weights' gradients: the CTAs' partial sums, added up in 64 bits in their order.  32 columns a CTA, every warp takes a stretch of CTAs.
 __global__ void __launch_bounds__(1024) k_rotate_weights(RotArgs A, int ctas)
 {
@@ -185,7 +348,7 @@ __global__ void __launch_bounds__(1024) k_rotate_weights(RotArgs A, int ctas)
 // ---------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------
-#define ROT_MAX_CTAS 1184                // CTAs of the gradient, at most (8 on each of 148 SMs): what the workspace is sized for
+#define ROT_MAX_CTAS 1184                // CTAs at most (8 on each of 148 SMs): what the workspace is sized for
 
 static int check_heads(const rp_rotary *r, const rp_heads *h, bool grad, RpOpDevice &dev)
 {
@@ -208,6 +371,23 @@ static void take_heads(RotTensor &o, const rp_heads *h, bool grad)
     o.x = h->x; o.x_token = h->x_token; o.x_head = h->x_head; o.y = h->y; o.y_token = h->y_token; o.y_head = h->y_head;
     o.w = h->weight; o.heads = h->n_heads;
     if (grad) { o.dy = h->y_grad; o.g_token = h->g_token; o.g_head = h->g_head; o.dw = h->weight_grad; }
+}
+
+template <typename X, int TPH> static void (*rows_kernel(bool interleaved, bool grad))(RotArgs)
+{
+    if (interleaved) return grad ? k_rotate_rows<X, TPH, true, true> : k_rotate_rows<X, TPH, true, false>;
+    return grad ? k_rotate_rows<X, TPH, false, true> : k_rotate_rows<X, TPH, false, false>;
+}
+template <typename X> static void (*rows_kernel(int tph, bool interleaved, bool grad))(RotArgs)
+{
+    switch (tph) {
+        case 1: return rows_kernel<X, 1>(interleaved, grad);
+        case 2: return rows_kernel<X, 2>(interleaved, grad);
+        case 4: return rows_kernel<X, 4>(interleaved, grad);
+        case 8: return rows_kernel<X, 8>(interleaved, grad);
+        case 16: return rows_kernel<X, 16>(interleaved, grad);
+        default: return rows_kernel<X, 32>(interleaved, grad);
+    }
 }
 
 static int rotate(const rp_rotary *r, i64 T, const double *freq, const i64 *start, int N, const i64 *first, const rp_heads *q, const rp_heads *k,
@@ -238,20 +418,32 @@ static int rotate(const rp_rotary *r, i64 T, const double *freq, const i64 *star
             if (A.h[w].dw) RP_CUDA(cudaMemsetAsync(A.h[w].dw, 0, sizeof(float) * A.d, stream));
         return RP_OK;
     }
-    const i64 warps = std::min((i64)ROT_MAX_CTAS, (i64)rp_op_sms(dev.device) * 8) * ROT_WARPS;
-    A.parts = T >= warps ? 1 : (int)std::min((i64)all, warps / T);
-    const i64 lanes = warps / A.parts;
-    A.run = (T + lanes - 1) / lanes;
+    // Heads of whole pieces, all rows on 16-byte boundaries (measured on 32768 tokens of 32 + 8 heads of 128, 16 bits: see the kernels)
+    bool pieces = A.d % 16 == 0 && A.d <= 512 && (A.half ? A.r % 16 == 0 : A.r % 8 == 0);
+    for (int w = 0; w < 2; ++w) {
+        const RotTensor &H = A.h[w];
+        if (!H.heads) continue;
+        const int e = 16 / rp_type_bytes(r->type);
+        pieces = pieces && rp_aligned(H.x, 16) && rp_aligned(H.y, 16) && rp_aligned(H.dy, 16) && H.x_token % e == 0 && H.x_head % e == 0 && H.y_token % e == 0 &&
+                 H.y_head % e == 0 && H.g_token % e == 0 && H.g_head % e == 0;
+    }
+    int tph = 1;
+    while (16 * tph < A.d) tph <<= 1;
+    // tokens and parts of their heads a warp: enough warps for all SMs, several rounds of them where there are many
+    const int ng = pieces ? 32 / tph : 1, steps = (A.h[0].heads + ng - 1) / ng + (A.h[1].heads + ng - 1) / ng;
+    const i64 most = (i64)ROT_MAX_CTAS * ROT_WARPS;
+    A.parts = (int)std::max((i64)1, std::min((i64)steps, most / 2 / T));
+    const i64 lanes = most / A.parts;
+    A.run = std::max((T + lanes - 1) / lanes, std::min((i64)ROT_CHUNK, T * A.parts / (most / 2) + 1));
     const i64 units = (T + A.run - 1) / A.run * A.parts;
     const int ctas = (int)((units + ROT_WARPS - 1) / ROT_WARPS);
-    const size_t smem = ROT_WARPS * (A.r / 2 * sizeof(float2) + (A.part ? 2 * A.d * sizeof(float) : 0));
-    if (grad) {
-        RP_FOR_TYPE(r->type, {
-            if (smem > 48 * 1024) RP_CUDA(cudaFuncSetAttribute(k_rotate_any<X, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, RP_SMEM_LIMIT));
-            k_rotate_any<X, true><<<ctas, ROT_THREADS, smem, stream>>>(A);
-        });
-    } else
-        RP_FOR_TYPE(r->type, (k_rotate_any<X, false><<<ctas, ROT_THREADS, smem, stream>>>(A)));
+    const size_t smem = ROT_WARPS * ((pieces ? ROT_CHUNK : 1) * (A.r / 2) * sizeof(float2) + (A.part ? 2 * A.d * sizeof(float) : 0));
+    RP_FOR_TYPE(r->type, {
+        void (*f)(RotArgs) = grad ? k_rotate_any<X, true> : k_rotate_any<X, false>;
+        if (pieces) f = rows_kernel<X>(tph, !A.half, grad);
+        if (smem > 48 * 1024) RP_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, RP_SMEM_LIMIT));
+        f<<<ctas, ROT_THREADS, smem, stream>>>(A);
+    });
     RP_TRY(rp_op_launched());
     if (A.part) {
         k_rotate_weights<<<(2 * A.d + 31) / 32, 1024, 0, stream>>>(A, ctas);
