@@ -28,7 +28,7 @@ struct RotTensor {
 struct RotArgs {
     RotTensor h[2];         // queries, keys
     int d, r, half, w32;    // head_dim, rotary_dim, half layout, weights in 32 bits
-    float eps, mscale;
+    float eps, mscale, inv_d;               // inv_d: 1 / head_dim
     i64 T, run;             // run: tokens of a warp
     int parts;              // a token's heads are dealt out to this many warps
     const double *freq;
@@ -178,27 +178,35 @@ __global__ void __launch_bounds__(ROT_THREADS) k_rotate_any(RotArgs A)
 
 // Heads of whole 16-byte pieces.  A head belongs to TPH neighbouring lanes of a warp with two pieces of eight elements each: those that are turned into one another
 // (half layout) or neighbours, so that a lane has all pairs that it needs and the mean of squares is a few shuffles.  A warp takes ROT_CHUNK tokens at a time:
-// their sines and cosines go to shared memory once, for all heads; then it goes through the heads of the queries, then of the keys, with the weights (and the sums for
-// their gradients) in registers.  STEPS heads' loads are issued before any is worked on.
+// their sines and cosines go to shared memory once, for all heads; then it goes through the heads of the queries, then of the keys, with a token's factors (and the
+// sums for the weights' gradients) in registers.  The loads of two steps are issued before either is worked on.
 #define ROT_CHUNK 4
+#define ROT_CTAS(GRAD) ((GRAD) ? 2 : 3)                  // resident on an SM
 template <typename X, int TPH, bool INTERLEAVED, bool GRAD>
-__global__ void __launch_bounds__(ROT_THREADS, GRAD ? 2 : 3) k_rotate_rows(RotArgs A)
+__global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(RotArgs A)
 {
     constexpr int NG = 32 / TPH, STEPS = 2;              // heads of a warp at a time; how many of them in flight
-    extern __shared__ float2 table[];                    // [warps][ROT_CHUNK][r / 2], then (GRAD) the CTA's weight gradients [warps][2][d]
+    constexpr int ROW = 8 * TPH;                         // pairs of a token in the table; those that are not turned have an angle of 0
+    extern __shared__ __align__(16) float2 table[];      // [warps][ROT_CHUNK][ROW], weights [2][16 TPH] in 32 bits, (GRAD) their gradients [warps][2][d]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pairs = A.r / 2, j = lane % TPH, group = lane / TPH;
-    float2 *cs = table + warp * ROT_CHUNK * pairs;
-    float *dw = (float *)(table + ROT_WARPS * ROT_CHUNK * pairs) + warp * 2 * A.d;
-    if (GRAD && A.part)
-        for (int i = lane; i < 2 * A.d; i += 32) dw[i] = 0.0f;
-    __syncwarp();
+    float2 *cs = table + warp * ROT_CHUNK * ROW;
+    float *weights = (float *)(table + ROT_WARPS * ROT_CHUNK * ROW), *dw = weights + 2 * 16 * TPH + warp * 2 * A.d;
     const bool mine = 16 * j < A.d;
     const int turned = A.r / 16;                         // half layout: pieces of a half
     const int pa = INTERLEAVED ? 16 * j : j < turned ? 8 * j : A.r + 16 * (j - turned);          // first elements of the lane's pieces
     const int pb = INTERLEAVED || j >= turned ? pa + 8 : pa + A.r / 2;
-    const i64 unit = (i64)blockIdx.x * ROT_WARPS + warp;
-    const i64 t0 = unit / A.parts * A.run, t1 = min(A.T, t0 + A.run);
-    const int share = (int)(unit % A.parts);
+    if (GRAD && A.part)
+        for (int i = lane; i < 2 * A.d; i += 32) dw[i] = 0.0f;
+    if (warp < 2 && group == 0) {
+        const RotTensor &H = A.h[warp];                  // in the lanes' order
+        for (int i = 0; i < 8; ++i) {
+            weights[warp * 16 * TPH + 16 * j + i] = H.w && mine ? weight_at<X>(A, H.w, pa + i) : 1.0f;
+            weights[warp * 16 * TPH + 16 * j + 8 + i] = H.w && mine ? weight_at<X>(A, H.w, pb + i) : 1.0f;
+        }
+    }
+    __syncthreads();
+    const int unit = blockIdx.x * ROT_WARPS + warp, lanes = gridDim.x * ROT_WARPS / A.parts, share = unit % A.parts;
+    const i64 t0 = unit / A.parts < lanes ? A.T * (unit / A.parts) / lanes : A.T, t1 = unit / A.parts < lanes ? A.T * (unit / A.parts + 1) / lanes : A.T;
     Place at;
     at.next = INT64_MIN;
     for (i64 c0 = t0; c0 < t1; c0 += ROT_CHUNK) {
@@ -208,52 +216,49 @@ __global__ void __launch_bounds__(ROT_THREADS, GRAD ? 2 : 3) k_rotate_rows(RotAr
         for (int i = 0; i < n; ++i) {
             if (c0 + i >= at.next) at.find(A, c0 + i);
             held |= (at.held ? 1u : 0u) << i;
-            for (int p = lane; p < pairs; p += 32) cs[i * pairs + p] = turn_of(A, c0 + i + at.base, p);
+            for (int p = lane; p < ROW; p += 32) cs[i * ROW + p] = p < pairs ? turn_of(A, c0 + i + at.base, p) : make_float2(1.0f, 0.0f);
         }
         __syncwarp();
         int before = 0;                                  // steps of the tensor before
         for (int which = 0; which < 2; ++which) {
             const RotTensor &H = A.h[which];
             const int steps = (H.heads + NG - 1) / NG;
-            const bool norm = H.w != nullptr;
-            float wa[8], wb[8], da[8], db[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                wa[i] = norm && mine ? weight_at<X>(A, H.w, pa + i) : 1.0f;
-                wb[i] = norm && mine ? weight_at<X>(A, H.w, pb + i) : 1.0f;
-                if (GRAD) { da[i] = 0.0f; db[i] = 0.0f; }
-            }
-            // a step's warps go by its number in both tensors
+            // a step's warp goes by its number in both tensors
             const int first = A.parts == 1 ? 0 : ((share - before) % A.parts + A.parts) % A.parts;
             before += steps;
+            if (first >= steps) continue;
+            const bool norm = H.w != nullptr;
+            const int head0 = first * NG + group, head_step = A.parts * NG;
+            float da[8], db[8];
+            if (GRAD) {
+#pragma unroll
+                for (int p = 0; p < 8; ++p) { da[p] = 0.0f; db[p] = 0.0f; }
+            }
             for (int i = 0; i < n; ++i) {
                 const i64 t = c0 + i;
                 float c[8], s[8];
 #pragma unroll
-                for (int p = 0; p < 8; ++p) {
-                    float2 v = make_float2(1.0f, 0.0f);
-                    if (8 * j + p < pairs) v = cs[i * pairs + 8 * j + p];
-                    c[p] = v.x; s[p] = v.y;
+                for (int p = 0; p < 8; p += 2) {
+                    const float4 v = *(const float4 *)(cs + i * ROW + 8 * j + p);
+                    c[p] = v.x; s[p] = v.y; c[p + 1] = v.z; s[p + 1] = v.w;
                 }
                 const bool there = held >> i & 1;
-                for (int st = first; st < steps; st += A.parts * STEPS) {
+                const X *x = (const X *)H.x + t * H.x_token + head0 * H.x_head, *g = GRAD ? (const X *)H.dy + t * H.g_token + head0 * H.g_head : nullptr;
+                X *y = (X *)H.y + t * H.y_token + head0 * H.y_head;
+                for (int st = first, head = head0; st < steps; st += A.parts * STEPS) {
                     Pack8<X> xa[STEPS], xb[STEPS], ga[STEPS], gb[STEPS];
                     bool ok[STEPS];
 #pragma unroll
                     for (int u = 0; u < STEPS; ++u) {
-                        const int head = (st + u * A.parts) * NG + group;
-                        ok[u] = mine && st + u * A.parts < steps && head < H.heads;
+                        ok[u] = mine && head < H.heads;
                         xa[u] = Pack8<X>(); xb[u] = Pack8<X>(); ga[u] = Pack8<X>(); gb[u] = Pack8<X>();
                         if (ok[u] && there) {
-                            if (!GRAD || norm) {
-                                const X *x = (const X *)H.x + t * H.x_token + head * H.x_head;
-                                xa[u] = rp_load8(x + pa); xb[u] = rp_load8(x + pb);
-                            }
-                            if (GRAD) {
-                                const X *g = (const X *)H.dy + t * H.g_token + head * H.g_head;
-                                ga[u] = rp_load8(g + pa); gb[u] = rp_load8(g + pb);
-                            }
+                            if (!GRAD || norm) { xa[u] = rp_load8(x + pa); xb[u] = rp_load8(x + pb); }
+                            if (GRAD) { ga[u] = rp_load8(g + pa); gb[u] = rp_load8(g + pb); }
                         }
+                        head += head_step;
+                        x += head_step * H.x_head;
+                        if (GRAD) g += head_step * H.g_head;
                     }
 #pragma unroll
                     for (int u = 0; u < STEPS; ++u) {
@@ -266,11 +271,18 @@ __global__ void __launch_bounds__(ROT_THREADS, GRAD ? 2 : 3) k_rotate_rows(RotAr
                             for (int p = 0; p < 8; ++p) sum = fmaf(a[p], a[p], fmaf(b[p], b[p], sum));
 #pragma unroll
                             for (int o = 1; o < TPH; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                            r = rsqrtf(sum / A.d + A.eps);
+                            r = rsqrtf(fmaf(sum, A.inv_d, A.eps));
                         }
+                        const float4 *w = (const float4 *)(weights + which * 16 * TPH + 16 * j);
                         if (!GRAD) {
+                            if (norm)
 #pragma unroll
-                            for (int p = 0; p < 8; ++p) { a[p] *= r * wa[p]; b[p] *= r * wb[p]; }
+                                for (int p = 0; p < 8; p += 4) {
+                                    const float4 v = w[p / 4], z = w[p / 4 + 2];
+                                    a[p] *= r * v.x; a[p + 1] *= r * v.y; a[p + 2] *= r * v.z; a[p + 3] *= r * v.w;
+                                    b[p] *= r * z.x; b[p + 1] *= r * z.y; b[p + 2] *= r * z.z; b[p + 3] *= r * z.w;
+                                }
+                            turn<INTERLEAVED, false>(a, b, c, s);
                         } else {
                             float g[8], h[8];
                             rp_open8(ga[u], g); rp_open8(gb[u], h);
@@ -281,28 +293,33 @@ __global__ void __launch_bounds__(ROT_THREADS, GRAD ? 2 : 3) k_rotate_rows(RotAr
                                 for (int p = 0; p < 8; ++p) {
                                     a[p] *= r; b[p] *= r;
                                     da[p] = fmaf(g[p], a[p], da[p]); db[p] = fmaf(h[p], b[p], db[p]);
-                                    g[p] *= wa[p]; h[p] *= wb[p];
-                                    dot = fmaf(g[p], a[p], fmaf(h[p], b[p], dot));
                                 }
 #pragma unroll
+                                for (int p = 0; p < 8; p += 4) {
+                                    const float4 v = w[p / 4], z = w[p / 4 + 2];
+                                    g[p] *= v.x; g[p + 1] *= v.y; g[p + 2] *= v.z; g[p + 3] *= v.w;
+                                    h[p] *= z.x; h[p + 1] *= z.y; h[p + 2] *= z.z; h[p + 3] *= z.w;
+                                }
+#pragma unroll
+                                for (int p = 0; p < 8; ++p) dot = fmaf(g[p], a[p], fmaf(h[p], b[p], dot));
+#pragma unroll
                                 for (int o = 1; o < TPH; o <<= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                                dot /= A.d;
+                                dot *= A.inv_d;
 #pragma unroll
                                 for (int p = 0; p < 8; ++p) { g[p] = r * (g[p] - a[p] * dot); h[p] = r * (h[p] - b[p] * dot); }
                             }
 #pragma unroll
                             for (int p = 0; p < 8; ++p) { a[p] = g[p]; b[p] = h[p]; }
                         }
-                        if (!GRAD) turn<INTERLEAVED, false>(a, b, c, s);
-                        if (ok[u]) {
-                            X *y = (X *)H.y + t * H.y_token + ((st + u * A.parts) * NG + group) * H.y_head;
-                            if (!there) {
+                        if (!there) {
 #pragma unroll
-                                for (int p = 0; p < 8; ++p) { a[p] = 0.0f; b[p] = 0.0f; }
-                            }
+                            for (int p = 0; p < 8; ++p) { a[p] = 0.0f; b[p] = 0.0f; }
+                        }
+                        if (ok[u]) {
                             rp_store8(y + pa, rp_close8<X>(a));
                             rp_store8(y + pb, rp_close8<X>(b));
                         }
+                        y += head_step * H.y_head;
                     }
                 }
             }
@@ -318,7 +335,7 @@ __global__ void __launch_bounds__(ROT_THREADS, GRAD ? 2 : 3) k_rotate_rows(RotAr
     }
     if (GRAD && A.part) {
         __syncthreads();
-        const float *from = (const float *)(table + ROT_WARPS * ROT_CHUNK * pairs);
+        const float *from = weights + 2 * 16 * TPH;
         for (int i = threadIdx.x; i < 2 * A.d; i += ROT_THREADS) {
             float sum = 0.0f;
             for (int w = 0; w < ROT_WARPS; ++w) sum += from[w * 2 * A.d + i];
@@ -411,7 +428,7 @@ static int rotate(const rp_rotary *r, i64 T, const double *freq, const i64 *star
     const int all = A.h[0].heads + A.h[1].heads;
     if (!all) return RP_ERR_ARG;
     A.d = r->head_dim; A.r = r->rotary_dim; A.half = r->layout == RP_ROTARY_HALF; A.w32 = r->weight_type == RP_F32;
-    A.eps = r->eps; A.mscale = r->mscale; A.T = T; A.freq = freq; A.start = start; A.first = first; A.N = N;
+    A.eps = r->eps; A.mscale = r->mscale; A.inv_d = 1.0f / r->head_dim; A.T = T; A.freq = freq; A.start = start; A.first = first; A.N = N;
     A.part = weights ? workspace : nullptr;
     if (T == 0) {
         for (int w = 0; w < 2; ++w)
@@ -429,15 +446,14 @@ static int rotate(const rp_rotary *r, i64 T, const double *freq, const i64 *star
     }
     int tph = 1;
     while (16 * tph < A.d) tph <<= 1;
-    // tokens and parts of their heads a warp: enough warps for all SMs, several rounds of them where there are many
+    // A CTA's warps share out the tokens, or each token's heads where there are fewer tokens than warps.
     const int ng = pieces ? 32 / tph : 1, steps = (A.h[0].heads + ng - 1) / ng + (A.h[1].heads + ng - 1) / ng;
-    const i64 most = (i64)ROT_MAX_CTAS * ROT_WARPS;
-    A.parts = (int)std::max((i64)1, std::min((i64)steps, most / 2 / T));
-    const i64 lanes = most / A.parts;
-    A.run = std::max((T + lanes - 1) / lanes, std::min((i64)ROT_CHUNK, T * A.parts / (most / 2) + 1));
-    const i64 units = (T + A.run - 1) / A.run * A.parts;
-    const int ctas = (int)((units + ROT_WARPS - 1) / ROT_WARPS);
-    const size_t smem = ROT_WARPS * ((pieces ? ROT_CHUNK : 1) * (A.r / 2) * sizeof(float2) + (A.part ? 2 * A.d * sizeof(float) : 0));
+    const i64 warps = std::min((i64)ROT_MAX_CTAS, (i64)rp_op_sms(dev.device) * (pieces ? ROT_CTAS(grad) : 8)) * ROT_WARPS;
+    A.parts = T >= warps ? 1 : (int)std::min((i64)steps, warps / T);
+    const i64 lanes = std::min(T, warps / A.parts);
+    A.run = (T + lanes - 1) / lanes;
+    const int ctas = (int)((lanes * A.parts + ROT_WARPS - 1) / ROT_WARPS);
+    size_t smem = ROT_WARPS * ((pieces ? ROT_CHUNK * 8 * tph : A.r / 2) * sizeof(float2) + (A.part ? 2 * A.d * sizeof(float) : 0)) + (pieces ? 2 * 16 * tph * sizeof(float) : 0);
     RP_FOR_TYPE(r->type, {
         void (*f)(RotArgs) = grad ? k_rotate_any<X, true> : k_rotate_any<X, false>;
         if (pieces) f = rows_kernel<X>(tph, !A.half, grad);
