@@ -198,11 +198,9 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
     if (GRAD && A.part)
         for (int i = lane; i < 2 * A.d; i += 32) dw[i] = 0.0f;
     if (warp < 2 && group == 0) {
-        const RotTensor &H = A.h[warp];                  // in the lanes' order
-        for (int i = 0; i < 8; ++i) {
-            weights[warp * 16 * TPH + 16 * j + i] = H.w && mine ? weight_at<X>(A, H.w, pa + i) : 1.0f;
-            weights[warp * 16 * TPH + 16 * j + 8 + i] = H.w && mine ? weight_at<X>(A, H.w, pb + i) : 1.0f;
-        }
+        const RotTensor &H = A.h[warp];                  // four of each lane side by side, lane after lane
+        for (int i = 0; i < 16; ++i)
+            weights[warp * 16 * TPH + (i >> 2) * 4 * TPH + 4 * j + (i & 3)] = H.w && mine ? weight_at<X>(A, H.w, i < 8 ? pa + i : pb + i - 8) : 1.0f;
     }
     __syncthreads();
     const int unit = blockIdx.x * ROT_WARPS + warp, lanes = gridDim.x * ROT_WARPS / A.parts, share = unit % A.parts;
@@ -216,7 +214,8 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
         for (int i = 0; i < n; ++i) {
             if (c0 + i >= at.next) at.find(A, c0 + i);
             held |= (at.held ? 1u : 0u) << i;
-            for (int p = lane; p < ROW; p += 32) cs[i * ROW + p] = p < pairs ? turn_of(A, c0 + i + at.base, p) : make_float2(1.0f, 0.0f);
+            for (int p = lane; p < ROW; p += 32)         // (two pairs of each lane side by side, lane after lane: no two of a load's lanes in one bank)
+                cs[i * ROW + ((p & 7) >> 1) * 2 * TPH + (p >> 3) * 2 + (p & 1)] = p < pairs ? turn_of(A, c0 + i + at.base, p) : make_float2(1.0f, 0.0f);
         }
         __syncwarp();
         int before = 0;                                  // steps of the tensor before
@@ -239,7 +238,7 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
                 float c[8], s[8];
 #pragma unroll
                 for (int p = 0; p < 8; p += 2) {
-                    const float4 v = *(const float4 *)(cs + i * ROW + 8 * j + p);
+                    const float4 v = *(const float4 *)(cs + i * ROW + p * TPH + 2 * j);
                     c[p] = v.x; s[p] = v.y; c[p + 1] = v.z; s[p + 1] = v.w;
                 }
                 const bool there = held >> i & 1;
@@ -273,12 +272,12 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
                             for (int o = 1; o < TPH; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                             r = rsqrtf(fmaf(sum, A.inv_d, A.eps));
                         }
-                        const float4 *w = (const float4 *)(weights + which * 16 * TPH + 16 * j);
+                        const float4 *w = (const float4 *)(weights + which * 16 * TPH) + j;
                         if (!GRAD) {
                             if (norm)
 #pragma unroll
                                 for (int p = 0; p < 8; p += 4) {
-                                    const float4 v = w[p / 4], z = w[p / 4 + 2];
+                                    const float4 v = w[p / 4 * TPH], z = w[(p / 4 + 2) * TPH];
                                     a[p] *= r * v.x; a[p + 1] *= r * v.y; a[p + 2] *= r * v.z; a[p + 3] *= r * v.w;
                                     b[p] *= r * z.x; b[p + 1] *= r * z.y; b[p + 2] *= r * z.z; b[p + 3] *= r * z.w;
                                 }
@@ -296,7 +295,7 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
                                 }
 #pragma unroll
                                 for (int p = 0; p < 8; p += 4) {
-                                    const float4 v = w[p / 4], z = w[p / 4 + 2];
+                                    const float4 v = w[p / 4 * TPH], z = w[(p / 4 + 2) * TPH];
                                     g[p] *= v.x; g[p + 1] *= v.y; g[p + 2] *= v.z; g[p + 3] *= v.w;
                                     h[p] *= z.x; h[p + 1] *= z.y; h[p + 2] *= z.z; h[p + 3] *= z.w;
                                 }
