@@ -64,18 +64,6 @@ template <typename X> __device__ __forceinline__ float weight_at(const RotArgs &
     return A.w32 ? ((const float *)w)[i] : rp_float(((const X *)w)[i]);
 }
 
-// Turns the pairs of a lane's two pieces, or turns them back: (a[p], b[p]), or neighbours in a and then in b.
-template <bool INTERLEAVED, bool BACK> __device__ __forceinline__ void turn(float *a, float *b, const float *c, const float *s)
-{
-#pragma unroll
-    for (int p = 0; p < 8; ++p) {
-        float &x = !INTERLEAVED ? a[p] : p < 4 ? a[2 * p] : b[2 * p - 8], &y = !INTERLEAVED ? b[p] : p < 4 ? a[2 * p + 1] : b[2 * p - 7];
-        const float sn = BACK ? -s[p] : s[p], was = x;
-        x = was * c[p] - y * sn;
-        y = was * sn + y * c[p];
-    }
-}
-
 // Any head size and alignment: a warp takes one head after the other, a lane the pairs lane, lane + 32, .. and then the elements behind them.
 // GRAD: y receives the gradient of x.
 template <typename X, bool GRAD>
@@ -180,6 +168,60 @@ __global__ void __launch_bounds__(ROT_THREADS) k_rotate_any(RotArgs A)
 // (half layout) or neighbours, so that a lane has all pairs that it needs and the mean of squares is a few shuffles.  A warp takes ROT_CHUNK tokens at a time:
 // their sines and cosines go to shared memory once, for all heads; then it goes through the heads of the queries, then of the keys, with a token's factors (and the
 // sums for the weights' gradients) in registers.  The loads of two steps are issued before either is worked on.
+// Element i of a lane's 16 in the order of its registers: the first of each pair (0 to 7), then the second.
+template <bool INTERLEAVED> __device__ __forceinline__ int place(int pa, int pb, int i)
+{
+    if (!INTERLEAVED) return i < 8 ? pa + i : pb + i - 8;
+    const int pair = i & 7;
+    return (pair < 4 ? pa + 2 * pair : pb + 2 * pair - 8) + (i >> 3);
+}
+template <typename X, bool INTERLEAVED> __device__ __forceinline__ void open_pairs(const Pack8<X> &p, const Pack8<X> &q, f2 *a, f2 *b)
+{
+    float x[8], y[8];
+    rp_open8(p, x); rp_open8(q, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (!INTERLEAVED) { a[i] = rp_f2(x[2 * i], x[2 * i + 1]); b[i] = rp_f2(y[2 * i], y[2 * i + 1]); }
+        else {
+            const float *z = i < 2 ? x + 4 * i : y + 4 * i - 8;
+            a[i] = rp_f2(z[0], z[2]); b[i] = rp_f2(z[1], z[3]);
+        }
+    }
+}
+template <typename X, bool INTERLEAVED> __device__ __forceinline__ void close_pairs(const f2 *a, const f2 *b, Pack8<X> &p, Pack8<X> &q)
+{
+    float x[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (!INTERLEAVED) { rp_parts(a[i], x[2 * i], x[2 * i + 1]); rp_parts(b[i], y[2 * i], y[2 * i + 1]); }
+        else {
+            float *z = i < 2 ? x + 4 * i : y + 4 * i - 8;
+            rp_parts(a[i], z[0], z[2]); rp_parts(b[i], z[1], z[3]);
+        }
+    }
+    p = rp_close8<X>(x); q = rp_close8<X>(y);
+}
+// Turns pairs, or turns them back.
+template <bool BACK> __device__ __forceinline__ void turn(f2 *a, f2 *b, const f2 *c, const f2 *s)
+{
+    const f2 minus = rp_f2(-1.0f, -1.0f);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const f2 x = a[p], n = rp_mul(s[p], minus);
+        a[p] = rp_fma(x, c[p], rp_mul(b[p], BACK ? s[p] : n));
+        b[p] = rp_fma(b[p], c[p], rp_mul(x, BACK ? n : s[p]));
+    }
+}
+// Sum over the lanes of a head.
+template <int TPH> __device__ __forceinline__ float head_sum(f2 v)
+{
+    float x, y;
+    rp_parts(v, x, y);
+    x += y;
+#pragma unroll
+    for (int o = 1; o < TPH; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
 #define ROT_CHUNK 4
 #define ROT_CTAS(GRAD) ((GRAD) ? 2 : 3)                  // resident on an SM
 template <typename X, int TPH, bool INTERLEAVED, bool GRAD>
@@ -198,24 +240,29 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
     if (GRAD && A.part)
         for (int i = lane; i < 2 * A.d; i += 32) dw[i] = 0.0f;
     if (warp < 2 && group == 0) {
-        const RotTensor &H = A.h[warp];                  // four of each lane side by side, lane after lane
+        const RotTensor &H = A.h[warp];                  // two of each lane side by side, lane after lane
         for (int i = 0; i < 16; ++i)
-            weights[warp * 16 * TPH + (i >> 2) * 4 * TPH + 4 * j + (i & 3)] = H.w && mine ? weight_at<X>(A, H.w, i < 8 ? pa + i : pb + i - 8) : 1.0f;
+            weights[warp * 16 * TPH + (i >> 1) * 2 * TPH + 2 * j + (i & 1)] = H.w && mine ? weight_at<X>(A, H.w, place<INTERLEAVED>(pa, pb, i)) : 1.0f;
     }
     __syncthreads();
     const int unit = blockIdx.x * ROT_WARPS + warp, lanes = gridDim.x * ROT_WARPS / A.parts, share = unit % A.parts;
-    const i64 t0 = unit / A.parts < lanes ? A.T * (unit / A.parts) / lanes : A.T, t1 = unit / A.parts < lanes ? A.T * (unit / A.parts + 1) / lanes : A.T;
+    // tokens unit / parts, + lanes, + 2 lanes ..: at any time the warps read neighbouring tokens
     Place at;
     at.next = INT64_MIN;
-    for (i64 c0 = t0; c0 < t1; c0 += ROT_CHUNK) {
-        const int n = (int)min((i64)ROT_CHUNK, t1 - c0);
+    for (i64 c0 = unit / A.parts; c0 < (unit / A.parts < lanes ? A.T : 0); c0 += (i64)ROT_CHUNK * lanes) {
+        const int n = (int)min((i64)ROT_CHUNK, (A.T - c0 + lanes - 1) / lanes);
         u32 held = 0;
         __syncwarp();
         for (int i = 0; i < n; ++i) {
-            if (c0 + i >= at.next) at.find(A, c0 + i);
+            const i64 t = c0 + (i64)i * lanes;
+            if (t >= at.next) at.find(A, t);
             held |= (at.held ? 1u : 0u) << i;
-            for (int p = lane; p < ROW; p += 32)         // (two pairs of each lane side by side, lane after lane: no two of a load's lanes in one bank)
-                cs[i * ROW + ((p & 7) >> 1) * 2 * TPH + (p >> 3) * 2 + (p & 1)] = p < pairs ? turn_of(A, c0 + i + at.base, p) : make_float2(1.0f, 0.0f);
+            for (int p = lane; p < ROW; p += 32) {
+                // two cosines and two sines of a lane side by side, lane after lane: no two of a load's lanes in one bank
+                const float2 v = p < pairs ? turn_of(A, t + at.base, p) : make_float2(1.0f, 0.0f);
+                float *to = (float *)(cs + i * ROW + ((p & 7) >> 1) * 2 * TPH + (p >> 3) * 2) + (p & 1);
+                to[0] = v.x; to[2] = v.y;
+            }
         }
         __syncwarp();
         int before = 0;                                  // steps of the tensor before
@@ -228,18 +275,20 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
             if (first >= steps) continue;
             const bool norm = H.w != nullptr;
             const int head0 = first * NG + group, head_step = A.parts * NG;
-            float da[8], db[8];
+            const i64 x_step = head_step * H.x_head, g_step = GRAD ? head_step * H.g_head : 0, y_step = head_step * H.y_head;
+            const f2 *w = (const f2 *)(weights + which * 16 * TPH) + j;
+            f2 da[4], db[4];
             if (GRAD) {
 #pragma unroll
-                for (int p = 0; p < 8; ++p) { da[p] = 0.0f; db[p] = 0.0f; }
+                for (int p = 0; p < 4; ++p) { da[p] = rp_f2(0.0f, 0.0f); db[p] = da[p]; }
             }
             for (int i = 0; i < n; ++i) {
-                const i64 t = c0 + i;
-                float c[8], s[8];
+                const i64 t = c0 + (i64)i * lanes;
+                f2 c[4], s[4];
 #pragma unroll
-                for (int p = 0; p < 8; p += 2) {
-                    const float4 v = *(const float4 *)(cs + i * ROW + p * TPH + 2 * j);
-                    c[p] = v.x; s[p] = v.y; c[p + 1] = v.z; s[p + 1] = v.w;
+                for (int p = 0; p < 4; ++p) {
+                    const ulonglong2 v = *(const ulonglong2 *)(cs + i * ROW + p * 2 * TPH + 2 * j);
+                    c[p].v = v.x; s[p].v = v.y;
                 }
                 const bool there = held >> i & 1;
                 const X *x = (const X *)H.x + t * H.x_token + head0 * H.x_head, *g = GRAD ? (const X *)H.dy + t * H.g_token + head0 * H.g_head : nullptr;
@@ -256,79 +305,73 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
                             if (GRAD) { ga[u] = rp_load8(g + pa); gb[u] = rp_load8(g + pb); }
                         }
                         head += head_step;
-                        x += head_step * H.x_head;
-                        if (GRAD) g += head_step * H.g_head;
+                        x += x_step;
+                        if (GRAD) g += g_step;
                     }
 #pragma unroll
                     for (int u = 0; u < STEPS; ++u) {
-                        float a[8], b[8];
-                        rp_open8(xa[u], a); rp_open8(xb[u], b);
-                        float r = 1.0f;
+                        f2 a[4], b[4];
+                        open_pairs<X, INTERLEAVED>(xa[u], xb[u], a, b);
+                        f2 r = rp_f2(1.0f, 1.0f);
                         if (norm) {
-                            float sum = 0.0f;
+                            f2 sum2 = rp_f2(0.0f, 0.0f);
 #pragma unroll
-                            for (int p = 0; p < 8; ++p) sum = fmaf(a[p], a[p], fmaf(b[p], b[p], sum));
-#pragma unroll
-                            for (int o = 1; o < TPH; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                            r = rsqrtf(fmaf(sum, A.inv_d, A.eps));
+                            for (int p = 0; p < 4; ++p) sum2 = rp_fma(a[p], a[p], rp_fma(b[p], b[p], sum2));
+                            const float sum = head_sum<TPH>(sum2), q = rsqrtf(fmaf(sum, A.inv_d, A.eps));
+                            r = rp_f2(q, q);
                         }
-                        const float4 *w = (const float4 *)(weights + which * 16 * TPH) + j;
                         if (!GRAD) {
                             if (norm)
 #pragma unroll
-                                for (int p = 0; p < 8; p += 4) {
-                                    const float4 v = w[p / 4 * TPH], z = w[(p / 4 + 2) * TPH];
-                                    a[p] *= r * v.x; a[p + 1] *= r * v.y; a[p + 2] *= r * v.z; a[p + 3] *= r * v.w;
-                                    b[p] *= r * z.x; b[p + 1] *= r * z.y; b[p + 2] *= r * z.z; b[p + 3] *= r * z.w;
-                                }
-                            turn<INTERLEAVED, false>(a, b, c, s);
+                                for (int p = 0; p < 4; ++p) { a[p] = rp_mul(a[p], rp_mul(r, w[p * TPH])); b[p] = rp_mul(b[p], rp_mul(r, w[(p + 4) * TPH])); }
+                            turn<false>(a, b, c, s);
                         } else {
-                            float g[8], h[8];
-                            rp_open8(ga[u], g); rp_open8(gb[u], h);
-                            turn<INTERLEAVED, true>(g, h, c, s);
+                            f2 g2[4], h2[4];
+                            open_pairs<X, INTERLEAVED>(ga[u], gb[u], g2, h2);
+                            turn<true>(g2, h2, c, s);
                             if (norm) {
-                                float dot = 0.0f;
+                                f2 dot2 = rp_f2(0.0f, 0.0f);
 #pragma unroll
-                                for (int p = 0; p < 8; ++p) {
-                                    a[p] *= r; b[p] *= r;
-                                    da[p] = fmaf(g[p], a[p], da[p]); db[p] = fmaf(h[p], b[p], db[p]);
+                                for (int p = 0; p < 4; ++p) {
+                                    a[p] = rp_mul(a[p], r); b[p] = rp_mul(b[p], r);
+                                    da[p] = rp_fma(g2[p], a[p], da[p]); db[p] = rp_fma(h2[p], b[p], db[p]);
+                                    g2[p] = rp_mul(g2[p], w[p * TPH]); h2[p] = rp_mul(h2[p], w[(p + 4) * TPH]);
+                                    dot2 = rp_fma(g2[p], a[p], rp_fma(h2[p], b[p], dot2));
                                 }
+                                const float dot = -head_sum<TPH>(dot2) * A.inv_d;
+                                const f2 d2 = rp_f2(dot, dot);
 #pragma unroll
-                                for (int p = 0; p < 8; p += 4) {
-                                    const float4 v = w[p / 4 * TPH], z = w[(p / 4 + 2) * TPH];
-                                    g[p] *= v.x; g[p + 1] *= v.y; g[p + 2] *= v.z; g[p + 3] *= v.w;
-                                    h[p] *= z.x; h[p + 1] *= z.y; h[p + 2] *= z.z; h[p + 3] *= z.w;
-                                }
-#pragma unroll
-                                for (int p = 0; p < 8; ++p) dot = fmaf(g[p], a[p], fmaf(h[p], b[p], dot));
-#pragma unroll
-                                for (int o = 1; o < TPH; o <<= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                                dot *= A.inv_d;
-#pragma unroll
-                                for (int p = 0; p < 8; ++p) { g[p] = r * (g[p] - a[p] * dot); h[p] = r * (h[p] - b[p] * dot); }
+                                for (int p = 0; p < 4; ++p) { g2[p] = rp_mul(r, rp_fma(a[p], d2, g2[p])); h2[p] = rp_mul(r, rp_fma(b[p], d2, h2[p])); }
                             }
 #pragma unroll
-                            for (int p = 0; p < 8; ++p) { a[p] = g[p]; b[p] = h[p]; }
+                            for (int p = 0; p < 4; ++p) { a[p] = g2[p]; b[p] = h2[p]; }
                         }
                         if (!there) {
 #pragma unroll
-                            for (int p = 0; p < 8; ++p) { a[p] = 0.0f; b[p] = 0.0f; }
+                            for (int p = 0; p < 4; ++p) { a[p] = rp_f2(0.0f, 0.0f); b[p] = a[p]; }
                         }
                         if (ok[u]) {
-                            rp_store8(y + pa, rp_close8<X>(a));
-                            rp_store8(y + pb, rp_close8<X>(b));
+                            Pack8<X> oa, ob;
+                            close_pairs<X, INTERLEAVED>(a, b, oa, ob);
+                            rp_store8(y + pa, oa);
+                            rp_store8(y + pb, ob);
                         }
-                        y += head_step * H.y_head;
+                        y += y_step;
                     }
                 }
             }
             if (GRAD && norm && A.part) {
 #pragma unroll
-                for (int p = 0; p < 8; ++p) {
+                for (int p = 0; p < 4; ++p)
 #pragma unroll
-                    for (int o = TPH; o < 32; o <<= 1) { da[p] += __shfl_xor_sync(0xffffffffu, da[p], o); db[p] += __shfl_xor_sync(0xffffffffu, db[p], o); }
-                    if (group == 0 && mine) { dw[which * A.d + pa + p] += da[p]; dw[which * A.d + pb + p] += db[p]; }
-                }
+                    for (int q = 0; q < 2; ++q) {
+                        float v[2];
+                        rp_parts(q ? db[p] : da[p], v[0], v[1]);
+#pragma unroll
+                        for (int o = TPH; o < 32; o <<= 1) { v[0] += __shfl_xor_sync(0xffffffffu, v[0], o); v[1] += __shfl_xor_sync(0xffffffffu, v[1], o); }
+                        const int e0 = place<INTERLEAVED>(pa, pb, 8 * q + 2 * p), e1 = place<INTERLEAVED>(pa, pb, 8 * q + 2 * p + 1);
+                        if (group == 0 && mine) { dw[which * A.d + e0] += v[0]; dw[which * A.d + e1] += v[1]; }
+                    }
             }
         }
     }
