@@ -364,6 +364,12 @@ def _torch():
     return torch
 
 
+def _current_stream(device: int) -> int:
+    """Handle of torch's current stream of a GPU (without the stream object, which takes ten times as long to make)."""
+    raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else _torch().cuda.current_stream(device).cuda_stream
+
+
 class _Queue:
     """Stream of a call: its handle, and as a context the stream that new tensors belong to."""
     __slots__ = ("handle", "scope")
@@ -371,7 +377,7 @@ class _Queue:
     def __init__(self, torch, tensor, stream):
         self.scope = None
         if stream is None:
-            self.handle = torch.cuda.current_stream(tensor.device).cuda_stream
+            self.handle = _current_stream(tensor.get_device())
             return
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=tensor.device)
@@ -430,7 +436,7 @@ def rp_count_routes(routes, start, n_experts: int, demand=None, stream=None):
     at, n = _starts(torch, start)
     with _Queue(torch, routes, stream) as queue:
         if demand is None:
-            demand = torch.empty((n, L, n_experts), dtype=torch.int32, device=routes.device)
+            demand = routes.new_empty((n, L, n_experts), dtype=torch.int32)
         _check(lib().rp_count_routes(routes.data_ptr() or at, size, T, L, k, n_experts, ts, ls, at, n,
                                      _dense(demand, torch.int32, (n, L, n_experts), "demand"), queue.handle), "rp_count_routes")
     return demand
@@ -471,23 +477,22 @@ def rp_route(logits, top_k: int, start, *, score: str = "softmax", normalise: bo
     T, E = logits.shape
     at, n = _starts(torch, start)
     r, ref = _router(E, top_k, _kind(logits, "logits"), score, normalise, scale, loss_coef)
-    dev = logits.device
     with _Queue(torch, logits, stream) as queue:
         if replay is not None:
             routes = replay
         elif routes is None:
-            routes = torch.empty((T, top_k), dtype=torch.int32, device=dev)
+            routes = logits.new_empty((T, top_k), dtype=torch.int32)
         if routes.shape != (T, top_k):
             raise ValueError(f"routes: {(T, top_k)} wanted, got {tuple(routes.shape)}")
         size, step = _route_layout(routes)
         if gates is None:
-            gates = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+            gates = logits.new_empty((T, top_k), dtype=torch.float32)
         if counts is None:
-            counts = torch.empty((n, E), dtype=torch.int32, device=dev)
+            counts = logits.new_empty((n, E), dtype=torch.int32)
         if loss is None:
-            loss = torch.empty(1, dtype=torch.float32, device=dev)
+            loss = logits.new_empty(1, dtype=torch.float32)
         nbytes = lib().rp_route_workspace(ref, n)
-        space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        space = logits.new_empty(nbytes, dtype=torch.uint8)
         # (an empty tensor has no address: any will do)
         _check(lib().rp_route(ref, logits.data_ptr() or at, row, T, _dense(choice_bias, torch.float32, (E,), "choice_bias"), at, n,
                               int(replay is not None), routes.data_ptr() or at, size, step,
@@ -510,7 +515,7 @@ def rp_route_grad(logits, routes, start, counts, *, gates_grad=None, loss_grad=N
     r, ref = _router(E, k, _kind(logits, "logits"), score, normalise, scale, loss_coef)
     with _Queue(torch, logits, stream) as queue:
         if logits_grad is None:
-            logits_grad = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+            logits_grad = logits.new_empty((T, E))
         if logits_grad.shape != logits.shape or logits_grad.dtype != logits.dtype:
             raise ValueError("logits_grad: shape and type of the logits wanted")
         if T:
@@ -554,7 +559,7 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
             if x is None:
                 continue
             if out is None:
-                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+                out = x.new_empty(x.shape)
             results[i] = out
             side = rp_heads(x.shape[1], x.data_ptr(), *_head_strides(x, x, "input"), out.data_ptr(), *_head_strides(out, x, "output"),
                             _dense(w, w_type, (d,), "weight"))
@@ -562,7 +567,7 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
                 side.y_grad = g.data_ptr()
                 side.g_token, side.g_head = _head_strides(g, x, "gradient")
                 if w is not None:
-                    dws[i] = torch.empty(d, dtype=torch.float32, device=x.device)
+                    dws[i] = x.new_empty(d, dtype=torch.float32)
                     side.weight_grad = dws[i].data_ptr()
             sides[i] = C.byref(side)
         freq = None if inv_freq is None else _dense(inv_freq, torch.float64, inv_freq.shape, "inv_freq")
@@ -578,7 +583,7 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
             space, nbytes = None, 0
             if dws[0] is not None or dws[1] is not None:
                 nbytes = lib().rp_rotate_workspace(ref)
-                space = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+                space = q.new_empty(nbytes, dtype=torch.uint8)
             _check(lib().rp_rotate_grad(*args, None if space is None else space.data_ptr(), nbytes, queue.handle), "rp_rotate_grad")
     return results, dws
 
@@ -636,11 +641,11 @@ def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = N
     T, H, _ = q.shape
     with _Queue(torch, q, stream) as queue:
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         if lse is None:
-            lse = torch.empty((H, T), dtype=torch.float32, device=q.device).t()      # a head's rows side by side: what the backward pass reads fastest
+            lse = q.new_empty((H, T), dtype=torch.float32).t()      # a head's rows side by side: what the backward pass reads fastest
         nbytes = lib().rp_attend_workspace(ref, T, n)
-        space = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+        space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         if T:
             _check(lib().rp_attend(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _view(out, q, "out"), _lse_view(lse, T, H, torch),
                                    space.data_ptr(), nbytes, queue.handle), "rp_attend")
@@ -654,11 +659,11 @@ def rp_attend_grad(out_grad, q, k, v, out, lse, start, *, causal: bool = True, s
     ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
     T, H, _ = q.shape
     with _Queue(torch, q, stream) as queue:
-        q_grad = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_grad is None else q_grad
-        k_grad = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_grad is None else k_grad
-        v_grad = torch.empty(v.shape, dtype=v.dtype, device=v.device) if v_grad is None else v_grad
+        q_grad = q.new_empty(q.shape) if q_grad is None else q_grad
+        k_grad = k.new_empty(k.shape) if k_grad is None else k_grad
+        v_grad = v.new_empty(v.shape) if v_grad is None else v_grad
         nbytes = lib().rp_attend_grad_workspace(ref, T, n)
-        space = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+        space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         if T:
             _check(lib().rp_attend_grad(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), _view(out, q, "out"), _lse_view(lse, T, H, torch),
                                         _view(out_grad, q, "out_grad"), at, n, _view(q_grad, q, "q_grad"), _view(k_grad, k, "k_grad"),
