@@ -39,7 +39,7 @@ struct RouteArgs {
     u64 *sums;
     RouteSpace *space;
     float *loss;
-    int wide;                               // rows can be read 16 bytes at a time
+    int wide;                               // rows can be read (and written) 16 bytes at a time
     int finish;                             // 0: one CTA does it all, 1: the last CTA works out the loss, 2: another launch does
     // gradient
     const float *gates_grad, *loss_grad;
@@ -70,52 +70,83 @@ template <int SUB> __device__ __forceinline__ u32 sub_max(u32 v)
     return v;
 }
 
-// A row's VPL elements of a lane; experts from E on do not exist.
+// A row's VPL elements of a lane, as they lie in memory (16 bytes at a time, or one by one where rows are not on such boundaries).
+template <typename X, int VPL> struct Row { Pack8<X> p[VPL / 8]; };
 template <typename X, int VPL>
-__device__ __forceinline__ void load_row(const RouteArgs &A, i64 t, int e0, float *x)
+__device__ __forceinline__ void load_row(const RouteArgs &A, i64 t, int e0, Row<X, VPL> &r)
 {
-    const X *row = (const X *)A.x + t * A.row;
-    if (A.wide) {
+    const X *row = (const X *)A.x + t * A.row + e0;
 #pragma unroll
-        for (int c = 0; c < VPL; c += 8)
-            if (e0 + c < A.E) rp_open8(rp_load8(row + e0 + c), x + c);
-    } else {
+    for (int c = 0; c < VPL; c += 8) {
+        if (A.wide) {
+            if (e0 + c < A.E) r.p[c / 8] = rp_load8(row + c);
+        } else {
+            X x[8];
 #pragma unroll
-        for (int c = 0; c < VPL; ++c)
-            if (e0 + c < A.E) x[c] = rp_float(row[e0 + c]);
+            for (int i = 0; i < 8; ++i) x[i] = e0 + c + i < A.E ? row[c + i] : rp_round<X>(0.0f);
+            memcpy(&r.p[c / 8], x, sizeof(x));
+        }
+    }
+}
+// Experts from E on have a logit of -inf.
+template <typename X, int VPL>
+__device__ __forceinline__ void open_row(const RouteArgs &A, int e0, const Row<X, VPL> &r, float *x)
+{
+#pragma unroll
+    for (int c = 0; c < VPL; c += 8) rp_open8(r.p[c / 8], x + c);
+    if (e0 + VPL > A.E) {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) x[i] = e0 + i < A.E ? x[i] : -INFINITY;
     }
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return __frcp_rn(1.0f + rp_exp2(-x * RP_LOG2E)); }
+__device__ __forceinline__ float reciprocal(float x)        // by the special function unit: 1 ulp
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float sigmoid(float x) { return reciprocal(1.0f + rp_exp2(-x * RP_LOG2E)); }
 
 // Scores of one token from its logits: softmax: e^(x - max) and 1 / their sum; sigmoid: s, and 1 / their sum.
 // `top` is what the largest logit is taken for: 0 where it is -inf (all scores are 0 then, and so is the inverse).
+// Two sigmoids share a reciprocal, 1 / (1 + a) = (1 + b) / ((1 + a)(1 + b)), which holds while either is above 2^-63; less counts as 0 beside scores of a
+// sum above 2^-40, and rows of nothing but such are worked out one by one.
 template <int VPL, int SUB>
-__device__ __forceinline__ void scores(const RouteArgs &A, const float *x, int e0, float *s, float &top, float &inv)
+__device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float *s, float &top, float &inv)
 {
     float sum = 0.0f;
+    top = 0.0f;
     if (A.score == RP_SCORE_SOFTMAX) {
-        float m = -INFINITY;
+        float m = x[0];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (e0 + i < A.E) m = fmaxf(m, x[i]);
+        for (int i = 1; i < VPL; ++i) m = fmaxf(m, x[i]);
         m = sub_max<SUB>(m);
         top = m == -INFINITY ? 0.0f : m;
         const float shift = -top * RP_LOG2E;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            s[i] = e0 + i < A.E ? rp_exp2(fmaf(x[i], RP_LOG2E, shift)) : 0.0f;
-            sum += s[i];
-        }
+        for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2(fmaf(x[i], RP_LOG2E, shift)); sum += s[i]; }
+        sum = sub_sum<SUB>(sum);
     } else {
-        top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            s[i] = e0 + i < A.E ? sigmoid(x[i]) : 0.0f;
-            sum += s[i];
+        for (int i = 0; i < VPL; i += 2) {
+            const float u = x[i] * -RP_LOG2E, v = x[i + 1] * -RP_LOG2E;
+            const float a = 1.0f + rp_exp2(u), b = 1.0f + rp_exp2(v), r = reciprocal(fminf(a, 9.0e18f) * fminf(b, 9.0e18f));
+            // (a comparison that a NaN fails keeps it)
+            s[i] = u > 63.0f ? 0.0f : r * fminf(b, 9.0e18f);
+            s[i + 1] = v > 63.0f ? 0.0f : r * fminf(a, 9.0e18f);
+            if (u != u) s[i] = u;
+            if (v != v) s[i + 1] = v;
+            sum += s[i] + s[i + 1];
+        }
+        sum = sub_sum<SUB>(sum);
+        if (__any_sync(0xffffffffu, sum < 1.0e-12f)) {
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) { s[i] = sigmoid(x[i]); sum += s[i]; }
+            sum = sub_sum<SUB>(sum);
         }
     }
-    sum = sub_sum<SUB>(sum);
     inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 }
 // Score of one expert as the gates use it.
@@ -127,9 +158,73 @@ __device__ __forceinline__ float score_of(const RouteArgs &A, float x, float top
 // Floats as unsigned numbers in the same order; -0 as 0, NaN above all.
 __device__ __forceinline__ u32 order_of(float x)
 {
-    const u32 b = __float_as_uint(x + 0.0f);
-    if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
-    return (b >> 31) ? ~b : b | 0x80000000u;
+    const int b = __float_as_int(x + 0.0f);                  // (any NaN becomes 0x7fffffff)
+    return (u32)b ^ ((u32)(b >> 31) | 0x80000000u);
+}
+
+// The k experts with the largest logits, in falling order, ties to the lower one: lane j of the token's gets the j-th, and its logit.
+// 16-bit logits leave their last 13 bits as floats free for the expert's number: keys that are all different and tell it all.  Every lane keeps its two largest; the
+// largest of all goes round by round, and a lane that has had both looks for its next two, those below the one that has just gone.
+template <int VPL, int SUB>
+__device__ __forceinline__ void choose_by_keys(const RouteArgs &A, const float *x, int e0, int sl, i64 &e, float &xe)
+{
+    u32 key[VPL], first = 0, second = 0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        key[i] = (order_of(x[i]) & ~0x1fffu) | (u32)(1023 - e0 - i) | 0x400u;
+        if (e0 + VPL > A.E) key[i] = e0 + i < A.E ? key[i] : 0u;
+        first = max(first, key[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) second = max(second, key[i] - first);      // (those below it wrap around to the largest numbers, in their order)
+    second += first;
+    u32 mine = 0;
+    for (int j = 0; j < A.k; ++j) {
+        const u32 best = sub_max<SUB>(first);
+        if (sl == j) mine = best;
+        const bool gone = first == best;
+        const bool both = gone && second == 0;
+        if (gone) { first = second; second = 0; }
+        if (__any_sync(0xffffffffu, both)) {
+            u32 f = 0, g = 0;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) f = max(f, key[i] - best);
+            f += best;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) g = max(g, key[i] - f);
+            g += f;
+            // (no key below: the wrapped distances are those of keys that have gone, which come back at `best` or above)
+            if (both) { first = f < best ? f : 0u; second = g < f && f < best ? g : 0u; }
+        }
+    }
+    e = 1023 - (int)(mine & 0x3ffu);
+    const u32 b = mine & ~0x1fffu;
+    xe = __uint_as_float((b >> 31) ? b ^ 0x80000000u : ~b & ~0x1fffu);
+}
+// The same by any number, round by round: the largest, the lowest lane that has it, and its lowest expert.
+template <int VPL, int SUB>
+__device__ __forceinline__ void choose_by_numbers(const RouteArgs &A, const float *number, int e0, int sl, i64 &e)
+{
+    const int first_lane = (threadIdx.x & 31) - sl;
+    u32 key[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) key[i] = e0 + i < A.E ? max(order_of(number[i]), 1u) : 0u;
+    for (int j = 0; j < A.k; ++j) {
+        u32 top = 0;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) top = max(top, key[i]);
+        const u32 best = sub_max<SUB>(top);
+        u32 who = __ballot_sync(0xffffffffu, top == best) >> first_lane;
+        if (SUB < 32) who &= (1u << (SUB & 31)) - 1u;
+        const int owner = __ffs((int)who) - 1;
+        int at = 0;
+#pragma unroll
+        for (int i = VPL - 1; i >= 0; --i) at = key[i] == best ? i : at;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) key[i] = sl == owner && i == at ? 0u : key[i];
+        const int found = __shfl_sync(0xffffffffu, e0 + at, first_lane + owner);
+        if (sl == j) e = found;
+    }
 }
 
 // One group's part of the loss, by one warp.
@@ -178,12 +273,10 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
 {
     constexpr int NSUB = ROUTE_THREADS / SUB, EP = VPL * SUB;             // groups of lanes, experts they hold
     __shared__ int cnt[NSUB][EP];
-    __shared__ u32 pick[NSUB][ROUTE_MAX_K];                               // chosen experts of the present token
     __shared__ int last[NSUB];                                           // group of tokens that a run ends in
     __shared__ double part[ROUTE_WARPS];
     __shared__ u32 turn;
     const int sub = threadIdx.x / SUB, sl = threadIdx.x % SUB, e0 = sl * VPL;
-    const int first_lane = threadIdx.x & 31 & ~(SUB - 1);
     const bool want_loss = A.loss != nullptr, want_counts = A.counts != nullptr;
     if (A.finish == 0 && want_counts) {
         // the only CTA: nobody has cleared its sums
@@ -197,12 +290,42 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
     const i64 t0 = ((i64)blockIdx.x * NSUB + sub) * A.run;
     int g = rp_sample_of(A.start, A.G, t0);
     i64 next = g < A.G ? A.start[g + 1] : INT64_MAX;                      // where the next group begins
-    float acc[VPL], x[VPL], s[VPL];
+    float acc[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) acc[i] = 0.0f;
+    Row<X, VPL> row = Row<X, VPL>();
+    if (t0 < A.T) load_row<X, VPL>(A, t0, e0, row);
+    int k_lanes = 1;                                                      // lanes that the sum over the chosen goes over
+    while (k_lanes < A.k) k_lanes <<= 1;
     for (i64 step = 0; step < A.run; ++step) {
         const i64 t = t0 + step;
         const bool there = t < A.T;
+        float x[VPL], s[VPL], top = 0.0f, inv = 0.0f, xe = 0.0f;
+        open_row<X, VPL>(A, e0, row, x);
+        if (step + 1 < A.run && t + 1 < A.T) load_row<X, VPL>(A, t + 1, e0, row);
+        // lane j of the token's has its j-th choice (there are at least k of them)
+        i64 e = -1;
+        if (A.replay && there && sl < A.k) e = rp_load_route(A.routes, A.route_bytes, t * A.route_row + sl);
+        if (want_loss || A.score == RP_SCORE_SOFTMAX || A.bias) scores<VPL, SUB>(A, x, s, top, inv);
+        if (!A.replay) {
+            if (sizeof(X) == 2 && !A.bias) choose_by_keys<VPL, SUB>(A, x, e0, sl, e, xe);
+            else {
+                float number[VPL];
+#pragma unroll
+                for (int i = 0; i < VPL; ++i)
+                    number[i] = !A.bias ? x[i] : (A.score == RP_SCORE_SOFTMAX ? s[i] * inv : s[i]) + (e0 + i < A.E ? A.bias[e0 + i] : 0.0f);
+                choose_by_numbers<VPL, SUB>(A, number, e0, sl, e);
+            }
+        }
+        const bool valid = there && sl < A.k && e >= 0 && e < A.E;
+        if (valid && (A.replay || sizeof(X) == 4 || A.bias)) xe = rp_float(((const X *)A.x)[t * A.row + e]);
+        const float v = valid ? score_of(A, xe, top, inv) : 0.0f;
+        float gate = v * A.scale;
+        if (A.normalise) {
+            float total = v;
+            for (int o = 1; o < k_lanes; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+            gate = total == 0.0f ? 0.0f : gate / total;
+        }
         if (there && t >= next) {
             // another group: what the run has of the one before goes out
             if (g >= 0 && g < A.G) {
@@ -218,83 +341,16 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
             g = rp_sample_of(A.start, A.G, t);
             next = g < A.G ? A.start[g + 1] : INT64_MAX;
         }
-        const bool held = there && g >= 0 && g < A.G;
         __syncwarp();
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
-        if (held) load_row<X, VPL>(A, t, e0, x);
-        float top, inv;
-        scores<VPL, SUB>(A, x, e0, s, top, inv);
+        const bool held = there && g >= 0 && g < A.G;
         if (want_loss && held) {
 #pragma unroll
             for (int i = 0; i < VPL; ++i) acc[i] = fmaf(s[i], inv, acc[i]);
         }
-        if (!A.replay) {
-            // The k largest, one after the other.  16-bit logits leave their last 13 bits as floats free for the expert; others need a second look
-            // for the lowest expert that has the number.
-            u32 key[VPL];
-            if (sizeof(X) == 2 && !A.bias) {
-#pragma unroll
-                for (int i = 0; i < VPL; ++i) key[i] = e0 + i < A.E ? (order_of(x[i]) & ~0x1fffu) | (u32)(1023 - e0 - i) | 0x400u : 0u;
-                for (int j = 0; j < A.k; ++j) {
-                    u32 best = 0;
-#pragma unroll
-                    for (int i = 0; i < VPL; ++i) best = max(best, key[i]);
-                    best = sub_max<SUB>(best);
-#pragma unroll
-                    for (int i = 0; i < VPL; ++i) key[i] = key[i] == best ? 0u : key[i];
-                    if (sl == 0) pick[sub][j] = 1023u - (best & 0x3ffu);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < VPL; ++i) {
-                    const float v = !A.bias ? x[i] : (A.score == RP_SCORE_SOFTMAX ? s[i] * inv : s[i]) + (e0 + i < A.E ? A.bias[e0 + i] : 0.0f);
-                    key[i] = e0 + i < A.E ? max(order_of(v), 1u) : 0u;
-                }
-                for (int j = 0; j < A.k; ++j) {
-                    u32 mine = 0;
-#pragma unroll
-                    for (int i = 0; i < VPL; ++i) mine = max(mine, key[i]);
-                    const u32 best = sub_max<SUB>(mine);
-                    u32 who = __ballot_sync(0xffffffffu, mine == best) >> first_lane;
-                    if (SUB < 32) who &= (1u << (SUB & 31)) - 1u;
-                    if (sl == __ffs((int)who) - 1) {
-                        bool gone = false;
-#pragma unroll
-                        for (int i = 0; i < VPL; ++i)
-                            if (!gone && key[i] == best) { gone = true; key[i] = 0; pick[sub][j] = (u32)(e0 + i); }
-                    }
-                }
-            }
-            __syncwarp();
-        }
-        float total = 0.0f;
-        for (int j = sl; j < A.k; j += SUB) {
-            i64 e = -1;
-            if (held) e = A.replay ? rp_load_route(A.routes, A.route_bytes, t * A.route_row + j) : (i64)pick[sub][j];
-            const bool valid = e >= 0 && e < A.E;
-            float v = 0.0f;
-            if (valid) {
-                v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv);
-                if (want_counts) atomicAdd(&cnt[sub][(int)e], 1);
-            }
-            total += v;
-        }
-        if (A.normalise) {
-            total = sub_sum<SUB>(total);
-            total = total == 0.0f ? 0.0f : 1.0f / total;
-        } else
-            total = 1.0f;
-        for (int j = sl; j < A.k; j += SUB) {
-            i64 e = -1;
-            if (held) e = A.replay ? rp_load_route(A.routes, A.route_bytes, t * A.route_row + j) : (i64)pick[sub][j];
-            const bool valid = e >= 0 && e < A.E;
-            float v = 0.0f;
-            if (valid) v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv) * total * A.scale;
-            if (there) {
-                A.gates[t * A.k + j] = v;
-                if (!A.replay) rp_store_route(A.routes, A.route_bytes, t * A.route_row + j, (int)e);
-            }
+        if (valid && held && want_counts) atomicAdd(&cnt[sub][(int)e], 1);
+        if (there && sl < A.k) {
+            A.gates[t * A.k + sl] = held ? gate : 0.0f;
+            if (!A.replay) rp_store_route(A.routes, A.route_bytes, t * A.route_row + sl, held ? (int)e : -1);
         }
         __syncwarp();
     }
@@ -352,23 +408,32 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_loss(RouteArgs A)
 // Gradient for the logits.  With b[e] = loss_grad * coef / G * E * counts[g][e] / (k T_g^2), a_j = scale * gates_grad_j and y_j = s_j / sum of the chosen:
 //   softmax: dx = p (b - sum p b) + at the chosen: y_j (a_j - sum y a), or, not normalised, p (b - sum p b - sum_j p_j a_j) + p_j a_j
 //   sigmoid: ds = (b - sum p b) / sum s + at the chosen: (a_j - sum y a) / sum of the chosen, or a_j;  dx = s (1 - s) ds
-// The token's row is put together in shared memory, where the parts of its chosen experts are added one after the other.
+// The token's row is put together in shared memory, where the lanes that have its chosen experts each add their part; an expert that a token has twice gets its
+// parts one after the other.
 template <typename X, int VPL, int SUB>
 __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
 {
     constexpr int NSUB = ROUTE_THREADS / SUB, EP = VPL * SUB;
     __shared__ __align__(16) float rows[NSUB][EP];
-    __shared__ int pick[NSUB][ROUTE_MAX_K];
-    __shared__ float add[NSUB][ROUTE_MAX_K];
-    const int sub = threadIdx.x / SUB, sl = threadIdx.x % SUB, e0 = sl * VPL;
-    const bool soft = A.score == RP_SCORE_SOFTMAX;
+    const int sub = threadIdx.x / SUB, sl = threadIdx.x % SUB, e0 = sl * VPL, first_lane = (threadIdx.x & 31) - sl;
+    const bool soft = A.score == RP_SCORE_SOFTMAX, gates = A.gates_grad != nullptr;
     const float loss_grad = A.loss_grad ? *A.loss_grad : 0.0f;
     const i64 t0 = ((i64)blockIdx.x * NSUB + sub) * A.run;
-    int g = -2;
+    int g = -2, k_lanes = 1;
+    while (k_lanes < A.k) k_lanes <<= 1;
     i64 next = INT64_MIN;
-    float b[VPL], x[VPL], s[VPL];
+    float b[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) b[i] = 0.0f;
+    Row<X, VPL> row = Row<X, VPL>();
+    // lane j of the token's has its j-th choice
+    i64 e_next = -1;
+    float a_next = 0.0f;
+    auto fetch = [&](i64 t) {
+        load_row<X, VPL>(A, t, e0, row);
+        if (gates && sl < A.k) { e_next = rp_load_route(A.routes, A.route_bytes, t * A.route_row + sl); a_next = A.gates_grad[t * A.k + sl]; }
+    };
+    if (t0 < A.T) fetch(t0);
     for (i64 step = 0; step < A.run; ++step) {
         const i64 t = t0 + step;
         const bool there = t < A.T;
@@ -383,64 +448,67 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
             }
         }
         const bool held = there && g >= 0 && g < A.G;
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) x[i] = -INFINITY;
-        if (held) load_row<X, VPL>(A, t, e0, x);
-        float top, inv;
-        scores<VPL, SUB>(A, x, e0, s, top, inv);
+        float x[VPL], s[VPL], top, inv;
+        open_row<X, VPL>(A, e0, row, x);
+        const bool valid = gates && held && sl < A.k && e_next >= 0 && e_next < A.E;
+        const int e = valid ? (int)e_next : -1;
+        const float a = A.scale * a_next;
+        if (step + 1 < A.run && t + 1 < A.T) fetch(t + 1);
+        scores<VPL, SUB>(A, x, s, top, inv);
         float pb = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) pb = fmaf(s[i], b[i], pb);
         pb = sub_sum<SUB>(pb) * inv;
-        if (A.gates_grad) {
-            float z = 0.0f, za = 0.0f;
-            for (int j = sl; j < A.k; j += SUB) {
-                i64 e = -1;
-                float a = 0.0f, v = 0.0f;
-                if (held) { e = rp_load_route(A.routes, A.route_bytes, t * A.route_row + j); a = A.scale * A.gates_grad[t * A.k + j]; }
-                const bool valid = e >= 0 && e < A.E;
-                if (valid) v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv);
-                pick[sub][j] = valid ? (int)e : -1;
-                z += v;
-                za += valid ? v * a : 0.0f;
-            }
-            z = sub_sum<SUB>(z);
-            za = sub_sum<SUB>(za);
+        float add = 0.0f;
+        if (gates) {
+            const float v = valid ? score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv) : 0.0f;
+            float z = v, za = valid ? v * a : 0.0f;
+            for (int o = 1; o < k_lanes; o <<= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); za += __shfl_xor_sync(0xffffffffu, za, o); }
+            // (lanes behind the choices have their own sums: what all lanes need is the first's)
             const float zi = z == 0.0f ? 0.0f : 1.0f / z;
-            for (int j = sl; j < A.k; j += SUB) {
-                const int e = pick[sub][j];
-                if (e < 0) continue;
-                const float a = A.scale * A.gates_grad[t * A.k + j];
-                const float v = score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv);
-                const float ds = A.normalise ? (a - za * zi) * zi : a;
-                add[sub][j] = ds * (soft ? v : v * (1.0f - v));
-            }
-            if (soft && !A.normalise) pb += za;
+            add = (A.normalise ? (a - za * zi) * zi : a) * (soft ? v : v * (1.0f - v));
+            if (soft && !A.normalise) pb += __shfl_sync(0xffffffffu, za, first_lane);
         }
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
             const float p = s[i] * inv;
-            rows[sub][e0 + i] = (b[i] - pb) * (soft ? p : p * (1.0f - s[i]));
+            s[i] = (b[i] - pb) * (soft ? p : p * (1.0f - s[i]));
         }
+#pragma unroll
+        for (int i = 0; i < VPL; i += 4) *(float4 *)&rows[sub][e0 + i] = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
         __syncwarp();
-        if (A.gates_grad && sl == 0 && held)
-            for (int j = 0; j < A.k; ++j)
-                if (pick[sub][j] >= 0) rows[sub][pick[sub][j]] += add[sub][j];
-        __syncwarp();
+        if (gates) {
+            const u32 same = __match_any_sync(0xffffffffu, valid ? (first_lane << 11) + e : 0x40000000 + (int)(threadIdx.x & 31));
+            if (!__any_sync(0xffffffffu, __popc(same) > 1)) {
+                if (valid) rows[sub][e] += add;
+            } else
+                for (int j = 0; j < A.k; ++j) {
+                    if (sl == j && valid) rows[sub][e] += add;
+                    __syncwarp();
+                }
+            __syncwarp();
+        }
         if (there) {
             X *out = (X *)A.dx + t * A.dx_row;
-            if (A.wide) {
 #pragma unroll
-                for (int c = 0; c < VPL; c += 8)
-                    if (e0 + c < A.E) {
-                        float f[8];
+            for (int c = 0; c < VPL; c += 8) {
+                float f[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = held ? rows[sub][e0 + c + i] : 0.0f;
-                        rp_store8(out + e0 + c, rp_close8<X>(f));
-                    }
-            } else
-                for (int i = 0; i < VPL; ++i)
-                    if (e0 + i < A.E) out[e0 + i] = rp_round<X>(held ? rows[sub][e0 + i] : 0.0f);
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 v = *(const float4 *)&rows[sub][e0 + c + i];
+                    f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+                }
+                if (!held) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+                }
+                if (A.wide) {
+                    if (e0 + c < A.E) rp_store8(out + e0 + c, rp_close8<X>(f));
+                } else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (e0 + c + i < A.E) out[e0 + c + i] = rp_round<X>(f[i]);
+            }
         }
         __syncwarp();
     }
@@ -449,7 +517,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
 // ---------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------
-// A lane holds 8 experts (more where a row of E needs more than a warp), so SUB lanes a token.
+// A lane holds 8 experts (more where a row of E needs more than a warp), so SUB lanes a token; never fewer lanes than choices.
 template <typename X, int VPL, int SUB>
 static int launch(RouteArgs &A, bool grad, int sms, cudaStream_t stream)
 {
@@ -482,11 +550,12 @@ static int launch(RouteArgs &A, bool grad, int sms, cudaStream_t stream)
 template <typename X>
 static int launch_for(RouteArgs &A, bool grad, int sms, cudaStream_t stream)
 {
-    if (A.E <= 16) return launch<X, 8, 2>(A, grad, sms, stream);
-    if (A.E <= 32) return launch<X, 8, 4>(A, grad, sms, stream);
-    if (A.E <= 64) return launch<X, 8, 8>(A, grad, sms, stream);
-    if (A.E <= 128) return launch<X, 8, 16>(A, grad, sms, stream);
-    if (A.E <= 256) return launch<X, 8, 32>(A, grad, sms, stream);
+    const int lanes = std::max((A.E + 7) / 8, A.k);
+    if (lanes <= 2) return launch<X, 8, 2>(A, grad, sms, stream);
+    if (lanes <= 4) return launch<X, 8, 4>(A, grad, sms, stream);
+    if (lanes <= 8) return launch<X, 8, 8>(A, grad, sms, stream);
+    if (lanes <= 16) return launch<X, 8, 16>(A, grad, sms, stream);
+    if (lanes <= 32) return launch<X, 8, 32>(A, grad, sms, stream);
     if (A.E <= 512) return launch<X, 16, 32>(A, grad, sms, stream);
     return launch<X, 32, 32>(A, grad, sms, stream);
 }
