@@ -70,8 +70,21 @@ template <int SUB> __device__ __forceinline__ u32 sub_max(u32 v)
     return v;
 }
 
-// A row's VPL elements of a lane, as they lie in memory (16 bytes at a time, or one by one where rows are not on such boundaries).
-template <typename X, int VPL> struct Row { Pack8<X> p[VPL / 8]; };
+// A row's VPL elements of a lane, as they lie in memory: read 16 bytes at a time (then a lane's eight all exist or none does), or one by one where rows are not on such
+// boundaries.  Experts from E on have a logit of -inf: they come behind all others and have a score of 0.
+template <typename X, int VPL> struct Row {
+    Pack8<X> p[VPL / 8];
+    __device__ __forceinline__ Row()
+    {
+#pragma unroll
+        for (int c = 0; c < VPL / 8; ++c)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(X) / 2; ++i) {
+                const u32 w = sizeof(X) == 4 ? 0xff800000u : std::is_same<X, bf16>::value ? 0xff80ff80u : 0xfc00fc00u;
+                p[c].w[i] = make_uint4(w, w, w, w);
+            }
+    }
+};
 template <typename X, int VPL>
 __device__ __forceinline__ void load_row(const RouteArgs &A, i64 t, int e0, Row<X, VPL> &r)
 {
@@ -83,21 +96,15 @@ __device__ __forceinline__ void load_row(const RouteArgs &A, i64 t, int e0, Row<
         } else {
             X x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = e0 + c + i < A.E ? row[c + i] : rp_round<X>(0.0f);
+            for (int i = 0; i < 8; ++i) x[i] = e0 + c + i < A.E ? row[c + i] : rp_round<X>(-INFINITY);
             memcpy(&r.p[c / 8], x, sizeof(x));
         }
     }
 }
-// Experts from E on have a logit of -inf.
-template <typename X, int VPL>
-__device__ __forceinline__ void open_row(const RouteArgs &A, int e0, const Row<X, VPL> &r, float *x)
+template <typename X, int VPL> __device__ __forceinline__ void open_row(const Row<X, VPL> &r, float *x)
 {
 #pragma unroll
     for (int c = 0; c < VPL; c += 8) rp_open8(r.p[c / 8], x + c);
-    if (e0 + VPL > A.E) {
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) x[i] = e0 + i < A.E ? x[i] : -INFINITY;
-    }
 }
 
 __device__ __forceinline__ float reciprocal(float x)        // by the special function unit: 1 ulp
@@ -108,11 +115,18 @@ __device__ __forceinline__ float reciprocal(float x)        // by the special fu
 }
 __device__ __forceinline__ float sigmoid(float x) { return reciprocal(1.0f + rp_exp2(-x * RP_LOG2E)); }
 
+__device__ __forceinline__ float min_or_nan(float x, float y)
+{
+    float z;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+
 // Scores of one token from its logits: softmax: e^(x - max) and 1 / their sum; sigmoid: s, and 1 / their sum.
 // `top` is what the largest logit is taken for: 0 where it is -inf (all scores are 0 then, and so is the inverse).
-// Two sigmoids share a reciprocal, 1 / (1 + a) = (1 + b) / ((1 + a)(1 + b)), which holds while either is above 2^-63; less counts as 0 beside scores of a
-// sum above 2^-40, and rows of nothing but such are worked out one by one.
-template <int VPL, int SUB>
+// SHARED: two sigmoids share a reciprocal, 1 / (1 + a) = (1 + b) / ((1 + a)(1 + b)), where a score of less than 2^-63 counts as 2^-63; rows whose scores add up to
+// less than 2^-40 are worked out one by one.
+template <int VPL, int SUB, bool SHARED>
 __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float *s, float &top, float &inv)
 {
     float sum = 0.0f;
@@ -128,26 +142,25 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
         for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2(fmaf(x[i], RP_LOG2E, shift)); sum += s[i]; }
         sum = sub_sum<SUB>(sum);
     } else {
+        if (SHARED) {
 #pragma unroll
-        for (int i = 0; i < VPL; i += 2) {
-            const float u = x[i] * -RP_LOG2E, v = x[i + 1] * -RP_LOG2E;
-            const float a = 1.0f + rp_exp2(u), b = 1.0f + rp_exp2(v), r = reciprocal(fminf(a, 9.0e18f) * fminf(b, 9.0e18f));
-            // (a comparison that a NaN fails keeps it)
-            s[i] = u > 63.0f ? 0.0f : r * fminf(b, 9.0e18f);
-            s[i + 1] = v > 63.0f ? 0.0f : r * fminf(a, 9.0e18f);
-            if (u != u) s[i] = u;
-            if (v != v) s[i + 1] = v;
-            sum += s[i] + s[i + 1];
+            for (int i = 0; i < VPL; i += 2) {
+                const float a = 1.0f + rp_exp2(min_or_nan(x[i] * -RP_LOG2E, 63.0f)), b = 1.0f + rp_exp2(min_or_nan(x[i + 1] * -RP_LOG2E, 63.0f));
+                const float r = reciprocal(a * b);
+                s[i] = r * b;
+                s[i + 1] = r * a;
+                sum += s[i] + s[i + 1];
+            }
+            sum = sub_sum<SUB>(sum);
         }
-        sum = sub_sum<SUB>(sum);
-        if (__any_sync(0xffffffffu, sum < 1.0e-12f)) {
+        if (!SHARED || __any_sync(0xffffffffu, sum < 1.0e-12f)) {
             sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) { s[i] = sigmoid(x[i]); sum += s[i]; }
             sum = sub_sum<SUB>(sum);
         }
     }
-    inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    inv = sum < 1.2e-38f ? 0.0f : reciprocal(sum);
 }
 // Score of one expert as the gates use it.
 __device__ __forceinline__ float score_of(const RouteArgs &A, float x, float top, float inv)
@@ -163,38 +176,43 @@ __device__ __forceinline__ u32 order_of(float x)
 }
 
 // The k experts with the largest logits, in falling order, ties to the lower one: lane j of the token's gets the j-th, and its logit.
-// 16-bit logits leave their last 13 bits as floats free for the expert's number: keys that are all different and tell it all.  Every lane keeps its two largest; the
-// largest of all goes round by round, and a lane that has had both looks for its next two, those below the one that has just gone.
+// 16-bit logits leave their last 13 bits as floats free for the expert's number: keys that are all different and tell it all.  The largest of all goes round by
+// round; a lane has only its two largest at hand.  Where one that has had both turns out to hold a third of the k (one token in 25 of independent logits,
+// 256 experts and k = 8), the token is done again by lanes that look for their next key each time.
 template <int VPL, int SUB>
 __device__ __forceinline__ void choose_by_keys(const RouteArgs &A, const float *x, int e0, int sl, i64 &e, float &xe)
 {
     u32 key[VPL], first = 0, second = 0;
+    const u32 code = (u32)(1023 - e0) | 0x400u;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-        key[i] = (order_of(x[i]) & ~0x1fffu) | (u32)(1023 - e0 - i) | 0x400u;
-        if (e0 + VPL > A.E) key[i] = e0 + i < A.E ? key[i] : 0u;
+        key[i] = (order_of(x[i]) & ~0x1fffu) | (code - i);
         first = max(first, key[i]);
     }
 #pragma unroll
     for (int i = 0; i < VPL; ++i) second = max(second, key[i] - first);      // (those below it wrap around to the largest numbers, in their order)
     second += first;
-    u32 mine = 0;
+    u32 mine = 0, best = 0;
+    bool both = false;
     for (int j = 0; j < A.k; ++j) {
-        const u32 best = sub_max<SUB>(first);
+        best = sub_max<SUB>(first);
         if (sl == j) mine = best;
-        const bool gone = first == best;
-        const bool both = gone && second == 0;
-        if (gone) { first = second; second = 0; }
-        if (__any_sync(0xffffffffu, both)) {
-            u32 f = 0, g = 0;
+        if (first == best) { both = second == 0; first = second; second = 0; }
+    }
+    if (__any_sync(0xffffffffu, both)) {
+        int more = 0;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) f = max(f, key[i] - best);
-            f += best;
+        for (int i = 0; i < VPL; ++i) more += key[i] >= best;
+        if (__any_sync(0xffffffffu, both && more > 2)) {
+            u32 limit = 0;
+            for (int j = 0; j < A.k; ++j) {
+                u32 f = 0;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) g = max(g, key[i] - f);
-            g += f;
-            // (no key below: the wrapped distances are those of keys that have gone, which come back at `best` or above)
-            if (both) { first = f < best ? f : 0u; second = g < f && f < best ? g : 0u; }
+                for (int i = 0; i < VPL; ++i) f = max(f, key[i] - limit);
+                best = sub_max<SUB>(f) + limit;
+                if (sl == j) mine = best;
+                limit = best;
+            }
         }
     }
     e = 1023 - (int)(mine & 0x3ffu);
@@ -293,7 +311,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
     float acc[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) acc[i] = 0.0f;
-    Row<X, VPL> row = Row<X, VPL>();
+    Row<X, VPL> row;
     if (t0 < A.T) load_row<X, VPL>(A, t0, e0, row);
     int k_lanes = 1;                                                      // lanes that the sum over the chosen goes over
     while (k_lanes < A.k) k_lanes <<= 1;
@@ -301,12 +319,12 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
         const i64 t = t0 + step;
         const bool there = t < A.T;
         float x[VPL], s[VPL], top = 0.0f, inv = 0.0f, xe = 0.0f;
-        open_row<X, VPL>(A, e0, row, x);
+        open_row<X, VPL>(row, x);
         if (step + 1 < A.run && t + 1 < A.T) load_row<X, VPL>(A, t + 1, e0, row);
         // lane j of the token's has its j-th choice (there are at least k of them)
         i64 e = -1;
         if (A.replay && there && sl < A.k) e = rp_load_route(A.routes, A.route_bytes, t * A.route_row + sl);
-        if (want_loss || A.score == RP_SCORE_SOFTMAX || A.bias) scores<VPL, SUB>(A, x, s, top, inv);
+        if (want_loss || A.score == RP_SCORE_SOFTMAX || A.bias) scores<VPL, SUB, true>(A, x, s, top, inv);
         if (!A.replay) {
             if (sizeof(X) == 2 && !A.bias) choose_by_keys<VPL, SUB>(A, x, e0, sl, e, xe);
             else {
@@ -324,7 +342,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
         if (A.normalise) {
             float total = v;
             for (int o = 1; o < k_lanes; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            gate = total == 0.0f ? 0.0f : gate / total;
+            gate = total < 1.2e-38f ? 0.0f : gate * reciprocal(total);
         }
         if (there && t >= next) {
             // another group: what the run has of the one before goes out
@@ -425,7 +443,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
     float b[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) b[i] = 0.0f;
-    Row<X, VPL> row = Row<X, VPL>();
+    Row<X, VPL> row;
     // lane j of the token's has its j-th choice
     i64 e_next = -1;
     float a_next = 0.0f;
@@ -449,12 +467,12 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
         }
         const bool held = there && g >= 0 && g < A.G;
         float x[VPL], s[VPL], top, inv;
-        open_row<X, VPL>(A, e0, row, x);
+        open_row<X, VPL>(row, x);
         const bool valid = gates && held && sl < A.k && e_next >= 0 && e_next < A.E;
         const int e = valid ? (int)e_next : -1;
         const float a = A.scale * a_next;
         if (step + 1 < A.run && t + 1 < A.T) fetch(t + 1);
-        scores<VPL, SUB>(A, x, s, top, inv);
+        scores<VPL, SUB, false>(A, x, s, top, inv);
         float pb = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) pb = fmaf(s[i], b[i], pb);
@@ -465,7 +483,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
             float z = v, za = valid ? v * a : 0.0f;
             for (int o = 1; o < k_lanes; o <<= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); za += __shfl_xor_sync(0xffffffffu, za, o); }
             // (lanes behind the choices have their own sums: what all lanes need is the first's)
-            const float zi = z == 0.0f ? 0.0f : 1.0f / z;
+            const float zi = z < 1.2e-38f ? 0.0f : reciprocal(z);
             add = (A.normalise ? (a - za * zi) * zi : a) * (soft ? v : v * (1.0f - v));
             if (soft && !A.normalise) pb += __shfl_sync(0xffffffffu, za, first_lane);
         }
