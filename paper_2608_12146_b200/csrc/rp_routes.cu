@@ -20,48 +20,156 @@ struct CountArgs {
     int L, k, E, N;
     const i64 *start;
     int *demand;
-    int layers;             // layers of a CTA
+    int lanes;              // lanes of a warp that share a token: 4 where a token's layers lie side by side, 1 where a layer's tokens do
+    int rows;               // experts of the counters in shared memory
     i64 tile;               // tokens of a CTA
 };
 
-#define COUNT_THREADS 256
-// A CTA owns a tile of tokens and a range of layers, whatever samples they belong to: it counts one sample after the other in shared memory and
-// adds what it found to the output (whole numbers: the order does not matter).
-template <typename R>
-__global__ void __launch_bounds__(COUNT_THREADS) k_count_routes(CountArgs A)
+#define COUNT_THREADS 512
+#define COUNT_SHORT 16      // samples of fewer tokens in a tile are counted in global memory at once
+// A lane's counters lie in a bank of its own (counter of expert e at e * 32 + lane), so that the 32 additions of a warp go in one go whatever they count; with one
+// counter for all lanes, skewed choices put 3 to 4 of them in one bank (900001 tokens of 32 layers, 8 of 128 experts in bytes: 207 us).
+template <int ENTRY> __device__ __forceinline__ void count_word(u32 at, u32 w, u32 hi, int E)
 {
-    extern __shared__ int hist[];                        // [layers][E]
+    if constexpr (ENTRY == 1) {
+        // 256 rows of counters: any byte has one
+        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w << 7) & 0x7f80u)) : "memory");
+        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w >> 1) & 0x7f80u)) : "memory");
+        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w >> 9) & 0x7f80u)) : "memory");
+        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w >> 17) & 0x7f80u)) : "memory");
+    } else if constexpr (ENTRY == 2) {
+        const u32 e = w & 0xffffu, f = w >> 16;
+        if (e < (u32)E) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + e * 128) : "memory");
+        if (f < (u32)E) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + f * 128) : "memory");
+    } else {
+        if (w < (u32)E && hi == 0) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + w * 128) : "memory");
+    }
+}
+// A CTA owns a tile of tokens and lanes * LAYERS layers, whatever samples the tokens belong to: it counts one sample after the other in shared memory and adds what
+// it found to the output (whole numbers: the order does not matter).  WORDS: 32-bit words of a token's choices in LAYERS layers, read as such; 0: any number of
+// choices, read one by one.
+template <typename R, int WORDS, int LAYERS>
+__global__ void __launch_bounds__(COUNT_THREADS, 3) k_count_routes(CountArgs A)
+{
+    extern __shared__ __align__(16) u32 hist[];          // [LAYERS][rows][32]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const i64 t0 = (i64)blockIdx.x * A.tile, t1 = min(A.T, t0 + A.tile);
-    const int l0 = blockIdx.y * A.layers, nl = min(A.L - l0, A.layers);
+    const int l0 = blockIdx.y * A.lanes * LAYERS, layer = l0 + lane % A.lanes * LAYERS;      // first of the CTA, first of the lane
+    const int per = 32 / A.lanes, tok = lane / A.lanes;  // tokens of a warp at a time
     const R *routes = (const R *)A.routes;
-    for (int x = threadIdx.x; x < nl * A.E; x += COUNT_THREADS) hist[x] = 0;
+    for (int x = threadIdx.x; x < LAYERS * A.rows * 8; x += COUNT_THREADS) ((uint4 *)hist)[x] = make_uint4(0, 0, 0, 0);
     __syncthreads();
+    const u32 base = (u32)__cvta_generic_to_shared(hist) + lane * 4;
     for (i64 t = t0; t < t1;) {
         const int i = rp_sample_of(A.start, A.N, t);
         i64 end = t1;
         if (i < A.N) end = min(end, __ldg(A.start + i + 1));
         if (end <= t) end = t + 1;                       // starts that decrease: every step makes headway all the same
         if (i >= 0 && i < A.N) {
-            const i64 items = (end - t) * nl;
-            for (i64 x = threadIdx.x; x < items; x += COUNT_THREADS) {
-                const i64 tok = A.ls < A.ts ? x / nl : x % (end - t);
-                const int l = (int)(A.ls < A.ts ? x % nl : x / (end - t));
-                const R *at = routes + (t + tok) * A.ts + (l0 + l) * A.ls;
-                for (int j = 0; j < A.k; ++j) {
-                    const i64 e = (i64)at[j];
-                    if (e >= 0 && e < A.E) atomicAdd(&hist[l * A.E + (int)e], 1);
+            int *out = A.demand + ((i64)i * A.L + l0) * A.E;
+            const int layers = min(A.L - l0, A.lanes * LAYERS);
+            if (end - t < COUNT_SHORT) {
+                const int items = (int)(end - t) * layers * A.k;
+                for (int x = threadIdx.x; x < items; x += COUNT_THREADS) {
+                    const int j = x % A.k, l = x / A.k % layers;
+                    const i64 e = (i64)routes[(t + x / A.k / layers) * A.ts + (l0 + l) * A.ls + j];
+                    if (e >= 0 && e < A.E) atomicAdd(out + l * A.E + (int)e, 1);
+                }
+                t = end;
+                continue;
+            }
+            if (layer < A.L) {
+                const R *at = routes + layer * A.ls;
+                if constexpr (WORDS > 0) {
+                    constexpr int AHEAD = WORDS <= 4 ? 4 : 2;        // tokens of a lane under way
+                    const i64 step = (i64)(COUNT_THREADS / 32) * per;
+                    for (i64 x = t + warp * per + tok; x < end; x += AHEAD * step) {
+                        u32 w[AHEAD][WORDS];
+#pragma unroll
+                        for (int u = 0; u < AHEAD; ++u) {
+                            const u32 *p = (const u32 *)(at + min(x + u * step, end - 1) * A.ts);
+                            if constexpr (WORDS % 4 == 0) {
+#pragma unroll
+                                for (int v = 0; v < WORDS; v += 4) {
+                                    const uint4 q = __ldcs((const uint4 *)(p + v));      // read once
+                                    w[u][v] = q.x; w[u][v + 1] = q.y; w[u][v + 2] = q.z; w[u][v + 3] = q.w;
+                                }
+                            } else if constexpr (WORDS == 2) {
+                                const uint2 q = __ldcs((const uint2 *)p);
+                                w[u][0] = q.x; w[u][1] = q.y;
+                            } else
+                                w[u][0] = __ldcs(p);
+                        }
+#pragma unroll
+                        for (int u = 0; u < AHEAD; ++u) {
+                            if (x + u * step >= end) break;
+#pragma unroll
+                            for (int v = 0; v < WORDS; ++v) {
+                                const u32 to = base + v / (WORDS / LAYERS) * A.rows * 128;
+                                if constexpr (sizeof(R) < 8) count_word<sizeof(R)>(to, w[u][v], 0, A.E);
+                                else if (v % 2 == 0) count_word<8>(to, w[u][v], w[u][v + 1], A.E);
+                            }
+                        }
+                    }
+                } else {
+                    for (i64 x = t + warp * per + tok; x < end; x += (i64)(COUNT_THREADS / 32) * per)
+                        for (int j = 0; j < A.k; ++j) {
+                            const i64 e = (i64)at[x * A.ts + j];
+                            if (e >= 0 && e < A.E) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(base + (u32)e * 128) : "memory");
+                        }
                 }
             }
             __syncthreads();
-            int *out = A.demand + ((i64)i * A.L + l0) * A.E;
-            for (int x = threadIdx.x; x < nl * A.E; x += COUNT_THREADS) {
-                const int c = hist[x];
-                if (c) { atomicAdd(out + x, c); hist[x] = 0; }
-            }
+            // Eight lanes add up an expert's 32 counters; those of lanes that share a token are layers of their own: at the end lane q of the eight has the sum of the
+            // counters q mod 4 of four lanes, and its neighbour four lanes on that of the others.
+#pragma unroll
+            for (int sub = 0; sub < LAYERS; ++sub)
+                for (int first = warp * 4; first < A.E; first += COUNT_THREADS / 8) {        // (the whole warp goes round as often)
+                    const int e = first + (lane >> 3), q = lane & 3, l = q * LAYERS + sub;
+                    uint4 *p = (uint4 *)(hist + (sub * A.rows + e) * 32) + (lane & 7), c = make_uint4(0, 0, 0, 0);
+                    if (e < A.E) { c = *p; *p = make_uint4(0, 0, 0, 0); }
+                    const bool odd = lane & 1, high = lane & 2;
+                    // the pair's even lane goes on with x and z, the odd one with y and w; of two pairs the lower with the first of those
+                    const u32 k0 = (odd ? c.y : c.x) + __shfl_xor_sync(0xffffffffu, odd ? c.x : c.y, 1);
+                    const u32 k1 = (odd ? c.w : c.z) + __shfl_xor_sync(0xffffffffu, odd ? c.z : c.w, 1);
+                    u32 v = (high ? k1 : k0) + __shfl_xor_sync(0xffffffffu, high ? k0 : k1, 2);
+                    v += __shfl_xor_sync(0xffffffffu, v, 4);
+                    if (A.lanes == 1) { v += __shfl_xor_sync(0xffffffffu, v, 1); v += __shfl_xor_sync(0xffffffffu, v, 2); }
+                    if ((lane & 7) < A.lanes && v && e < A.E && l < layers) atomicAdd(out + l * A.E + e, (int)v);
+                }
             __syncthreads();
         }
         t = end;
     }
+}
+
+template <typename R>
+static int launch_count(CountArgs &A, int sms, cudaStream_t stream)
+{
+    const int bytes = A.k * (int)sizeof(R);
+    const auto words = [&](int n) {                      // can a token's choices be read as n bytes at a time?
+        const int w = n >= 16 ? 16 : n;
+        return rp_aligned(A.routes, w) && A.ts * (i64)sizeof(R) % w == 0 && (A.lanes == 1 && A.L == 1 ? true : A.ls * (i64)sizeof(R) % w == 0);
+    };
+    // Bytes of eight choices: two layers of a lane's in 16 bytes (one layer in 8 leaves half of every 64 bytes from memory to another CTA)
+    const bool two = sizeof(R) == 1 && bytes == 8 && A.lanes == 4 && A.ls == A.k && A.L % 2 == 0 && A.L >= 8 && rp_aligned(A.routes, 16) && A.ts % 16 == 0;
+    void (*f)(CountArgs) = k_count_routes<R, 0, 1>;
+    const int layers = two ? 2 : 1;
+    if (two) { if constexpr (sizeof(R) == 1) f = k_count_routes<R, 4, 2>; }
+    else if (bytes == 4 && words(4)) f = k_count_routes<R, sizeof(R) == 8 ? 2 : 1, 1>;
+    else if (bytes == 8 && words(8)) f = k_count_routes<R, 2, 1>;
+    else if (bytes == 16 && words(16)) f = k_count_routes<R, 4, 1>;
+    else if (bytes == 32 && words(16)) f = k_count_routes<R, 8, 1>;
+    else if (bytes == 64 && words(16)) f = k_count_routes<R, 16, 1>;
+    A.rows = sizeof(R) == 1 ? 256 : A.E;
+    const size_t smem = (size_t)layers * A.rows * 128;
+    if (smem > 48 * 1024) RP_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, RP_SMEM_LIMIT));
+    // as many CTAs as stay resident; a tile is not so short that setting its counters to zero and adding them up costs more than counting
+    const int groups = (A.L + A.lanes * layers - 1) / (A.lanes * layers);
+    const i64 resident = (i64)sms * std::min((size_t)3, (size_t)(224 * 1024) / (smem + 1024));
+    A.tile = std::max((A.T + std::max((i64)1, resident / groups) - 1) / std::max((i64)1, resident / groups), (i64)256);
+    f<<<dim3((unsigned)((A.T + A.tile - 1) / A.tile), groups), COUNT_THREADS, smem, stream>>>(A);
+    return rp_op_launched();
 }
 
 // Queues the count on a stream of the current device; `demand` is written whole.
@@ -70,20 +178,14 @@ int rp_launch_count(int device, const void *routes, int bytes, i64 T, int L, int
 {
     RP_CUDA(cudaMemsetAsync(demand, 0, sizeof(int) * (size_t)N * L * E, stream));
     if (T < 1) return RP_OK;
-    CountArgs A = { routes, T, ts, ls, L, k, E, N, start, demand, 0, 0 };
-    A.layers = std::max(1, std::min(L, 32 * 1024 / 4 / E));
-    const int groups = (L + A.layers - 1) / A.layers;
-    const i64 want = std::max((i64)1, (i64)rp_op_sms(device) * 8 / groups);
-    A.tile = std::max((T + want - 1) / want, (i64)16);
-    const dim3 grid((unsigned)((T + A.tile - 1) / A.tile), groups);
-    const size_t smem = sizeof(int) * (size_t)A.layers * E;
+    CountArgs A = { routes, T, ts, ls, L, k, E, N, start, demand, ls < ts && L > 1 ? 4 : 1, 0, 0 };
+    const int sms = rp_op_sms(device);
     switch (bytes) {
-        case 1: k_count_routes<unsigned char><<<grid, COUNT_THREADS, smem, stream>>>(A); break;
-        case 2: k_count_routes<short><<<grid, COUNT_THREADS, smem, stream>>>(A); break;
-        case 4: k_count_routes<int><<<grid, COUNT_THREADS, smem, stream>>>(A); break;
-        default: k_count_routes<i64><<<grid, COUNT_THREADS, smem, stream>>>(A); break;
+        case 1: return launch_count<unsigned char>(A, sms, stream);
+        case 2: return launch_count<short>(A, sms, stream);
+        case 4: return launch_count<int>(A, sms, stream);
+        default: return launch_count<i64>(A, sms, stream);
     }
-    return rp_op_launched();
 }
 
 // start[i] = lengths[0] + .. + lengths[i-1], by one CTA (N <= 2^20).
