@@ -26,99 +26,110 @@ struct CountArgs {
 };
 
 #define COUNT_THREADS 512
-#define COUNT_SHORT 16      // samples of fewer tokens in a tile are counted in global memory at once
 // A lane's counters lie in a bank of its own (counter of expert e at e * 32 + lane), so that the 32 additions of a warp go in one go whatever they count; with one
 // counter for all lanes, skewed choices put 3 to 4 of them in one bank (900001 tokens of 32 layers, 8 of 128 experts in bytes: 207 us).
+__device__ __forceinline__ void count_one(u32 at, u32 e)
+{
+    u32 to;
+    asm("mad.lo.u32 %0, %1, 128, %2;" : "=r"(to) : "r"(e), "r"(at));
+    asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(to) : "memory");
+}
 template <int ENTRY> __device__ __forceinline__ void count_word(u32 at, u32 w, u32 hi, int E)
 {
     if constexpr (ENTRY == 1) {
         // 256 rows of counters: any byte has one
-        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w << 7) & 0x7f80u)) : "memory");
-        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w >> 1) & 0x7f80u)) : "memory");
-        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w >> 9) & 0x7f80u)) : "memory");
-        asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + ((w >> 17) & 0x7f80u)) : "memory");
+#pragma unroll
+        for (int b = 0; b < 4; ++b) count_one(at, __byte_perm(w, 0, 0x4440 | b));
     } else if constexpr (ENTRY == 2) {
-        const u32 e = w & 0xffffu, f = w >> 16;
-        if (e < (u32)E) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + e * 128) : "memory");
-        if (f < (u32)E) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + f * 128) : "memory");
+        if ((w & 0xffffu) < (u32)E) count_one(at, w & 0xffffu);
+        if ((w >> 16) < (u32)E) count_one(at, w >> 16);
     } else {
-        if (w < (u32)E && hi == 0) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(at + w * 128) : "memory");
+        if (w < (u32)E && hi == 0) count_one(at, w);
     }
 }
 // A CTA owns a tile of tokens and lanes * LAYERS layers, whatever samples the tokens belong to: it counts one sample after the other in shared memory and adds what
-// it found to the output (whole numbers: the order does not matter).  WORDS: 32-bit words of a token's choices in LAYERS layers, read as such; 0: any number of
-// choices, read one by one.
+// it found to the output (whole numbers: the order does not matter).  WORDS: 32-bit words of a token's choices in LAYERS layers, copied as such into a ring of the
+// lane's own, DEPTH tokens ahead, across the samples' ends; 0: any number of choices, read one by one.
+template <int WORDS> struct CountRing { static constexpr int DEPTH = WORDS <= 4 ? 4 : WORDS == 8 ? 3 : 2, BYTES = WORDS ? DEPTH * WORDS * 4 * COUNT_THREADS : 0; };
 template <typename R, int WORDS, int LAYERS>
-__global__ void __launch_bounds__(COUNT_THREADS, 3) k_count_routes(CountArgs A)
+__global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
 {
-    extern __shared__ __align__(16) u32 hist[];          // [LAYERS][rows][32]
+    constexpr int DEPTH = CountRing<WORDS>::DEPTH, COPY = WORDS >= 4 ? 16 : 4 * WORDS;       // bytes of a copy
+    extern __shared__ __align__(16) u32 hist[];          // [LAYERS][rows][32], ring
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const i64 t0 = (i64)blockIdx.x * A.tile, t1 = min(A.T, t0 + A.tile);
     const int l0 = blockIdx.y * A.lanes * LAYERS, layer = l0 + lane % A.lanes * LAYERS;      // first of the CTA, first of the lane
-    const int per = 32 / A.lanes, tok = lane / A.lanes;  // tokens of a warp at a time
+    const int per = 32 / A.lanes, step = COUNT_THREADS / 32 * per;                          // tokens of a warp, of the CTA at a time
     const R *routes = (const R *)A.routes;
-    for (int x = threadIdx.x; x < LAYERS * A.rows * 8; x += COUNT_THREADS) ((uint4 *)hist)[x] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
     const u32 base = (u32)__cvta_generic_to_shared(hist) + lane * 4;
+    // the lane's tokens: x, x + step, ..; fetched so far: up to `far`
+    i64 x = layer < A.L ? t0 + warp * per + lane / A.lanes : t1, far = x;
+    const i64 inc = step * A.ts * (i64)sizeof(R);
+    const char *from = (const char *)(routes + (layer < A.L ? layer * A.ls + x * A.ts : 0));
+    const char *ring = (const char *)(hist + LAYERS * A.rows * 32) + threadIdx.x * (COPY ? COPY : 4);
+    const u32 ring_at = (u32)__cvta_generic_to_shared(ring);
+    auto fetch = [&](int slot) {
+        if constexpr (WORDS > 0) {
+            if (far < t1) {
+                const u32 to = ring_at + slot * (WORDS * 4 * COUNT_THREADS);
+                if constexpr (COPY == 16) {
+#pragma unroll
+                    for (int v = 0; v < WORDS / 4; ++v)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + v * 16 * COUNT_THREADS), "l"(from + 16 * v) : "memory");
+                } else
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(COPY ? COPY : 4) : "memory");
+                from += inc;
+                far += step;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    int slot = 0;
+#pragma unroll
+    for (int u = 0; u < DEPTH; ++u) fetch(u);
+    for (int y = threadIdx.x; y < LAYERS * A.rows * 8; y += COUNT_THREADS) ((uint4 *)hist)[y] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
     for (i64 t = t0; t < t1;) {
         const int i = rp_sample_of(A.start, A.N, t);
         i64 end = t1;
         if (i < A.N) end = min(end, __ldg(A.start + i + 1));
         if (end <= t) end = t + 1;                       // starts that decrease: every step makes headway all the same
-        if (i >= 0 && i < A.N) {
-            int *out = A.demand + ((i64)i * A.L + l0) * A.E;
-            const int layers = min(A.L - l0, A.lanes * LAYERS);
-            if (end - t < COUNT_SHORT) {
-                const int items = (int)(end - t) * layers * A.k;
-                for (int x = threadIdx.x; x < items; x += COUNT_THREADS) {
-                    const int j = x % A.k, l = x / A.k % layers;
-                    const i64 e = (i64)routes[(t + x / A.k / layers) * A.ts + (l0 + l) * A.ls + j];
-                    if (e >= 0 && e < A.E) atomicAdd(out + l * A.E + (int)e, 1);
-                }
-                t = end;
-                continue;
-            }
-            if (layer < A.L) {
-                const R *at = routes + layer * A.ls;
-                if constexpr (WORDS > 0) {
-                    constexpr int AHEAD = WORDS <= 4 ? 4 : 2;        // tokens of a lane under way
-                    const i64 step = (i64)(COUNT_THREADS / 32) * per;
-                    for (i64 x = t + warp * per + tok; x < end; x += AHEAD * step) {
-                        u32 w[AHEAD][WORDS];
+        const bool held = i >= 0 && i < A.N;
+        if constexpr (WORDS > 0) {
+            for (; x < end; x += step) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+                u32 w[WORDS];
+                const char *p = ring + slot * (WORDS * 4 * COUNT_THREADS);
+                if constexpr (COPY == 16) {
 #pragma unroll
-                        for (int u = 0; u < AHEAD; ++u) {
-                            const u32 *p = (const u32 *)(at + min(x + u * step, end - 1) * A.ts);
-                            if constexpr (WORDS % 4 == 0) {
-#pragma unroll
-                                for (int v = 0; v < WORDS; v += 4) {
-                                    const uint4 q = __ldcs((const uint4 *)(p + v));      // read once
-                                    w[u][v] = q.x; w[u][v + 1] = q.y; w[u][v + 2] = q.z; w[u][v + 3] = q.w;
-                                }
-                            } else if constexpr (WORDS == 2) {
-                                const uint2 q = __ldcs((const uint2 *)p);
-                                w[u][0] = q.x; w[u][1] = q.y;
-                            } else
-                                w[u][0] = __ldcs(p);
-                        }
-#pragma unroll
-                        for (int u = 0; u < AHEAD; ++u) {
-                            if (x + u * step >= end) break;
-#pragma unroll
-                            for (int v = 0; v < WORDS; ++v) {
-                                const u32 to = base + v / (WORDS / LAYERS) * A.rows * 128;
-                                if constexpr (sizeof(R) < 8) count_word<sizeof(R)>(to, w[u][v], 0, A.E);
-                                else if (v % 2 == 0) count_word<8>(to, w[u][v], w[u][v + 1], A.E);
-                            }
-                        }
+                    for (int v = 0; v < WORDS; v += 4) {
+                        const uint4 q = *(const uint4 *)(p + v * 4 * COUNT_THREADS);
+                        w[v] = q.x; w[v + 1] = q.y; w[v + 2] = q.z; w[v + 3] = q.w;
                     }
                 } else {
-                    for (i64 x = t + warp * per + tok; x < end; x += (i64)(COUNT_THREADS / 32) * per)
-                        for (int j = 0; j < A.k; ++j) {
-                            const i64 e = (i64)at[x * A.ts + j];
-                            if (e >= 0 && e < A.E) asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(base + (u32)e * 128) : "memory");
-                        }
+#pragma unroll
+                    for (int v = 0; v < WORDS; ++v) w[v] = ((const u32 *)p)[v];
                 }
+                fetch(slot);
+                slot = slot + 1 == DEPTH ? 0 : slot + 1;
+                if (held)
+#pragma unroll
+                    for (int v = 0; v < WORDS; ++v) {
+                        const u32 to = base + v / (WORDS / LAYERS) * A.rows * 128;
+                        if constexpr (sizeof(R) < 8) count_word<sizeof(R)>(to, w[v], 0, A.E);
+                        else if (v % 2 == 0) count_word<8>(to, w[v], w[v + 1], A.E);
+                    }
             }
+        } else {
+            for (; x < end; x += step)
+                for (int j = 0; held && j < A.k; ++j) {
+                    const i64 e = (i64)routes[x * A.ts + layer * A.ls + j];
+                    if (e >= 0 && e < A.E) count_one(base, (u32)e);
+                }
+        }
+        if (held) {
+            int *out = A.demand + ((i64)i * A.L + l0) * A.E;
+            const int layers = min(A.L - l0, A.lanes * LAYERS);
             __syncthreads();
             // Eight lanes add up an expert's 32 counters; those of lanes that share a token are layers of their own: at the end lane q of the eight has the sum of the
             // counters q mod 4 of four lanes, and its neighbour four lanes on that of the others.
@@ -155,18 +166,20 @@ static int launch_count(CountArgs &A, int sms, cudaStream_t stream)
     const bool two = sizeof(R) == 1 && bytes == 8 && A.lanes == 4 && A.ls == A.k && A.L % 2 == 0 && A.L >= 8 && rp_aligned(A.routes, 16) && A.ts % 16 == 0;
     void (*f)(CountArgs) = k_count_routes<R, 0, 1>;
     const int layers = two ? 2 : 1;
-    if (two) { if constexpr (sizeof(R) == 1) f = k_count_routes<R, 4, 2>; }
-    else if (bytes == 4 && words(4)) f = k_count_routes<R, sizeof(R) == 8 ? 2 : 1, 1>;
-    else if (bytes == 8 && words(8)) f = k_count_routes<R, 2, 1>;
-    else if (bytes == 16 && words(16)) f = k_count_routes<R, 4, 1>;
-    else if (bytes == 32 && words(16)) f = k_count_routes<R, 8, 1>;
-    else if (bytes == 64 && words(16)) f = k_count_routes<R, 16, 1>;
+    size_t ring = 0;
+    const auto pick = [&](void (*g)(CountArgs), int bytes_ahead) { f = g; ring = bytes_ahead; };
+    if (two) { if constexpr (sizeof(R) == 1) pick(k_count_routes<R, 4, 2>, CountRing<4>::BYTES); }
+    else if (bytes == 4 && words(4)) { if constexpr (sizeof(R) <= 4) pick(k_count_routes<R, 1, 1>, CountRing<1>::BYTES); }
+    else if (bytes == 8 && words(8)) pick(k_count_routes<R, 2, 1>, CountRing<2>::BYTES);
+    else if (bytes == 16 && words(16)) pick(k_count_routes<R, 4, 1>, CountRing<4>::BYTES);
+    else if (bytes == 32 && words(16)) pick(k_count_routes<R, 8, 1>, CountRing<8>::BYTES);
+    else if (bytes == 64 && words(16)) pick(k_count_routes<R, 16, 1>, CountRing<16>::BYTES);
     A.rows = sizeof(R) == 1 ? 256 : A.E;
-    const size_t smem = (size_t)layers * A.rows * 128;
+    const size_t smem = (size_t)layers * A.rows * 128 + ring;
     if (smem > 48 * 1024) RP_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, RP_SMEM_LIMIT));
     // as many CTAs as stay resident; a tile is not so short that setting its counters to zero and adding them up costs more than counting
     const int groups = (A.L + A.lanes * layers - 1) / (A.lanes * layers);
-    const i64 resident = (i64)sms * std::min((size_t)3, (size_t)(224 * 1024) / (smem + 1024));
+    const i64 resident = (i64)sms * std::min((size_t)2, (size_t)(224 * 1024) / (smem + 1024));
     A.tile = std::max((A.T + std::max((i64)1, resident / groups) - 1) / std::max((i64)1, resident / groups), (i64)256);
     f<<<dim3((unsigned)((A.T + A.tile - 1) / A.tile), groups), COUNT_THREADS, smem, stream>>>(A);
     return rp_op_launched();
