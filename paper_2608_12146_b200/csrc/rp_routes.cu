@@ -22,7 +22,6 @@ struct CountArgs {
     int *demand;
     int lanes;              // lanes of a warp that share a token: 4 where a token's layers lie side by side, 1 where a layer's tokens do
     int rows;               // experts of the counters in shared memory
-    i64 tile;               // tokens of a CTA
 };
 
 #define COUNT_THREADS 512
@@ -47,6 +46,22 @@ template <int ENTRY> __device__ __forceinline__ void count_word(u32 at, u32 w, u
         if (w < (u32)E && hi == 0) count_one(at, w);
     }
 }
+// Where tile b of n begins: a sample's end costs as much as COUNT_END tokens (two meetings of the CTA, and adding up its counters), and the tiles are of one cost.
+#define COUNT_END 160
+__device__ __forceinline__ i64 tile_start(const CountArgs &A, int b, int n)
+{
+    if (b <= 0) return 0;
+    if (b >= n) return A.T;
+    const i64 cost = A.T + (i64)COUNT_END * A.N, want = cost / n * b + cost % n * b / n;
+    int lo = 0, hi = A.N + 1;                            // first i with start[i] + COUNT_END * i above it
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(A.start + mid) + (i64)COUNT_END * mid <= want) lo = mid + 1; else hi = mid;
+    }
+    i64 t = want - (i64)COUNT_END * max(lo - 1, 0);
+    if (lo <= A.N) t = min(t, __ldg(A.start + lo));
+    return min(max(t, (i64)0), A.T);
+}
 // A CTA owns a tile of tokens and lanes * LAYERS layers, whatever samples the tokens belong to: it counts one sample after the other in shared memory and adds what
 // it found to the output (whole numbers: the order does not matter).  WORDS: 32-bit words of a token's choices in LAYERS layers, copied as such into a ring of the
 // lane's own, DEPTH tokens ahead, across the samples' ends; 0: any number of choices, read one by one.
@@ -57,20 +72,21 @@ __global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
     constexpr int DEPTH = CountRing<WORDS>::DEPTH, COPY = WORDS >= 4 ? 16 : 4 * WORDS;       // bytes of a copy
     extern __shared__ __align__(16) u32 hist[];          // [LAYERS][rows][32], ring
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const i64 t0 = (i64)blockIdx.x * A.tile, t1 = min(A.T, t0 + A.tile);
+    const i64 t0 = tile_start(A, blockIdx.x, gridDim.x), t1 = max(t0, tile_start(A, blockIdx.x + 1, gridDim.x));
     const int l0 = blockIdx.y * A.lanes * LAYERS, layer = l0 + lane % A.lanes * LAYERS;      // first of the CTA, first of the lane
     const int per = 32 / A.lanes, step = COUNT_THREADS / 32 * per;                          // tokens of a warp, of the CTA at a time
     const R *routes = (const R *)A.routes;
     const u32 base = (u32)__cvta_generic_to_shared(hist) + lane * 4;
-    // the lane's tokens: x, x + step, ..; fetched so far: up to `far`
-    i64 x = layer < A.L ? t0 + warp * per + lane / A.lanes : t1, far = x;
+    // the lane's tokens, from the tile's first: x, x + step, ..; fetched so far: up to `far`
+    const int len = (int)(t1 - t0);
+    int x = layer < A.L ? warp * per + lane / A.lanes : len, far = x;
     const i64 inc = step * A.ts * (i64)sizeof(R);
-    const char *from = (const char *)(routes + (layer < A.L ? layer * A.ls + x * A.ts : 0));
+    const char *from = (const char *)(routes + (layer < A.L ? layer * A.ls + (t0 + x) * A.ts : 0));
     const char *ring = (const char *)(hist + LAYERS * A.rows * 32) + threadIdx.x * (COPY ? COPY : 4);
     const u32 ring_at = (u32)__cvta_generic_to_shared(ring);
     auto fetch = [&](int slot) {
         if constexpr (WORDS > 0) {
-            if (far < t1) {
+            if (far < len) {
                 const u32 to = ring_at + slot * (WORDS * 4 * COUNT_THREADS);
                 if constexpr (COPY == 16) {
 #pragma unroll
@@ -95,8 +111,9 @@ __global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
         if (i < A.N) end = min(end, __ldg(A.start + i + 1));
         if (end <= t) end = t + 1;                       // starts that decrease: every step makes headway all the same
         const bool held = i >= 0 && i < A.N;
+        const int stop = (int)(end - t0);
         if constexpr (WORDS > 0) {
-            for (; x < end; x += step) {
+            for (; x < stop; x += step) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
                 u32 w[WORDS];
                 const char *p = ring + slot * (WORDS * 4 * COUNT_THREADS);
@@ -121,9 +138,9 @@ __global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
                     }
             }
         } else {
-            for (; x < end; x += step)
+            for (; x < stop; x += step)
                 for (int j = 0; held && j < A.k; ++j) {
-                    const i64 e = (i64)routes[x * A.ts + layer * A.ls + j];
+                    const i64 e = (i64)routes[(t0 + x) * A.ts + layer * A.ls + j];
                     if (e >= 0 && e < A.E) count_one(base, (u32)e);
                 }
         }
@@ -180,8 +197,9 @@ static int launch_count(CountArgs &A, int sms, cudaStream_t stream)
     // as many CTAs as stay resident; a tile is not so short that setting its counters to zero and adding them up costs more than counting
     const int groups = (A.L + A.lanes * layers - 1) / (A.lanes * layers);
     const i64 resident = (i64)sms * std::min((size_t)2, (size_t)(224 * 1024) / (smem + 1024));
-    A.tile = std::max((A.T + std::max((i64)1, resident / groups) - 1) / std::max((i64)1, resident / groups), (i64)256);
-    f<<<dim3((unsigned)((A.T + A.tile - 1) / A.tile), groups), COUNT_THREADS, smem, stream>>>(A);
+    const i64 most = std::max((i64)1, resident / groups), cost = A.T + (i64)COUNT_END * A.N;
+    const i64 tiles = std::max(std::min(most, (cost + 511) / 512), (A.T >> 30) + 1);          // (a tile's tokens are counted in 32 bits)
+    f<<<dim3((unsigned)tiles, groups), COUNT_THREADS, smem, stream>>>(A);
     return rp_op_launched();
 }
 
@@ -191,7 +209,7 @@ int rp_launch_count(int device, const void *routes, int bytes, i64 T, int L, int
 {
     RP_CUDA(cudaMemsetAsync(demand, 0, sizeof(int) * (size_t)N * L * E, stream));
     if (T < 1) return RP_OK;
-    CountArgs A = { routes, T, ts, ls, L, k, E, N, start, demand, ls < ts && L > 1 ? 4 : 1, 0, 0 };
+    CountArgs A = { routes, T, ts, ls, L, k, E, N, start, demand, ls < ts && L > 1 ? 4 : 1, 0 };
     const int sms = rp_op_sms(device);
     switch (bytes) {
         case 1: return launch_count<unsigned char>(A, sms, stream);
@@ -237,7 +255,7 @@ int rp_count_args(const void *routes, int bytes, i64 T, int L, int k, int E)
 {
     if (!routes || T < 0 || L < 1 || k < 1 || E < 1 || (bytes != 1 && bytes != 2 && bytes != 4 && bytes != 8)) return RP_ERR_ARG;
     if (!rp_aligned(routes, bytes)) return RP_ERR_ARG;
-    if (E > 1024 || k > 1024 || (i64)L * E >= (1ll << 31) || T > (1ll << 40)) return RP_ERR_RANGE;
+    if (E > 1024 || k > 1024 || (i64)L * E >= (1ll << 31) || T > (1ll << 36)) return RP_ERR_RANGE;
     return RP_OK;
 }
 
