@@ -67,16 +67,18 @@ __device__ __forceinline__ void store_row(u32 at, X *out, int d, bool there, flo
 // ---------------------------------------------------------------------------------------
 // keys: dk and dv
 // ---------------------------------------------------------------------------------------
-// The tiles are 64 queries wide, so that scores and do v^T of two of them fit beside the two sums (2 * 64 + 2 * 64 + 2 * head_dim columns): while one tile's weights
-// are worked out, by four warps of its own, the tensor cores work on the other.
+// Tiles of 128 queries: scores, do v^T and the two sums fill the tensor memory (2 * 128 + 2 * head_dim columns).  Both groups of four warps work on a tile, 64 columns
+// each.  The products come in the order dv(j), s(j + 1), dk(j), do v^T(j + 1): while the weights of a tile are worked out, the tensor cores add up dk of the one
+// before and multiply do v^T of this one; while the gradients of its scores are, dv of this and scores of the next.  Weights and gradients lie as operands where the
+// scores and the products of their group were.  (Tiles of 64 queries, two of them at a time, one for each group: 435 us in place of the figure in the launch's comment.)
 template <int D> struct KeySmem {
-    static constexpr int TILE = 128 * D * 2, HALF = 64 * D * 2, STAGES = 4;
+    static constexpr int TILE = 128 * D * 2, STAGES = 2;
     alignas(1024) unsigned char k[TILE];
     alignas(1024) unsigned char v[TILE];
-    alignas(1024) unsigned char q[STAGES][HALF];
-    alignas(1024) unsigned char g[STAGES][HALF];
-    float2 stats[2][2][64];
-    u64 kv_full, kv_empty, q_full[STAGES], q_empty[STAGES], s_full[2], dp_full[2], p_full[2], ds_full[2], st_full[2], acc_full, acc_empty, done;
+    alignas(1024) unsigned char q[STAGES][TILE];
+    alignas(1024) unsigned char g[STAGES][TILE];
+    alignas(16) float stats[2][2][2][64];    // [turn][group][lse / ln 2, delta][column]
+    u64 kv_full, kv_empty, q_full[STAGES], q_empty[STAGES], s_full, dp_full, p_full, ds_full, st_full[2], acc_full, acc_empty, done;
     u32 tmem;
     volatile int gave_up;
 };
@@ -87,17 +89,15 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               const __grid_constant__ CUtensorMap map_g, const GradArgs A)
 {
     typedef KeySmem<D> Smem;
-    constexpr int STAGES = Smem::STAGES, PANELS = D / 64, PANEL = 128 * 128, HALF = 64 * 128;
+    constexpr int STAGES = Smem::STAGES, PANELS = D / 64, PANEL = 128 * 128;
     extern __shared__ __align__(1024) unsigned char raw[];
     Smem &sm = *(Smem *)(raw + ((1024 - (rp_smem(raw) & 1023)) & 1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         bar_init(rp_smem(&sm.kv_full), 1); bar_init(rp_smem(&sm.kv_empty), 1);
         for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.q_full[s]), 1); bar_init(rp_smem(&sm.q_empty[s]), 1); }
-        for (int i = 0; i < 2; ++i) {
-            bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.dp_full[i]), 1);
-            bar_init(rp_smem(&sm.p_full[i]), 128); bar_init(rp_smem(&sm.ds_full[i]), 128); bar_init(rp_smem(&sm.st_full[i]), 128);
-        }
+        bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.dp_full), 1); bar_init(rp_smem(&sm.p_full), 256); bar_init(rp_smem(&sm.ds_full), 256);
+        for (int i = 0; i < 2; ++i) bar_init(rp_smem(&sm.st_full[i]), 128);
         bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 256); bar_init(rp_smem(&sm.done), 1);
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -121,7 +121,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
-                const int hk = at % A.Hk, first = A.causal ? t.row0 >> 6 : 0, per = ((t.len + 63) >> 6) - first;
+                const int hk = at % A.Hk, first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first;
                 if (n && !(ok = bar_wait(rp_smem(&sm.kv_empty), (n - 1) & 1, gave_up))) break;
                 bar_expect(rp_smem(&sm.kv_full), 2 * Smem::TILE);
                 for (int p = 0; p < PANELS; ++p) {
@@ -132,10 +132,10 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     for (int j = 0; j < per; ++j, ++fill) {
                         const u32 s = fill % STAGES, turn = fill / STAGES;
                         if (turn && !(ok = bar_wait(rp_smem(&sm.q_empty[s]), (turn - 1) & 1, gave_up))) break;
-                        bar_expect(rp_smem(&sm.q_full[s]), 2 * Smem::HALF);
+                        bar_expect(rp_smem(&sm.q_full[s]), 2 * Smem::TILE);
                         for (int p = 0; p < PANELS; ++p) {
-                            tma_load3(rp_smem(sm.q[s]) + p * HALF, &map_q, p * 64, h, (int)t.base + (first + j) * 64, rp_smem(&sm.q_full[s]));
-                            tma_load3(rp_smem(sm.g[s]) + p * HALF, &map_g, p * 64, h, (int)t.base + (first + j) * 64, rp_smem(&sm.q_full[s]));
+                            tma_load3(rp_smem(sm.q[s]) + p * PANEL, &map_q, p * 64, h, (int)t.base + (first + j) * 128, rp_smem(&sm.q_full[s]));
+                            tma_load3(rp_smem(sm.g[s]) + p * PANEL, &map_g, p * 64, h, (int)t.base + (first + j) * 128, rp_smem(&sm.q_full[s]));
                         }
                     }
             }
@@ -147,61 +147,66 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             }
         }
         if (warp == ATTEND_MMA_WARP) {
-            const u32 shape_s = mma_shape<X>(64, false), shape_o = mma_shape<X>(D, true);
-            u32 base = 0, uses[2] = { 0, 0 };               // tiles of the items before; weights taken of each half
+            const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
+            u32 base = 0;                               // tiles of the items before
             bool ok = true;
             for (int n = 0; ok; ++n) {
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
-                const int first = A.causal ? t.row0 >> 6 : 0, per = ((t.len + 63) >> 6) - first, nt = per * A.share;
+                const int first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first, nt = per * A.share;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full), n & 1, gave_up))) break;
-                auto scores = [&](int j) -> bool {          // scores and do v^T of a tile
+                // 128 keys against a tile's queries, or their values against the gradients
+                auto against = [&](u32 to, const unsigned char *keys, const unsigned char *queries, u32 bar) {
+                    if (lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const u32 off = (x / 4) * PANEL + (x % 4) * 32;
+                            mma_ss(to, mma_operand(rp_smem(keys) + off, true, 0), mma_operand(rp_smem(queries) + off, true, 0), shape_s, x > 0);
+                        }
+                        mma_commit(bar);
+                    }
+                };
+                auto arrived = [&](int j) -> bool {     // a tile's queries and gradients
                     const u32 f = base + j, s = f % STAGES;
-                    const int b = j & 1, left = t.len - (first + j % per) * 64;
+                    const int left = t.len - (first + j % per) * 128;
                     if (!bar_wait_warp(rp_smem(&sm.q_full[s]), (f / STAGES) & 1, gave_up)) return false;
                     // queries behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
-                    if (left < 64) { rp_clear_rows<D, 64>(sm.q[s], left, 64, lane); rp_clear_rows<D, 64>(sm.g[s], left, 64, lane); }
-                    if (lane == 0) {
-#pragma unroll
-                        for (int x = 0; x < D / 16; ++x) {
-                            const u32 oa = (x / 4) * PANEL + (x % 4) * 32, ob = (x / 4) * HALF + (x % 4) * 32;
-                            mma_ss(tm + b * 64, mma_operand(rp_smem(sm.k) + oa, true, 0), mma_operand(rp_smem(sm.q[s]) + ob, true, 0), shape_s, x > 0);
-                        }
-                        mma_commit(rp_smem(&sm.s_full[b]));
-#pragma unroll
-                        for (int x = 0; x < D / 16; ++x) {
-                            const u32 oa = (x / 4) * PANEL + (x % 4) * 32, ob = (x / 4) * HALF + (x % 4) * 32;
-                            mma_ss(tm + 128 + b * 64, mma_operand(rp_smem(sm.v) + oa, true, 0), mma_operand(rp_smem(sm.g[s]) + ob, true, 0), shape_s, x > 0);
-                        }
-                        mma_commit(rp_smem(&sm.dp_full[b]));
-                        if (j == nt - 1) mma_commit(rp_smem(&sm.kv_empty));
-                    }
+                    if (left < 128) { rp_clear_rows<D>(sm.q[s], left, 128, lane); rp_clear_rows<D>(sm.g[s], left, 128, lane); }
                     return true;
                 };
-                if (!(ok = scores(0))) break;
-                if (nt > 1 && !(ok = scores(1))) break;
-                if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
-                for (int j = 0; j < nt; ++j) {
-                    const int b = j & 1;
-                    const u32 s = (base + j) % STAGES;
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[b]), uses[b] & 1, gave_up))) break;
-                    tmem_after();
+                // a tile's weights (or gradients of its scores) times its gradients (or queries)
+                auto add = [&](u32 to, u32 weights, const unsigned char *rows, bool more) {
                     if (lane == 0)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            mma_ts(tm + 256, tm + b * 64 + x * 8, mma_operand(rp_smem(sm.g[s]) + x * 2048, false, HALF), shape_o, j > 0 || x > 0);
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full[b]), uses[b] & 1, gave_up))) break;
-                    ++uses[b];
+                        for (int x = 0; x < 8; ++x)
+                            mma_ts(to, weights + (x / 4) * 64 + (x % 4) * 8, mma_operand(rp_smem(rows) + x * 2048, false, PANEL), shape_o, more || x > 0);
+                };
+                if (!(ok = arrived(0))) break;
+                against(tm, sm.k, sm.q[base % STAGES], rp_smem(&sm.s_full));
+                against(tm + 128, sm.v, sm.g[base % STAGES], rp_smem(&sm.dp_full));
+                if (nt == 1 && lane == 0) mma_commit(rp_smem(&sm.kv_empty));
+                if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
+                for (int j = 0; j < nt; ++j) {
+                    const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.p_full), f & 1, gave_up))) break;
                     tmem_after();
+                    add(tm + 256, tm, sm.g[s], j > 0);
+                    if (j + 1 < nt) {
+                        if (!(ok = arrived(j + 1))) break;
+                        against(tm, sm.k, sm.q[s1], rp_smem(&sm.s_full));
+                    }
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
+                    tmem_after();
+                    add(tm + 256 + D, tm + 128, sm.q[s], j > 0);
                     if (lane == 0) {
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            mma_ts(tm + 256 + D, tm + 128 + b * 64 + x * 8, mma_operand(rp_smem(sm.q[s]) + x * 2048, false, HALF), shape_o, j > 0 || x > 0);
                         mma_commit(rp_smem(&sm.q_empty[s]));
                         if (j == nt - 1) mma_commit(rp_smem(&sm.acc_full));
                     }
-                    if (j + 2 < nt && !(ok = scores(j + 2))) break;
+                    if (j + 1 < nt) {
+                        against(tm + 128, sm.v, sm.g[s1], rp_smem(&sm.dp_full));
+                        if (j + 2 == nt && lane == 0) mma_commit(rp_smem(&sm.kv_empty));
+                    }
                 }
                 base += nt;
             }
@@ -213,21 +218,27 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         const int b = warp >> 2, row = threadIdx.x & 127;
         const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + b * 64, td = tm + lanes + 128 + b * 64;
         const float sl = A.scale * RP_LOG2E;
-        u32 uses = 0;
+        u32 f = 0;                                      // tiles so far
         for (int n = 0;; ++n) {
             const int at = rp_attend_item(n, total);
             if (at < 0) break;
             const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
-            const int hk = at % A.Hk, first = A.causal ? t.row0 >> 6 : 0, per = ((t.len + 63) >> 6) - first, nt = per * A.share, r = t.row0 + row;
+            const int hk = at % A.Hk, first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first, nt = per * A.share, r = t.row0 + row;
             bool ok = true;
-            for (int j = b; j < nt; j += 2) {
-                const int h = hk * A.share + j / per, q0 = (first + j % per) * 64;
+            auto stats = [&](int j) {                   // of one column of a tile
+                const int q = (first + j % per) * 128 + b * 64 + row;
+                return row < 64 && q < t.len ? A.stats[(i64)(hk * A.share + j / per) * A.T + t.base + q] : make_float2(0.0f, 0.0f);
+            };
+            float2 next = stats(0);
+            for (int j = 0; j < nt; ++j, ++f) {
+                const int q0 = (first + j % per) * 128 + b * 64;
                 // (two places in turn: who has come to a tile's barrier has read the tile before)
-                float2 *st = sm.stats[b][uses & 1];
-                if (row < 64) st[row] = q0 + row < t.len ? A.stats[(i64)h * A.T + t.base + q0 + row] : make_float2(0.0f, 0.0f);
+                float (*st)[64] = sm.stats[f & 1][b];
+                if (row < 64) { st[0][row] = next.x; st[1][row] = next.y; }
+                if (j + 1 < nt) next = stats(j + 1);
                 bar_arrive(rp_smem(&sm.st_full[b]));
-                if (!(ok = bar_wait_warp(rp_smem(&sm.st_full[b]), uses & 1, gave_up))) break;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[b]), uses & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.st_full[b]), f & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, gave_up))) break;
                 tmem_after();
                 u32 s[64];
                 float p[64];
@@ -235,7 +246,11 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_load32(ts + 32, s + 32);
                 tmem_loaded();
 #pragma unroll
-                for (int c = 0; c < 64; ++c) p[c] = rp_exp2(fmaf(__uint_as_float(s[c]), sl, -st[c].x));
+                for (int c = 0; c < 64; c += 4) {
+                    const float4 l = *(const float4 *)&st[0][c];
+                    p[c] = rp_exp2(fmaf(__uint_as_float(s[c]), sl, -l.x)); p[c + 1] = rp_exp2(fmaf(__uint_as_float(s[c + 1]), sl, -l.y));
+                    p[c + 2] = rp_exp2(fmaf(__uint_as_float(s[c + 2]), sl, -l.z)); p[c + 3] = rp_exp2(fmaf(__uint_as_float(s[c + 3]), sl, -l.w));
+                }
                 if (q0 + 64 > t.len || (A.causal && q0 < t.row0 + 128)) {
                     const int lo = A.causal ? r - q0 : 0, hi = t.len - q0;
 #pragma unroll
@@ -246,20 +261,22 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_store32(ts, s);
                 tmem_stored();
                 tmem_before();
-                bar_arrive(rp_smem(&sm.p_full[b]));
-                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full[b]), uses & 1, gave_up))) break;
-                ++uses;
+                bar_arrive(rp_smem(&sm.p_full));
+                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, gave_up))) break;
                 tmem_after();
                 tmem_load32(td, s);
                 tmem_load32(td + 32, s + 32);
                 tmem_loaded();
 #pragma unroll
-                for (int c = 0; c < 32; ++c)
-                    s[c] = rp_pair(p[2 * c] * (__uint_as_float(s[2 * c]) - st[2 * c].y), p[2 * c + 1] * (__uint_as_float(s[2 * c + 1]) - st[2 * c + 1].y), X());
+                for (int c = 0; c < 64; c += 4) {
+                    const float4 e = *(const float4 *)&st[1][c];
+                    s[c / 2] = rp_pair(p[c] * (__uint_as_float(s[c]) - e.x), p[c + 1] * (__uint_as_float(s[c + 1]) - e.y), X());
+                    s[c / 2 + 1] = rp_pair(p[c + 2] * (__uint_as_float(s[c + 2]) - e.z), p[c + 3] * (__uint_as_float(s[c + 3]) - e.w), X());
+                }
                 tmem_store32(td, s);
                 tmem_stored();
                 tmem_before();
-                bar_arrive(rp_smem(&sm.ds_full[b]));
+                bar_arrive(rp_smem(&sm.ds_full));
             }
             if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
             tmem_after();
@@ -279,15 +296,16 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 // ---------------------------------------------------------------------------------------
 // queries: dq
 // ---------------------------------------------------------------------------------------
-// Tiles of 128 keys; the scores of the next tile are there when a tile's are worked on (two groups of four warps take tiles in turn), do v^T of the next one comes as
-// soon as it has been read.  The gradients of the scores take the scores' place as operand.  Columns: 2 * 128 + 128 + head_dim.
+// Tiles of 128 keys, 64 columns to each of the two groups of four warps.  The scores of the next tile are there when a tile's are worked on; do v^T of the next one, dq
+// of this one and the scores after the next are multiplied while the weights of the next one are worked out.  The gradients of the scores take their group's
+// scores' place as operand.  Columns: 2 * 128 + 128 + head_dim.
 template <int D> struct QuerySmem {
     static constexpr int TILE = 128 * D * 2, KS = 3, VS = 2;
     alignas(1024) unsigned char q[TILE];
     alignas(1024) unsigned char g[TILE];
     alignas(1024) unsigned char k[KS][TILE];
     alignas(1024) unsigned char v[VS][TILE];
-    u64 q_full, q_empty, k_full[KS], k_empty[KS], v_full[VS], v_empty[VS], s_full[2], dp_full[2], dp_empty, ds_full[2], acc_full, acc_empty, done;
+    u64 q_full, q_empty, k_full[KS], k_empty[KS], v_full[VS], v_empty[VS], s_full[2], dp_full, ds_full, acc_full, acc_empty, done;
     u32 tmem;
     volatile int gave_up;
 };
@@ -306,8 +324,8 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         bar_init(rp_smem(&sm.q_full), 1); bar_init(rp_smem(&sm.q_empty), 1);
         for (int s = 0; s < KS; ++s) { bar_init(rp_smem(&sm.k_full[s]), 1); bar_init(rp_smem(&sm.k_empty[s]), 1); }
         for (int s = 0; s < VS; ++s) { bar_init(rp_smem(&sm.v_full[s]), 1); bar_init(rp_smem(&sm.v_empty[s]), 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.dp_full[i]), 1); bar_init(rp_smem(&sm.ds_full[i]), 128); }
-        bar_init(rp_smem(&sm.dp_empty), 128);
+        for (int i = 0; i < 2; ++i) bar_init(rp_smem(&sm.s_full[i]), 1);
+        bar_init(rp_smem(&sm.dp_full), 1); bar_init(rp_smem(&sm.ds_full), 256);
         bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 256); bar_init(rp_smem(&sm.done), 1);
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -358,7 +376,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
-            u32 base = 0, ds[2] = { 0, 0 };                 // tiles of the items before; tiles taken of each group
+            u32 base = 0;                               // tiles of the items before
             bool ok = true;
             for (int n = 0; ok; ++n) {
                 const int at = rp_attend_item(n, total);
@@ -368,7 +386,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), n & 1, gave_up))) break;
                 auto scores = [&](int j) -> bool {
                     const u32 f = base + j, s = f % KS;
-                    const int b = j & 1;
+                    const int b = f & 1;
                     if (!bar_wait_warp(rp_smem(&sm.k_full[s]), (f / KS) & 1, gave_up)) return false;
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
                     if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.k[s], t.len - j * 128, 128, lane);
@@ -391,7 +409,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                             const u32 off = (x / 4) * PANEL + (x % 4) * 32;
                             mma_ss(tm + 256, mma_operand(rp_smem(sm.g) + off, true, 0), mma_operand(rp_smem(sm.v[s]) + off, true, 0), shape_s, x > 0);
                         }
-                        mma_commit(rp_smem(&sm.dp_full[j & 1]));
+                        mma_commit(rp_smem(&sm.dp_full));
                         mma_commit(rp_smem(&sm.v_empty[s]));
                         if (j == nk - 1) mma_commit(rp_smem(&sm.q_empty));
                     }
@@ -403,20 +421,14 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 if (!(ok = products(0))) break;
                 if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
                 for (int j = 0; j < nk; ++j) {
-                    const int b = j & 1;
                     const u32 f = base + j;
-                    if (j + 1 < nk) {
-                        if (!(ok = bar_wait_warp(rp_smem(&sm.dp_empty), f & 1, gave_up))) break;
-                        tmem_after();
-                        if (!(ok = products(j + 1))) break;
-                    }
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full[b]), ds[b] & 1, gave_up))) break;
-                    ++ds[b];
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
                     tmem_after();
+                    if (j + 1 < nk && !(ok = products(j + 1))) break;
                     if (lane == 0) {
 #pragma unroll
                         for (int x = 0; x < 8; ++x)
-                            mma_ts(tm + 384, tm + b * 128 + x * 8, mma_operand(rp_smem(sm.k[f % KS]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
+                            mma_ts(tm + 384, tm + (f & 1) * 128 + (x / 4) * 64 + (x % 4) * 8, mma_operand(rp_smem(sm.k[f % KS]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
                         mma_commit(rp_smem(&sm.k_empty[f % KS]));
                         if (j == nk - 1) mma_commit(rp_smem(&sm.acc_full));
                     }
@@ -430,9 +442,9 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     } else {
         rp_many_registers();
         const int b = warp >> 2, row = threadIdx.x & 127;
-        const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + b * 128, td = tm + lanes + 256;
+        const u32 lanes = (u32)(warp & 3) << 21, td = tm + lanes + 256 + b * 64;
         const float sl = A.scale * RP_LOG2E;
-        u32 uses = 0;
+        u32 f = 0;                                      // tiles so far
         for (int n = 0;; ++n) {
             const int at = rp_attend_item(n, total);
             if (at < 0) break;
@@ -440,42 +452,35 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             const int h = at % A.Hq, nk = rp_attend_tiles(t, 0, A.causal), r = t.row0 + row;
             const float2 st = r < t.len ? A.stats[(i64)h * A.T + t.base + r] : make_float2(0.0f, 0.0f);
             bool ok = true;
-            for (int j = b; j < nk; j += 2) {
-                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[b]), uses & 1, gave_up))) break;
+            for (int j = 0; j < nk; ++j, ++f) {
+                const u32 ts = tm + lanes + (f & 1) * 128 + b * 64;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[f & 1]), (f >> 1) & 1, gave_up))) break;
                 tmem_after();
-                u32 s[128];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_load32(ts + 32 * c, s + 32 * c);
+                u32 s[64];
+                float p[64];
+                tmem_load32(ts, s);
+                tmem_load32(ts + 32, s + 32);
                 tmem_loaded();
 #pragma unroll
-                for (int c = 0; c < 128; ++c) s[c] = __float_as_uint(rp_exp2(fmaf(__uint_as_float(s[c]), sl, -st.x)));
-                const bool edge = j * 128 + 128 > t.len || (A.causal && j * 128 + 127 > t.row0);
-                const int lim = (A.causal ? min(t.len, r + 1) : t.len) - j * 128;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full[b]), uses & 1, gave_up))) break;
-                ++uses;
+                for (int c = 0; c < 64; ++c) p[c] = rp_exp2(fmaf(__uint_as_float(s[c]), sl, -st.x));
+                const int k0 = j * 128 + b * 64, lim = (A.causal ? min(t.len, r + 1) : t.len) - k0;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, gave_up))) break;
                 tmem_after();
+                tmem_load32(td, s);
+                tmem_load32(td + 32, s + 32);
+                tmem_loaded();
 #pragma unroll
-                for (int c = 0; c < 128; c += 32) {
-                    u32 dp[32];
-                    tmem_load32(td + c, dp);
-                    tmem_loaded();
-                    float ds[32];
+                for (int c = 0; c < 64; ++c) p[c] *= __uint_as_float(s[c]) - st.y;
+                if (k0 + 64 > t.len || (A.causal && k0 + 63 > t.row0)) {
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) ds[x] = __uint_as_float(s[c + x]) * (__uint_as_float(dp[x]) - st.y);
-                    if (edge) {
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) ds[x] = c + x < lim ? ds[x] : 0.0f;
-                    }
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) s[c / 2 + x] = rp_pair(ds[2 * x], ds[2 * x + 1], X());
+                    for (int c = 0; c < 64; ++c) p[c] = c < lim ? p[c] : 0.0f;
                 }
-                tmem_before();
-                bar_arrive(rp_smem(&sm.dp_empty));
+#pragma unroll
+                for (int c = 0; c < 32; ++c) s[c] = rp_pair(p[2 * c], p[2 * c + 1], X());
                 tmem_store32(ts, s);
-                tmem_store32(ts + 32, s + 32);
                 tmem_stored();
                 tmem_before();
-                bar_arrive(rp_smem(&sm.ds_full[b]));
+                bar_arrive(rp_smem(&sm.ds_full));
             }
             if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
             tmem_after();
@@ -504,7 +509,7 @@ extern "C" int64_t rp_attend_grad_workspace(const rp_attend_config *a, int64_t n
     return 2 * plan_bytes(n_tokens, n_samples) + 8 * n_tokens * a->q_heads;
 }
 
-struct GradMaps { CUtensorMap q64, q, k, v, g64, g; };
+struct GradMaps { CUtensorMap q, k, v, g; };
 
 template <typename X, int D>
 static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most, int sms, cudaStream_t stream)
@@ -512,7 +517,7 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     const size_t sk = sizeof(KeySmem<D>) + 1024, sq = sizeof(QuerySmem<D>) + 1024;
     RP_CUDA(cudaFuncSetAttribute(k_attend_keys<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sk));
     RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
-    k_attend_keys<X, D><<<(int)std::min((i64)sms, most * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q64, M.k, M.v, M.g64, keys);
+    k_attend_keys<X, D><<<(int)std::min((i64)sms, most * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
     RP_TRY(rp_op_launched());
     k_attend_queries<X, D><<<(int)std::min((i64)sms, most * keys.Hq), ATTEND_THREADS, sq, stream>>>(M.q, M.k, M.v, M.g, queries);
     return rp_op_launched();
@@ -539,11 +544,9 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     float2 *stats = (float2 *)((char *)workspace + 2 * plan);
     const int d = a->head_dim, Hq = a->q_heads, Hk = a->kv_heads;
     GradMaps M;
-    RP_TRY(rp_tensor_map(&M.q64, a->type, q->x, T, Hq, d, q->token, q->head, 64));
     RP_TRY(rp_tensor_map(&M.q, a->type, q->x, T, Hq, d, q->token, q->head, 128));
     RP_TRY(rp_tensor_map(&M.k, a->type, k->x, T, Hk, d, k->token, k->head, 128));
     RP_TRY(rp_tensor_map(&M.v, a->type, v->x, T, Hk, d, v->token, v->head, 128));
-    RP_TRY(rp_tensor_map(&M.g64, a->type, out_grad->x, T, Hq, d, out_grad->token, out_grad->head, 64));
     RP_TRY(rp_tensor_map(&M.g, a->type, out_grad->x, T, Hq, d, out_grad->token, out_grad->head, 128));
     AttendPlan P = {};
     P.start = (const i64 *)start; P.T = T; P.N = n_samples; P.rows = 128; P.causal = a->causal; P.most = (int)(T / 128 + n_samples);
