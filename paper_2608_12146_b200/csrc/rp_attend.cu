@@ -170,15 +170,15 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
             u32 used = 0, ps[2] = { 0, 0 };                 // copies taken from the ring; weights taken of each tile
             bool ok = true;
+            const u32 one = lane == 0;
             auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
-                if (lane == 0) {
+                const u32 a = mma_operand(rp_smem(sm.q[i]), true, 0), b = mma_operand(rp_smem(sm.kv[stage]), true, 0);
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        const u32 off = (x / 4) * PANEL + (x % 4) * 32;
-                        mma_ss(tm + i * 128, mma_operand(rp_smem(sm.q[i]) + off, true, 0), mma_operand(rp_smem(sm.kv[stage]) + off, true, 0), shape_s, x > 0);
-                    }
-                    mma_commit(rp_smem(&sm.s_full[i]));
+                for (int x = 0; x < D / 16; ++x) {
+                    const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
+                    mma_ss(one, tm + i * 128, a + off, b + off, shape_s, x > 0);
                 }
+                mma_commit(one, rp_smem(&sm.s_full[i]));
             };
             for (int round = 0; ok; ++round) {
                 const int at = rp_attend_item(round, total);
@@ -189,7 +189,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), round & 1, gave_up))) break;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up))) break;
                 for (int i = 0; i < tiles; ++i) scores(i, used % STAGES);
-                if (lane == 0) { mma_commit(rp_smem(&sm.kv_empty[used % STAGES])); if (nk == 1) mma_commit(rp_smem(&sm.q_empty)); }
+                mma_commit(one, rp_smem(&sm.kv_empty[used % STAGES]));
+                if (nk == 1) mma_commit(one, rp_smem(&sm.q_empty));
                 ++used;
                 for (int j = 0; ok && j < nk; ++j) {
                     const u32 sv = used % STAGES, sk = (used + 1) % STAGES;
@@ -203,12 +204,11 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[i]), ps[i] & 1, gave_up))) break;
                         ++ps[i];
                         tmem_after();
-                        if (lane == 0) {
+                        const u32 v = mma_operand(rp_smem(sm.kv[sv]), false, PANEL);
 #pragma unroll
-                            for (int x = 0; x < 8; ++x)
-                                mma_ts(tm + 256 + i * D, tm + i * 128 + x * 8, mma_operand(rp_smem(sm.kv[sv]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
-                            if (j == ni - 1) mma_commit(rp_smem(&sm.o_full[i]));
-                        }
+                        for (int x = 0; x < 8; ++x)
+                            mma_ts(one, tm + 256 + i * D, tm + i * 128 + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        if (j == ni - 1) mma_commit(one, rp_smem(&sm.o_full[i]));
                         if (j + 1 < ni) {
                             if (!keys && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;
                             keys = true;
@@ -216,16 +216,15 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         }
                     }
                     if (!ok) break;
-                    if (lane == 0) {
-                        mma_commit(rp_smem(&sm.kv_empty[sv]));
-                        if (j + 1 < nk) mma_commit(rp_smem(&sm.kv_empty[sk]));
-                        if (j + 2 == nk) mma_commit(rp_smem(&sm.q_empty));
-                    }
+                    mma_commit(one, rp_smem(&sm.kv_empty[sv]));
+                    if (j + 1 < nk) mma_commit(one, rp_smem(&sm.kv_empty[sk]));
+                    if (j + 2 == nk) mma_commit(one, rp_smem(&sm.q_empty));
                     used += j + 1 < nk ? 2 : 1;
                 }
             }
             // nobody may leave while products are under way
-            if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
+            mma_commit(one, rp_smem(&sm.done));
+            if (lane == 0) rp_drain(rp_smem(&sm.done), 0);
         }
     } else {
         rp_many_registers();

@@ -148,6 +148,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
+            const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
             bool ok = true;
             for (int n = 0; ok; ++n) {
@@ -158,14 +159,13 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full), n & 1, gave_up))) break;
                 // 128 keys against a tile's queries, or their values against the gradients
                 auto against = [&](u32 to, const unsigned char *keys, const unsigned char *queries, u32 bar) {
-                    if (lane == 0) {
+                    const u32 a = mma_operand(rp_smem(keys), true, 0), b = mma_operand(rp_smem(queries), true, 0);
 #pragma unroll
-                        for (int x = 0; x < D / 16; ++x) {
-                            const u32 off = (x / 4) * PANEL + (x % 4) * 32;
-                            mma_ss(to, mma_operand(rp_smem(keys) + off, true, 0), mma_operand(rp_smem(queries) + off, true, 0), shape_s, x > 0);
-                        }
-                        mma_commit(bar);
+                    for (int x = 0; x < D / 16; ++x) {
+                        const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
+                        mma_ss(one, to, a + off, b + off, shape_s, x > 0);
                     }
+                    mma_commit(one, bar);
                 };
                 auto arrived = [&](int j) -> bool {     // a tile's queries and gradients
                     const u32 f = base + j, s = f % STAGES;
@@ -177,15 +177,15 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 };
                 // a tile's weights (or gradients of its scores) times its gradients (or queries)
                 auto add = [&](u32 to, u32 weights, const unsigned char *rows, bool more) {
-                    if (lane == 0)
+                    const u32 b = mma_operand(rp_smem(rows), false, PANEL);
 #pragma unroll
-                        for (int x = 0; x < 8; ++x)
-                            mma_ts(to, weights + (x / 4) * 64 + (x % 4) * 8, mma_operand(rp_smem(rows) + x * 2048, false, PANEL), shape_o, more || x > 0);
+                    for (int x = 0; x < 8; ++x)
+                        mma_ts(one, to, weights + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
                 };
                 if (!(ok = arrived(0))) break;
                 against(tm, sm.k, sm.q[base % STAGES], rp_smem(&sm.s_full));
                 against(tm + 128, sm.v, sm.g[base % STAGES], rp_smem(&sm.dp_full));
-                if (nt == 1 && lane == 0) mma_commit(rp_smem(&sm.kv_empty));
+                if (nt == 1) mma_commit(one, rp_smem(&sm.kv_empty));
                 if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
                 for (int j = 0; j < nt; ++j) {
                     const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
@@ -199,19 +199,18 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
                     tmem_after();
                     add(tm + 256 + D, tm + 128, sm.q[s], j > 0);
-                    if (lane == 0) {
-                        mma_commit(rp_smem(&sm.q_empty[s]));
-                        if (j == nt - 1) mma_commit(rp_smem(&sm.acc_full));
-                    }
+                    mma_commit(one, rp_smem(&sm.q_empty[s]));
+                    if (j == nt - 1) mma_commit(one, rp_smem(&sm.acc_full));
                     if (j + 1 < nt) {
                         against(tm + 128, sm.v, sm.g[s1], rp_smem(&sm.dp_full));
-                        if (j + 2 == nt && lane == 0) mma_commit(rp_smem(&sm.kv_empty));
+                        if (j + 2 == nt) mma_commit(one, rp_smem(&sm.kv_empty));
                     }
                 }
                 base += nt;
             }
             // nobody may leave while products are under way
-            if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
+            mma_commit(one, rp_smem(&sm.done));
+            if (lane == 0) rp_drain(rp_smem(&sm.done), 0);
         }
     } else {
         rp_many_registers();
@@ -376,6 +375,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
+            const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
             bool ok = true;
             for (int n = 0; ok; ++n) {
@@ -390,29 +390,27 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (!bar_wait_warp(rp_smem(&sm.k_full[s]), (f / KS) & 1, gave_up)) return false;
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
                     if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.k[s], t.len - j * 128, 128, lane);
-                    if (lane == 0) {
+                    const u32 q = mma_operand(rp_smem(sm.q), true, 0), k = mma_operand(rp_smem(sm.k[s]), true, 0);
 #pragma unroll
-                        for (int x = 0; x < D / 16; ++x) {
-                            const u32 off = (x / 4) * PANEL + (x % 4) * 32;
-                            mma_ss(tm + b * 128, mma_operand(rp_smem(sm.q) + off, true, 0), mma_operand(rp_smem(sm.k[s]) + off, true, 0), shape_s, x > 0);
-                        }
-                        mma_commit(rp_smem(&sm.s_full[b]));
+                    for (int x = 0; x < D / 16; ++x) {
+                        const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
+                        mma_ss(one, tm + b * 128, q + off, k + off, shape_s, x > 0);
                     }
+                    mma_commit(one, rp_smem(&sm.s_full[b]));
                     return true;
                 };
                 auto products = [&](int j) -> bool {        // do v^T
                     const u32 f = base + j, s = f % VS;
                     if (!bar_wait_warp(rp_smem(&sm.v_full[s]), (f / VS) & 1, gave_up)) return false;
-                    if (lane == 0) {
+                    const u32 g = mma_operand(rp_smem(sm.g), true, 0), v = mma_operand(rp_smem(sm.v[s]), true, 0);
 #pragma unroll
-                        for (int x = 0; x < D / 16; ++x) {
-                            const u32 off = (x / 4) * PANEL + (x % 4) * 32;
-                            mma_ss(tm + 256, mma_operand(rp_smem(sm.g) + off, true, 0), mma_operand(rp_smem(sm.v[s]) + off, true, 0), shape_s, x > 0);
-                        }
-                        mma_commit(rp_smem(&sm.dp_full));
-                        mma_commit(rp_smem(&sm.v_empty[s]));
-                        if (j == nk - 1) mma_commit(rp_smem(&sm.q_empty));
+                    for (int x = 0; x < D / 16; ++x) {
+                        const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
+                        mma_ss(one, tm + 256, g + off, v + off, shape_s, x > 0);
                     }
+                    mma_commit(one, rp_smem(&sm.dp_full));
+                    mma_commit(one, rp_smem(&sm.v_empty[s]));
+                    if (j == nk - 1) mma_commit(one, rp_smem(&sm.q_empty));
                     return true;
                 };
                 // (the last tile's do v^T is issued behind its scores: when q_empty is arrived at, both are done with q and do)
@@ -425,19 +423,19 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
                     tmem_after();
                     if (j + 1 < nk && !(ok = products(j + 1))) break;
-                    if (lane == 0) {
+                    const u32 k = mma_operand(rp_smem(sm.k[f % KS]), false, PANEL);
 #pragma unroll
-                        for (int x = 0; x < 8; ++x)
-                            mma_ts(tm + 384, tm + (f & 1) * 128 + (x / 4) * 64 + (x % 4) * 8, mma_operand(rp_smem(sm.k[f % KS]) + x * 2048, false, PANEL), shape_o, j > 0 || x > 0);
-                        mma_commit(rp_smem(&sm.k_empty[f % KS]));
-                        if (j == nk - 1) mma_commit(rp_smem(&sm.acc_full));
-                    }
+                    for (int x = 0; x < 8; ++x)
+                        mma_ts(one, tm + 384, tm + (f & 1) * 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                    mma_commit(one, rp_smem(&sm.k_empty[f % KS]));
+                    if (j == nk - 1) mma_commit(one, rp_smem(&sm.acc_full));
                     if (j + 2 < nk && !(ok = scores(j + 2))) break;
                 }
                 base += nk;
             }
             // nobody may leave while products are under way
-            if (lane == 0) { mma_commit(rp_smem(&sm.done)); rp_drain(rp_smem(&sm.done), 0); }
+            mma_commit(one, rp_smem(&sm.done));
+            if (lane == 0) rp_drain(rp_smem(&sm.done), 0);
         }
     } else {
         rp_many_registers();

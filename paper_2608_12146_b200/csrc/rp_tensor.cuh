@@ -96,32 +96,35 @@ __device__ __forceinline__ void tmem_store32(u32 at, const u32 *r)
 // leaves them; eight rows are 1024 bytes.
 // `along_k`: rows are rows (or columns) of the product and the 64 elements run along the summed dimension; a step of 16 of those is 32 bytes on.
 // Otherwise the rows run along the summed dimension; a step of 16 is 2048 bytes on, the next 64 elements are `panel` bytes on.
-__device__ __forceinline__ u64 mma_operand(u32 at, bool along_k, u32 panel)
-{
-    const u64 fixed = ((u64)1 << 46) | ((u64)2 << 61) | ((u64)(1024 >> 4) << 32);          // descriptor version, 128-byte swizzle, eight rows
-    return fixed | ((u64)(along_k ? 1 : panel >> 4) << 16) | (u64)((at & 0x3ffff) >> 4);
-}
+// Descriptor of an operand: the low word has its address, the high word is fixed (eight rows of 128 bytes, version, swizzle).
+#define MMA_HIGH ((1024u >> 4) | (1u << 14) | (2u << 29))
+__device__ __forceinline__ u32 mma_operand(u32 at, bool along_k, u32 panel) { return ((at & 0x3ffffu) >> 4) | ((along_k ? 1u : panel >> 4) << 16); }
 // 16-bit operands, 32-bit sums, 128 rows, `n` columns; `b_rows_k`: B's rows run along the summed dimension.
 template <typename X> __device__ __forceinline__ constexpr u32 mma_shape(int n, bool b_rows_k)
 {
     return (1u << 4) | ((std::is_same<X, bf16>::value ? 1u : 0u) << 7) | ((std::is_same<X, bf16>::value ? 1u : 0u) << 10) |
            ((b_rows_k ? 1u : 0u) << 16) | ((u32)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
-// One step of 16 along the summed dimension, by one thread; `more`: added to what the accumulator holds.
-__device__ __forceinline__ void mma_ss(u32 d, u64 a, u64 b, u32 shape, bool more)
+// One step of 16 along the summed dimension; `more`: added to what the accumulator holds.  The whole warp comes here, `one` is set in the lane that issues: what the
+// instruction takes is then worked out once for the warp, in registers of its own.  (Within a branch that one lane takes, a step took 105 to 130 cycles to issue and
+// 64 to run.)
+__device__ __forceinline__ void mma_ss(u32 one, u32 d, u32 a, u32 b, u32 shape, bool more)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"((u32)more) : "memory");
+    asm volatile("{\n .reg .pred p, q;\n .reg .b64 x, y;\n setp.ne.u32 q, %0, 0;\n setp.ne.u32 p, %5, 0;\n mov.b64 x, {%2, %6};\n mov.b64 y, {%3, %6};\n"
+                 " @q tcgen05.mma.cta_group::1.kind::f16 [%1], x, y, %4, p;\n}"
+                 ::"r"(one), "r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)more), "r"(MMA_HIGH) : "memory");
 }
-__device__ __forceinline__ void mma_ts(u32 d, u32 a, u64 b, u32 shape, bool more)           // A from tensor memory, two elements a column
+__device__ __forceinline__ void mma_ts(u32 one, u32 d, u32 a, u32 b, u32 shape, bool more)           // A from tensor memory, two elements a column
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(shape), "r"((u32)more) : "memory");
+    asm volatile("{\n .reg .pred p, q;\n .reg .b64 y;\n setp.ne.u32 q, %0, 0;\n setp.ne.u32 p, %5, 0;\n mov.b64 y, {%3, %6};\n"
+                 " @q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], y, %4, p;\n}"
+                 ::"r"(one), "r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)more), "r"(MMA_HIGH) : "memory");
 }
-// The barrier is arrived at when all products that this thread has issued are done.
-__device__ __forceinline__ void mma_commit(u32 bar)
+// The barrier is arrived at when all products that this lane has issued are done.
+__device__ __forceinline__ void mma_commit(u32 one, u32 bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{\n .reg .pred q;\n setp.ne.u32 q, %0, 0;\n @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n}"
+                 ::"r"(one), "r"(bar) : "memory");
 }
 
 // ---- host: a tensor [tokens][heads][dim] as 64-element panels of `rows` tokens of one head ----
