@@ -128,7 +128,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     tmem_before();
     __syncthreads();
     tmem_after();
-    const u32 tm = sm.tmem;
+    const u32 tm = rp_uniform(sm.tmem);
     const int total = A.head->count * A.Hq;
     volatile int *gave_up = &sm.gave_up;
 
@@ -172,7 +172,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             bool ok = true;
             const u32 one = lane == 0;
             auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
-                const u32 a = mma_operand(rp_smem(sm.q[i]), true, 0), b = mma_operand(rp_smem(sm.kv[stage]), true, 0);
+                const u32 a = rp_uniform(mma_operand(rp_smem(sm.q[i]), true, 0)), b = rp_uniform(mma_operand(rp_smem(sm.kv[stage]), true, 0));
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
                     const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
@@ -204,10 +204,10 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[i]), ps[i] & 1, gave_up))) break;
                         ++ps[i];
                         tmem_after();
-                        const u32 v = mma_operand(rp_smem(sm.kv[sv]), false, PANEL);
+                        const u32 w = rp_uniform(tm + i * 128), v = rp_uniform(mma_operand(rp_smem(sm.kv[sv]), false, PANEL));
 #pragma unroll
                         for (int x = 0; x < 8; ++x)
-                            mma_ts(one, tm + 256 + i * D, tm + i * 128 + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                            mma_ts(one, tm + 256 + i * D, w + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
                         if (j == ni - 1) mma_commit(one, rp_smem(&sm.o_full[i]));
                         if (j + 1 < ni) {
                             if (!keys && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;

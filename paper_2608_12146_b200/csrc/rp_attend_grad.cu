@@ -106,7 +106,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     tmem_before();
     __syncthreads();
     tmem_after();
-    const u32 tm = sm.tmem;
+    const u32 tm = rp_uniform(sm.tmem);
     const int total = A.head->count * A.Hk;
     volatile int *gave_up = &sm.gave_up;
 
@@ -159,7 +159,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full), n & 1, gave_up))) break;
                 // 128 keys against a tile's queries, or their values against the gradients
                 auto against = [&](u32 to, const unsigned char *keys, const unsigned char *queries, u32 bar) {
-                    const u32 a = mma_operand(rp_smem(keys), true, 0), b = mma_operand(rp_smem(queries), true, 0);
+                    const u32 a = rp_uniform(mma_operand(rp_smem(keys), true, 0)), b = rp_uniform(mma_operand(rp_smem(queries), true, 0));
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x) {
                         const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
@@ -177,10 +177,10 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 };
                 // a tile's weights (or gradients of its scores) times its gradients (or queries)
                 auto add = [&](u32 to, u32 weights, const unsigned char *rows, bool more) {
-                    const u32 b = mma_operand(rp_smem(rows), false, PANEL);
+                    const u32 a = rp_uniform(weights), b = rp_uniform(mma_operand(rp_smem(rows), false, PANEL));
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
-                        mma_ts(one, to, weights + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
+                        mma_ts(one, to, a + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
                 };
                 if (!(ok = arrived(0))) break;
                 against(tm, sm.k, sm.q[base % STAGES], rp_smem(&sm.s_full));
@@ -333,7 +333,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     tmem_before();
     __syncthreads();
     tmem_after();
-    const u32 tm = sm.tmem;
+    const u32 tm = rp_uniform(sm.tmem);
     const int total = A.head->count * A.Hq;
     volatile int *gave_up = &sm.gave_up;
 
@@ -390,7 +390,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (!bar_wait_warp(rp_smem(&sm.k_full[s]), (f / KS) & 1, gave_up)) return false;
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
                     if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.k[s], t.len - j * 128, 128, lane);
-                    const u32 q = mma_operand(rp_smem(sm.q), true, 0), k = mma_operand(rp_smem(sm.k[s]), true, 0);
+                    const u32 q = rp_uniform(mma_operand(rp_smem(sm.q), true, 0)), k = rp_uniform(mma_operand(rp_smem(sm.k[s]), true, 0));
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x) {
                         const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
@@ -402,7 +402,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 auto products = [&](int j) -> bool {        // do v^T
                     const u32 f = base + j, s = f % VS;
                     if (!bar_wait_warp(rp_smem(&sm.v_full[s]), (f / VS) & 1, gave_up)) return false;
-                    const u32 g = mma_operand(rp_smem(sm.g), true, 0), v = mma_operand(rp_smem(sm.v[s]), true, 0);
+                    const u32 g = rp_uniform(mma_operand(rp_smem(sm.g), true, 0)), v = rp_uniform(mma_operand(rp_smem(sm.v[s]), true, 0));
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x) {
                         const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
@@ -423,10 +423,10 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
                     tmem_after();
                     if (j + 1 < nk && !(ok = products(j + 1))) break;
-                    const u32 k = mma_operand(rp_smem(sm.k[f % KS]), false, PANEL);
+                    const u32 a = rp_uniform(tm + (f & 1) * 128), k = rp_uniform(mma_operand(rp_smem(sm.k[f % KS]), false, PANEL));
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
-                        mma_ts(one, tm + 384, tm + (f & 1) * 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        mma_ts(one, tm + 384, a + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
                     mma_commit(one, rp_smem(&sm.k_empty[f % KS]));
                     if (j == nk - 1) mma_commit(one, rp_smem(&sm.acc_full));
                     if (j + 2 < nk && !(ok = scores(j + 2))) break;

@@ -96,6 +96,9 @@ __device__ __forceinline__ void tmem_store32(u32 at, const u32 *r)
 // leaves them; eight rows are 1024 bytes.
 // `along_k`: rows are rows (or columns) of the product and the 64 elements run along the summed dimension; a step of 16 of those is 32 bytes on.
 // Otherwise the rows run along the summed dimension; a step of 16 is 2048 bytes on, the next 64 elements are `panel` bytes on.
+// A value that all lanes of a warp have alike, in a register that the warp has once: the products take their operands from such, and what is worked out from
+// one stays there (moved over one by one they issue at half the rate).
+__device__ __forceinline__ u32 rp_uniform(u32 x) { return __reduce_or_sync(0xffffffffu, x); }
 // Descriptor of an operand: the low word has its address, the high word is fixed (eight rows of 128 bytes, version, swizzle).
 #define MMA_HIGH ((1024u >> 4) | (1u << 14) | (2u << 29))
 __device__ __forceinline__ u32 mma_operand(u32 at, bool along_k, u32 panel) { return ((at & 0x3ffffu) >> 4) | ((along_k ? 1u : panel >> 4) << 16); }
