@@ -119,7 +119,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     if (threadIdx.x == 0) {
         bar_init(rp_smem(&sm.q_full), 1); bar_init(rp_smem(&sm.q_empty), 1);
         for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.kv_full[s]), 1); bar_init(rp_smem(&sm.kv_empty[s]), 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.p_full[i]), 128); bar_init(rp_smem(&sm.o_full[i]), 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.p_full[i]), 4); bar_init(rp_smem(&sm.o_full[i]), 1); }
         bar_init(rp_smem(&sm.done), 1);
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -129,7 +129,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     __syncthreads();
     tmem_after();
     const u32 tm = rp_uniform(sm.tmem);
-    const int total = A.head->count * A.Hq;
+    const int total = rp_uniform(A.head->count * A.Hq);
     volatile int *gave_up = &sm.gave_up;
 
     if (warp >= 8) {
@@ -168,11 +168,11 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
-            u32 used = 0, ps[2] = { 0, 0 };                 // copies taken from the ring; weights taken of each tile
-            bool ok = true;
             const u32 one = lane == 0;
+            u32 used = 0, p0 = 0, p1 = 0;                   // copies taken from the ring; weights taken of each tile
+            bool ok = true;
             auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
-                const u32 a = rp_uniform(mma_operand(rp_smem(sm.q[i]), true, 0)), b = rp_uniform(mma_operand(rp_smem(sm.kv[stage]), true, 0));
+                const u32 a = mma_operand(rp_smem(sm.q[i]), true, 0), b = mma_operand(rp_smem(sm.kv[stage]), true, 0);
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
                     const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
@@ -184,38 +184,39 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 const int at = rp_attend_item(round, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
-                const int tiles = t.row0 + 128 < t.len ? 2 : 1, n0 = rp_attend_tiles(t, 0, A.causal), n1 = tiles == 2 ? rp_attend_tiles(t, 1, A.causal) : 0;
-                const int nk = max(n0, n1);
+                const int left = rp_uniform(t.len - t.row0), tiles = left > 128 ? 2 : 1, len = rp_uniform(t.len);
+                const int n0 = rp_uniform(rp_attend_tiles(t, 0, A.causal)), n1 = tiles == 2 ? rp_uniform(rp_attend_tiles(t, 1, A.causal)) : 0, nk = max(n0, n1);
                 if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), round & 1, gave_up))) break;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up))) break;
-                for (int i = 0; i < tiles; ++i) scores(i, used % STAGES);
+                scores(0, used % STAGES);
+                if (tiles == 2) scores(1, used % STAGES);
                 mma_commit(one, rp_smem(&sm.kv_empty[used % STAGES]));
                 if (nk == 1) mma_commit(one, rp_smem(&sm.q_empty));
                 ++used;
-                for (int j = 0; ok && j < nk; ++j) {
+                for (int j = 0; j < nk; ++j) {
                     const u32 sv = used % STAGES, sk = (used + 1) % STAGES;
+                    // (what is copied has mostly come when the weights have)
                     if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[sv]), (used / STAGES) & 1, gave_up))) break;
+                    if (j + 1 < nk && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;
                     // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
-                    if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.kv[sv], t.len - j * 128, 128, lane);
-                    bool keys = false;                      // the next keys have come
-                    for (int i = 0; i < tiles; ++i) {
-                        const int ni = i ? n1 : n0;
-                        if (j >= ni) continue;
-                        if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[i]), ps[i] & 1, gave_up))) break;
-                        ++ps[i];
+                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.kv[sv], len - j * 128, 128, lane);
+                    const u32 v = mma_operand(rp_smem(sm.kv[sv]), false, PANEL);
+                    if (j < n0) {
+                        if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[0]), p0++ & 1, gave_up))) break;
                         tmem_after();
-                        const u32 w = rp_uniform(tm + i * 128), v = rp_uniform(mma_operand(rp_smem(sm.kv[sv]), false, PANEL));
 #pragma unroll
-                        for (int x = 0; x < 8; ++x)
-                            mma_ts(one, tm + 256 + i * D, w + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
-                        if (j == ni - 1) mma_commit(one, rp_smem(&sm.o_full[i]));
-                        if (j + 1 < ni) {
-                            if (!keys && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;
-                            keys = true;
-                            scores(i, sk);
-                        }
+                        for (int x = 0; x < 8; ++x) mma_ts(one, tm + 256, tm + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        if (j == n0 - 1) mma_commit(one, rp_smem(&sm.o_full[0]));
+                        else scores(0, sk);
                     }
-                    if (!ok) break;
+                    if (j < n1) {
+                        if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[1]), p1++ & 1, gave_up))) break;
+                        tmem_after();
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) mma_ts(one, tm + 256 + D, tm + 128 + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        if (j == n1 - 1) mma_commit(one, rp_smem(&sm.o_full[1]));
+                        else scores(1, sk);
+                    }
                     mma_commit(one, rp_smem(&sm.kv_empty[sv]));
                     if (j + 1 < nk) mma_commit(one, rp_smem(&sm.kv_empty[sk]));
                     if (j + 2 == nk) mma_commit(one, rp_smem(&sm.q_empty));
@@ -289,7 +290,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 tmem_store32(ts + 32, s + 32);
                 tmem_stored();
                 tmem_before();
-                bar_arrive(rp_smem(&sm.p_full[i]));
+                bar_arrive_warp(rp_smem(&sm.p_full[i]), lane);
             }
             if (ok) ok = bar_wait_warp(rp_smem(&sm.o_full[i]), os & 1, gave_up);
             ++os;

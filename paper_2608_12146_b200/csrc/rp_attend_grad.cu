@@ -20,6 +20,8 @@ struct GradArgs {
     void *x[2];                              // dv, dk, or dq
     i64 token[2], hd[2];
     int *status;
+    const void *rows[2];                     // queries' kernel: q, do
+    i64 r_token[2], r_head[2];
 };
 
 // lse / ln 2 and delta of every token and query head: 16 lanes a head, 16 bytes of do and o a lane.
@@ -96,9 +98,9 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     if (threadIdx.x == 0) {
         bar_init(rp_smem(&sm.kv_full), 1); bar_init(rp_smem(&sm.kv_empty), 1);
         for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.q_full[s]), 1); bar_init(rp_smem(&sm.q_empty[s]), 1); }
-        bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.dp_full), 1); bar_init(rp_smem(&sm.p_full), 256); bar_init(rp_smem(&sm.ds_full), 256);
-        for (int i = 0; i < 2; ++i) bar_init(rp_smem(&sm.st_full[i]), 128);
-        bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 256); bar_init(rp_smem(&sm.done), 1);
+        bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.dp_full), 1); bar_init(rp_smem(&sm.p_full), 8); bar_init(rp_smem(&sm.ds_full), 8);
+        for (int i = 0; i < 2; ++i) bar_init(rp_smem(&sm.st_full[i]), 4);
+        bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 8); bar_init(rp_smem(&sm.done), 1);
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -107,7 +109,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     __syncthreads();
     tmem_after();
     const u32 tm = rp_uniform(sm.tmem);
-    const int total = A.head->count * A.Hk;
+    const int total = rp_uniform(A.head->count * A.Hk);
     volatile int *gave_up = &sm.gave_up;
 
     if (warp >= 8) {
@@ -155,11 +157,11 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
-                const int first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first, nt = per * A.share;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full), n & 1, gave_up))) break;
+                const int len = rp_uniform(t.len), first = A.causal ? (int)rp_uniform(t.row0 >> 7) : 0, per = ((len + 127) >> 7) - first, nt = per * A.share;
+                int tile = first;                       // of queries: the next to arrive
                 // 128 keys against a tile's queries, or their values against the gradients
                 auto against = [&](u32 to, const unsigned char *keys, const unsigned char *queries, u32 bar) {
-                    const u32 a = rp_uniform(mma_operand(rp_smem(keys), true, 0)), b = rp_uniform(mma_operand(rp_smem(queries), true, 0));
+                    const u32 a = mma_operand(rp_smem(keys), true, 0), b = mma_operand(rp_smem(queries), true, 0);
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x) {
                         const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
@@ -167,44 +169,43 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     }
                     mma_commit(one, bar);
                 };
-                auto arrived = [&](int j) -> bool {     // a tile's queries and gradients
-                    const u32 f = base + j, s = f % STAGES;
-                    const int left = t.len - (first + j % per) * 128;
+                auto arrived = [&](u32 f) -> bool {     // a tile's queries and gradients
+                    const u32 s = f % STAGES;
                     if (!bar_wait_warp(rp_smem(&sm.q_full[s]), (f / STAGES) & 1, gave_up)) return false;
                     // queries behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
+                    const int left = len - tile * 128;
                     if (left < 128) { rp_clear_rows<D>(sm.q[s], left, 128, lane); rp_clear_rows<D>(sm.g[s], left, 128, lane); }
+                    tile = tile + 1 == first + per ? first : tile + 1;
                     return true;
                 };
                 // a tile's weights (or gradients of its scores) times its gradients (or queries)
                 auto add = [&](u32 to, u32 weights, const unsigned char *rows, bool more) {
-                    const u32 a = rp_uniform(weights), b = rp_uniform(mma_operand(rp_smem(rows), false, PANEL));
+                    const u32 b = mma_operand(rp_smem(rows), false, PANEL);
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        mma_ts(one, to, a + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
+                    for (int x = 0; x < 8; ++x) mma_ts(one, to, weights + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
                 };
-                if (!(ok = arrived(0))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full), n & 1, gave_up))) break;
+                if (!(ok = arrived(base))) break;
                 against(tm, sm.k, sm.q[base % STAGES], rp_smem(&sm.s_full));
                 against(tm + 128, sm.v, sm.g[base % STAGES], rp_smem(&sm.dp_full));
                 if (nt == 1) mma_commit(one, rp_smem(&sm.kv_empty));
                 if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
                 for (int j = 0; j < nt; ++j) {
                     const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
+                    if (j + 1 < nt && !(ok = arrived(f + 1))) break;        // (mostly before the weights have)
                     if (!(ok = bar_wait_warp(rp_smem(&sm.p_full), f & 1, gave_up))) break;
                     tmem_after();
                     add(tm + 256, tm, sm.g[s], j > 0);
-                    if (j + 1 < nt) {
-                        if (!(ok = arrived(j + 1))) break;
-                        against(tm, sm.k, sm.q[s1], rp_smem(&sm.s_full));
-                    }
+                    if (j + 1 < nt) against(tm, sm.k, sm.q[s1], rp_smem(&sm.s_full));
                     if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
                     tmem_after();
                     add(tm + 256 + D, tm + 128, sm.q[s], j > 0);
                     mma_commit(one, rp_smem(&sm.q_empty[s]));
-                    if (j == nt - 1) mma_commit(one, rp_smem(&sm.acc_full));
                     if (j + 1 < nt) {
                         against(tm + 128, sm.v, sm.g[s1], rp_smem(&sm.dp_full));
                         if (j + 2 == nt) mma_commit(one, rp_smem(&sm.kv_empty));
-                    }
+                    } else
+                        mma_commit(one, rp_smem(&sm.acc_full));
                 }
                 base += nt;
             }
@@ -216,7 +217,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         rp_many_registers();
         const int b = warp >> 2, row = threadIdx.x & 127;
         const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + b * 64, td = tm + lanes + 128 + b * 64;
-        const float sl = A.scale * RP_LOG2E;
+        const f2 sl2 = rp_f2(A.scale * RP_LOG2E, A.scale * RP_LOG2E);
         u32 f = 0;                                      // tiles so far
         for (int n = 0;; ++n) {
             const int at = rp_attend_item(n, total);
@@ -233,9 +234,9 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 const int q0 = (first + j % per) * 128 + b * 64;
                 // (two places in turn: who has come to a tile's barrier has read the tile before)
                 float (*st)[64] = sm.stats[f & 1][b];
-                if (row < 64) { st[0][row] = next.x; st[1][row] = next.y; }
+                if (row < 64) { st[0][row] = -next.x; st[1][row] = -next.y; }
                 if (j + 1 < nt) next = stats(j + 1);
-                bar_arrive(rp_smem(&sm.st_full[b]));
+                bar_arrive_warp(rp_smem(&sm.st_full[b]), lane);
                 if (!(ok = bar_wait_warp(rp_smem(&sm.st_full[b]), f & 1, gave_up))) break;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, gave_up))) break;
                 tmem_after();
@@ -246,9 +247,12 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_loaded();
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
-                    const float4 l = *(const float4 *)&st[0][c];
-                    p[c] = rp_exp2(fmaf(__uint_as_float(s[c]), sl, -l.x)); p[c + 1] = rp_exp2(fmaf(__uint_as_float(s[c + 1]), sl, -l.y));
-                    p[c + 2] = rp_exp2(fmaf(__uint_as_float(s[c + 2]), sl, -l.z)); p[c + 3] = rp_exp2(fmaf(__uint_as_float(s[c + 3]), sl, -l.w));
+                    const ulonglong2 l = *(const ulonglong2 *)&st[0][c];         // (of the other sign)
+                    float a, e;
+                    rp_parts(rp_fma(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sl2, f2{ l.x }), a, e);
+                    p[c] = rp_exp2(a); p[c + 1] = rp_exp2(e);
+                    rp_parts(rp_fma(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), sl2, f2{ l.y }), a, e);
+                    p[c + 2] = rp_exp2(a); p[c + 3] = rp_exp2(e);
                 }
                 if (q0 + 64 > t.len || (A.causal && q0 < t.row0 + 128)) {
                     const int lo = A.causal ? r - q0 : 0, hi = t.len - q0;
@@ -260,7 +264,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_store32(ts, s);
                 tmem_stored();
                 tmem_before();
-                bar_arrive(rp_smem(&sm.p_full));
+                bar_arrive_warp(rp_smem(&sm.p_full), lane);
                 if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, gave_up))) break;
                 tmem_after();
                 tmem_load32(td, s);
@@ -268,14 +272,17 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_loaded();
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
-                    const float4 e = *(const float4 *)&st[1][c];
-                    s[c / 2] = rp_pair(p[c] * (__uint_as_float(s[c]) - e.x), p[c + 1] * (__uint_as_float(s[c + 1]) - e.y), X());
-                    s[c / 2 + 1] = rp_pair(p[c + 2] * (__uint_as_float(s[c + 2]) - e.z), p[c + 3] * (__uint_as_float(s[c + 3]) - e.w), X());
+                    const ulonglong2 e = *(const ulonglong2 *)&st[1][c];         // (of the other sign)
+                    float a, z;
+                    rp_parts(rp_mul(rp_f2(p[c], p[c + 1]), rp_add(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), f2{ e.x })), a, z);
+                    s[c / 2] = rp_pair(a, z, X());
+                    rp_parts(rp_mul(rp_f2(p[c + 2], p[c + 3]), rp_add(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), f2{ e.y })), a, z);
+                    s[c / 2 + 1] = rp_pair(a, z, X());
                 }
                 tmem_store32(td, s);
                 tmem_stored();
                 tmem_before();
-                bar_arrive(rp_smem(&sm.ds_full));
+                bar_arrive_warp(rp_smem(&sm.ds_full), lane);
             }
             if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
             tmem_after();
@@ -283,7 +290,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             X *out = b ? (X *)A.x[1] + (t.base + r) * A.token[1] + hk * A.hd[1] : (X *)A.x[0] + (t.base + r) * A.token[0] + hk * A.hd[0];
             store_row<X, D>(tm + lanes + 256 + b * D, out, A.d, r < t.len, !ok ? NAN : b ? A.scale : 1.0f);
             tmem_before();
-            bar_arrive(rp_smem(&sm.acc_empty));
+            bar_arrive_warp(rp_smem(&sm.acc_empty), lane);
         }
     }
     __syncwarp();
@@ -295,24 +302,22 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 // ---------------------------------------------------------------------------------------
 // queries: dq
 // ---------------------------------------------------------------------------------------
-// Tiles of 128 keys, 64 columns to each of the two groups of four warps.  The scores of the next tile are there when a tile's are worked on; do v^T of the next one, dq
-// of this one and the scores after the next are multiplied while the weights of the next one are worked out.  The gradients of the scores take their group's
-// scores' place as operand.  Columns: 2 * 128 + 128 + head_dim.
+// Tiles of 128 keys, 64 columns to each of the two groups of four warps.  q and do, which all tiles of a block share, lie in tensor memory as the operands of their
+// products: from shared memory a product of 128 x 128 x 16 reads all of the 128 bytes that a cycle of it has, with the copies coming in beside (220 us for what
+// takes the figure in the launch's comment).  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
+// tile and do v^T of the next while the weights of the next are.  Columns: scores 128, do v^T 128 (and in its place ds as operand), dq, q and do 64 each.
 template <int D> struct QuerySmem {
-    static constexpr int TILE = 128 * D * 2, KS = 3, VS = 2;
-    alignas(1024) unsigned char q[TILE];
-    alignas(1024) unsigned char g[TILE];
+    static constexpr int TILE = 128 * D * 2, KS = 3, VS = 3;
     alignas(1024) unsigned char k[KS][TILE];
     alignas(1024) unsigned char v[VS][TILE];
-    u64 q_full, q_empty, k_full[KS], k_empty[KS], v_full[VS], v_empty[VS], s_full[2], dp_full, ds_full, acc_full, acc_empty, done;
+    u64 q_full, k_full[KS], k_empty[KS], v_full[VS], v_empty[VS], s_full, s_empty, dp_full, ds_full, acc_full, done;
     u32 tmem;
     volatile int gave_up;
 };
 
 template <typename X, int D>
 __global__ void __launch_bounds__(ATTEND_THREADS, 1)
-k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                 const __grid_constant__ CUtensorMap map_g, const GradArgs A)
+k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const GradArgs A)
 {
     typedef QuerySmem<D> Smem;
     constexpr int KS = Smem::KS, VS = Smem::VS, PANELS = D / 64, PANEL = 128 * 128;
@@ -320,12 +325,10 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     Smem &sm = *(Smem *)(raw + ((1024 - (rp_smem(raw) & 1023)) & 1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        bar_init(rp_smem(&sm.q_full), 1); bar_init(rp_smem(&sm.q_empty), 1);
         for (int s = 0; s < KS; ++s) { bar_init(rp_smem(&sm.k_full[s]), 1); bar_init(rp_smem(&sm.k_empty[s]), 1); }
         for (int s = 0; s < VS; ++s) { bar_init(rp_smem(&sm.v_full[s]), 1); bar_init(rp_smem(&sm.v_empty[s]), 1); }
-        for (int i = 0; i < 2; ++i) bar_init(rp_smem(&sm.s_full[i]), 1);
-        bar_init(rp_smem(&sm.dp_full), 1); bar_init(rp_smem(&sm.ds_full), 256);
-        bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 256); bar_init(rp_smem(&sm.done), 1);
+        bar_init(rp_smem(&sm.q_full), 8); bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.s_empty), 8); bar_init(rp_smem(&sm.dp_full), 1);
+        bar_init(rp_smem(&sm.ds_full), 8); bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.done), 1);
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -334,27 +337,20 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     __syncthreads();
     tmem_after();
     const u32 tm = rp_uniform(sm.tmem);
-    const int total = A.head->count * A.Hq;
+    const int total = rp_uniform(A.head->count * A.Hq);
     volatile int *gave_up = &sm.gave_up;
 
     if (warp >= 8) {
         rp_few_registers();
         if (warp == ATTEND_COPY_WARP && lane == 0) {
-            tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v); tma_prefetch(&map_g);
-            int n = 0;
+            tma_prefetch(&map_k); tma_prefetch(&map_v);
             u32 fill = 0;
             bool ok = true;
-            for (; ok; ++n) {
+            for (int n = 0; ok; ++n) {
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
-                const int h = at % A.Hq, hk = h / A.share, nk = rp_attend_tiles(t, 0, A.causal);
-                if (n && !(ok = bar_wait(rp_smem(&sm.q_empty), (n - 1) & 1, gave_up))) break;
-                bar_expect(rp_smem(&sm.q_full), 2 * Smem::TILE);
-                for (int p = 0; p < PANELS; ++p) {
-                    tma_load3(rp_smem(sm.q) + p * PANEL, &map_q, p * 64, h, (int)t.base + t.row0, rp_smem(&sm.q_full));
-                    tma_load3(rp_smem(sm.g) + p * PANEL, &map_g, p * 64, h, (int)t.base + t.row0, rp_smem(&sm.q_full));
-                }
+                const int hk = at % A.Hq / A.share, nk = rp_attend_tiles(t, 0, A.causal);
                 for (int j = 0; j < nk; ++j, ++fill) {
                     const u32 ks = fill % KS, kt = fill / KS, vs = fill % VS, vt = fill / VS;
                     if (kt && !(ok = bar_wait(rp_smem(&sm.k_empty[ks]), (kt - 1) & 1, gave_up))) break;
@@ -369,8 +365,6 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 // nobody may leave while copies are under way
                 for (u32 f = fill > (u32)KS ? fill - KS : 0; f < fill; ++f) rp_drain(rp_smem(&sm.k_full[f % KS]), (f / KS) & 1);
                 for (u32 f = fill > (u32)VS ? fill - VS : 0; f < fill; ++f) rp_drain(rp_smem(&sm.v_full[f % VS]), (f / VS) & 1);
-                if (n) rp_drain(rp_smem(&sm.q_full), (n - 1) & 1);
-                rp_drain(rp_smem(&sm.q_full), n & 1);
             }
         }
         if (warp == ATTEND_MMA_WARP) {
@@ -382,54 +376,46 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
-                const int nk = rp_attend_tiles(t, 0, A.causal);
-                if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), n & 1, gave_up))) break;
-                auto scores = [&](int j) -> bool {
-                    const u32 f = base + j, s = f % KS;
-                    const int b = f & 1;
-                    if (!bar_wait_warp(rp_smem(&sm.k_full[s]), (f / KS) & 1, gave_up)) return false;
+                const int len = rp_uniform(t.len), nk = rp_uniform(rp_attend_tiles(t, 0, A.causal));
+                // 128 queries (or gradients) against a tile's keys (or values)
+                auto against = [&](u32 to, u32 rows, const unsigned char *tile, u32 bar) {
+                    const u32 b = mma_operand(rp_smem(tile), true, 0);
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x) mma_ts(one, to, rows + x * 8, b + (((x / 4) * PANEL + (x % 4) * 32) >> 4), shape_s, x > 0);
+                    mma_commit(one, bar);
+                };
+                auto arrived = [&](int j) -> bool {     // a tile's keys and values
+                    const u32 f = base + j;
+                    if (!bar_wait_warp(rp_smem(&sm.k_full[f % KS]), (f / KS) & 1, gave_up) || !bar_wait_warp(rp_smem(&sm.v_full[f % VS]), (f / VS) & 1, gave_up)) return false;
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
-                    if (t.len - j * 128 < 128) rp_clear_rows<D>(sm.k[s], t.len - j * 128, 128, lane);
-                    const u32 q = rp_uniform(mma_operand(rp_smem(sm.q), true, 0)), k = rp_uniform(mma_operand(rp_smem(sm.k[s]), true, 0));
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
-                        mma_ss(one, tm + b * 128, q + off, k + off, shape_s, x > 0);
-                    }
-                    mma_commit(one, rp_smem(&sm.s_full[b]));
+                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.k[f % KS], len - j * 128, 128, lane);
                     return true;
                 };
-                auto products = [&](int j) -> bool {        // do v^T
-                    const u32 f = base + j, s = f % VS;
-                    if (!bar_wait_warp(rp_smem(&sm.v_full[s]), (f / VS) & 1, gave_up)) return false;
-                    const u32 g = rp_uniform(mma_operand(rp_smem(sm.g), true, 0)), v = rp_uniform(mma_operand(rp_smem(sm.v[s]), true, 0));
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
-                        mma_ss(one, tm + 256, g + off, v + off, shape_s, x > 0);
-                    }
-                    mma_commit(one, rp_smem(&sm.dp_full));
-                    mma_commit(one, rp_smem(&sm.v_empty[s]));
-                    if (j == nk - 1) mma_commit(one, rp_smem(&sm.q_empty));
-                    return true;
-                };
-                // (the last tile's do v^T is issued behind its scores: when q_empty is arrived at, both are done with q and do)
-                if (!(ok = scores(0))) break;
-                if (nk > 1 && !(ok = scores(1))) break;
-                if (!(ok = products(0))) break;
-                if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
+                if (!(ok = arrived(0))) break;
+                // (who has handed over q and do has taken dq of the block before)
+                if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), n & 1, gave_up))) break;
+                tmem_after();
+                against(tm, tm + 384, sm.k[base % KS], rp_smem(&sm.s_full));
+                against(tm + 128, tm + 448, sm.v[base % VS], rp_smem(&sm.dp_full));
+                mma_commit(one, rp_smem(&sm.v_empty[base % VS]));
                 for (int j = 0; j < nk; ++j) {
                     const u32 f = base + j;
+                    if (j + 1 < nk && !(ok = arrived(j + 1))) break;
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.s_empty), f & 1, gave_up))) break;
+                    tmem_after();
+                    if (j + 1 < nk) against(tm, tm + 384, sm.k[(f + 1) % KS], rp_smem(&sm.s_full));
                     if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
                     tmem_after();
-                    if (j + 1 < nk && !(ok = products(j + 1))) break;
-                    const u32 a = rp_uniform(tm + (f & 1) * 128), k = rp_uniform(mma_operand(rp_smem(sm.k[f % KS]), false, PANEL));
+                    const u32 k = mma_operand(rp_smem(sm.k[f % KS]), false, PANEL);
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
-                        mma_ts(one, tm + 384, a + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        mma_ts(one, tm + 256, tm + 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                    if (j + 1 < nk) {
+                        against(tm + 128, tm + 448, sm.v[(f + 1) % VS], rp_smem(&sm.dp_full));
+                        mma_commit(one, rp_smem(&sm.v_empty[(f + 1) % VS]));
+                    } else
+                        mma_commit(one, rp_smem(&sm.acc_full));
                     mma_commit(one, rp_smem(&sm.k_empty[f % KS]));
-                    if (j == nk - 1) mma_commit(one, rp_smem(&sm.acc_full));
-                    if (j + 2 < nk && !(ok = scores(j + 2))) break;
                 }
                 base += nk;
             }
@@ -440,27 +426,53 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     } else {
         rp_many_registers();
         const int b = warp >> 2, row = threadIdx.x & 127;
-        const u32 lanes = (u32)(warp & 3) << 21, td = tm + lanes + 256 + b * 64;
-        const float sl = A.scale * RP_LOG2E;
+        const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + b * 64, td = tm + lanes + 128 + b * 64;
+        const f2 sl2 = rp_f2(A.scale * RP_LOG2E, A.scale * RP_LOG2E);
         u32 f = 0;                                      // tiles so far
+        u32 w[64];                                      // a row of q (first group) or of do (second): two elements a word
+        auto fetch = [&](int n) {
+            const int at = rp_attend_item(n, total);
+            if (at < 0) return;
+            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
+            const int r = t.row0 + row;
+            const X *p = (b ? (const X *)A.rows[1] + (t.base + r) * A.r_token[1] + at % A.Hq * A.r_head[1] : (const X *)A.rows[0] + (t.base + r) * A.r_token[0] + at % A.Hq * A.r_head[0]);
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (r < t.len && c * 8 < A.d) v = *(const uint4 *)(p + c * 8);
+                w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
+            }
+        };
+        fetch(0);
         for (int n = 0;; ++n) {
             const int at = rp_attend_item(n, total);
             if (at < 0) break;
             const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
             const int h = at % A.Hq, nk = rp_attend_tiles(t, 0, A.causal), r = t.row0 + row;
+#pragma unroll
+            for (int c = 0; c < D / 2; c += 32) tmem_store32(tm + lanes + 384 + b * 64 + c, w + c);
+            tmem_stored();
+            tmem_before();
+            bar_arrive_warp(rp_smem(&sm.q_full), lane);
             const float2 st = r < t.len ? A.stats[(i64)h * A.T + t.base + r] : make_float2(0.0f, 0.0f);
+            const f2 lse2 = rp_f2(-st.x, -st.x), delta2 = rp_f2(-st.y, -st.y);
             bool ok = true;
             for (int j = 0; j < nk; ++j, ++f) {
-                const u32 ts = tm + lanes + (f & 1) * 128 + b * 64;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[f & 1]), (f >> 1) & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, gave_up))) break;
                 tmem_after();
                 u32 s[64];
-                float p[64];
+                f2 p[32];
                 tmem_load32(ts, s);
                 tmem_load32(ts + 32, s + 32);
                 tmem_loaded();
+                tmem_before();
+                bar_arrive_warp(rp_smem(&sm.s_empty), lane);
 #pragma unroll
-                for (int c = 0; c < 64; ++c) p[c] = rp_exp2(fmaf(__uint_as_float(s[c]), sl, -st.x));
+                for (int c = 0; c < 32; ++c) {
+                    float x, y;
+                    rp_parts(rp_fma(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sl2, lse2), x, y);
+                    p[c] = rp_f2(rp_exp2(x), rp_exp2(y));
+                }
                 const int k0 = j * 128 + b * 64, lim = (A.causal ? min(t.len, r + 1) : t.len) - k0;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, gave_up))) break;
                 tmem_after();
@@ -468,25 +480,34 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 tmem_load32(td + 32, s + 32);
                 tmem_loaded();
 #pragma unroll
-                for (int c = 0; c < 64; ++c) p[c] *= __uint_as_float(s[c]) - st.y;
+                for (int c = 0; c < 32; ++c) p[c] = rp_mul(p[c], rp_add(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), delta2));
                 if (k0 + 64 > t.len || (A.causal && k0 + 63 > t.row0)) {
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) p[c] = c < lim ? p[c] : 0.0f;
-                }
+                    for (int c = 0; c < 32; ++c) {
+                        float x, y;
+                        rp_parts(p[c], x, y);
+                        s[c] = rp_pair(2 * c < lim ? x : 0.0f, 2 * c + 1 < lim ? y : 0.0f, X());
+                    }
+                } else {
 #pragma unroll
-                for (int c = 0; c < 32; ++c) s[c] = rp_pair(p[2 * c], p[2 * c + 1], X());
-                tmem_store32(ts, s);
+                    for (int c = 0; c < 32; ++c) {
+                        float x, y;
+                        rp_parts(p[c], x, y);
+                        s[c] = rp_pair(x, y, X());
+                    }
+                }
+                tmem_store32(td, s);
                 tmem_stored();
                 tmem_before();
-                bar_arrive(rp_smem(&sm.ds_full));
+                bar_arrive_warp(rp_smem(&sm.ds_full), lane);
             }
+            fetch(n + 1);                               // while dq is finished and handed over
             if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
             tmem_after();
             // each group hands over one half of the columns
             X *out = (X *)A.x[0] + (t.base + r) * A.token[0] + h * A.hd[0] + b * (D / 2);
-            store_row<X, D / 2>(tm + lanes + 384 + b * (D / 2), out, A.d - b * (D / 2), r < t.len, ok ? A.scale : NAN);
+            store_row<X, D / 2>(tm + lanes + 256 + b * (D / 2), out, A.d - b * (D / 2), r < t.len, ok ? A.scale : NAN);
             tmem_before();
-            bar_arrive(rp_smem(&sm.acc_empty));
         }
     }
     __syncwarp();
@@ -517,7 +538,7 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
     k_attend_keys<X, D><<<(int)std::min((i64)sms, most * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
     RP_TRY(rp_op_launched());
-    k_attend_queries<X, D><<<(int)std::min((i64)sms, most * keys.Hq), ATTEND_THREADS, sq, stream>>>(M.q, M.k, M.v, M.g, queries);
+    k_attend_queries<X, D><<<(int)std::min((i64)sms, most * keys.Hq), ATTEND_THREADS, sq, stream>>>(M.k, M.v, queries);
     return rp_op_launched();
 }
 
@@ -564,6 +585,8 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     }
     G[0].x[0] = v_grad->x; G[0].token[0] = v_grad->token; G[0].hd[0] = v_grad->head;
     G[0].x[1] = k_grad->x; G[0].token[1] = k_grad->token; G[0].hd[1] = k_grad->head;
+    G[1].rows[0] = q->x; G[1].r_token[0] = q->token; G[1].r_head[0] = q->head;
+    G[1].rows[1] = out_grad->x; G[1].r_token[1] = out_grad->token; G[1].r_head[1] = out_grad->head;
     G[1].x[0] = q_grad->x; G[1].token[0] = q_grad->token; G[1].hd[0] = q_grad->head;
     const int sms = rp_op_sms(dev.device);
     const int ctas = (int)std::min((T * Hq + 15) / 16, (i64)sms * 8);

@@ -12,6 +12,13 @@ __device__ __forceinline__ u32 rp_smem(const void *p) { return (u32)__cvta_gener
 // ---- barriers ---------------------------------------------------------------------------
 __device__ __forceinline__ void bar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// One arrival for a warp, behind what all its lanes have done.
+__device__ __forceinline__ void bar_arrive_warp(u32 bar, int lane)
+{
+    __syncwarp();
+    if (lane == 0) bar_arrive(bar);
+    __syncwarp();
+}
 __device__ __forceinline__ void bar_expect(u32 bar, u32 bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -97,7 +104,7 @@ __device__ __forceinline__ void tmem_store32(u32 at, const u32 *r)
 // `along_k`: rows are rows (or columns) of the product and the 64 elements run along the summed dimension; a step of 16 of those is 32 bytes on.
 // Otherwise the rows run along the summed dimension; a step of 16 is 2048 bytes on, the next 64 elements are `panel` bytes on.
 // A value that all lanes of a warp have alike, in a register that the warp has once: the products take their operands from such, and what is worked out from
-// one stays there (moved over one by one they issue at half the rate).
+// such ones in branches and loops that go by them stays there (moved over one by one for each product, they issue at half the rate).
 __device__ __forceinline__ u32 rp_uniform(u32 x) { return __reduce_or_sync(0xffffffffu, x); }
 // Descriptor of an operand: the low word has its address, the high word is fixed (eight rows of 128 bytes, version, swizzle).
 #define MMA_HIGH ((1024u >> 4) | (1u << 14) | (2u << 29))
