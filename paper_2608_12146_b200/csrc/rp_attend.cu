@@ -98,10 +98,13 @@ struct AttendArgs {
     int *status;
 };
 
+// A stage holds the values of one tile and the keys of the next, which are waited for and let go of together: of nk tiles there are nk + 1 stages, the first without
+// values, the last without keys.
 template <int D> struct FwdSmem {
-    static constexpr int TILE = 128 * D * 2, STAGES = D == 128 ? 4 : 6;
+    static constexpr int TILE = 128 * D * 2, STAGES = D == 128 ? 2 : 4;
     alignas(1024) unsigned char q[2][TILE];
-    alignas(1024) unsigned char kv[STAGES][TILE];
+    alignas(1024) unsigned char v[STAGES][TILE];
+    alignas(1024) unsigned char k[STAGES][TILE];
     u64 q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_full[2], o_full[2], done;
     u32 tmem;
     volatile int gave_up;
@@ -151,12 +154,14 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     for (int p = 0; p < PANELS; ++p)
                         tma_load3(rp_smem(sm.q[i]) + p * PANEL, &map_q, p * 64, h, (int)t.base + t.row0 + 128 * i, rp_smem(&sm.q_full));
                 const int nk = rp_attend_tiles(t, tiles - 1, A.causal);
-                for (int j = 0; j < 2 * nk; ++j, ++fill) {
+                for (int j = 0; j <= nk; ++j, ++fill) {
                     const u32 s = fill % STAGES, turn = fill / STAGES;
                     if (turn && !(ok = bar_wait(rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, gave_up))) break;
-                    bar_expect(rp_smem(&sm.kv_full[s]), Smem::TILE);
-                    for (int p = 0; p < PANELS; ++p)
-                        tma_load3(rp_smem(sm.kv[s]) + p * PANEL, j & 1 ? &map_v : &map_k, p * 64, hk, (int)t.base + (j >> 1) * 128, rp_smem(&sm.kv_full[s]));
+                    bar_expect(rp_smem(&sm.kv_full[s]), j && j < nk ? 2 * Smem::TILE : Smem::TILE);
+                    for (int p = 0; p < PANELS; ++p) {
+                        if (j) tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + (j - 1) * 128, rp_smem(&sm.kv_full[s]));
+                        if (j < nk) tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
+                    }
                 }
             }
             if (!ok) {
@@ -169,10 +174,9 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
             const u32 one = lane == 0;
-            u32 used = 0, p0 = 0, p1 = 0;                   // copies taken from the ring; weights taken of each tile
-            bool ok = true;
+            u32 used = 0, p0 = 0, p1 = 0;                   // stages taken; weights taken of each tile
             auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
-                const u32 a = mma_operand(rp_smem(sm.q[i]), true, 0), b = mma_operand(rp_smem(sm.kv[stage]), true, 0);
+                const u32 a = mma_operand(rp_smem(sm.q[i]), true, 0), b = mma_operand(rp_smem(sm.k[stage]), true, 0);
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
                     const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
@@ -180,47 +184,46 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 }
                 mma_commit(one, rp_smem(&sm.s_full[i]));
             };
-            for (int round = 0; ok; ++round) {
+            auto outputs = [&](int i, u32 stage, bool more) {          // its weights times the values in a stage
+                const u32 v = mma_operand(rp_smem(sm.v[stage]), false, PANEL);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) mma_ts(one, tm + 256 + i * D, tm + i * 128 + x * 8, v + x * (2048 >> 4), shape_o, more || x > 0);
+            };
+            for (int round = 0;; ++round) {
                 const int at = rp_attend_item(round, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
                 const int left = rp_uniform(t.len - t.row0), tiles = left > 128 ? 2 : 1, len = rp_uniform(t.len);
                 const int n0 = rp_uniform(rp_attend_tiles(t, 0, A.causal)), n1 = tiles == 2 ? rp_uniform(rp_attend_tiles(t, 1, A.causal)) : 0, nk = max(n0, n1);
-                if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), round & 1, gave_up))) break;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up))) break;
+                bar_hold(rp_smem(&sm.q_full), round & 1, gave_up);
+                bar_hold(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up);
                 scores(0, used % STAGES);
                 if (tiles == 2) scores(1, used % STAGES);
                 mma_commit(one, rp_smem(&sm.kv_empty[used % STAGES]));
                 if (nk == 1) mma_commit(one, rp_smem(&sm.q_empty));
                 ++used;
-                for (int j = 0; j < nk; ++j) {
-                    const u32 sv = used % STAGES, sk = (used + 1) % STAGES;
+                for (int j = 0; j < nk; ++j, ++used) {
+                    const u32 s = used % STAGES;
                     // (what is copied has mostly come when the weights have)
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full[sv]), (used / STAGES) & 1, gave_up))) break;
-                    if (j + 1 < nk && !(ok = bar_wait_warp(rp_smem(&sm.kv_full[sk]), ((used + 1) / STAGES) & 1, gave_up))) break;
+                    bar_hold(rp_smem(&sm.kv_full[s]), (used / STAGES) & 1, gave_up);
                     // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
-                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.kv[sv], len - j * 128, 128, lane);
-                    const u32 v = mma_operand(rp_smem(sm.kv[sv]), false, PANEL);
+                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.v[s], len - j * 128, 128, lane);
                     if (j < n0) {
-                        if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[0]), p0++ & 1, gave_up))) break;
+                        bar_hold(rp_smem(&sm.p_full[0]), p0++ & 1, gave_up);
                         tmem_after();
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) mma_ts(one, tm + 256, tm + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        outputs(0, s, j > 0);
                         if (j == n0 - 1) mma_commit(one, rp_smem(&sm.o_full[0]));
-                        else scores(0, sk);
+                        else scores(0, s);
                     }
                     if (j < n1) {
-                        if (!(ok = bar_wait_warp(rp_smem(&sm.p_full[1]), p1++ & 1, gave_up))) break;
+                        bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, gave_up);
                         tmem_after();
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) mma_ts(one, tm + 256 + D, tm + 128 + x * 8, v + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        outputs(1, s, j > 0);
                         if (j == n1 - 1) mma_commit(one, rp_smem(&sm.o_full[1]));
-                        else scores(1, sk);
+                        else scores(1, s);
                     }
-                    mma_commit(one, rp_smem(&sm.kv_empty[sv]));
-                    if (j + 1 < nk) mma_commit(one, rp_smem(&sm.kv_empty[sk]));
-                    if (j + 2 == nk) mma_commit(one, rp_smem(&sm.q_empty));
-                    used += j + 1 < nk ? 2 : 1;
+                    mma_commit(one, rp_smem(&sm.kv_empty[s]));
+                    if (j == nk - 2) mma_commit(one, rp_smem(&sm.q_empty));
                 }
             }
             // nobody may leave while products are under way
@@ -292,7 +295,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 tmem_before();
                 bar_arrive_warp(rp_smem(&sm.p_full[i]), lane);
             }
-            if (ok) ok = bar_wait_warp(rp_smem(&sm.o_full[i]), os & 1, gave_up);
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.o_full[i]), os & 1, gave_up) && !*gave_up;
             ++os;
             tmem_after();
             const float f = ok ? 1.0f / l : NAN;

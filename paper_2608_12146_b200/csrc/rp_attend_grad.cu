@@ -152,8 +152,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
             const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
-            bool ok = true;
-            for (int n = 0; ok; ++n) {
+            for (int n = 0;; ++n) {
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
@@ -169,14 +168,13 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     }
                     mma_commit(one, bar);
                 };
-                auto arrived = [&](u32 f) -> bool {     // a tile's queries and gradients
+                auto arrived = [&](u32 f) {     // a tile's queries and gradients
                     const u32 s = f % STAGES;
-                    if (!bar_wait_warp(rp_smem(&sm.q_full[s]), (f / STAGES) & 1, gave_up)) return false;
+                    bar_hold(rp_smem(&sm.q_full[s]), (f / STAGES) & 1, gave_up);
                     // queries behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
                     const int left = len - tile * 128;
                     if (left < 128) { rp_clear_rows<D>(sm.q[s], left, 128, lane); rp_clear_rows<D>(sm.g[s], left, 128, lane); }
                     tile = tile + 1 == first + per ? first : tile + 1;
-                    return true;
                 };
                 // a tile's weights (or gradients of its scores) times its gradients (or queries)
                 auto add = [&](u32 to, u32 weights, const unsigned char *rows, bool more) {
@@ -184,20 +182,20 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
                     for (int x = 0; x < 8; ++x) mma_ts(one, to, weights + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
                 };
-                if (!(ok = bar_wait_warp(rp_smem(&sm.kv_full), n & 1, gave_up))) break;
-                if (!(ok = arrived(base))) break;
+                bar_hold(rp_smem(&sm.kv_full), n & 1, gave_up);
+                arrived(base);
                 against(tm, sm.k, sm.q[base % STAGES], rp_smem(&sm.s_full));
                 against(tm + 128, sm.v, sm.g[base % STAGES], rp_smem(&sm.dp_full));
                 if (nt == 1) mma_commit(one, rp_smem(&sm.kv_empty));
-                if (n && !(ok = bar_wait_warp(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up))) break;
+                if (n) bar_hold(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up);
                 for (int j = 0; j < nt; ++j) {
                     const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
-                    if (j + 1 < nt && !(ok = arrived(f + 1))) break;        // (mostly before the weights have)
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.p_full), f & 1, gave_up))) break;
+                    if (j + 1 < nt) arrived(f + 1);         // (mostly before the weights have)
+                    bar_hold(rp_smem(&sm.p_full), f & 1, gave_up);
                     tmem_after();
                     add(tm + 256, tm, sm.g[s], j > 0);
                     if (j + 1 < nt) against(tm, sm.k, sm.q[s1], rp_smem(&sm.s_full));
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
+                    bar_hold(rp_smem(&sm.ds_full), f & 1, gave_up);
                     tmem_after();
                     add(tm + 256 + D, tm + 128, sm.q[s], j > 0);
                     mma_commit(one, rp_smem(&sm.q_empty[s]));
@@ -284,7 +282,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_before();
                 bar_arrive_warp(rp_smem(&sm.ds_full), lane);
             }
-            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up) && !*gave_up;
             tmem_after();
             // the first group hands over dv, the second dk
             X *out = b ? (X *)A.x[1] + (t.base + r) * A.token[1] + hk * A.hd[1] : (X *)A.x[0] + (t.base + r) * A.token[0] + hk * A.hd[0];
@@ -307,10 +305,10 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 // takes the figure in the launch's comment).  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
 // tile and do v^T of the next while the weights of the next are.  Columns: scores 128, do v^T 128 (and in its place ds as operand), dq, q and do 64 each.
 template <int D> struct QuerySmem {
-    static constexpr int TILE = 128 * D * 2, KS = 3, VS = 3;
-    alignas(1024) unsigned char k[KS][TILE];
-    alignas(1024) unsigned char v[VS][TILE];
-    u64 q_full, k_full[KS], k_empty[KS], v_full[VS], v_empty[VS], s_full, s_empty, dp_full, ds_full, acc_full, done;
+    static constexpr int TILE = 128 * D * 2, STAGES = 3;
+    alignas(1024) unsigned char k[STAGES][TILE];
+    alignas(1024) unsigned char v[STAGES][TILE];
+    u64 q_full, kv_full[STAGES], kv_empty[STAGES], s_full, s_empty, dp_full, ds_full, acc_full, done;
     u32 tmem;
     volatile int gave_up;
 };
@@ -320,13 +318,12 @@ __global__ void __launch_bounds__(ATTEND_THREADS, 1)
 k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const GradArgs A)
 {
     typedef QuerySmem<D> Smem;
-    constexpr int KS = Smem::KS, VS = Smem::VS, PANELS = D / 64, PANEL = 128 * 128;
+    constexpr int STAGES = Smem::STAGES, PANELS = D / 64, PANEL = 128 * 128;
     extern __shared__ __align__(1024) unsigned char raw[];
     Smem &sm = *(Smem *)(raw + ((1024 - (rp_smem(raw) & 1023)) & 1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < KS; ++s) { bar_init(rp_smem(&sm.k_full[s]), 1); bar_init(rp_smem(&sm.k_empty[s]), 1); }
-        for (int s = 0; s < VS; ++s) { bar_init(rp_smem(&sm.v_full[s]), 1); bar_init(rp_smem(&sm.v_empty[s]), 1); }
+        for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.kv_full[s]), 1); bar_init(rp_smem(&sm.kv_empty[s]), 1); }
         bar_init(rp_smem(&sm.q_full), 8); bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.s_empty), 8); bar_init(rp_smem(&sm.dp_full), 1);
         bar_init(rp_smem(&sm.ds_full), 8); bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.done), 1);
         sm.gave_up = 0;
@@ -352,27 +349,25 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
                 const int hk = at % A.Hq / A.share, nk = rp_attend_tiles(t, 0, A.causal);
                 for (int j = 0; j < nk; ++j, ++fill) {
-                    const u32 ks = fill % KS, kt = fill / KS, vs = fill % VS, vt = fill / VS;
-                    if (kt && !(ok = bar_wait(rp_smem(&sm.k_empty[ks]), (kt - 1) & 1, gave_up))) break;
-                    if (vt && !(ok = bar_wait(rp_smem(&sm.v_empty[vs]), (vt - 1) & 1, gave_up))) break;
-                    bar_expect(rp_smem(&sm.k_full[ks]), Smem::TILE);
-                    for (int p = 0; p < PANELS; ++p) tma_load3(rp_smem(sm.k[ks]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.k_full[ks]));
-                    bar_expect(rp_smem(&sm.v_full[vs]), Smem::TILE);
-                    for (int p = 0; p < PANELS; ++p) tma_load3(rp_smem(sm.v[vs]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.v_full[vs]));
+                    const u32 s = fill % STAGES, turn = fill / STAGES;
+                    if (turn && !(ok = bar_wait(rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, gave_up))) break;
+                    bar_expect(rp_smem(&sm.kv_full[s]), 2 * Smem::TILE);
+                    for (int p = 0; p < PANELS; ++p) {
+                        tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
+                        tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
+                    }
                 }
             }
             if (!ok) {
                 // nobody may leave while copies are under way
-                for (u32 f = fill > (u32)KS ? fill - KS : 0; f < fill; ++f) rp_drain(rp_smem(&sm.k_full[f % KS]), (f / KS) & 1);
-                for (u32 f = fill > (u32)VS ? fill - VS : 0; f < fill; ++f) rp_drain(rp_smem(&sm.v_full[f % VS]), (f / VS) & 1);
+                for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1);
             }
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
             const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
-            bool ok = true;
-            for (int n = 0; ok; ++n) {
+            for (int n = 0;; ++n) {
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
@@ -384,38 +379,35 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     for (int x = 0; x < D / 16; ++x) mma_ts(one, to, rows + x * 8, b + (((x / 4) * PANEL + (x % 4) * 32) >> 4), shape_s, x > 0);
                     mma_commit(one, bar);
                 };
-                auto arrived = [&](int j) -> bool {     // a tile's keys and values
+                auto arrived = [&](int j) {             // a tile's keys and values
                     const u32 f = base + j;
-                    if (!bar_wait_warp(rp_smem(&sm.k_full[f % KS]), (f / KS) & 1, gave_up) || !bar_wait_warp(rp_smem(&sm.v_full[f % VS]), (f / VS) & 1, gave_up)) return false;
+                    bar_hold(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1, gave_up);
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
-                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.k[f % KS], len - j * 128, 128, lane);
-                    return true;
+                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.k[f % STAGES], len - j * 128, 128, lane);
                 };
-                if (!(ok = arrived(0))) break;
+                arrived(0);
                 // (who has handed over q and do has taken dq of the block before)
-                if (!(ok = bar_wait_warp(rp_smem(&sm.q_full), n & 1, gave_up))) break;
+                bar_hold(rp_smem(&sm.q_full), n & 1, gave_up);
                 tmem_after();
-                against(tm, tm + 384, sm.k[base % KS], rp_smem(&sm.s_full));
-                against(tm + 128, tm + 448, sm.v[base % VS], rp_smem(&sm.dp_full));
-                mma_commit(one, rp_smem(&sm.v_empty[base % VS]));
+                against(tm, tm + 384, sm.k[base % STAGES], rp_smem(&sm.s_full));
+                against(tm + 128, tm + 448, sm.v[base % STAGES], rp_smem(&sm.dp_full));
                 for (int j = 0; j < nk; ++j) {
-                    const u32 f = base + j;
-                    if (j + 1 < nk && !(ok = arrived(j + 1))) break;
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.s_empty), f & 1, gave_up))) break;
+                    const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
+                    if (j + 1 < nk) {
+                        arrived(j + 1);
+                        bar_hold(rp_smem(&sm.s_empty), f & 1, gave_up);
+                        tmem_after();
+                        against(tm, tm + 384, sm.k[s1], rp_smem(&sm.s_full));
+                    }
+                    bar_hold(rp_smem(&sm.ds_full), f & 1, gave_up);
                     tmem_after();
-                    if (j + 1 < nk) against(tm, tm + 384, sm.k[(f + 1) % KS], rp_smem(&sm.s_full));
-                    if (!(ok = bar_wait_warp(rp_smem(&sm.ds_full), f & 1, gave_up))) break;
-                    tmem_after();
-                    const u32 k = mma_operand(rp_smem(sm.k[f % KS]), false, PANEL);
+                    const u32 k = mma_operand(rp_smem(sm.k[s]), false, PANEL);
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
                         mma_ts(one, tm + 256, tm + 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
-                    if (j + 1 < nk) {
-                        against(tm + 128, tm + 448, sm.v[(f + 1) % VS], rp_smem(&sm.dp_full));
-                        mma_commit(one, rp_smem(&sm.v_empty[(f + 1) % VS]));
-                    } else
-                        mma_commit(one, rp_smem(&sm.acc_full));
-                    mma_commit(one, rp_smem(&sm.k_empty[f % KS]));
+                    mma_commit(one, rp_smem(&sm.kv_empty[s]));
+                    if (j + 1 < nk) against(tm + 128, tm + 448, sm.v[s1], rp_smem(&sm.dp_full));
+                    else mma_commit(one, rp_smem(&sm.acc_full));
                 }
                 base += nk;
             }
@@ -502,7 +494,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 bar_arrive_warp(rp_smem(&sm.ds_full), lane);
             }
             fetch(n + 1);                               // while dq is finished and handed over
-            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up);
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up) && !*gave_up;
             tmem_after();
             // each group hands over one half of the columns
             X *out = (X *)A.x[0] + (t.base + r) * A.token[0] + h * A.hd[0] + b * (D / 2);
