@@ -13,72 +13,10 @@
 
 #include "rp_attend.cuh"
 
-// ---------------------------------------------------------------------------------------
-// what is to be done
-// ---------------------------------------------------------------------------------------
-// CTA 0 lists the blocks of `rows` tokens of all samples, those with the most tiles of others first; the other CTAs clear the rows that no sample holds.
-#define PLAN_BUCKETS 1024
-__global__ void __launch_bounds__(1024) k_attend_plan(AttendPlan A)
+__global__ void __launch_bounds__(1024) k_attend_plan(AttendPlan P, AttendClears C)
 {
-    if (blockIdx.x) {
-        i64 head = A.start[0], tail = A.start[A.N];
-        head = min(max(head, (i64)0), A.T); tail = min(max(tail, head), A.T);
-        const i64 gone = head + A.T - tail;
-        for (int o = 0; o < A.n_clear; ++o) {
-            const AttendClear &C = A.clear[o];
-            const i64 width = (i64)C.heads * C.d;
-            for (i64 x = (i64)(blockIdx.x - 1) * 1024 + threadIdx.x; x < gone * width; x += (i64)(gridDim.x - 1) * 1024) {
-                i64 t = x / width;
-                const i64 h = x % width / C.d, i = x % C.d;
-                t = t < head ? t : tail + t - head;
-                const i64 at = t * C.token + h * C.head + i;
-                if (C.bytes == 2) ((unsigned short *)C.x)[at] = 0; else ((float *)C.x)[at] = 0.0f;
-            }
-        }
-        return;
-    }
-    __shared__ int count[PLAN_BUCKETS];
-    __shared__ int from[PLAN_BUCKETS];
-    for (int x = threadIdx.x; x < PLAN_BUCKETS; x += 1024) count[x] = 0;
-    __syncthreads();
-    // work of a block: queries (by_key 0) see the keys up to them, keys (by_key 1) are seen by the queries from them on
-    for (int pass = 0; pass < 2; ++pass) {
-        for (int i = threadIdx.x >> 5; i < A.N; i += 32) {
-            const i64 lo = max(A.start[i], (i64)0), hi = min(A.start[i + 1], A.T);
-            const int blocks = hi > lo ? (int)((hi - lo + A.rows - 1) / A.rows) : 0;
-            for (int b = threadIdx.x & 31; b < blocks; b += 32) {
-                const int work = !A.causal ? blocks : A.by_key ? blocks - b : b + 1;
-                const int bucket = PLAN_BUCKETS - 1 - min(work - 1, PLAN_BUCKETS - 1);
-                if (pass == 0) atomicAdd(&count[bucket], 1);
-                else {
-                    const int at = atomicAdd(&from[bucket], 1);
-                    if (at < A.most) A.items[at] = make_int2(i, b);
-                }
-            }
-        }
-        __syncthreads();
-        if (pass == 0 && threadIdx.x < 32) {
-            int sum = 0;
-            for (int base = 0; base < PLAN_BUCKETS; base += 32) {
-                int c = count[base + threadIdx.x], x = c;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int y = __shfl_up_sync(0xffffffffu, x, o);
-                    if ((int)threadIdx.x >= o) x += y;
-                }
-                from[base + threadIdx.x] = sum + x - c;
-                sum += __shfl_sync(0xffffffffu, x, 31);
-            }
-            if (threadIdx.x == 0) { A.head->count = min(sum, A.most); A.head->status = 0; }
-        }
-        __syncthreads();
-    }
-}
-
-int rp_launch_attend_plan(const AttendPlan &A, cudaStream_t stream)
-{
-    k_attend_plan<<<1 + 32, 1024, 0, stream>>>(A);
-    return rp_op_launched();
+    if (blockIdx.x == 0) rp_attend_plan(P);
+    else rp_attend_clear(C, P.start, P.N, P.T, blockIdx.x - 1, gridDim.x - 1);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -235,6 +173,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         const int i = warp >> 2, row = threadIdx.x & 127;
         const u32 lanes = (u32)(warp & 3) << 21, ts = tm + lanes + i * 128, to = tm + lanes + 256 + i * D;
         const float sl = A.scale * RP_LOG2E;
+        const f2 sl2 = rp_f2(sl, sl);
         u32 ss = 0, os = 0;
         for (int round = 0;; ++round) {
             const int at = rp_attend_item(round, total);
@@ -280,15 +219,19 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         }
                     }
                 }
-                const float shift = -m * sl;
-                float sum0 = 0.0f, sum1 = 0.0f;
+                const f2 shift = rp_f2(-m * sl, -m * sl);
+                f2 sum0 = rp_f2(0.0f, 0.0f), sum1 = sum0;
 #pragma unroll
-                for (int c = 0; c < 128; c += 2) {
-                    const float a = rp_exp2(fmaf(__uint_as_float(s[c]), sl, shift)), b = rp_exp2(fmaf(__uint_as_float(s[c + 1]), sl, shift));
-                    sum0 += a; sum1 += b;
-                    s[c / 2] = rp_pair(a, b, X());
+                for (int c = 0; c < 64; ++c) {
+                    const f2 e = rp_exp2(rp_fma(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sl2, shift));
+                    if (c & 1) sum1 = rp_add(sum1, e); else sum0 = rp_add(sum0, e);
+                    float a, b;
+                    rp_parts(e, a, b);
+                    s[c] = rp_pair(a, b, X());
                 }
-                l += sum0 + sum1;
+                float a, b;
+                rp_parts(rp_add(sum0, sum1), a, b);
+                l += a + b;
                 tmem_store32(ts, s);
                 tmem_store32(ts + 32, s + 32);
                 tmem_stored();
@@ -400,14 +343,16 @@ extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_v
     int2 *items = (int2 *)(head + 1);
     AttendPlan P = {};
     P.start = (const i64 *)start; P.T = n_tokens; P.N = n_samples; P.rows = 256; P.causal = a->causal; P.by_key = 0; P.most = (int)(n_tokens / 256 + n_samples);
-    P.head = head; P.items = items; P.n_clear = 1;
-    P.clear[0] = { out->x, out->token, out->head, a->q_heads, a->head_dim, 2 };
-    if (lse && lse->x) P.clear[P.n_clear++] = { lse->x, lse->token, lse->head, a->q_heads, 1, 4 };
+    P.head = head; P.items = items;
+    AttendClears C = {};
+    C.x[C.n++] = { out->x, out->token, out->head, a->q_heads, a->head_dim, 2 };
+    if (lse && lse->x) C.x[C.n++] = { lse->x, lse->token, lse->head, a->q_heads, 1, 4 };
     CUtensorMap mq, mk, mv;
     RP_TRY(rp_tensor_map(&mq, a->type, q->x, n_tokens, a->q_heads, a->head_dim, q->token, q->head, 128));
     RP_TRY(rp_tensor_map(&mk, a->type, k->x, n_tokens, a->kv_heads, a->head_dim, k->token, k->head, 128));
     RP_TRY(rp_tensor_map(&mv, a->type, v->x, n_tokens, a->kv_heads, a->head_dim, v->token, v->head, 128));
-    RP_TRY(rp_launch_attend_plan(P, stream));
+    k_attend_plan<<<1 + 32, 1024, 0, stream>>>(P, C);
+    RP_TRY(rp_op_launched());
     AttendArgs A = {};
     A.head = head; A.items = items; A.start = (const i64 *)start; A.T = n_tokens; A.N = n_samples; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads;
     A.d = a->head_dim; A.causal = a->causal; A.scale = a->scale; A.out = out->x; A.o_token = out->token; A.o_head = out->head;

@@ -3,7 +3,7 @@
 
 #include "rp_tensor.cuh"
 
-struct AttendHead { int status, count, pad[2]; };       // front of the workspace; items [count] behind it: (sample, block of its tokens)
+struct AttendHead { int status, count, ticket, pad; };  // front of the workspace; items [count] behind it: (sample, block of its tokens); ticket: items taken so far
 struct AttendClear { void *x; i64 token, head; int heads, d, bytes; };
 struct AttendPlan {
     const i64 *start;
@@ -11,10 +11,68 @@ struct AttendPlan {
     int N, rows, causal, by_key, most;                  // most: room for items
     AttendHead *head;
     int2 *items;
-    AttendClear clear[3];                                // outputs whose rows of no sample are cleared
-    int n_clear;
 };
-int rp_launch_attend_plan(const AttendPlan &A, cudaStream_t stream);
+struct AttendClears { AttendClear x[3]; int n; };       // outputs whose rows of no sample are cleared
+
+// By one CTA of 1024 threads: lists the blocks of `rows` tokens of all samples, those with the most tiles of others first.
+// Work of a block: queries (by_key 0) see the keys up to them, keys (by_key 1) are seen by the queries from them on.
+#define PLAN_BUCKETS 1024
+static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
+{
+    __shared__ int count[PLAN_BUCKETS];
+    __shared__ int from[PLAN_BUCKETS];
+    for (int x = threadIdx.x; x < PLAN_BUCKETS; x += 1024) count[x] = 0;
+    __syncthreads();
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int i = threadIdx.x >> 5; i < A.N; i += 32) {
+            const i64 lo = max(A.start[i], (i64)0), hi = min(A.start[i + 1], A.T);
+            const int blocks = hi > lo ? (int)((hi - lo + A.rows - 1) / A.rows) : 0;
+            for (int b = threadIdx.x & 31; b < blocks; b += 32) {
+                const int work = !A.causal ? blocks : A.by_key ? blocks - b : b + 1;
+                const int bucket = PLAN_BUCKETS - 1 - min(work - 1, PLAN_BUCKETS - 1);
+                if (pass == 0) atomicAdd(&count[bucket], 1);
+                else {
+                    const int at = atomicAdd(&from[bucket], 1);
+                    if (at < A.most) A.items[at] = make_int2(i, b);
+                }
+            }
+        }
+        __syncthreads();
+        if (pass == 0 && threadIdx.x < 32) {
+            int sum = 0;
+            for (int base = 0; base < PLAN_BUCKETS; base += 32) {
+                int c = count[base + threadIdx.x], x = c;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, x, o);
+                    if ((int)threadIdx.x >= o) x += y;
+                }
+                from[base + threadIdx.x] = sum + x - c;
+                sum += __shfl_sync(0xffffffffu, x, 31);
+            }
+            if (threadIdx.x == 0) { A.head->count = min(sum, A.most); A.head->status = 0; A.head->ticket = 0; }
+        }
+        __syncthreads();
+    }
+}
+// By CTAs of 1024 threads, this one the b-th of n: clears the rows that no sample holds.
+static __device__ __noinline__ void rp_attend_clear(const AttendClears &A, const i64 *start, int N, i64 T, int b, int n)
+{
+    i64 head = start[0], tail = start[N];
+    head = min(max(head, (i64)0), T); tail = min(max(tail, head), T);
+    const i64 gone = head + T - tail;
+    for (int o = 0; o < A.n; ++o) {
+        const AttendClear &C = A.x[o];
+        const i64 width = (i64)C.heads * C.d;
+        for (i64 x = (i64)b * 1024 + threadIdx.x; x < gone * width; x += (i64)n * 1024) {
+            i64 t = x / width;
+            const i64 h = x % width / C.d, i = x % C.d;
+            t = t < head ? t : tail + t - head;
+            const i64 at = t * C.token + h * C.head + i;
+            if (C.bytes == 2) ((unsigned short *)C.x)[at] = 0; else ((float *)C.x)[at] = 0.0f;
+        }
+    }
+}
 int rp_attend_check(const rp_attend_config *a, i64 T, int N);
 int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev);
 

@@ -11,7 +11,7 @@
 
 struct GradArgs {
     const int2 *items;
-    const AttendHead *head;
+    AttendHead *head;
     const i64 *start;
     i64 T;
     int Hq, Hk, share, d, causal;
@@ -24,26 +24,38 @@ struct GradArgs {
     i64 r_token[2], r_head[2];
 };
 
-// lse / ln 2 and delta of every token and query head: 16 lanes a head, 16 bytes of do and o a lane.
+// Before the two kernels: CTA 0 lists the blocks of keys, CTA 1 those of queries, the others clear the rows that no sample holds and work out lse / ln 2 and delta of
+// every token and query head: 16 lanes a head, 16 bytes of do and o a lane.
+struct StatsArgs {
+    const void *o, *g;
+    const float *lse;
+    i64 o_token, o_head, g_token, g_head, l_token, l_head;
+    int H, d;
+    float2 *stats;
+};
 template <typename X>
-__global__ void __launch_bounds__(256) k_attend_stats(i64 T, int H, int d, const X *o, i64 o_token, i64 o_head, const X *g, i64 g_token, i64 g_head, const float *lse, i64 l_token,
-                                                      i64 l_head, float2 *stats)
+__global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, AttendPlan queries, AttendClears C, StatsArgs A)
 {
-    const int lane = threadIdx.x & 15;
-    for (i64 x = ((i64)blockIdx.x * 256 + threadIdx.x) >> 4; x - (threadIdx.x >> 4 & 1) < T * H; x += (i64)gridDim.x * 16) {
-        const i64 t = x / H;
-        const int h = (int)(x % H);
+    if (blockIdx.x == 0) { rp_attend_plan(keys); return; }
+    if (blockIdx.x == 1) { rp_attend_plan(queries); return; }
+    const int b = blockIdx.x - 2, n = gridDim.x - 2, lane = threadIdx.x & 15;
+    rp_attend_clear(C, keys.start, keys.N, keys.T, b, n);
+    const i64 T = keys.T, all = T * A.H;
+    // (two rows a step: a warp's halves go round as often)
+    for (i64 x = (((i64)b * 1024 + threadIdx.x) >> 5) * 2; x < all; x += (i64)n * 64) {
+        const i64 y = x + (threadIdx.x >> 4 & 1), t = y / A.H;
+        const int h = (int)(y % A.H);
         float sum = 0.0f;
-        if (x < T * H && lane * 8 < d) {
-            float a[8], b[8];
-            rp_open8(rp_load8(o + t * o_token + h * o_head + lane * 8), a);
-            rp_open8(rp_load8(g + t * g_token + h * g_head + lane * 8), b);
+        if (y < all && lane * 8 < A.d) {
+            float p[8], q[8];
+            rp_open8(rp_load8((const X *)A.o + t * A.o_token + h * A.o_head + lane * 8), p);
+            rp_open8(rp_load8((const X *)A.g + t * A.g_token + h * A.g_head + lane * 8), q);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(a[i], b[i], sum);
+            for (int i = 0; i < 8; ++i) sum = fmaf(p[i], q[i], sum);
         }
 #pragma unroll
-        for (int o2 = 1; o2 < 16; o2 <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o2);
-        if (x < T * H && lane == 0) stats[(i64)h * T + t] = make_float2(lse[t * l_token + h * l_head] * RP_LOG2E, sum);
+        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (y < all && lane == 0) A.stats[(i64)h * T + t] = make_float2(A.lse[t * A.l_token + h * A.l_head] * RP_LOG2E, sum);
     }
 }
 
@@ -104,6 +116,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    rp_let_next_launch_start();              // the queries' kernel takes the SMs that run out of work here
     if (warp == ATTEND_COPY_WARP) tmem_alloc(rp_smem(&sm.tmem), 512);
     tmem_before();
     __syncthreads();
@@ -246,11 +259,8 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
                     const ulonglong2 l = *(const ulonglong2 *)&st[0][c];         // (of the other sign)
-                    float a, e;
-                    rp_parts(rp_fma(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sl2, f2{ l.x }), a, e);
-                    p[c] = rp_exp2(a); p[c + 1] = rp_exp2(e);
-                    rp_parts(rp_fma(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), sl2, f2{ l.y }), a, e);
-                    p[c + 2] = rp_exp2(a); p[c + 3] = rp_exp2(e);
+                    rp_parts(rp_exp2(rp_fma(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sl2, f2{ l.x })), p[c], p[c + 1]);
+                    rp_parts(rp_exp2(rp_fma(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), sl2, f2{ l.y })), p[c + 2], p[c + 3]);
                 }
                 if (q0 + 64 > t.len || (A.causal && q0 < t.row0 + 128)) {
                     const int lo = A.causal ? r - q0 : 0, hi = t.len - q0;
@@ -308,8 +318,9 @@ template <int D> struct QuerySmem {
     static constexpr int TILE = 128 * D * 2, STAGES = 3;
     alignas(1024) unsigned char k[STAGES][TILE];
     alignas(1024) unsigned char v[STAGES][TILE];
-    u64 q_full, kv_full[STAGES], kv_empty[STAGES], s_full, s_empty, dp_full, ds_full, acc_full, done;
+    u64 q_full, kv_full[STAGES], kv_empty[STAGES], s_full, s_empty, dp_full, ds_full, acc_full, item_full[2], item_empty[2], done;
     u32 tmem;
+    volatile int item[2];
     volatile int gave_up;
 };
 
@@ -326,6 +337,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.kv_full[s]), 1); bar_init(rp_smem(&sm.kv_empty[s]), 1); }
         bar_init(rp_smem(&sm.q_full), 8); bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.s_empty), 8); bar_init(rp_smem(&sm.dp_full), 1);
         bar_init(rp_smem(&sm.ds_full), 8); bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.done), 1);
+        for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.item_full[i]), 1); bar_init(rp_smem(&sm.item_empty[i]), 9); }
         sm.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -344,7 +356,12 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             u32 fill = 0;
             bool ok = true;
             for (int n = 0; ok; ++n) {
-                const int at = rp_attend_item(n, total);
+                // the next of the list for whoever is free: CTAs start as the keys' kernel leaves them an SM
+                if (n > 1 && !(ok = bar_wait(rp_smem(&sm.item_empty[n & 1]), ((n >> 1) - 1) & 1, gave_up))) break;
+                int at = atomicAdd(&A.head->ticket, 1);
+                if (at >= total) at = -1;
+                sm.item[n & 1] = at;
+                bar_arrive(rp_smem(&sm.item_full[n & 1]));
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
                 const int hk = at % A.Hq / A.share, nk = rp_attend_tiles(t, 0, A.causal);
@@ -368,8 +385,10 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
             for (int n = 0;; ++n) {
-                const int at = rp_attend_item(n, total);
-                if (at < 0) break;
+                bar_hold(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, gave_up);
+                const int at = rp_uniform(sm.item[n & 1]);
+                if (at < 0 || rp_uniform(*gave_up)) break;
+                bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
                 const int len = rp_uniform(t.len), nk = rp_uniform(rp_attend_tiles(t, 0, A.causal));
                 // 128 queries (or gradients) against a tile's keys (or values)
@@ -422,9 +441,12 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const f2 sl2 = rp_f2(A.scale * RP_LOG2E, A.scale * RP_LOG2E);
         u32 f = 0;                                      // tiles so far
         u32 w[64];                                      // a row of q (first group) or of do (second): two elements a word
+        int at = 0;                                     // the item
         auto fetch = [&](int n) {
-            const int at = rp_attend_item(n, total);
+            at = -1;
+            if (bar_wait_warp(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, gave_up)) at = sm.item[n & 1];
             if (at < 0) return;
+            bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
             const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
             const int r = t.row0 + row;
             const X *p = (b ? (const X *)A.rows[1] + (t.base + r) * A.r_token[1] + at % A.Hq * A.r_head[1] : (const X *)A.rows[0] + (t.base + r) * A.r_token[0] + at % A.Hq * A.r_head[0]);
@@ -436,9 +458,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             }
         };
         fetch(0);
-        for (int n = 0;; ++n) {
-            const int at = rp_attend_item(n, total);
-            if (at < 0) break;
+        for (int n = 0; at >= 0; ++n) {
             const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
             const int h = at % A.Hq, nk = rp_attend_tiles(t, 0, A.causal), r = t.row0 + row;
 #pragma unroll
@@ -460,11 +480,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 tmem_before();
                 bar_arrive_warp(rp_smem(&sm.s_empty), lane);
 #pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    float x, y;
-                    rp_parts(rp_fma(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sl2, lse2), x, y);
-                    p[c] = rp_f2(rp_exp2(x), rp_exp2(y));
-                }
+                for (int c = 0; c < 32; ++c) p[c] = rp_exp2(rp_fma(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sl2, lse2));
                 const int k0 = j * 128 + b * 64, lim = (A.causal ? min(t.len, r + 1) : t.len) - k0;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, gave_up))) break;
                 tmem_after();
@@ -505,6 +521,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     __syncwarp();
     __syncthreads();
     if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
+    rp_wait_for_launch_before();                     // this launch is not over before the keys' is
     if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);
 }
 
@@ -530,7 +547,17 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
     k_attend_keys<X, D><<<(int)std::min((i64)sms, most * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
     RP_TRY(rp_op_launched());
-    k_attend_queries<X, D><<<(int)std::min((i64)sms, most * keys.Hq), ATTEND_THREADS, sq, stream>>>(M.k, M.v, queries);
+    // (8192 tokens in three samples, 16 heads on 4: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 249 us; the queries' 166)
+    cudaLaunchConfig_t how = {};
+    how.gridDim = dim3((unsigned)std::min((i64)sms, most * keys.Hq));
+    how.blockDim = dim3(ATTEND_THREADS);
+    how.dynamicSmemBytes = sq;
+    how.stream = stream;
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    how.attrs = &early; how.numAttrs = 1;
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_queries<X, D>, M.k, M.v, (const GradArgs)queries));
     return rp_op_launched();
 }
 
@@ -559,20 +586,18 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     RP_TRY(rp_tensor_map(&M.k, a->type, k->x, T, Hk, d, k->token, k->head, 128));
     RP_TRY(rp_tensor_map(&M.v, a->type, v->x, T, Hk, d, v->token, v->head, 128));
     RP_TRY(rp_tensor_map(&M.g, a->type, out_grad->x, T, Hq, d, out_grad->token, out_grad->head, 128));
-    AttendPlan P = {};
-    P.start = (const i64 *)start; P.T = T; P.N = n_samples; P.rows = 128; P.causal = a->causal; P.most = (int)(T / 128 + n_samples);
+    AttendPlan P[2] = {};
+    AttendClears C = {};
+    C.x[C.n++] = { k_grad->x, k_grad->token, k_grad->head, Hk, d, 2 };
+    C.x[C.n++] = { v_grad->x, v_grad->token, v_grad->head, Hk, d, 2 };
+    C.x[C.n++] = { q_grad->x, q_grad->token, q_grad->head, Hq, d, 2 };
     GradArgs G[2];
     for (int w = 0; w < 2; ++w) {
-        P.by_key = w == 0; P.head = head[w]; P.items = (int2 *)(head[w] + 1); P.n_clear = 0;
-        if (w == 0) {
-            P.clear[P.n_clear++] = { k_grad->x, k_grad->token, k_grad->head, Hk, d, 2 };
-            P.clear[P.n_clear++] = { v_grad->x, v_grad->token, v_grad->head, Hk, d, 2 };
-        } else
-            P.clear[P.n_clear++] = { q_grad->x, q_grad->token, q_grad->head, Hq, d, 2 };
-        RP_TRY(rp_launch_attend_plan(P, stream));
+        P[w].start = (const i64 *)start; P[w].T = T; P[w].N = n_samples; P[w].rows = 128; P[w].causal = a->causal; P[w].most = (int)(T / 128 + n_samples);
+        P[w].by_key = w == 0; P[w].head = head[w]; P[w].items = (int2 *)(head[w] + 1);
         GradArgs &A = G[w];
         A = GradArgs();
-        A.items = P.items; A.head = head[w]; A.start = (const i64 *)start; A.T = T; A.Hq = Hq; A.Hk = Hk; A.share = Hq / Hk; A.d = d; A.causal = a->causal;
+        A.items = P[w].items; A.head = head[w]; A.start = (const i64 *)start; A.T = T; A.Hq = Hq; A.Hk = Hk; A.share = Hq / Hk; A.d = d; A.causal = a->causal;
         A.scale = a->scale; A.stats = stats; A.status = &head[0]->status;
     }
     G[0].x[0] = v_grad->x; G[0].token[0] = v_grad->token; G[0].hd[0] = v_grad->head;
@@ -581,14 +606,11 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     G[1].rows[1] = out_grad->x; G[1].r_token[1] = out_grad->token; G[1].r_head[1] = out_grad->head;
     G[1].x[0] = q_grad->x; G[1].token[0] = q_grad->token; G[1].hd[0] = q_grad->head;
     const int sms = rp_op_sms(dev.device);
-    const int ctas = (int)std::min((T * Hq + 15) / 16, (i64)sms * 8);
-    if (a->type == RP_F16)
-        k_attend_stats<__half><<<ctas, 256, 0, stream>>>(T, Hq, d, (const __half *)out->x, out->token, out->head, (const __half *)out_grad->x, out_grad->token, out_grad->head,
-                                                         (const float *)lse->x, lse->token, lse->head, stats);
-    else
-        k_attend_stats<bf16><<<ctas, 256, 0, stream>>>(T, Hq, d, (const bf16 *)out->x, out->token, out->head, (const bf16 *)out_grad->x, out_grad->token, out_grad->head,
-                                                       (const float *)lse->x, lse->token, lse->head, stats);
+    const StatsArgs S = { out->x, out_grad->x, (const float *)lse->x, out->token, out->head, out_grad->token, out_grad->head, lse->token, lse->head, Hq, d, stats };
+    const int ctas = 2 + (int)std::min((T * Hq + 63) / 64, (i64)sms * 2 - 2);
+    if (a->type == RP_F16) k_attend_prepare<__half><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
+    else k_attend_prepare<bf16><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
     RP_TRY(rp_op_launched());
-    if (a->type == RP_F16) return d <= 64 ? launch<__half, 64>(M, G[0], G[1], P.most, sms, stream) : launch<__half, 128>(M, G[0], G[1], P.most, sms, stream);
-    return d <= 64 ? launch<bf16, 64>(M, G[0], G[1], P.most, sms, stream) : launch<bf16, 128>(M, G[0], G[1], P.most, sms, stream);
+    if (a->type == RP_F16) return d <= 64 ? launch<__half, 64>(M, G[0], G[1], P[0].most, sms, stream) : launch<__half, 128>(M, G[0], G[1], P[0].most, sms, stream);
+    return d <= 64 ? launch<bf16, 64>(M, G[0], G[1], P[0].most, sms, stream) : launch<bf16, 128>(M, G[0], G[1], P[0].most, sms, stream);
 }

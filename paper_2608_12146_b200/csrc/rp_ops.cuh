@@ -170,6 +170,12 @@ __device__ __forceinline__ float rp_exp2(float x)        // 2^x by the special f
     return y;
 }
 #define RP_LOG2E 1.4426950408889634f
+__device__ __forceinline__ f2 rp_exp2(f2 x)
+{
+    float a, b;
+    rp_parts(x, a, b);
+    return rp_f2(rp_exp2(a), rp_exp2(b));
+}
 
 // Launch of `f` for one of the three element types, in a scope where X names it.
 #define RP_FOR_TYPE(type, ...)                                     \
