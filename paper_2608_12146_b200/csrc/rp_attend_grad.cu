@@ -40,22 +40,36 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
     if (blockIdx.x == 1) { rp_attend_plan(queries); return; }
     const int b = blockIdx.x - 2, n = gridDim.x - 2, lane = threadIdx.x & 15;
     rp_attend_clear(C, keys.start, keys.N, keys.T, b, n);
-    const i64 T = keys.T, all = T * A.H;
-    // (two rows a step: a warp's halves go round as often)
-    for (i64 x = (((i64)b * 1024 + threadIdx.x) >> 5) * 2; x < all; x += (i64)n * 64) {
-        const i64 y = x + (threadIdx.x >> 4 & 1), t = y / A.H;
-        const int h = (int)(y % A.H);
-        float sum = 0.0f;
-        if (y < all && lane * 8 < A.d) {
-            float p[8], q[8];
-            rp_open8(rp_load8((const X *)A.o + t * A.o_token + h * A.o_head + lane * 8), p);
-            rp_open8(rp_load8((const X *)A.g + t * A.g_token + h * A.g_head + lane * 8), q);
+    // 64 rows of a CTA: heads of a token, tokens; four steps on their way at a time (all lanes go round as often)
+    constexpr int AHEAD = 4;
+    const i64 T = keys.T;
+    const int heads = min(A.H, 64), tokens = 64 / heads, row = threadIdx.x >> 4, dt = row / heads;
+    for (int h0 = 0; h0 < A.H; h0 += heads) {
+        const int h = h0 + row % heads;
+        const bool mine = dt < tokens && h < A.H;
+        const X *o = (const X *)A.o + h * A.o_head + lane * 8, *g = (const X *)A.g + h * A.g_head + lane * 8;
+        for (i64 t0 = (i64)b * tokens; t0 < T; t0 += (i64)AHEAD * n * tokens) {
+            Pack8<X> p[AHEAD], q[AHEAD];
+            float l[AHEAD];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(p[i], q[i], sum);
+            for (int u = 0; u < AHEAD; ++u) {
+                const i64 t = t0 + (i64)u * n * tokens + dt;
+                p[u] = Pack8<X>(); q[u] = Pack8<X>(); l[u] = 0.0f;
+                if (mine && t < T && lane * 8 < A.d) { p[u] = rp_load8(o + t * A.o_token); q[u] = rp_load8(g + t * A.g_token); }
+                if (mine && t < T && lane == 0) l[u] = A.lse[t * A.l_token + h * A.l_head];
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const i64 t = t0 + (i64)u * n * tokens + dt;
+                float a[8], c[8], sum = 0.0f;
+                rp_open8(p[u], a); rp_open8(q[u], c);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = fmaf(a[i], c[i], sum);
+#pragma unroll
+                for (int i = 1; i < 16; i <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
+                if (mine && t < T && lane == 0) A.stats[h * T + t] = make_float2(l[u] * RP_LOG2E, sum);
+            }
         }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (y < all && lane == 0) A.stats[(i64)h * T + t] = make_float2(A.lse[t * A.l_token + h * A.l_head] * RP_LOG2E, sum);
     }
 }
 
