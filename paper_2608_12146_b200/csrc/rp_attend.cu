@@ -15,6 +15,7 @@
 
 __global__ void __launch_bounds__(1024) k_attend_plan(AttendPlan P, AttendClears C)
 {
+    rp_let_next_launch_start();
     if (blockIdx.x == 0) rp_attend_plan(P);
     else rp_attend_clear(C, P.start, P.N, P.T, blockIdx.x - 1, gridDim.x - 1);
 }
@@ -70,6 +71,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     __syncthreads();
     tmem_after();
     const u32 tm = rp_uniform(sm.tmem);
+    rp_wait_for_launch_before();             // the list of blocks: nothing of it before this line
     const int total = rp_uniform(A.head->count * A.Hq);
     volatile int *gave_up = &sm.gave_up;
 
@@ -321,7 +323,16 @@ static int launch(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap 
 {
     const size_t smem = sizeof(FwdSmem<D>) + 1024;
     RP_CUDA(cudaFuncSetAttribute(k_attend<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    k_attend<X, D><<<ctas, ATTEND_THREADS, smem, stream>>>(q, k, v, A);
+    cudaLaunchConfig_t how = {};                         // (barriers, tensor memory and maps are got ready beside the planning)
+    how.gridDim = dim3((unsigned)ctas);
+    how.blockDim = dim3(ATTEND_THREADS);
+    how.dynamicSmemBytes = smem;
+    how.stream = stream;
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    how.attrs = &early; how.numAttrs = 1;
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend<X, D>, q, k, v, A));
     return rp_op_launched();
 }
 

@@ -20,7 +20,7 @@ struct AttendClears { AttendClear x[3]; int n; };       // outputs whose rows of
 static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
 {
     __shared__ int count[PLAN_BUCKETS];
-    __shared__ int from[PLAN_BUCKETS];
+    __shared__ int from[PLAN_BUCKETS], sums[32];
     for (int x = threadIdx.x; x < PLAN_BUCKETS; x += 1024) count[x] = 0;
     __syncthreads();
     for (int pass = 0; pass < 2; ++pass) {
@@ -38,21 +38,24 @@ static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
             }
         }
         __syncthreads();
-        if (pass == 0 && threadIdx.x < 32) {
-            int sum = 0;
-            for (int base = 0; base < PLAN_BUCKETS; base += 32) {
-                int c = count[base + threadIdx.x], x = c;
+        if (pass == 0) {
+            // a thread a bucket
+            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = count[threadIdx.x];
+            int x = c;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int y = __shfl_up_sync(0xffffffffu, x, o);
-                    if ((int)threadIdx.x >= o) x += y;
-                }
-                from[base + threadIdx.x] = sum + x - c;
-                sum += __shfl_sync(0xffffffffu, x, 31);
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
             }
-            if (threadIdx.x == 0) { A.head->count = min(sum, A.most); A.head->status = 0; A.head->ticket = 0; }
+            if (lane == 31) sums[warp] = x;
+            __syncthreads();
+            int before = warp ? sums[lane < warp ? lane : 0] : 0;
+            if (lane >= warp) before = 0;
+            before = __reduce_add_sync(0xffffffffu, before);
+            from[threadIdx.x] = before + x - c;
+            if (threadIdx.x == 1023) { A.head->count = min(before + x, A.most); A.head->status = 0; A.head->ticket = 0; }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 // By CTAs of 1024 threads, this one the b-th of n: clears the rows that no sample holds.
