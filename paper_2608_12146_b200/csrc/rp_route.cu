@@ -9,6 +9,8 @@
 // sums over experts are shuffles.  Every such group of lanes owns a run of neighbouring tokens and carries the sums of p of the run's
 // present group of tokens in registers, its counts in shared memory; what a CTA's last runs hold meets in shared memory before it goes out.
 // Sums of p leave a CTA in fixed point (2^-36): additions of whole numbers, so their order does not matter.
+#include <limits.h>
+
 #include <algorithm>
 
 #include "rp_ops.cuh"
@@ -54,20 +56,27 @@ template <int SUB> __device__ __forceinline__ float sub_sum(float v)
     for (int o = 1; o < SUB; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+template <int SUB> __device__ __forceinline__ u32 sub_max(u32 v);
+__device__ __forceinline__ u32 order_of(float x);
 template <int SUB> __device__ __forceinline__ float sub_max(float v)      // of numbers; NaN loses against any
 {
+    if constexpr (SUB == 32) {                              // by one instruction of the whole warp, on numbers in the floats' order (fmaxf has taken NaN out, or all are)
+        const u32 m = sub_max<SUB>(v == v ? order_of(v) : 0u);
+        return m == 0 ? NAN : __uint_as_float((m >> 31) ? m ^ 0x80000000u : ~m);
+    } else {
 #pragma unroll
-    for (int o = 1; o < SUB; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+        for (int o = 1; o < SUB; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+        return v;
+    }
 }
 template <int SUB> __device__ __forceinline__ u32 sub_max(u32 v)
 {
-    if constexpr (SUB == 32) v = __reduce_max_sync(0xffffffffu, v);
+    if constexpr (SUB == 32) return __reduce_max_sync(0xffffffffu, v);
     else {
 #pragma unroll
         for (int o = 1; o < SUB; o <<= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+        return v;
     }
-    return v;
 }
 
 // A row's VPL elements of a lane, as they lie in memory: read 16 bytes at a time (then a lane's eight all exist or none does), or one by one where rows are not on such
@@ -86,9 +95,8 @@ template <typename X, int VPL> struct Row {
     }
 };
 template <typename X, int VPL>
-__device__ __forceinline__ void load_row(const RouteArgs &A, i64 t, int e0, Row<X, VPL> &r)
+__device__ __forceinline__ void load_row(const RouteArgs &A, const X *row, int e0, Row<X, VPL> &r)      // row: of the lane's first expert
 {
-    const X *row = (const X *)A.x + t * A.row + e0;
 #pragma unroll
     for (int c = 0; c < VPL; c += 8) {
         if (A.wide) {
@@ -287,7 +295,7 @@ __device__ __forceinline__ void add_sums(const RouteArgs &A, int g, int e0, cons
 }
 
 template <typename X, int VPL, int SUB>
-__global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
+__global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route(RouteArgs A)
 {
     constexpr int NSUB = ROUTE_THREADS / SUB, EP = VPL * SUB;             // groups of lanes, experts they hold
     __shared__ int cnt[NSUB][EP];
@@ -305,25 +313,36 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
     for (int x = threadIdx.x; x < NSUB * EP; x += ROUTE_THREADS) (&cnt[0][0])[x] = 0;
     __syncthreads();
 
+    // the run's tokens are counted from 0; `next`: where the next group begins
     const i64 t0 = ((i64)blockIdx.x * NSUB + sub) * A.run;
+    const int run = (int)A.run, n = (int)max(min(A.T - t0, A.run), (i64)0);
     int g = rp_sample_of(A.start, A.G, t0);
-    i64 next = g < A.G ? A.start[g + 1] : INT64_MAX;                      // where the next group begins
+    int next = g < A.G ? (int)min(A.start[g + 1] - t0, (i64)INT_MAX) : INT_MAX;
     float acc[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) acc[i] = 0.0f;
+    const X *x_at = (const X *)A.x + t0 * A.row;
+    float *gate_at = A.gates + t0 * A.k + sl;
+    char *route_at = (char *)A.routes + (t0 * A.route_row + sl) * A.route_bytes;
+    const i64 route_step = A.route_row * A.route_bytes;
     Row<X, VPL> row;
-    if (t0 < A.T) load_row<X, VPL>(A, t0, e0, row);
+    i64 e_next = -1;
+    if (n > 0) {
+        load_row<X, VPL>(A, x_at + e0, e0, row);
+        if (A.replay && sl < A.k) e_next = rp_load_route(route_at, A.route_bytes, 0);
+    }
     int k_lanes = 1;                                                      // lanes that the sum over the chosen goes over
     while (k_lanes < A.k) k_lanes <<= 1;
-    for (i64 step = 0; step < A.run; ++step) {
-        const i64 t = t0 + step;
-        const bool there = t < A.T;
+    for (int step = 0; step < run; ++step, x_at += A.row, gate_at += A.k, route_at += route_step) {
+        const bool there = step < n;
         float x[VPL], s[VPL], top = 0.0f, inv = 0.0f, xe = 0.0f;
         open_row<X, VPL>(row, x);
-        if (step + 1 < A.run && t + 1 < A.T) load_row<X, VPL>(A, t + 1, e0, row);
         // lane j of the token's has its j-th choice (there are at least k of them)
-        i64 e = -1;
-        if (A.replay && there && sl < A.k) e = rp_load_route(A.routes, A.route_bytes, t * A.route_row + sl);
+        i64 e = e_next;
+        if (step + 1 < n) {
+            load_row<X, VPL>(A, x_at + A.row + e0, e0, row);
+            if (A.replay && sl < A.k) e_next = rp_load_route(route_at + route_step, A.route_bytes, 0);
+        }
         if (want_loss || A.score == RP_SCORE_SOFTMAX || A.bias) scores<VPL, SUB, true>(A, x, s, top, inv);
         if (!A.replay) {
             if (sizeof(X) == 2 && !A.bias) choose_by_keys<VPL, SUB>(A, x, e0, sl, e, xe);
@@ -336,7 +355,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
             }
         }
         const bool valid = there && sl < A.k && e >= 0 && e < A.E;
-        if (valid && (A.replay || sizeof(X) == 4 || A.bias)) xe = rp_float(((const X *)A.x)[t * A.row + e]);
+        if (valid && (A.replay || sizeof(X) == 4 || A.bias)) xe = rp_float(x_at[e]);
         const float v = valid ? score_of(A, xe, top, inv) : 0.0f;
         float gate = v * A.scale;
         if (A.normalise) {
@@ -344,7 +363,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
             for (int o = 1; o < k_lanes; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
             gate = total < 1.2e-38f ? 0.0f : gate * reciprocal(total);
         }
-        if (there && t >= next) {
+        if (there && step >= next) {
             // another group: what the run has of the one before goes out
             if (g >= 0 && g < A.G) {
                 if (want_loss) add_sums<VPL>(A, g, e0, acc);
@@ -356,8 +375,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
 #pragma unroll
                 for (int i = 0; i < VPL; ++i) acc[i] = 0.0f;
             }
-            g = rp_sample_of(A.start, A.G, t);
-            next = g < A.G ? A.start[g + 1] : INT64_MAX;
+            g = rp_sample_of(A.start, A.G, t0 + step);
+            next = g < A.G ? (int)min(A.start[g + 1] - t0, (i64)INT_MAX) : INT_MAX;
         }
         __syncwarp();
         const bool held = there && g >= 0 && g < A.G;
@@ -367,8 +386,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route(RouteArgs A)
         }
         if (valid && held && want_counts) atomicAdd(&cnt[sub][(int)e], 1);
         if (there && sl < A.k) {
-            A.gates[t * A.k + sl] = held ? gate : 0.0f;
-            if (!A.replay) rp_store_route(A.routes, A.route_bytes, t * A.route_row + sl, held ? (int)e : -1);
+            *gate_at = held ? gate : 0.0f;
+            if (!A.replay) rp_store_route(route_at, A.route_bytes, 0, held ? (int)e : -1);
         }
         __syncwarp();
     }
@@ -429,7 +448,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_loss(RouteArgs A)
 // The token's row is put together in shared memory, where the lanes that have its chosen experts each add their part; an expert that a token has twice gets its
 // parts one after the other.
 template <typename X, int VPL, int SUB>
-__global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
+__global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route_grad(RouteArgs A)
 {
     constexpr int NSUB = ROUTE_THREADS / SUB, EP = VPL * SUB;
     __shared__ __align__(16) float rows[NSUB][EP];
@@ -437,30 +456,36 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
     const bool soft = A.score == RP_SCORE_SOFTMAX, gates = A.gates_grad != nullptr;
     const float loss_grad = A.loss_grad ? *A.loss_grad : 0.0f;
     const i64 t0 = ((i64)blockIdx.x * NSUB + sub) * A.run;
-    int g = -2, k_lanes = 1;
+    const int run = (int)A.run, n = (int)max(min(A.T - t0, A.run), (i64)0);
+    int g = -2, k_lanes = 1, next = INT_MIN;               // (tokens of the run are counted from 0)
     while (k_lanes < A.k) k_lanes <<= 1;
-    i64 next = INT64_MIN;
     float b[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) b[i] = 0.0f;
+    const X *x_at = (const X *)A.x + t0 * A.row;
+    X *out = (X *)A.dx + t0 * A.dx_row;
+    const char *route_at = (const char *)A.routes + (t0 * A.route_row + sl) * A.route_bytes;
+    const float *gate_at = A.gates_grad + t0 * A.k + sl;
+    const i64 route_step = A.route_row * A.route_bytes;
     Row<X, VPL> row;
     // lane j of the token's has its j-th choice
     i64 e_next = -1;
     float a_next = 0.0f;
-    auto fetch = [&](i64 t) {
-        load_row<X, VPL>(A, t, e0, row);
-        if (gates && sl < A.k) { e_next = rp_load_route(A.routes, A.route_bytes, t * A.route_row + sl); a_next = A.gates_grad[t * A.k + sl]; }
+    auto fetch = [&](const X *x) {
+        load_row<X, VPL>(A, x + e0, e0, row);
+        if (gates && sl < A.k) { e_next = rp_load_route(route_at, A.route_bytes, 0); a_next = *gate_at; }
+        route_at += route_step;
+        gate_at += A.k;
     };
-    if (t0 < A.T) fetch(t0);
-    for (i64 step = 0; step < A.run; ++step) {
-        const i64 t = t0 + step;
-        const bool there = t < A.T;
-        if (there && t >= next) {
-            g = rp_sample_of(A.start, A.G, t);
-            next = g < A.G ? A.start[g + 1] : INT64_MAX;
+    if (n > 0) fetch(x_at);
+    for (int step = 0; step < run; ++step, x_at += A.row, out += A.dx_row) {
+        const bool there = step < n;
+        if (there && step >= next) {
+            g = rp_sample_of(A.start, A.G, t0 + step);
+            next = g < A.G ? (int)min(A.start[g + 1] - t0, (i64)INT_MAX) : INT_MAX;
             if (A.loss_grad && g >= 0 && g < A.G) {
                 const i64 lo = max(A.start[g], (i64)0), hi = min(A.start[g + 1], A.T);
-                const float n = (float)(hi - lo), f = loss_grad * (A.coef / A.G) * A.E / A.k / n / n;
+                const float m = (float)(hi - lo), f = loss_grad * (A.coef / A.G) * A.E / A.k / m / m;
 #pragma unroll
                 for (int i = 0; i < VPL; ++i) b[i] = e0 + i < A.E ? f * (float)A.counts_in[(i64)g * A.E + e0 + i] : 0.0f;
             }
@@ -470,16 +495,18 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
         open_row<X, VPL>(row, x);
         const bool valid = gates && held && sl < A.k && e_next >= 0 && e_next < A.E;
         const int e = valid ? (int)e_next : -1;
-        const float a = A.scale * a_next;
-        if (step + 1 < A.run && t + 1 < A.T) fetch(t + 1);
+        const float a = A.scale * a_next, xe = valid ? rp_float(x_at[e]) : 0.0f;
+        if (step + 1 < n) fetch(x_at + A.row);
         scores<VPL, SUB, false>(A, x, s, top, inv);
         float pb = 0.0f;
+        if (A.loss_grad) {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) pb = fmaf(s[i], b[i], pb);
-        pb = sub_sum<SUB>(pb) * inv;
+            for (int i = 0; i < VPL; ++i) pb = fmaf(s[i], b[i], pb);
+            pb = sub_sum<SUB>(pb) * inv;
+        }
         float add = 0.0f;
         if (gates) {
-            const float v = valid ? score_of(A, rp_float(((const X *)A.x)[t * A.row + e]), top, inv) : 0.0f;
+            const float v = valid ? score_of(A, xe, top, inv) : 0.0f;
             float z = v, za = valid ? v * a : 0.0f;
             for (int o = 1; o < k_lanes; o <<= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); za += __shfl_xor_sync(0xffffffffu, za, o); }
             // (lanes behind the choices have their own sums: what all lanes need is the first's)
@@ -507,7 +534,6 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_grad(RouteArgs A)
             __syncwarp();
         }
         if (there) {
-            X *out = (X *)A.dx + t * A.dx_row;
 #pragma unroll
             for (int c = 0; c < VPL; c += 8) {
                 float f[8];
