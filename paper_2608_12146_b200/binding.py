@@ -537,10 +537,11 @@ def _rotary(head_dim, rotary_dim, layout, kind, weight_kind, eps, mscale):
 
 def _head_strides(x, like, what: str):
     """Strides of tokens and heads of a tensor of the shape and type of `like`."""
-    if x.shape != like.shape or x.dtype != like.dtype or not x.is_cuda or (x.shape[2] != 1 and x.stride(2) != 1):
+    step = x.stride()
+    if (x is not like and (x.shape != like.shape or x.dtype != like.dtype)) or not x.is_cuda or (step[2] != 1 and x.shape[2] != 1):
         raise ValueError(f"{what}: CUDA tensor {tuple(like.shape)} of {like.dtype} with its last dimension side by side wanted, "
                          f"got {tuple(x.shape)} of {x.dtype}")
-    return x.stride(0), x.stride(1)
+    return step[0], step[1]
 
 
 def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale, outs, grads, stream):
@@ -555,20 +556,23 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
     back = grads[0] is not None
     with _Queue(torch, q, stream) as queue:
         sides, results, dws = [None, None], [None, None], [None, None]
-        for i, (x, w, out, g) in enumerate(zip((q, k), weights, outs, grads)):
-            if x is None:
-                continue
+        for i in (0, 1) if k is not None else (0,):
+            x, w, out, g = (q, k)[i], weights[i], outs[i], grads[i]
+            xt, xh = _head_strides(x, x, "input")
             if out is None:
                 out = x.new_empty(x.shape)
+                yt, yh = x.shape[1] * d, d
+            else:
+                yt, yh = _head_strides(out, x, "output")
             results[i] = out
-            side = rp_heads(x.shape[1], x.data_ptr(), *_head_strides(x, x, "input"), out.data_ptr(), *_head_strides(out, x, "output"),
-                            _dense(w, w_type, (d,), "weight"))
-            if back:
-                side.y_grad = g.data_ptr()
-                side.g_token, side.g_head = _head_strides(g, x, "gradient")
+            if not back:
+                side = rp_heads(x.shape[1], x.data_ptr(), xt, xh, out.data_ptr(), yt, yh, _dense(w, w_type, (d,), "weight"))
+            else:
+                gt, gh = _head_strides(g, x, "gradient")
                 if w is not None:
                     dws[i] = x.new_empty(d, dtype=torch.float32)
-                    side.weight_grad = dws[i].data_ptr()
+                side = rp_heads(x.shape[1], x.data_ptr(), xt, xh, out.data_ptr(), yt, yh, _dense(w, w_type, (d,), "weight"), g.data_ptr(), gt, gh,
+                                None if w is None else dws[i].data_ptr())
             sides[i] = C.byref(side)
         freq = None if inv_freq is None else _dense(inv_freq, torch.float64, inv_freq.shape, "inv_freq")
         r, ref = _rotary(d, 0 if inv_freq is None else 2 * inv_freq.numel(), layout, kind, _TYPES[w_type], eps, mscale)
