@@ -146,16 +146,16 @@ __global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
         }
         if (held) {
             int *out = A.demand + ((i64)i * A.L + l0) * A.E;
-            const int layers = min(A.L - l0, A.lanes * LAYERS);
+            const int layers = min(A.L - l0, A.lanes * LAYERS), experts = min(A.E, A.rows);        // (a byte has no choice above 255)
             __syncthreads();
             // Eight lanes add up an expert's 32 counters; those of lanes that share a token are layers of their own: at the end lane q of the eight has the sum of the
             // counters q mod 4 of four lanes, and its neighbour four lanes on that of the others.
 #pragma unroll
             for (int sub = 0; sub < LAYERS; ++sub)
-                for (int first = warp * 4; first < A.E; first += COUNT_THREADS / 8) {        // (the whole warp goes round as often)
+                for (int first = warp * 4; first < experts; first += COUNT_THREADS / 8) {    // (the whole warp goes round as often)
                     const int e = first + (lane >> 3), q = lane & 3, l = q * LAYERS + sub;
                     uint4 *p = (uint4 *)(hist + (sub * A.rows + e) * 32) + (lane & 7), c = make_uint4(0, 0, 0, 0);
-                    if (e < A.E) { c = *p; *p = make_uint4(0, 0, 0, 0); }
+                    if (e < experts) { c = *p; *p = make_uint4(0, 0, 0, 0); }
                     const bool odd = lane & 1, high = lane & 2;
                     // the pair's even lane goes on with x and z, the odd one with y and w; of two pairs the lower with the first of those
                     const u32 k0 = (odd ? c.y : c.x) + __shfl_xor_sync(0xffffffffu, odd ? c.x : c.y, 1);
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
                     u32 v = (high ? k1 : k0) + __shfl_xor_sync(0xffffffffu, high ? k0 : k1, 2);
                     v += __shfl_xor_sync(0xffffffffu, v, 4);
                     if (A.lanes == 1) { v += __shfl_xor_sync(0xffffffffu, v, 1); v += __shfl_xor_sync(0xffffffffu, v, 2); }
-                    if ((lane & 7) < A.lanes && v && e < A.E && l < layers) atomicAdd(out + l * A.E + e, (int)v);
+                    if ((lane & 7) < A.lanes && v && e < experts && l < layers) atomicAdd(out + l * A.E + e, (int)v);
                 }
             __syncthreads();
         }

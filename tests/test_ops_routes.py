@@ -96,6 +96,17 @@ def test_counts(case, kind, order):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("E", [257, 512, 1000, 1024])
+@pytest.mark.parametrize("L,k", [(1, 8), (3, 2), (8, 8)])
+def test_bytes_where_there_are_more_experts_than_a_byte_names(E, L, k):
+    import torch
+    host = np.random.default_rng(E + L).integers(0, 256, (2000, L, k)).astype(np.uint8)
+    start = [0, 3, 1200, 1990]
+    got = rp.rp_count_routes(torch.from_numpy(host).cuda(), torch.tensor(start, device="cuda"), E)
+    assert (got.cpu().numpy() == count(host, start, E)).all()
+
+
+@pytest.mark.gpu
 def test_output_is_written_whole_and_nothing_behind_it():
     import torch
     out = torch.full((4, 2, 8), -7, dtype=torch.int32, device="cuda")
