@@ -63,12 +63,12 @@ static inline int rp_type_bytes(int type) { return type == RP_F32 ? 4 : 2; }
 // The last i with start[i] <= t: -1 before the first sample, n behind the last one.  Reads start[0..n] and nothing else, whatever it holds.
 __device__ __forceinline__ int rp_sample_of(const i64 *__restrict__ start, int n, i64 t)
 {
-    int lo = 0, hi = n + 1;
+    u32 lo = 0, hi = (u32)n + 1;                         // (n may be 2^31 - 1)
     while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
+        const u32 mid = (lo + hi) >> 1;
         if (__ldg(start + mid) <= t) lo = mid + 1; else hi = mid;
     }
-    return lo - 1;
+    return (int)(lo - 1);
 }
 
 // Recorded choices of an expert: 1 byte without a sign, 2, 4 or 8 with one.

@@ -53,13 +53,13 @@ __device__ __forceinline__ i64 tile_start(const CountArgs &A, int b, int n)
     if (b <= 0) return 0;
     if (b >= n) return A.T;
     const i64 cost = A.T + (i64)COUNT_END * A.N, want = cost / n * b + cost % n * b / n;
-    int lo = 0, hi = A.N + 1;                            // first i with start[i] + COUNT_END * i above it
+    u32 lo = 0, hi = (u32)A.N + 1;                       // first i with start[i] + COUNT_END * i above it
     while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
+        const u32 mid = (lo + hi) >> 1;
         if (__ldg(A.start + mid) + (i64)COUNT_END * mid <= want) lo = mid + 1; else hi = mid;
     }
-    i64 t = want - (i64)COUNT_END * max(lo - 1, 0);
-    if (lo <= A.N) t = min(t, __ldg(A.start + lo));
+    i64 t = want - (i64)COUNT_END * max((i64)lo - 1, (i64)0);
+    if (lo <= (u32)A.N) t = min(t, __ldg(A.start + lo));
     return min(max(t, (i64)0), A.T);
 }
 // A CTA owns a tile of tokens and lanes * LAYERS layers, whatever samples the tokens belong to: it counts one sample after the other in shared memory and adds what
@@ -198,7 +198,7 @@ static int launch_count(CountArgs &A, int sms, cudaStream_t stream)
     const int groups = (A.L + A.lanes * layers - 1) / (A.lanes * layers);
     const i64 resident = (i64)sms * std::min((size_t)2, (size_t)(224 * 1024) / (smem + 1024));
     const i64 most = std::max((i64)1, resident / groups), cost = A.T + (i64)COUNT_END * A.N;
-    const i64 tiles = std::max(std::min(most, (cost + 511) / 512), (A.T >> 30) + 1);          // (a tile's tokens are counted in 32 bits)
+    const i64 tiles = std::max(std::min(most, (cost + 511) / 512), (cost >> 30) + 1);            // (a tile's tokens are counted in 32 bits)
     f<<<dim3((unsigned)tiles, groups), COUNT_THREADS, smem, stream>>>(A);
     return rp_op_launched();
 }
@@ -255,7 +255,7 @@ int rp_count_args(const void *routes, int bytes, i64 T, int L, int k, int E)
 {
     if (!routes || T < 0 || L < 1 || k < 1 || E < 1 || (bytes != 1 && bytes != 2 && bytes != 4 && bytes != 8)) return RP_ERR_ARG;
     if (!rp_aligned(routes, bytes)) return RP_ERR_ARG;
-    if (E > 1024 || k > 1024 || (i64)L * E >= (1ll << 31) || T > (1ll << 36)) return RP_ERR_RANGE;
+    if (E > 1024 || k > 1024 || L > 65535 || (i64)L * E >= (1ll << 31) || T > (1ll << 36)) return RP_ERR_RANGE;
     return RP_OK;
 }
 

@@ -32,7 +32,7 @@ def test_refusals():
     assert call(routes=None) == -1 and call(start=None) == -1 and call(demand=None) == -1
     assert call(size=3) == -1 and call(size=0) == -1 and call(T=-1) == -1 and call(L=0) == -1 and call(k=0) == -1 and call(N=0) == -1
     assert call(routes=p + 1, size=2) == -1 and call(start=p + 4) == -1 and call(demand=p + 2) == -1
-    assert call(E=1025) == -5 and call(k=1025) == -5
+    assert call(E=1025) == -5 and call(k=1025) == -5 and call(L=65536) == -5 and call(T=(1 << 36) + 1) == -5
     out = C.c_void_p(123)
     assert lib.rp_window_load_routes(C.byref(out), None, None, None, 1, 1, 1, 1, None) == -1 and out.value is None
 
