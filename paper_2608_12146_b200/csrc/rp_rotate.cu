@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
                             f2 sum2 = rp_f2(0.0f, 0.0f);
 #pragma unroll
                             for (int p = 0; p < 4; ++p) sum2 = rp_fma(a[p], a[p], rp_fma(b[p], b[p], sum2));
-                            const float sum = head_sum<TPH>(sum2), q = rsqrtf(fmaf(sum, A.inv_d, A.eps));
+                            const float sum = head_sum<TPH>(sum2), q = ok[u] && there ? rsqrtf(fmaf(sum, A.inv_d, A.eps)) : 0.0f;       // (eps may be 0)
                             r = rp_f2(q, q);
                         }
                         if (!GRAD) {

@@ -213,6 +213,31 @@ def test_in_place_and_rows_behind(d, r):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,heads", [(128, 3), (96, 1), (33, 2)])
+def test_norm_without_eps(d, heads):
+    """eps = 0: what a warp has no head or no token for is not a row of zeros to be divided by its norm."""
+    import torch
+    q, _, inv, _, g = inputs((40, heads, 0, d, 16, [2, 30, 36], None), "float32")
+    st, w = torch.tensor([2, 30, 36], device="cuda"), torch.rand(d, generator=g).cuda() + 0.5
+    dy = torch.randn(40, heads, d, generator=g).cuda()
+    out = rp.rp_rotate(q, None, inv.cuda(), st, q_weight=w, eps=0.0)[0]
+    grad = rp.rp_rotate_grad(dy, None, q, None, inv.cuda(), st, q_weight=w, eps=0.0)
+    pos, held = positions(40, [2, 30, 36])
+    x, w64 = q.double().cpu().requires_grad_(), w.double().cpu().requires_grad_()
+    y = reference(x, w64, pos, held, inv, eps=0.0)
+    y.backward(dy.double().cpu())
+    rstd = torch.rsqrt((x * x).mean(-1, keepdim=True)).detach()
+    hat, top = (x * rstd).detach(), 1.5 * dy.double().cpu().abs().amax(-1, keepdim=True)
+    half = torch.finfo(torch.float32).eps / 2
+    # (bounds as in test_rows)
+    assert ((out.double().cpu() - y).abs() <= (half * y.abs() + FLOAT * y.abs().amax(-1, keepdim=True)).detach()).all()
+    size = top * w64.detach().max() * rstd * (1 + hat.abs().amax(-1, keepdim=True))
+    assert ((grad[0].double().cpu() - x.grad).abs() <= half * x.grad.abs() + 2 * FLOAT * size).all()
+    total = (top * hat.abs() * held[:, None, None]).sum((0, 1))
+    assert ((grad[2].double().cpu() - w64.grad).abs() <= FLOAT * total + 1e-30).all()
+
+
+@pytest.mark.gpu
 def test_repeated_streamed_and_captured_calls_agree_bit_for_bit():
     import torch
     case = (3000, 8, 2, 128, 64, [0, 1000, 3000], None)
