@@ -273,7 +273,8 @@ int rp_diagnostics(rp_ctx *ctx, const int32_t *layout, rp_diag *out);
  *    (as far as they are in 0 .. n_tokens-1).  Samples may be empty.  A token that no sample holds gets zeros in every output
  *    (routes: -1, which one byte holds as 255) and adds to no sum, whatever its inputs hold.  Rows of outputs behind n_tokens
  *    are not touched.
- *  - Strides count elements and may be negative or 0 for inputs; the last dimension is contiguous. */
+ *  - Strides count elements and may be negative or 0 for inputs; the last dimension is contiguous.
+ *  - Outputs overlap neither inputs nor one another, unless a call says that they may. */
 typedef enum { RP_F32 = 0, RP_F16 = 1, RP_BF16 = 2 } rp_type;
 
 /* Per-expert counts of recorded routes: demand[i][l][e] = how often the tokens of sample i chose expert e in layer l.
@@ -353,7 +354,7 @@ typedef struct {                /* one tensor of heads; n_heads = 0: none       
     const void *weight;         /* [head_dim], NULL: no norm                                 */
     const void *y_grad;         /* rp_rotate_grad: gradient of the output                    */
     int64_t g_token, g_head;
-    float *weight_grad;         /* rp_rotate_grad: [head_dim] out, nullable                  */
+    float *weight_grad;         /* rp_rotate_grad: [head_dim] out, nullable; not one place for queries and keys */
 } rp_heads;
 int rp_rotate(const rp_rotary *r, int64_t n_tokens, const double *inv_freq, const int64_t *start, int32_t n_samples,
               const int64_t *first_position, const rp_heads *q, const rp_heads *k, void *cuda_stream);
@@ -367,9 +368,10 @@ int rp_rotate_grad(const rp_rotary *r, int64_t n_tokens, const double *inv_freq,
 /* Attention of the tokens of a packed row inside their samples: token t sees the tokens s of its sample (causal: s <= t).
  *   o[t][h] = sum_s softmax_s(scale * q[t][h] . k[s][h']) v[s][h'],  h' = h / (q_heads / kv_heads);  lse[t][h] = log sum_s exp(scale * q . k).
  *   Weights are rounded to `type` before their product with v (the sums they are divided by are not); sums are held in 32 bits.
- *   What tokens of other samples hold, infinities and NaN too, does not matter.
+ *   What tokens of other samples hold, infinities and NaN too, does not matter.  Infinities and NaN in the values of a token's own sample may reach it from
+ *   tokens that it does not see: their weight is 0, and 0 times those is NaN.
  *   Strides and addresses of q, k, v, out and their gradients have to be multiples of 16 bytes, strides positive.
- *   lse [n_tokens][q_heads] float, strides as given; nullable in rp_attend.
+ *   lse [n_tokens][q_heads] float, any strides; nullable in rp_attend.
  *   workspace: rp_attend_workspace(a, n_tokens, n_samples) bytes, 16-byte aligned.  Its first int32 is 0 when the kernels are done, or RP_ERR_TIMEOUT if one of their
  *     waits (two seconds each) ran out: outputs that had not been worked out are NaN then.
  * Limits: head_dim <= 128 and a multiple of 8, q_heads a multiple of kv_heads, type RP_F16 or RP_BF16, scale > 0, n_tokens < 2^31 - 512, n_samples <= 2^24. */

@@ -341,8 +341,14 @@ extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_v
 {
     RP_TRY(rp_attend_check(a, n_tokens, n_samples));
     if (!start || !rp_aligned(start, 8) || !workspace || !rp_aligned(workspace, 16) || workspace_bytes < rp_attend_workspace(a, n_tokens, n_samples)) return RP_ERR_ARG;
-    if (n_tokens == 0) return RP_OK;
     RpOpDevice dev;
+    if (n_tokens == 0) {
+        RP_TRY(rp_op_enter(dev, workspace));
+        RP_CUDA(cudaMemsetAsync(workspace, 0, sizeof(AttendHead), (cudaStream_t)cuda_stream));
+        return RP_OK;
+    }
+    const rp_view *const places[] = { out, lse, q, k, v };
+    if (rp_attend_shared(places, 2, 3)) return RP_ERR_ARG;
     RP_TRY(rp_attend_view(q, n_tokens, a->q_heads, dev));
     RP_TRY(rp_attend_view(k, n_tokens, a->kv_heads, dev));
     RP_TRY(rp_attend_view(v, n_tokens, a->kv_heads, dev));

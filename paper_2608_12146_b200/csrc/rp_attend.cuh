@@ -78,6 +78,14 @@ static __device__ __noinline__ void rp_attend_clear(const AttendClears &A, const
 }
 int rp_attend_check(const rp_attend_config *a, i64 T, int N);
 int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev);
+// Is one of the first `n_out` views the same memory as another of them or as one of the `n` behind them?
+static inline bool rp_attend_shared(const rp_view *const *v, int n_out, int n)
+{
+    for (int i = 0; i < n_out; ++i)
+        for (int j = i + 1; j < n_out + n; ++j)
+            if (v[i] && v[j] && v[i]->x && v[i]->x == v[j]->x) return true;
+    return false;
+}
 
 // The attention kernels have twelve warps: eight for the softmax, in two groups of four (a warp reaches the 32 rows of tensor memory that go by its number), one that
 // copies, one that issues the products, two that wait.  The latter four give registers to the former eight: 4 * 32 * 72 + 8 * 32 * 216 = 12 * 32 * 168.

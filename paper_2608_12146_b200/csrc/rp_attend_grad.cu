@@ -582,8 +582,14 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     RP_TRY(rp_attend_check(a, n_tokens, n_samples));
     if (!start || !rp_aligned(start, 8) || !workspace || !rp_aligned(workspace, 16) || workspace_bytes < rp_attend_grad_workspace(a, n_tokens, n_samples)) return RP_ERR_ARG;
     if (!lse || !lse->x || !rp_aligned(lse->x, 4)) return RP_ERR_ARG;
-    if (n_tokens == 0) return RP_OK;
     RpOpDevice dev;
+    if (n_tokens == 0) {
+        RP_TRY(rp_op_enter(dev, workspace));
+        RP_CUDA(cudaMemsetAsync(workspace, 0, sizeof(AttendHead), (cudaStream_t)cuda_stream));
+        return RP_OK;
+    }
+    const rp_view *const places[] = { q_grad, k_grad, v_grad, q, k, v, out, lse, out_grad };
+    if (rp_attend_shared(places, 3, 6)) return RP_ERR_ARG;
     const rp_view *by_q[4] = { q, out, out_grad, q_grad }, *by_k[4] = { k, v, k_grad, v_grad };
     for (int i = 0; i < 4; ++i) {
         RP_TRY(rp_attend_view(by_q[i], n_tokens, a->q_heads, dev));

@@ -461,6 +461,7 @@ static int rotate(const rp_rotary *r, i64 T, const double *freq, const i64 *star
     RpOpDevice dev;
     RP_TRY(check_heads(r, q, grad, dev));
     RP_TRY(check_heads(r, k, grad, dev));
+    if (q && k && q->n_heads && k->n_heads && (q->y == k->y || (grad && q->weight_grad && q->weight_grad == k->weight_grad))) return RP_ERR_ARG;   // two outputs in one place
     const bool weights = grad && ((q && q->n_heads && q->weight_grad) || (k && k->n_heads && k->weight_grad));
     if (weights && (!workspace || workspace_bytes < rp_rotate_workspace(r) || !rp_aligned(workspace, 16))) return RP_ERR_ARG;
     RP_TRY(rp_op_enter(dev, freq, start, first, weights ? workspace : nullptr));

@@ -149,8 +149,31 @@ def test_repeated_streamed_and_captured_calls_agree_bit_for_bit():
 def test_no_tokens():
     import torch
     q = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
-    out, lse = rp.rp_attend(q, q, q, torch.tensor([0, 0], device="cuda"))
+    start = torch.tensor([0, 0], device="cuda")
+    out, lse = rp.rp_attend(q, q, q, start)
     assert out.shape == (0, 2, 64) and lse.shape == (0, 2)
+    space, view = torch.full((64,), 7, dtype=torch.int32, device="cuda"), C.byref(rp.rp_view(start.data_ptr(), 128, 64))
+    cfg, stream = C.byref(rp.rp_attend_config(2, 2, 64, 2, 1, 0.1)), torch.cuda.current_stream().cuda_stream
+    assert rp.lib().rp_attend(cfg, 0, view, view, view, start.data_ptr(), 1, view, None, space.data_ptr(), 256, stream) == 0 and space[0].item() == 0
+    space.fill_(7)
+    views = [view] * 6
+    assert rp.lib().rp_attend_grad(cfg, 0, *views, start.data_ptr(), 1, view, view, view, space.data_ptr(), 256, stream) == 0 and space[0].item() == 0
+
+
+@pytest.mark.gpu
+def test_outputs_in_the_place_of_inputs_are_refused():
+    import torch
+    q, k, v, o = [torch.zeros(4, 1, 64, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    start = torch.tensor([0, 4], device="cuda")
+    for bad in (q, k, v):
+        with pytest.raises(rp.RpError, match="ARG"):
+            rp.rp_attend(q, k, v, start, out=bad)
+    out, lse = rp.rp_attend(q, k, v, start)
+    for kw in (dict(q_grad=q), dict(q_grad=o), dict(k_grad=out), dict(v_grad=v), dict(k_grad=q.clone(), v_grad=None)):
+        if kw.get("v_grad", 0) is None:
+            kw["v_grad"] = kw["k_grad"]
+        with pytest.raises(rp.RpError, match="ARG"):
+            rp.rp_attend_grad(o, q, k, v, out, lse, start, **kw)
 
 
 # ---- gradient ---------------------------------------------------------------------------

@@ -264,6 +264,22 @@ def test_repeated_streamed_and_captured_calls_agree_bit_for_bit():
 
 
 @pytest.mark.gpu
+def test_two_outputs_in_one_place_are_refused():
+    import torch
+    q, w, dw = torch.zeros(2, 1, 8, device="cuda"), torch.ones(8, device="cuda"), torch.zeros(8, device="cuda")
+    y = [torch.zeros_like(q) for _ in range(2)]
+    freq, st, space = torch.ones(4, dtype=torch.float64, device="cuda"), torch.tensor([0, 2], device="cuda"), torch.zeros(1 << 20, device="cuda")
+    with pytest.raises(rp.RpError, match="ARG"):
+        rp.rp_rotate(q, q, freq, st, q_out=y[0], k_out=y[0])
+    cfg, stream = C.byref(rp.rp_rotary(8, 8, 0, 0, 0, 1e-6, 1.0)), torch.cuda.current_stream().cuda_stream
+
+    def call(dk):
+        sides = [C.byref(rp.rp_heads(1, q.data_ptr(), 8, 8, out.data_ptr(), 8, 8, w.data_ptr(), q.data_ptr(), 8, 8, at.data_ptr())) for out, at in zip(y, (dw, dk))]
+        return rp.lib().rp_rotate_grad(cfg, 2, freq.data_ptr(), st.data_ptr(), 1, None, *sides, space.data_ptr(), 4 << 20, stream)
+    assert call(dw) == -1 and call(torch.zeros_like(dw)) == 0
+
+
+@pytest.mark.gpu
 def test_no_tokens():
     import torch
     q = torch.zeros(0, 4, 64, device="cuda")
