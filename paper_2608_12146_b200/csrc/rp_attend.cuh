@@ -24,23 +24,33 @@ static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
     for (int x = threadIdx.x; x < PLAN_BUCKETS; x += 1024) count[x] = 0;
     __syncthreads();
     for (int pass = 0; pass < 2; ++pass) {
-        for (int i = threadIdx.x >> 5; i < A.N; i += 32) {
-            const i64 lo = max(A.start[i], (i64)0), hi = min(A.start[i + 1], A.T);
+        // A lane a sample; samples of many blocks then by the whole warp, one after the other.  (4096 samples of 8 tokens, 8 heads on 2: 891 us with a warp a
+        // sample, 729 so.)
+        const int lane = threadIdx.x & 31;
+        for (int i0 = threadIdx.x & ~31; i0 < A.N; i0 += 1024) {
+            const int i = i0 + lane;
+            const i64 lo = i < A.N ? max(A.start[i], (i64)0) : 0, hi = i < A.N ? min(A.start[i + 1], A.T) : 0;
             const int blocks = hi > lo ? (int)((hi - lo + A.rows - 1) / A.rows) : 0;
-            for (int b = threadIdx.x & 31; b < blocks; b += 32) {
-                const int work = !A.causal ? blocks : A.by_key ? blocks - b : b + 1;
+            const auto take = [&](int sample, int n, int b) {
+                const int work = !A.causal ? n : A.by_key ? n - b : b + 1;
                 const int bucket = PLAN_BUCKETS - 1 - min(work - 1, PLAN_BUCKETS - 1);
                 if (pass == 0) atomicAdd(&count[bucket], 1);
                 else {
                     const int at = atomicAdd(&from[bucket], 1);
-                    if (at < A.most) A.items[at] = make_int2(i, b);
+                    if (at < A.most) A.items[at] = make_int2(sample, b);
                 }
+            };
+            if (blocks <= 4)
+                for (int b = 0; b < blocks; ++b) take(i, blocks, b);
+            for (u32 many = __ballot_sync(0xffffffffu, blocks > 4); many; many &= many - 1) {
+                const int who = __ffs((int)many) - 1, n = __shfl_sync(0xffffffffu, blocks, who);
+                for (int b = lane; b < n; b += 32) take(i0 + who, n, b);
             }
         }
         __syncthreads();
         if (pass == 0) {
             // a thread a bucket
-            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = count[threadIdx.x];
+            const int warp = threadIdx.x >> 5, c = count[threadIdx.x];
             int x = c;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
