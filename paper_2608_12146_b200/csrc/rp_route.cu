@@ -486,6 +486,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route_grad(
 {
     constexpr int NSUB = ROUTE_THREADS / SUB, EP = VPL * SUB;
     __shared__ __align__(16) float rows[NSUB][EP];
+    __shared__ unsigned char tags[NSUB][EP];
     const int sub = threadIdx.x / SUB, sl = threadIdx.x % SUB, e0 = sl * VPL, first_lane = (threadIdx.x & 31) - sl;
     const bool soft = A.score == RP_SCORE_SOFTMAX, gates = A.gates_grad != nullptr;
     const float loss_grad = A.loss_grad ? *A.loss_grad : 0.0f;
@@ -557,8 +558,10 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route_grad(
         for (int i = 0; i < VPL; i += 4) *(float4 *)&rows[sub][e0 + i] = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
         __syncwarp();
         if (gates) {
-            const u32 same = __match_any_sync(0xffffffffu, valid ? (first_lane << 11) + e : 0x40000000 + (int)(threadIdx.x & 31));
-            if (!__any_sync(0xffffffffu, __popc(same) > 1)) {
+            // (does an expert come twice? its tag is then another lane's)
+            if (valid) tags[sub][e] = (unsigned char)sl;
+            __syncwarp();
+            if (!__any_sync(0xffffffffu, valid && tags[sub][e] != sl)) {
                 if (valid) rows[sub][e] += add;
             } else
                 for (int j = 0; j < A.k; ++j) {
