@@ -8,7 +8,11 @@
  * objective and refines a population of layouts by population annealing.  Every step
  * runs in CUDA kernels of this library; there is no CPU fallback.
  *
- * Conventions
+ * Beside the planner it has the operators of a layer that work with what the planner does:
+ * recorded routes, the router with its balance loss, positions and attention inside the
+ * samples of a packed row.  They have conventions of their own, given in their section.
+ *
+ * Conventions of the planner
  *  - All functions return RP_OK (0) or a negative rp_status; none throws, prints, aborts
  *    or traps.  rp_strerror() names a status.  Calling out of order gives RP_ERR_STATE.
  *  - Array arguments are plain pointers to HOST or DEVICE memory (either is accepted for

@@ -98,7 +98,8 @@ __device__ __forceinline__ void store_row(u32 at, X *out, int d, bool there, flo
 // Tiles of 128 queries: scores, do v^T and the two sums fill the tensor memory (2 * 128 + 2 * head_dim columns).  Both groups of four warps work on a tile, 64 columns
 // each.  The products come in the order dv(j), s(j + 1), dk(j), do v^T(j + 1): while the weights of a tile are worked out, the tensor cores add up dk of the one
 // before and multiply do v^T of this one; while the gradients of its scores are, dv of this and scores of the next.  Weights and gradients lie as operands where the
-// scores and the products of their group were.  (Tiles of 64 queries, two of them at a time, one for each group: 435 us in place of the figure in the launch's comment.)
+// scores and the products of their group were.  (Tiles of 64 queries, two of them at a time, one for each group: 435 us
+// for what takes 249; see the launch.)
 template <int D> struct KeySmem {
     static constexpr int TILE = 128 * D * 2, STAGES = 2;
     alignas(1024) unsigned char k[TILE];
@@ -326,7 +327,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 // ---------------------------------------------------------------------------------------
 // Tiles of 128 keys, 64 columns to each of the two groups of four warps.  q and do, which all tiles of a block share, lie in tensor memory as the operands of their
 // products: from shared memory a product of 128 x 128 x 16 reads all of the 128 bytes that a cycle of it has, with the copies coming in beside (220 us for what
-// takes the figure in the launch's comment).  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
+// takes 166).  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
 // tile and do v^T of the next while the weights of the next are.  Columns: scores 128, do v^T 128 (and in its place ds as operand), dq, q and do 64 each.
 template <int D> struct QuerySmem {
     static constexpr int TILE = 128 * D * 2, STAGES = 3;
@@ -561,7 +562,9 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
     k_attend_keys<X, D><<<(int)std::min((i64)sms, most * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
     RP_TRY(rp_op_launched());
-    // (8192 tokens in three samples, 16 heads on 4: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 249 us; the queries' 166)
+    // (8192 tokens in three samples, 16 heads on 4, 128 wide: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 249 us, the
+    // queries' 166; 398 us for the whole call.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
+    // sample of 2048 tokens, 5 heads on 1: 193 -> 69 us - but a sample's gradients then depend on what else is in its row.)
     cudaLaunchConfig_t how = {};
     how.gridDim = dim3((unsigned)std::min((i64)sms, most * keys.Hq));
     how.blockDim = dim3(ATTEND_THREADS);

@@ -9,6 +9,8 @@
 // sums over experts are shuffles.  Every such group of lanes owns a run of neighbouring tokens and carries the sums of p of the run's
 // present group of tokens in registers, its counts in shared memory; what a CTA's last runs hold meets in shared memory before it goes out.
 // Sums of p leave a CTA in fixed point (2^-36): additions of whole numbers, so their order does not matter.
+// Bound by instructions: 131072 tokens of 256 experts, k = 8, take 86 us where their bytes take 12: 470 warp instructions a token (scores of 8 experts a lane, their keys,
+// k rounds of the largest), 71 % of the issue slots, the integer units 60 %.  The gradient, 320 a token, 61 us (its bytes 22): it waits for shuffles and shared memory.
 #include <limits.h>
 
 #include <algorithm>

@@ -26,7 +26,7 @@ struct CountArgs {
 
 #define COUNT_THREADS 512
 // A lane's counters lie in a bank of its own (counter of expert e at e * 32 + lane), so that the 32 additions of a warp go in one go whatever they count; with one
-// counter for all lanes, skewed choices put 3 to 4 of them in one bank (900001 tokens of 32 layers, 8 of 128 experts in bytes: 207 us).
+// counter for all lanes, skewed choices put 3 to 4 of them in one bank (900001 tokens of 32 layers, 8 of 128 experts in bytes: 207 us for what takes 91).
 __device__ __forceinline__ void count_one(u32 at, u32 e)
 {
     u32 to;
@@ -62,6 +62,7 @@ __device__ __forceinline__ i64 tile_start(const CountArgs &A, int b, int n)
     if (lo <= (u32)A.N) t = min(t, __ldg(A.start + lo));
     return min(max(t, (i64)0), A.T);
 }
+// Bound by the additions: 230 million of them for those 230 MB, 58 % of what shared memory takes (52 us), 2.7 TB/s from memory of 6.5.
 // A CTA owns a tile of tokens and lanes * LAYERS layers, whatever samples the tokens belong to: it counts one sample after the other in shared memory and adds what
 // it found to the output (whole numbers: the order does not matter).  WORDS: 32-bit words of a token's choices in LAYERS layers, copied as such into a ring of the
 // lane's own, DEPTH tokens ahead, across the samples' ends; 0: any number of choices, read one by one.
