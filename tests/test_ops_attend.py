@@ -161,6 +161,41 @@ def test_no_tokens():
 
 
 @pytest.mark.gpu
+def test_without_the_logs_of_the_sums():
+    import torch
+    q, k, v, _ = inputs((300, 2, 1, 64, [0, 100, 300]), "bfloat16")
+    start = torch.tensor([0, 100, 300], device="cuda")
+    want, _ = rp.rp_attend(q, k, v, start)
+    out, space = torch.zeros(300, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1024, dtype=torch.int32, device="cuda")
+
+    def view(x):
+        return C.byref(rp.rp_view(x.data_ptr(), x.stride(0), x.stride(1)))
+    cfg, stream = C.byref(rp.rp_attend_config(2, 1, 64, 2, 1, 64 ** -0.5)), torch.cuda.current_stream().cuda_stream
+    for lse in (None, C.byref(rp.rp_view(None, 0, 0))):
+        out.zero_()
+        assert rp.lib().rp_attend(cfg, 300, view(q), view(k), view(v), start.data_ptr(), 2, view(out), lse, space.data_ptr(), 4096, stream) == 0
+        assert (out == want).all() and space[0].item() == 0
+
+
+@pytest.mark.gpu
+def test_samples_of_every_short_length():
+    """Lists of samples of 0 to 6 blocks, many of no token."""
+    import torch
+    lengths = [0, 1, 127, 128, 129, 255, 256, 257, 0, 0, 700, 1400, 2, 0] + [1] * 40 + [0] * 1500 + [33]
+    start = [0] + np.cumsum(lengths).tolist()
+    q, k, v, g = inputs((start[-1], 2, 1, 64, start), "bfloat16")
+    out, lse = rp.rp_attend(q, k, v, torch.tensor(start, device="cuda"))
+    do = torch.randn(start[-1], 2, 64, generator=g).bfloat16().cuda()
+    grads = rp.rp_attend_grad(do, q, k, v, out, lse, torch.tensor(start, device="cuda"))
+    for lo, hi in samples(start, start[-1]):
+        st = torch.tensor([0, hi - lo], device="cuda")
+        o, l = rp.rp_attend(q[lo:hi], k[lo:hi], v[lo:hi], st)
+        assert (o == out[lo:hi]).all() and (l == lse[lo:hi]).all()
+        for a, b in zip(rp.rp_attend_grad(do[lo:hi], q[lo:hi], k[lo:hi], v[lo:hi], o, l, st), grads):
+            assert (a == b[lo:hi]).all()
+
+
+@pytest.mark.gpu
 def test_outputs_in_the_place_of_inputs_are_refused():
     import torch
     q, k, v, o = [torch.zeros(4, 1, 64, dtype=torch.bfloat16, device="cuda") for _ in range(4)]

@@ -287,3 +287,18 @@ def test_no_tokens():
     inv, st = torch.ones(32, dtype=torch.float64, device="cuda"), torch.tensor([0, 0], device="cuda")
     assert rp.rp_rotate(q, None, inv, st)[0].shape == (0, 4, 64)
     assert (rp.rp_rotate_grad(q, None, q, None, inv, st, q_weight=w)[2] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [128, 34])
+def test_heads_and_tokens_that_repeat(d):
+    import torch
+    g = torch.Generator().manual_seed(d)
+    inv, st, w = 100.0 ** (-torch.arange(0, d, 2, dtype=torch.float64, device="cuda") / d), torch.tensor([0, 4, 30], device="cuda"), torch.rand(d, generator=g).cuda()
+    for base in (torch.randn(30, 1, d, generator=g), torch.randn(1, 5, d, generator=g)):
+        q = base.bfloat16().cuda().expand(30, 5, d)
+        dy = torch.randn(30, 1, d, generator=g).bfloat16().cuda().expand(30, 5, d)
+        for a, b in zip(rp.rp_rotate(q, q, inv, st, q_weight=w), rp.rp_rotate(q.contiguous(), q.contiguous(), inv, st, q_weight=w)):
+            assert (a == b).all()
+        one, two = rp.rp_rotate_grad(dy, None, q, None, inv, st, q_weight=w), rp.rp_rotate_grad(dy.contiguous(), None, q.contiguous(), None, inv, st, q_weight=w)
+        assert (one[0] == two[0]).all() and (one[2] == two[2]).all()

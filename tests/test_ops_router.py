@@ -291,3 +291,53 @@ def test_no_tokens():
     routes, gates, counts, loss = rp.rp_route(x, 2, torch.tensor([0, 0], device="cuda"), loss_coef=1.0)
     assert routes.shape == (0, 2) and (counts == 0).all() and loss.item() == 0
     assert rp.rp_route_grad(x, routes, torch.tensor([0, 0], device="cuda"), counts, gates_grad=gates).shape == (0, 16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 3000])
+def test_outputs_that_may_be_left_out(T):
+    import torch
+    x = torch.randn(T, 64, generator=torch.Generator().manual_seed(T)).bfloat16().cuda()
+    start = torch.tensor([0, T // 2, T], device="cuda")
+    want = rp.rp_route(x, 4, start)
+    cfg, stream = C.byref(rp.rp_router(64, 4, 2, 0, 1, 1.0, 0.0)), torch.cuda.current_stream().cuda_stream
+    for with_counts in (False, True):
+        routes, gates, counts = torch.full((T, 4), 9, dtype=torch.int32, device="cuda"), torch.zeros(T, 4, device="cuda"), torch.full((2, 64), 7, dtype=torch.int32, device="cuda")
+        assert rp.lib().rp_route(cfg, x.data_ptr(), 64, T, None, start.data_ptr(), 2, 0, routes.data_ptr(), 4, 4, gates.data_ptr(),
+                                 counts.data_ptr() if with_counts else None, None, None, 0, stream) == 0
+        assert (routes == want[0]).all() and (gates == want[1]).all() and (counts == (want[2] if with_counts else 7)).all()
+
+
+@pytest.mark.gpu
+def test_rows_that_repeat_or_run_backwards():
+    import torch
+    x = torch.randn(50, 40, generator=torch.Generator().manual_seed(2)).cuda()
+    start = torch.tensor([0, 20, 50], device="cuda")
+    same = x[:1].expand(50, 40)
+    assert all((a == b).all() for a, b in zip(rp.rp_route(same, 3, start, loss_coef=0.1), rp.rp_route(same.contiguous(), 3, start, loss_coef=0.1)))
+    want = rp.rp_route(x.flip(0), 3, start)
+    cfg, stream = C.byref(rp.rp_router(40, 3, 0, 0, 1, 1.0, 0.0)), torch.cuda.current_stream().cuda_stream
+    routes, gates = torch.zeros(50, 3, dtype=torch.int32, device="cuda"), torch.zeros(50, 3, device="cuda")
+    assert rp.lib().rp_route(cfg, x[49:].data_ptr(), -40, 50, None, start.data_ptr(), 2, 0, routes.data_ptr(), 4, 3, gates.data_ptr(), None, None, None, 0, stream) == 0
+    assert (routes == want[0]).all() and (gates == want[1]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E,k", [(16, 2), (64, 4), (300, 8)])
+def test_many_groups_in_runs_of_many_shapes(E, k):
+    """Groups that end inside, between and across the runs of a CTA; as many as take a launch of their own for the loss."""
+    import torch
+    T = 6000
+    x = torch.randn(T, E, generator=torch.Generator().manual_seed(E)).cuda()
+    for cuts in ([0, 1, 2, 3, 2000, 2001, 5000, T], list(range(0, T + 1, 7)) + [T], [0] * 18 + [3000] * 5 + [T], [100, 4000, 4001]):
+        start = torch.tensor(cuts, device="cuda")
+        routes, _, counts, loss = rp.rp_route(x, k, start, loss_coef=0.5)
+        p = torch.softmax(x.double(), 1)
+        want, total = torch.zeros(len(cuts) - 1, E, dtype=torch.int64), 0.0
+        for i, (lo, hi) in enumerate(zip(cuts, cuts[1:])):
+            if hi > lo:
+                want[i] = torch.bincount(routes[lo:hi].reshape(-1).long(), minlength=E).cpu()
+                total += E / (k * (hi - lo) ** 2) * (want[i].double().cuda() * p[lo:hi].sum(0)).sum().item()
+        assert (counts.cpu() == want).all()
+        # (p to FLOAT of itself, sums of a run and of a CTA in 32 bits: 40 terms)
+        assert abs(loss.item() - 0.5 / (len(cuts) - 1) * total) <= (2 * FLOAT + 40 * 2.0 ** -24) * 0.5 / (len(cuts) - 1) * total

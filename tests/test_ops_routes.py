@@ -118,6 +118,16 @@ def test_output_is_written_whole_and_nothing_behind_it():
 
 
 @pytest.mark.gpu
+def test_records_that_repeat():
+    import torch
+    start = torch.tensor([0, 5, 700], device="cuda")
+    for wide in (torch.randint(0, 32, (1, 6, 8), device="cuda"), torch.randint(0, 32, (700, 1, 8), device="cuda")):
+        for kind in (torch.uint8, torch.int16, torch.int32):
+            routes = wide.to(kind).expand(700, 6, 8)
+            assert (rp.rp_count_routes(routes, start, 32) == rp.rp_count_routes(routes.contiguous(), start, 32)).all()
+
+
+@pytest.mark.gpu
 def test_far_elements_of_a_long_record():
     """Offsets that pass 32 bits: the last tokens of a record of 2^32 + bytes."""
     import torch
