@@ -9,8 +9,8 @@
 // sums over experts are shuffles.  Every such group of lanes owns a run of neighbouring tokens and carries the sums of p of the run's
 // present group of tokens in registers, its counts in shared memory; what a CTA's last runs hold meets in shared memory before it goes out.
 // Sums of p leave a CTA in fixed point (2^-36): additions of whole numbers, so their order does not matter.
-// Bound by instructions: 131072 tokens of 256 experts, k = 8, take 86 us where their bytes take 12: 470 warp instructions a token (scores of 8 experts a lane, their keys,
-// k rounds of the largest), 71 % of the issue slots, the integer units 60 %.  The gradient, 320 a token, 61 us (its bytes 22): it waits for shuffles and shared memory.
+// Bound by instructions: 131072 tokens of 256 experts, k = 8, take 78 us where their bytes take 12: 420 warp instructions a token (scores of 8 experts a lane, their keys,
+// k rounds of the largest), 72 % of the issue slots, the integer units 59 %.  The gradient, 320 a token, 61 us (its bytes 22): it waits for shuffles and shared memory.
 #include <limits.h>
 
 #include <algorithm>
@@ -153,15 +153,20 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
         sum = sub_sum<SUB>(sum);
     } else {
         if (SHARED) {
+            f2 both = rp_f2(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < VPL; i += 2) {
-                const float a = 1.0f + rp_exp2(min_or_nan(x[i] * -RP_LOG2E, 63.0f)), b = 1.0f + rp_exp2(min_or_nan(x[i + 1] * -RP_LOG2E, 63.0f));
+                float a, b;
+                rp_parts(rp_mul(rp_f2(x[i], x[i + 1]), rp_f2(-RP_LOG2E, -RP_LOG2E)), a, b);
+                rp_parts(rp_add(rp_f2(rp_exp2(min_or_nan(a, 63.0f)), rp_exp2(min_or_nan(b, 63.0f))), rp_f2(1.0f, 1.0f)), a, b);
                 const float r = reciprocal(a * b);
-                s[i] = r * b;
-                s[i + 1] = r * a;
-                sum += s[i] + s[i + 1];
+                const f2 v = rp_mul(rp_f2(b, a), rp_f2(r, r));
+                both = rp_add(both, v);
+                rp_parts(v, s[i], s[i + 1]);
             }
-            sum = sub_sum<SUB>(sum);
+            float other;
+            rp_parts(both, sum, other);
+            sum = sub_sum<SUB>(sum + other);
         }
         if (!SHARED || __any_sync(0xffffffffu, sum < 1.0e-12f)) {
             sum = 0.0f;
@@ -185,30 +190,41 @@ __device__ __forceinline__ u32 order_of(float x)
     return (u32)b ^ ((u32)(b >> 31) | 0x80000000u);
 }
 
+// Two 16-bit numbers as unsigned ones in the same order; -0 as 0, NaN above all.
+__device__ __forceinline__ u32 signs_of_pair(u32 w) { u32 m; asm("prmt.b32 %0, %1, 0, 0xbb99;" : "=r"(m) : "r"(w)); return m; }      // 0xffff where the sign is set
+__device__ __forceinline__ u32 order_of_pair(u32 w, bf16) { asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(w) : "r"(0u)); return w ^ (signs_of_pair(w) | 0x80008000u); }
+__device__ __forceinline__ u32 order_of_pair(u32 w, __half) { asm("add.rn.f16x2 %0, %0, %1;" : "+r"(w) : "r"(0u)); return w ^ (signs_of_pair(w) | 0x80008000u); }
+__device__ __forceinline__ float of_16(u32 w, bf16) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float of_16(u32 w, __half) { return __half2float(__ushort_as_half((unsigned short)w)); }
+
 // The k experts with the largest logits, in falling order, ties to the lower one: lane j of the token's gets the j-th, and its logit.
-// 16-bit logits leave their last 13 bits as floats free for the expert's number: keys that are all different and tell it all.  The largest of all goes round by
+// 16-bit logits leave half a word for the expert's number: keys that are all different and tell it all.  The largest of all goes round by
 // round; a lane has only its two largest at hand.  Where one that has had both turns out to hold a third of the k (one token in 25 of independent logits,
 // 256 experts and k = 8), the token is done again by lanes that look for their next key each time.
-template <int VPL, int SUB>
-__device__ __forceinline__ void choose_by_keys(const RouteArgs &A, const float *x, int e0, int sl, i64 &e, float &xe)
+template <typename X, int VPL, int SUB>
+__device__ __forceinline__ void choose_by_keys(const RouteArgs &A, const Row<X, VPL> &row, int e0, int sl, i64 &e, float &xe)
 {
     u32 key[VPL], first = 0, second = 0;
     const u32 code = (u32)(1023 - e0) | 0x400u;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        key[i] = (order_of(x[i]) & ~0x1fffu) | (code - i);
-        first = max(first, key[i]);
+    for (int i = 0; i < VPL; i += 2) {
+        const uint4 &q = row.p[i / 8].w[0];
+        const u32 w = order_of_pair(i % 8 == 0 ? q.x : i % 8 == 2 ? q.y : i % 8 == 4 ? q.z : q.w, X()), codes = (code - i) | (code - i - 1) << 16;
+        key[i] = __byte_perm(codes, w, 0x5410);
+        key[i + 1] = __byte_perm(codes, w, 0x7632);
+        first = max(max(first, key[i]), key[i + 1]);
     }
 #pragma unroll
     for (int i = 0; i < VPL; ++i) second = max(second, key[i] - first);      // (those below it wrap around to the largest numbers, in their order)
     second += first;
     u32 mine = 0, best = 0;
-    bool both = false;
+#pragma unroll 4
     for (int j = 0; j < A.k; ++j) {
         best = sub_max<SUB>(first);
         if (sl == j) mine = best;
-        if (first == best) { both = second == 0; first = second; second = 0; }
+        if (first == best) { first = second; second = 0; }
     }
+    const bool both = first == 0;
     if (__any_sync(0xffffffffu, both)) {
         int more = 0;
 #pragma unroll
@@ -226,8 +242,8 @@ __device__ __forceinline__ void choose_by_keys(const RouteArgs &A, const float *
         }
     }
     e = 1023 - (int)(mine & 0x3ffu);
-    const u32 b = mine & ~0x1fffu;
-    xe = __uint_as_float((b >> 31) ? b ^ 0x80000000u : ~b & ~0x1fffu);
+    const u32 b = mine >> 16;
+    xe = of_16(b & 0x8000u ? b ^ 0x8000u : b ^ 0xffffu, X());
 }
 // The same by any number, round by round: the largest, the lowest lane that has it, and its lowest expert.
 template <int VPL, int SUB>
@@ -384,17 +400,19 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route(Route
     for (int step = 0; step < run; ++step, x_at += A.row, gate_at += A.k, route_at += route_step) {
         const bool there = step < n;
         float x[VPL], s[VPL], top = 0.0f, inv = 0.0f, xe = 0.0f;
-        open_row<X, VPL>(row, x);
+        const Row<X, VPL> here = row;
         // lane j of the token's has its j-th choice (there are at least k of them)
         i64 e = e_next;
         if (step + 1 < n) {
             load_row<X, VPL>(A, x_at + A.row + e0, e0, row);
             if (A.replay && sl < A.k) e_next = rp_load_route(route_at + route_step, A.route_bytes, 0);
         }
+        if constexpr (sizeof(X) == 2)
+            if (!A.replay && !A.bias) choose_by_keys<X, VPL, SUB>(A, here, e0, sl, e, xe);
+        open_row<X, VPL>(here, x);
         if (want_loss || A.score == RP_SCORE_SOFTMAX || A.bias) scores<VPL, SUB, true>(A, x, s, top, inv);
         if (!A.replay) {
-            if (sizeof(X) == 2 && !A.bias) choose_by_keys<VPL, SUB>(A, x, e0, sl, e, xe);
-            else {
+            if (sizeof(X) == 4 || A.bias) {
                 float number[VPL];
 #pragma unroll
                 for (int i = 0; i < VPL; ++i)
@@ -430,7 +448,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route(Route
         const bool held = there && g >= 0 && g < A.G;
         if (want_loss && held) {
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) acc[i] = fmaf(s[i], inv, acc[i]);
+            for (int i = 0; i < VPL; i += 2) rp_parts(rp_fma(rp_f2(s[i], s[i + 1]), rp_f2(inv, inv), rp_f2(acc[i], acc[i + 1])), acc[i], acc[i + 1]);
         }
         if (valid && held && want_counts) atomicAdd(&cnt[sub][(int)e], 1);
         if (there && sl < A.k) {

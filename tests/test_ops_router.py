@@ -1,5 +1,6 @@
 """Router with its balance loss and gradient, against the formulas in 64 bits."""
 import ctypes as C
+import math
 
 import numpy as np
 import pytest
@@ -239,6 +240,19 @@ def test_numbers_that_are_none_stay_in_their_row():
     assert counts.sum().item() == 240 and (routes[60:] == -1).all() and (gates[60:] == 0).all()
     grad = rp.rp_route_grad(x.cuda(), routes, torch.tensor([0, 60], device="cuda"), counts, gates_grad=torch.ones_like(gates))
     assert torch.isfinite(grad[rows]).all() and (grad[60:] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+def test_order_of_every_16_bit_number(kind):
+    """All bit patterns in rows of 64 neighbours of a shuffled list: falling order, NaN of either sign above all, subnormal numbers apart."""
+    import torch
+    bits = torch.randperm(1 << 16, generator=torch.Generator().manual_seed(4)).to(torch.int32)
+    x = (bits - (1 << 15)).to(torch.int16).view(getattr(torch, kind)).view(-1, 64)
+    place = torch.where(x.isnan(), math.inf, x.double().clamp(-1e300, 1e300))
+    want = torch.argsort(-(place + 0.0), dim=1, stable=True)[:, :8]
+    routes, _, counts, _ = rp.rp_route(x.cuda(), 8, torch.tensor([0, len(x)], device="cuda"), score="sigmoid")
+    assert (routes.cpu().long() == want).all() and counts.sum().item() == 8 * len(x)
 
 
 @pytest.mark.gpu
