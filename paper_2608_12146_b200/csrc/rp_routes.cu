@@ -73,7 +73,8 @@ __global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
     constexpr int DEPTH = CountRing<WORDS>::DEPTH, COPY = WORDS >= 4 ? 16 : 4 * WORDS;       // bytes of a copy
     extern __shared__ __align__(16) u32 hist[];          // [LAYERS][rows][32], ring
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const i64 t0 = tile_start(A, blockIdx.x, gridDim.x), t1 = max(t0, tile_start(A, blockIdx.x + 1, gridDim.x));
+    // (no tile is as long as 2^30 tokens where the starts do not decrease)
+    const i64 t0 = tile_start(A, blockIdx.x, gridDim.x), t1 = min(max(t0, tile_start(A, blockIdx.x + 1, gridDim.x)), t0 + (1ll << 30));
     const int l0 = blockIdx.y * A.lanes * LAYERS, layer = l0 + lane % A.lanes * LAYERS;      // first of the CTA, first of the lane
     const int per = 32 / A.lanes, step = COUNT_THREADS / 32 * per;                          // tokens of a warp, of the CTA at a time
     const R *routes = (const R *)A.routes;

@@ -201,3 +201,46 @@ def test_window_from_a_record_plans_as_from_its_demand(host_lengths):
     with pytest.raises(rp.RpError, match="ARG"):
         rp._check(rp.lib().rp_window_load_routes(C.byref(C.c_void_p()), C.byref(rp._window_config(n, L, E, k, s.token_cap, s.dp_width, s.ep_width, 2, None, (1.0,), (0.0,), 0, 0)[0]),
                                                  w.lengths.ctypes.data, routes.ctypes.data, 1, T, L * k, k, None), "host record")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("order", ["token", "layer"])
+@pytest.mark.parametrize("kind", ["uint8", "int16", "int32", "int64"])
+def test_window_from_records_of_every_type_and_order(kind, order):
+    import torch
+    rng = np.random.default_rng(3)
+    lengths = np.array([30, 1, 64, 17, 40, 40, 9, 55], np.int32)
+    T, L, E, k = int(lengths.sum()), 3, 16, 2
+    host = rng.integers(0, E, (T, L, k)).astype(getattr(np, kind))
+    record = torch.from_numpy(host if order == "token" else np.ascontiguousarray(host.transpose(1, 0, 2))).cuda()
+    record = record if order == "token" else record.transpose(0, 1)
+    kw = dict(token_cap=128, dp_width=2, ep_width=4, pop_size=8, seed=1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    demand = count(host, [0] + np.cumsum(lengths).tolist(), E).astype(np.int32)
+    got = []
+    for ctx in (rp.rp_window_load(lengths, demand, top_k=k, **kw), rp.rp_window_load_routes(lengths, record, E, stream=side, **kw)):
+        got.append(rp.rp_place_experts(ctx))
+        rp.rp_destroy(ctx)
+    for a, b in zip(*got):
+        assert np.array_equal(np.asarray(a), np.asarray(b))
+
+
+@pytest.mark.gpu
+def test_lengths_that_make_no_window_are_refused():
+    import torch
+    record = torch.zeros(100, 2, 1, dtype=torch.uint8, device="cuda")
+    kw = dict(token_cap=128, dp_width=1, ep_width=1, pop_size=8)
+    for lengths in ([40, -20, 80], [-1, 50, 51], [0, 50, 50], [100, 100, 100], [200, -50, -50]):
+        with pytest.raises(rp.RpError, match="CONSERVATION"):
+            rp.rp_window_load_routes(np.array(lengths, np.int32), record, 4, **kw)
+
+
+@pytest.mark.gpu
+def test_starts_that_decrease_read_nothing_else():
+    """Not allowed, and without a promise for the counts; nothing outside the record is counted all the same."""
+    import torch
+    routes = torch.full((500, 2, 3), 1, dtype=torch.int16, device="cuda")
+    for start in ([0, 400, 100, 500], [500, 0, 500], [300, 200, 100, 0], [10 ** 12, -10 ** 12, 10 ** 12]):
+        got = rp.rp_count_routes(routes, torch.tensor(start, device="cuda"), 4)
+        assert (got[:, :, [0, 2, 3]] == 0).all() and (got >= 0).all() and got.sum().item() <= 500 * 2 * 3 * (len(start) - 1)
