@@ -135,7 +135,8 @@ __device__ __forceinline__ float min_or_nan(float x, float y)
 // Scores of one token from its logits: softmax: e^(x - max) and 1 / their sum; sigmoid: s, and 1 / their sum.
 // `top` is what the largest logit is taken for: 0 where it is -inf (all scores are 0 then, and so is the inverse).
 // SHARED: two sigmoids share a reciprocal, 1 / (1 + a) = (1 + b) / ((1 + a)(1 + b)), where a score of less than 2^-63 counts as 2^-63; rows whose scores add up to
-// less than 2^-40 are worked out one by one.
+// less than 2^-40 are worked out one by one.  So are all rows whose experts are chosen by score and bias: a score may not depend on its neighbour's logit there (equal
+// logits are ties, and a NaN stays where it is).
 template <int VPL, int SUB, bool SHARED>
 __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float *s, float &top, float &inv)
 {
@@ -152,7 +153,7 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
         for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2(fmaf(x[i], RP_LOG2E, shift)); sum += s[i]; }
         sum = sub_sum<SUB>(sum);
     } else {
-        if (SHARED) {
+        if (SHARED && !A.bias) {
             f2 both = rp_f2(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < VPL; i += 2) {
@@ -168,7 +169,7 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
             rp_parts(both, sum, other);
             sum = sub_sum<SUB>(sum + other);
         }
-        if (!SHARED || __any_sync(0xffffffffu, sum < 1.0e-12f)) {
+        if (!SHARED || A.bias || __any_sync(0xffffffffu, sum < 1.0e-12f)) {
             sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) { s[i] = sigmoid(x[i]); sum += s[i]; }

@@ -355,3 +355,42 @@ def test_many_groups_in_runs_of_many_shapes(E, k):
         assert (counts.cpu() == want).all()
         # (p to FLOAT of itself, sums of a run and of a CTA in 32 bits: 40 terms)
         assert abs(loss.item() - 0.5 / (len(cuts) - 1) * total) <= (2 * FLOAT + 40 * 2.0 ** -24) * 0.5 / (len(cuts) - 1) * total
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("constant", [0.0, 0.25])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("E,k", [(16, 3), (64, 8), (256, 8), (600, 12)])
+def test_equal_logits_under_one_bias_are_ties(E, k, kind, constant):
+    """Sigmoid scores of logits in steps of 1/8 up to 8: neighbours are 4e-5 apart, so a bias that all have alike chooses what none does."""
+    import torch
+    x = (torch.randn(500, E, generator=torch.Generator().manual_seed(E)) * 16).round().clamp(-64, 64) / 8
+    x[::7, 1] = x[::7, 0]
+    x[3, 5] = float("nan")                               # counts as largest, and its neighbours by their own scores
+    x[4, 2], x[4, 11] = float("nan"), float("nan")
+    x = x.to(getattr(torch, kind))
+    want = torch.argsort(-torch.where(x.isnan(), math.inf, x.double()), dim=1, stable=True)[:, :k]
+    start = torch.tensor([0, 200, 500], device="cuda")
+    bias = torch.full((E,), constant, device="cuda")
+    routes, gates, counts, _ = rp.rp_route(x.cuda(), k, start, score="sigmoid", choice_bias=bias, loss_coef=0.1)
+    assert (routes.cpu().long() == want).all()
+    without = rp.rp_route(x.cuda(), k, start, score="sigmoid", loss_coef=0.1)
+    rows = [t for t in range(500) if t not in (3, 4)]
+    assert (without[0] == routes).all() and (without[1][rows] == gates[rows]).all() and (without[2] == counts).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_experts_taken_out_come_last_under_a_bias(kind):
+    """A score of 0 comes behind any other, however small (sigmoid(-50) = 2e-22)."""
+    import torch
+    x = torch.full((40, 64), -50.0)
+    x[:, :20] = -math.inf
+    x[:, 63] = 0.0
+    x[1::2, 30:34] = torch.tensor([-48.0, -60.0, -45.0, -48.0])
+    x = x.to(getattr(torch, kind))
+    want = torch.argsort(-x.double(), dim=1, stable=True)[:, :6]
+    routes, gates, _, _ = rp.rp_route(x.cuda(), 6, torch.tensor([0, 40], device="cuda"), score="sigmoid", choice_bias=torch.zeros(64, device="cuda"))
+    assert (routes.cpu().long() == want).all()
+    chosen = torch.sigmoid(x.double()).gather(1, want)
+    assert ((gates.cpu().double() - chosen / chosen.sum(1, keepdim=True)).abs() <= FLOAT).all()
