@@ -169,11 +169,17 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
             rp_parts(both, sum, other);
             sum = sub_sum<SUB>(sum + other);
         }
-        if (!SHARED || A.bias || __any_sync(0xffffffffu, sum < 1.0e-12f)) {
-            sum = 0.0f;
+        const bool alone = !SHARED || A.bias || sum < 1.0e-12f;
+        if (__any_sync(0xffffffffu, alone)) {
+            float s1[VPL], sum1 = 0.0f;                      // (the warp's other tokens keep theirs)
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) { s[i] = sigmoid(x[i]); sum += s[i]; }
-            sum = sub_sum<SUB>(sum);
+            for (int i = 0; i < VPL; ++i) { s1[i] = sigmoid(x[i]); sum1 += s1[i]; }
+            sum1 = sub_sum<SUB>(sum1);
+            if (alone) {
+                sum = sum1;
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) s[i] = s1[i];
+            }
         }
     }
     inv = sum < 1.2e-38f ? 0.0f : reciprocal(sum);

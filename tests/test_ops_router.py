@@ -394,3 +394,17 @@ def test_experts_taken_out_come_last_under_a_bias(kind):
     assert (routes.cpu().long() == want).all()
     chosen = torch.sigmoid(x.double()).gather(1, want)
     assert ((gates.cpu().double() - chosen / chosen.sum(1, keepdim=True)).abs() <= FLOAT).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E", [16, 64, 128])
+def test_tokens_with_tiny_scores_leave_those_beside_them_alone(E):
+    """The loss of one token's group, bit for bit, whatever a token of no group beside it holds."""
+    import torch
+    start = torch.tensor([0, 1], device="cuda")
+    for seed in range(60):
+        x = logits_of(64, E, torch.float32, seed).cuda()
+        want = rp.rp_route(x, 2, start, score="sigmoid", loss_coef=1.0)
+        x[1:] = -100.0
+        got = rp.rp_route(x, 2, start, score="sigmoid", loss_coef=1.0)
+        assert all((a == b).all() for a, b in zip(want, got)), seed
