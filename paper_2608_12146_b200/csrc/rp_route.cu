@@ -135,8 +135,8 @@ __device__ __forceinline__ float min_or_nan(float x, float y)
 // Scores of one token from its logits: softmax: e^(x - max) and 1 / their sum; sigmoid: s, and 1 / their sum.
 // `top` is what the largest logit is taken for: 0 where it is -inf (all scores are 0 then, and so is the inverse).
 // SHARED: two sigmoids share a reciprocal, 1 / (1 + a) = (1 + b) / ((1 + a)(1 + b)), where a score of less than 2^-63 counts as 2^-63; rows whose scores add up to
-// less than 2^-40 are worked out one by one.  So are all rows whose experts are chosen by score and bias: a score may not depend on its neighbour's logit there (equal
-// logits are ties, and a NaN stays where it is).
+// less than 2^-28 are worked out one by one (1024 such experts are 2^-25 of that).  So are all rows whose experts are chosen by score and bias: a score may not
+// depend on its neighbour's logit there (equal logits are ties, and a NaN stays where it is).
 template <int VPL, int SUB, bool SHARED>
 __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float *s, float &top, float &inv)
 {
@@ -169,7 +169,7 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
             rp_parts(both, sum, other);
             sum = sub_sum<SUB>(sum + other);
         }
-        const bool alone = !SHARED || A.bias || sum < 1.0e-12f;
+        const bool alone = !SHARED || A.bias || sum < 4.0e-9f;
         if (__any_sync(0xffffffffu, alone)) {
             float s1[VPL], sum1 = 0.0f;                      // (the warp's other tokens keep theirs)
 #pragma unroll

@@ -408,3 +408,15 @@ def test_tokens_with_tiny_scores_leave_those_beside_them_alone(E):
         x[1:] = -100.0
         got = rp.rp_route(x, 2, start, score="sigmoid", loss_coef=1.0)
         assert all((a == b).all() for a, b in zip(want, got)), seed
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("logit", [-22.0, -24.0, -26.0, -27.0, -40.0])
+def test_one_expert_left_with_a_small_score(logit, kind):
+    """All other experts taken out: its part of the scores is 1, so the loss of a token is coef E / k."""
+    import torch
+    x = torch.full((1, 1000), -math.inf)
+    x[0, 7] = logit
+    routes, gates, _, loss = rp.rp_route(x.to(getattr(torch, kind)).cuda(), 1, torch.tensor([0, 1], device="cuda"), score="sigmoid", loss_coef=1.0)
+    assert routes.item() == 7 and abs(gates.item() - 1) <= FLOAT and abs(loss.item() - 1000) <= FLOAT * 1000
