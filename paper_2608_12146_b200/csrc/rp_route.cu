@@ -132,6 +132,10 @@ __device__ __forceinline__ float min_or_nan(float x, float y)
     return z;
 }
 
+// Rounding top / ln 2 gives all scores of a softmax one factor, which their sum takes out again: 2^32 at most up to here.  Of larger numbers (a row of nothing but the
+// type's lowest value, which is what some masks write) the difference is taken first: two logits that differ do so by 32 and more there.
+__device__ __forceinline__ bool far_out(float top) { return fabsf(top) > 5.0e8f; }
+
 // Scores of one token from its logits: softmax: e^(x - max) and 1 / their sum; sigmoid: s, and 1 / their sum.
 // `top` is what the largest logit is taken for: 0 where it is -inf (all scores are 0 then, and so is the inverse).
 // SHARED: two sigmoids share a reciprocal, 1 / (1 + a) = (1 + b) / ((1 + a)(1 + b)), where a score of less than 2^-63 counts as 2^-63; rows whose scores add up to
@@ -148,9 +152,15 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
         for (int i = 1; i < VPL; ++i) m = fmaxf(m, x[i]);
         m = sub_max<SUB>(m);
         top = m == -INFINITY ? 0.0f : m;
-        const float shift = -top * RP_LOG2E;
+        if (far_out(top)) {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2(fmaf(x[i], RP_LOG2E, shift)); sum += s[i]; }
+            for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2((x[i] - top) * RP_LOG2E); sum += s[i]; }
+        } else {
+            const float shift = -top * RP_LOG2E;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2(fmaf(x[i], RP_LOG2E, shift)); sum += s[i]; }
+        }
+        __syncwarp();
         sum = sub_sum<SUB>(sum);
     } else {
         if (SHARED && !A.bias) {
@@ -187,7 +197,8 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
 // Score of one expert as the gates use it.
 __device__ __forceinline__ float score_of(const RouteArgs &A, float x, float top, float inv)
 {
-    return A.score == RP_SCORE_SOFTMAX ? rp_exp2(fmaf(x, RP_LOG2E, -top * RP_LOG2E)) * inv : sigmoid(x);
+    if (A.score != RP_SCORE_SOFTMAX) return sigmoid(x);
+    return rp_exp2(far_out(top) ? (x - top) * RP_LOG2E : fmaf(x, RP_LOG2E, -top * RP_LOG2E)) * inv;
 }
 
 // Floats as unsigned numbers in the same order; -0 as 0, NaN above all.

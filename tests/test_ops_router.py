@@ -420,3 +420,40 @@ def test_one_expert_left_with_a_small_score(logit, kind):
     x[0, 7] = logit
     routes, gates, _, loss = rp.rp_route(x.to(getattr(torch, kind)).cuda(), 1, torch.tensor([0, 1], device="cuda"), score="sigmoid", loss_coef=1.0)
     assert routes.item() == 7 and abs(gates.item() - 1) <= FLOAT and abs(loss.item() - 1000) <= FLOAT * 1000
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("E", [16, 100, 256])
+def test_rows_of_the_lowest_value_and_of_large_ones(E, kind):
+    """A row whose every logit is the type's lowest value has equal scores; large logits as any others."""
+    import torch
+    dtype = getattr(torch, kind)
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    x = logits_of(8, E, dtype, E)
+    x[0] = low
+    x[1] = high
+    x[2] = low
+    x[2, 3], x[2, 9] = 1.0, 1.0
+    x[3, 5] = high
+    x[4] = low
+    x[4, 7] = high
+    x[5] = min(1e30, high)
+    x[5, 1] = low
+    x[6] = -min(1e9, high)
+    start = [0, 1, 2, 3, 4, 5, 6, 7, 8]
+    want = reference(x, 2, start, coef=0.5)
+    st = torch.tensor(start, device="cuda")
+    routes, gates, counts, loss = rp.rp_route(x.cuda(), 2, st, loss_coef=0.5)
+    assert (routes.cpu().long() == want[0]).all() and (counts.cpu().double() == want[2]).all()
+    assert ((gates.cpu().double() - want[1]).abs() <= FLOAT * want[1]).all()
+    assert abs(loss.item() - want[3].item()) <= 2 * FLOAT * want[3].item()
+    x64 = x.double().requires_grad_(True)
+    p = torch.softmax(x64, 1)
+    dg = torch.tensor([[1.0, -2.0]]).expand(8, 2).contiguous()
+    g = p.gather(1, want[0])
+    value = (g / g.sum(1, keepdim=True) * dg.double()).sum() + 3.0 * 0.5 / 8 * E / 2 * sum((want[2][t] * p[t]).sum() for t in range(8))
+    grad = torch.autograd.grad(value, x64)[0]
+    got = rp.rp_route_grad(x.cuda(), routes, st, counts, gates_grad=dg.cuda(), loss_grad=torch.tensor([3.0], device="cuda"), loss_coef=0.5)
+    tol = torch.finfo(dtype).eps / 2 * grad.abs() + 4 * FLOAT * (2.0 * 2 + 3.0 * 0.5 / 8 * E / 2) + 1e-7 * (kind == "float16")
+    assert ((got.cpu().double() - grad).abs() <= tol).all()
