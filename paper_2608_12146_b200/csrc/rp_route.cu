@@ -201,6 +201,19 @@ __device__ __forceinline__ float score_of(const RouteArgs &A, float x, float top
     return rp_exp2(far_out(top) ? (x - top) * RP_LOG2E : fmaf(x, RP_LOG2E, -top * RP_LOG2E)) * inv;
 }
 
+// Shares of a token's choices in their sum, over the lanes that have them, from the logits alone: for sums under SHARES_FROM, where scores leave the numbers' range while
+// their shares do not.  (A sigmoid of less than that is e^x.)  No choice with a score: 0.
+#define SHARES_FROM 1.0e-30f
+__device__ __forceinline__ float shares(bool valid, float x, int k_lanes)
+{
+    float m = valid ? x : -INFINITY;
+    for (int o = 1; o < k_lanes; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float v = valid && m > -INFINITY ? rp_exp2((x - m) * RP_LOG2E) : 0.0f;
+    float total = v;
+    for (int o = 1; o < k_lanes; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    return total > 0.0f ? v * reciprocal(total) : 0.0f;
+}
+
 // Floats as unsigned numbers in the same order; -0 as 0, NaN above all.
 __device__ __forceinline__ u32 order_of(float x)
 {
@@ -445,7 +458,12 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route(Route
         if (A.normalise) {
             float total = v;
             for (int o = 1; o < k_lanes; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            gate = total < 1.2e-38f ? 0.0f : gate * reciprocal(total);
+            const bool tiny = valid && total < SHARES_FROM;
+            gate = total < SHARES_FROM ? 0.0f : gate * reciprocal(total);
+            if (__any_sync(0xffffffffu, tiny)) {
+                const float y = shares(valid, xe, k_lanes);
+                if (tiny) gate = y * A.scale;
+            }
         }
         if (there && step >= next) {
             // another group: what the run has of the one before goes out
@@ -583,8 +601,15 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route_grad(
             float z = v, za = valid ? v * a : 0.0f;
             for (int o = 1; o < k_lanes; o <<= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); za += __shfl_xor_sync(0xffffffffu, za, o); }
             // (lanes behind the choices have their own sums: what all lanes need is the first's)
-            const float zi = z < 1.2e-38f ? 0.0f : reciprocal(z);
-            add = (A.normalise ? (a - za * zi) * zi : a) * (soft ? v : v * (1.0f - v));
+            const float zi = z < SHARES_FROM ? 0.0f : reciprocal(z), ds = soft ? v : v * (1.0f - v);
+            add = A.normalise ? (a - za * zi) * (zi * ds) : a * ds;       // (zi may be large: the score is multiplied with it first)
+            const bool tiny = A.normalise && valid && z < SHARES_FROM;
+            if (__any_sync(0xffffffffu, tiny)) {
+                const float y = shares(valid, xe, k_lanes);
+                float ya = valid ? y * a : 0.0f;
+                for (int o = 1; o < k_lanes; o <<= 1) ya += __shfl_xor_sync(0xffffffffu, ya, o);
+                if (tiny) add = (a - ya) * y;
+            }
             if (soft && !A.normalise) pb += __shfl_sync(0xffffffffu, za, first_lane);
         }
 #pragma unroll

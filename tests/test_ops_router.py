@@ -457,3 +457,25 @@ def test_rows_of_the_lowest_value_and_of_large_ones(E, kind):
     got = rp.rp_route_grad(x.cuda(), routes, st, counts, gates_grad=dg.cuda(), loss_grad=torch.tensor([3.0], device="cuda"), loss_coef=0.5)
     tol = torch.finfo(dtype).eps / 2 * grad.abs() + 4 * FLOAT * (2.0 * 2 + 3.0 * 0.5 / 8 * E / 2) + 1e-7 * (kind == "float16")
     assert ((got.cpu().double() - grad).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_gradient_of_gates_whose_scores_are_tiny(score):
+    """Replayed experts that this pass gives next to nothing: their gates are shares of it, and so are the gradients."""
+    import torch
+    x = torch.zeros(4, 32)
+    x[:, 4], x[:, 9], x[:, 30] = -86.0, -86.5, -85.0
+    if score == "sigmoid":
+        x[:, :] -= 0.5
+    ids = torch.tensor([[4, 9, 30]]).expand(4, 3).contiguous()
+    start = torch.tensor([0, 4], device="cuda")
+    _, gates, counts, _ = rp.rp_route(x.cuda(), 3, start, score=score, replay=ids.cuda())
+    dg = torch.tensor([[100.0, -300.0, 7.0], [1.0, 2.0, 3.0], [1e4, 0.0, 0.0], [0.0, 0.0, 1e-3]])
+    x64 = x.double().requires_grad_(True)
+    want_gates = reference(x64, 3, [0, 4], score, replay=ids)[1]
+    want = torch.autograd.grad((want_gates * dg.double()).sum(), x64)[0]
+    assert ((gates.cpu().double() - want_gates).abs() <= 16 * FLOAT * want_gates).all()
+    got = rp.rp_route_grad(x.cuda(), ids.cuda(), start, counts, gates_grad=dg.cuda(), score=score)
+    # (logits to 87: ex2's argument to 125 is off by 2^-18, so a score by 6e-6)
+    assert ((got.cpu().double() - want).abs() <= 16 * FLOAT * dg.abs().amax(1, keepdim=True).double()).all()
