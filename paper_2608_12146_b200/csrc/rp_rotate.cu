@@ -203,16 +203,21 @@ template <typename X, bool INTERLEAVED> __device__ __forceinline__ void close_pa
     }
     p = rp_close8<X>(x); q = rp_close8<X>(y);
 }
-// Turns pairs, or turns them back.
-template <bool BACK> __device__ __forceinline__ void turn(f2 *a, f2 *b, const f2 *c, const f2 *s)
+// Turns pairs, or turns them back: the lane's first two of each piece where that piece is turned at all (0 times what an element behind rotary_dim holds may be NaN).
+template <bool BACK> __device__ __forceinline__ void turn_piece(f2 *a, f2 *b, const f2 *c, const f2 *s)
 {
     const f2 minus = rp_f2(-1.0f, -1.0f);
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
+    for (int p = 0; p < 2; ++p) {
         const f2 x = a[p], n = rp_mul(s[p], minus);
         a[p] = rp_fma(x, c[p], rp_mul(b[p], BACK ? s[p] : n));
         b[p] = rp_fma(b[p], c[p], rp_mul(x, BACK ? n : s[p]));
     }
+}
+template <bool BACK> __device__ __forceinline__ void turn(f2 *a, f2 *b, const f2 *c, const f2 *s, bool first, bool second)
+{
+    if (first) turn_piece<BACK>(a, b, c, s);
+    if (second) turn_piece<BACK>(a + 2, b + 2, c + 2, s + 2);
 }
 // Sum over the lanes of a head.
 template <int TPH> __device__ __forceinline__ float head_sum(f2 v)
@@ -239,6 +244,7 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
     const int turned = A.r / 16;                         // half layout: pieces of a half
     const int pa = INTERLEAVED ? 16 * j : j < turned ? 8 * j : A.r + 16 * (j - turned);          // first elements of the lane's pieces
     const int pb = INTERLEAVED || j >= turned ? pa + 8 : pa + A.r / 2;
+    const bool turns_a = INTERLEAVED ? 16 * j < A.r : j < turned, turns_b = INTERLEAVED ? 16 * j + 8 < A.r : j < turned;
     if (GRAD && A.part)
         for (int i = lane; i < 2 * A.d; i += 32) dw[i] = 0.0f;
     if (warp < 2 && group == 0) {
@@ -326,11 +332,11 @@ __global__ void __launch_bounds__(ROT_THREADS, ROT_CTAS(GRAD)) k_rotate_rows(Rot
                             if (norm)
 #pragma unroll
                                 for (int p = 0; p < 4; ++p) { a[p] = rp_mul(a[p], rp_mul(r, w[p * TPH])); b[p] = rp_mul(b[p], rp_mul(r, w[(p + 4) * TPH])); }
-                            turn<false>(a, b, c, s);
+                            turn<false>(a, b, c, s, turns_a, turns_b);
                         } else {
                             f2 g2[4], h2[4];
                             open_pairs<X, INTERLEAVED>(ga[u], gb[u], g2, h2);
-                            turn<true>(g2, h2, c, s);
+                            turn<true>(g2, h2, c, s, turns_a, turns_b);
                             if (norm) {
                                 f2 dot2 = rp_f2(0.0f, 0.0f);
 #pragma unroll

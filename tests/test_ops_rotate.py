@@ -302,3 +302,27 @@ def test_heads_and_tokens_that_repeat(d):
             assert (a == b).all()
         one, two = rp.rp_rotate_grad(dy, None, q, None, inv, st, q_weight=w), rp.rp_rotate_grad(dy.contiguous(), None, q.contiguous(), None, inv, st, q_weight=w)
         assert (one[0] == two[0]).all() and (one[2] == two[2]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("d,r", [(128, 64), (64, 16), (64, 24), (256, 64), (80, 40), (32, 0), (96, 90)])
+def test_elements_that_are_not_turned_are_handed_on_alone(d, r, kind, layout):
+    """What stands behind rotary_dim, infinities and NaN too, comes out as it is and reaches no other element."""
+    import torch
+    T = 50
+    q, _, inv, _, g = inputs((T, 3, 0, d, r, [0, 20, 45], None), kind)
+    q = q.contiguous()
+    start, inv = torch.tensor([0, 20, 45], device="cuda"), inv.cuda() if r else None
+    clean, dirty = rp.rp_rotate(q, None, inv, start, layout=layout)[0], q.clone()
+    places = sorted({r, r + 1, d - 1})
+    for i, e in enumerate(places):
+        dirty[::2, :2, e] = (math.inf, math.nan, -math.inf)[i % 3]
+    y = rp.rp_rotate(dirty, None, inv, start, layout=layout)[0]
+    dx = rp.rp_rotate_grad(dirty, None, q, None, inv, start, layout=layout)[0]
+    back = rp.rp_rotate_grad(q, None, q, None, inv, start, layout=layout)[0]
+    rest = [e for e in range(d) if e not in places]
+    assert (y[..., rest] == clean[..., rest]).all() and (dx[..., rest] == back[..., rest]).all()
+    for got in (y, dx):
+        assert torch.equal(got[:45, :, places].nan_to_num(7.0), dirty[:45, :, places].nan_to_num(7.0)) and (got[45:] == 0).all()
