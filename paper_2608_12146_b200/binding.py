@@ -570,7 +570,7 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
             else:
                 gt, gh = _head_strides(g, x, "gradient")
                 if w is not None:
-                    dws[i] = x.new_empty(d, dtype=torch.float32)
+                    dws[i] = (x.new_empty if x.shape[1] else x.new_zeros)(d, dtype=torch.float32)        # (without heads nothing is written)
                 side = rp_heads(x.shape[1], x.data_ptr(), xt, xh, out.data_ptr(), yt, yh, _dense(w, w_type, (d,), "weight"), g.data_ptr(), gt, gh,
                                 None if w is None else dws[i].data_ptr())
             sides[i] = C.byref(side)

@@ -326,3 +326,15 @@ def test_elements_that_are_not_turned_are_handed_on_alone(d, r, kind, layout):
     assert (y[..., rest] == clean[..., rest]).all() and (dx[..., rest] == back[..., rest]).all()
     for got in (y, dx):
         assert torch.equal(got[:45, :, places].nan_to_num(7.0), dirty[:45, :, places].nan_to_num(7.0)) and (got[45:] == 0).all()
+
+
+@pytest.mark.gpu
+def test_weights_of_no_heads_have_a_gradient_of_zero():
+    import torch
+    q, k, inv, _, g = inputs((20, 0, 2, 64, 64, [0, 20], None), "float32")
+    start, w = torch.tensor([0, 20], device="cuda"), torch.ones(64, device="cuda")
+    junk = [torch.full((64,), math.nan, device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    del junk                                             # (what the allocator hands out next)
+    dq, dk, dwq, dwk = rp.rp_rotate_grad(q, k, q, k, inv.cuda(), start, q_weight=w, k_weight=w)
+    assert dq.shape == (20, 0, 64) and (dwq == 0).all() and torch.isfinite(dwk).all() and (dwk != 0).any()
