@@ -205,12 +205,13 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 float top = __uint_as_float(s[0]);
 #pragma unroll
                 for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(s[c]));
-                if (j == 0) m = top == -INFINITY ? 0.0f : top;
+                if (j == 0) m = top;
                 else {
-                    // (a maximum that grows by less than 2^8 stays: weights up to 256 and their sums lose nothing)
+                    // (a maximum that grows by less than 2^8 stays: weights up to 256 and their sums lose nothing; -inf, as long as no score is above it, goes with the
+                    // first that is)
                     const float grown = (top - m) * sl;
                     if (__any_sync(0xffffffffu, grown > 8.0f)) {
-                        const float up = fmaxf(top, m), f = rp_exp2((m - up) * sl);
+                        const float up = fmaxf(top, m), f = m == up ? 1.0f : rp_exp2((m - up) * sl);
                         m = up;
                         l *= f;
 #pragma unroll
@@ -224,7 +225,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         }
                     }
                 }
-                const f2 shift = rp_f2(-m * sl, -m * sl);
+                const float less = m == -INFINITY ? 0.0f : -m * sl;
+                const f2 shift = rp_f2(less, less);
                 f2 sum0 = rp_f2(0.0f, 0.0f), sum1 = sum0;
 #pragma unroll
                 for (int c = 0; c < 64; ++c) {

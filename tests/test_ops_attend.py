@@ -343,3 +343,28 @@ def test_refusals_of_the_gradient():
         return lib.rp_attend_grad(C.byref(cfg), 2, q, k, v, o, lse, g, p, 1, dq, dk, dv, space, nbytes, None)
     assert call() == -1 and all(call(at=i) == -1 for i in range(8)) and call(lse=None) == -1 and call(nbytes=16) == -1 and call(space=None) == -1
     assert lib.rp_attend_grad_workspace(None, 1, 1) == 0 and lib.rp_attend_grad_workspace(C.byref(cfg), 100, 1) >= 100 * 2 * 8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+@pytest.mark.parametrize("d,n", [(64, 128), (128, 128), (128, 300), (64, 512)])
+def test_keys_at_minus_infinity_before_low_scores(d, n, kind, causal):
+    """The first n keys give scores of -inf, those behind them scores around -200: rows that see any of those have an ordinary softmax."""
+    import torch
+    T, scale = n + 200, 0.5
+    q, k, v, _ = inputs((T, 2, 1, d, [0, T]), kind)
+    q, k = q.clone(), k.clone()
+    q[..., 0], q[..., 1] = 1.0, 20.0
+    k[:n, :, 0], k[n:, :, 0], k[:, :, 1] = -math.inf, 0.0, -20.0
+    out, lse = rp.rp_attend(q, k, v, torch.tensor([0, T], device="cuda"), causal=causal, scale=scale)
+    half = torch.finfo(q.dtype).eps / 2
+    rows = slice(n, T) if causal else slice(0, T)
+    for h in range(2):
+        p, w_lse = weights(q[:, h].double(), k[:, 0].double(), scale, causal)
+        want, size = (p @ v[:, 0].double())[rows], (p @ v[:, 0].double().abs())[rows]
+        # (scores to 250: 32 bits leave them 2e-5, so 3e-5 of a weight)
+        assert ((out[rows, h].double() - want).abs() <= half * (size + want.abs()) + 6e-5 * size + 1e-7).all()
+        assert ((lse[rows, h].double() - w_lse[rows]).abs() <= 4e-6 * (1 + w_lse[rows].abs())).all()
+    if causal:
+        assert (lse[:n] == -math.inf).all()
