@@ -208,8 +208,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 if (j == 0) m = top;
                 else {
                     // (a maximum that grows by less than 2^8 stays: weights up to 256 and their sums lose nothing; -inf, as long as no score is above it, goes with the
-                    // first that is)
-                    const float grown = (top - m) * sl;
+                    // first that is; rows behind the sample's end are other samples', which do not matter)
+                    const float grown = r < t.len ? (top - m) * sl : 0.0f;
                     if (__any_sync(0xffffffffu, grown > 8.0f)) {
                         const float up = fmaxf(top, m), f = m == up ? 1.0f : rp_exp2((m - up) * sl);
                         m = up;

@@ -368,3 +368,19 @@ def test_keys_at_minus_infinity_before_low_scores(d, n, kind, causal):
         assert ((lse[rows, h].double() - w_lse[rows]).abs() <= 4e-6 * (1 + w_lse[rows].abs())).all()
     if causal:
         assert (lse[:n] == -math.inf).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n", [130, 140, 400])
+def test_large_scores_of_the_next_sample_change_no_bit(n, causal):
+    """Queries behind a sample's end, in the tile of its last ones, whose scores with its later keys are far above those with its first."""
+    import torch
+    q, k, v, _ = inputs((n + 100, 16, 16, 64, [0, n]), "bfloat16")
+    k = k.clone()
+    k[128:n] *= 1.7
+    want = rp.rp_attend(q[:n], k[:n], v[:n], torch.tensor([0, n], device="cuda"), causal=causal)
+    q = q.clone()
+    q[n:] = 40 * k[n - 1]
+    got = rp.rp_attend(q, k, v, torch.tensor([0, n, n + 100], device="cuda"), causal=causal)
+    assert (got[0][:n] == want[0]).all() and (got[1][:n] == want[1]).all()
