@@ -384,3 +384,27 @@ def test_large_scores_of_the_next_sample_change_no_bit(n, causal):
     q[n:] = 40 * k[n - 1]
     got = rp.rp_attend(q, k, v, torch.tensor([0, n, n + 100], device="cuda"), causal=causal)
     assert (got[0][:n] == want[0]).all() and (got[1][:n] == want[1]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+@pytest.mark.parametrize("under", [10.0, 17.0, 17.5, 20.0])
+def test_many_small_weights_beside_a_large_one(under, kind):
+    """131072 keys whose scores are far under that of one: what they add up to is not lost."""
+    import torch
+    T = 131073
+    q, k, v = [torch.zeros(T, 1, 64, dtype=getattr(torch, kind), device="cuda") for _ in range(3)]
+    q[:, 0, 0], k[1:, 0, 0] = 1.0, -under
+    v[1:, 0, :], v[0, 0, 1] = 1.0, 1.0
+    out, lse = rp.rp_attend(q, k, v, torch.tensor([0, T], device="cuda"), causal=True, scale=1.0)
+    part = (T - 1) * math.exp(-under)
+    want = part / (1 + part)
+    half = torch.finfo(q.dtype).eps / 2
+    # (weights and output rounded once; float16 weights under its normal range off by half a step, 2^-25, of 2^7 times their size; T / 16 additions to a sum of 32 bits that grows by
+    # numbers of one sign, which the tensor cores cut off: 2^-23 of it each at most)
+    off = 2 * half + 1e-5 + T / 16 * 2.0 ** -23
+    assert abs(out[-1, 0, 0].item() - want) <= off * want + (T - 1) * 2.0 ** -32 * (kind == "float16")
+    # (where the sum has the large weight from the start, each product is cut off at 2^-23 of it before they are added: T of them)
+    assert abs(out[-1, 0, 1].item() - 1) <= off + T * 2.0 ** -23
+    # (a sum in 32 bits that takes T / 128 more numbers, each time to 2^-24 of itself)
+    assert abs(lse[-1, 0].item() - math.log1p(part)) <= 4e-6 * (1 + math.log1p(part)) + (T / 128 + 1) * 2.0 ** -24
