@@ -44,7 +44,7 @@ typedef enum {
     RP_ERR_RANGE = -5,         /* fixed-point range or on-chip memory budget exceeded       */
     RP_ERR_CUDA = -6,          /* a CUDA call failed; see rp_last_cuda_error()              */
     RP_ERR_STATE = -7,         /* call out of order                                         */
-    RP_ERR_TIMEOUT = -8,       /* rp_anneal: a bounded device-side wait ran out (see there) */
+    RP_ERR_TIMEOUT = -8,       /* rp_anneal, rp_attend: a bounded device-side wait ran out (see there) */
     RP_ERR_INVALID_PLAN = -9   /* rp_best: the incumbent failed validation                  */
 } rp_status;
 
@@ -460,6 +460,9 @@ typedef enum { RP_KNOB_BARRIER_WORKSPACE = 1, RP_KNOB_WAIT_POLLS = 2, RP_KNOB_ST
                RP_KNOB_RANK_LOAD_SLICES = 4, RP_KNOB_LAUNCH_PER_LEVEL = 5, RP_KNOB_CHAIN_KERNEL = 6,
                RP_KNOB_RESIDENT_SMS = 7 } rp_knob;
 int rp_debug_set_knob(rp_ctx *ctx, int knob, int64_t value);
+/* Limit of the waits inside the attention kernels (process-wide, calls from then on): 2000000000 by default.  With 0 they wait for nothing and give up at once, as if a
+ * wait had run out: outputs NaN, RP_ERR_TIMEOUT in the workspace. */
+int rp_debug_set_wait_limit(int64_t nanoseconds);
 /* Device time of the stages that have no statistics struct of their own.  After
  * rp_debug_set_stage_timing(1) (process-wide; contexts loaded later record CUDA events around the
  * kernels, a few microseconds of host time per call), rp_debug_stage_times synchronises the

@@ -30,7 +30,7 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_debug_chain_kernel", "rp_debug_chain_form",
            "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad",
            "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad", "rp_attend_workspace", "rp_attend",
-           "rp_attend_grad_workspace", "rp_attend_grad")
+           "rp_attend_grad_workspace", "rp_attend_grad", "rp_debug_set_wait_limit")
 
 
 class RpError(RuntimeError):
@@ -132,6 +132,7 @@ def lib():
         L.rp_debug_l2_read_rate.argtypes = [C.c_int64, C.c_int32, C.POINTER(C.c_double)]
         L.rp_debug_chain_kernel.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
         L.rp_debug_chain_form.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
+        L.rp_debug_set_wait_limit.argtypes = [C.c_int64]
         V, I, Q = C.c_void_p, C.c_int32, C.c_int64
         L.rp_count_routes.argtypes = [V, I, Q, I, I, I, Q, Q, V, I, V, V]
         L.rp_window_load_routes.argtypes = [C.POINTER(C.c_void_p), C.POINTER(rp_config), V, V, I, Q, Q, Q, V]
@@ -635,14 +636,22 @@ def _attend_args(torch, q, k, v, start, causal, scale):
     return _attention(q.shape[1], k.shape[1], q.shape[2], _kind(q, "q"), causal, scale)[1], at, n
 
 
-def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = None, out=None, lse=None, stream=None):
+def _hand_out(status, space, T, torch):
+    """What the kernels leave at the front of their workspace goes into a tensor of the caller's."""
+    if status is not None:
+        status.copy_(space[:4].view(torch.int32)) if T else status.zero_()
+
+
+def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = None, out=None, lse=None, status=None, stream=None):
     """Attention inside the samples of a packed row: (out [n_tokens, q_heads, head_dim], lse [n_tokens, q_heads] float32).
 
     ``q`` [n_tokens, q_heads, head_dim], ``k`` and ``v`` [n_tokens, kv_heads, head_dim] of float16 or bfloat16; ``scale`` is head_dim ** -0.5 by default.
+    ``status``: [1] int32 on the GPU, receives 0, or -8 (RP_ERR_TIMEOUT) where a wait inside the kernel ran out (outputs that were not worked out are NaN then).
     """
     torch = _torch()
     ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
     T, H, _ = q.shape
+    _dense(status, torch.int32, (1,), "status")
     with _Queue(torch, q, stream) as queue:
         if out is None:
             out = q.new_empty(q.shape)
@@ -653,15 +662,17 @@ def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = N
         if T:
             _check(lib().rp_attend(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _view(out, q, "out"), _lse_view(lse, T, H, torch),
                                    space.data_ptr(), nbytes, queue.handle), "rp_attend")
+        _hand_out(status, space, T, torch)
     return out, lse
 
 
 def rp_attend_grad(out_grad, q, k, v, out, lse, start, *, causal: bool = True, scale: Optional[float] = None, q_grad=None, k_grad=None, v_grad=None,
-                   stream=None):
-    """Gradients (q_grad, k_grad, v_grad) of rp_attend from that of its output, its inputs, ``out`` and ``lse``."""
+                   status=None, stream=None):
+    """Gradients (q_grad, k_grad, v_grad) of rp_attend from that of its output, its inputs, ``out`` and ``lse``; ``status`` as there."""
     torch = _torch()
     ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
     T, H, _ = q.shape
+    _dense(status, torch.int32, (1,), "status")
     with _Queue(torch, q, stream) as queue:
         q_grad = q.new_empty(q.shape) if q_grad is None else q_grad
         k_grad = k.new_empty(k.shape) if k_grad is None else k_grad
@@ -672,6 +683,7 @@ def rp_attend_grad(out_grad, q, k, v, out, lse, start, *, causal: bool = True, s
             _check(lib().rp_attend_grad(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), _view(out, q, "out"), _lse_view(lse, T, H, torch),
                                         _view(out_grad, q, "out_grad"), at, n, _view(q_grad, q, "q_grad"), _view(k_grad, k, "k_grad"),
                                         _view(v_grad, v, "v_grad"), space.data_ptr(), nbytes, queue.handle), "rp_attend_grad")
+        _hand_out(status, space, T, torch)
     return q_grad, k_grad, v_grad
 
 
@@ -705,6 +717,11 @@ KNOB = dict(BARRIER_WORKSPACE=1, WAIT_POLLS=2, STALL_ONE_CHAIN=3, RANK_LOAD_SLIC
 
 def rp_debug_set_knob(ctx: Context, knob: str, value: int):
     _check(lib().rp_debug_set_knob(ctx.handle, KNOB[knob], int(value)), f"rp_debug_set_knob({knob})")
+
+
+def rp_debug_set_wait_limit(nanoseconds: int = 2_000_000_000):
+    """Limit of the waits inside the attention kernels; 0: they give up at once."""
+    _check(lib().rp_debug_set_wait_limit(int(nanoseconds)), "rp_debug_set_wait_limit")
 
 
 def rp_debug_dump(ctx: Context, what: str, shape, dtype, index: int = 0) -> np.ndarray:

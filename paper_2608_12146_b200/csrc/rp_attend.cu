@@ -38,6 +38,7 @@ struct AttendArgs {
     float *lse;
     i64 l_token, l_head;
     int *status;
+    u64 wait_ns;
 };
 
 // A stage holds the values of one tile and the keys of the next, which are waited for and let go of together: of nk tiles there are nk + 1 stages, the first without
@@ -49,7 +50,7 @@ template <int D> struct FwdSmem {
     alignas(1024) unsigned char k[STAGES][TILE];
     u64 q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_full[2], o_full[2], done;
     u32 tmem;
-    volatile int gave_up;
+    Waits waits;
 };
 
 template <typename X, int D>
@@ -69,7 +70,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.kv_full[s]), 1); bar_init(rp_smem(&sm.kv_empty[s]), 1); }
         for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.p_full[i]), 4); bar_init(rp_smem(&sm.o_full[i]), 1); }
         bar_init(rp_smem(&sm.done), 1);
-        sm.gave_up = 0;
+        sm.waits.start(A.wait_ns);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == ATTEND_COPY_WARP) tmem_alloc(rp_smem(&sm.tmem), 512);
@@ -79,21 +80,21 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     const u32 tm = rp_uniform(sm.tmem);
     rp_wait_for_launch_before();             // the list of blocks: nothing of it before this line
     const int total = rp_uniform(A.head->count * A.Hq);
-    volatile int *gave_up = &sm.gave_up;
+    Waits *const waits = &sm.waits;
 
     if (warp >= 8) {
         rp_few_registers();
         if (warp == ATTEND_COPY_WARP && lane == 0) {
             tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v);
-            int n = 0;
-            u32 fill = 0;                               // copies into the ring so far
+            u32 blocks = 0, fill = 0;                   // copies of queries and into the ring so far
             bool ok = true;
-            for (int round = 0; ok; ++round, ++n) {
+            for (int round = 0; ok; ++round) {
                 const int at = rp_attend_item(round, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
                 const int h = at % A.Hq, hk = h / A.share;
-                if (n && !(ok = bar_wait(rp_smem(&sm.q_empty), (n - 1) & 1, gave_up))) break;
+                if (!(ok = bar_place(round, rp_smem(&sm.q_empty), (round - 1) & 1, waits))) break;
+                ++blocks;
                 const int tiles = t.row0 + 128 < t.len ? 2 : 1;
                 bar_expect(rp_smem(&sm.q_full), tiles * Smem::TILE);
                 for (int i = 0; i < tiles; ++i)
@@ -102,7 +103,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 const int nk = rp_attend_tiles(t, tiles - 1, A.causal);
                 for (int j = 0; j <= nk; ++j, ++fill) {
                     const u32 s = fill % STAGES, turn = fill / STAGES;
-                    if (turn && !(ok = bar_wait(rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, gave_up))) break;
+                    if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), j && j < nk ? 2 * Smem::TILE : Smem::TILE);
                     for (int p = 0; p < PANELS; ++p) {
                         if (j) tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + (j - 1) * 128, rp_smem(&sm.kv_full[s]));
@@ -110,12 +111,9 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     }
                 }
             }
-            if (!ok) {
-                // nobody may leave while copies are under way
-                for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1);
-                if (n) rp_drain(rp_smem(&sm.q_full), (n - 1) & 1);
-                rp_drain(rp_smem(&sm.q_full), n & 1);
-            }
+            // nobody may leave while copies are under way (whoever should have waited for them may have given up)
+            for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1);
+            if (blocks) rp_drain(rp_smem(&sm.q_full), (blocks - 1) & 1);
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
@@ -137,12 +135,12 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             };
             for (int round = 0;; ++round) {
                 const int at = rp_attend_item(round, total);
-                if (at < 0) break;
+                if (at < 0 || rp_uniform(waits->gave_up)) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
                 const int left = rp_uniform(t.len - t.row0), tiles = left > 128 ? 2 : 1, len = rp_uniform(t.len);
                 const int n0 = rp_uniform(rp_attend_tiles(t, 0, A.causal)), n1 = tiles == 2 ? rp_uniform(rp_attend_tiles(t, 1, A.causal)) : 0, nk = max(n0, n1);
-                bar_hold(rp_smem(&sm.q_full), round & 1, gave_up);
-                bar_hold(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, gave_up);
+                bar_hold(rp_smem(&sm.q_full), round & 1, waits);
+                bar_hold(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, waits);
                 scores(0, used % STAGES);
                 if (tiles == 2) scores(1, used % STAGES);
                 mma_commit(one, rp_smem(&sm.kv_empty[used % STAGES]));
@@ -151,18 +149,18 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 for (int j = 0; j < nk; ++j, ++used) {
                     const u32 s = used % STAGES;
                     // (what is copied has mostly come when the weights have)
-                    bar_hold(rp_smem(&sm.kv_full[s]), (used / STAGES) & 1, gave_up);
+                    bar_hold(rp_smem(&sm.kv_full[s]), (used / STAGES) & 1, waits);
                     // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
                     if (len - j * 128 < 128) rp_clear_rows<D>(sm.v[s], len - j * 128, 128, lane);
                     if (j < n0) {
-                        bar_hold(rp_smem(&sm.p_full[0]), p0++ & 1, gave_up);
+                        bar_hold(rp_smem(&sm.p_full[0]), p0++ & 1, waits);
                         tmem_after();
                         outputs(0, s, j > 0);
                         if (j == n0 - 1) mma_commit(one, rp_smem(&sm.o_full[0]));
                         else scores(0, s);
                     }
                     if (j < n1) {
-                        bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, gave_up);
+                        bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, waits);
                         tmem_after();
                         outputs(1, s, j > 0);
                         if (j == n1 - 1) mma_commit(one, rp_smem(&sm.o_full[1]));
@@ -193,7 +191,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             float m = -INFINITY, l = 0.0f;
             bool ok = true;
             for (int j = 0; j < nk; ++j) {
-                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[i]), ss & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[i]), ss & 1, waits))) break;
                 ++ss;
                 tmem_after();
                 u32 s[128];
@@ -248,7 +246,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 tmem_before();
                 bar_arrive_warp(rp_smem(&sm.p_full[i]), lane);
             }
-            if (ok) ok = bar_wait_warp(rp_smem(&sm.o_full[i]), os & 1, gave_up) && !*gave_up;
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.o_full[i]), os & 1, waits) && !waits->gave_up;
             ++os;
             tmem_after();
             const float f = ok ? 1.0f / l : NAN;
@@ -273,7 +271,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
     }
     __syncwarp();
     __syncthreads();
-    if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
+    if (threadIdx.x == 0 && sm.waits.gave_up) *A.status = RP_ERR_TIMEOUT;
     if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);
 }
 
@@ -317,6 +315,13 @@ int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev)
     if (!v || !v->x || !rp_aligned(v->x, 16)) return RP_ERR_ARG;
     if ((T > 1 && (v->token < 1 || v->token % 8 || v->token >= (1ll << 39))) || (heads > 1 && (v->head < 1 || v->head % 8 || v->head >= (1ll << 39)))) return RP_ERR_ARG;
     return dev.hold(v->x);
+}
+i64 g_attend_wait_ns = 2000000000;
+extern "C" int rp_debug_set_wait_limit(int64_t nanoseconds)
+{
+    if (nanoseconds < 0) return RP_ERR_ARG;
+    g_attend_wait_ns = nanoseconds;
+    return RP_OK;
 }
 static i64 plan_bytes(i64 T, int N, int rows) { return (i64)sizeof(AttendHead) + 8 * (T / rows + N); }
 
@@ -382,7 +387,7 @@ extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_v
     A.head = head; A.items = items; A.start = (const i64 *)start; A.T = n_tokens; A.N = n_samples; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads;
     A.d = a->head_dim; A.causal = a->causal; A.scale = a->scale; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
     if (lse && lse->x) { A.lse = (float *)lse->x; A.l_token = lse->token; A.l_head = lse->head; }
-    A.status = &head->status;
+    A.status = &head->status; A.wait_ns = (u64)g_attend_wait_ns;
     const int ctas = (int)std::min((i64)rp_op_sms(dev.device), (i64)P.most * a->q_heads);
     if (a->type == RP_F16) return a->head_dim <= 64 ? launch<__half, 64>(mq, mk, mv, A, ctas, stream) : launch<__half, 128>(mq, mk, mv, A, ctas, stream);
     return a->head_dim <= 64 ? launch<bf16, 64>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128>(mq, mk, mv, A, ctas, stream);

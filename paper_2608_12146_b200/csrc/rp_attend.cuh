@@ -86,6 +86,7 @@ static __device__ __noinline__ void rp_attend_clear(const AttendClears &A, const
         }
     }
 }
+extern i64 g_attend_wait_ns;             // limit of the kernels' waits (rp_debug_set_wait_limit)
 int rp_attend_check(const rp_attend_config *a, i64 T, int N);
 int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev);
 // Is one of the first `n_out` views the same memory as another of them or as one of the `n` behind them?

@@ -20,6 +20,7 @@ struct GradArgs {
     void *x[2];                              // dv, dk, or dq
     i64 token[2], hd[2];
     int *status;
+    u64 wait_ns;
     const void *rows[2];                     // queries' kernel: q, do
     i64 r_token[2], r_head[2];
 };
@@ -109,7 +110,7 @@ template <int D> struct KeySmem {
     alignas(16) float stats[2][2][2][64];    // [turn][group][lse / ln 2, delta][column]
     u64 kv_full, kv_empty, q_full[STAGES], q_empty[STAGES], s_full, dp_full, p_full, ds_full, st_full[2], acc_full, acc_empty, done;
     u32 tmem;
-    volatile int gave_up;
+    Waits waits;
 };
 
 template <typename X, int D>
@@ -128,7 +129,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.dp_full), 1); bar_init(rp_smem(&sm.p_full), 8); bar_init(rp_smem(&sm.ds_full), 8);
         for (int i = 0; i < 2; ++i) bar_init(rp_smem(&sm.st_full[i]), 4);
         bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.acc_empty), 8); bar_init(rp_smem(&sm.done), 1);
-        sm.gave_up = 0;
+        sm.waits.start(A.wait_ns);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     rp_let_next_launch_start();              // the queries' kernel takes the SMs that run out of work here
@@ -138,21 +139,21 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     tmem_after();
     const u32 tm = rp_uniform(sm.tmem);
     const int total = rp_uniform(A.head->count * A.Hk);
-    volatile int *gave_up = &sm.gave_up;
+    Waits *const waits = &sm.waits;
 
     if (warp >= 8) {
         rp_few_registers();
         if (warp == ATTEND_COPY_WARP && lane == 0) {
             tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v); tma_prefetch(&map_g);
-            int n = 0;
-            u32 fill = 0;
+            u32 blocks = 0, fill = 0;                   // copies of keys and values and into the ring so far
             bool ok = true;
-            for (; ok; ++n) {
+            for (int n = 0; ok; ++n) {
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
                 const int hk = at % A.Hk, first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first;
-                if (n && !(ok = bar_wait(rp_smem(&sm.kv_empty), (n - 1) & 1, gave_up))) break;
+                if (!(ok = bar_place(n, rp_smem(&sm.kv_empty), (n - 1) & 1, waits))) break;
+                ++blocks;
                 bar_expect(rp_smem(&sm.kv_full), 2 * Smem::TILE);
                 for (int p = 0; p < PANELS; ++p) {
                     tma_load3(rp_smem(sm.k) + p * PANEL, &map_k, p * 64, hk, (int)t.base + t.row0, rp_smem(&sm.kv_full));
@@ -161,7 +162,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 for (int h = hk * A.share; ok && h < (hk + 1) * A.share; ++h)
                     for (int j = 0; j < per; ++j, ++fill) {
                         const u32 s = fill % STAGES, turn = fill / STAGES;
-                        if (turn && !(ok = bar_wait(rp_smem(&sm.q_empty[s]), (turn - 1) & 1, gave_up))) break;
+                        if (!(ok = bar_place(turn, rp_smem(&sm.q_empty[s]), (turn - 1) & 1, waits))) break;
                         bar_expect(rp_smem(&sm.q_full[s]), 2 * Smem::TILE);
                         for (int p = 0; p < PANELS; ++p) {
                             tma_load3(rp_smem(sm.q[s]) + p * PANEL, &map_q, p * 64, h, (int)t.base + (first + j) * 128, rp_smem(&sm.q_full[s]));
@@ -169,12 +170,9 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                         }
                     }
             }
-            if (!ok) {
-                // nobody may leave while copies are under way
-                for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.q_full[f % STAGES]), (f / STAGES) & 1);
-                if (n) rp_drain(rp_smem(&sm.kv_full), (n - 1) & 1);
-                rp_drain(rp_smem(&sm.kv_full), n & 1);
-            }
+            // nobody may leave while copies are under way (whoever should have waited for them may have given up)
+            for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.q_full[f % STAGES]), (f / STAGES) & 1);
+            if (blocks) rp_drain(rp_smem(&sm.kv_full), (blocks - 1) & 1);
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
@@ -182,7 +180,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             u32 base = 0;                               // tiles of the items before
             for (int n = 0;; ++n) {
                 const int at = rp_attend_item(n, total);
-                if (at < 0) break;
+                if (at < 0 || rp_uniform(waits->gave_up)) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
                 const int len = rp_uniform(t.len), first = A.causal ? (int)rp_uniform(t.row0 >> 7) : 0, per = ((len + 127) >> 7) - first, nt = per * A.share;
                 int tile = first;                       // of queries: the next to arrive
@@ -198,7 +196,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 };
                 auto arrived = [&](u32 f) {     // a tile's queries and gradients
                     const u32 s = f % STAGES;
-                    bar_hold(rp_smem(&sm.q_full[s]), (f / STAGES) & 1, gave_up);
+                    bar_hold(rp_smem(&sm.q_full[s]), (f / STAGES) & 1, waits);
                     // queries behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
                     const int left = len - tile * 128;
                     if (left < 128) { rp_clear_rows<D>(sm.q[s], left, 128, lane); rp_clear_rows<D>(sm.g[s], left, 128, lane); }
@@ -210,20 +208,20 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 #pragma unroll
                     for (int x = 0; x < 8; ++x) mma_ts(one, to, weights + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
                 };
-                bar_hold(rp_smem(&sm.kv_full), n & 1, gave_up);
+                bar_hold(rp_smem(&sm.kv_full), n & 1, waits);
                 arrived(base);
                 against(tm, sm.k, sm.q[base % STAGES], rp_smem(&sm.s_full));
                 against(tm + 128, sm.v, sm.g[base % STAGES], rp_smem(&sm.dp_full));
                 if (nt == 1) mma_commit(one, rp_smem(&sm.kv_empty));
-                if (n) bar_hold(rp_smem(&sm.acc_empty), (n - 1) & 1, gave_up);
+                if (n) bar_hold(rp_smem(&sm.acc_empty), (n - 1) & 1, waits);
                 for (int j = 0; j < nt; ++j) {
                     const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
                     if (j + 1 < nt) arrived(f + 1);         // (mostly before the weights have)
-                    bar_hold(rp_smem(&sm.p_full), f & 1, gave_up);
+                    bar_hold(rp_smem(&sm.p_full), f & 1, waits);
                     tmem_after();
                     add(tm + 256, tm, sm.g[s], j > 0);
                     if (j + 1 < nt) against(tm, sm.k, sm.q[s1], rp_smem(&sm.s_full));
-                    bar_hold(rp_smem(&sm.ds_full), f & 1, gave_up);
+                    bar_hold(rp_smem(&sm.ds_full), f & 1, waits);
                     tmem_after();
                     add(tm + 256 + D, tm + 128, sm.q[s], j > 0);
                     mma_commit(one, rp_smem(&sm.q_empty[s]));
@@ -263,8 +261,8 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 if (row < 64) { st[0][row] = -next.x; st[1][row] = -next.y; }
                 if (j + 1 < nt) next = stats(j + 1);
                 bar_arrive_warp(rp_smem(&sm.st_full[b]), lane);
-                if (!(ok = bar_wait_warp(rp_smem(&sm.st_full[b]), f & 1, gave_up))) break;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.st_full[b]), f & 1, waits))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, waits))) break;
                 tmem_after();
                 u32 s[64];
                 float p[64];
@@ -288,7 +286,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_stored();
                 tmem_before();
                 bar_arrive_warp(rp_smem(&sm.p_full), lane);
-                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, waits))) break;
                 tmem_after();
                 tmem_load32(td, s);
                 tmem_load32(td + 32, s + 32);
@@ -307,7 +305,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_before();
                 bar_arrive_warp(rp_smem(&sm.ds_full), lane);
             }
-            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up) && !*gave_up;
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, waits) && !waits->gave_up;
             tmem_after();
             // the first group hands over dv, the second dk
             X *out = b ? (X *)A.x[1] + (t.base + r) * A.token[1] + hk * A.hd[1] : (X *)A.x[0] + (t.base + r) * A.token[0] + hk * A.hd[0];
@@ -318,7 +316,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     }
     __syncwarp();
     __syncthreads();
-    if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
+    if (threadIdx.x == 0 && sm.waits.gave_up) *A.status = RP_ERR_TIMEOUT;
     if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);
 }
 
@@ -336,7 +334,7 @@ template <int D> struct QuerySmem {
     u64 q_full, kv_full[STAGES], kv_empty[STAGES], s_full, s_empty, dp_full, ds_full, acc_full, item_full[2], item_empty[2], done;
     u32 tmem;
     volatile int item[2];
-    volatile int gave_up;
+    Waits waits;
 };
 
 template <typename X, int D>
@@ -353,7 +351,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         bar_init(rp_smem(&sm.q_full), 8); bar_init(rp_smem(&sm.s_full), 1); bar_init(rp_smem(&sm.s_empty), 8); bar_init(rp_smem(&sm.dp_full), 1);
         bar_init(rp_smem(&sm.ds_full), 8); bar_init(rp_smem(&sm.acc_full), 1); bar_init(rp_smem(&sm.done), 1);
         for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.item_full[i]), 1); bar_init(rp_smem(&sm.item_empty[i]), 9); }
-        sm.gave_up = 0;
+        sm.waits.start(A.wait_ns);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == ATTEND_COPY_WARP) tmem_alloc(rp_smem(&sm.tmem), 512);
@@ -362,7 +360,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     tmem_after();
     const u32 tm = rp_uniform(sm.tmem);
     const int total = rp_uniform(A.head->count * A.Hq);
-    volatile int *gave_up = &sm.gave_up;
+    Waits *const waits = &sm.waits;
 
     if (warp >= 8) {
         rp_few_registers();
@@ -372,7 +370,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             bool ok = true;
             for (int n = 0; ok; ++n) {
                 // the next of the list for whoever is free: CTAs start as the keys' kernel leaves them an SM
-                if (n > 1 && !(ok = bar_wait(rp_smem(&sm.item_empty[n & 1]), ((n >> 1) - 1) & 1, gave_up))) break;
+                if (!(ok = bar_place(n > 1, rp_smem(&sm.item_empty[n & 1]), ((n >> 1) - 1) & 1, waits))) break;
                 int at = atomicAdd(&A.head->ticket, 1);
                 if (at >= total) at = -1;
                 sm.item[n & 1] = at;
@@ -382,7 +380,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 const int hk = at % A.Hq / A.share, nk = rp_attend_tiles(t, 0, A.causal);
                 for (int j = 0; j < nk; ++j, ++fill) {
                     const u32 s = fill % STAGES, turn = fill / STAGES;
-                    if (turn && !(ok = bar_wait(rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, gave_up))) break;
+                    if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), 2 * Smem::TILE);
                     for (int p = 0; p < PANELS; ++p) {
                         tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
@@ -390,19 +388,17 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     }
                 }
             }
-            if (!ok) {
-                // nobody may leave while copies are under way
-                for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1);
-            }
+            // nobody may leave while copies are under way (whoever should have waited for them may have given up)
+            for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1);
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
             const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
             for (int n = 0;; ++n) {
-                bar_hold(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, gave_up);
+                bar_hold(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, waits);
                 const int at = rp_uniform(sm.item[n & 1]);
-                if (at < 0 || rp_uniform(*gave_up)) break;
+                if (at < 0 || rp_uniform(waits->gave_up)) break;
                 bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
                 const int len = rp_uniform(t.len), nk = rp_uniform(rp_attend_tiles(t, 0, A.causal));
@@ -415,13 +411,13 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 };
                 auto arrived = [&](int j) {             // a tile's keys and values
                     const u32 f = base + j;
-                    bar_hold(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1, gave_up);
+                    bar_hold(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1, waits);
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
                     if (len - j * 128 < 128) rp_clear_rows<D>(sm.k[f % STAGES], len - j * 128, 128, lane);
                 };
                 arrived(0);
                 // (who has handed over q and do has taken dq of the block before)
-                bar_hold(rp_smem(&sm.q_full), n & 1, gave_up);
+                bar_hold(rp_smem(&sm.q_full), n & 1, waits);
                 tmem_after();
                 against(tm, tm + 384, sm.k[base % STAGES], rp_smem(&sm.s_full));
                 against(tm + 128, tm + 448, sm.v[base % STAGES], rp_smem(&sm.dp_full));
@@ -429,11 +425,11 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
                     if (j + 1 < nk) {
                         arrived(j + 1);
-                        bar_hold(rp_smem(&sm.s_empty), f & 1, gave_up);
+                        bar_hold(rp_smem(&sm.s_empty), f & 1, waits);
                         tmem_after();
                         against(tm, tm + 384, sm.k[s1], rp_smem(&sm.s_full));
                     }
-                    bar_hold(rp_smem(&sm.ds_full), f & 1, gave_up);
+                    bar_hold(rp_smem(&sm.ds_full), f & 1, waits);
                     tmem_after();
                     const u32 k = mma_operand(rp_smem(sm.k[s]), false, PANEL);
 #pragma unroll
@@ -459,7 +455,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         int at = 0;                                     // the item
         auto fetch = [&](int n) {
             at = -1;
-            if (bar_wait_warp(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, gave_up)) at = sm.item[n & 1];
+            if (bar_wait_warp(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, waits)) at = sm.item[n & 1];
             if (at < 0) return;
             bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
             const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
@@ -485,7 +481,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             const f2 lse2 = rp_f2(-st.x, -st.x), delta2 = rp_f2(-st.y, -st.y);
             bool ok = true;
             for (int j = 0; j < nk; ++j, ++f) {
-                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, waits))) break;
                 tmem_after();
                 u32 s[64];
                 f2 p[32];
@@ -497,7 +493,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
                 for (int c = 0; c < 32; ++c) p[c] = rp_exp2(rp_fma(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sl2, lse2));
                 const int k0 = j * 128 + b * 64, lim = (A.causal ? min(t.len, r + 1) : t.len) - k0;
-                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, gave_up))) break;
+                if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, waits))) break;
                 tmem_after();
                 tmem_load32(td, s);
                 tmem_load32(td + 32, s + 32);
@@ -525,7 +521,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 bar_arrive_warp(rp_smem(&sm.ds_full), lane);
             }
             fetch(n + 1);                               // while dq is finished and handed over
-            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, gave_up) && !*gave_up;
+            if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, waits) && !waits->gave_up;
             tmem_after();
             // each group hands over one half of the columns
             X *out = (X *)A.x[0] + (t.base + r) * A.token[0] + h * A.hd[0] + b * (D / 2);
@@ -535,7 +531,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
     __syncwarp();
     __syncthreads();
-    if (threadIdx.x == 0 && sm.gave_up) *A.status = RP_ERR_TIMEOUT;
+    if (threadIdx.x == 0 && sm.waits.gave_up) *A.status = RP_ERR_TIMEOUT;
     rp_wait_for_launch_before();                     // this launch is not over before the keys' is
     if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);
 }
@@ -621,7 +617,7 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
         GradArgs &A = G[w];
         A = GradArgs();
         A.items = P[w].items; A.head = head[w]; A.start = (const i64 *)start; A.T = T; A.Hq = Hq; A.Hk = Hk; A.share = Hq / Hk; A.d = d; A.causal = a->causal;
-        A.scale = a->scale; A.stats = stats; A.status = &head[0]->status;
+        A.scale = a->scale; A.stats = stats; A.status = &head[0]->status; A.wait_ns = (u64)g_attend_wait_ns;
     }
     G[0].x[0] = v_grad->x; G[0].token[0] = v_grad->token; G[0].hd[0] = v_grad->head;
     G[0].x[1] = k_grad->x; G[0].token[1] = k_grad->token; G[0].hd[1] = k_grad->head;

@@ -35,34 +35,46 @@ __device__ __forceinline__ u64 rp_nanoseconds()
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// Waits for the end of a barrier's phase, two seconds at most (a step of these kernels takes microseconds): false when they ran out.  `gave_up` is the CTA's
-// word for it: whoever waits longer than that sets it, and all others stop waiting when they see it.
-__device__ __forceinline__ bool bar_wait_long(u32 bar, u32 parity, volatile int *gave_up)
+// A CTA's waits, in its shared memory: whoever waits for longer than the limit sets `gave_up`, and all others stop waiting when they see it.
+struct Waits {
+    volatile int gave_up;
+    u64 limit;                                           // nanoseconds; 0: nothing is waited for
+    __device__ __forceinline__ void start(u64 ns) { gave_up = ns == 0; limit = ns; }
+};
+// Waits for the end of a barrier's phase, up to the limit (two seconds; a step of these kernels takes microseconds): false when it ran out.
+__device__ __forceinline__ bool bar_wait_long(u32 bar, u32 parity, Waits *w)
 {
-    const u64 since = rp_nanoseconds();
+    const u64 since = rp_nanoseconds(), limit = w->limit;
     for (u32 n = 0;; ++n) {
+        if (w->gave_up) return false;
         if (bar_try(bar, parity)) return true;
-        if (*gave_up) return false;
-        if ((n & 63) == 63 && rp_nanoseconds() - since > 2000000000ull) { *gave_up = 1; return false; }
+        if ((n & 63) == 63 && rp_nanoseconds() - since > limit) { w->gave_up = 1; return false; }
     }
 }
-__device__ __forceinline__ bool bar_wait(u32 bar, u32 parity, volatile int *gave_up)
+__device__ __forceinline__ bool bar_wait(u32 bar, u32 parity, Waits *w)
 {
     if (bar_try(bar, parity)) return true;
-    return bar_wait_long(bar, parity, gave_up);
+    return bar_wait_long(bar, parity, w);
 }
 
 // The same for a whole warp, which goes on together.
-__device__ __forceinline__ bool bar_wait_warp(u32 bar, u32 parity, volatile int *gave_up)
+__device__ __forceinline__ bool bar_wait_warp(u32 bar, u32 parity, Waits *w)
 {
-    return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up));
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, w));
 }
 
-// The same for the warp that issues products, which does not ask: when a wait ran out it goes on with whatever there is, all its waits end at once from then on, and
-// the blocks that are handed over afterwards are marked.  (A vote and a branch less a wait: 50 of 125 cycles in which the tensor cores run dry.)
-__device__ __forceinline__ void bar_hold(u32 bar, u32 parity, volatile int *gave_up)
+// The same for the warp that copies: a place that is free again, or has not been used yet.  Nothing is copied any more once a wait has run out, since who has let go of
+// a place then need not be done with it.
+__device__ __forceinline__ bool bar_place(bool used, u32 bar, u32 parity, Waits *w)
 {
-    if (!bar_try(bar, parity)) bar_wait_long(bar, parity, gave_up);
+    return (!used || bar_wait(bar, parity, w)) && !w->gave_up;
+}
+
+// The same for the warp that issues products, which does not ask: when a wait ran out it goes on to the end of its block with whatever there is, all its waits end at once
+// from then on, and the blocks that are handed over afterwards are marked.  (A vote and a branch less a wait: 50 of 125 cycles in which the tensor cores run dry.)
+__device__ __forceinline__ void bar_hold(u32 bar, u32 parity, Waits *w)
+{
+    if (!bar_try(bar, parity)) bar_wait_long(bar, parity, w);
     __syncwarp();
 }
 

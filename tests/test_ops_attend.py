@@ -408,3 +408,68 @@ def test_many_small_weights_beside_a_large_one(under, kind):
     assert abs(out[-1, 0, 1].item() - 1) <= off + T * 2.0 ** -23
     # (a sum in 32 bits that takes T / 128 more numbers, each time to 2^-24 of itself)
     assert abs(lse[-1, 0].item() - math.log1p(part)) <= 4e-6 * (1 + math.log1p(part)) + (T / 128 + 1) * 2.0 ** -24
+
+
+def test_refusals_of_the_status_and_the_limit():
+    assert rp.lib().rp_debug_set_wait_limit(-1) == -1
+    rp.rp_debug_set_wait_limit()
+
+
+def run_out_inputs(shape, kind="bfloat16"):
+    """(q, k, v, do, start, right results, views of which rows a sample holds)"""
+    import torch
+    T, hq, hk, d, start = shape
+    q, k, v, g = inputs(shape, kind)
+    st = torch.tensor(start, device="cuda")
+    do = torch.randn(T, hq, d, generator=g).to(q.dtype).cuda()
+    out, lse = rp.rp_attend(q, k, v, st)
+    grads = rp.rp_attend_grad(do, q, k, v, out, lse, st)
+    held = torch.zeros(T, dtype=torch.bool, device="cuda")
+    for lo, hi in samples(start, T):
+        held[lo:hi] = True
+    return q, k, v, do, st, out, lse, grads, held
+
+
+RUN_OUT = [(2000, 4, 2, 128, [5, 700, 701, 1990]), (3000, 16, 4, 64, [0, 3000]), (900, 8, 8, 64, list(range(0, 900, 9)))]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", RUN_OUT, ids=[str(s[:4]) for s in RUN_OUT])
+def test_waits_that_run_out_leave_nan_and_a_status(shape):
+    """A limit of 0, with which the kernels give up before their first wait; the calls before and after are as ever."""
+    import torch
+    q, k, v, do, st, out, lse, grads, held = run_out_inputs(shape)
+    status = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    o, l = torch.full_like(out, 3.0), torch.full_like(lse, 3.0)
+    try:
+        rp.rp_debug_set_wait_limit(0)
+        rp.rp_attend(q, k, v, st, out=o, lse=l, status=status)
+        assert status.item() == -8
+        assert o[held].isnan().all() and l[held].isnan().all() and (o[~held] == 0).all() and (l[~held] == 0).all()
+        status.fill_(7)
+        got = [torch.full(x.shape, 3.0, dtype=x.dtype, device="cuda") for x in grads]
+        rp.rp_attend_grad(do, q, k, v, out, lse, st, q_grad=got[0], k_grad=got[1], v_grad=got[2], status=status)
+        assert status.item() == -8
+        for x in got[1:]:
+            assert x[held].isnan().all() and (x[~held] == 0).all()
+    finally:
+        rp.rp_debug_set_wait_limit()
+    o, l = rp.rp_attend(q, k, v, st, status=status)
+    assert status.item() == 0 and (o == out).all() and (l == lse).all()
+    status.fill_(7)
+    got = rp.rp_attend_grad(do, q, k, v, out, lse, st, status=status)
+    assert status.item() == 0 and all((a == b).all() for a, b in zip(got, grads))
+
+
+@pytest.mark.gpu
+def test_status_of_no_tokens():
+    import torch
+    q, start = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.tensor([0, 0], device="cuda")
+    status = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    out, lse = rp.rp_attend(q, q, q, start, status=status)
+    assert status.item() == 0
+    status.fill_(7)
+    rp.rp_attend_grad(q, q, q, q, out, lse, start, status=status)
+    assert status.item() == 0
+    with pytest.raises(ValueError, match="status"):
+        rp.rp_attend(q, q, q, start, status=torch.zeros(2, dtype=torch.int32, device="cuda"))
