@@ -334,6 +334,7 @@ template <int D> struct QuerySmem {
     u64 q_full, kv_full[STAGES], kv_empty[STAGES], s_full, s_empty, dp_full, ds_full, acc_full, item_full[2], item_empty[2], done;
     u32 tmem;
     volatile int item[2];
+    int taken, handled[8];                   // when a wait has run out: blocks that the CTA took, blocks that each warp of the softmax handed over
     Waits waits;
 };
 
@@ -367,6 +368,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (warp == ATTEND_COPY_WARP && lane == 0) {
             tma_prefetch(&map_k); tma_prefetch(&map_v);
             u32 fill = 0;
+            int taken = 0;
             bool ok = true;
             for (int n = 0; ok; ++n) {
                 // the next of the list for whoever is free: CTAs start as the keys' kernel leaves them an SM
@@ -376,6 +378,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 sm.item[n & 1] = at;
                 bar_arrive(rp_smem(&sm.item_full[n & 1]));
                 if (at < 0) break;
+                taken = n + 1;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
                 const int hk = at % A.Hq / A.share, nk = rp_attend_tiles(t, 0, A.causal);
                 for (int j = 0; j < nk; ++j, ++fill) {
@@ -388,6 +391,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     }
                 }
             }
+            sm.taken = taken;
             // nobody may leave while copies are under way (whoever should have waited for them may have given up)
             for (u32 f = fill > (u32)STAGES ? fill - STAGES : 0; f < fill; ++f) rp_drain(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1);
         }
@@ -469,7 +473,8 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             }
         };
         fetch(0);
-        for (int n = 0; at >= 0; ++n) {
+        int n = 0;
+        for (; at >= 0; ++n) {
             const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
             const int h = at % A.Hq, nk = rp_attend_tiles(t, 0, A.causal), r = t.row0 + row;
 #pragma unroll
@@ -528,9 +533,28 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             store_row<X, D / 2>(tm + lanes + 256 + b * (D / 2), out, A.d - b * (D / 2), r < t.len, ok ? A.scale : NAN);
             tmem_before();
         }
+        if (lane == 0) sm.handled[warp] = n;
     }
     __syncwarp();
     __syncthreads();
+    if (warp < 8 && sm.waits.gave_up) {
+        // A wait ran out: blocks that were taken and not handed over become NaN, and so does what nobody has taken.
+        const int b = warp >> 2, row = threadIdx.x & 127;
+        auto mark = [&](int at, int r0, int rows, int c0, int columns) {
+            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
+            for (int x = lane; x < rows * columns; x += 32) {
+                const int r = t.row0 + r0 + x / columns, c = c0 + x % columns;
+                if (r < t.len && c < A.d) ((X *)A.x[0])[(t.base + r) * A.token[0] + at % A.Hq * A.hd[0] + c] = rp_round<X>(NAN);
+            }
+        };
+        for (int n = sm.handled[warp]; n < sm.taken; ++n) mark(sm.item[n & 1], row & ~31, 32, b * (D / 2), D / 2);
+        for (;;) {
+            int at = lane == 0 ? atomicAdd(&A.head->ticket, 1) : 0;
+            at = __shfl_sync(0xffffffffu, at, 0);
+            if (at >= total || at < 0) break;
+            mark(at, 0, 128, 0, D);
+        }
+    }
     if (threadIdx.x == 0 && sm.waits.gave_up) *A.status = RP_ERR_TIMEOUT;
     rp_wait_for_launch_before();                     // this launch is not over before the keys' is
     if (warp == ATTEND_COPY_WARP) tmem_free(tm, 512);

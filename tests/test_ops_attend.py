@@ -473,3 +473,44 @@ def test_status_of_no_tokens():
     assert status.item() == 0
     with pytest.raises(ValueError, match="status"):
         rp.rp_attend(q, q, q, start, status=torch.zeros(2, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+@pytest.mark.parametrize("shape", RUN_OUT, ids=[str(s[:4]) for s in RUN_OUT])
+def test_waits_that_run_out_leave_no_row_of_the_queries_gradient(shape, kind):
+    """Blocks that a CTA took and did not hand over, and those that nobody took."""
+    import torch
+    q, k, v, do, st, out, lse, grads, held = run_out_inputs(shape, kind)
+    status, got = torch.full((1,), 7, dtype=torch.int32, device="cuda"), torch.full_like(grads[0], 3.0)
+    try:
+        rp.rp_debug_set_wait_limit(0)
+        rp.rp_attend_grad(do, q, k, v, out, lse, st, q_grad=got, status=status)
+        assert status.item() == -8 and got[held].isnan().all() and (got[~held] == 0).all()
+    finally:
+        rp.rp_debug_set_wait_limit()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("limit", [1, 2000, 20000])
+@pytest.mark.parametrize("shape", RUN_OUT, ids=[str(s[:4]) for s in RUN_OUT])
+def test_short_limits_leave_right_rows_or_nan(shape, limit):
+    """Waits that run out anywhere or not at all: what is not NaN is right, and NaN comes with a status."""
+    import torch
+    q, k, v, do, st, out, lse, grads, held = run_out_inputs(shape)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    try:
+        rp.rp_debug_set_wait_limit(limit)
+        for _ in range(5):
+            o, l = torch.full_like(out, 3.0), torch.full_like(lse, 3.0)
+            rp.rp_attend(q, k, v, st, out=o, lse=l, status=status)
+            pairs = [(o, out), (l, lse)]
+            assert status.item() in (0, -8) and all(((a == b) | a.isnan()).all() for a, b in pairs)
+            assert status.item() == -8 or not any(a.isnan().any() for a, _ in pairs)
+            got = [torch.full(x.shape, 3.0, dtype=x.dtype, device="cuda") for x in grads]
+            rp.rp_attend_grad(do, q, k, v, out, lse, st, q_grad=got[0], k_grad=got[1], v_grad=got[2], status=status)
+            assert status.item() in (0, -8) and all(((a == b) | a.isnan()).all() for a, b in zip(got, grads))
+            assert status.item() == -8 or not any(a.isnan().any() for a in got)
+    finally:
+        rp.rp_debug_set_wait_limit()
+    assert all((a == b).all() for a, b in zip(rp.rp_attend_grad(do, q, k, v, out, lse, st), grads))
