@@ -377,7 +377,7 @@ int rp_rotate_grad(const rp_rotary *r, int64_t n_tokens, const double *inv_freq,
  *   Strides and addresses of q, k, v, out and their gradients have to be multiples of 16 bytes, strides positive.
  *   lse [n_tokens][q_heads] float, any strides; nullable in rp_attend.
  *   workspace: rp_attend_workspace(a, n_tokens, n_samples) bytes, 16-byte aligned.  Its first int32 is 0 when the kernels are done, or RP_ERR_TIMEOUT if one of their
- *     waits (two seconds each) ran out: outputs that had not been worked out are NaN then.
+ *     waits ran out (two seconds in which a CTA copied nothing more): outputs that had not been worked out are NaN then.
  * Limits: head_dim <= 128 and a multiple of 8, q_heads a multiple of kv_heads, type RP_F16 or RP_BF16, scale > 0, n_tokens < 2^31 - 512, n_samples <= 2^24. */
 typedef struct {
     int32_t q_heads, kv_heads, head_dim;

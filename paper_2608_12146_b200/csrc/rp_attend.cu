@@ -105,6 +105,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     const u32 s = fill % STAGES, turn = fill / STAGES;
                     if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), j && j < nk ? 2 * Smem::TILE : Smem::TILE);
+                    waits->copied = fill + 1;
                     for (int p = 0; p < PANELS; ++p) {
                         if (j) tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + (j - 1) * 128, rp_smem(&sm.kv_full[s]));
                         if (j < nk) tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));

@@ -164,6 +164,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                         const u32 s = fill % STAGES, turn = fill / STAGES;
                         if (!(ok = bar_place(turn, rp_smem(&sm.q_empty[s]), (turn - 1) & 1, waits))) break;
                         bar_expect(rp_smem(&sm.q_full[s]), 2 * Smem::TILE);
+                        waits->copied = fill + 1;
                         for (int p = 0; p < PANELS; ++p) {
                             tma_load3(rp_smem(sm.q[s]) + p * PANEL, &map_q, p * 64, h, (int)t.base + (first + j) * 128, rp_smem(&sm.q_full[s]));
                             tma_load3(rp_smem(sm.g[s]) + p * PANEL, &map_g, p * 64, h, (int)t.base + (first + j) * 128, rp_smem(&sm.q_full[s]));
@@ -385,6 +386,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     const u32 s = fill % STAGES, turn = fill / STAGES;
                     if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), 2 * Smem::TILE);
+                    waits->copied = fill + 1;
                     for (int p = 0; p < PANELS; ++p) {
                         tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
                         tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));

@@ -38,17 +38,22 @@ __device__ __forceinline__ u64 rp_nanoseconds()
 // A CTA's waits, in its shared memory: whoever waits for longer than the limit sets `gave_up`, and all others stop waiting when they see it.
 struct Waits {
     volatile int gave_up;
+    volatile u32 copied;                                 // how often something was copied: a CTA that goes on is not stuck, however long one of its warps has nothing to do
     u64 limit;                                           // nanoseconds; 0: nothing is waited for
-    __device__ __forceinline__ void start(u64 ns) { gave_up = ns == 0; limit = ns; }
+    __device__ __forceinline__ void start(u64 ns) { gave_up = ns == 0; copied = 0; limit = ns; }
 };
-// Waits for the end of a barrier's phase, up to the limit (two seconds; a step of these kernels takes microseconds): false when it ran out.
+// Waits for the end of a barrier's phase, up to the limit without a copy (two seconds; a step of these kernels takes microseconds): false when it ran out.
 __device__ __forceinline__ bool bar_wait_long(u32 bar, u32 parity, Waits *w)
 {
-    const u64 since = rp_nanoseconds(), limit = w->limit;
+    u64 since = rp_nanoseconds();
+    u32 seen = w->copied;
     for (u32 n = 0;; ++n) {
         if (w->gave_up) return false;
         if (bar_try(bar, parity)) return true;
-        if ((n & 63) == 63 && rp_nanoseconds() - since > limit) { w->gave_up = 1; return false; }
+        if ((n & 63) != 63) continue;
+        const u64 now = rp_nanoseconds();
+        if (w->copied != seen) { seen = w->copied; since = now; }
+        else if (now - since > w->limit) { w->gave_up = 1; return false; }
     }
 }
 __device__ __forceinline__ bool bar_wait(u32 bar, u32 parity, Waits *w)

@@ -514,3 +514,22 @@ def test_short_limits_leave_right_rows_or_nan(shape, limit):
     finally:
         rp.rp_debug_set_wait_limit()
     assert all((a == b).all() for a, b in zip(rp.rp_attend_grad(do, q, k, v, out, lse, st), grads))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_short_blocks_before_a_long_one_are_no_wait(causal):
+    """Two of the forward kernel's warp groups share a block of 256 queries; one of them has nothing to do in the blocks of 60000 samples of one token, and does not count
+    that as a wait: milliseconds, with a limit of 0.1."""
+    import torch
+    start = list(range(60000)) + list(range(60000, 100001, 200))
+    q, k, v, _ = inputs((100000, 1, 1, 64, start), "bfloat16")
+    st, status = torch.tensor(start, device="cuda"), torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    want = rp.rp_attend(q, k, v, st, causal=causal)
+    try:
+        rp.rp_debug_set_wait_limit(100_000)
+        got = rp.rp_attend(q, k, v, st, causal=causal, status=status)
+        assert status.item() == 0 and all((a == b).all() for a, b in zip(got, want))
+    finally:
+        rp.rp_debug_set_wait_limit()
+    assert (want[0][:60000] == v[:60000]).all()
