@@ -132,10 +132,6 @@ __device__ __forceinline__ float min_or_nan(float x, float y)
     return z;
 }
 
-// Rounding top / ln 2 gives all scores of a softmax one factor, which their sum takes out again: 2^32 at most up to here.  Of larger numbers (a row of nothing but the
-// type's lowest value, which is what some masks write) the difference is taken first: two logits that differ do so by 32 and more there.
-__device__ __forceinline__ bool far_out(float top) { return fabsf(top) > 5.0e8f; }
-
 // Scores of one token from its logits: softmax: e^(x - max) and 1 / their sum; sigmoid: s, and 1 / their sum.
 // `top` is what the largest logit is taken for: 0 where it is -inf (all scores are 0 then, and so is the inverse).
 // SHARED: two sigmoids share a reciprocal, 1 / (1 + a) = (1 + b) / ((1 + a)(1 + b)), where a score of less than 2^-63 counts as 2^-63; rows whose scores add up to
@@ -152,15 +148,17 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
         for (int i = 1; i < VPL; ++i) m = fmaxf(m, x[i]);
         m = sub_max<SUB>(m);
         top = m == -INFINITY ? 0.0f : m;
-        if (far_out(top)) {
+        // (the difference first: a maximum beyond 2^30, such as a row of nothing but the type's lowest value, would shift all exponents by an error of its own)
+        f2 both = rp_f2(0.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2((x[i] - top) * RP_LOG2E); sum += s[i]; }
-        } else {
-            const float shift = -top * RP_LOG2E;
-#pragma unroll
-            for (int i = 0; i < VPL; ++i) { s[i] = rp_exp2(fmaf(x[i], RP_LOG2E, shift)); sum += s[i]; }
+        for (int i = 0; i < VPL; i += 2) {
+            const f2 v = rp_exp2(rp_mul(rp_add(rp_f2(x[i], x[i + 1]), rp_f2(-top, -top)), rp_f2(RP_LOG2E, RP_LOG2E)));
+            both = rp_add(both, v);
+            rp_parts(v, s[i], s[i + 1]);
         }
-        __syncwarp();
+        float other;
+        rp_parts(both, sum, other);
+        sum += other;
         sum = sub_sum<SUB>(sum);
     } else {
         if (SHARED && !A.bias) {
@@ -179,8 +177,11 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
             rp_parts(both, sum, other);
             sum = sub_sum<SUB>(sum + other);
         }
-        const bool alone = !SHARED || A.bias || sum < 4.0e-9f;
-        if (__any_sync(0xffffffffu, alone)) {
+        if constexpr (!SHARED) {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) { s[i] = sigmoid(x[i]); sum += s[i]; }
+            sum = sub_sum<SUB>(sum);
+        } else if (const bool alone = A.bias || sum < 4.0e-9f; __any_sync(0xffffffffu, alone)) {
             float s1[VPL], sum1 = 0.0f;                      // (the warp's other tokens keep theirs)
 #pragma unroll
             for (int i = 0; i < VPL; ++i) { s1[i] = sigmoid(x[i]); sum1 += s1[i]; }
@@ -198,7 +199,7 @@ __device__ __forceinline__ void scores(const RouteArgs &A, const float *x, float
 __device__ __forceinline__ float score_of(const RouteArgs &A, float x, float top, float inv)
 {
     if (A.score != RP_SCORE_SOFTMAX) return sigmoid(x);
-    return rp_exp2(far_out(top) ? (x - top) * RP_LOG2E : fmaf(x, RP_LOG2E, -top * RP_LOG2E)) * inv;
+    return rp_exp2((x - top) * RP_LOG2E) * inv;
 }
 
 // Shares of a token's choices in their sum, over the lanes that have them, from the logits alone: for sums under SHARES_FROM, where scores leave the numbers' range while
@@ -596,6 +597,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route_grad(
             pb = sub_sum<SUB>(pb) * inv;
         }
         float add = 0.0f;
+        bool tiny = false;
         if (gates) {
             const float v = valid ? score_of(A, xe, top, inv) : 0.0f;
             float z = v, za = valid ? v * a : 0.0f;
@@ -603,13 +605,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route_grad(
             // (lanes behind the choices have their own sums: what all lanes need is the first's)
             const float zi = z < SHARES_FROM ? 0.0f : reciprocal(z), ds = soft ? v : v * (1.0f - v);
             add = A.normalise ? (a - za * zi) * (zi * ds) : a * ds;       // (zi may be large: the score is multiplied with it first)
-            const bool tiny = A.normalise && valid && z < SHARES_FROM;
-            if (__any_sync(0xffffffffu, tiny)) {
-                const float y = shares(valid, xe, k_lanes);
-                float ya = valid ? y * a : 0.0f;
-                for (int o = 1; o < k_lanes; o <<= 1) ya += __shfl_xor_sync(0xffffffffu, ya, o);
-                if (tiny) add = (a - ya) * y;
-            }
+            tiny = A.normalise && z < SHARES_FROM;
             if (soft && !A.normalise) pb += __shfl_sync(0xffffffffu, za, first_lane);
         }
 #pragma unroll
@@ -624,13 +620,18 @@ __global__ void __launch_bounds__(ROUTE_THREADS, VPL == 8 ? 4 : 1) k_route_grad(
             // (does an expert come twice? its tag is then another lane's)
             if (valid) tags[sub][e] = (unsigned char)sl;
             __syncwarp();
-            if (!__any_sync(0xffffffffu, valid && tags[sub][e] != sl)) {
+            if (!__any_sync(0xffffffffu, valid && (tiny || tags[sub][e] != sl))) {
                 if (valid) rows[sub][e] += add;
-            } else
+            } else {
+                const float y = shares(valid, xe, k_lanes);
+                float ya = valid ? y * a : 0.0f;
+                for (int o = 1; o < k_lanes; o <<= 1) ya += __shfl_xor_sync(0xffffffffu, ya, o);
+                if (tiny) add = (a - ya) * y;
                 for (int j = 0; j < A.k; ++j) {
                     if (sl == j && valid) rows[sub][e] += add;
                     __syncwarp();
                 }
+            }
             __syncwarp();
         }
         if (there) {
