@@ -233,9 +233,14 @@ def rp_window_load(lengths, demand, *, top_k: int, token_cap: int, dp_width: int
 def rp_window_load_routes(lengths, routes, n_experts: int, *, token_cap: int, dp_width: int, ep_width: int, pop_size: int,
                           edp_of_dp: Optional[Sequence[int]] = None, alpha: Sequence[float] = (1.0, 1.0),
                           beta: Sequence[float] = (0.0, 1.0), min_rows: int = 0, seed: int = 0, stream=None) -> Context:
-    """A window from recorded routes (CUDA tensor [n_tokens, n_layers, top_k] of integers, any strides with the choices side by side)."""
+    """A window from recorded routes (CUDA tensor [n_tokens, n_layers, top_k] of integers, any strides with the choices side by side).
+
+    ``stream``: torch's current one by default, on which the record is written; the context works on it.
+    """
     T, l, k = routes.shape
     size, ts, ls = _route_layout(routes)
+    if stream is None:
+        stream = _current_stream(routes.get_device())
     cfg, al, be, edp = _window_config(int(lengths.shape[0]), l, n_experts, k, token_cap, dp_width, ep_width, pop_size, edp_of_dp, alpha, beta,
                                       min_rows, seed)
     out = C.c_void_p(None)

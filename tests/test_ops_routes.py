@@ -244,3 +244,25 @@ def test_starts_that_decrease_read_nothing_else():
     for start in ([0, 400, 100, 500], [500, 0, 500], [300, 200, 100, 0], [10 ** 12, -10 ** 12, 10 ** 12]):
         got = rp.rp_count_routes(routes, torch.tensor(start, device="cuda"), 4)
         assert (got[:, :, [0, 2, 3]] == 0).all() and (got >= 0).all() and got.sum().item() <= 500 * 2 * 3 * (len(start) - 1)
+
+
+@pytest.mark.gpu
+def test_window_from_a_record_that_the_current_stream_still_writes():
+    import torch
+    rng = np.random.default_rng(8)
+    lengths = np.array([30, 1, 64, 17, 40, 40, 9, 55], np.int32)
+    T, L, E, k = int(lengths.sum()), 3, 16, 2
+    host = rng.integers(0, E, (T, L, k)).astype(np.uint8)
+    kw = dict(token_cap=128, dp_width=2, ep_width=4, pop_size=8, seed=1)
+    want = rp.rp_window_load(lengths, count(host, [0] + np.cumsum(lengths).tolist(), E).astype(np.int32), top_k=k, **kw)
+    right, record = torch.from_numpy(host).cuda(), torch.zeros(T, L, k, dtype=torch.uint8, device="cuda")
+    rp.rp_destroy(rp.rp_window_load_routes(lengths, record, E, **kw))          # (kernels are loaded, which waits for the GPU)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda._sleep(100_000_000)                   # about 50 ms
+        record.copy_(right)
+        got = rp.rp_window_load_routes(lengths, record, E, **kw)
+        for a, b in zip(rp.rp_place_experts(got), rp.rp_place_experts(want)):
+            assert np.array_equal(np.asarray(a), np.asarray(b))
+    rp.rp_destroy(got)
+    rp.rp_destroy(want)
