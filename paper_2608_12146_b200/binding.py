@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import warnings
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -360,6 +361,7 @@ def rp_release_cached_memory():
 # ---- operators on the tokens of a window ------------------------------------------------
 # Arrays are CUDA tensors of one GPU; calls queue on ``stream`` (default: torch's current stream of that GPU) and return.
 # Outputs that the caller does not pass are allocated on that stream.
+# Autograd does not record them: the forward calls warn where an input needs a gradient, the way back is a call of its own (rp_..._grad).
 _TYPES = {}
 
 
@@ -403,6 +405,13 @@ class _Queue:
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
+
+
+def _unrecorded(torch, call: str, *inputs):
+    """Says so where autograd would be expected to follow a call that it does not see."""
+    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in inputs):
+        warnings.warn(f"{call}: an input needs a gradient, but autograd does not record this call and its outputs have none; call it inside a "
+                      f"torch.autograd.Function (or under torch.no_grad()) with {call}_grad for the way back", stacklevel=3)
 
 
 def _dense(t, dtype, shape, what: str):
@@ -479,6 +488,7 @@ def rp_route(logits, top_k: int, start, *, score: str = "softmax", normalise: bo
     ones go (any integer type, rows with a stride: a slice of a record); int32 by default.
     """
     torch = _torch()
+    _unrecorded(torch, "rp_route", logits)
     row = _rows(logits, "logits")
     T, E = logits.shape
     at, n = _starts(torch, start)
@@ -604,6 +614,7 @@ def rp_rotate(q, k, inv_freq, start, *, first_position=None, q_weight=None, k_we
 
     ``inv_freq`` float64 [rotary_dim / 2] on the GPU, radians per position (None: no rotation); ``k`` may be None; outputs may be the inputs.
     """
+    _unrecorded(_torch(), "rp_rotate", q, k, q_weight, k_weight)
     results, _ = _rotate(q, k, inv_freq, start, first_position, (q_weight, k_weight), eps, layout, mscale, (q_out, k_out), (None, None), stream)
     return tuple(results)
 
@@ -654,6 +665,7 @@ def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = N
     ``status``: [1] int32 on the GPU, receives 0, or -8 (RP_ERR_TIMEOUT) where a wait inside the kernel ran out (outputs that were not worked out are NaN then).
     """
     torch = _torch()
+    _unrecorded(torch, "rp_attend", q, k, v)
     ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
     T, H, _ = q.shape
     _dense(status, torch.int32, (1,), "status")

@@ -73,3 +73,25 @@ def test_a_window_from_its_routers_to_its_rows():
             # gates of one token add up to 1, and so do the shares of the loss: a row's gradient adds up to nothing
             assert dx.float().sum(1).abs().max() <= 32 * 2.0 ** -8 * dx.float().abs().max() + 1e-6
     assert (seen == rp.rp_count_routes(record, start, E)[:, 0]).all()
+
+
+@pytest.mark.gpu
+def test_inputs_that_need_a_gradient_are_warned_about():
+    """Autograd does not see these calls: said once where it would be expected to, and not where the caller has it switched off."""
+    import warnings
+
+    import torch
+    start = torch.tensor([0, 8], device="cuda")
+    q, w = torch.randn(8, 2, 64, device="cuda").half(), torch.ones(64, device="cuda")
+    x = torch.randn(8, 16, device="cuda")
+    calls = {"rp_attend": lambda g: rp.rp_attend(q.clone().requires_grad_(g), q, q, start), "rp_rotate": lambda g: rp.rp_rotate(q, q, None, start, q_weight=w.clone().requires_grad_(g), k_weight=w),
+             "rp_route": lambda g: rp.rp_route(x.clone().requires_grad_(g), 2, start)}
+    for name, call in calls.items():
+        with pytest.warns(UserWarning, match=name + "_grad"):
+            got = call(True)
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            want = call(False)
+            with torch.no_grad():
+                call(True)
+        assert all((a == b).all() and not a.requires_grad for a, b in zip(got, want))
