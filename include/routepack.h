@@ -392,7 +392,8 @@ int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, con
 
 /* Gradient of rp_attend: from out_grad, the inputs, out and lse of the forward call to q_grad, k_grad and v_grad.
  *   Weights and the scores' gradients are rounded to `type` before their products; a key's gradients are summed over the query heads that share it in
- *   a fixed order.  Errors and limits as above; workspace: rp_attend_grad_workspace(a, n_tokens, n_samples) bytes. */
+ *   a fixed order.  For RP_F16 a sample's scores' gradients are rounded as multiples of a power of two that goes by the largest norm of its rows of out_grad; rows of v
+ *   up to a norm of 2047 cannot leave the type's range so.  Errors and limits as above; workspace: rp_attend_grad_workspace(a, n_tokens, n_samples) bytes. */
 int64_t rp_attend_grad_workspace(const rp_attend_config *a, int64_t n_tokens, int32_t n_samples);
 int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const rp_view *out,
                    const rp_view *lse, const rp_view *out_grad, const int64_t *start, int32_t n_samples, const rp_view *q_grad,

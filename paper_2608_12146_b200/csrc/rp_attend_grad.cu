@@ -2,6 +2,9 @@
 //
 //   p = exp(scale q k^T - lse), ds = p (do v^T - delta), delta = sum_d do o;   dv = p^T do, dk = scale ds^T q, dq = scale ds k
 //
+// float16 has few powers of two: a sample's gradients of scores are multiplied with one that puts the norm of its largest row of do between 8 and 16 before they are
+// rounded (so that values to a norm of 2047 cannot leave the range, and gradients of 10^-4 keep their bits), weights with 2^15; both are taken out of the sums.
+//
 // Two kernels: one takes 128 keys and goes through the queries that see them (dk, dv), one takes 128 queries and goes through the keys that they see
 // (dq).  Each output is summed by one CTA in a fixed order: no additions from several CTAs to one place, whose order would change the last bits.  The price is
 // that scores and do v^T are worked out twice, 14 multiply-adds a pair and element in place of 10.  Bound by the tensor cores.
@@ -17,6 +20,7 @@ struct GradArgs {
     int Hq, Hk, share, d, causal;
     float scale;
     const float2 *stats;                     // [Hq][T]: lse / ln 2, delta
+    const u32 *tops;                         // float16: [samples] square of the norm of the largest row of do, as bits
     void *x[2];                              // dv, dk, or dq
     i64 token[2], hd[2];
     int *status;
@@ -33,7 +37,10 @@ struct StatsArgs {
     i64 o_token, o_head, g_token, g_head, l_token, l_head;
     int H, d;
     float2 *stats;
+    float *norms;                            // float16: [H][T] squares of the norms of the rows of do
+    u32 *tops;
 };
+template <typename X> struct Narrow { static constexpr bool value = !std::is_same<X, bf16>::value; };
 template <typename X>
 __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, AttendPlan queries, AttendClears C, StatsArgs A)
 {
@@ -41,6 +48,8 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
     if (blockIdx.x == 1) { rp_attend_plan(queries); return; }
     const int b = blockIdx.x - 2, n = gridDim.x - 2, lane = threadIdx.x & 15;
     rp_attend_clear(C, keys.start, keys.N, keys.T, b, n);
+    if constexpr (Narrow<X>::value)
+        for (int i = b * 1024 + threadIdx.x; i < keys.N; i += n * 1024) A.tops[i] = 0;
     // 64 rows of a CTA: heads of a token, tokens; four steps on their way at a time (all lanes go round as often)
     constexpr int AHEAD = 4;
     const i64 T = keys.T;
@@ -69,9 +78,41 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
 #pragma unroll
                 for (int i = 1; i < 16; i <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
                 if (mine && t < T && lane == 0) A.stats[h * T + t] = make_float2(l[u] * RP_LOG2E, sum);
+                if constexpr (Narrow<X>::value) {
+                    float norm = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) norm = fmaf(c[i], c[i], norm);
+#pragma unroll
+                    for (int i = 1; i < 16; i <<= 1) norm += __shfl_xor_sync(0xffffffffu, norm, i);
+                    if (mine && t < T && lane == 0) A.norms[h * T + t] = norm;
+                }
             }
         }
     }
+}
+
+// The largest of a sample's rows of do, for float16 (infinities and NaN, which no factor mends, do not count): a thread a token.
+__global__ void __launch_bounds__(256) k_attend_tops(const i64 *start, int N, i64 T, int H, const float *norms, u32 *tops)
+{
+    const i64 t = (i64)blockIdx.x * 256 + threadIdx.x;
+    float top = 0.0f;
+    for (int h = 0; t < T && h < H; ++h) {
+        const float x = norms[h * T + t];
+        if (x < INFINITY) top = fmaxf(top, x);
+    }
+    const int i = t < T ? rp_sample_of(start, N, t) : -1;
+    u32 bits = i >= 0 && i < N ? __float_as_uint(top) : 0u;
+    if (__all_sync(0xffffffffu, i == __shfl_sync(0xffffffffu, i, 0))) {
+        bits = __reduce_max_sync(0xffffffffu, bits);
+        if (threadIdx.x & 31) bits = 0;
+    }
+    if (bits) atomicMax(tops + i, bits);
+}
+// Power of two for the gradients of a sample's scores, from its largest row.
+__device__ __forceinline__ float ds_scale(u32 top)
+{
+    const int e = (int)(__float_as_uint(sqrtf(__uint_as_float(top))) >> 23) - 127;         // 2^e <= norm < 2^(e + 1)
+    return top ? __uint_as_float((u32)(127 + 3 - e) << 23) : 1.0f;
 }
 
 // One row of an accumulator in tensor memory, D columns, goes out.
@@ -250,6 +291,9 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
             const int hk = at % A.Hk, first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first, nt = per * A.share, r = t.row0 + row;
             bool ok = true;
+            float c1 = 1.0f;                            // float16: the factors of ds (without the weights') and of the outputs
+            if constexpr (Narrow<X>::value) c1 = ds_scale(A.tops[A.items[at / A.Hk].x]);
+            const f2 c2 = rp_f2(c1 * (1.0f / 32768.0f), c1 * (1.0f / 32768.0f));
             auto stats = [&](int j) {                   // of one column of a tile
                 const int q = (first + j % per) * 128 + b * 64 + row;
                 return row < 64 && q < t.len ? A.stats[(i64)(hk * A.share + j / per) * A.T + t.base + q] : make_float2(0.0f, 0.0f);
@@ -259,7 +303,10 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 const int q0 = (first + j % per) * 128 + b * 64;
                 // (two places in turn: who has come to a tile's barrier has read the tile before)
                 float (*st)[64] = sm.stats[f & 1][b];
-                if (row < 64) { st[0][row] = -next.x; st[1][row] = -next.y; }
+                if (row < 64) {
+                    st[0][row] = Narrow<X>::value ? 15.0f - next.x : -next.x;
+                    st[1][row] = Narrow<X>::value ? -next.y * (c1 * (1.0f / 32768.0f)) : -next.y;
+                }
                 if (j + 1 < nt) next = stats(j + 1);
                 bar_arrive_warp(rp_smem(&sm.st_full[b]), lane);
                 if (!(ok = bar_wait_warp(rp_smem(&sm.st_full[b]), f & 1, waits))) break;
@@ -292,13 +339,14 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_load32(td, s);
                 tmem_load32(td + 32, s + 32);
                 tmem_loaded();
+                auto less = [&](f2 dp, f2 delta) { return Narrow<X>::value ? rp_fma(dp, c2, delta) : rp_add(dp, delta); };
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
                     const ulonglong2 e = *(const ulonglong2 *)&st[1][c];         // (of the other sign)
                     float a, z;
-                    rp_parts(rp_mul(rp_f2(p[c], p[c + 1]), rp_add(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), f2{ e.x })), a, z);
+                    rp_parts(rp_mul(rp_f2(p[c], p[c + 1]), less(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), f2{ e.x })), a, z);
                     s[c / 2] = rp_pair(a, z, X());
-                    rp_parts(rp_mul(rp_f2(p[c + 2], p[c + 3]), rp_add(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), f2{ e.y })), a, z);
+                    rp_parts(rp_mul(rp_f2(p[c + 2], p[c + 3]), less(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), f2{ e.y })), a, z);
                     s[c / 2 + 1] = rp_pair(a, z, X());
                 }
                 tmem_store32(td, s);
@@ -310,7 +358,8 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             tmem_after();
             // the first group hands over dv, the second dk
             X *out = b ? (X *)A.x[1] + (t.base + r) * A.token[1] + hk * A.hd[1] : (X *)A.x[0] + (t.base + r) * A.token[0] + hk * A.hd[0];
-            store_row<X, D>(tm + lanes + 256 + b * D, out, A.d, r < t.len, !ok ? NAN : b ? A.scale : 1.0f);
+            const float f0 = Narrow<X>::value ? 1.0f / 32768.0f : 1.0f, f1 = Narrow<X>::value ? A.scale / c1 : A.scale;      // (c1: a power of two)
+            store_row<X, D>(tm + lanes + 256 + b * D, out, A.d, r < t.len, !ok ? NAN : b ? f1 : f0);
             tmem_before();
             bar_arrive_warp(rp_smem(&sm.acc_empty), lane);
         }
@@ -485,7 +534,9 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             tmem_before();
             bar_arrive_warp(rp_smem(&sm.q_full), lane);
             const float2 st = r < t.len ? A.stats[(i64)h * A.T + t.base + r] : make_float2(0.0f, 0.0f);
-            const f2 lse2 = rp_f2(-st.x, -st.x), delta2 = rp_f2(-st.y, -st.y);
+            float c1 = 1.0f;                            // float16: the factor of ds
+            if constexpr (Narrow<X>::value) c1 = ds_scale(A.tops[A.items[at / A.Hq].x]);
+            const f2 lse2 = rp_f2(-st.x, -st.x), delta2 = rp_f2(-st.y * c1, -st.y * c1), c2 = rp_f2(c1, c1);
             bool ok = true;
             for (int j = 0; j < nk; ++j, ++f) {
                 if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, waits))) break;
@@ -506,7 +557,10 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 tmem_load32(td + 32, s + 32);
                 tmem_loaded();
 #pragma unroll
-                for (int c = 0; c < 32; ++c) p[c] = rp_mul(p[c], rp_add(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), delta2));
+                for (int c = 0; c < 32; ++c) {
+                    const f2 dp = rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
+                    p[c] = rp_mul(p[c], Narrow<X>::value ? rp_fma(dp, c2, delta2) : rp_add(dp, delta2));
+                }
                 if (k0 + 64 > t.len || (A.causal && k0 + 63 > t.row0)) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) {
@@ -532,7 +586,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             tmem_after();
             // each group hands over one half of the columns
             X *out = (X *)A.x[0] + (t.base + r) * A.token[0] + h * A.hd[0] + b * (D / 2);
-            store_row<X, D / 2>(tm + lanes + 256 + b * (D / 2), out, A.d - b * (D / 2), r < t.len, ok ? A.scale : NAN);
+            store_row<X, D / 2>(tm + lanes + 256 + b * (D / 2), out, A.d - b * (D / 2), r < t.len, !ok ? NAN : Narrow<X>::value ? A.scale / c1 : A.scale);
             tmem_before();
         }
         if (lane == 0) sm.handled[warp] = n;
@@ -565,13 +619,13 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 // ---------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------
-// Workspace: front and items of the keys' kernel, the same of the queries', statistics.
+// Workspace: front and items of the keys' kernel, the same of the queries', statistics; for float16 norms of rows and the largest of each sample.
 static i64 plan_bytes(i64 T, int N) { return ((i64)sizeof(AttendHead) + 8 * (T / 128 + N) + 15) / 16 * 16; }
 
 extern "C" int64_t rp_attend_grad_workspace(const rp_attend_config *a, int64_t n_tokens, int32_t n_samples)
 {
     if (rp_attend_check(a, n_tokens, n_samples) != RP_OK) return 0;
-    return 2 * plan_bytes(n_tokens, n_samples) + 8 * n_tokens * a->q_heads;
+    return 2 * plan_bytes(n_tokens, n_samples) + 8 * n_tokens * a->q_heads + (a->type == RP_F16 ? 4 * (n_tokens * a->q_heads + n_samples) : 0);
 }
 
 struct GradMaps { CUtensorMap q, k, v, g; };
@@ -651,9 +705,16 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     G[1].rows[1] = out_grad->x; G[1].r_token[1] = out_grad->token; G[1].r_head[1] = out_grad->head;
     G[1].x[0] = q_grad->x; G[1].token[0] = q_grad->token; G[1].hd[0] = q_grad->head;
     const int sms = rp_op_sms(dev.device);
-    const StatsArgs S = { out->x, out_grad->x, (const float *)lse->x, out->token, out->head, out_grad->token, out_grad->head, lse->token, lse->head, Hq, d, stats };
+    float *const norms = (float *)(stats + T * Hq);
+    u32 *const tops = (u32 *)(norms + T * Hq);           // (float16)
+    G[0].tops = G[1].tops = tops;
+    const StatsArgs S = { out->x, out_grad->x, (const float *)lse->x, out->token, out->head, out_grad->token, out_grad->head, lse->token, lse->head, Hq, d, stats, norms, tops };
     const int ctas = 2 + (int)std::min((T * Hq + 63) / 64, (i64)sms * 2 - 2);
-    if (a->type == RP_F16) k_attend_prepare<__half><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
+    if (a->type == RP_F16) {
+        k_attend_prepare<__half><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
+        RP_TRY(rp_op_launched());
+        k_attend_tops<<<(unsigned)((T + 255) / 256), 256, 0, stream>>>((const i64 *)start, n_samples, T, Hq, norms, tops);
+    }
     else k_attend_prepare<bf16><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
     RP_TRY(rp_op_launched());
     if (a->type == RP_F16) return d <= 64 ? launch<__half, 64>(M, G[0], G[1], P[0].most, sms, stream) : launch<__half, 128>(M, G[0], G[1], P[0].most, sms, stream);

@@ -533,3 +533,36 @@ def test_many_short_blocks_before_a_long_one_are_no_wait(causal):
     finally:
         rp.rp_debug_set_wait_limit()
     assert (want[0][:60000] == v[:60000]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("size,T,scale", [(1e-5, 1500, 0.125), (1e-4, 2048, 0.125), (1e-3, 2048, 0.125), (1.0, 700, 0.125), (1e4, 300, 0.02)])
+def test_gradients_of_any_size_in_float16(size, T, scale, causal):
+    """Gradients whose scores' gradients lie under float16's normal range or beyond its largest number, beside a sample with ordinary ones."""
+    import torch
+    q, k, v, g = inputs((T + 100, 1, 1, 64, [0, T]), "float16")
+    do = torch.randn(T + 100, 1, 64, generator=g).cuda()
+    do[:T] *= size
+    do = do.half()
+    v = v * 4 if size > 1 else v                         # (do v^T to 10^6)
+    st = torch.tensor([0, T, T + 100], device="cuda")
+    out, lse = rp.rp_attend(q, k, v, st, causal=causal, scale=scale)
+    got = rp.rp_attend_grad(do, q, k, v, out, lse, st, causal=causal, scale=scale)
+    for lo, hi in ((0, T), (T, T + 100)):
+        q64, k64, v64, d64 = [x[lo:hi, 0].double() for x in (q, k, v, do)]
+        p, _ = weights(q64, k64, scale, causal)
+        o = p @ v64
+        ds = p * (d64 @ v64.T - (d64 * o).sum(1, keepdim=True))
+        slip = p * (d64 * o).abs().sum(1, keepdim=True)
+        # Norms over all elements: weights and gradients of scores are off by 2^-11 of themselves (or by half a step of 2^-24 where they were multiplied with 2^15, with 8 over the
+        # largest row's norm or more), the latter by the rounding of o too, both by 2e-5 for 32 bits; a product is off by that times the other factor's largest singular
+        # value, and each result is rounded once
+        n = hi - lo
+        off_p = (2.0 ** -11 + 2e-5) * p.norm() + n * 2.0 ** -40
+        off_ds = (2.0 ** -11 + 2e-5) * (ds.norm() + slip.norm()) + n * 2.0 ** -25 * d64.norm(dim=1).max() / 8
+        want = (ds @ k64 * scale, ds.T @ q64 * scale, p.T @ d64)
+        offs = (off_ds * torch.linalg.matrix_norm(k64, 2) * scale, off_ds * torch.linalg.matrix_norm(q64, 2) * scale, off_p * torch.linalg.matrix_norm(d64, 2))
+        for x, w, off in zip(got, want, offs):
+            assert torch.isfinite(x).all()
+            assert (x[lo:hi, 0].double() - w).norm() <= off + (2.0 ** -11 * w.abs() + 2.0 ** -25).norm()
