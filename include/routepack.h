@@ -285,7 +285,8 @@ typedef enum { RP_F32 = 0, RP_F16 = 1, RP_BF16 = 2 } rp_type;
  *   routes: element (t, l, j) at t * token_stride + l * layer_stride + j, j < top_k; route_bytes = 1 (unsigned), 2, 4 or 8 (signed).
  *     Values outside [0, n_experts) (places left empty) are not counted.
  *   demand [n_samples][n_layers][n_experts] int32, written whole: the input of rp_window_load.
- * Limits: n_experts <= 1024, top_k <= 1024, n_layers <= 65535, n_layers * n_experts < 2^31, n_tokens <= 2^36. */
+ * Limits: n_experts <= 1024, top_k <= 1024, n_layers <= 65535, n_layers * n_experts < 2^31, n_tokens <= 2^36; a count is an int32, so a sample's tokens times top_k
+ * stay below 2^31 (lengths are not looked at on the host: more wrap around). */
 int rp_count_routes(const void *routes, int32_t route_bytes, int64_t n_tokens, int32_t n_layers, int32_t top_k, int32_t n_experts,
                     int64_t token_stride, int64_t layer_stride, const int64_t *start, int32_t n_samples, int32_t *demand,
                     void *cuda_stream);

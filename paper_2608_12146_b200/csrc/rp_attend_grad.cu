@@ -7,7 +7,8 @@
 //
 // Two kernels: one takes 128 keys and goes through the queries that see them (dk, dv), one takes 128 queries and goes through the keys that they see
 // (dq).  Each output is summed by one CTA in a fixed order: no additions from several CTAs to one place, whose order would change the last bits.  The price is
-// that scores and do v^T are worked out twice, 14 multiply-adds a pair and element in place of 10.  Bound by the tensor cores.
+// that scores and do v^T are worked out twice, 14 multiply-adds a pair and element in place of 10.  Bound by the hand-overs between the warp that issues products and
+// those of the softmax: at 4096 tokens the tensor cores are busy for 21 % (keys, which also wait for the largest block) and 41 % (queries) of the time.
 #include <algorithm>
 
 #include "rp_attend.cuh"

@@ -64,7 +64,9 @@ template <typename X> __device__ __forceinline__ float weight_at(const RotArgs &
     return A.w32 ? ((const float *)w)[i] : rp_float(((const X *)w)[i]);
 }
 
-// Any head size and alignment: a warp takes one head after the other, a lane the pairs lane, lane + 32, .. and then the elements behind them.
+// Any head size and alignment: a warp takes one head after the other, a lane the pairs lane, lane + 32, .. and then the elements behind them.  Elements are read one by one,
+// once for the norm and again for each pass behind it, and one head at a time is on its way: 16384 tokens of 32 + 8 heads of 72 take 310 us (gradient 511), of 128 in
+// pieces 71 (122).
 // GRAD: y receives the gradient of x.
 template <typename X, bool GRAD>
 __global__ void __launch_bounds__(ROT_THREADS) k_rotate_any(RotArgs A)
@@ -168,8 +170,10 @@ __global__ void __launch_bounds__(ROT_THREADS) k_rotate_any(RotArgs A)
 // (half layout) or neighbours, so that a lane has all pairs that it needs and the mean of squares is a few shuffles.  A warp takes ROT_CHUNK tokens at a time:
 // their sines and cosines go to shared memory once, for all heads; then it goes through the heads of the queries, then of the keys, with a token's factors (and the
 // sums for the weights' gradients) in registers.  The loads of two steps are issued before either is worked on.
-// Of the measured copy rate 78 % forward, 70 % backward (128 registers, 16 warps an SM): it waits for memory.  Tried: a third step in flight (spills, 300 us for
-// 131), rows through shared memory by asynchronous copies (136 to 150), rows asked into L2 ahead (147).
+// 32768 tokens of 32 + 8 heads of 128 in bf16 129 us, 81 % of the measured copy rate; the gradient of 16411 with half of each head turned 114 us, 69 % (128 registers,
+// 16 warps an SM): it waits for memory.  All forms keep some registers in local memory: 12 to 60 bytes a thread forward in 16 bits (52 for these rows), 28 to 124
+// backward, 76 to 128 in 32 bits.  Tried: a third step in flight (more of that, 300 us for 131), rows through shared memory by asynchronous copies (136 to 150), rows
+// asked into L2 ahead (147).
 // Element i of a lane's 16 in the order of its registers: the first of each pair (0 to 7), then the second.
 template <bool INTERLEAVED> __device__ __forceinline__ int place(int pa, int pb, int i)
 {
@@ -486,7 +490,7 @@ static int rotate(const rp_rotary *r, i64 T, const double *freq, const i64 *star
             if (A.h[w].dw) RP_CUDA(cudaMemsetAsync(A.h[w].dw, 0, sizeof(float) * A.d, stream));
         return RP_OK;
     }
-    // Heads of whole 16-byte pieces, all rows on 16-byte boundaries: 32768 tokens of 32 + 8 heads of 128, 16 bits, take 131 us (gradient 220), by the other kernel
+    // Heads of whole 16-byte pieces, all rows on 16-byte boundaries: 32768 tokens of 32 + 8 heads of 128, 16 bits, take 129 us (gradient 220), by the other kernel
     // 522 (969); 64 tokens 5.3 us and 5.0
     bool pieces = A.d % 16 == 0 && A.d <= 512 && (A.half ? A.r % 16 == 0 : A.r % 8 == 0);
     for (int w = 0; w < 2; ++w) {

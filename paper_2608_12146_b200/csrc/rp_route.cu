@@ -9,8 +9,8 @@
 // sums over experts are shuffles.  Every such group of lanes owns a run of neighbouring tokens and carries the sums of p of the run's
 // present group of tokens in registers, its counts in shared memory; what a CTA's last runs hold meets in shared memory before it goes out.
 // Sums of p leave a CTA in fixed point (2^-36): additions of whole numbers, so their order does not matter.
-// Bound by instructions: 131072 tokens of 256 experts, k = 8, take 78 us where their bytes take 12: 420 warp instructions a token (scores of 8 experts a lane, their keys,
-// k rounds of the largest), 72 % of the issue slots, the integer units 59 %.  The gradient, 320 a token, 61 us (its bytes 22): it waits for shuffles and shared memory.
+// Bound by instructions: 131072 tokens of 256 experts, k = 8, take 80 us where their bytes take 12: 427 warp instructions a token (scores of 8 experts a lane, their keys,
+// k rounds of the largest), 73 % of the issue slots, the integer units 58 %.  The gradient, 344 a token, 64 us (its bytes 22): it waits for shuffles and shared memory.
 #include <limits.h>
 
 #include <algorithm>

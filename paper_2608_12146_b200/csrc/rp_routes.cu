@@ -65,7 +65,8 @@ __device__ __forceinline__ i64 tile_start(const CountArgs &A, int b, int n)
 // Bound by the additions: 230 million of them for those 230 MB, 58 % of what shared memory takes (52 us), 2.7 TB/s from memory of 6.5.
 // A CTA owns a tile of tokens and lanes * LAYERS layers, whatever samples the tokens belong to: it counts one sample after the other in shared memory and adds what
 // it found to the output (whole numbers: the order does not matter).  WORDS: 32-bit words of a token's choices in LAYERS layers, copied as such into a ring of the
-// lane's own, DEPTH tokens ahead, across the samples' ends; 0: any number of choices, read one by one.
+// lane's own, DEPTH tokens ahead, across the samples' ends; 0: any number of choices, read one by one (450001 tokens of 32 layers, 2 or 6 of 128 experts in bytes: 79 and
+// 120 us, where 8, copied, take 54).
 template <int WORDS> struct CountRing { static constexpr int DEPTH = WORDS <= 4 ? 4 : WORDS == 8 ? 3 : 2, BYTES = WORDS ? DEPTH * WORDS * 4 * COUNT_THREADS : 0; };
 template <typename R, int WORDS, int LAYERS>
 __global__ void __launch_bounds__(COUNT_THREADS, 2) k_count_routes(CountArgs A)
