@@ -221,7 +221,10 @@ def rp_window_load(lengths, demand, *, top_k: int, token_cap: int, dp_width: int
                    pop_size: int, edp_of_dp: Optional[Sequence[int]] = None,
                    alpha: Sequence[float] = (1.0, 1.0), beta: Sequence[float] = (0.0, 1.0),
                    min_rows: int = 0, seed: int = 0, stream=None) -> Context:
+    """``stream``: by default that of the input, where it is a CUDA tensor (torch's current one, on which it is written), or the default stream."""
     n, l, e = tuple(demand.shape)
+    if stream is None:
+        stream = next((_current_stream(x.get_device()) for x in (demand, lengths) if getattr(x, "is_cuda", False)), None)
     cfg, al, be, edp = _window_config(n, l, e, top_k, token_cap, dp_width, ep_width, pop_size, edp_of_dp, alpha, beta, min_rows, seed)
     out = C.c_void_p(None)
     st = lib().rp_window_load(C.byref(out), C.byref(cfg), _ptr(lengths), _ptr(demand), _stream_handle(stream))

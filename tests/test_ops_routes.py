@@ -266,3 +266,27 @@ def test_window_from_a_record_that_the_current_stream_still_writes():
             assert np.array_equal(np.asarray(a), np.asarray(b))
     rp.rp_destroy(got)
     rp.rp_destroy(want)
+
+
+@pytest.mark.gpu
+def test_window_from_counts_that_the_current_stream_still_makes():
+    """Record, counts and window one after the other on a stream of the caller's."""
+    import torch
+    rng = np.random.default_rng(9)
+    lengths = np.array([30, 1, 64, 17, 40, 40, 9, 55], np.int32)
+    T, L, E, k = int(lengths.sum()), 3, 16, 2
+    host, cuts = rng.integers(0, E, (T, L, k)).astype(np.uint8), [0] + np.cumsum(lengths).tolist()
+    kw = dict(top_k=k, token_cap=128, dp_width=2, ep_width=4, pop_size=8, seed=1)
+    want = rp.rp_window_load(lengths, count(host, cuts, E).astype(np.int32), **kw)
+    record, start = torch.from_numpy(host).cuda(), torch.tensor(cuts, device="cuda")
+    demand = rp.rp_count_routes(torch.zeros_like(record), start, E)
+    rp.rp_destroy(rp.rp_window_load(lengths, demand, **kw))                    # (kernels are loaded, which waits for the GPU)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda._sleep(100_000_000)                   # about 50 ms
+        rp.rp_count_routes(record, start, E, demand=demand)
+        got = rp.rp_window_load(lengths, demand, **kw)
+        for a, b in zip(rp.rp_place_experts(got), rp.rp_place_experts(want)):
+            assert np.array_equal(np.asarray(a), np.asarray(b))
+    rp.rp_destroy(got)
+    rp.rp_destroy(want)
