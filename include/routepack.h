@@ -400,6 +400,20 @@ int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const rp_view *q
                    const rp_view *lse, const rp_view *out_grad, const int64_t *start, int32_t n_samples, const rp_view *q_grad,
                    const rp_view *k_grad, const rp_view *v_grad, void *workspace, int64_t workspace_bytes, void *cuda_stream);
 
+/* Attention with a sliding window, in layers that do not see all of a sample: token i of a sample sees its tokens j <= i with i - j < window (window >= 1, itself among
+ * them) or j < sinks (the sample's first tokens, which stay visible).  For all else as rp_attend and rp_attend_grad, whose formulas, types, strides, errors and limits
+ * these are; a->causal has to be 1, sinks <= 128, n_tokens < 2^30 - 512.  Infinities and NaN in the values of a token's own sample may reach it from tokens that it does
+ * not see, as there.
+ *   workspace: rp_attend_workspace(a, n_tokens, n_samples) bytes; the gradient's is rp_attend_window_grad_workspace(a, window, sinks, n_tokens, n_samples).
+ *   The gradients of first tokens in samples longer than max(window + 127, 2048) tokens, give or take a tile, are summed over chunks of the queries, in their order, in 32 bits. */
+int rp_attend_window(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v,
+                     const int64_t *start, int32_t n_samples, const rp_view *out, const rp_view *lse, void *workspace, int64_t workspace_bytes,
+                     void *cuda_stream);
+int64_t rp_attend_window_grad_workspace(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, int32_t n_samples);
+int rp_attend_window_grad(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v,
+                          const rp_view *out, const rp_view *lse, const rp_view *out_grad, const int64_t *start, int32_t n_samples, const rp_view *q_grad,
+                          const rp_view *k_grad, const rp_view *v_grad, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
 /* Frees the context.  Its device memory goes back to a per-device cache inside the library
  * (so that the next window does not pay for allocation); rp_release_cached_memory() returns
  * that cache to the driver. */

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import operator
 import os
 import warnings
 from typing import Optional, Sequence, Tuple
@@ -31,7 +32,8 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_debug_chain_kernel", "rp_debug_chain_form",
            "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad",
            "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad", "rp_attend_workspace", "rp_attend",
-           "rp_attend_grad_workspace", "rp_attend_grad", "rp_debug_set_wait_limit")
+           "rp_attend_grad_workspace", "rp_attend_grad", "rp_attend_window", "rp_attend_window_grad_workspace",
+           "rp_attend_window_grad", "rp_debug_set_wait_limit")
 
 
 class RpError(RuntimeError):
@@ -153,6 +155,10 @@ def lib():
         L.rp_attend_grad_workspace.restype = Q
         L.rp_attend_grad_workspace.argtypes = [C.POINTER(rp_attend_config), Q, I]
         L.rp_attend_grad.argtypes = [C.POINTER(rp_attend_config), Q, W, W, W, W, W, W, V, I, W, W, W, V, Q, V]
+        L.rp_attend_window.argtypes = [C.POINTER(rp_attend_config), I, I, Q, W, W, W, V, I, W, W, V, Q, V]
+        L.rp_attend_window_grad_workspace.restype = Q
+        L.rp_attend_window_grad_workspace.argtypes = [C.POINTER(rp_attend_config), I, I, Q, I]
+        L.rp_attend_window_grad.argtypes = [C.POINTER(rp_attend_config), I, I, Q, W, W, W, W, W, W, V, I, W, W, W, V, Q, V]
         _lib = L
     return _lib
 
@@ -661,14 +667,16 @@ def _hand_out(status, space, T, torch):
         status.copy_(space[:4].view(torch.int32)) if T else status.zero_()
 
 
-def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = None, out=None, lse=None, status=None, stream=None):
-    """Attention inside the samples of a packed row: (out [n_tokens, q_heads, head_dim], lse [n_tokens, q_heads] float32).
+def _int32(x, what: str) -> int:
+    """A whole number for the C entries, what lies outside 32 bits as the next that does not (a window longer than any row, or one that is refused)."""
+    try:
+        return max(-0x80000000, min(0x7fffffff, operator.index(x)))
+    except TypeError:
+        raise ValueError(f"{what}: a whole number wanted, got {x!r}") from None
 
-    ``q`` [n_tokens, q_heads, head_dim], ``k`` and ``v`` [n_tokens, kv_heads, head_dim] of float16 or bfloat16; ``scale`` is head_dim ** -0.5 by default.
-    ``status``: [1] int32 on the GPU, receives 0, or -8 (RP_ERR_TIMEOUT) where a wait inside the kernel ran out (outputs that were not worked out are NaN then).
-    """
+
+def _attend(window, q, k, v, start, causal, scale, out, lse, status, stream):
     torch = _torch()
-    _unrecorded(torch, "rp_attend", q, k, v)
     ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
     T, H, _ = q.shape
     _dense(status, torch.int32, (1,), "status")
@@ -680,15 +688,17 @@ def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = N
         nbytes = lib().rp_attend_workspace(ref, T, n)
         space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         if T:
-            _check(lib().rp_attend(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _view(out, q, "out"), _lse_view(lse, T, H, torch),
-                                   space.data_ptr(), nbytes, queue.handle), "rp_attend")
+            args = (T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _view(out, q, "out"), _lse_view(lse, T, H, torch), space.data_ptr(), nbytes,
+                    queue.handle)
+            if window is None:
+                _check(lib().rp_attend(ref, *args), "rp_attend")
+            else:
+                _check(lib().rp_attend_window(ref, *window, *args), "rp_attend_window")
         _hand_out(status, space, T, torch)
     return out, lse
 
 
-def rp_attend_grad(out_grad, q, k, v, out, lse, start, *, causal: bool = True, scale: Optional[float] = None, q_grad=None, k_grad=None, v_grad=None,
-                   status=None, stream=None):
-    """Gradients (q_grad, k_grad, v_grad) of rp_attend from that of its output, its inputs, ``out`` and ``lse``; ``status`` as there."""
+def _attend_grad(window, out_grad, q, k, v, out, lse, start, causal, scale, q_grad, k_grad, v_grad, status, stream):
     torch = _torch()
     ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
     T, H, _ = q.shape
@@ -697,14 +707,45 @@ def rp_attend_grad(out_grad, q, k, v, out, lse, start, *, causal: bool = True, s
         q_grad = q.new_empty(q.shape) if q_grad is None else q_grad
         k_grad = k.new_empty(k.shape) if k_grad is None else k_grad
         v_grad = v.new_empty(v.shape) if v_grad is None else v_grad
-        nbytes = lib().rp_attend_grad_workspace(ref, T, n)
+        nbytes = lib().rp_attend_grad_workspace(ref, T, n) if window is None else lib().rp_attend_window_grad_workspace(ref, *window, T, n)
         space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         if T:
-            _check(lib().rp_attend_grad(ref, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), _view(out, q, "out"), _lse_view(lse, T, H, torch),
-                                        _view(out_grad, q, "out_grad"), at, n, _view(q_grad, q, "q_grad"), _view(k_grad, k, "k_grad"),
-                                        _view(v_grad, v, "v_grad"), space.data_ptr(), nbytes, queue.handle), "rp_attend_grad")
+            args = (T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), _view(out, q, "out"), _lse_view(lse, T, H, torch), _view(out_grad, q, "out_grad"), at, n,
+                    _view(q_grad, q, "q_grad"), _view(k_grad, k, "k_grad"), _view(v_grad, v, "v_grad"), space.data_ptr(), nbytes, queue.handle)
+            if window is None:
+                _check(lib().rp_attend_grad(ref, *args), "rp_attend_grad")
+            else:
+                _check(lib().rp_attend_window_grad(ref, *window, *args), "rp_attend_window_grad")
         _hand_out(status, space, T, torch)
     return q_grad, k_grad, v_grad
+
+
+def rp_attend(q, k, v, start, *, causal: bool = True, scale: Optional[float] = None, out=None, lse=None, status=None, stream=None):
+    """Attention inside the samples of a packed row: (out [n_tokens, q_heads, head_dim], lse [n_tokens, q_heads] float32).
+
+    ``q`` [n_tokens, q_heads, head_dim], ``k`` and ``v`` [n_tokens, kv_heads, head_dim] of float16 or bfloat16; ``scale`` is head_dim ** -0.5 by default.
+    ``status``: [1] int32 on the GPU, receives 0, or -8 (RP_ERR_TIMEOUT) where a wait inside the kernel ran out (outputs that were not worked out are NaN then).
+    """
+    _unrecorded(_torch(), "rp_attend", q, k, v)
+    return _attend(None, q, k, v, start, causal, scale, out, lse, status, stream)
+
+
+def rp_attend_grad(out_grad, q, k, v, out, lse, start, *, causal: bool = True, scale: Optional[float] = None, q_grad=None, k_grad=None, v_grad=None,
+                   status=None, stream=None):
+    """Gradients (q_grad, k_grad, v_grad) of rp_attend from that of its output, its inputs, ``out`` and ``lse``; ``status`` as there."""
+    return _attend_grad(None, out_grad, q, k, v, out, lse, start, causal, scale, q_grad, k_grad, v_grad, status, stream)
+
+
+def rp_attend_window(q, k, v, start, *, window: int, sinks: int = 0, scale: Optional[float] = None, out=None, lse=None, status=None, stream=None):
+    """Attention with a sliding window: token i of a sample sees its tokens j <= i with i - j < ``window`` or j < ``sinks`` (0 to 128); all else as rp_attend."""
+    _unrecorded(_torch(), "rp_attend_window", q, k, v)
+    return _attend((_int32(window, "window"), _int32(sinks, "sinks")), q, k, v, start, True, scale, out, lse, status, stream)
+
+
+def rp_attend_window_grad(out_grad, q, k, v, out, lse, start, *, window: int, sinks: int = 0, scale: Optional[float] = None, q_grad=None, k_grad=None,
+                          v_grad=None, status=None, stream=None):
+    """Gradients (q_grad, k_grad, v_grad) of rp_attend_window, as those of rp_attend."""
+    return _attend_grad((_int32(window, "window"), _int32(sinks, "sinks")), out_grad, q, k, v, out, lse, start, True, scale, q_grad, k_grad, v_grad, status, stream)
 
 
 # ---- inspection hooks -------------------------------------------------------------------

@@ -33,6 +33,7 @@ struct AttendArgs {
     const i64 *start;
     i64 T;
     int N, Hq, share, d, causal;            // share: query heads to a key head
+    int window, sinks;
     float scale;
     void *out;
     i64 o_token, o_head;
@@ -54,7 +55,7 @@ template <int D> struct FwdSmem {
     Waits waits;
 };
 
-template <typename X, int D>
+template <typename X, int D, bool WINDOW>
 __global__ void __launch_bounds__(ATTEND_THREADS, 1)
 k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttendArgs A)
 {
@@ -101,15 +102,17 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 for (int i = 0; i < tiles; ++i)
                     for (int p = 0; p < PANELS; ++p)
                         tma_load3(rp_smem(sm.q[i]) + p * PANEL, &map_q, p * 64, h, (int)t.base + t.row0 + 128 * i, rp_smem(&sm.q_full));
-                const int nk = rp_attend_tiles(t, tiles - 1, A.causal);
+                const AttendSteps w(WINDOW ? t.row0 : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
+                const int seen = rp_attend_tiles(t, tiles - 1, A.causal), nk = WINDOW ? w.steps(seen) : seen;
+                const auto tile = [&](int j) { return (int)t.base + (WINDOW ? w.tile(j) : j) * 128; };
                 for (int j = 0; j <= nk; ++j, ++fill) {
                     const u32 s = fill % STAGES, turn = fill / STAGES;
                     if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), j && j < nk ? 2 * Smem::TILE : Smem::TILE);
                     waits->copied = fill + 1;
                     for (int p = 0; p < PANELS; ++p) {
-                        if (j) tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + (j - 1) * 128, rp_smem(&sm.kv_full[s]));
-                        if (j < nk) tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
+                        if (j) tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, tile(j - 1), rp_smem(&sm.kv_full[s]));
+                        if (j < nk) tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, tile(j), rp_smem(&sm.kv_full[s]));
                     }
                 }
             }
@@ -140,11 +143,14 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 if (at < 0 || rp_uniform(waits->gave_up)) break;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
                 const int left = rp_uniform(t.len - t.row0), tiles = left > 128 ? 2 : 1, len = rp_uniform(t.len);
-                const int n0 = rp_uniform(rp_attend_tiles(t, 0, A.causal)), n1 = tiles == 2 ? rp_uniform(rp_attend_tiles(t, 1, A.causal)) : 0, nk = max(n0, n1);
+                int n0 = rp_uniform(rp_attend_tiles(t, 0, A.causal)), n1 = tiles == 2 ? rp_uniform(rp_attend_tiles(t, 1, A.causal)) : 0, skip = -1;
+                const AttendSteps w(WINDOW ? (int)rp_uniform(t.row0) : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
+                if (WINDOW) { n0 = w.steps(n0); n1 = tiles == 2 ? w.steps(n1) : 0; skip = w.skip; }
+                const int nk = max(n0, n1);
                 bar_hold(rp_smem(&sm.q_full), round & 1, waits);
                 bar_hold(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, waits);
                 scores(0, used % STAGES);
-                if (tiles == 2) scores(1, used % STAGES);
+                if (tiles == 2 && (!WINDOW || skip != 0)) scores(1, used % STAGES);
                 mma_commit(one, rp_smem(&sm.kv_empty[used % STAGES]));
                 if (nk == 1) mma_commit(one, rp_smem(&sm.q_empty));
                 ++used;
@@ -153,7 +159,8 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                     // (what is copied has mostly come when the weights have)
                     bar_hold(rp_smem(&sm.kv_full[s]), (used / STAGES) & 1, waits);
                     // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
-                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.v[s], len - j * 128, 128, lane);
+                    const int behind = len - (WINDOW ? w.tile(j) : j) * 128;
+                    if (behind < 128) rp_clear_rows<D>(sm.v[s], behind, 128, lane);
                     if (j < n0) {
                         bar_hold(rp_smem(&sm.p_full[0]), p0++ & 1, waits);
                         tmem_after();
@@ -162,11 +169,13 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                         else scores(0, s);
                     }
                     if (j < n1) {
-                        bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, waits);
-                        tmem_after();
-                        outputs(1, s, j > 0);
+                        if (!WINDOW || j != skip) {
+                            bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, waits);
+                            tmem_after();
+                            outputs(1, s, WINDOW ? j > (skip == 0) : j > 0);
+                        }
                         if (j == n1 - 1) mma_commit(one, rp_smem(&sm.o_full[1]));
-                        else scores(1, s);
+                        else if (!WINDOW || j + 1 != skip) scores(1, s);
                     }
                     mma_commit(one, rp_smem(&sm.kv_empty[s]));
                     if (j == nk - 2) mma_commit(one, rp_smem(&sm.q_empty));
@@ -189,10 +198,12 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
             const int h = at % A.Hq, r0 = t.row0 + 128 * i, r = r0 + row;
             if (r0 >= t.len) continue;
-            const int nk = rp_attend_tiles(t, i, A.causal);
+            const AttendSteps w(WINDOW ? t.row0 : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
+            const int seen = rp_attend_tiles(t, i, A.causal), nk = WINDOW ? w.steps(seen) : seen, none = WINDOW && i ? w.skip : -1, first = none == 0;
             float m = -INFINITY, l = 0.0f;
             bool ok = true;
-            for (int j = 0; j < nk; ++j) {
+            for (int j = first; j < nk; ++j) {
+                if (WINDOW && j == none) continue;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[i]), ss & 1, waits))) break;
                 ++ss;
                 tmem_after();
@@ -200,7 +211,14 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_load32(ts + 32 * c, s + 32 * c);
                 tmem_loaded();
-                if (j * 128 + 128 > t.len || (A.causal && j * 128 + 127 > r0)) {
+                if (WINDOW) {
+                    // the last key that the row sees, the first of its window, first tokens
+                    const int k0 = w.tile(j) * 128, lim = min(t.len, r + 1) - k0, from = r - A.window + 1 - k0, ahead = A.sinks - k0;
+                    if (k0 + 128 > t.len || k0 + 127 > r0 || k0 <= r0 + 127 - A.window) {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) s[c] = c < lim && (c >= from || c < ahead) ? s[c] : 0xff800000u;
+                    }
+                } else if (j * 128 + 128 > t.len || (A.causal && j * 128 + 127 > r0)) {
                     const int lim = (A.causal ? min(t.len, r + 1) : t.len) - j * 128;
 #pragma unroll
                     for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : 0xff800000u;
@@ -208,7 +226,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 float top = __uint_as_float(s[0]);
 #pragma unroll
                 for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(s[c]));
-                if (j == 0) m = top;
+                if (j == first) m = top;
                 else {
                     // (a maximum that grows by less than 2^8 stays: weights up to 256 and their sums lose nothing; -inf, as long as no score is above it, goes with the
                     // first that is; rows behind the sample's end are other samples', which do not matter)
@@ -333,11 +351,11 @@ extern "C" int64_t rp_attend_workspace(const rp_attend_config *a, int64_t n_toke
     return plan_bytes(n_tokens, n_samples, 256);
 }
 
-template <typename X, int D>
+template <typename X, int D, bool WINDOW>
 static int launch(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const AttendArgs &A, int ctas, cudaStream_t stream)
 {
     const size_t smem = sizeof(FwdSmem<D>) + 1024;
-    RP_CUDA(cudaFuncSetAttribute(k_attend<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    RP_CUDA(cudaFuncSetAttribute(k_attend<X, D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t how = {};                         // (barriers, tensor memory and maps are got ready beside the planning)
     how.gridDim = dim3((unsigned)ctas);
     how.blockDim = dim3(ATTEND_THREADS);
@@ -347,14 +365,21 @@ static int launch(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap 
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     how.attrs = &early; how.numAttrs = 1;
-    RP_CUDA(cudaLaunchKernelEx(&how, k_attend<X, D>, q, k, v, A));
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend<X, D, WINDOW>, q, k, v, A));
     return rp_op_launched();
 }
 
-extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const int64_t *start,
-                         int32_t n_samples, const rp_view *out, const rp_view *lse, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+// Limits of a window besides those of the attention: sums of a place and the window stay inside 32 bits.
+int rp_attend_check_window(const rp_attend_config *a, int window, int sinks, i64 T, int N)
 {
-    RP_TRY(rp_attend_check(a, n_tokens, n_samples));
+    RP_TRY(rp_attend_check(a, T, N));
+    if (!a->causal || window < 1 || sinks < 0) return RP_ERR_ARG;
+    return sinks > ATTEND_SINKS || T >= (1 << 30) - 512 ? RP_ERR_RANGE : RP_OK;
+}
+
+static int attend(const rp_attend_config *a, int window, int sinks, i64 n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const int64_t *start,
+                  int n_samples, const rp_view *out, const rp_view *lse, void *workspace, i64 workspace_bytes, void *cuda_stream)
+{
     if (!start || !rp_aligned(start, 8) || !workspace || !rp_aligned(workspace, 16) || workspace_bytes < rp_attend_workspace(a, n_tokens, n_samples)) return RP_ERR_ARG;
     RpOpDevice dev;
     if (n_tokens == 0) {
@@ -374,7 +399,8 @@ extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_v
     AttendHead *head = (AttendHead *)workspace;
     int2 *items = (int2 *)(head + 1);
     AttendPlan P = {};
-    P.start = (const i64 *)start; P.T = n_tokens; P.N = n_samples; P.rows = 256; P.causal = a->causal; P.by_key = 0; P.most = (int)(n_tokens / 256 + n_samples);
+    P.start = (const i64 *)start; P.T = n_tokens; P.N = n_samples; P.rows = 256; P.causal = a->causal; P.by_key = 0;
+    P.window = window; P.sinks = sinks; P.most = (int)(n_tokens / 256 + n_samples);
     P.head = head; P.items = items;
     AttendClears C = {};
     C.x[C.n++] = { out->x, out->token, out->head, a->q_heads, a->head_dim, 2 };
@@ -387,10 +413,30 @@ extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_v
     RP_TRY(rp_op_launched());
     AttendArgs A = {};
     A.head = head; A.items = items; A.start = (const i64 *)start; A.T = n_tokens; A.N = n_samples; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads;
-    A.d = a->head_dim; A.causal = a->causal; A.scale = a->scale; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
+    A.d = a->head_dim; A.causal = a->causal; A.window = window; A.sinks = sinks; A.scale = a->scale; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
     if (lse && lse->x) { A.lse = (float *)lse->x; A.l_token = lse->token; A.l_head = lse->head; }
     A.status = &head->status; A.wait_ns = (u64)g_attend_wait_ns;
     const int ctas = (int)std::min((i64)rp_op_sms(dev.device), (i64)P.most * a->q_heads);
-    if (a->type == RP_F16) return a->head_dim <= 64 ? launch<__half, 64>(mq, mk, mv, A, ctas, stream) : launch<__half, 128>(mq, mk, mv, A, ctas, stream);
-    return a->head_dim <= 64 ? launch<bf16, 64>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128>(mq, mk, mv, A, ctas, stream);
+    const bool half = a->type == RP_F16, narrow = a->head_dim <= 64;
+    if (window) {
+        if (half) return narrow ? launch<__half, 64, true>(mq, mk, mv, A, ctas, stream) : launch<__half, 128, true>(mq, mk, mv, A, ctas, stream);
+        return narrow ? launch<bf16, 64, true>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128, true>(mq, mk, mv, A, ctas, stream);
+    }
+    if (half) return narrow ? launch<__half, 64, false>(mq, mk, mv, A, ctas, stream) : launch<__half, 128, false>(mq, mk, mv, A, ctas, stream);
+    return narrow ? launch<bf16, 64, false>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128, false>(mq, mk, mv, A, ctas, stream);
+}
+
+extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const int64_t *start,
+                         int32_t n_samples, const rp_view *out, const rp_view *lse, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    RP_TRY(rp_attend_check(a, n_tokens, n_samples));
+    return attend(a, 0, 0, n_tokens, q, k, v, start, n_samples, out, lse, workspace, workspace_bytes, cuda_stream);
+}
+
+extern "C" int rp_attend_window(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v,
+                                const int64_t *start, int32_t n_samples, const rp_view *out, const rp_view *lse, void *workspace, int64_t workspace_bytes,
+                                void *cuda_stream)
+{
+    RP_TRY(rp_attend_check_window(a, window, sinks, n_tokens, n_samples));
+    return attend(a, rp_attend_window_of(window, n_tokens), sinks, n_tokens, q, k, v, start, n_samples, out, lse, workspace, workspace_bytes, cuda_stream);
 }

@@ -9,10 +9,48 @@ struct AttendPlan {
     const i64 *start;
     i64 T;
     int N, rows, causal, by_key, most;                  // most: room for items
+    int window, sinks;                                  // window 0: all that the causal order leaves
     AttendHead *head;
     int2 *items;
 };
 struct AttendClears { AttendClear x[3]; int n; };       // outputs whose rows of no sample are cleared
+
+// ---- window -----------------------------------------------------------------------------
+// Token i of a sample sees j <= i with i - j < window or j < sinks.  The first tokens lie in the sample's first tile of 128 keys (sinks <= 128).
+#define ATTEND_SINKS 128
+// What a block of queries goes through: the sample's first tile where its queries see first tokens from afar, then the tiles [lo, ..) up to its last query.
+// The block's second tile of 128 queries does not see one of those: `skip`, the first behind the first tokens' (-1: it sees them all).
+struct AttendSteps {
+    int ahead, lo, skip;                                // ahead: 1 with a tile of first tokens in front
+    __device__ __forceinline__ AttendSteps(int row0, int window, int sinks)
+    {
+        const int x = row0 - window + 1;                // the first that the block's first query sees
+        lo = max(x, 0) >> 7;
+        ahead = sinks > 0 && lo > 0;
+        skip = x >= 0 && !(sinks > 0 && lo == 0) ? ahead : -1;
+    }
+    __device__ __forceinline__ int steps(int tiles) const { return ahead + tiles - lo; }             // of queries that see keys up to tile `tiles`
+    __device__ __forceinline__ int tile(int step) const { return step < ahead ? 0 : lo + step - ahead; }
+};
+// Tiles of 128 queries that see a block of 128 keys: from the block's own on, as far as the window goes.  The first block with first tokens is seen by all: its queries
+// are shared out in chunks of as many tiles, all of the window's in the first one.
+__host__ __device__ __forceinline__ int rp_attend_chunk(int window) { const int w = ((window + 126) >> 7) + 1; return w < 16 ? 16 : w; }
+struct AttendRange {
+    int first, per;
+    __device__ __forceinline__ AttendRange(int len, int block, int chunk, int window, int sinks)
+    {
+        const int all = (len + 127) >> 7;
+        if (sinks > 0 && block == 0) {
+            const int c = rp_attend_chunk(window);
+            first = chunk * c;
+            per = min(all, first + c) - first;
+        } else {
+            first = block;
+            per = min(all, ((block * 128 + 126 + window) >> 7) + 1) - first;
+        }
+    }
+};
+__device__ __forceinline__ int rp_attend_chunks(int len, int window) { const int c = rp_attend_chunk(window); return (((len + 127) >> 7) + c - 1) / c; }
 
 // By one CTA of 1024 threads: lists the blocks of `rows` tokens of all samples, those with the most tiles of others first.
 // Work of a block: queries (by_key 0) see the keys up to them, keys (by_key 1) are seen by the queries from them on.
@@ -31,8 +69,16 @@ static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
             const int i = i0 + lane;
             const i64 lo = i < A.N ? max(A.start[i], (i64)0) : 0, hi = i < A.N ? min(A.start[i + 1], A.T) : 0;
             const int blocks = hi > lo ? (int)((hi - lo + A.rows - 1) / A.rows) : 0;
+            // (chunks of a first block behind its first one follow the blocks here, and are listed as -1, -2, ..)
+            const int all = blocks + (A.by_key && A.sinks && blocks ? rp_attend_chunks((int)(hi - lo), A.window) - 1 : 0);
             const auto take = [&](int sample, int n, int b) {
-                const int work = !A.causal ? n : A.by_key ? n - b : b + 1;
+                int work = !A.causal ? n : A.by_key ? n - b : b + 1;
+                if (A.window) {
+                    const int chunk = rp_attend_chunk(A.window);
+                    if (!A.by_key) work = AttendSteps(b * A.rows, A.window, A.sinks).steps((b + 1) * (A.rows >> 7));
+                    else if (b >= n) { work = min(chunk, n - (b - n + 1) * chunk); b = n - 1 - b; }
+                    else work = b == 0 && A.sinks ? min(n, chunk) : min(n, ((b * 128 + 126 + A.window) >> 7) + 1) - b;
+                }
                 const int bucket = PLAN_BUCKETS - 1 - min(work - 1, PLAN_BUCKETS - 1);
                 if (pass == 0) atomicAdd(&count[bucket], 1);
                 else {
@@ -40,11 +86,11 @@ static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
                     if (at < A.most) A.items[at] = make_int2(sample, b);
                 }
             };
-            if (blocks <= 4)
-                for (int b = 0; b < blocks; ++b) take(i, blocks, b);
-            for (u32 many = __ballot_sync(0xffffffffu, blocks > 4); many; many &= many - 1) {
-                const int who = __ffs((int)many) - 1, n = __shfl_sync(0xffffffffu, blocks, who);
-                for (int b = lane; b < n; b += 32) take(i0 + who, n, b);
+            if (all <= 4)
+                for (int b = 0; b < all; ++b) take(i, blocks, b);
+            for (u32 many = __ballot_sync(0xffffffffu, all > 4); many; many &= many - 1) {
+                const int who = __ffs((int)many) - 1, n = __shfl_sync(0xffffffffu, blocks, who), m = __shfl_sync(0xffffffffu, all, who);
+                for (int b = lane; b < m; b += 32) take(i0 + who, n, b);
             }
         }
         __syncthreads();
@@ -88,7 +134,9 @@ static __device__ __noinline__ void rp_attend_clear(const AttendClears &A, const
 }
 extern i64 g_attend_wait_ns;             // limit of the kernels' waits (rp_debug_set_wait_limit)
 int rp_attend_check(const rp_attend_config *a, i64 T, int N);
+int rp_attend_check_window(const rp_attend_config *a, int window, int sinks, i64 T, int N);
 int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev);
+static inline int rp_attend_window_of(int window, i64 T) { return (int)(window < T ? window : T < 1 ? 1 : T); }        // (one longer than the row is one as long as it)
 // Is one of the first `n_out` views the same memory as another of them or as one of the `n` behind them?
 static inline bool rp_attend_shared(const rp_view *const *v, int n_out, int n)
 {

@@ -19,6 +19,8 @@ struct GradArgs {
     const i64 *start;
     i64 T;
     int Hq, Hk, share, d, causal;
+    int window, sinks;
+    float *parts;                            // sums of chunks for the first tokens: [place][Hk][dv, dk][sinks][d]
     float scale;
     const float2 *stats;                     // [Hq][T]: lse / ln 2, delta
     const u32 *tops;                         // float16: [samples] square of the norm of the largest row of do, as bits
@@ -135,6 +137,27 @@ __device__ __forceinline__ void store_row(u32 at, X *out, int d, bool there, flo
     }
 }
 
+// The same in 32 bits.
+template <int D>
+__device__ __forceinline__ void store_part(u32 at, float *out, int d, bool there, float f)
+{
+#pragma unroll
+    for (int c = 0; c < D; c += 32) {
+        u32 o[32];
+        tmem_load32(at + c, o);
+        tmem_loaded();
+#pragma unroll
+        for (int x = 0; x < 32; x += 4)
+            if (there && c + x < d)
+                *(float4 *)(out + c + x) = make_float4(__uint_as_float(o[x]) * f, __uint_as_float(o[x + 1]) * f, __uint_as_float(o[x + 2]) * f, __uint_as_float(o[x + 3]) * f);
+        __syncwarp();
+    }
+}
+
+// Where a chunk of a first block's queries leaves the sums for the first tokens.  Chunks of a sample start `chunk` tokens apart and a sample with several is longer than
+// that, so no two of those that start in one stretch of as many tokens are both the first of their sample, and no two both are not.
+__host__ __device__ __forceinline__ i64 part_place(i64 base, int chunk, int tokens) { return 2 * ((base + (i64)chunk * tokens) / tokens) + (chunk > 0); }
+
 // ---------------------------------------------------------------------------------------
 // keys: dk and dv
 // ---------------------------------------------------------------------------------------
@@ -155,7 +178,25 @@ template <int D> struct KeySmem {
     Waits waits;
 };
 
-template <typename X, int D>
+// A block of keys, and the tiles of queries that see it.
+template <bool WINDOW> struct KeyItem {
+    AttendTile t;
+    int chunk, first, per;
+    __device__ __forceinline__ KeyItem(const GradArgs &A, int item) : t(A.items, A.start, A.T, item, 128), chunk(0)
+    {
+        if (!WINDOW) {
+            first = A.causal ? t.row0 >> 7 : 0;
+            per = ((t.len + 127) >> 7) - first;
+            return;
+        }
+        if (t.row0 < 0) { chunk = -t.row0 >> 7; t.row0 = 0; }
+        const AttendRange r(t.len, t.row0 >> 7, chunk, A.window, A.sinks);
+        first = r.first;
+        per = r.per;
+    }
+};
+
+template <typename X, int D, bool WINDOW>
 __global__ void __launch_bounds__(ATTEND_THREADS, 1)
 k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
               const __grid_constant__ CUtensorMap map_g, const GradArgs A)
@@ -192,8 +233,9 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             for (int n = 0; ok; ++n) {
                 const int at = rp_attend_item(n, total);
                 if (at < 0) break;
-                const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
-                const int hk = at % A.Hk, first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first;
+                const KeyItem<WINDOW> item(A, at / A.Hk);
+                const AttendTile &t = item.t;
+                const int hk = at % A.Hk, first = item.first, per = item.per;
                 if (!(ok = bar_place(n, rp_smem(&sm.kv_empty), (n - 1) & 1, waits))) break;
                 ++blocks;
                 bar_expect(rp_smem(&sm.kv_full), 2 * Smem::TILE);
@@ -224,8 +266,8 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             for (int n = 0;; ++n) {
                 const int at = rp_attend_item(n, total);
                 if (at < 0 || rp_uniform(waits->gave_up)) break;
-                const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
-                const int len = rp_uniform(t.len), first = A.causal ? (int)rp_uniform(t.row0 >> 7) : 0, per = ((len + 127) >> 7) - first, nt = per * A.share;
+                const KeyItem<WINDOW> item(A, at / A.Hk);
+                const int len = rp_uniform(item.t.len), first = (int)rp_uniform(item.first), per = (int)rp_uniform(item.per), nt = per * A.share;
                 int tile = first;                       // of queries: the next to arrive
                 // 128 keys against a tile's queries, or their values against the gradients
                 auto against = [&](u32 to, const unsigned char *keys, const unsigned char *queries, u32 bar) {
@@ -289,8 +331,9 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         for (int n = 0;; ++n) {
             const int at = rp_attend_item(n, total);
             if (at < 0) break;
-            const AttendTile t(A.items, A.start, A.T, at / A.Hk, 128);
-            const int hk = at % A.Hk, first = A.causal ? t.row0 >> 7 : 0, per = ((t.len + 127) >> 7) - first, nt = per * A.share, r = t.row0 + row;
+            const KeyItem<WINDOW> item(A, at / A.Hk);
+            const AttendTile &t = item.t;
+            const int hk = at % A.Hk, first = item.first, per = item.per, nt = per * A.share, r = t.row0 + row;
             bool ok = true;
             float c1 = 1.0f;                            // float16: the factors of ds (without the weights') and of the outputs
             if constexpr (Narrow<X>::value) c1 = ds_scale(A.tops[A.items[at / A.Hk].x]);
@@ -324,8 +367,8 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     rp_parts(rp_exp2(rp_fma(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sl2, f2{ l.x })), p[c], p[c + 1]);
                     rp_parts(rp_exp2(rp_fma(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), sl2, f2{ l.y })), p[c + 2], p[c + 3]);
                 }
-                if (q0 + 64 > t.len || (A.causal && q0 < t.row0 + 128)) {
-                    const int lo = A.causal ? r - q0 : 0, hi = t.len - q0;
+                if (q0 + 64 > t.len || (A.causal && q0 < t.row0 + 128) || (WINDOW && q0 + 63 >= t.row0 + A.window)) {
+                    const int lo = A.causal ? r - q0 : 0, hi = (WINDOW && r >= A.sinks ? min(t.len, r + A.window) : t.len) - q0;
 #pragma unroll
                     for (int c = 0; c < 64; ++c) p[c] = c >= lo && c < hi ? p[c] : 0.0f;
                 }
@@ -360,7 +403,16 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             // the first group hands over dv, the second dk
             X *out = b ? (X *)A.x[1] + (t.base + r) * A.token[1] + hk * A.hd[1] : (X *)A.x[0] + (t.base + r) * A.token[0] + hk * A.hd[0];
             const float f0 = Narrow<X>::value ? 1.0f / 32768.0f : 1.0f, f1 = Narrow<X>::value ? A.scale / c1 : A.scale;      // (c1: a power of two)
-            store_row<X, D>(tm + lanes + 256 + b * D, out, A.d, r < t.len, !ok ? NAN : b ? f1 : f0);
+            bool mine = r < t.len;
+            if (WINDOW && A.sinks > 0 && t.row0 == 0 && t.len > rp_attend_chunk(A.window) * 128) {
+                // one of several chunks: the first tokens' sums meet those of the others; the rest of the keys are seen in the first chunk alone
+                const bool ahead = mine && r < A.sinks;
+                const i64 place = part_place(t.base, item.chunk, rp_attend_chunk(A.window) * 128);
+                if (__any_sync(0xffffffffu, ahead))
+                    store_part<D>(tm + lanes + 256 + b * D, A.parts + (((place * A.Hk + hk) * 2 + b) * A.sinks + r) * A.d, A.d, ahead, !ok ? NAN : b ? f1 : f0);
+                mine = mine && !ahead && item.chunk == 0;
+            }
+            store_row<X, D>(tm + lanes + 256 + b * D, out, A.d, mine, !ok ? NAN : b ? f1 : f0);
             tmem_before();
             bar_arrive_warp(rp_smem(&sm.acc_empty), lane);
         }
@@ -389,7 +441,7 @@ template <int D> struct QuerySmem {
     Waits waits;
 };
 
-template <typename X, int D>
+template <typename X, int D, bool WINDOW>
 __global__ void __launch_bounds__(ATTEND_THREADS, 1)
 k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const GradArgs A)
 {
@@ -431,15 +483,17 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 if (at < 0) break;
                 taken = n + 1;
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
-                const int hk = at % A.Hq / A.share, nk = rp_attend_tiles(t, 0, A.causal);
+                const AttendSteps w(WINDOW ? t.row0 : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
+                const int hk = at % A.Hq / A.share, seen = rp_attend_tiles(t, 0, A.causal), nk = WINDOW ? w.steps(seen) : seen;
                 for (int j = 0; j < nk; ++j, ++fill) {
+                    const int from = (int)t.base + (WINDOW ? w.tile(j) : j) * 128;
                     const u32 s = fill % STAGES, turn = fill / STAGES;
                     if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), 2 * Smem::TILE);
                     waits->copied = fill + 1;
                     for (int p = 0; p < PANELS; ++p) {
-                        tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
-                        tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
+                        tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, from, rp_smem(&sm.kv_full[s]));
+                        tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, from, rp_smem(&sm.kv_full[s]));
                     }
                 }
             }
@@ -457,7 +511,8 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 if (at < 0 || rp_uniform(waits->gave_up)) break;
                 bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
                 const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
-                const int len = rp_uniform(t.len), nk = rp_uniform(rp_attend_tiles(t, 0, A.causal));
+                const AttendSteps w(WINDOW ? (int)rp_uniform(t.row0) : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
+                const int len = rp_uniform(t.len), seen = rp_uniform(rp_attend_tiles(t, 0, A.causal)), nk = WINDOW ? w.steps(seen) : seen;
                 // 128 queries (or gradients) against a tile's keys (or values)
                 auto against = [&](u32 to, u32 rows, const unsigned char *tile, u32 bar) {
                     const u32 b = mma_operand(rp_smem(tile), true, 0);
@@ -469,7 +524,8 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     const u32 f = base + j;
                     bar_hold(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1, waits);
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
-                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.k[f % STAGES], len - j * 128, 128, lane);
+                    const int behind = len - (WINDOW ? w.tile(j) : j) * 128;
+                    if (behind < 128) rp_clear_rows<D>(sm.k[f % STAGES], behind, 128, lane);
                 };
                 arrived(0);
                 // (who has handed over q and do has taken dq of the block before)
@@ -528,7 +584,8 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         int n = 0;
         for (; at >= 0; ++n) {
             const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
-            const int h = at % A.Hq, nk = rp_attend_tiles(t, 0, A.causal), r = t.row0 + row;
+            const AttendSteps steps(WINDOW ? t.row0 : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
+            const int h = at % A.Hq, seen = rp_attend_tiles(t, 0, A.causal), nk = WINDOW ? steps.steps(seen) : seen, r = t.row0 + row;
 #pragma unroll
             for (int c = 0; c < D / 2; c += 32) tmem_store32(tm + lanes + 384 + b * 64 + c, w + c);
             tmem_stored();
@@ -551,7 +608,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 bar_arrive_warp(rp_smem(&sm.s_empty), lane);
 #pragma unroll
                 for (int c = 0; c < 32; ++c) p[c] = rp_exp2(rp_fma(rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sl2, lse2));
-                const int k0 = j * 128 + b * 64, lim = (A.causal ? min(t.len, r + 1) : t.len) - k0;
+                const int k0 = (WINDOW ? steps.tile(j) : j) * 128 + b * 64, lim = (A.causal ? min(t.len, r + 1) : t.len) - k0;
                 if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, waits))) break;
                 tmem_after();
                 tmem_load32(td, s);
@@ -562,7 +619,15 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     const f2 dp = rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
                     p[c] = rp_mul(p[c], Narrow<X>::value ? rp_fma(dp, c2, delta2) : rp_add(dp, delta2));
                 }
-                if (k0 + 64 > t.len || (A.causal && k0 + 63 > t.row0)) {
+                if (WINDOW && k0 <= t.row0 + 127 - A.window) {
+                    const int from = r - A.window + 1 - k0, ahead = A.sinks - k0;
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        float x, y;
+                        rp_parts(p[c], x, y);
+                        s[c] = rp_pair(2 * c < lim && (2 * c >= from || 2 * c < ahead) ? x : 0.0f, 2 * c + 1 < lim && (2 * c + 1 >= from || 2 * c + 1 < ahead) ? y : 0.0f, X());
+                    }
+                } else if (k0 + 64 > t.len || (A.causal && k0 + 63 > t.row0)) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) {
                         float x, y;
@@ -621,23 +686,60 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 // launches
 // ---------------------------------------------------------------------------------------
 // Workspace: front and items of the keys' kernel, the same of the queries', statistics; for float16 norms of rows and the largest of each sample.
-static i64 plan_bytes(i64 T, int N) { return ((i64)sizeof(AttendHead) + 8 * (T / 128 + N) + 15) / 16 * 16; }
+static i64 plan_bytes(i64 T, int N, i64 more) { return ((i64)sizeof(AttendHead) + 8 * (T / 128 + N + more) + 15) / 16 * 16; }
 
+// With a window: room for the chunks of first blocks, and behind all else their sums.
+static i64 more_items(i64 T, int window, int sinks) { return sinks ? T / (128 * rp_attend_chunk(window)) : 0; }
+static i64 parts_at(const rp_attend_config *a, i64 T, int N, int window, int sinks)
+{
+    const i64 all = 2 * plan_bytes(T, N, more_items(T, window, sinks)) + 8 * T * a->q_heads + (a->type == RP_F16 ? 4 * (T * a->q_heads + N) : 0);
+    return window ? (all + 15) / 16 * 16 : all;
+}
+static i64 grad_bytes(const rp_attend_config *a, i64 T, int N, int window, int sinks)
+{
+    const i64 more = more_items(T, window, sinks);
+    return parts_at(a, T, N, window, sinks) + (more ? 2 * (more + 1) * a->kv_heads * 2 * sinks * a->head_dim * 4 : 0);
+}
 extern "C" int64_t rp_attend_grad_workspace(const rp_attend_config *a, int64_t n_tokens, int32_t n_samples)
 {
-    if (rp_attend_check(a, n_tokens, n_samples) != RP_OK) return 0;
-    return 2 * plan_bytes(n_tokens, n_samples) + 8 * n_tokens * a->q_heads + (a->type == RP_F16 ? 4 * (n_tokens * a->q_heads + n_samples) : 0);
+    return rp_attend_check(a, n_tokens, n_samples) == RP_OK ? grad_bytes(a, n_tokens, n_samples, 0, 0) : 0;
+}
+extern "C" int64_t rp_attend_window_grad_workspace(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, int32_t n_samples)
+{
+    return rp_attend_check_window(a, window, sinks, n_tokens, n_samples) == RP_OK ? grad_bytes(a, n_tokens, n_samples, rp_attend_window_of(window, n_tokens), sinks) : 0;
+}
+
+// Gradients of the first tokens that several chunks have parts of, in the order of the chunks.
+template <typename X>
+__global__ void __launch_bounds__(256) k_attend_sinks(const i64 *start, int N, i64 T, int window, int sinks, int Hk, int d, const float *parts, X *dv, X *dk, i64 v_token,
+                                                      i64 v_head, i64 k_token, i64 k_head)
+{
+    const int hk = blockIdx.y >> 1, b = blockIdx.y & 1, tokens = rp_attend_chunk(window) * 128;
+    for (int i = blockIdx.x; i < N; i += gridDim.x) {
+        const i64 base = max(start[i], (i64)0);
+        const i64 len = min(start[i + 1], T) - base;
+        if (len <= tokens) continue;
+        const int chunks = rp_attend_chunks((int)len, window);
+        for (int x = threadIdx.x; x < sinks * d; x += 256) {
+            float sum = 0.0f;
+#pragma unroll 4
+            for (int c = 0; c < chunks; ++c) sum += parts[((part_place(base, c, tokens) * Hk + hk) * 2 + b) * sinks * d + x];
+            const int r = x / d, e = x % d;
+            if (b) dk[(base + r) * k_token + hk * k_head + e] = rp_round<X>(sum);
+            else dv[(base + r) * v_token + hk * v_head + e] = rp_round<X>(sum);
+        }
+    }
 }
 
 struct GradMaps { CUtensorMap q, k, v, g; };
 
-template <typename X, int D>
-static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most, int sms, cudaStream_t stream)
+template <typename X, int D, bool WINDOW>
+static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most_keys, i64 most, int sms, cudaStream_t stream)
 {
     const size_t sk = sizeof(KeySmem<D>) + 1024, sq = sizeof(QuerySmem<D>) + 1024;
-    RP_CUDA(cudaFuncSetAttribute(k_attend_keys<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sk));
-    RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
-    k_attend_keys<X, D><<<(int)std::min((i64)sms, most * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
+    RP_CUDA(cudaFuncSetAttribute(k_attend_keys<X, D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sk));
+    RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
+    k_attend_keys<X, D, WINDOW><<<(int)std::min((i64)sms, most_keys * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
     RP_TRY(rp_op_launched());
     // (8192 tokens in three samples, 16 heads on 4, 128 wide: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 249 us, the
     // queries' 166; 398 us for the whole call.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
@@ -651,16 +753,15 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     how.attrs = &early; how.numAttrs = 1;
-    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_queries<X, D>, M.k, M.v, (const GradArgs)queries));
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_queries<X, D, WINDOW>, M.k, M.v, (const GradArgs)queries));
     return rp_op_launched();
 }
 
-extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const rp_view *out,
-                              const rp_view *lse, const rp_view *out_grad, const int64_t *start, int32_t n_samples, const rp_view *q_grad,
-                              const rp_view *k_grad, const rp_view *v_grad, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const rp_view *out,
+                       const rp_view *lse, const rp_view *out_grad, const int64_t *start, int n_samples, const rp_view *q_grad, const rp_view *k_grad,
+                       const rp_view *v_grad, void *workspace, i64 workspace_bytes, void *cuda_stream)
 {
-    RP_TRY(rp_attend_check(a, n_tokens, n_samples));
-    if (!start || !rp_aligned(start, 8) || !workspace || !rp_aligned(workspace, 16) || workspace_bytes < rp_attend_grad_workspace(a, n_tokens, n_samples)) return RP_ERR_ARG;
+    if (!start || !rp_aligned(start, 8) || !workspace || !rp_aligned(workspace, 16) || workspace_bytes < grad_bytes(a, n_tokens, n_samples, window, sinks)) return RP_ERR_ARG;
     if (!lse || !lse->x || !rp_aligned(lse->x, 4)) return RP_ERR_ARG;
     RpOpDevice dev;
     if (n_tokens == 0) {
@@ -677,7 +778,7 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     }
     RP_TRY(rp_op_enter(dev, start, workspace, lse->x));
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
-    const i64 T = n_tokens, plan = plan_bytes(T, n_samples);
+    const i64 T = n_tokens, more = more_items(T, window, sinks), plan = plan_bytes(T, n_samples, more);
     AttendHead *head[2] = { (AttendHead *)workspace, (AttendHead *)((char *)workspace + plan) };
     float2 *stats = (float2 *)((char *)workspace + 2 * plan);
     const int d = a->head_dim, Hq = a->q_heads, Hk = a->kv_heads;
@@ -693,11 +794,13 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     C.x[C.n++] = { q_grad->x, q_grad->token, q_grad->head, Hq, d, 2 };
     GradArgs G[2];
     for (int w = 0; w < 2; ++w) {
-        P[w].start = (const i64 *)start; P[w].T = T; P[w].N = n_samples; P[w].rows = 128; P[w].causal = a->causal; P[w].most = (int)(T / 128 + n_samples);
+        P[w].start = (const i64 *)start; P[w].T = T; P[w].N = n_samples; P[w].rows = 128; P[w].causal = a->causal; P[w].most = (int)(T / 128 + n_samples + (w ? 0 : more));
+        P[w].window = window; P[w].sinks = sinks;
         P[w].by_key = w == 0; P[w].head = head[w]; P[w].items = (int2 *)(head[w] + 1);
         GradArgs &A = G[w];
         A = GradArgs();
         A.items = P[w].items; A.head = head[w]; A.start = (const i64 *)start; A.T = T; A.Hq = Hq; A.Hk = Hk; A.share = Hq / Hk; A.d = d; A.causal = a->causal;
+        A.window = window; A.sinks = sinks; A.parts = (float *)((char *)workspace + parts_at(a, T, n_samples, window, sinks));
         A.scale = a->scale; A.stats = stats; A.status = &head[0]->status; A.wait_ns = (u64)g_attend_wait_ns;
     }
     G[0].x[0] = v_grad->x; G[0].token[0] = v_grad->token; G[0].hd[0] = v_grad->head;
@@ -718,6 +821,38 @@ extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const
     }
     else k_attend_prepare<bf16><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
     RP_TRY(rp_op_launched());
-    if (a->type == RP_F16) return d <= 64 ? launch<__half, 64>(M, G[0], G[1], P[0].most, sms, stream) : launch<__half, 128>(M, G[0], G[1], P[0].most, sms, stream);
-    return d <= 64 ? launch<bf16, 64>(M, G[0], G[1], P[0].most, sms, stream) : launch<bf16, 128>(M, G[0], G[1], P[0].most, sms, stream);
+    const bool half = a->type == RP_F16;
+    const i64 mk = P[0].most, mq = P[1].most;
+    if (!window) {
+        if (half) return d <= 64 ? launch<__half, 64, false>(M, G[0], G[1], mk, mq, sms, stream) : launch<__half, 128, false>(M, G[0], G[1], mk, mq, sms, stream);
+        return d <= 64 ? launch<bf16, 64, false>(M, G[0], G[1], mk, mq, sms, stream) : launch<bf16, 128, false>(M, G[0], G[1], mk, mq, sms, stream);
+    }
+    if (half) RP_TRY((d <= 64 ? launch<__half, 64, true>(M, G[0], G[1], mk, mq, sms, stream) : launch<__half, 128, true>(M, G[0], G[1], mk, mq, sms, stream)));
+    else RP_TRY((d <= 64 ? launch<bf16, 64, true>(M, G[0], G[1], mk, mq, sms, stream) : launch<bf16, 128, true>(M, G[0], G[1], mk, mq, sms, stream)));
+    if (!more) return RP_OK;
+    const dim3 grid((unsigned)std::min(n_samples, 256), 2 * Hk);
+    if (half)
+        k_attend_sinks<<<grid, 256, 0, stream>>>((const i64 *)start, n_samples, T, window, sinks, Hk, d, G[0].parts, (__half *)v_grad->x, (__half *)k_grad->x, v_grad->token,
+                                                 v_grad->head, k_grad->token, k_grad->head);
+    else
+        k_attend_sinks<<<grid, 256, 0, stream>>>((const i64 *)start, n_samples, T, window, sinks, Hk, d, G[0].parts, (bf16 *)v_grad->x, (bf16 *)k_grad->x, v_grad->token,
+                                                 v_grad->head, k_grad->token, k_grad->head);
+    return rp_op_launched();
+}
+
+extern "C" int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const rp_view *out,
+                              const rp_view *lse, const rp_view *out_grad, const int64_t *start, int32_t n_samples, const rp_view *q_grad,
+                              const rp_view *k_grad, const rp_view *v_grad, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    RP_TRY(rp_attend_check(a, n_tokens, n_samples));
+    return attend_grad(a, 0, 0, n_tokens, q, k, v, out, lse, out_grad, start, n_samples, q_grad, k_grad, v_grad, workspace, workspace_bytes, cuda_stream);
+}
+
+extern "C" int rp_attend_window_grad(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v,
+                                     const rp_view *out, const rp_view *lse, const rp_view *out_grad, const int64_t *start, int32_t n_samples, const rp_view *q_grad,
+                                     const rp_view *k_grad, const rp_view *v_grad, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    RP_TRY(rp_attend_check_window(a, window, sinks, n_tokens, n_samples));
+    return attend_grad(a, rp_attend_window_of(window, n_tokens), sinks, n_tokens, q, k, v, out, lse, out_grad, start, n_samples, q_grad, k_grad, v_grad, workspace, workspace_bytes,
+                       cuda_stream);
 }
