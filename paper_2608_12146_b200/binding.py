@@ -33,7 +33,7 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad",
            "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad", "rp_attend_workspace", "rp_attend",
            "rp_attend_grad_workspace", "rp_attend_grad", "rp_attend_window", "rp_attend_window_grad_workspace",
-           "rp_attend_window_grad", "rp_debug_set_wait_limit")
+           "rp_attend_window_grad", "rp_attend_step_workspace", "rp_attend_step", "rp_debug_set_wait_limit")
 
 
 class RpError(RuntimeError):
@@ -159,6 +159,9 @@ def lib():
         L.rp_attend_window_grad_workspace.restype = Q
         L.rp_attend_window_grad_workspace.argtypes = [C.POINTER(rp_attend_config), I, I, Q, I]
         L.rp_attend_window_grad.argtypes = [C.POINTER(rp_attend_config), I, I, Q, W, W, W, W, W, W, V, I, W, W, W, V, Q, V]
+        L.rp_attend_step_workspace.restype = Q
+        L.rp_attend_step_workspace.argtypes = [C.POINTER(rp_attend_config), I, I, Q, I]
+        L.rp_attend_step.argtypes = [C.POINTER(rp_attend_config), I, I, Q, W, W, W, V, I, V, W, W, V, Q, V]
         _lib = L
     return _lib
 
@@ -416,11 +419,11 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _unrecorded(torch, call: str, *inputs):
+def _unrecorded(torch, call: str, *inputs, back: bool = True):
     """Says so where autograd would be expected to follow a call that it does not see."""
     if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in inputs):
-        warnings.warn(f"{call}: an input needs a gradient, but autograd does not record this call and its outputs have none; call it inside a "
-                      f"torch.autograd.Function (or under torch.no_grad()) with {call}_grad for the way back", stacklevel=3)
+        how = f"call it inside a torch.autograd.Function (or under torch.no_grad()) with {call}_grad for the way back" if back else "it has no way back"
+        warnings.warn(f"{call}: an input needs a gradient, but autograd does not record this call and its outputs have none; {how}", stacklevel=3)
 
 
 def _dense(t, dtype, shape, what: str):
@@ -746,6 +749,33 @@ def rp_attend_window_grad(out_grad, q, k, v, out, lse, start, *, window: int, si
                           v_grad=None, status=None, stream=None):
     """Gradients (q_grad, k_grad, v_grad) of rp_attend_window, as those of rp_attend."""
     return _attend_grad((_int32(window, "window"), _int32(sinks, "sinks")), out_grad, q, k, v, out, lse, start, True, scale, q_grad, k_grad, v_grad, status, stream)
+
+
+def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int = 0, scale: Optional[float] = None, out=None, lse=None, stream=None):
+    """Attention of one new token of each sequence against its cache: (out [n_samples, q_heads, head_dim], lse [n_samples, q_heads] float32).
+
+    ``q`` [n_samples, q_heads, head_dim]; ``k`` and ``v`` [n_tokens, kv_heads, head_dim]: sequence i has the rows start[i] to start[i + 1], the first ``length[i]`` of
+    them filled (int64; None: all), the last of those the new token's own.  The token sees the last ``window`` filled rows (0: all) and the first ``sinks``.
+    """
+    torch = _torch()
+    _unrecorded(torch, "rp_attend_step", q, k, v, back=False)
+    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.dtype == q.dtype and v.dtype == q.dtype and k.shape[2] == q.shape[2],
+          "q [n_samples, q_heads, head_dim], k and v [n_tokens, kv_heads, head_dim] of one type and head size wanted")
+    at, n = _starts(torch, start)
+    N, H, d = q.shape
+    _need(N == n, "q: a token for each sequence wanted")
+    ref = _attention(H, k.shape[1], d, _kind(q, "q"), True, scale)[1]
+    window, sinks, T = _int32(window, "window"), _int32(sinks, "sinks"), k.shape[0]
+    with _Queue(torch, q, stream) as queue:
+        if out is None:
+            out = q.new_empty(q.shape)
+        if lse is None:
+            lse = q.new_empty((N, H), dtype=torch.float32)
+        nbytes = lib().rp_attend_step_workspace(ref, window, sinks, T, n)
+        space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
+        _check(lib().rp_attend_step(ref, window, sinks, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _dense(length, torch.int64, (n,), "length"),
+                                    _view(out, q, "out"), _lse_view(lse, N, H, torch), space.data_ptr(), nbytes, queue.handle), "rp_attend_step")
+    return out, lse
 
 
 # ---- inspection hooks -------------------------------------------------------------------
