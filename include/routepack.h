@@ -370,6 +370,21 @@ int rp_rotate_grad(const rp_rotary *r, int64_t n_tokens, const double *inv_freq,
                    const int64_t *first_position, const rp_heads *q, const rp_heads *k, void *workspace, int64_t workspace_bytes,
                    void *cuda_stream);
 
+/* Norm of each head and rotation by positions on several axes, as rows with pictures and video have them (time, height, width): as rp_rotate, but the position that turns
+ * pair p of token t is position[axis[p]][t] (int64, any sign; axis_stride and token_stride elements apart, 0 allowed), so that a sample's places start again where the
+ * table says so.  axis [rotary_dim / 2] int32; a pair whose axis is none of them is at place 0.  inv_freq [rotary_dim / 2] belongs to the pairs, whatever their axis.  All
+ * tokens are turned; rotary_dim > 0, 1 <= n_axes <= 8.  The gradient's workspace is rp_rotate_workspace(r). */
+typedef struct {
+    int32_t n_axes;
+    const int32_t *axis;
+    const int64_t *position;
+    int64_t axis_stride, token_stride;
+} rp_axes;
+int rp_rotate_axes(const rp_rotary *r, int64_t n_tokens, const double *inv_freq, const rp_axes *axes, const rp_heads *q, const rp_heads *k,
+                   void *cuda_stream);
+int rp_rotate_axes_grad(const rp_rotary *r, int64_t n_tokens, const double *inv_freq, const rp_axes *axes, const rp_heads *q, const rp_heads *k,
+                        void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
 /* Attention of the tokens of a packed row inside their samples: token t sees the tokens s of its sample (causal: s <= t).
  *   o[t][h] = sum_s softmax_s(scale * q[t][h] . k[s][h']) v[s][h'],  h' = h / (q_heads / kv_heads);  lse[t][h] = log sum_s exp(scale * q . k).
  *   Weights are rounded to `type` before their product with v (the sums they are divided by are not); sums are held in 32 bits.

@@ -33,7 +33,8 @@ EXPORTS = ("rp_window_load", "rp_place_experts", "rp_pack_rows", "rp_seed_popula
            "rp_count_routes", "rp_window_load_routes", "rp_route_workspace", "rp_route", "rp_route_grad",
            "rp_rotate", "rp_rotate_workspace", "rp_rotate_grad", "rp_attend_workspace", "rp_attend",
            "rp_attend_grad_workspace", "rp_attend_grad", "rp_attend_window", "rp_attend_window_grad_workspace",
-           "rp_attend_window_grad", "rp_attend_step_workspace", "rp_attend_step", "rp_debug_set_wait_limit")
+           "rp_attend_window_grad", "rp_attend_step_workspace", "rp_attend_step", "rp_rotate_axes", "rp_rotate_axes_grad",
+           "rp_debug_set_wait_limit")
 
 
 class RpError(RuntimeError):
@@ -78,6 +79,10 @@ class rp_heads(C.Structure):
     _fields_ = [("n_heads", C.c_int32), ("x", C.c_void_p), ("x_token", C.c_int64), ("x_head", C.c_int64),
                 ("y", C.c_void_p), ("y_token", C.c_int64), ("y_head", C.c_int64), ("weight", C.c_void_p),
                 ("y_grad", C.c_void_p), ("g_token", C.c_int64), ("g_head", C.c_int64), ("weight_grad", C.c_void_p)]
+
+
+class rp_axes(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("axis", C.c_void_p), ("position", C.c_void_p), ("axis_stride", C.c_int64), ("token_stride", C.c_int64)]
 
 
 class rp_attend_config(C.Structure):
@@ -148,6 +153,8 @@ def lib():
         L.rp_rotate_workspace.restype = Q
         L.rp_rotate_workspace.argtypes = [C.POINTER(rp_rotary)]
         L.rp_rotate_grad.argtypes = [C.POINTER(rp_rotary), Q, V, V, I, V, H, H, V, Q, V]
+        L.rp_rotate_axes.argtypes = [C.POINTER(rp_rotary), Q, V, C.POINTER(rp_axes), H, H, V]
+        L.rp_rotate_axes_grad.argtypes = [C.POINTER(rp_rotary), Q, V, C.POINTER(rp_axes), H, H, V, Q, V]
         W = C.POINTER(rp_view)
         L.rp_attend_workspace.restype = Q
         L.rp_attend_workspace.argtypes = [C.POINTER(rp_attend_config), Q, I]
@@ -572,13 +579,21 @@ def _head_strides(x, like, what: str):
     return step[0], step[1]
 
 
-def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale, outs, grads, stream):
+def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale, outs, grads, stream, axes=None):
+    """``axes``: (axis, position) in the place of ``start`` and ``first_position``."""
     torch = _torch()
     _need(q.dim() == 3 and (k is None or (k.dim() == 3 and k.dtype == q.dtype and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2])),
           "q and k: [n_tokens, n_heads, head_dim] of one type, as many tokens and one head size wanted")
     T, _, d = q.shape
     kind = _kind(q, "q")
-    at, n = _starts(torch, start)
+    if axes is None:
+        at, n = _starts(torch, start)
+    else:
+        _need(inv_freq is not None, "inv_freq: [rotary_dim / 2] wanted")
+        axis, place = axes
+        if place.dim() != 2 or place.shape[1] != T or place.dtype != torch.int64 or not place.is_cuda:
+            raise ValueError(f"position: CUDA tensor [n_axes, {T}] of int64 wanted, got {tuple(place.shape)} of {place.dtype} on {place.device}")
+        table = rp_axes(place.shape[0], _dense(axis, torch.int32, inv_freq.shape, "axis"), place.data_ptr(), *place.stride())
     w_type = next((w.dtype for w in weights if w is not None), q.dtype)
     _need(w_type == q.dtype or w_type == torch.float32, "weights: float32 or the type of q wanted")
     back = grads[0] is not None
@@ -604,19 +619,24 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
             sides[i] = C.byref(side)
         freq = None if inv_freq is None else _dense(inv_freq, torch.float64, inv_freq.shape, "inv_freq")
         r, ref = _rotary(d, 0 if inv_freq is None else 2 * inv_freq.numel(), layout, kind, _TYPES[w_type], eps, mscale)
-        args = (ref, T, freq, at, n, _dense(first_position, torch.int64, (n,), "first_position"), *sides)
+        if axes is None:
+            forward, backward, name = lib().rp_rotate, lib().rp_rotate_grad, "rp_rotate"
+            args = (ref, T, freq, at, n, _dense(first_position, torch.int64, (n,), "first_position"), *sides)
+        else:
+            forward, backward, name = lib().rp_rotate_axes, lib().rp_rotate_axes_grad, "rp_rotate_axes"
+            args = (ref, T, freq, C.byref(table), *sides)
         if not T:
             for dw in dws:
                 if dw is not None:
                     dw.zero_()
         elif not back:
-            _check(lib().rp_rotate(*args, queue.handle), "rp_rotate")
+            _check(forward(*args, queue.handle), name)
         else:
             space, nbytes = None, 0
             if dws[0] is not None or dws[1] is not None:
                 nbytes = lib().rp_rotate_workspace(ref)
                 space = q.new_empty(nbytes, dtype=torch.uint8)
-            _check(lib().rp_rotate_grad(*args, None if space is None else space.data_ptr(), nbytes, queue.handle), "rp_rotate_grad")
+            _check(backward(*args, None if space is None else space.data_ptr(), nbytes, queue.handle), name + "_grad")
     return results, dws
 
 
@@ -637,6 +657,26 @@ def rp_rotate_grad(q_out_grad, k_out_grad, q, k, inv_freq, start, *, first_posit
     _need(q_out_grad is not None and (k is None) == (k_out_grad is None), "a gradient for each of q and k wanted")
     results, dws = _rotate(q, k, inv_freq, start, first_position, (q_weight, k_weight), eps, layout, mscale, (q_grad, k_grad),
                            (q_out_grad, k_out_grad), stream)
+    return (*results, *dws)
+
+
+def rp_rotate_axes(q, k, inv_freq, axis, position, *, q_weight=None, k_weight=None, eps: float = 1e-6, layout: str = "half", mscale: float = 1.0,
+                   q_out=None, k_out=None, stream=None):
+    """rp_rotate with positions on several axes: pair p of token t is turned by position[axis[p], t] * inv_freq[p].
+
+    ``axis`` int32 [rotary_dim / 2] (what is none of the axes turns nothing), ``position`` int64 [n_axes, n_tokens] with any strides, 8 axes at most, all on the GPU.
+    """
+    _unrecorded(_torch(), "rp_rotate_axes", q, k, q_weight, k_weight)
+    results, _ = _rotate(q, k, inv_freq, None, None, (q_weight, k_weight), eps, layout, mscale, (q_out, k_out), (None, None), stream, (axis, position))
+    return tuple(results)
+
+
+def rp_rotate_axes_grad(q_out_grad, k_out_grad, q, k, inv_freq, axis, position, *, q_weight=None, k_weight=None, eps: float = 1e-6, layout: str = "half",
+                        mscale: float = 1.0, q_grad=None, k_grad=None, stream=None):
+    """Gradients of rp_rotate_axes, as those of rp_rotate."""
+    _need(q_out_grad is not None and (k is None) == (k_out_grad is None), "a gradient for each of q and k wanted")
+    results, dws = _rotate(q, k, inv_freq, None, None, (q_weight, k_weight), eps, layout, mscale, (q_grad, k_grad), (q_out_grad, k_out_grad), stream,
+                           (axis, position))
     return (*results, *dws)
 
 
