@@ -5,18 +5,17 @@
 // Bound by HBM: each visible key and value is read once, 4 * head_dim bytes for 4 * share * head_dim operations (share: query heads to a key head).  The products go
 // through the warps' matrix instruction, 16 query heads by 16 keys at a time, of which `share` rows are something: with a few rows to a tile there is nothing that
 // fuller instructions could add.
-// The keys that a sequence's token sees are cut into chunks of 256, or of a 64th of them where that is more; a chunk and a key head are a unit, and CTAs stay resident
-// and take units in turn.  The cut goes by the sequence alone, so that its bits do not depend on the others of the batch.  A warp takes every fourth tile of 16 keys through
-// a ring of its own in shared memory, which runs on into the next unit; the four meet at the unit's end.  The last CTA to be done with a sequence's head adds up its
-// chunks, in their order.
+// The keys that a sequence's token sees are cut into chunks of 128, or of a 128th of them where that is more; a chunk and a key head are a unit of one warp, which takes
+// them 16 keys at a time through a ring of its own in shared memory.  Warps stay resident and take units in turn, and the ring runs on into the next unit; no warp waits
+// for another.  The cut goes by the sequence alone, so that its bits do not depend on the others of the batch.  A second kernel adds up the chunks, in their order.
 #include <algorithm>
 
 #include "rp_attend.cuh"
 
 #define STEP_WARPS 4
 #define STEP_THREADS (32 * STEP_WARPS)
-#define STEP_CHUNK 256                   // keys of a chunk at least
-#define STEP_CHUNKS 64                   // chunks of a sequence at most
+#define STEP_CHUNK 128                   // keys of a chunk at least
+#define STEP_CHUNKS 128                  // chunks of a sequence at most
 #define STEP_ROWS 16                     // query heads of a unit at most
 
 struct StepHead { int count, pad[3]; };
@@ -26,20 +25,16 @@ struct alignas(16) StepItem { i64 base; int sample, chunk, chunks, x0, x1, ahead
 struct StepPlan {
     const i64 *start, *length;
     i64 T;
-    int N, window, sinks, most, units;                  // units: of a chunk (key heads, in groups of 16 query heads)
+    int N, window, sinks, most;
     StepHead *head;
     StepItem *items;
-    int *done;                                          // [N][units] chunks that are worked out
+    int2 *where;                                        // [N] first item and number of items
 };
 
-// CTA 0 lists the chunks, sequence after sequence; the others set the counters to 0.
+// Lists the chunks, sequence after sequence.
 __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P)
 {
     rp_let_next_launch_start();
-    if (blockIdx.x) {
-        for (i64 i = (i64)(blockIdx.x - 1) * 1024 + threadIdx.x; i < (i64)P.N * P.units; i += (i64)(gridDim.x - 1) * 1024) P.done[i] = 0;
-        return;
-    }
     __shared__ int sums[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int total = 0;
@@ -68,6 +63,7 @@ __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P)
         const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums[lane] : 0), all = __reduce_add_sync(0xffffffffu, sums[lane]);
         __syncthreads();
         const int at = total + before + x - n;
+        if (i < P.N) P.where[i] = make_int2(at, at + n <= P.most ? n : 0);
         for (int c = 0; c < n && at + c < P.most; ++c) {
             StepItem it;
             it.base = base; it.sample = i; it.chunk = c; it.chunks = n; it.x0 = c * size; it.x1 = min((c + 1) * size, seen); it.ahead = ahead; it.first = first; it.pad = 0;
@@ -81,8 +77,8 @@ __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P)
 struct StepArgs {
     const StepHead *head;
     const StepItem *items;
-    int *done;
-    int Hq, share, groups, d, units;        // groups: of 16 query heads to a key head
+    const int2 *where;
+    int N, Hq, share, groups, d, units;        // groups: of 16 query heads to a key head
     float scale;
     const void *q, *k, *v;
     i64 q_token, q_head, k_token, k_head, v_token, v_head;
@@ -131,16 +127,16 @@ template <typename X> __device__ __forceinline__ void two_pairs(float a, float b
     low = rp_pair(a - x, b - y, X());
 }
 
-// The tiles that a warp copies: its own of one unit after the other.
+// The tiles that a warp copies: those of one of its units after the other.
 struct StepCursor {
     int unit, x, x1, ahead, first;
     const char *k, *v;
-    template <typename X> __device__ __forceinline__ void open(const StepArgs &A, int total, int warp)
+    template <typename X> __device__ __forceinline__ void open(const StepArgs &A, int total)
     {
-        for (; unit < total; unit += gridDim.x) {
+        for (; unit < total; unit += gridDim.x * STEP_WARPS) {
             const StepItem it = A.items[unit / A.units];
-            x = it.x0 + 16 * warp; x1 = it.x1;
-            if (x >= x1) continue;
+            x = it.x0; x1 = it.x1;
+            if (x >= x1) continue;                      // a sequence without keys
             ahead = it.ahead; first = it.first;
             const int hk = unit % A.units / A.groups;
             k = (const char *)((const X *)A.k + it.base * A.k_token + hk * A.k_head);
@@ -151,15 +147,8 @@ struct StepCursor {
 };
 
 template <int D> struct StepSmem {
-    static constexpr int TILE = 16 * D * 2, STAGES = 12288 / TILE;       // 96 KB of keys and values, 113 KB in all: two CTAs to an SM
+    static constexpr int TILE = 16 * D * 2, STAGES = 12288 / TILE;       // 96 KB of keys and values: two CTAs to an SM
     unsigned char ring[STEP_WARPS][STAGES][2][TILE];
-    union {
-        float o[STEP_WARPS][8][D + 4];                   // the warps' sums
-        float f[STEP_ROWS][STEP_CHUNKS];                 // the chunks' factors
-    };
-    float2 top[STEP_WARPS][8];
-    float inv[STEP_ROWS];
-    int last;
 };
 
 template <typename X, int D>
@@ -172,13 +161,14 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs 
     Smem &sm = *(Smem *)raw;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const u32 ring = rp_smem(sm.ring[warp]);
+    rp_let_next_launch_start();
     rp_wait_for_launch_before();
     const int total = A.head->count * A.units;
     const float sl = A.scale * RP_LOG2E;
 
     StepCursor in;
-    in.unit = blockIdx.x;
-    in.open<X>(A, total, warp);
+    in.unit = blockIdx.x * STEP_WARPS + warp;
+    in.open<X>(A, total);
     auto copy = [&](int stage) {                         // the next tile, if there is one
         if (in.unit < total) {
             const int p = lane % PIECES;
@@ -192,14 +182,14 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs 
                 copy16(to, in.k + row * A.k_token * 2 + c, there);
                 copy16(to + Smem::TILE, in.v + row * A.v_token * 2 + c, there);
             }
-            in.x += 16 * STEP_WARPS;
-            if (in.x >= in.x1) { in.unit += gridDim.x; in.open<X>(A, total, warp); }
+            in.x += 16;
+            if (in.x >= in.x1) { in.unit += gridDim.x * STEP_WARPS; in.open<X>(A, total); }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     for (int s = 0; s < STAGES; ++s) copy(s);
     int stage = 0;
-    for (int unit = blockIdx.x; unit < total; unit += gridDim.x) {
+    for (int unit = blockIdx.x * STEP_WARPS + warp; unit < total; unit += gridDim.x * STEP_WARPS) {
         const StepItem it = A.items[unit / A.units];
         const int hg = unit % A.units, hk = hg / A.groups, h0 = hk * A.share + hg % A.groups * STEP_ROWS, rows = min(A.share - hg % A.groups * STEP_ROWS, STEP_ROWS);
         u32 q[KS][4];
@@ -216,7 +206,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs 
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
-        for (int x = it.x0 + 16 * warp; x < it.x1; x += 16 * STEP_WARPS) {
+        for (int x = it.x0; x < it.x1; x += 16) {
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
             __syncwarp();
             const u32 kt = ring + stage * 2 * Smem::TILE, vt = kt + Smem::TILE;
@@ -284,93 +274,87 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs 
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
         }
-        // The warps meet, eight heads at a time.
-        const bool whole = it.chunks == 1;
         const int item = unit / A.units;
-        for (int half = 0; half < (rows > 8 ? 2 : 1); ++half) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) *(float2 *)&sm.o[warp][g][n * 8 + t * 2] = half ? make_float2(o[n][2], o[n][3]) : make_float2(o[n][0], o[n][1]);
-            if (t == 0) sm.top[warp][g] = half ? make_float2(m[1], l[1]) : make_float2(m[0], l[0]);
-            __syncthreads();
-            for (int e = threadIdx.x * 2; e < 8 * D; e += STEP_THREADS * 2) {
-                const int r = e / D, c = e % D, h = h0 + half * 8 + r;
-                if (half * 8 + r >= rows || c >= A.d) continue;
-                float top = -INFINITY, sum = 0.0f, a = 0.0f, b = 0.0f;
+        for (int i = 0; i < 2; ++i) {
+            const int r = g + 8 * i, h = h0 + r;
+            if (r >= rows) continue;
+            if (it.chunks > 1) {
+                float *part = A.parts + ((i64)item * A.Hq + h) * A.d;
 #pragma unroll
-                for (int w = 0; w < STEP_WARPS; ++w) top = fmaxf(top, sm.top[w][r].x);
-#pragma unroll
-                for (int w = 0; w < STEP_WARPS; ++w) {
-                    const float2 y = sm.top[w][r], z = *(const float2 *)&sm.o[w][r][c];
-                    const float f = y.x == top ? 1.0f : rp_exp2(y.x - top);
-                    sum = fmaf(y.y, f, sum);
-                    a = fmaf(z.x, f, a); b = fmaf(z.y, f, b);
-                }
-                if (!whole) {
-                    *(float2 *)(A.parts + ((i64)item * A.Hq + h) * A.d + c) = make_float2(a, b);
-                    if (c == 0) A.tops[(i64)item * A.Hq + h] = make_float2(top, sum);
-                } else {
-                    const bool none = it.x1 <= it.x0;    // no key at all: nothing, and the log of nothing
-                    const float f = none ? 0.0f : 1.0f / (sum * LIFT);
-                    *(u32 *)((X *)A.out + it.sample * A.o_token + h * A.o_head + c) = rp_pair(a * f, b * f, X());
-                    if (c == 0 && A.lse) A.lse[it.sample * A.l_token + h * A.l_head] = none ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-                }
+                for (int n = 0; n < NT; ++n)
+                    if (n * 8 < A.d) *(float2 *)(part + n * 8 + t * 2) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+                if (t == 0) A.tops[(i64)item * A.Hq + h] = make_float2(m[i], l[i]);
+                continue;
             }
-            __syncthreads();
+            const bool none = it.x1 <= it.x0;            // no key at all: nothing, and the log of nothing
+            const float f = none ? 0.0f : 1.0f / (l[i] * LIFT);
+            X *out = (X *)A.out + it.sample * A.o_token + h * A.o_head;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                if (n * 8 < A.d) *(u32 *)(out + n * 8 + t * 2) = rp_pair(o[n][2 * i] * f, o[n][2 * i + 1] * f, X());
+            if (t == 0 && A.lse) A.lse[it.sample * A.l_token + h * A.l_head] = none ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
         }
-        if (whole) continue;
-        // (what this CTA's threads have written is there for the others before the count goes up)
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) sm.last = atomicAdd(A.done + (i64)it.sample * A.units + hg, 1) == it.chunks - 1;
-        __syncthreads();
-        if (!sm.last) continue;
-        __threadfence();
-        const i64 item0 = item - it.chunk;
-        for (int r = warp; r < rows; r += STEP_WARPS) {
-            float2 y[STEP_CHUNKS / 32];
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < STEP_CHUNKS / 32; ++i) {
-                const int c = i * 32 + lane;
-                y[i] = c < it.chunks ? __ldcg(A.tops + (item0 + c) * A.Hq + h0 + r) : make_float2(-INFINITY, 0.0f);
-                top = fmaxf(top, y[i].x);
-            }
-#pragma unroll
-            for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-#pragma unroll
-            for (int i = 0; i < STEP_CHUNKS / 32; ++i) {
-                const float f = y[i].x == top ? 1.0f : rp_exp2(y[i].x - top);
-                sum = fmaf(y[i].y, f, sum);
-                sm.f[r][i * 32 + lane] = f;
-            }
-#pragma unroll
-            for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-            if (lane == 0) {
-                sm.inv[r] = 1.0f / (sum * LIFT);
-                if (A.lse) A.lse[it.sample * A.l_token + (h0 + r) * A.l_head] = (top + log2f(sum)) * 0.6931471805599453f;
-            }
-        }
-        __syncthreads();
-        for (int e = threadIdx.x * 2; e < rows * A.d; e += STEP_THREADS * 2) {
-            const int r = e / A.d, c = e % A.d, h = h0 + r;
-            const float *p = A.parts + (item0 * A.Hq + h) * A.d + c;
-            float a = 0.0f, b = 0.0f;
-#pragma unroll 8
-            for (int i = 0; i < it.chunks; ++i) {
-                const float2 z = __ldcg((const float2 *)(p + (i64)i * A.Hq * A.d));
-                a = fmaf(z.x, sm.f[r][i], a); b = fmaf(z.y, sm.f[r][i], b);
-            }
-            *(u32 *)((X *)A.out + it.sample * A.o_token + h * A.o_head + c) = rp_pair(a * sm.inv[r], b * sm.inv[r], X());
-        }
-        __syncthreads();
+        __syncwarp();
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// Sequences of several chunks: a warp a query head, a lane four of its columns.
+template <typename X>
+__global__ void __launch_bounds__(STEP_THREADS) k_step_join(const StepArgs A)
+{
+    constexpr float LIFT = std::is_same<X, bf16>::value ? 1.0f : 32768.0f;
+    constexpr int MINE = STEP_CHUNKS / 32, AHEAD = 8;
+    const int lane = threadIdx.x & 31;
+    rp_wait_for_launch_before();
+    for (i64 unit = (i64)blockIdx.x * STEP_WARPS + (threadIdx.x >> 5); unit < (i64)A.N * A.Hq; unit += (i64)gridDim.x * STEP_WARPS) {
+        const int sample = (int)(unit / A.Hq), h = (int)(unit % A.Hq);
+        const int2 at = A.where[sample];
+        if (at.y <= 1) continue;
+        float2 y[MINE];
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int c = i * 32 + lane;
+            y[i] = c < at.y ? A.tops[(i64)(at.x + c) * A.Hq + h] : make_float2(-INFINITY, 0.0f);
+            top = fmaxf(top, y[i].x);
+        }
+#pragma unroll
+        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            y[i].x = y[i].x == top ? 1.0f : rp_exp2(y[i].x - top);
+            sum = fmaf(y[i].y, y[i].x, sum);
+        }
+#pragma unroll
+        for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        const int e = lane * 4;
+        const float *part = A.parts + ((i64)at.x * A.Hq + h) * A.d + (e < A.d ? e : 0);
+        float o[4] = { };
+#pragma unroll
+        for (int i = 0; i < MINE; ++i)
+            for (int c0 = i * 32; c0 < min(at.y, i * 32 + 32); c0 += AHEAD) {
+                float4 z[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) z[u] = c0 + u < at.y ? *(const float4 *)(part + (i64)(c0 + u) * A.Hq * A.d) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float f = __shfl_sync(0xffffffffu, y[i].x, (c0 + u) & 31);
+                    if (c0 + u >= at.y) continue;
+                    o[0] = fmaf(z[u].x, f, o[0]); o[1] = fmaf(z[u].y, f, o[1]); o[2] = fmaf(z[u].z, f, o[2]); o[3] = fmaf(z[u].w, f, o[3]);
+                }
+            }
+        const float f = 1.0f / (sum * LIFT);
+        if (e < A.d) *(uint2 *)((X *)A.out + sample * A.o_token + h * A.o_head + e) = make_uint2(rp_pair(o[0] * f, o[1] * f, X()), rp_pair(o[2] * f, o[3] * f, X()));
+        if (lane == 0 && A.lse) A.lse[sample * A.l_token + h * A.l_head] = (top + log2f(sum)) * 0.6931471805599453f;
+    }
 }
 
 // ---------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------
-struct StepSpace { i64 items, done, tops, parts, all; };
+struct StepSpace { i64 items, where, tops, parts, all; };
 static int step_units(const rp_attend_config *a) { return a->kv_heads * ((a->q_heads / a->kv_heads + STEP_ROWS - 1) / STEP_ROWS); }
 static i64 step_most(i64 T, int N, int window, int sinks)
 {
@@ -384,8 +368,8 @@ static StepSpace step_space(const rp_attend_config *a, i64 T, int N, int window,
     const auto up = [](i64 x) { return (x + 15) / 16 * 16; };
     StepSpace s;
     s.items = sizeof(StepHead);
-    s.done = s.items + most * (i64)sizeof(StepItem);
-    s.tops = up(s.done + 4ll * N * step_units(a));
+    s.where = s.items + most * (i64)sizeof(StepItem);
+    s.tops = up(s.where + 8ll * N);
     s.parts = up(s.tops + most * a->q_heads * 8);
     s.all = s.parts + most * a->q_heads * a->head_dim * 4;
     return s;
@@ -402,12 +386,12 @@ extern "C" int64_t rp_attend_step_workspace(const rp_attend_config *a, int32_t w
 }
 
 template <typename X, int D>
-static int launch(const StepArgs &A, i64 units, int sms, cudaStream_t stream)
+static int launch(const StepArgs &A, i64 units, bool several, int sms, cudaStream_t stream)
 {
     const size_t smem = sizeof(StepSmem<D>);
     RP_CUDA(cudaFuncSetAttribute(k_attend_step<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t how = {};
-    how.gridDim = dim3((unsigned)std::min((i64)sms * 2, units));
+    how.gridDim = dim3((unsigned)std::min((i64)sms * 2, (units + STEP_WARPS - 1) / STEP_WARPS));
     how.blockDim = dim3(STEP_THREADS);
     how.dynamicSmemBytes = smem;
     how.stream = stream;
@@ -416,6 +400,11 @@ static int launch(const StepArgs &A, i64 units, int sms, cudaStream_t stream)
     early.val.programmaticStreamSerializationAllowed = 1;
     how.attrs = &early; how.numAttrs = 1;
     RP_CUDA(cudaLaunchKernelEx(&how, k_attend_step<X, D>, A));
+    RP_TRY(rp_op_launched());
+    if (!several) return RP_OK;
+    how.gridDim = dim3((unsigned)std::min((i64)sms * 8, ((i64)A.N * A.Hq + STEP_WARPS - 1) / STEP_WARPS));
+    how.dynamicSmemBytes = 0;
+    RP_CUDA(cudaLaunchKernelEx(&how, k_step_join<X>, A));
     return rp_op_launched();
 }
 
@@ -442,18 +431,18 @@ extern "C" int rp_attend_step(const rp_attend_config *a, int32_t window, int32_t
     char *const w = (char *)workspace;
     StepPlan P = {};
     P.start = (const i64 *)start; P.length = (const i64 *)length; P.T = n_tokens; P.N = N; P.window = window; P.sinks = sinks;
-    P.most = (int)step_most(n_tokens, N, window, sinks); P.units = step_units(a); P.head = (StepHead *)w; P.items = (StepItem *)(w + space.items);
-    P.done = (int *)(w + space.done);
-    k_step_plan<<<1 + (int)std::min(((i64)N * P.units + 1023) / 1024, (i64)32), 1024, 0, stream>>>(P);
+    P.most = (int)step_most(n_tokens, N, window, sinks); P.head = (StepHead *)w; P.items = (StepItem *)(w + space.items); P.where = (int2 *)(w + space.where);
+    k_step_plan<<<1, 1024, 0, stream>>>(P);
     RP_TRY(rp_op_launched());
     StepArgs A = {};
-    A.head = P.head; A.items = P.items; A.done = P.done; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads; A.groups = P.units / a->kv_heads; A.d = a->head_dim;
-    A.units = P.units; A.scale = a->scale; A.q = q->x; A.q_token = q->token; A.q_head = q->head; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
+    A.head = P.head; A.items = P.items; A.where = P.where; A.N = N; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads; A.units = step_units(a);
+    A.groups = A.units / a->kv_heads; A.d = a->head_dim; A.scale = a->scale; A.q = q->x; A.q_token = q->token; A.q_head = q->head; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
     if (n_tokens) { A.k = k->x; A.k_token = k->token; A.k_head = k->head; A.v = v->x; A.v_token = v->token; A.v_head = v->head; }
     if (lse && lse->x) { A.lse = (float *)lse->x; A.l_token = lse->token; A.l_head = lse->head; }
     A.tops = (float2 *)(w + space.tops); A.parts = (float *)(w + space.parts);
     const int sms = rp_op_sms(dev.device);
-    const i64 units = (i64)P.most * P.units;
-    if (a->type == RP_F16) return a->head_dim <= 64 ? launch<__half, 64>(A, units, sms, stream) : launch<__half, 128>(A, units, sms, stream);
-    return a->head_dim <= 64 ? launch<bf16, 64>(A, units, sms, stream) : launch<bf16, 128>(A, units, sms, stream);
+    const i64 units = (i64)P.most * A.units;
+    const bool several = n_tokens > STEP_CHUNK && (!window || (i64)window + sinks > STEP_CHUNK);
+    if (a->type == RP_F16) return a->head_dim <= 64 ? launch<__half, 64>(A, units, several, sms, stream) : launch<__half, 128>(A, units, several, sms, stream);
+    return a->head_dim <= 64 ? launch<bf16, 64>(A, units, several, sms, stream) : launch<bf16, 128>(A, units, several, sms, stream);
 }
