@@ -433,10 +433,11 @@ int rp_attend_window_grad(const rp_attend_config *a, int32_t window, int32_t sin
  * rows start[i] .. start[i + 1] of k and v [n_tokens][kv_heads][head_dim], of which the first length[i] are filled (int64, nullable: all of them; values below 0 and above
  * the room are taken as those).  The last filled row is the new token's own.  Its query q [n_samples][q_heads][head_dim] sees the last `window` filled rows (0: all) and the
  * first `sinks` ones.
- *   o[i][h], lse[i][h] as in rp_attend; weights keep 16 bits or more in their product with v.  A sequence without filled rows gets zeros, and -inf for lse.  Rows that are
- *   not seen are not read.  A sequence's results do not depend on the others of the call.
+ *   o[i][h], lse[i][h] as in rp_attend; weights keep 16 bits or more in their product with v.  A sequence without filled rows gets zeros, and -inf for lse.  What rows
+ *   hold that are not seen, infinities and NaN too, does not matter.  A sequence's results do not depend on the others of the call.
  *   a->causal is not used; types, strides and limits as in rp_attend (n_tokens: rows of the cache); any sinks >= 0.  lse nullable.
- *   workspace: rp_attend_step_workspace(a, window, sinks, n_tokens, n_samples) bytes, 16-byte aligned; contents need not be set. */
+ *   workspace: rp_attend_step_workspace(a, window, sinks, n_tokens, n_samples) bytes, 16-byte aligned; contents need not be set.  Its first int32 is 0 when the kernels
+ *     are done, or RP_ERR_TIMEOUT, as in rp_attend. */
 int64_t rp_attend_step_workspace(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, int32_t n_samples);
 int rp_attend_step(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v,
                    const int64_t *start, int32_t n_samples, const int64_t *length, const rp_view *out, const rp_view *lse, void *workspace,

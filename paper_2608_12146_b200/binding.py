@@ -791,11 +791,13 @@ def rp_attend_window_grad(out_grad, q, k, v, out, lse, start, *, window: int, si
     return _attend_grad((_int32(window, "window"), _int32(sinks, "sinks")), out_grad, q, k, v, out, lse, start, True, scale, q_grad, k_grad, v_grad, status, stream)
 
 
-def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int = 0, scale: Optional[float] = None, out=None, lse=None, stream=None):
+def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int = 0, scale: Optional[float] = None, out=None, lse=None, status=None,
+                   stream=None):
     """Attention of one new token of each sequence against its cache: (out [n_samples, q_heads, head_dim], lse [n_samples, q_heads] float32).
 
     ``q`` [n_samples, q_heads, head_dim]; ``k`` and ``v`` [n_tokens, kv_heads, head_dim]: sequence i has the rows start[i] to start[i + 1], the first ``length[i]`` of
     them filled (int64; None: all), the last of those the new token's own.  The token sees the last ``window`` filled rows (0: all) and the first ``sinks``.
+    ``status`` as in rp_attend.
     """
     torch = _torch()
     _unrecorded(torch, "rp_attend_step", q, k, v, back=False)
@@ -806,6 +808,7 @@ def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int =
     _need(N == n, "q: a token for each sequence wanted")
     ref = _attention(H, k.shape[1], d, _kind(q, "q"), True, scale)[1]
     window, sinks, T = _int32(window, "window"), _int32(sinks, "sinks"), k.shape[0]
+    _dense(status, torch.int32, (1,), "status")
     with _Queue(torch, q, stream) as queue:
         if out is None:
             out = q.new_empty(q.shape)
@@ -815,6 +818,7 @@ def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int =
         space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         _check(lib().rp_attend_step(ref, window, sinks, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _dense(length, torch.int64, (n,), "length"),
                                     _view(out, q, "out"), _lse_view(lse, N, H, torch), space.data_ptr(), nbytes, queue.handle), "rp_attend_step")
+        _hand_out(status, space, 1, torch)
     return out, lse
 
 

@@ -18,40 +18,43 @@
 #define STEP_CHUNKS 128                  // chunks of a sequence at most
 #define STEP_ROWS 16                     // query heads of a unit at most
 
-struct StepHead { int count, pad[3]; };
-// Keys x0 to x1 of those that a token sees: the first `ahead` of its sequence, then those from `first` on.
-struct alignas(16) StepItem { i64 base; int sample, chunk, chunks, x0, x1, ahead, first, pad; };
+struct StepHead { int status, count, pad[2]; };
+// Places x0 to x1 of the keys that a token sees: the first `ahead` rows of its sequence, their number rounded up to whole tiles, then the rows from `first` on.
+struct alignas(16) StepItem { int base, sample, chunks, x0, x1, ahead, first, pad; };
 
 struct StepPlan {
     const i64 *start, *length;
     i64 T;
-    int N, window, sinks, most;
+    int N, window, sinks, most, tile;                   // tile: keys that a warp takes at a time
     StepHead *head;
     StepItem *items;
     int2 *where;                                        // [N] first item and number of items
 };
 
-// Lists the chunks, sequence after sequence.
+// Lists the chunks, sequence after sequence: a thread a sequence, then a thread a chunk.
+struct StepSeen {
+    int base, seen, ahead, first, size, n;              // n: chunks, of `size` places each
+    __device__ __forceinline__ StepSeen(const StepPlan &P, int i)
+    {
+        const i64 from = max(P.start[i], (i64)0), room = max(min(P.start[i + 1], P.T) - from, (i64)0);
+        const int filled = (int)(P.length ? min(max(P.length[i], (i64)0), room) : room);
+        base = (int)min(from, P.T);                     // (rows: less than 2^31)
+        first = P.window ? max(filled - P.window, 0) : 0;
+        ahead = min(P.sinks, first);
+        seen = (ahead + P.tile - 1) / P.tile * P.tile + filled - first;
+        size = max(STEP_CHUNK, ((seen + STEP_CHUNKS - 1) / STEP_CHUNKS + 31) & ~31);
+        n = max((seen + size - 1) / size, 1);           // (one without keys as well: it writes the outputs)
+    }
+};
 __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P)
 {
     rp_let_next_launch_start();
-    __shared__ int sums[32];
+    __shared__ int sums[32], from[1024];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int total = 0;
     for (int i0 = 0; i0 < P.N; i0 += 1024) {
         const int i = i0 + threadIdx.x;
-        i64 base = 0;
-        int n = 0, seen = 0, ahead = 0, first = 0, size = STEP_CHUNK;
-        if (i < P.N) {
-            base = max(P.start[i], (i64)0);
-            const i64 room = max(min(P.start[i + 1], P.T) - base, (i64)0);
-            const int filled = (int)(P.length ? min(max(P.length[i], (i64)0), room) : room);
-            first = P.window ? max(filled - P.window, 0) : 0;
-            ahead = min(P.sinks, first);
-            seen = ahead + filled - first;
-            size = max(STEP_CHUNK, ((seen + STEP_CHUNKS - 1) / STEP_CHUNKS + 15) & ~15);
-            n = max((seen + size - 1) / size, 1);       // (one without keys as well: it writes the outputs)
-        }
+        const int n = i < P.N ? StepSeen(P, i).n : 0;
         int x = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -61,17 +64,26 @@ __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P)
         if (lane == 31) sums[warp] = x;
         __syncthreads();
         const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums[lane] : 0), all = __reduce_add_sync(0xffffffffu, sums[lane]);
-        __syncthreads();
         const int at = total + before + x - n;
+        from[threadIdx.x] = at;
         if (i < P.N) P.where[i] = make_int2(at, at + n <= P.most ? n : 0);
-        for (int c = 0; c < n && at + c < P.most; ++c) {
+        __syncthreads();
+        for (int c = total + threadIdx.x; c < min(total + all, P.most); c += 1024) {
+            int lo = 0, hi = min(P.N - i0, 1024);       // the last sequence whose first chunk is not behind c
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (from[mid] <= c) lo = mid; else hi = mid;
+            }
+            const StepSeen S(P, i0 + lo);
             StepItem it;
-            it.base = base; it.sample = i; it.chunk = c; it.chunks = n; it.x0 = c * size; it.x1 = min((c + 1) * size, seen); it.ahead = ahead; it.first = first; it.pad = 0;
-            P.items[at + c] = it;
+            it.base = S.base; it.sample = i0 + lo; it.chunks = S.n; it.x0 = (c - from[lo]) * S.size; it.x1 = (int)min((i64)it.x0 + S.size, (i64)S.seen);
+            it.ahead = S.ahead; it.first = S.first; it.pad = 0;
+            P.items[c] = it;
         }
+        __syncthreads();
         total += all;
     }
-    if (threadIdx.x == 0) P.head->count = min(total, P.most);
+    if (threadIdx.x == 0) { P.head->count = min(total, P.most); P.head->status = 0; }
 }
 
 struct StepArgs {
@@ -80,20 +92,19 @@ struct StepArgs {
     const int2 *where;
     int N, Hq, share, groups, d, units;        // groups: of 16 query heads to a key head
     float scale;
-    const void *q, *k, *v;
-    i64 q_token, q_head, k_token, k_head, v_token, v_head;
+    const void *q;
+    i64 q_token, q_head;
     void *out;
     i64 o_token, o_head;
     float *lse;
     i64 l_token, l_head;
     float2 *tops;                            // [item][Hq] maximum and sum of a chunk
     float *parts;                            // [item][Hq][d] its values
+    int *status;
+    u64 wait_ns;
+    bool keys;                               // is there a cache at all?
 };
 
-__device__ __forceinline__ void copy16(u32 to, const void *from, bool there)         // 16 bytes, or as many zeros
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void load_matrices(u32 at, u32 *r)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -127,115 +138,149 @@ template <typename X> __device__ __forceinline__ void two_pairs(float a, float b
     low = rp_pair(a - x, b - y, X());
 }
 
-// The tiles that a warp copies: those of one of its units after the other.
-struct StepCursor {
-    int unit, x, x1, ahead, first;
-    const char *k, *v;
-    template <typename X> __device__ __forceinline__ void open(const StepArgs &A, int total)
+// A warp's units, one after the other: the words of the next one are on their way, a lane each.
+struct StepUnits {
+    int unit, next, total, words;
+    const StepArgs &A;
+    __device__ __forceinline__ StepUnits(const StepArgs &A, int first, int total) : unit(total), next(first), total(total), words(0), A(A) { fetch(); }
+    __device__ __forceinline__ void fetch() { if (next < total) words = ((const int *)(A.items + next / A.units))[threadIdx.x & 7]; }
+    __device__ __forceinline__ bool take(StepItem &it)
     {
-        for (; unit < total; unit += gridDim.x * STEP_WARPS) {
-            const StepItem it = A.items[unit / A.units];
-            x = it.x0; x1 = it.x1;
-            if (x >= x1) continue;                      // a sequence without keys
-            ahead = it.ahead; first = it.first;
-            const int hk = unit % A.units / A.groups;
-            k = (const char *)((const X *)A.k + it.base * A.k_token + hk * A.k_head);
-            v = (const char *)((const X *)A.v + it.base * A.v_token + hk * A.v_head);
-            return;
-        }
+        unit = next;
+        if (unit >= total) return false;
+        it.base = __shfl_sync(0xffffffffu, words, 0); it.sample = __shfl_sync(0xffffffffu, words, 1); it.chunks = __shfl_sync(0xffffffffu, words, 2);
+        it.x0 = __shfl_sync(0xffffffffu, words, 3); it.x1 = __shfl_sync(0xffffffffu, words, 4); it.ahead = __shfl_sync(0xffffffffu, words, 5);
+        it.first = __shfl_sync(0xffffffffu, words, 6);
+        next += gridDim.x * STEP_WARPS;
+        fetch();
+        return true;
     }
 };
 
+// A tile is 4 KB of keys and as many of values.
 template <int D> struct StepSmem {
-    static constexpr int TILE = 16 * D * 2, STAGES = 12288 / TILE;       // 96 KB of keys and values: two CTAs to an SM
-    unsigned char ring[STEP_WARPS][STAGES][2][TILE];
+    static constexpr int KEYS = 2048 / D, TILE = 4096, STAGES = 3;       // 96 KB of keys and values: two CTAs to an SM
+    alignas(1024) unsigned char ring[STEP_WARPS][STAGES][2][TILE];
+    u64 full[STEP_WARPS][STAGES];
+    Waits waits;
 };
 
-template <typename X, int D>
-__global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs A)
+// FEW: eight query heads at most, whose places the instruction's other eight rows give the weights' lower halves.
+template <typename X, int D, bool FEW>
+__global__ void __launch_bounds__(STEP_THREADS, 2)
+k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const StepArgs A)
 {
     typedef StepSmem<D> Smem;
-    constexpr int STAGES = Smem::STAGES, PIECES = D / 8, NT = D / 8, KS = D / 16;
+    constexpr int STAGES = Smem::STAGES, PANELS = D / 64, KEYS = Smem::KEYS, PANEL = KEYS * 128, NT = D / 8, KS = D / 16, NK = KEYS / 8, R = FEW ? 1 : 2;
     constexpr float LIFT = std::is_same<X, bf16>::value ? 1.0f : 32768.0f;            // float16: weights of 1 as 2^15, so that small ones stay something
-    extern __shared__ __align__(128) unsigned char raw[];
-    Smem &sm = *(Smem *)raw;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    Smem &sm = *(Smem *)(raw + ((1024 - (rp_smem(raw) & 1023)) & 1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const u32 ring = rp_smem(sm.ring[warp]);
+    const u32 ring = rp_smem(sm.ring[warp]), full = rp_smem(sm.full[warp]);
+    Waits *const waits = &sm.waits;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STEP_WARPS * STAGES; ++i) bar_init(rp_smem(&sm.full[0][0]) + 8 * i, 1);
+        waits->start(A.wait_ns);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (A.keys) { tma_prefetch(&map_k); tma_prefetch(&map_v); }
+    }
+    __syncthreads();
     rp_let_next_launch_start();
     rp_wait_for_launch_before();
-    const int total = A.head->count * A.units;
+    const int total = A.head->count * A.units, mine = blockIdx.x * STEP_WARPS + warp;
     const float sl = A.scale * RP_LOG2E;
 
-    StepCursor in;
-    in.unit = blockIdx.x * STEP_WARPS + warp;
-    in.open<X>(A, total);
+    // The tiles that the warp copies, in the order in which it takes them.
+    StepUnits in(A, mine, total);
+    StepItem to;
+    int at = 0, hk_in = 0;
+    u32 copied = 0;
+    bool some = true;
+    auto open = [&]() {                                  // the next unit with keys
+        while ((some = in.take(to)))
+            if (to.x0 < to.x1) { at = to.x0; hk_in = in.unit % A.units / A.groups; break; }
+    };
+    open();
     auto copy = [&](int stage) {                         // the next tile, if there is one
-        if (in.unit < total) {
-            const int p = lane % PIECES;
-#pragma unroll
-            for (int i = 0; i < 16 / (32 / PIECES); ++i) {
-                const int r = lane / PIECES + i * (32 / PIECES), x = min(in.x + r, in.x1 - 1);
-                const i64 row = x < in.ahead ? x : in.first + (x - in.ahead);
-                const bool there = in.x + r < in.x1 && p * 8 < A.d;
-                const u32 to = ring + stage * 2 * Smem::TILE + r * (D * 2) + ((p ^ (r & 7)) << 4);
-                const int c = there ? p * 16 : 0;
-                copy16(to, in.k + row * A.k_token * 2 + c, there);
-                copy16(to + Smem::TILE, in.v + row * A.v_token * 2 + c, there);
+        if (!some || waits->gave_up) return;
+        if (lane == 0) {
+            const int whole = (to.ahead + KEYS - 1) & ~(KEYS - 1), row = to.base + (at < whole ? at : to.first + at - whole);
+            const u32 dst = ring + stage * 2 * Smem::TILE, bar = full + 8 * stage;
+            bar_expect(bar, 2 * Smem::TILE);
+            for (int p = 0; p < PANELS; ++p) {
+                tma_load3(dst + p * PANEL, &map_k, p * 64, hk_in, row, bar);
+                tma_load3(dst + Smem::TILE + p * PANEL, &map_v, p * 64, hk_in, row, bar);
             }
-            in.x += 16;
-            if (in.x >= in.x1) { in.unit += gridDim.x * STEP_WARPS; in.open<X>(A, total); }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        ++copied;
+        if ((at += KEYS) >= to.x1) open();
     };
     for (int s = 0; s < STAGES; ++s) copy(s);
-    int stage = 0;
-    for (int unit = blockIdx.x * STEP_WARPS + warp; unit < total; unit += gridDim.x * STEP_WARPS) {
-        const StepItem it = A.items[unit / A.units];
-        const int hg = unit % A.units, hk = hg / A.groups, h0 = hk * A.share + hg % A.groups * STEP_ROWS, rows = min(A.share - hg % A.groups * STEP_ROWS, STEP_ROWS);
-        u32 q[KS][4];
-        const X *from = (const X *)A.q + it.sample * A.q_token;
+
+    u32 q[KS][2 * R];
+    auto load_q = [&](int unit, int sample) {
+        if (unit >= total) return;
+        const int hg = unit % A.units, first = hg % A.groups * STEP_ROWS, rows = min(A.share - first, STEP_ROWS);
+        const X *from = (const X *)A.q + sample * A.q_token + (hg / A.groups * A.share + first) * A.q_head;
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = g + (i & 1) * 8, c = s * 16 + t * 2 + (i >> 1) * 8;
-                q[s][i] = r < rows && c < A.d ? *(const u32 *)(from + (h0 + r) * A.q_head + c) : 0u;
+            for (int i = 0; i < 2 * R; ++i) {
+                const int r = g + i % R * 8, c = s * 16 + t * 2 + i / R * 8;
+                q[s][i] = r < rows && c < A.d ? *(const u32 *)(from + r * A.q_head + c) : 0u;
             }
+    };
+    StepUnits mines(A, mine, total);
+    StepItem it;
+    load_q(mine, __shfl_sync(0xffffffffu, mines.words, 1));
+    u32 taken = 0;
+    int stage = 0;
+    while (mines.take(it)) {
+        const int unit = mines.unit, hg = unit % A.units, hk = hg / A.groups, h0 = hk * A.share + hg % A.groups * STEP_ROWS, rows = min(A.share - hg % A.groups * STEP_ROWS, STEP_ROWS);
+        const int whole = (it.ahead + KEYS - 1) & ~(KEYS - 1);
         float o[NT][4], m[2] = { -INFINITY, -INFINITY }, l[2] = { 0.0f, 0.0f };
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
-        for (int x = it.x0; x < it.x1; x += 16) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-            __syncwarp();
+        bool ok = true;
+        for (int x = it.x0; x < it.x1; x += KEYS) {
+            if (!(ok = bar_wait_warp(full + 8 * stage, taken / STAGES & 1, waits))) break;
+            ++taken;
             const u32 kt = ring + stage * 2 * Smem::TILE, vt = kt + Smem::TILE;
-            float s[2][4] = { };
+            const int there = min(x < whole ? it.ahead - x : it.x1 - x, KEYS);           // keys of the tile; behind them may be anything
+            float s[NK][4] = { };
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                u32 b[4];
-                const int r = (lane >> 4) * 8 + (lane & 7), p = 2 * ks + ((lane >> 3) & 1);
-                load_matrices(kt + r * (D * 2) + ((p ^ (r & 7)) << 4), b);
-                multiply(s[0], q[ks], b, X());
-                multiply(s[1], q[ks], b + 2, X());
-            }
-            float top[2] = { m[0], m[1] };
+                const u32 a[4] = { q[ks][0], FEW ? 0u : q[ks][1], q[ks][R], FEW ? 0u : q[ks][2 * R - 1] };
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[n][i] = x + n * 8 + t * 2 + (i & 1) < it.x1 ? s[n][i] * sl : -INFINITY;
-                    top[i >> 1] = fmaxf(top[i >> 1], s[n][i]);
+                for (int n = 0; n < NK; n += 2) {
+                    u32 b[4];
+                    const int r = n * 8 + (lane >> 4) * 8 + (lane & 7), p = 2 * ks + ((lane >> 3) & 1);
+                    load_matrices(kt + (p >> 3) * PANEL + r * 128 + (((p & 7) ^ (r & 7)) << 4), b);
+                    multiply(s[n], a, b, X());
+                    multiply(s[n + 1], a, b + 2, X());
                 }
+            }
+            if (x + KEYS >= it.x1) load_q(mines.next, __shfl_sync(0xffffffffu, mines.words, 1));         // of the next unit, while this one is finished
+            float top[R];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < R; ++i) {
+                top[i] = m[i];
+#pragma unroll
+                for (int n = 0; n < NK; ++n)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        s[n][2 * i + j] = n * 8 + t * 2 + j < there ? s[n][2 * i + j] * sl : -INFINITY;
+                        top[i] = fmaxf(top[i], s[n][2 * i + j]);
+                    }
                 top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
                 top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
             }
-            if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
-                float f[2];
+            if (__any_sync(0xffffffffu, top[0] > m[0] || top[R - 1] > m[R - 1])) {
+                float f[R];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < R; ++i) {
                     f[i] = top[i] == m[i] ? 1.0f : rp_exp2(m[i] - top[i]);
                     l[i] *= f[i];
                     m[i] = top[i];
@@ -243,40 +288,66 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs 
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[n][i] *= f[i >> 1];
+                    for (int i = 0; i < 4; ++i) o[n][i] *= f[i / 2 % R];
             }
-            u32 high[4], low[4];
+            u32 high[NK][R], low[NK][R];
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int i = 0; i < R; ++i) {
+                const float less = m[i] == -INFINITY ? 0.0f : m[i];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float less = m[i] == -INFINITY ? 0.0f : m[i];
+                for (int n = 0; n < NK; ++n) {
                     const float a = rp_exp2(s[n][2 * i] - less), b = rp_exp2(s[n][2 * i + 1] - less);
                     l[i] += a + b;
-                    two_pairs<X>(a * LIFT, b * LIFT, high[2 * n + i], low[2 * n + i]);
+                    two_pairs<X>(a * LIFT, b * LIFT, high[n][i], low[n][i]);
                 }
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-                u32 b[4];
-                const int r = ((lane >> 3) & 1) * 8 + (lane & 7), p = n + (lane >> 4);
-                load_matrices_across(vt + r * (D * 2) + ((p ^ (r & 7)) << 4), b);
-                multiply(o[n], high, b, X());
-                multiply(o[n + 1], high, b + 2, X());
-                multiply(o[n], low, b, X());
-                multiply(o[n + 1], low, b + 2, X());
             }
+            const auto values = [&](auto part) {
+#pragma unroll
+                for (int kk = 0; kk < NK; kk += 2) {
+                    u32 keep[2] = { 0xffffffffu, 0xffffffffu };      // values behind the keys are cleared: 0 times NaN would not be 0
+                    if constexpr (decltype(part)::value) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int n = there - (kk * 8 + i * 8 + t * 2);
+                            keep[i] = n >= 2 ? 0xffffffffu : n == 1 ? 0xffffu : 0u;
+                        }
+                    }
+                    const u32 a[4] = { high[kk][0], FEW ? low[kk][0] : high[kk][R - 1], high[kk + 1][0], FEW ? low[kk + 1][0] : high[kk + 1][R - 1] };
+                    const u32 rest[4] = { low[kk][0], low[kk][R - 1], low[kk + 1][0], low[kk + 1][R - 1] };
+#pragma unroll
+                    for (int n = 0; n < NT; n += 2) {
+                        u32 b[4];
+                        const int r = kk * 8 + ((lane >> 3) & 1) * 8 + (lane & 7), p = n + (lane >> 4);
+                        load_matrices_across(vt + (p >> 3) * PANEL + r * 128 + (((p & 7) ^ (r & 7)) << 4), b);
+                        if constexpr (decltype(part)::value) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) b[i] &= keep[i & 1];
+                        }
+                        multiply(o[n], a, b, X());
+                        multiply(o[n + 1], a, b + 2, X());
+                        if (!FEW) { multiply(o[n], rest, b, X()); multiply(o[n + 1], rest, b + 2, X()); }
+                    }
+                }
+            };
+            if (there < KEYS) values(std::true_type()); else values(std::false_type());
             __syncwarp();
             copy(stage);
             stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
+        if (it.x0 >= it.x1) load_q(mines.next, __shfl_sync(0xffffffffu, mines.words, 1));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < R; ++i) {
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+            if (!ok || waits->gave_up) { l[i] = NAN; m[i] = 0.0f; }
+        }
+        if (FEW) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) { o[n][0] += o[n][2]; o[n][1] += o[n][3]; }
         }
         const int item = unit / A.units;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < R; ++i) {
             const int r = g + 8 * i, h = h0 + r;
             if (r >= rows) continue;
             if (it.chunks > 1) {
@@ -287,7 +358,7 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs 
                 if (t == 0) A.tops[(i64)item * A.Hq + h] = make_float2(m[i], l[i]);
                 continue;
             }
-            const bool none = it.x1 <= it.x0;            // no key at all: nothing, and the log of nothing
+            const bool none = it.x1 <= it.x0 && l[i] == 0.0f;        // no key at all: nothing, and the log of nothing
             const float f = none ? 0.0f : 1.0f / (l[i] * LIFT);
             X *out = (X *)A.out + it.sample * A.o_token + h * A.o_head;
 #pragma unroll
@@ -297,57 +368,76 @@ __global__ void __launch_bounds__(STEP_THREADS, 2) k_attend_step(const StepArgs 
         }
         __syncwarp();
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    // nobody may leave while copies are under way (whoever should have waited for them may have given up)
+    if (waits->gave_up) {
+        for (u32 f = taken; f < copied; ++f) rp_drain(full + 8 * (f % STAGES), f / STAGES & 1);
+        if (lane == 0) *A.status = RP_ERR_TIMEOUT;
+    }
 }
 
-// Sequences of several chunks: a warp a query head, a lane four of its columns.
+// Sequences of several chunks: a CTA a query head, each warp every fourth chunk, a lane four columns.
 template <typename X>
 __global__ void __launch_bounds__(STEP_THREADS) k_step_join(const StepArgs A)
 {
     constexpr float LIFT = std::is_same<X, bf16>::value ? 1.0f : 32768.0f;
-    constexpr int MINE = STEP_CHUNKS / 32, AHEAD = 8;
-    const int lane = threadIdx.x & 31;
+    constexpr int MINE = STEP_CHUNKS / STEP_WARPS;       // 32: a lane a chunk of the warp's
+    static_assert(MINE == 32, "a lane for each chunk of a warp");
+    __shared__ float4 part[STEP_WARPS][32];
+    __shared__ float tops[STEP_WARPS], sums[STEP_WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane * 4;
     rp_wait_for_launch_before();
-    for (i64 unit = (i64)blockIdx.x * STEP_WARPS + (threadIdx.x >> 5); unit < (i64)A.N * A.Hq; unit += (i64)gridDim.x * STEP_WARPS) {
+    for (i64 unit = blockIdx.x; unit < (i64)A.N * A.Hq; unit += gridDim.x) {
         const int sample = (int)(unit / A.Hq), h = (int)(unit % A.Hq);
         const int2 at = A.where[sample];
         if (at.y <= 1) continue;
-        float2 y[MINE];
-        float top = -INFINITY, sum = 0.0f;
+        const int mine = (at.y - warp + STEP_WARPS - 1) / STEP_WARPS;          // chunks warp, warp + 4, ..
+        const float2 y = lane < mine ? A.tops[(i64)(at.x + warp + STEP_WARPS * lane) * A.Hq + h] : make_float2(-INFINITY, 0.0f);
+        const float *from = A.parts + ((i64)(at.x + warp) * A.Hq + h) * A.d + (e < A.d ? e : 0);
+        const i64 step = (i64)STEP_WARPS * A.Hq * A.d;
+        constexpr int AHEAD = 8;
+        float4 z[AHEAD];
 #pragma unroll
-        for (int i = 0; i < MINE; ++i) {
-            const int c = i * 32 + lane;
-            y[i] = c < at.y ? A.tops[(i64)(at.x + c) * A.Hq + h] : make_float2(-INFINITY, 0.0f);
-            top = fmaxf(top, y[i].x);
-        }
+        for (int u = 0; u < AHEAD; ++u) z[u] = u < mine ? *(const float4 *)(from + u * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float top = y.x;
 #pragma unroll
         for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        if (lane == 0) tops[warp] = top;
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < MINE; ++i) {
-            y[i].x = y[i].x == top ? 1.0f : rp_exp2(y[i].x - top);
-            sum = fmaf(y[i].y, y[i].x, sum);
-        }
+        for (int w = 0; w < STEP_WARPS; ++w) top = fmaxf(top, tops[w]);
+        const float f = y.x == top ? 1.0f : rp_exp2(y.x - top);
+        float sum = y.y * f;
+        if (lane >= mine) sum = 0.0f;
 #pragma unroll
         for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-        const int e = lane * 4;
-        const float *part = A.parts + ((i64)at.x * A.Hq + h) * A.d + (e < A.d ? e : 0);
-        float o[4] = { };
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int c0 = 0; c0 < mine; c0 += AHEAD) {
 #pragma unroll
-        for (int i = 0; i < MINE; ++i)
-            for (int c0 = i * 32; c0 < min(at.y, i * 32 + 32); c0 += AHEAD) {
-                float4 z[AHEAD];
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) z[u] = c0 + u < at.y ? *(const float4 *)(part + (i64)(c0 + u) * A.Hq * A.d) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const float f = __shfl_sync(0xffffffffu, y[i].x, (c0 + u) & 31);
-                    if (c0 + u >= at.y) continue;
-                    o[0] = fmaf(z[u].x, f, o[0]); o[1] = fmaf(z[u].y, f, o[1]); o[2] = fmaf(z[u].z, f, o[2]); o[3] = fmaf(z[u].w, f, o[3]);
-                }
+            for (int u = 0; u < AHEAD; ++u) {
+                const float w = __shfl_sync(0xffffffffu, f, (c0 + u) & 31);
+                if (c0 + u < mine) { o.x = fmaf(z[u].x, w, o.x); o.y = fmaf(z[u].y, w, o.y); o.z = fmaf(z[u].z, w, o.z); o.w = fmaf(z[u].w, w, o.w); }
             }
-        const float f = 1.0f / (sum * LIFT);
-        if (e < A.d) *(uint2 *)((X *)A.out + sample * A.o_token + h * A.o_head + e) = make_uint2(rp_pair(o[0] * f, o[1] * f, X()), rp_pair(o[2] * f, o[3] * f, X()));
-        if (lane == 0 && A.lse) A.lse[sample * A.l_token + h * A.l_head] = (top + log2f(sum)) * 0.6931471805599453f;
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (c0 + AHEAD + u < mine) z[u] = *(const float4 *)(from + (c0 + AHEAD + u) * step);
+        }
+        part[warp][lane] = o;
+        if (lane == 0) sums[warp] = sum;
+        __syncthreads();
+        if (warp == 0) {
+            sum = 0.0f;
+            o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < STEP_WARPS; ++w) {
+                const float4 a = part[w][lane];
+                o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
+                sum += sums[w];
+            }
+            const float g = 1.0f / (sum * LIFT);
+            if (e < A.d) *(uint2 *)((X *)A.out + sample * A.o_token + h * A.o_head + e) = make_uint2(rp_pair(o.x * g, o.y * g, X()), rp_pair(o.z * g, o.w * g, X()));
+            if (lane == 0 && A.lse) A.lse[sample * A.l_token + h * A.l_head] = (top + log2f(sum)) * 0.6931471805599453f;
+        }
+        __syncthreads();
     }
 }
 
@@ -359,8 +449,8 @@ static int step_units(const rp_attend_config *a) { return a->kv_heads * ((a->q_h
 static i64 step_most(i64 T, int N, int window, int sinks)
 {
     i64 each = STEP_CHUNKS;
-    if (window) each = std::min(each, ((i64)window + sinks) / STEP_CHUNK + 1);
-    return std::min(T / STEP_CHUNK + N, N * each);
+    if (window) each = std::min(each, ((i64)window + sinks + 31) / STEP_CHUNK + 1);
+    return std::min((T + 31ll * N) / STEP_CHUNK + N, N * each);
 }
 static StepSpace step_space(const rp_attend_config *a, i64 T, int N, int window, int sinks)
 {
@@ -385,11 +475,11 @@ extern "C" int64_t rp_attend_step_workspace(const rp_attend_config *a, int32_t w
     return check_step(a, window, sinks, n_tokens, n_samples) == RP_OK ? step_space(a, n_tokens, n_samples, window, sinks).all : 0;
 }
 
-template <typename X, int D>
-static int launch(const StepArgs &A, i64 units, bool several, int sms, cudaStream_t stream)
+template <typename X, int D, bool FEW>
+static int launch(const CUtensorMap &k, const CUtensorMap &v, const StepArgs &A, i64 units, bool several, int sms, cudaStream_t stream)
 {
-    const size_t smem = sizeof(StepSmem<D>);
-    RP_CUDA(cudaFuncSetAttribute(k_attend_step<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const size_t smem = sizeof(StepSmem<D>) + 1024;
+    RP_CUDA(cudaFuncSetAttribute(k_attend_step<X, D, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t how = {};
     how.gridDim = dim3((unsigned)std::min((i64)sms * 2, (units + STEP_WARPS - 1) / STEP_WARPS));
     how.blockDim = dim3(STEP_THREADS);
@@ -399,10 +489,10 @@ static int launch(const StepArgs &A, i64 units, bool several, int sms, cudaStrea
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     how.attrs = &early; how.numAttrs = 1;
-    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_step<X, D>, A));
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_step<X, D, FEW>, k, v, A));
     RP_TRY(rp_op_launched());
     if (!several) return RP_OK;
-    how.gridDim = dim3((unsigned)std::min((i64)sms * 8, ((i64)A.N * A.Hq + STEP_WARPS - 1) / STEP_WARPS));
+    how.gridDim = dim3((unsigned)std::min((i64)sms * 16, (i64)A.N * A.Hq));
     how.dynamicSmemBytes = 0;
     RP_CUDA(cudaLaunchKernelEx(&how, k_step_join<X>, A));
     return rp_op_launched();
@@ -432,17 +522,30 @@ extern "C" int rp_attend_step(const rp_attend_config *a, int32_t window, int32_t
     StepPlan P = {};
     P.start = (const i64 *)start; P.length = (const i64 *)length; P.T = n_tokens; P.N = N; P.window = window; P.sinks = sinks;
     P.most = (int)step_most(n_tokens, N, window, sinks); P.head = (StepHead *)w; P.items = (StepItem *)(w + space.items); P.where = (int2 *)(w + space.where);
+    const int tile = a->head_dim <= 64 ? StepSmem<64>::KEYS : StepSmem<128>::KEYS;
+    P.tile = tile;
+    CUtensorMap mk = {}, mv = {};
+    if (n_tokens) {
+        RP_TRY(rp_tensor_map(&mk, a->type, k->x, n_tokens, a->kv_heads, a->head_dim, k->token, k->head, tile));
+        RP_TRY(rp_tensor_map(&mv, a->type, v->x, n_tokens, a->kv_heads, a->head_dim, v->token, v->head, tile));
+    }
     k_step_plan<<<1, 1024, 0, stream>>>(P);
     RP_TRY(rp_op_launched());
     StepArgs A = {};
     A.head = P.head; A.items = P.items; A.where = P.where; A.N = N; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads; A.units = step_units(a);
     A.groups = A.units / a->kv_heads; A.d = a->head_dim; A.scale = a->scale; A.q = q->x; A.q_token = q->token; A.q_head = q->head; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
-    if (n_tokens) { A.k = k->x; A.k_token = k->token; A.k_head = k->head; A.v = v->x; A.v_token = v->token; A.v_head = v->head; }
     if (lse && lse->x) { A.lse = (float *)lse->x; A.l_token = lse->token; A.l_head = lse->head; }
     A.tops = (float2 *)(w + space.tops); A.parts = (float *)(w + space.parts);
+    A.status = &P.head->status; A.wait_ns = (u64)g_attend_wait_ns; A.keys = n_tokens > 0;
     const int sms = rp_op_sms(dev.device);
     const i64 units = (i64)P.most * A.units;
-    const bool several = n_tokens > STEP_CHUNK && (!window || (i64)window + sinks > STEP_CHUNK);
-    if (a->type == RP_F16) return a->head_dim <= 64 ? launch<__half, 64>(A, units, several, sms, stream) : launch<__half, 128>(A, units, several, sms, stream);
-    return a->head_dim <= 64 ? launch<bf16, 64>(A, units, several, sms, stream) : launch<bf16, 128>(A, units, several, sms, stream);
+    const bool several = n_tokens + 31 > STEP_CHUNK && (!window || (i64)window + sinks + 31 > STEP_CHUNK);
+    // Up to eight query heads of a key head: half the exponentials and half the products with values (64 ragged sequences of 16 heads on 4: main kernel ## for ## us).
+    const bool few = A.share <= 8, narrow = a->head_dim <= 64;
+    const auto go = [&](auto type) {
+        typedef decltype(type) X;
+        if (narrow) return few ? launch<X, 64, true>(mk, mv, A, units, several, sms, stream) : launch<X, 64, false>(mk, mv, A, units, several, sms, stream);
+        return few ? launch<X, 128, true>(mk, mv, A, units, several, sms, stream) : launch<X, 128, false>(mk, mv, A, units, several, sms, stream);
+    };
+    return a->type == RP_F16 ? go(__half()) : go(bf16());
 }

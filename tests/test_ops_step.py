@@ -235,3 +235,20 @@ def test_arguments_in_python():
         rp.rp_attend_step(q, k, v, st, window=-1)
     with pytest.warns(UserWarning, match="rp_attend_step"):
         rp.rp_attend_step(q.clone().requires_grad_(True), k, v, st)
+
+
+@pytest.mark.gpu
+def test_waits_that_run_out_leave_nan_and_a_status():
+    import torch
+    q, k, v, start = inputs((8, 2, 128, [3000, 1, 0, 200], 0, 0, 0), "bfloat16")
+    st = torch.tensor(start, device="cuda")
+    status = [torch.full((1,), 7, dtype=torch.int32, device="cuda") for _ in range(3)]
+    want = rp.rp_attend_step(q, k, v, st, status=status[0])
+    rp.rp_debug_set_wait_limit(0)
+    try:
+        got = rp.rp_attend_step(q, k, v, st, status=status[1])
+        torch.cuda.synchronize()
+    finally:
+        rp.rp_debug_set_wait_limit()
+    again = rp.rp_attend_step(q, k, v, st, status=status[2])
+    assert [s.item() for s in status] == [0, -8, 0] and all(torch.isnan(x).all() for x in got) and all((a == b).all() for a, b in zip(again, want))
