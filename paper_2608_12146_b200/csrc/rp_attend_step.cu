@@ -18,43 +18,49 @@
 #define STEP_CHUNKS 128                  // chunks of a sequence at most
 #define STEP_ROWS 16                     // query heads of a unit at most
 
-struct StepHead { int status, count, pad[2]; };
-// Places x0 to x1 of the keys that a token sees: the first `ahead` rows of its sequence, their number rounded up to whole tiles, then the rows from `first` on.
-struct alignas(16) StepItem { int base, sample, chunks, x0, x1, ahead, first, pad; };
+#define STEP_TABLE 1024                  // sequences whose places a CTA works out for itself
 
+struct StepHead { int status, pad[3]; };
 struct StepPlan {
     const i64 *start, *length;
     i64 T;
-    int N, window, sinks, most, tile;                   // tile: keys that a warp takes at a time
-    StepHead *head;
-    StepItem *items;
-    int2 *where;                                        // [N] first item and number of items
+    int N, window, sinks, most, tile;        // most: room for chunks; tile: keys that a warp takes at a time
+    int *from;                               // [N + 1] chunks of the sequences before, when there are many
+    int2 *place;                             // [N] first row, rows that are filled
 };
-
-// Lists the chunks, sequence after sequence: a thread a sequence, then a thread a chunk.
+// Rows of a sequence, and how they are cut: the first `ahead` ones, their number rounded up to whole tiles, then those from `first` on.
+__device__ __forceinline__ int2 step_place(const StepPlan &P, int i)
+{
+    const i64 from = max(P.start[i], (i64)0), room = max(min(P.start[i + 1], P.T) - from, (i64)0);
+    return make_int2((int)min(from, P.T), (int)(P.length ? min(max(P.length[i], (i64)0), room) : room));          // (rows: less than 2^31)
+}
 struct StepSeen {
-    int base, seen, ahead, first, size, n;              // n: chunks, of `size` places each
-    __device__ __forceinline__ StepSeen(const StepPlan &P, int i)
+    int ahead, first, seen, size, n;         // n: chunks, of `size` places each
+    __device__ __forceinline__ StepSeen(const StepPlan &P, int filled)
     {
-        const i64 from = max(P.start[i], (i64)0), room = max(min(P.start[i + 1], P.T) - from, (i64)0);
-        const int filled = (int)(P.length ? min(max(P.length[i], (i64)0), room) : room);
-        base = (int)min(from, P.T);                     // (rows: less than 2^31)
         first = P.window ? max(filled - P.window, 0) : 0;
         ahead = min(P.sinks, first);
-        seen = (ahead + P.tile - 1) / P.tile * P.tile + filled - first;
+        seen = ((ahead + P.tile - 1) & -P.tile) + filled - first;
         size = max(STEP_CHUNK, ((seen + STEP_CHUNKS - 1) / STEP_CHUNKS + 31) & ~31);
         n = max((seen + size - 1) / size, 1);           // (one without keys as well: it writes the outputs)
     }
 };
-__global__ void __launch_bounds__(1024) k_step_plan(StepPlan P)
+
+// More sequences than a CTA has a table for, or none long enough for the second kernel: counts the chunks before each.
+__global__ void __launch_bounds__(1024) k_step_plan(StepPlan P, StepHead *head)
 {
     rp_let_next_launch_start();
-    __shared__ int sums[32], from[1024];
+    __shared__ int sums[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int total = 0;
     for (int i0 = 0; i0 < P.N; i0 += 1024) {
         const int i = i0 + threadIdx.x;
-        const int n = i < P.N ? StepSeen(P, i).n : 0;
+        int n = 0;
+        if (i < P.N) {
+            const int2 place = step_place(P, i);
+            P.place[i] = place;
+            n = StepSeen(P, place.y).n;
+        }
         int x = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -64,33 +70,18 @@ __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P)
         if (lane == 31) sums[warp] = x;
         __syncthreads();
         const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums[lane] : 0), all = __reduce_add_sync(0xffffffffu, sums[lane]);
-        const int at = total + before + x - n;
-        from[threadIdx.x] = at;
-        if (i < P.N) P.where[i] = make_int2(at, at + n <= P.most ? n : 0);
-        __syncthreads();
-        for (int c = total + threadIdx.x; c < min(total + all, P.most); c += 1024) {
-            int lo = 0, hi = min(P.N - i0, 1024);       // the last sequence whose first chunk is not behind c
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (from[mid] <= c) lo = mid; else hi = mid;
-            }
-            const StepSeen S(P, i0 + lo);
-            StepItem it;
-            it.base = S.base; it.sample = i0 + lo; it.chunks = S.n; it.x0 = (c - from[lo]) * S.size; it.x1 = (int)min((i64)it.x0 + S.size, (i64)S.seen);
-            it.ahead = S.ahead; it.first = S.first; it.pad = 0;
-            P.items[c] = it;
-        }
+        if (i < P.N) P.from[i] = total + before + x - n;
         __syncthreads();
         total += all;
     }
-    if (threadIdx.x == 0) { P.head->count = min(total, P.most); P.head->status = 0; }
+    if (threadIdx.x == 0) { P.from[P.N] = total; head->status = 0; }
 }
 
 struct StepArgs {
-    const StepHead *head;
-    const StepItem *items;
-    const int2 *where;
-    int N, Hq, share, groups, d, units;        // groups: of 16 query heads to a key head
+    StepPlan plan;
+    bool table, keys;                        // table: a CTA works out the places for itself; keys: is there a cache at all?
+    int2 *where;                             // [N] first item and number of items, for the second kernel
+    int Hq, share, groups, d, units;         // groups: of 16 query heads to a key head; units: of a chunk
     float scale;
     const void *q;
     i64 q_token, q_head;
@@ -100,9 +91,10 @@ struct StepArgs {
     i64 l_token, l_head;
     float2 *tops;                            // [item][Hq] maximum and sum of a chunk
     float *parts;                            // [item][Hq][d] its values
-    int *status;
+    StepHead *head;
+    int *states;                             // of the CTAs: whether a wait ran out
+    int ctas;
     u64 wait_ns;
-    bool keys;                               // is there a cache at all?
 };
 
 __device__ __forceinline__ void load_matrices(u32 at, u32 *r)
@@ -138,24 +130,43 @@ template <typename X> __device__ __forceinline__ void two_pairs(float a, float b
     low = rp_pair(a - x, b - y, X());
 }
 
-// A warp's units, one after the other: the words of the next one are on their way, a lane each.
-struct StepUnits {
-    int unit, next, total, words;
-    const StepArgs &A;
-    __device__ __forceinline__ StepUnits(const StepArgs &A, int first, int total) : unit(total), next(first), total(total), words(0), A(A) { fetch(); }
-    __device__ __forceinline__ void fetch() { if (next < total) words = ((const int *)(A.items + next / A.units))[threadIdx.x & 7]; }
-    __device__ __forceinline__ bool take(StepItem &it)
+// Places x0 to x1 of the keys that a token sees.
+struct StepItem { int base, sample, chunks, x0, x1, ahead, first; };
+struct StepTable {
+    const int *from;
+    const int2 *place;
+    // Chunk c of the call: the last sequence that has none behind it.  By a warp, which looks at 32 sequences at a time.
+    __device__ __forceinline__ StepItem item(const StepPlan &P, int c) const
     {
-        unit = next;
-        if (unit >= total) return false;
-        it.base = __shfl_sync(0xffffffffu, words, 0); it.sample = __shfl_sync(0xffffffffu, words, 1); it.chunks = __shfl_sync(0xffffffffu, words, 2);
-        it.x0 = __shfl_sync(0xffffffffu, words, 3); it.x1 = __shfl_sync(0xffffffffu, words, 4); it.ahead = __shfl_sync(0xffffffffu, words, 5);
-        it.first = __shfl_sync(0xffffffffu, words, 6);
-        next += gridDim.x * STEP_WARPS;
-        fetch();
-        return true;
+        const int lane = threadIdx.x & 31;
+        int lo = 0, n = P.N;
+        while (n > 1) {
+            const int step = (n + 31) >> 5;
+            const u32 hit = __ballot_sync(0xffffffffu, lane * step < n && from[lo + lane * step] <= c);
+            const int skip = (__popc(hit) - 1) * step;
+            lo += skip;
+            n = min(step, n - skip);
+        }
+        const int2 at = place[lo];
+        const StepSeen S(P, at.y);
+        StepItem it;
+        it.base = at.x; it.sample = lo; it.chunks = S.n; it.x0 = (c - from[lo]) * S.size; it.x1 = (int)min((i64)it.x0 + S.size, (i64)S.seen);
+        it.ahead = S.ahead; it.first = S.first;
+        return it;
     }
 };
+// K and V pass through once: they go out of L2 before what the second kernel reads.
+__device__ __forceinline__ u64 passing()
+{
+    u64 p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void tma_load3_passing(u32 dst, const CUtensorMap *map, int x, int y, int z, u32 bar, u64 policy)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy) : "memory");
+}
 
 // A tile is 4 KB of keys and as many of values.
 template <int D> struct StepSmem {
@@ -163,6 +174,9 @@ template <int D> struct StepSmem {
     alignas(1024) unsigned char ring[STEP_WARPS][STAGES][2][TILE];
     u64 full[STEP_WARPS][STAGES];
     Waits waits;
+    int sums[STEP_WARPS];
+    int from[STEP_TABLE + 1];
+    int2 place[STEP_TABLE];
 };
 
 // FEW: eight query heads at most, whose places the instruction's other eight rows give the weights' lower halves.
@@ -187,33 +201,77 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     __syncthreads();
     rp_let_next_launch_start();
     rp_wait_for_launch_before();
-    const int total = A.head->count * A.units, mine = blockIdx.x * STEP_WARPS + warp;
+    StepTable table = { A.plan.from, A.plan.place };
+    if (A.table) {
+        // a thread up to eight neighbouring sequences
+        constexpr int EACH = STEP_TABLE / STEP_THREADS;
+        const int each = (A.plan.N + STEP_THREADS - 1) / STEP_THREADS, i0 = threadIdx.x * each;
+        int2 place[EACH];
+        int n[EACH], own = 0;
+#pragma unroll
+        for (int u = 0; u < EACH; ++u)
+            if (u < each && i0 + u < A.plan.N) place[u] = step_place(A.plan, i0 + u);
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            n[u] = u < each && i0 + u < A.plan.N ? StepSeen(A.plan, place[u].y).n : 0;
+            own += n[u];
+        }
+        int x = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) sm.sums[warp] = x;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) x += sm.sums[w];
+        int at = x - own;
+#pragma unroll
+        for (int u = 0; u < EACH; ++u)
+            if (u < each && i0 + u < A.plan.N) {
+                sm.from[i0 + u] = at;
+                sm.place[i0 + u] = place[u];
+                if (blockIdx.x == 0) A.where[i0 + u] = make_int2(at, at + n[u] <= A.plan.most ? n[u] : 0);
+                at += n[u];
+            }
+        if (threadIdx.x == STEP_THREADS - 1) sm.from[A.plan.N] = x;
+        __syncthreads();
+        table = { sm.from, sm.place };
+    } else if (A.where)
+        for (int i = blockIdx.x * STEP_THREADS + threadIdx.x; i < A.plan.N; i += gridDim.x * STEP_THREADS) {
+            const int at = table.from[i], n = table.from[i + 1] - at;
+            A.where[i] = make_int2(at, at + n <= A.plan.most ? n : 0);
+        }
+    const int total = min(table.from[A.plan.N], A.plan.most) * A.units, mine = blockIdx.x * STEP_WARPS + warp, step = gridDim.x * STEP_WARPS;
     const float sl = A.scale * RP_LOG2E;
+    const u64 policy = passing();
 
     // The tiles that the warp copies, in the order in which it takes them.
-    StepUnits in(A, mine, total);
+    int unit_in = mine, at = 0, hk_in = 0;
     StepItem to;
-    int at = 0, hk_in = 0;
     u32 copied = 0;
-    bool some = true;
     auto open = [&]() {                                  // the next unit with keys
-        while ((some = in.take(to)))
-            if (to.x0 < to.x1) { at = to.x0; hk_in = in.unit % A.units / A.groups; break; }
+        for (; unit_in < total; unit_in += step) {
+            to = table.item(A.plan, unit_in / A.units);
+            at = to.x0;
+            hk_in = unit_in % A.units / A.groups;
+            if (to.x0 < to.x1) break;
+        }
     };
     open();
     auto copy = [&](int stage) {                         // the next tile, if there is one
-        if (!some || waits->gave_up) return;
+        if (unit_in >= total || waits->gave_up) return;
         if (lane == 0) {
             const int whole = (to.ahead + KEYS - 1) & ~(KEYS - 1), row = to.base + (at < whole ? at : to.first + at - whole);
             const u32 dst = ring + stage * 2 * Smem::TILE, bar = full + 8 * stage;
             bar_expect(bar, 2 * Smem::TILE);
             for (int p = 0; p < PANELS; ++p) {
-                tma_load3(dst + p * PANEL, &map_k, p * 64, hk_in, row, bar);
-                tma_load3(dst + Smem::TILE + p * PANEL, &map_v, p * 64, hk_in, row, bar);
+                tma_load3_passing(dst + p * PANEL, &map_k, p * 64, hk_in, row, bar, policy);
+                tma_load3_passing(dst + Smem::TILE + p * PANEL, &map_v, p * 64, hk_in, row, bar, policy);
             }
         }
         ++copied;
-        if ((at += KEYS) >= to.x1) open();
+        if ((at += KEYS) >= to.x1) { unit_in += step; open(); }
     };
     for (int s = 0; s < STAGES; ++s) copy(s);
 
@@ -230,13 +288,18 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                 q[s][i] = r < rows && c < A.d ? *(const u32 *)(from + r * A.q_head + c) : 0u;
             }
     };
-    StepUnits mines(A, mine, total);
-    StepItem it;
-    load_q(mine, __shfl_sync(0xffffffffu, mines.words, 1));
+    StepItem it = {}, next = {};
+    if (mine < total) it = table.item(A.plan, mine / A.units);
+    load_q(mine, it.sample);
+    auto look = [&](int unit) {                          // the next unit, and its queries
+        if (unit >= total) return;
+        next = table.item(A.plan, unit / A.units);
+        load_q(unit, next.sample);
+    };
     u32 taken = 0;
     int stage = 0;
-    while (mines.take(it)) {
-        const int unit = mines.unit, hg = unit % A.units, hk = hg / A.groups, h0 = hk * A.share + hg % A.groups * STEP_ROWS, rows = min(A.share - hg % A.groups * STEP_ROWS, STEP_ROWS);
+    for (int unit = mine; unit < total; unit += step, it = next) {
+        const int hg = unit % A.units, hk = hg / A.groups, h0 = hk * A.share + hg % A.groups * STEP_ROWS, rows = min(A.share - hg % A.groups * STEP_ROWS, STEP_ROWS);
         const int whole = (it.ahead + KEYS - 1) & ~(KEYS - 1);
         float o[NT][4], m[2] = { -INFINITY, -INFINITY }, l[2] = { 0.0f, 0.0f };
 #pragma unroll
@@ -262,7 +325,7 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     multiply(s[n + 1], a, b + 2, X());
                 }
             }
-            if (x + KEYS >= it.x1) load_q(mines.next, __shfl_sync(0xffffffffu, mines.words, 1));         // of the next unit, while this one is finished
+            if (x + KEYS >= it.x1) look(unit + step);        // while this one is finished
             float top[R];
 #pragma unroll
             for (int i = 0; i < R; ++i) {
@@ -334,7 +397,7 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             copy(stage);
             stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
-        if (it.x0 >= it.x1) load_q(mines.next, __shfl_sync(0xffffffffu, mines.words, 1));
+        if (it.x0 >= it.x1 || !ok) look(unit + step);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
@@ -369,9 +432,11 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         __syncwarp();
     }
     // nobody may leave while copies are under way (whoever should have waited for them may have given up)
-    if (waits->gave_up) {
-        for (u32 f = taken; f < copied; ++f) rp_drain(full + 8 * (f % STAGES), f / STAGES & 1);
-        if (lane == 0) *A.status = RP_ERR_TIMEOUT;
+    for (u32 f = taken; f < copied; ++f) rp_drain(full + 8 * (f % STAGES), f / STAGES & 1);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        if (A.where) A.states[blockIdx.x] = waits->gave_up;
+        else if (waits->gave_up) A.head->status = RP_ERR_TIMEOUT;
     }
 }
 
@@ -386,7 +451,13 @@ __global__ void __launch_bounds__(STEP_THREADS) k_step_join(const StepArgs A)
     __shared__ float tops[STEP_WARPS], sums[STEP_WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane * 4;
     rp_wait_for_launch_before();
-    for (i64 unit = blockIdx.x; unit < (i64)A.N * A.Hq; unit += gridDim.x) {
+    if (blockIdx.x == 0) {
+        int late = 0;
+        for (int i = threadIdx.x; i < A.ctas; i += STEP_THREADS) late |= A.states[i];
+        late = __syncthreads_or(late);
+        if (threadIdx.x == 0) A.head->status = late ? RP_ERR_TIMEOUT : RP_OK;
+    }
+    for (i64 unit = blockIdx.x; unit < (i64)A.plan.N * A.Hq; unit += gridDim.x) {
         const int sample = (int)(unit / A.Hq), h = (int)(unit % A.Hq);
         const int2 at = A.where[sample];
         if (at.y <= 1) continue;
@@ -444,7 +515,7 @@ __global__ void __launch_bounds__(STEP_THREADS) k_step_join(const StepArgs A)
 // ---------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------
-struct StepSpace { i64 items, where, tops, parts, all; };
+struct StepSpace { i64 states, from, place, where, tops, parts, all; };
 static int step_units(const rp_attend_config *a) { return a->kv_heads * ((a->q_heads / a->kv_heads + STEP_ROWS - 1) / STEP_ROWS); }
 static i64 step_most(i64 T, int N, int window, int sinks)
 {
@@ -452,13 +523,17 @@ static i64 step_most(i64 T, int N, int window, int sinks)
     if (window) each = std::min(each, ((i64)window + sinks + 31) / STEP_CHUNK + 1);
     return std::min((T + 31ll * N) / STEP_CHUNK + N, N * each);
 }
+static bool step_several(i64 T, int window, int sinks) { return T + 31 > STEP_CHUNK && (!window || (i64)window + sinks + 31 > STEP_CHUNK); }
+#define STEP_MOST_CTAS 512                               // (two on each of 148 SMs)
 static StepSpace step_space(const rp_attend_config *a, i64 T, int N, int window, int sinks)
 {
     const i64 most = step_most(T, N, window, sinks);
     const auto up = [](i64 x) { return (x + 15) / 16 * 16; };
     StepSpace s;
-    s.items = sizeof(StepHead);
-    s.where = s.items + most * (i64)sizeof(StepItem);
+    s.states = sizeof(StepHead);
+    s.from = s.states + 4 * STEP_MOST_CTAS;
+    s.place = up(s.from + 4ll * (N + 1));
+    s.where = s.place + 8ll * N;
     s.tops = up(s.where + 8ll * N);
     s.parts = up(s.tops + most * a->q_heads * 8);
     s.all = s.parts + most * a->q_heads * a->head_dim * 4;
@@ -476,25 +551,27 @@ extern "C" int64_t rp_attend_step_workspace(const rp_attend_config *a, int32_t w
 }
 
 template <typename X, int D, bool FEW>
-static int launch(const CUtensorMap &k, const CUtensorMap &v, const StepArgs &A, i64 units, bool several, int sms, cudaStream_t stream)
+static int launch(const CUtensorMap &k, const CUtensorMap &v, StepArgs &A, i64 units, int sms, cudaStream_t stream)
 {
     const size_t smem = sizeof(StepSmem<D>) + 1024;
     RP_CUDA(cudaFuncSetAttribute(k_attend_step<X, D, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    A.ctas = (int)std::min(std::min((i64)sms * 2, (i64)STEP_MOST_CTAS), (units + STEP_WARPS - 1) / STEP_WARPS);
     cudaLaunchConfig_t how = {};
-    how.gridDim = dim3((unsigned)std::min((i64)sms * 2, (units + STEP_WARPS - 1) / STEP_WARPS));
+    how.gridDim = dim3((unsigned)A.ctas);
     how.blockDim = dim3(STEP_THREADS);
     how.dynamicSmemBytes = smem;
     how.stream = stream;
     cudaLaunchAttribute early = {};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
-    how.attrs = &early; how.numAttrs = 1;
-    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_step<X, D, FEW>, k, v, A));
+    how.attrs = &early; how.numAttrs = A.table ? 0 : 1;                  // (behind the plan)
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_step<X, D, FEW>, k, v, (const StepArgs)A));
     RP_TRY(rp_op_launched());
-    if (!several) return RP_OK;
-    how.gridDim = dim3((unsigned)std::min((i64)sms * 16, (i64)A.N * A.Hq));
+    if (!A.where) return RP_OK;
+    how.gridDim = dim3((unsigned)std::min((i64)sms * 16, (i64)A.plan.N * A.Hq));
     how.dynamicSmemBytes = 0;
-    RP_CUDA(cudaLaunchKernelEx(&how, k_step_join<X>, A));
+    how.numAttrs = 1;
+    RP_CUDA(cudaLaunchKernelEx(&how, k_step_join<X>, (const StepArgs)A));
     return rp_op_launched();
 }
 
@@ -519,33 +596,37 @@ extern "C" int rp_attend_step(const rp_attend_config *a, int32_t window, int32_t
     RP_TRY(rp_op_enter(dev, start, length, workspace, lse ? lse->x : nullptr));
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
     char *const w = (char *)workspace;
-    StepPlan P = {};
-    P.start = (const i64 *)start; P.length = (const i64 *)length; P.T = n_tokens; P.N = N; P.window = window; P.sinks = sinks;
-    P.most = (int)step_most(n_tokens, N, window, sinks); P.head = (StepHead *)w; P.items = (StepItem *)(w + space.items); P.where = (int2 *)(w + space.where);
+    const bool several = step_several(n_tokens, window, sinks);
     const int tile = a->head_dim <= 64 ? StepSmem<64>::KEYS : StepSmem<128>::KEYS;
-    P.tile = tile;
+    StepArgs A = {};
+    StepPlan &P = A.plan;
+    P.start = (const i64 *)start; P.length = (const i64 *)length; P.T = n_tokens; P.N = N; P.window = window; P.sinks = sinks;
+    P.most = (int)step_most(n_tokens, N, window, sinks); P.tile = tile; P.from = (int *)(w + space.from); P.place = (int2 *)(w + space.place);
+    A.table = several && N <= STEP_TABLE;
+    A.where = several ? (int2 *)(w + space.where) : nullptr;
+    A.head = (StepHead *)w; A.states = (int *)(w + space.states);
     CUtensorMap mk = {}, mv = {};
     if (n_tokens) {
         RP_TRY(rp_tensor_map(&mk, a->type, k->x, n_tokens, a->kv_heads, a->head_dim, k->token, k->head, tile));
         RP_TRY(rp_tensor_map(&mv, a->type, v->x, n_tokens, a->kv_heads, a->head_dim, v->token, v->head, tile));
     }
-    k_step_plan<<<1, 1024, 0, stream>>>(P);
-    RP_TRY(rp_op_launched());
-    StepArgs A = {};
-    A.head = P.head; A.items = P.items; A.where = P.where; A.N = N; A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads; A.units = step_units(a);
-    A.groups = A.units / a->kv_heads; A.d = a->head_dim; A.scale = a->scale; A.q = q->x; A.q_token = q->token; A.q_head = q->head; A.out = out->x; A.o_token = out->token; A.o_head = out->head;
+    if (!A.table) {
+        k_step_plan<<<1, 1024, 0, stream>>>(P, A.head);
+        RP_TRY(rp_op_launched());
+    }
+    A.Hq = a->q_heads; A.share = a->q_heads / a->kv_heads; A.units = step_units(a); A.groups = A.units / a->kv_heads; A.d = a->head_dim; A.scale = a->scale;
+    A.q = q->x; A.q_token = q->token; A.q_head = q->head; A.out = out->x; A.o_token = out->token; A.o_head = out->head; A.keys = n_tokens > 0;
     if (lse && lse->x) { A.lse = (float *)lse->x; A.l_token = lse->token; A.l_head = lse->head; }
     A.tops = (float2 *)(w + space.tops); A.parts = (float *)(w + space.parts);
-    A.status = &P.head->status; A.wait_ns = (u64)g_attend_wait_ns; A.keys = n_tokens > 0;
+    A.wait_ns = (u64)g_attend_wait_ns;
     const int sms = rp_op_sms(dev.device);
     const i64 units = (i64)P.most * A.units;
-    const bool several = n_tokens + 31 > STEP_CHUNK && (!window || (i64)window + sinks + 31 > STEP_CHUNK);
     // Up to eight query heads of a key head: half the exponentials and half the products with values (64 ragged sequences of 16 heads on 4: main kernel ## for ## us).
     const bool few = A.share <= 8, narrow = a->head_dim <= 64;
     const auto go = [&](auto type) {
         typedef decltype(type) X;
-        if (narrow) return few ? launch<X, 64, true>(mk, mv, A, units, several, sms, stream) : launch<X, 64, false>(mk, mv, A, units, several, sms, stream);
-        return few ? launch<X, 128, true>(mk, mv, A, units, several, sms, stream) : launch<X, 128, false>(mk, mv, A, units, several, sms, stream);
+        if (narrow) return few ? launch<X, 64, true>(mk, mv, A, units, sms, stream) : launch<X, 64, false>(mk, mv, A, units, sms, stream);
+        return few ? launch<X, 128, true>(mk, mv, A, units, sms, stream) : launch<X, 128, false>(mk, mv, A, units, sms, stream);
     };
     return a->type == RP_F16 ? go(__half()) : go(bf16());
 }
