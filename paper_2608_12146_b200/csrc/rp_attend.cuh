@@ -18,19 +18,40 @@ struct AttendClears { AttendClear x[3]; int n; };       // outputs whose rows of
 // ---- window -----------------------------------------------------------------------------
 // Token i of a sample sees j <= i with i - j < window or j < sinks.  The first tokens lie in the sample's first tile of 128 keys (sinks <= 128).
 #define ATTEND_SINKS 128
-// What a block of queries goes through: the sample's first tile where its queries see first tokens from afar, then the tiles [lo, ..) up to its last query.
-// The block's second tile of 128 queries does not see one of those: `skip`, the first behind the first tokens' (-1: it sees them all).
+// What a block of 128 queries goes through: the sample's first tile where its queries see first tokens from afar, then the tiles from `lo` on up to its last query.
 struct AttendSteps {
-    int ahead, lo, skip;                                // ahead: 1 with a tile of first tokens in front
+    int ahead, lo;                                      // ahead: 1 with a tile of first tokens in front
     __device__ __forceinline__ AttendSteps(int row0, int window, int sinks)
     {
-        const int x = row0 - window + 1;                // the first that the block's first query sees
-        lo = max(x, 0) >> 7;
+        lo = max(row0 - window + 1, 0) >> 7;
         ahead = sinks > 0 && lo > 0;
-        skip = x >= 0 && !(sinks > 0 && lo == 0) ? ahead : -1;
     }
     __device__ __forceinline__ int steps(int tiles) const { return ahead + tiles - lo; }             // of queries that see keys up to tile `tiles`
     __device__ __forceinline__ int tile(int step) const { return step < ahead ? 0 : lo + step - ahead; }
+};
+// The same for two tiles of 128 queries that go through their keys together.  Where the window has left the sample's first token behind, they go from the last key
+// down, the first tokens at the end: so that no row begins with a tile of which it sees nothing, after which its sums would have to be taken up anew.
+struct AttendOrder {
+    bool down, one;                                     // one: there is no second tile
+    int high, lo, steps, last[2], hole;                 // tile i takes part in the steps first(i) to last[i], the second one not in step `hole`
+    __device__ __forceinline__ AttendOrder(int row0, int len, int window, int sinks)
+    {
+        const int x = row0 - window + 1, both = len > row0 + 128;
+        lo = max(x, 0) >> 7;
+        const int ahead = sinks > 0 && lo > 0;
+        down = x > -both;                               // (x = 0 alone: all that is there is seen)
+        high = (min(len, row0 + 256) + 127) >> 7;       // tiles that the block sees
+        steps = high - lo + ahead;
+        last[0] = down ? steps - 1 : high - 1 - both;
+        const bool lowest = !down || (sinks > 0 && lo == 0);          // the second tile sees the lowest of the window's, too
+        last[1] = steps - 1 - (!lowest && !ahead);
+        hole = lowest ? -1 : high - lo - 1;
+        one = !both;
+    }
+    __device__ __forceinline__ int first(int i) const { return i == 0 && down && !one; }
+    __device__ __forceinline__ bool active(int i, int step) const { return step >= first(i) && step <= last[i] && !(i == 1 && (one || step == hole)); }
+    __device__ __forceinline__ bool first_tokens(int step) const { return down && step >= high - lo; }        // first tokens alone, from afar
+    __device__ __forceinline__ int tile(int step) const { return !down ? step : step < high - lo ? high - 1 - step : 0; }
 };
 // Tiles of 128 queries that see a block of 128 keys: from the block's own on, as far as the window goes.  The first block with first tokens is seen by all: its queries
 // are shared out in chunks of as many tiles, all of the window's in the first one.
@@ -136,7 +157,7 @@ extern i64 g_attend_wait_ns;             // limit of the kernels' waits (rp_debu
 int rp_attend_check(const rp_attend_config *a, i64 T, int N);
 int rp_attend_check_window(const rp_attend_config *a, int window, int sinks, i64 T, int N);
 int rp_attend_view(const rp_view *v, i64 T, int heads, RpOpDevice &dev);
-static inline int rp_attend_window_of(int window, i64 T) { return (int)(window < T ? window : T < 1 ? 1 : T); }        // (one longer than the row is one as long as it)
+static inline int rp_attend_window_of(int window, i64 T) { return (int)(window < T + 256 ? window : T + 256); }         // (longer than any sample: no block is cut)
 // Is one of the first `n_out` views the same memory as another of them or as one of the `n` behind them?
 static inline bool rp_attend_shared(const rp_view *const *v, int n_out, int n)
 {
@@ -151,6 +172,7 @@ static inline bool rp_attend_shared(const rp_view *const *v, int n_out, int n)
 #define ATTEND_THREADS 384
 #define ATTEND_COPY_WARP 8
 #define ATTEND_MMA_WARP 9
+#define ATTEND_LIST_WARP 10
 __device__ __forceinline__ void rp_many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
 __device__ __forceinline__ void rp_few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
 
@@ -174,6 +196,7 @@ struct AttendTile {
         len = (int)(min(start[it.x + 1], T) - base);
         row0 = it.y * rows;
     }
+    __device__ __forceinline__ explicit AttendTile(const volatile int *block) { base = block[1]; len = block[2]; row0 = block[3]; }     // as a warp has looked it up
 };
 // Tiles of 128 keys that the i-th tile of 128 queries of a block sees.
 __device__ __forceinline__ int rp_attend_tiles(const AttendTile &t, int i, int causal)

@@ -261,7 +261,6 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
-            const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
             for (int n = 0;; ++n) {
                 const int at = rp_attend_item(n, total);
@@ -272,12 +271,15 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 // 128 keys against a tile's queries, or their values against the gradients
                 auto against = [&](u32 to, const unsigned char *keys, const unsigned char *queries, u32 bar) {
                     const u32 a = mma_operand(rp_smem(keys), true, 0), b = mma_operand(rp_smem(queries), true, 0);
+                    if (rp_elect()) {
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
-                        mma_ss(one, to, a + off, b + off, shape_s, x > 0);
+                        for (int x = 0; x < D / 16; ++x) {
+                            const u32 off = ((x / 4) * PANEL + (x % 4) * 32) >> 4;
+                            mma_ss(to, a + off, b + off, shape_s, x > 0);
+                        }
+                        mma_commit(bar);
                     }
-                    mma_commit(one, bar);
+                    __syncwarp();
                 };
                 auto arrived = [&](u32 f) {     // a tile's queries and gradients
                     const u32 s = f % STAGES;
@@ -290,14 +292,17 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 // a tile's weights (or gradients of its scores) times its gradients (or queries)
                 auto add = [&](u32 to, u32 weights, const unsigned char *rows, bool more) {
                     const u32 b = mma_operand(rp_smem(rows), false, PANEL);
+                    if (rp_elect()) {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) mma_ts(one, to, weights + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
+                        for (int x = 0; x < 8; ++x) mma_ts(to, weights + (x / 4) * 64 + (x % 4) * 8, b + x * (2048 >> 4), shape_o, more || x > 0);
+                    }
+                    __syncwarp();
                 };
                 bar_hold(rp_smem(&sm.kv_full), n & 1, waits);
                 arrived(base);
                 against(tm, sm.k, sm.q[base % STAGES], rp_smem(&sm.s_full));
                 against(tm + 128, sm.v, sm.g[base % STAGES], rp_smem(&sm.dp_full));
-                if (nt == 1) mma_commit(one, rp_smem(&sm.kv_empty));
+                if (nt == 1) mma_commit_warp(rp_smem(&sm.kv_empty));
                 if (n) bar_hold(rp_smem(&sm.acc_empty), (n - 1) & 1, waits);
                 for (int j = 0; j < nt; ++j) {
                     const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
@@ -309,17 +314,17 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     bar_hold(rp_smem(&sm.ds_full), f & 1, waits);
                     tmem_after();
                     add(tm + 256 + D, tm + 128, sm.q[s], j > 0);
-                    mma_commit(one, rp_smem(&sm.q_empty[s]));
+                    mma_commit_warp(rp_smem(&sm.q_empty[s]));
                     if (j + 1 < nt) {
                         against(tm + 128, sm.v, sm.g[s1], rp_smem(&sm.dp_full));
-                        if (j + 2 == nt) mma_commit(one, rp_smem(&sm.kv_empty));
+                        if (j + 2 == nt) mma_commit_warp(rp_smem(&sm.kv_empty));
                     } else
-                        mma_commit(one, rp_smem(&sm.acc_full));
+                        mma_commit_warp(rp_smem(&sm.acc_full));
                 }
                 base += nt;
             }
             // nobody may leave while products are under way
-            mma_commit(one, rp_smem(&sm.done));
+            mma_commit_warp(rp_smem(&sm.done));
             if (lane == 0) rp_drain(rp_smem(&sm.done), 0);
         }
     } else {
@@ -503,7 +508,6 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
-            const u32 one = lane == 0;
             u32 base = 0;                               // tiles of the items before
             for (int n = 0;; ++n) {
                 bar_hold(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, waits);
@@ -516,9 +520,12 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 // 128 queries (or gradients) against a tile's keys (or values)
                 auto against = [&](u32 to, u32 rows, const unsigned char *tile, u32 bar) {
                     const u32 b = mma_operand(rp_smem(tile), true, 0);
+                    if (rp_elect()) {
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x) mma_ts(one, to, rows + x * 8, b + (((x / 4) * PANEL + (x % 4) * 32) >> 4), shape_s, x > 0);
-                    mma_commit(one, bar);
+                        for (int x = 0; x < D / 16; ++x) mma_ts(to, rows + x * 8, b + (((x / 4) * PANEL + (x % 4) * 32) >> 4), shape_s, x > 0);
+                        mma_commit(bar);
+                    }
+                    __syncwarp();
                 };
                 auto arrived = [&](int j) {             // a tile's keys and values
                     const u32 f = base + j;
@@ -544,17 +551,19 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     bar_hold(rp_smem(&sm.ds_full), f & 1, waits);
                     tmem_after();
                     const u32 k = mma_operand(rp_smem(sm.k[s]), false, PANEL);
+                    if (rp_elect()) {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        mma_ts(one, tm + 256, tm + 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
-                    mma_commit(one, rp_smem(&sm.kv_empty[s]));
+                        for (int x = 0; x < 8; ++x) mma_ts(tm + 256, tm + 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                    }
+                    __syncwarp();
+                    mma_commit_warp(rp_smem(&sm.kv_empty[s]));
                     if (j + 1 < nk) against(tm + 128, tm + 448, sm.v[s1], rp_smem(&sm.dp_full));
-                    else mma_commit(one, rp_smem(&sm.acc_full));
+                    else mma_commit_warp(rp_smem(&sm.acc_full));
                 }
                 base += nk;
             }
             // nobody may leave while products are under way
-            mma_commit(one, rp_smem(&sm.done));
+            mma_commit_warp(rp_smem(&sm.done));
             if (lane == 0) rp_drain(rp_smem(&sm.done), 0);
         }
     } else {

@@ -140,26 +140,37 @@ template <typename X> __device__ __forceinline__ constexpr u32 mma_shape(int n, 
     return (1u << 4) | ((std::is_same<X, bf16>::value ? 1u : 0u) << 7) | ((std::is_same<X, bf16>::value ? 1u : 0u) << 10) |
            ((b_rows_k ? 1u : 0u) << 16) | ((u32)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
-// One step of 16 along the summed dimension; `more`: added to what the accumulator holds.  The whole warp comes here, `one` is set in the lane that issues: what the
-// instruction takes is then worked out once for the warp, in registers of its own.  (Within a branch that one lane takes, a step took 105 to 130 cycles to issue and
-// 64 to run.)
-__device__ __forceinline__ void mma_ss(u32 one, u32 d, u32 a, u32 b, u32 shape, bool more)
+// Whoever of the warp's lanes issues products; the whole warp asks.  The compiler knows then that one lane goes in, and the operands that the instructions take are
+// worked out once for the warp, in registers of its own.  (An attention block of ten tiles 26.5 us with a comparison of the lane's number at each instruction, 23.5 with
+// this choice at each, 22.5 with a branch for all products of a tile.)
+__device__ __forceinline__ bool rp_elect()
 {
-    asm volatile("{\n .reg .pred p, q;\n .reg .b64 x, y;\n setp.ne.u32 q, %0, 0;\n setp.ne.u32 p, %5, 0;\n mov.b64 x, {%2, %6};\n mov.b64 y, {%3, %6};\n"
-                 " @q tcgen05.mma.cta_group::1.kind::f16 [%1], x, y, %4, p;\n}"
-                 ::"r"(one), "r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)more), "r"(MMA_HIGH) : "memory");
+    u32 r;
+    asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r)::"memory");
+    return r != 0;
 }
-__device__ __forceinline__ void mma_ts(u32 one, u32 d, u32 a, u32 b, u32 shape, bool more)           // A from tensor memory, two elements a column
+// One step of 16 along the summed dimension; `more`: added to what the accumulator holds.  By the lane that rp_elect() chooses.
+__device__ __forceinline__ void mma_ss(u32 d, u32 a, u32 b, u32 shape, bool more)
 {
-    asm volatile("{\n .reg .pred p, q;\n .reg .b64 y;\n setp.ne.u32 q, %0, 0;\n setp.ne.u32 p, %5, 0;\n mov.b64 y, {%3, %6};\n"
-                 " @q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], y, %4, p;\n}"
-                 ::"r"(one), "r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)more), "r"(MMA_HIGH) : "memory");
+    asm volatile("{\n .reg .pred p;\n .reg .b64 x, y;\n setp.ne.u32 p, %4, 0;\n mov.b64 x, {%1, %5};\n mov.b64 y, {%2, %5};\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)more), "r"(MMA_HIGH) : "memory");
 }
-// The barrier is arrived at when all products that this lane has issued are done.
-__device__ __forceinline__ void mma_commit(u32 one, u32 bar)
+__device__ __forceinline__ void mma_ts(u32 d, u32 a, u32 b, u32 shape, bool more)           // A from tensor memory, two elements a column
 {
-    asm volatile("{\n .reg .pred q;\n setp.ne.u32 q, %0, 0;\n @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n}"
-                 ::"r"(one), "r"(bar) : "memory");
+    asm volatile("{\n .reg .pred p;\n .reg .b64 y;\n setp.ne.u32 p, %4, 0;\n mov.b64 y, {%2, %5};\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"((u32)more), "r"(MMA_HIGH) : "memory");
+}
+// The barrier is arrived at when all products that the chosen lane has issued are done: by that lane, or by the whole warp.
+__device__ __forceinline__ void mma_commit(u32 bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_commit_warp(u32 bar)
+{
+    if (rp_elect()) mma_commit(bar);
+    __syncwarp();
 }
 
 // ---- host: a tensor [tokens][heads][dim] as 64-element panels of `rows` tokens of one head ----
