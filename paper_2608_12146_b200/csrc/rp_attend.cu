@@ -27,42 +27,23 @@ __global__ void __launch_bounds__(1024) k_attend_plan(AttendPlan P, AttendClears
 // ---------------------------------------------------------------------------------------
 // the kernel
 // ---------------------------------------------------------------------------------------
-struct AttendArgs {
-    const AttendHead *head;
-    const int2 *items;
-    const i64 *start;
-    i64 T;
-    int N, Hq, share, d, causal;            // share: query heads to a key head
-    int window, sinks;
-    float scale;
-    void *out;
-    i64 o_token, o_head;
-    float *lse;
-    i64 l_token, l_head;
-    int *status;
-    u64 wait_ns;
-};
-
 // A stage holds the values of one tile and the keys of the next, which are waited for and let go of together: of nk tiles there are nk + 1 stages, the first without
 // values, the last without keys.
-template <int D, bool WINDOW> struct FwdSmem {
+template <int D> struct FwdSmem {
     static constexpr int TILE = 128 * D * 2, STAGES = D == 128 ? 2 : 4;
     alignas(1024) unsigned char q[2][TILE];
     alignas(1024) unsigned char v[STAGES][TILE];
     alignas(1024) unsigned char k[STAGES][TILE];
     u64 q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_full[2], o_full[2], done;
     u32 tmem;
-    u64 block_full[2], block_empty[2];
-    alignas(16) volatile int block[2][4];               // WINDOW: blocks to come: the item, its sample's first row and length, its own first row
-    alignas(16) unsigned char rows[8][WINDOW ? 4096 : 16];           // of each warp, half of what it hands over
     Waits waits;
 };
 
-template <typename X, int D, bool WINDOW>
+template <typename X, int D>
 __global__ void __launch_bounds__(ATTEND_THREADS, 1)
 k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttendArgs A)
 {
-    typedef FwdSmem<D, WINDOW> Smem;
+    typedef FwdSmem<D> Smem;
     constexpr int STAGES = Smem::STAGES, PANELS = D / 64, PANEL = 128 * 128;
     // Weights of float16 times 2^7, up to 2^15 with what a maximum may lag behind: as 2^-25 and less of the largest they would be lost from the product with the values, and
     // many of them are something (131072 keys 17.5 under the largest: 0.0033 of their values).
@@ -75,7 +56,6 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         for (int s = 0; s < STAGES; ++s) { bar_init(rp_smem(&sm.kv_full[s]), 1); bar_init(rp_smem(&sm.kv_empty[s]), 1); }
         for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.s_full[i]), 1); bar_init(rp_smem(&sm.p_full[i]), 4); bar_init(rp_smem(&sm.o_full[i]), 1); }
         bar_init(rp_smem(&sm.done), 1);
-        for (int i = 0; i < 2; ++i) { bar_init(rp_smem(&sm.block_full[i]), 1); bar_init(rp_smem(&sm.block_empty[i]), 10); }
         sm.waits.start(A.wait_ns);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -90,31 +70,14 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
 
     if (warp >= 8) {
         rp_few_registers();
-        if (WINDOW && warp == ATTEND_LIST_WARP && lane == 0) {
-            // With few steps to a block its place must not be waited for at its start: one warp looks it up two blocks ahead for the others.  (Every warp for itself: the
-            // tensor cores stood still for 3500 of 49000 cycles of a block with a window of 1024.)
-            for (int round = 0; bar_place(round > 1, rp_smem(&sm.block_empty[round & 1]), ((round >> 1) - 1) & 1, waits); ++round) {
-                const int at = rp_attend_item(round, total);
-                volatile int *const to = sm.block[round & 1];
-                to[0] = at;
-                if (at >= 0) {
-                    const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
-                    to[1] = (int)t.base; to[2] = t.len; to[3] = t.row0;
-                }
-                bar_arrive(rp_smem(&sm.block_full[round & 1]));
-                if (at < 0) break;
-            }
-        }
         if (warp == ATTEND_COPY_WARP && lane == 0) {
             tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v);
             u32 blocks = 0, fill = 0;                   // copies of queries and into the ring so far
             bool ok = true;
             for (int round = 0; ok; ++round) {
-                if (WINDOW && !(ok = bar_wait(rp_smem(&sm.block_full[round & 1]), (round >> 1) & 1, waits))) break;
-                const int at = WINDOW ? sm.block[round & 1][0] : rp_attend_item(round, total);
+                const int at = rp_attend_item(round, total);
                 if (at < 0) break;
-                const AttendTile t = WINDOW ? AttendTile(sm.block[round & 1]) : AttendTile(A.items, A.start, A.T, at / A.Hq, 256);
-                if (WINDOW) bar_arrive(rp_smem(&sm.block_empty[round & 1]));
+                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
                 const int h = at % A.Hq, hk = h / A.share;
                 if (!(ok = bar_place(round, rp_smem(&sm.q_empty), (round - 1) & 1, waits))) break;
                 ++blocks;
@@ -123,17 +86,15 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 for (int i = 0; i < tiles; ++i)
                     for (int p = 0; p < PANELS; ++p)
                         tma_load3(rp_smem(sm.q[i]) + p * PANEL, &map_q, p * 64, h, (int)t.base + t.row0 + 128 * i, rp_smem(&sm.q_full));
-                const AttendOrder w(t.row0, t.len, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
-                const int nk = WINDOW ? w.steps : rp_attend_tiles(t, tiles - 1, A.causal);
-                const auto tile = [&](int j) { return (int)t.base + (WINDOW ? w.tile(j) : j) * 128; };
+                const int nk = rp_attend_tiles(t, tiles - 1, A.causal);
                 for (int j = 0; j <= nk; ++j, ++fill) {
                     const u32 s = fill % STAGES, turn = fill / STAGES;
                     if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), j && j < nk ? 2 * Smem::TILE : Smem::TILE);
                     waits->copied = fill + 1;
                     for (int p = 0; p < PANELS; ++p) {
-                        if (j) tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, tile(j - 1), rp_smem(&sm.kv_full[s]));
-                        if (j < nk) tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, tile(j), rp_smem(&sm.kv_full[s]));
+                        if (j) tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, (int)t.base + (j - 1) * 128, rp_smem(&sm.kv_full[s]));
+                        if (j < nk) tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, (int)t.base + j * 128, rp_smem(&sm.kv_full[s]));
                     }
                 }
             }
@@ -144,7 +105,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
             u32 used = 0, p0 = 0, p1 = 0;                   // stages taken; weights taken of each tile
-            auto scores = [&](int i, u32 stage, u32 shape_s) {           // tile i's scores for the keys in a stage
+            auto scores = [&](int i, u32 stage) {           // tile i's scores for the keys in a stage
                 const u32 a = mma_operand(rp_smem(sm.q[i]), true, 0), b = mma_operand(rp_smem(sm.k[stage]), true, 0);
                 if (rp_elect()) {
 #pragma unroll
@@ -164,77 +125,38 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                 }
                 __syncwarp();
             };
-            auto outputs_first = [&](int i, u32 stage, int groups) {   // the same for the first tokens from afar, 32 keys at a time
-                const u32 v = mma_operand(rp_smem(sm.v[stage]), false, PANEL);
-                if (rp_elect())
-                    for (int x = 0; x < 2 * groups; ++x) mma_ts(tm + 256 + i * D, tm + i * 128 + x * 8, v + x * (2048 >> 4), shape_o, true);
-                __syncwarp();
-            };
-            const int groups = WINDOW ? (int)rp_uniform((A.sinks + 31) >> 5) : 0;
-            const u32 shape_first = mma_shape<X>(32 * groups, false);
             for (int round = 0;; ++round) {
-                if (WINDOW) bar_hold(rp_smem(&sm.block_full[round & 1]), (round >> 1) & 1, waits);
-                const int at = WINDOW ? sm.block[round & 1][0] : rp_attend_item(round, total);
+                const int at = rp_attend_item(round, total);
                 if (at < 0 || rp_uniform(waits->gave_up)) break;
-                const AttendTile t = WINDOW ? AttendTile(sm.block[round & 1]) : AttendTile(A.items, A.start, A.T, at / A.Hq, 256);
-                if (WINDOW) bar_arrive_warp(rp_smem(&sm.block_empty[round & 1]), lane);
+                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
                 const int left = rp_uniform(t.len - t.row0), tiles = left > 128 ? 2 : 1, len = rp_uniform(t.len);
-                const int n0 = rp_uniform(rp_attend_tiles(t, 0, A.causal)), n1 = tiles == 2 ? rp_uniform(rp_attend_tiles(t, 1, A.causal)) : 0;
-                const AttendOrder w((int)rp_uniform(t.row0), len, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
-                const int nk = WINDOW ? w.steps : max(n0, n1);
+                const int n0 = rp_uniform(rp_attend_tiles(t, 0, A.causal)), n1 = tiles == 2 ? rp_uniform(rp_attend_tiles(t, 1, A.causal)) : 0, nk = max(n0, n1);
                 bar_hold(rp_smem(&sm.q_full), round & 1, waits);
                 bar_hold(rp_smem(&sm.kv_full[used % STAGES]), (used / STAGES) & 1, waits);
-                if (!WINDOW || rp_uniform(w.active(0, 0))) scores(0, used % STAGES, shape_s);
-                if (tiles == 2) scores(1, used % STAGES, shape_s);
+                scores(0, used % STAGES);
+                if (tiles == 2) scores(1, used % STAGES);
                 mma_commit_warp(rp_smem(&sm.kv_empty[used % STAGES]));
                 if (nk == 1) mma_commit_warp(rp_smem(&sm.q_empty));
                 ++used;
                 for (int j = 0; j < nk; ++j, ++used) {
                     const u32 s = used % STAGES;
-                    const int behind = len - (WINDOW ? w.tile(j) : j) * 128;
-                    // WINDOW: which tiles take part in the step (1, 2), and in the next (4, 8), whose last it is (16, 32), whether it is not the first tile's first (64),
-                    // whether it is the first tokens' (128), and the next (256); in one register of the warp, so that branches by it leave the products' operands there
-                    u32 how = 0;
-                    if (WINDOW)
-                        how = rp_uniform((w.active(0, j) ? 1 : 0) | (w.active(1, j) ? 2 : 0) | (j + 1 < nk && w.active(0, j + 1) ? 4 : 0) | (j + 1 < nk && w.active(1, j + 1) ? 8 : 0) |
-                                         (j == w.last[0] ? 16 : 0) | (j == w.last[1] ? 32 : 0) | (j > w.first(0) ? 64 : 0) | (w.first_tokens(j) ? 128 : 0) | (w.first_tokens(j + 1) ? 256 : 0));
                     // (what is copied has mostly come when the weights have)
                     bar_hold(rp_smem(&sm.kv_full[s]), (used / STAGES) & 1, waits);
                     // values behind the sample's end are another sample's: their weights are 0, and 0 times NaN would not be
-                    if (behind < 128) rp_clear_rows<D>(sm.v[s], behind, 128, lane);
-                    if (WINDOW) {
-                        if (how & 128) rp_clear_rows<D>(sm.v[s], A.sinks, 32 * groups, lane);
-                        if (how & 1) {
-                            bar_hold(rp_smem(&sm.p_full[0]), p0++ & 1, waits);
-                            tmem_after();
-                            if (how & 128) outputs_first(0, s, groups);
-                            else outputs(0, s, how & 64);
-                            if (how & 16) mma_commit_warp(rp_smem(&sm.o_full[0]));
-                        }
-                        if (how & 4) scores(0, s, how & 256 ? shape_first : shape_s);
-                        if (how & 2) {
-                            bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, waits);
-                            tmem_after();
-                            if (how & 128) outputs_first(1, s, groups);
-                            else outputs(1, s, j > 0);
-                            if (how & 32) mma_commit_warp(rp_smem(&sm.o_full[1]));
-                        }
-                        if (how & 8) scores(1, s, how & 256 ? shape_first : shape_s);
-                    } else {
-                        if (j < n0) {
-                            bar_hold(rp_smem(&sm.p_full[0]), p0++ & 1, waits);
-                            tmem_after();
-                            outputs(0, s, j > 0);
-                            if (j == n0 - 1) mma_commit_warp(rp_smem(&sm.o_full[0]));
-                            else scores(0, s, shape_s);
-                        }
-                        if (j < n1) {
-                            bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, waits);
-                            tmem_after();
-                            outputs(1, s, j > 0);
-                            if (j == n1 - 1) mma_commit_warp(rp_smem(&sm.o_full[1]));
-                            else scores(1, s, shape_s);
-                        }
+                    if (len - j * 128 < 128) rp_clear_rows<D>(sm.v[s], len - j * 128, 128, lane);
+                    if (j < n0) {
+                        bar_hold(rp_smem(&sm.p_full[0]), p0++ & 1, waits);
+                        tmem_after();
+                        outputs(0, s, j > 0);
+                        if (j == n0 - 1) mma_commit_warp(rp_smem(&sm.o_full[0]));
+                        else scores(0, s);
+                    }
+                    if (j < n1) {
+                        bar_hold(rp_smem(&sm.p_full[1]), p1++ & 1, waits);
+                        tmem_after();
+                        outputs(1, s, j > 0);
+                        if (j == n1 - 1) mma_commit_warp(rp_smem(&sm.o_full[1]));
+                        else scores(1, s);
                     }
                     mma_commit_warp(rp_smem(&sm.kv_empty[s]));
                     if (j == nk - 2) mma_commit_warp(rp_smem(&sm.q_empty));
@@ -252,44 +174,35 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
         const f2 sl2 = rp_f2(sl, sl);
         u32 ss = 0, os = 0;
         for (int round = 0;; ++round) {
-            // (beside a row's scores there is no room for much: with a window, what a block's steps go by stays in shared memory and is worked out anew in each)
-            volatile int *const block = sm.block[round & 1];
-            const bool told = WINDOW && bar_wait_warp(rp_smem(&sm.block_full[round & 1]), (round >> 1) & 1, waits);
-            const int at = told ? block[0] : rp_attend_item(round, total);
+            const int at = rp_attend_item(round, total);
             if (at < 0) break;
-            const AttendTile t = told ? AttendTile(block) : AttendTile(A.items, A.start, A.T, at / A.Hq, 256);
-            if (t.row0 + 128 * i >= t.len) {
-                if (told) bar_arrive_warp(rp_smem(&sm.block_empty[round & 1]), lane);
-                continue;
-            }
-            const AttendOrder order(t.row0, t.len, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
-            const int first = WINDOW ? order.first(i) : 0, nk = WINDOW ? order.last[i] + 1 : rp_attend_tiles(t, i, A.causal);
+            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 256);
+            const int h = at % A.Hq, r0 = t.row0 + 128 * i, r = r0 + row;
+            if (r0 >= t.len) continue;
+            const int nk = rp_attend_tiles(t, i, A.causal);
             float m = -INFINITY, l = 0.0f;
-            bool ok = told || !WINDOW;                   // (what is not told is not worked out: a wait has run out)
-            for (int j = first; ok && j < nk; ++j) {
-                // WINDOW: columns that the row sees - those before `lim`, of these the ones from `from` on and the `ahead` first - and whether there are others (1: behind, 2: before)
-                int lim = 0, from = 0, ahead = 0, hidden = 0;
-                bool first_tokens = false, held;
-                if (WINDOW) {
-                    const int row0 = block[3], len = block[2], r0 = row0 + 128 * i, r = r0 + row;
-                    const AttendOrder w(row0, len, A.window, A.sinks);
-                    if (i == 1 && j == w.hole) continue;
-                    const int k0 = w.tile(j) * 128;
-                    lim = min(len, r + 1) - k0; from = r - A.window + 1 - k0; ahead = A.sinks - k0;
-                    hidden = (k0 + 128 > len || k0 + 127 > r0 ? 1 : 0) | (k0 <= r0 + 127 - A.window ? 2 : 0);
-                    first_tokens = w.first_tokens(j);
-                    held = r < len;
-                } else
-                    held = t.row0 + 128 * i + row < t.len;
+            bool ok = true;
+            for (int j = 0; j < nk; ++j) {
                 if (!(ok = bar_wait_warp(rp_smem(&sm.s_full[i]), ss & 1, waits))) break;
                 ++ss;
                 tmem_after();
-                // the row's maximum with the tile's
-                const auto grow = [&](float top) {
-                    if (j == first) { m = top; return; }
+                u32 s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_load32(ts + 32 * c, s + 32 * c);
+                tmem_loaded();
+                if (j * 128 + 128 > t.len || (A.causal && j * 128 + 127 > r0)) {
+                    const int lim = (A.causal ? min(t.len, r + 1) : t.len) - j * 128;
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : 0xff800000u;
+                }
+                float top = __uint_as_float(s[0]);
+#pragma unroll
+                for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(s[c]));
+                if (j == 0) m = top;
+                else {
                     // (a maximum that grows by less than 2^8 stays: weights up to 256 and their sums lose nothing; -inf, as long as no score is above it, goes with the
                     // first that is; rows behind the sample's end are other samples', which do not matter)
-                    const float grown = held ? (top - m) * sl : 0.0f;
+                    const float grown = r < t.len ? (top - m) * sl : 0.0f;
                     if (__any_sync(0xffffffffu, grown > 8.0f)) {
                         const float up = fmaxf(top, m), f = m == up ? 1.0f : rp_exp2((m - up) * sl);
                         m = up;
@@ -304,69 +217,7 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
                             tmem_store32(to + c, o);
                         }
                     }
-                };
-                if (WINDOW && first_tokens) {
-                    // first tokens from afar: the same ones for all rows, 32 columns at a time
-                    float top = -INFINITY;
-                    for (int g = 0; g < A.sinks; g += 32) {
-                        u32 s[32];
-                        tmem_load32(ts + g, s);
-                        tmem_loaded();
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) top = g + c < A.sinks ? fmaxf(top, __uint_as_float(s[c])) : top;
-                    }
-                    grow(top);
-                    const float less = m == -INFINITY ? LIFT : fmaf(-m, sl, LIFT);
-                    for (int g = 0; g < A.sinks; g += 64) {
-                        u32 p[32];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            u32 s[32];
-                            if (!u || g + 32 < A.sinks) {
-                                tmem_load32(ts + g + 32 * u, s);
-                                tmem_loaded();
-                            }
-#pragma unroll
-                            for (int c = 0; c < 32; c += 2) {
-                                const int k = g + 32 * u + c;
-                                const float a = k < A.sinks ? rp_exp2(fmaf(__uint_as_float(s[c]), sl, less)) : 0.0f;
-                                const float b = k + 1 < A.sinks ? rp_exp2(fmaf(__uint_as_float(s[c + 1]), sl, less)) : 0.0f;
-                                l += a + b;
-                                p[16 * u + c / 2] = rp_pair(a, b, X());
-                            }
-                        }
-                        tmem_store32(ts + g / 2, p);
-                    }
-                    tmem_stored();
-                    tmem_before();
-                    bar_arrive_warp(rp_smem(&sm.p_full[i]), lane);
-                    continue;
                 }
-                u32 s[128];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_load32(ts + 32 * c, s + 32 * c);
-                tmem_loaded();
-                if (WINDOW) {
-                    // (a comparison a column where one will do: a block of 18 steps, four of them such, 26.4 us with all three, ## so)
-                    if (hidden == 1) {
-#pragma unroll
-                        for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : 0xff800000u;
-                    } else if (hidden == 2 && ahead <= 0) {
-#pragma unroll
-                        for (int c = 0; c < 128; ++c) s[c] = c >= from ? s[c] : 0xff800000u;
-                    } else if (hidden) {
-#pragma unroll
-                        for (int c = 0; c < 128; ++c) s[c] = c < lim && (c >= from || c < ahead) ? s[c] : 0xff800000u;
-                    }
-                } else if (j * 128 + 128 > t.len || (A.causal && j * 128 + 127 > t.row0 + 128 * i)) {
-                    const int lim = (A.causal ? min(t.len, t.row0 + 128 * i + row + 1) : t.len) - j * 128;
-#pragma unroll
-                    for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : 0xff800000u;
-                }
-                float top = __uint_as_float(s[0]);
-#pragma unroll
-                for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(s[c]));
-                grow(top);
                 const float less = m == -INFINITY ? LIFT : fmaf(-m, sl, LIFT);
                 const f2 shift = rp_f2(less, less);
                 f2 sum0 = rp_f2(0.0f, 0.0f), sum1 = sum0;
@@ -391,51 +242,23 @@ k_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUte
             ++os;
             tmem_after();
             const float f = ok ? 1.0f / l : NAN;
-            const AttendTile u = told ? AttendTile(block) : t;
-            const int r0 = u.row0 + 128 * i, r = r0 + row, h = at % A.Hq;
-            X *const out = (X *)A.out + u.base * A.o_token + h * A.o_head;
-            if (WINDOW) {
-                // through shared memory, 64 columns at a time: rows of 128 bytes go out whole (each lane its own row, 16 bytes at a time: 2000 cycles for 500)
-                unsigned char *const rows = sm.rows[warp];
+            X *out = (X *)A.out + (t.base + r) * A.o_token + h * A.o_head;
 #pragma unroll
-                for (int c = 0; c < D; c += 64) {
-                    u32 o[64];
-                    tmem_load32(to + c, o);
-                    tmem_load32(to + c + 32, o + 32);
-                    tmem_loaded();
-                    float v[64];
+            for (int c = 0; c < D; c += 32) {
+                u32 o[32];
+                tmem_load32(to + c, o);
+                tmem_loaded();
+                float v[32];
 #pragma unroll
-                    for (int x = 0; x < 64; ++x) v[x] = __uint_as_float(o[x]) * f;
+                for (int x = 0; x < 32; ++x) v[x] = __uint_as_float(o[x]) * f;
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) *(Pack8<X> *)(rows + lane * 128 + ((x ^ (lane & 7)) << 4)) = rp_close8<X>(v + 8 * x);
-                    __syncwarp();
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        const int y = x * 4 + (lane >> 3), p = lane & 7, q = r0 + (row & ~31) + y;
-                        const Pack8<X> w = *(const Pack8<X> *)(rows + y * 128 + ((p ^ (y & 7)) << 4));
-                        if (q < u.len && c + 8 * p < A.d) rp_store8(out + q * A.o_token + c + 8 * p, w);
-                    }
-                    __syncwarp();
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < D; c += 32) {
-                    u32 o[32];
-                    tmem_load32(to + c, o);
-                    tmem_loaded();
-                    float v[32];
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) v[x] = __uint_as_float(o[x]) * f;
-#pragma unroll
-                    for (int x = 0; x < 32; x += 8)
-                        if (r < u.len && c + x < A.d) rp_store8(out + r * A.o_token + c + x, rp_close8<X>(v + x));
-                    __syncwarp();
-                }
+                for (int x = 0; x < 32; x += 8)
+                    if (r < t.len && c + x < A.d) rp_store8(out + c + x, rp_close8<X>(v + x));
+                __syncwarp();
             }
-            if (r < u.len && A.lse) A.lse[(u.base + r) * A.l_token + h * A.l_head] = ok ? fmaf(m, A.scale, logf(l * exp2f(-LIFT))) : NAN;
+            if (r < t.len && A.lse) A.lse[(t.base + r) * A.l_token + h * A.l_head] = ok ? fmaf(m, A.scale, logf(l * exp2f(-LIFT))) : NAN;
             __syncwarp();
             tmem_before();
-            if (told) bar_arrive_warp(rp_smem(&sm.block_empty[round & 1]), lane);
         }
     }
     __syncwarp();
@@ -500,11 +323,11 @@ extern "C" int64_t rp_attend_workspace(const rp_attend_config *a, int64_t n_toke
     return plan_bytes(n_tokens, n_samples, 256);
 }
 
-template <typename X, int D, bool WINDOW>
+template <typename X, int D>
 static int launch(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const AttendArgs &A, int ctas, cudaStream_t stream)
 {
-    const size_t smem = sizeof(FwdSmem<D, WINDOW>) + 1024;
-    RP_CUDA(cudaFuncSetAttribute(k_attend<X, D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const size_t smem = sizeof(FwdSmem<D>) + 1024;
+    RP_CUDA(cudaFuncSetAttribute(k_attend<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t how = {};                         // (barriers, tensor memory and maps are got ready beside the planning)
     how.gridDim = dim3((unsigned)ctas);
     how.blockDim = dim3(ATTEND_THREADS);
@@ -514,7 +337,7 @@ static int launch(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap 
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     how.attrs = &early; how.numAttrs = 1;
-    RP_CUDA(cudaLaunchKernelEx(&how, k_attend<X, D, WINDOW>, q, k, v, A));
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend<X, D>, q, k, v, A));
     return rp_op_launched();
 }
 
@@ -567,12 +390,9 @@ static int attend(const rp_attend_config *a, int window, int sinks, i64 n_tokens
     A.status = &head->status; A.wait_ns = (u64)g_attend_wait_ns;
     const int ctas = (int)std::min((i64)rp_op_sms(dev.device), (i64)P.most * a->q_heads);
     const bool half = a->type == RP_F16, narrow = a->head_dim <= 64;
-    if (window) {
-        if (half) return narrow ? launch<__half, 64, true>(mq, mk, mv, A, ctas, stream) : launch<__half, 128, true>(mq, mk, mv, A, ctas, stream);
-        return narrow ? launch<bf16, 64, true>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128, true>(mq, mk, mv, A, ctas, stream);
-    }
-    if (half) return narrow ? launch<__half, 64, false>(mq, mk, mv, A, ctas, stream) : launch<__half, 128, false>(mq, mk, mv, A, ctas, stream);
-    return narrow ? launch<bf16, 64, false>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128, false>(mq, mk, mv, A, ctas, stream);
+    if (window) return rp_launch_attend_window(a->type, a->head_dim, mq, mk, mv, A, ctas, stream);
+    if (half) return narrow ? launch<__half, 64>(mq, mk, mv, A, ctas, stream) : launch<__half, 128>(mq, mk, mv, A, ctas, stream);
+    return narrow ? launch<bf16, 64>(mq, mk, mv, A, ctas, stream) : launch<bf16, 128>(mq, mk, mv, A, ctas, stream);
 }
 
 extern "C" int rp_attend(const rp_attend_config *a, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v, const int64_t *start,

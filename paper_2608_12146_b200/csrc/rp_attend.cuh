@@ -153,6 +153,23 @@ static __device__ __noinline__ void rp_attend_clear(const AttendClears &A, const
         }
     }
 }
+struct AttendArgs {
+    const AttendHead *head;
+    const int2 *items;
+    const i64 *start;
+    i64 T;
+    int N, Hq, share, d, causal;            // share: query heads to a key head
+    int window, sinks;
+    float scale;
+    void *out;
+    i64 o_token, o_head;
+    float *lse;
+    i64 l_token, l_head;
+    int *status;
+    u64 wait_ns;
+};
+
+int rp_launch_attend_window(int type, int d, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const AttendArgs &A, int ctas, cudaStream_t stream);
 extern i64 g_attend_wait_ns;             // limit of the kernels' waits (rp_debug_set_wait_limit)
 int rp_attend_check(const rp_attend_config *a, i64 T, int N);
 int rp_attend_check_window(const rp_attend_config *a, int window, int sinks, i64 T, int N);
@@ -172,7 +189,6 @@ static inline bool rp_attend_shared(const rp_view *const *v, int n_out, int n)
 #define ATTEND_THREADS 384
 #define ATTEND_COPY_WARP 8
 #define ATTEND_MMA_WARP 9
-#define ATTEND_LIST_WARP 10
 __device__ __forceinline__ void rp_many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 216;"); }
 __device__ __forceinline__ void rp_few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
 

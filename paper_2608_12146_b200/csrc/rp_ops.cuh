@@ -169,6 +169,12 @@ __device__ __forceinline__ float rp_exp2(float x)        // 2^x by the special f
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float rp_max3(float x, float y, float z)        // the largest of three; NaN counts as none
+{
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+    return m;
+}
 #define RP_LOG2E 1.4426950408889634f
 __device__ __forceinline__ f2 rp_exp2(f2 x)
 {
