@@ -193,19 +193,31 @@ k_attend_window(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         const float sl = A.scale * RP_LOG2E;
         const f2 sl2 = rp_f2(sl, sl);
         u32 ss = 0, os = 0;
-        for (int round = 0;; ++round) {
-            // (beside a row's scores there is no room for much: with a window, what a block's steps go by stays in shared memory and is worked out anew in each)
+        // A block as the group sees it: the item (-1: none any more), whether the warp was told of it, the steps that its tile takes part in.  (Beside a row's scores there
+        // is no room for much: what a block's steps go by stays in shared memory and is worked out anew in each.)
+        struct Block { int at, first, end; bool told; };
+        const auto look = [&](int round) {
+            Block x;
             volatile int *const block = sm.block[round & 1];
-            const bool told = bar_wait_warp(rp_smem(&sm.block_full[round & 1]), (round >> 1) & 1, waits);
-            const int at = told ? block[0] : rp_attend_item(round, total);
-            if (at < 0) break;
-            const AttendTile t = told ? AttendTile(block) : AttendTile(A.items, A.start, A.T, at / A.Hq, 256);
-            if (t.row0 + 128 * i >= t.len) {
+            x.told = bar_wait_warp(rp_smem(&sm.block_full[round & 1]), (round >> 1) & 1, waits);
+            x.at = x.told ? block[0] : rp_attend_item(round, total);
+            x.first = x.end = 0;
+            if (x.at < 0) return x;
+            const AttendTile t = x.told ? AttendTile(block) : AttendTile(A.items, A.start, A.T, x.at / A.Hq, 256);
+            const AttendOrder order(t.row0, t.len, A.window, A.sinks);
+            if (t.row0 + 128 * i < t.len) { x.first = order.first(i); x.end = order.last[i] + 1; }
+            return x;
+        };
+        Block next = look(0);
+        for (int round = 0; next.at >= 0; ++round) {
+            volatile int *const block = sm.block[round & 1];
+            const int at = next.at, first = next.first, nk = next.end;
+            const bool told = next.told;
+            if (nk == 0) {                               // no rows of its own
                 if (told) bar_arrive_warp(rp_smem(&sm.block_empty[round & 1]), lane);
+                next = look(round + 1);
                 continue;
             }
-            const AttendOrder order(t.row0, t.len, A.window, A.sinks);
-            const int first = order.first(i), nk = order.last[i] + 1;
             float m = -INFINITY, l = 0.0f;
             bool ok = told;                              // (what is not told is not worked out: a wait has run out)
             for (int j = first; ok && j < nk; ++j) {
@@ -318,24 +330,25 @@ k_attend_window(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 tmem_before();
                 bar_arrive_warp(rp_smem(&sm.p_full[i]), lane);
             }
+            next = look(round + 1);                      // (while the last products are made)
             if (ok) ok = bar_wait_warp(rp_smem(&sm.o_full[i]), os & 1, waits) && !waits->gave_up;
             ++os;
             tmem_after();
             const float f = ok ? 1.0f / l : NAN;
-            const AttendTile u = told ? AttendTile(block) : t;
+            const AttendTile u = told ? AttendTile(block) : AttendTile(A.items, A.start, A.T, at / A.Hq, 256);
             const int r0 = u.row0 + 128 * i, r = r0 + row, h = at % A.Hq;
             X *const out = (X *)A.out + u.base * A.o_token + h * A.o_head;
             // through shared memory, 64 columns at a time: rows of 128 bytes go out whole (each lane its own row, 16 bytes at a time: 2000 cycles for 500)
             unsigned char *const rows = sm.rows[warp];
+            u32 o[D];
+#pragma unroll
+            for (int c = 0; c < D; c += 32) tmem_load32(to + c, o + c);
+            tmem_loaded();
 #pragma unroll
             for (int c = 0; c < D; c += 64) {
-                u32 o[64];
-                tmem_load32(to + c, o);
-                tmem_load32(to + c + 32, o + 32);
-                tmem_loaded();
                 float v[64];
 #pragma unroll
-                for (int x = 0; x < 64; ++x) v[x] = __uint_as_float(o[x]) * f;
+                for (int x = 0; x < 64; ++x) v[x] = __uint_as_float(o[c + x]) * f;
 #pragma unroll
                 for (int x = 0; x < 8; ++x) *(Pack8<X> *)(rows + lane * 128 + ((x ^ (lane & 7)) << 4)) = rp_close8<X>(v + 8 * x);
                 __syncwarp();
