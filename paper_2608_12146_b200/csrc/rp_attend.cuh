@@ -205,6 +205,7 @@ __device__ __forceinline__ int rp_attend_item(int round, int total)
 struct AttendTile {
     i64 base;
     int len, row0;
+    __device__ __forceinline__ AttendTile() : base(0), len(0), row0(0) { }
     __device__ __forceinline__ AttendTile(const int2 *items, const i64 *start, i64 T, int item, int rows)
     {
         const int2 it = items[item];

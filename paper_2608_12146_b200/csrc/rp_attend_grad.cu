@@ -372,7 +372,18 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     rp_parts(rp_exp2(rp_fma(rp_f2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sl2, f2{ l.x })), p[c], p[c + 1]);
                     rp_parts(rp_exp2(rp_fma(rp_f2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), sl2, f2{ l.y })), p[c + 2], p[c + 3]);
                 }
-                if (q0 + 64 > t.len || (A.causal && q0 < t.row0 + 128) || (WINDOW && q0 + 63 >= t.row0 + A.window)) {
+                const bool behind = q0 + 64 > t.len || (WINDOW && q0 + 63 >= t.row0 + A.window), before = A.causal && q0 < t.row0 + 128;
+                if (WINDOW && before != behind) {
+                    // (one comparison a column, where one will do)
+                    const int lo = r - q0, hi = (r >= A.sinks ? min(t.len, r + A.window) : t.len) - q0;
+                    if (before) {
+#pragma unroll
+                        for (int c = 0; c < 64; ++c) p[c] = c >= lo ? p[c] : 0.0f;
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 64; ++c) p[c] = c < hi ? p[c] : 0.0f;
+                    }
+                } else if (before || behind) {
                     const int lo = A.causal ? r - q0 : 0, hi = (WINDOW && r >= A.sinks ? min(t.len, r + A.window) : t.len) - q0;
 #pragma unroll
                     for (int c = 0; c < 64; ++c) p[c] = c >= lo && c < hi ? p[c] : 0.0f;
@@ -441,7 +452,7 @@ template <int D> struct QuerySmem {
     alignas(1024) unsigned char v[STAGES][TILE];
     u64 q_full, kv_full[STAGES], kv_empty[STAGES], s_full, s_empty, dp_full, ds_full, acc_full, item_full[2], item_empty[2], done;
     u32 tmem;
-    volatile int item[2];
+    alignas(16) volatile int item[2][4];     // the item, its sample's first row and length, its own first row
     int taken, handled[8];                   // when a wait has run out: blocks that the CTA took, blocks that each warp of the softmax handed over
     Waits waits;
 };
@@ -483,11 +494,11 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 if (!(ok = bar_place(n > 1, rp_smem(&sm.item_empty[n & 1]), ((n >> 1) - 1) & 1, waits))) break;
                 int at = atomicAdd(&A.head->ticket, 1);
                 if (at >= total) at = -1;
-                sm.item[n & 1] = at;
+                const AttendTile t = at < 0 ? AttendTile() : AttendTile(A.items, A.start, A.T, at / A.Hq, 128);
+                sm.item[n & 1][0] = at; sm.item[n & 1][1] = (int)t.base; sm.item[n & 1][2] = t.len; sm.item[n & 1][3] = t.row0;
                 bar_arrive(rp_smem(&sm.item_full[n & 1]));
                 if (at < 0) break;
                 taken = n + 1;
-                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
                 const AttendSteps w(WINDOW ? t.row0 : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
                 const int hk = at % A.Hq / A.share, seen = rp_attend_tiles(t, 0, A.causal), nk = WINDOW ? w.steps(seen) : seen;
                 for (int j = 0; j < nk; ++j, ++fill) {
@@ -508,17 +519,19 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
         if (warp == ATTEND_MMA_WARP) {
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
+            const int groups = WINDOW ? (int)rp_uniform((A.sinks + 31) >> 5) : 0;         // first tokens by 32: as narrow is the step that they are from afar
+            const u32 shape_first = mma_shape<X>(32 * groups, false);
             u32 base = 0;                               // tiles of the items before
             for (int n = 0;; ++n) {
                 bar_hold(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, waits);
-                const int at = rp_uniform(sm.item[n & 1]);
+                const int at = rp_uniform(sm.item[n & 1][0]);
                 if (at < 0 || rp_uniform(waits->gave_up)) break;
+                const AttendTile t(sm.item[n & 1]);
                 bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
-                const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
                 const AttendSteps w(WINDOW ? (int)rp_uniform(t.row0) : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
                 const int len = rp_uniform(t.len), seen = rp_uniform(rp_attend_tiles(t, 0, A.causal)), nk = WINDOW ? w.steps(seen) : seen;
                 // 128 queries (or gradients) against a tile's keys (or values)
-                auto against = [&](u32 to, u32 rows, const unsigned char *tile, u32 bar) {
+                auto against = [&](u32 to, u32 rows, const unsigned char *tile, u32 shape_s, u32 bar) {
                     const u32 b = mma_operand(rp_smem(tile), true, 0);
                     if (rp_elect()) {
 #pragma unroll
@@ -533,31 +546,36 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
                     const int behind = len - (WINDOW ? w.tile(j) : j) * 128;
                     if (behind < 128) rp_clear_rows<D>(sm.k[f % STAGES], behind, 128, lane);
+                    if (WINDOW && j < w.ahead) rp_clear_rows<D>(sm.k[f % STAGES], A.sinks, 32 * groups, lane);           // (neither are those behind the first tokens seen)
                 };
                 arrived(0);
                 // (who has handed over q and do has taken dq of the block before)
                 bar_hold(rp_smem(&sm.q_full), n & 1, waits);
                 tmem_after();
-                against(tm, tm + 384, sm.k[base % STAGES], rp_smem(&sm.s_full));
-                against(tm + 128, tm + 448, sm.v[base % STAGES], rp_smem(&sm.dp_full));
+                against(tm, tm + 384, sm.k[base % STAGES], w.ahead ? shape_first : shape_s, rp_smem(&sm.s_full));
+                against(tm + 128, tm + 448, sm.v[base % STAGES], w.ahead ? shape_first : shape_s, rp_smem(&sm.dp_full));
                 for (int j = 0; j < nk; ++j) {
                     const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
                     if (j + 1 < nk) {
                         arrived(j + 1);
                         bar_hold(rp_smem(&sm.s_empty), f & 1, waits);
                         tmem_after();
-                        against(tm, tm + 384, sm.k[s1], rp_smem(&sm.s_full));
+                        against(tm, tm + 384, sm.k[s1], shape_s, rp_smem(&sm.s_full));
                     }
                     bar_hold(rp_smem(&sm.ds_full), f & 1, waits);
                     tmem_after();
                     const u32 k = mma_operand(rp_smem(sm.k[s]), false, PANEL);
                     if (rp_elect()) {
+                        if (WINDOW && j < w.ahead)
+                            for (int x = 0; x < 2 * groups; ++x) mma_ts(tm + 256, tm + 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, x > 0);
+                        else {
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) mma_ts(tm + 256, tm + 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                            for (int x = 0; x < 8; ++x) mma_ts(tm + 256, tm + 128 + (x / 4) * 64 + (x % 4) * 8, k + x * (2048 >> 4), shape_o, j > 0 || x > 0);
+                        }
                     }
                     __syncwarp();
                     mma_commit_warp(rp_smem(&sm.kv_empty[s]));
-                    if (j + 1 < nk) against(tm + 128, tm + 448, sm.v[s1], rp_smem(&sm.dp_full));
+                    if (j + 1 < nk) against(tm + 128, tm + 448, sm.v[s1], shape_s, rp_smem(&sm.dp_full));
                     else mma_commit_warp(rp_smem(&sm.acc_full));
                 }
                 base += nk;
@@ -574,12 +592,13 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         u32 f = 0;                                      // tiles so far
         u32 w[64];                                      // a row of q (first group) or of do (second): two elements a word
         int at = 0;                                     // the item
+        AttendTile block;
         auto fetch = [&](int n) {
             at = -1;
-            if (bar_wait_warp(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, waits)) at = sm.item[n & 1];
+            if (bar_wait_warp(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, waits)) at = sm.item[n & 1][0];
             if (at < 0) return;
+            const AttendTile t = block = AttendTile(sm.item[n & 1]);
             bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
-            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
             const int r = t.row0 + row;
             const X *p = (b ? (const X *)A.rows[1] + (t.base + r) * A.r_token[1] + at % A.Hq * A.r_head[1] : (const X *)A.rows[0] + (t.base + r) * A.r_token[0] + at % A.Hq * A.r_head[0]);
 #pragma unroll
@@ -592,7 +611,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         fetch(0);
         int n = 0;
         for (; at >= 0; ++n) {
-            const AttendTile t(A.items, A.start, A.T, at / A.Hq, 128);
+            const AttendTile t = block;
             const AttendSteps steps(WINDOW ? t.row0 : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
             const int h = at % A.Hq, seen = rp_attend_tiles(t, 0, A.causal), nk = WINDOW ? steps.steps(seen) : seen, r = t.row0 + row;
 #pragma unroll
@@ -608,6 +627,13 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             for (int j = 0; j < nk; ++j, ++f) {
                 if (!(ok = bar_wait_warp(rp_smem(&sm.s_full), f & 1, waits))) break;
                 tmem_after();
+                if (WINDOW && j < steps.ahead && b * 64 >= A.sinks) {
+                    // first tokens from afar, of which there are none in this group's columns
+                    bar_arrive_warp(rp_smem(&sm.s_empty), lane);
+                    if (!(ok = bar_wait_warp(rp_smem(&sm.dp_full), f & 1, waits))) break;
+                    bar_arrive_warp(rp_smem(&sm.ds_full), lane);
+                    continue;
+                }
                 u32 s[64];
                 f2 p[32];
                 tmem_load32(ts, s);
@@ -628,20 +654,31 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     const f2 dp = rp_f2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
                     p[c] = rp_mul(p[c], Narrow<X>::value ? rp_fma(dp, c2, delta2) : rp_add(dp, delta2));
                 }
-                if (WINDOW && k0 <= t.row0 + 127 - A.window) {
-                    const int from = r - A.window + 1 - k0, ahead = A.sinks - k0;
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        float x, y;
-                        rp_parts(p[c], x, y);
-                        s[c] = rp_pair(2 * c < lim && (2 * c >= from || 2 * c < ahead) ? x : 0.0f, 2 * c + 1 < lim && (2 * c + 1 >= from || 2 * c + 1 < ahead) ? y : 0.0f, X());
-                    }
-                } else if (k0 + 64 > t.len || (A.causal && k0 + 63 > t.row0)) {
+                const bool behind = k0 + 64 > t.len || (A.causal && k0 + 63 > t.row0), before = WINDOW && k0 <= t.row0 + 127 - A.window;
+                if (behind && !before) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) {
                         float x, y;
                         rp_parts(p[c], x, y);
                         s[c] = rp_pair(2 * c < lim ? x : 0.0f, 2 * c + 1 < lim ? y : 0.0f, X());
+                    }
+                } else if (before) {
+                    // (the end of the window's reach and the row's own place are never both in 64 columns but with short windows)
+                    const int from = r - A.window + 1 - k0, ahead = A.sinks - k0;
+                    if (!behind && ahead <= 0) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            float x, y;
+                            rp_parts(p[c], x, y);
+                            s[c] = rp_pair(2 * c >= from ? x : 0.0f, 2 * c + 1 >= from ? y : 0.0f, X());
+                        }
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            float x, y;
+                            rp_parts(p[c], x, y);
+                            s[c] = rp_pair(2 * c < lim && (2 * c >= from || 2 * c < ahead) ? x : 0.0f, 2 * c + 1 < lim && (2 * c + 1 >= from || 2 * c + 1 < ahead) ? y : 0.0f, X());
+                        }
                     }
                 } else {
 #pragma unroll
@@ -678,7 +715,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 if (r < t.len && c < A.d) ((X *)A.x[0])[(t.base + r) * A.token[0] + at % A.Hq * A.hd[0] + c] = rp_round<X>(NAN);
             }
         };
-        for (int n = sm.handled[warp]; n < sm.taken; ++n) mark(sm.item[n & 1], row & ~31, 32, b * (D / 2), D / 2);
+        for (int n = sm.handled[warp]; n < sm.taken; ++n) mark(sm.item[n & 1][0], row & ~31, 32, b * (D / 2), D / 2);
         for (;;) {
             int at = lane == 0 ? atomicAdd(&A.head->ticket, 1) : 0;
             at = __shfl_sync(0xffffffffu, at, 0);
