@@ -28,8 +28,6 @@ struct GradArgs {
     i64 token[2], hd[2];
     int *status;
     u64 wait_ns;
-    const void *rows[2];                     // queries' kernel: q, do
-    i64 r_token[2], r_head[2];
 };
 
 // Before the two kernels: CTA 0 lists the blocks of keys, CTA 1 those of queries, the others clear the rows that no sample holds and work out lse / ln 2 and delta of
@@ -135,6 +133,34 @@ __device__ __forceinline__ void store_row(u32 at, X *out, int d, bool there, flo
             if (there && c + x < d) rp_store8(out + c + x, rp_close8<X>(v + x));
         __syncwarp();
     }
+}
+
+// The same for 32 rows of a warp, through `rows` in shared memory (2 D bytes a row): pieces of 16 bytes side by side go out together.  (Each lane its own row: 32 lines
+// an instruction.)
+template <typename X, int D>
+__device__ __forceinline__ void store_rows(u32 at, X *out, i64 step, int d, int left, float f, unsigned char *rows, int lane)
+{
+    constexpr int PIECES = D / 8, EACH = 32 / PIECES;
+    const auto place = [](int row, int piece) { return row * (2 * D) + ((piece ^ (PIECES == 8 ? row & 7 : row >> 1 & 3)) << 4); };
+    u32 o[D];
+#pragma unroll
+    for (int c = 0; c < D; c += 32) tmem_load32(at + c, o + c);
+    tmem_loaded();
+#pragma unroll
+    for (int x = 0; x < PIECES; ++x) {
+        float v[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) v[y] = __uint_as_float(o[8 * x + y]) * f;
+        *(Pack8<X> *)(rows + place(lane, x)) = rp_close8<X>(v);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int x = 0; x < PIECES; ++x) {
+        const int row = x * EACH + lane / PIECES, piece = lane % PIECES;
+        const Pack8<X> w = *(const Pack8<X> *)(rows + place(row, piece));
+        if (row < left && 8 * piece < d) rp_store8(out + row * step + 8 * piece, w);
+    }
+    __syncwarp();
 }
 
 // The same in 32 bits.
@@ -444,7 +470,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 // ---------------------------------------------------------------------------------------
 // Tiles of 128 keys, 64 columns to each of the two groups of four warps.  q and do, which all tiles of a block share, lie in tensor memory as the operands of their
 // products: from shared memory a product of 128 x 128 x 16 reads all of the 128 bytes that a cycle of it has, with the copies coming in beside (220 us for what
-// takes 166).  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
+// takes 166).  They come through the ring that brings keys and values, ahead of these: each lane reads its row there and puts it into tensor memory.  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
 // tile and do v^T of the next while the weights of the next are.  Columns: scores 128, do v^T 128 (and in its place ds as operand), dq, q and do 64 each.
 template <int D> struct QuerySmem {
     static constexpr int TILE = 128 * D * 2, STAGES = 3;
@@ -453,13 +479,15 @@ template <int D> struct QuerySmem {
     u64 q_full, kv_full[STAGES], kv_empty[STAGES], s_full, s_empty, dp_full, ds_full, acc_full, item_full[2], item_empty[2], done;
     u32 tmem;
     alignas(16) volatile int item[2][4];     // the item, its sample's first row and length, its own first row
+    alignas(16) unsigned char rows[8][64 * D / 2];      // of each warp, what it hands over
     int taken, handled[8];                   // when a wait has run out: blocks that the CTA took, blocks that each warp of the softmax handed over
     Waits waits;
 };
 
 template <typename X, int D, bool WINDOW>
 __global__ void __launch_bounds__(ATTEND_THREADS, 1)
-k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const GradArgs A)
+k_attend_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                 const __grid_constant__ CUtensorMap map_g, const GradArgs A)
 {
     typedef QuerySmem<D> Smem;
     constexpr int STAGES = Smem::STAGES, PANELS = D / 64, PANEL = 128 * 128;
@@ -485,7 +513,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (warp >= 8) {
         rp_few_registers();
         if (warp == ATTEND_COPY_WARP && lane == 0) {
-            tma_prefetch(&map_k); tma_prefetch(&map_v);
+            tma_prefetch(&map_q); tma_prefetch(&map_k); tma_prefetch(&map_v); tma_prefetch(&map_g);
             u32 fill = 0;
             int taken = 0;
             bool ok = true;
@@ -501,15 +529,15 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 taken = n + 1;
                 const AttendSteps w(WINDOW ? t.row0 : 0, WINDOW ? A.window : 1, WINDOW ? A.sinks : 0);
                 const int hk = at % A.Hq / A.share, seen = rp_attend_tiles(t, 0, A.causal), nk = WINDOW ? w.steps(seen) : seen;
-                for (int j = 0; j < nk; ++j, ++fill) {
-                    const int from = (int)t.base + (WINDOW ? w.tile(j) : j) * 128;
+                for (int j = -1; j < nk; ++j, ++fill) {             // (-1: the block's own q and do)
+                    const int from = j < 0 ? (int)t.base + t.row0 : (int)t.base + (WINDOW ? w.tile(j) : j) * 128, head = j < 0 ? at % A.Hq : hk;
                     const u32 s = fill % STAGES, turn = fill / STAGES;
                     if (!(ok = bar_place(turn, rp_smem(&sm.kv_empty[s]), (turn - 1) & 1, waits))) break;
                     bar_expect(rp_smem(&sm.kv_full[s]), 2 * Smem::TILE);
                     waits->copied = fill + 1;
                     for (int p = 0; p < PANELS; ++p) {
-                        tma_load3(rp_smem(sm.k[s]) + p * PANEL, &map_k, p * 64, hk, from, rp_smem(&sm.kv_full[s]));
-                        tma_load3(rp_smem(sm.v[s]) + p * PANEL, &map_v, p * 64, hk, from, rp_smem(&sm.kv_full[s]));
+                        tma_load3(rp_smem(sm.k[s]) + p * PANEL, j < 0 ? &map_q : &map_k, p * 64, head, from, rp_smem(&sm.kv_full[s]));
+                        tma_load3(rp_smem(sm.v[s]) + p * PANEL, j < 0 ? &map_g : &map_v, p * 64, head, from, rp_smem(&sm.kv_full[s]));
                     }
                 }
             }
@@ -521,8 +549,8 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             const u32 shape_s = mma_shape<X>(128, false), shape_o = mma_shape<X>(D, true);
             const int groups = WINDOW ? (int)rp_uniform((A.sinks + 31) >> 5) : 0;         // first tokens by 32: as narrow is the step that they are from afar
             const u32 shape_first = mma_shape<X>(32 * groups, false);
-            u32 base = 0;                               // tiles of the items before
-            for (int n = 0;; ++n) {
+            u32 base = 0, stage = 0;                    // tiles of the items before, and stages
+            for (int n = 0;; ++n, ++stage) {
                 bar_hold(rp_smem(&sm.item_full[n & 1]), (n >> 1) & 1, waits);
                 const int at = rp_uniform(sm.item[n & 1][0]);
                 if (at < 0 || rp_uniform(waits->gave_up)) break;
@@ -540,8 +568,9 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     }
                     __syncwarp();
                 };
+                const u32 own = stage % STAGES;
                 auto arrived = [&](int j) {             // a tile's keys and values
-                    const u32 f = base + j;
+                    const u32 f = stage + 1 + j;
                     bar_hold(rp_smem(&sm.kv_full[f % STAGES]), (f / STAGES) & 1, waits);
                     // keys behind the sample's end are another sample's: the gradients of their scores are 0, and 0 times NaN would not be
                     const int behind = len - (WINDOW ? w.tile(j) : j) * 128;
@@ -549,13 +578,14 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     if (WINDOW && j < w.ahead) rp_clear_rows<D>(sm.k[f % STAGES], A.sinks, 32 * groups, lane);           // (neither are those behind the first tokens seen)
                 };
                 arrived(0);
-                // (who has handed over q and do has taken dq of the block before)
+                // (who has handed over q and do has taken dq of the block before, and has read them in their stage)
                 bar_hold(rp_smem(&sm.q_full), n & 1, waits);
                 tmem_after();
-                against(tm, tm + 384, sm.k[base % STAGES], w.ahead ? shape_first : shape_s, rp_smem(&sm.s_full));
-                against(tm + 128, tm + 448, sm.v[base % STAGES], w.ahead ? shape_first : shape_s, rp_smem(&sm.dp_full));
+                bar_arrive_warp(rp_smem(&sm.kv_empty[own]), lane);
+                against(tm, tm + 384, sm.k[(stage + 1) % STAGES], w.ahead ? shape_first : shape_s, rp_smem(&sm.s_full));
+                against(tm + 128, tm + 448, sm.v[(stage + 1) % STAGES], w.ahead ? shape_first : shape_s, rp_smem(&sm.dp_full));
                 for (int j = 0; j < nk; ++j) {
-                    const u32 f = base + j, s = f % STAGES, s1 = (f + 1) % STAGES;
+                    const u32 f = base + j, s = (stage + 1 + j) % STAGES, s1 = (stage + 2 + j) % STAGES;
                     if (j + 1 < nk) {
                         arrived(j + 1);
                         bar_hold(rp_smem(&sm.s_empty), f & 1, waits);
@@ -579,6 +609,7 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     else mma_commit_warp(rp_smem(&sm.acc_full));
                 }
                 base += nk;
+                stage += nk;
             }
             // nobody may leave while products are under way
             mma_commit_warp(rp_smem(&sm.done));
@@ -599,12 +630,14 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             if (at < 0) return;
             const AttendTile t = block = AttendTile(sm.item[n & 1]);
             bar_arrive_warp(rp_smem(&sm.item_empty[n & 1]), lane);
-            const int r = t.row0 + row;
-            const X *p = (b ? (const X *)A.rows[1] + (t.base + r) * A.r_token[1] + at % A.Hq * A.r_head[1] : (const X *)A.rows[0] + (t.base + r) * A.r_token[0] + at % A.Hq * A.r_head[0]);
+            // its own row, from the stage ahead of its block's keys (tiles and blocks so far)
+            const u32 g = f + n, s = g % STAGES;
+            const bool come = bar_wait_warp(rp_smem(&sm.kv_full[s]), (g / STAGES) & 1, waits) && t.row0 + row < t.len;
+            const unsigned char *p = (b ? sm.v[s] : sm.k[s]) + row * 128;
 #pragma unroll
             for (int c = 0; c < D / 8; ++c) {
                 uint4 v = make_uint4(0, 0, 0, 0);
-                if (r < t.len && c * 8 < A.d) v = *(const uint4 *)(p + c * 8);
+                if (come) v = *(const uint4 *)(p + (c >> 3) * PANEL + (((c & 7) ^ (row & 7)) << 4));
                 w[4 * c] = v.x; w[4 * c + 1] = v.y; w[4 * c + 2] = v.z; w[4 * c + 3] = v.w;
             }
         };
@@ -697,8 +730,9 @@ k_attend_queries(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             if (ok) ok = bar_wait_warp(rp_smem(&sm.acc_full), n & 1, waits) && !waits->gave_up;
             tmem_after();
             // each group hands over one half of the columns
-            X *out = (X *)A.x[0] + (t.base + r) * A.token[0] + h * A.hd[0] + b * (D / 2);
-            store_row<X, D / 2>(tm + lanes + 256 + b * (D / 2), out, A.d - b * (D / 2), r < t.len, !ok ? NAN : Narrow<X>::value ? A.scale / c1 : A.scale);
+            X *out = (X *)A.x[0] + (t.base + t.row0 + (row & ~31)) * A.token[0] + h * A.hd[0] + b * (D / 2);
+            store_rows<X, D / 2>(tm + lanes + 256 + b * (D / 2), out, A.token[0], A.d - b * (D / 2), t.len - t.row0 - (row & ~31),
+                                 !ok ? NAN : Narrow<X>::value ? A.scale / c1 : A.scale, sm.rows[warp], lane);
             tmem_before();
         }
         if (lane == 0) sm.handled[warp] = n;
@@ -799,7 +833,7 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     how.attrs = &early; how.numAttrs = 1;
-    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_queries<X, D, WINDOW>, M.k, M.v, (const GradArgs)queries));
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_queries<X, D, WINDOW>, M.q, M.k, M.v, M.g, (const GradArgs)queries));
     return rp_op_launched();
 }
 
@@ -851,8 +885,6 @@ static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_t
     }
     G[0].x[0] = v_grad->x; G[0].token[0] = v_grad->token; G[0].hd[0] = v_grad->head;
     G[0].x[1] = k_grad->x; G[0].token[1] = k_grad->token; G[0].hd[1] = k_grad->head;
-    G[1].rows[0] = q->x; G[1].r_token[0] = q->token; G[1].r_head[0] = q->head;
-    G[1].rows[1] = out_grad->x; G[1].r_token[1] = out_grad->token; G[1].r_head[1] = out_grad->head;
     G[1].x[0] = q_grad->x; G[1].token[0] = q_grad->token; G[1].hd[0] = q_grad->head;
     const int sms = rp_op_sms(dev.device);
     float *const norms = (float *)(stats + T * Hq);
