@@ -15,6 +15,18 @@ struct AttendPlan {
 };
 struct AttendClears { AttendClear x[3]; int n; };       // outputs whose rows of no sample are cleared
 
+// 16 rows by 8 columns by 16 of a warp's own product, for what is too small for the tensor cores' large ones: operands and sums in registers.
+__device__ __forceinline__ void rp_multiply(float *c, const u32 *a, const u32 *b, bf16)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ void rp_multiply(float *c, const u32 *a, const u32 *b, __half)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
 // ---- window -----------------------------------------------------------------------------
 // Token i of a sample sees j <= i with i - j < window or j < sinks.  The first tokens lie in the sample's first tile of 128 keys (sinks <= 128).
 #define ATTEND_SINKS 128

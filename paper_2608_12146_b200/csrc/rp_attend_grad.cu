@@ -93,9 +93,9 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
 }
 
 // The largest of a sample's rows of do, for float16 (infinities and NaN, which no factor mends, do not count): a thread a token.
-__global__ void __launch_bounds__(256) k_attend_tops(const i64 *start, int N, i64 T, int H, const float *norms, u32 *tops)
+static __device__ __forceinline__ void rp_attend_tops(const i64 *start, int N, i64 T, int H, const float *norms, u32 *tops, int block)
 {
-    const i64 t = (i64)blockIdx.x * 256 + threadIdx.x;
+    const i64 t = (i64)block * 256 + threadIdx.x;
     float top = 0.0f;
     for (int h = 0; t < T && h < H; ++h) {
         const float x = norms[h * T + t];
@@ -108,6 +108,76 @@ __global__ void __launch_bounds__(256) k_attend_tops(const i64 *start, int N, i6
         if (threadIdx.x & 31) bits = 0;
     }
     if (bits) atomicMax(tops + i, bits);
+}
+__global__ void __launch_bounds__(256) k_attend_tops(const i64 *start, int N, i64 T, int H, const float *norms, u32 *tops) { rp_attend_tops(start, N, T, H, norms, tops, blockIdx.x); }
+
+// With a window: delta of each sample's first tokens from its definition, sum_j p_j do v_j.  They see few keys, o is as large as v there, and what its rounding leaves in
+// do o is as much as the rounding of their scores' gradients (samples of 60 tokens: gradients of queries and keys 1.6 times as far off as with their own rounding alone,
+// 1.42 so; from the 33rd token on it is a sixth of that rounding and less).  A warp half of a sample's and a query head's.  Behind `first` such CTAs of eight warps those
+// for float16's largest rows.
+#define FIRST_TOKENS 32
+struct FirstArgs {
+    const i64 *start;
+    i64 T;
+    int N, H, share, d, window, sinks;
+    float scale;
+    const void *q, *k, *v, *g;
+    i64 q_token, q_head, k_token, k_head, v_token, v_head, g_token, g_head;
+    const float *lse;
+    i64 l_token, l_head;
+    float2 *stats;
+    const float *norms;
+    u32 *tops;
+    int first;
+};
+template <typename X>
+__global__ void __launch_bounds__(256) k_attend_first(const FirstArgs A)
+{
+    if ((int)blockIdx.x >= A.first) { rp_attend_tops(A.start, A.N, A.T, A.H, A.norms, A.tops, blockIdx.x - A.first); return; }
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    for (i64 unit = (i64)blockIdx.x * 8 + (threadIdx.x >> 5); unit < (i64)A.N * A.H * 2; unit += (i64)A.first * 8) {
+        const int i = (int)(unit / (2 * A.H)), h = (int)(unit % (2 * A.H)) >> 1, r0 = 16 * (int)(unit & 1), hk = h / A.share;
+        const i64 base = max(A.start[i], (i64)0);
+        const int n = (int)min(min(A.start[i + 1], A.T) - base, (i64)FIRST_TOKENS);
+        if (r0 >= n) continue;
+        // (rows behind the sample's end are read as its last one: nothing comes of them)
+        const int r[2] = { min(r0 + g, n - 1), min(r0 + g + 8, n - 1) };
+        const X *q = (const X *)A.q + base * A.q_token + h * A.q_head + 2 * t, *o = (const X *)A.g + base * A.g_token + h * A.g_head + 2 * t;
+        const X *k = (const X *)A.k + base * A.k_token + hk * A.k_head + 2 * t, *v = (const X *)A.v + base * A.v_token + hk * A.v_head + 2 * t;
+        float s[4][4] = { }, dp[4][4] = { };
+#pragma unroll 4
+        for (int c = 0; c < A.d; c += 16) {
+            const bool more = c + 8 < A.d;               // (a head of 8, 24, .. elements ends in the middle of a step)
+            const auto at = [&](const X *x, i64 row) { return *(const u32 *)(x + row + c); };
+            const auto behind = [&](const X *x, i64 row) { return more ? *(const u32 *)(x + row + c + 8) : 0u; };
+            const u32 a[4] = { at(q, r[0] * A.q_token), at(q, r[1] * A.q_token), behind(q, r[0] * A.q_token), behind(q, r[1] * A.q_token) };
+            const u32 b[4] = { at(o, r[0] * A.g_token), at(o, r[1] * A.g_token), behind(o, r[0] * A.g_token), behind(o, r[1] * A.g_token) };
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int j = min(8 * x + g, n - 1);
+                const u32 e[2] = { at(k, j * A.k_token), behind(k, j * A.k_token) }, f[2] = { at(v, j * A.v_token), behind(v, j * A.v_token) };
+                rp_multiply(s[x], a, e, X());
+                rp_multiply(dp[x], b, f, X());
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int row = r0 + g + 8 * u;
+            const float lse = A.lse[(base + r[u]) * A.l_token + h * A.l_head];
+            float delta = 0.0f;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int j = 8 * x + 2 * t + y;
+                    const bool sees = j <= row && j < n && (row - j < A.window || j < A.sinks);
+                    delta += sees ? rp_exp2((s[x][2 * u + y] * A.scale - lse) * RP_LOG2E) * dp[x][2 * u + y] : 0.0f;
+                }
+            delta += __shfl_xor_sync(0xffffffffu, delta, 1);
+            delta += __shfl_xor_sync(0xffffffffu, delta, 2);
+            if (row < n && t == 0) A.stats[(i64)h * A.T + base + row].y = delta;
+        }
+    }
 }
 // Power of two for the gradients of a sample's scores, from its largest row.
 __device__ __forceinline__ float ds_scale(u32 top)
@@ -794,8 +864,9 @@ template <typename X>
 __global__ void __launch_bounds__(256) k_attend_sinks(const i64 *start, int N, i64 T, int window, int sinks, int Hk, int d, const float *parts, X *dv, X *dk, i64 v_token,
                                                       i64 v_head, i64 k_token, i64 k_head)
 {
-    const int hk = blockIdx.y >> 1, b = blockIdx.y & 1, tokens = rp_attend_chunk(window) * 128;
-    for (int i = blockIdx.x; i < N; i += gridDim.x) {
+    const int tokens = rp_attend_chunk(window) * 128;
+    for (i64 unit = blockIdx.x; unit < (i64)N * Hk * 2; unit += gridDim.x) {
+        const int i = (int)(unit / (2 * Hk)), hk = (int)(unit % (2 * Hk)) >> 1, b = (int)(unit & 1);
         const i64 base = max(start[i], (i64)0);
         const i64 len = min(start[i + 1], T) - base;
         if (len <= tokens) continue;
@@ -892,14 +963,22 @@ static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_t
     G[0].tops = G[1].tops = tops;
     const StatsArgs S = { out->x, out_grad->x, (const float *)lse->x, out->token, out->head, out_grad->token, out_grad->head, lse->token, lse->head, Hq, d, stats, norms, tops };
     const int ctas = 2 + (int)std::min((T * Hq + 63) / 64, (i64)sms * 2 - 2);
-    if (a->type == RP_F16) {
-        k_attend_prepare<__half><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
-        RP_TRY(rp_op_launched());
-        k_attend_tops<<<(unsigned)((T + 255) / 256), 256, 0, stream>>>((const i64 *)start, n_samples, T, Hq, norms, tops);
-    }
+    const bool half = a->type == RP_F16;
+    if (half) k_attend_prepare<__half><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
     else k_attend_prepare<bf16><<<ctas, 1024, 0, stream>>>(P[0], P[1], C, S);
     RP_TRY(rp_op_launched());
-    const bool half = a->type == RP_F16;
+    const unsigned blocks = (unsigned)((T + 255) / 256);
+    if (window) {
+        const int first = (int)std::min(((i64)n_samples * Hq * 2 + 7) / 8, (i64)sms * 4);
+        const FirstArgs F = { (const i64 *)start, T, n_samples, Hq, Hq / Hk, d, window, sinks, a->scale, q->x, k->x, v->x, out_grad->x, q->token, q->head, k->token, k->head,
+                              v->token, v->head, out_grad->token, out_grad->head, (const float *)lse->x, lse->token, lse->head, stats, norms, tops, first };
+        if (half) k_attend_first<__half><<<first + blocks, 256, 0, stream>>>(F);
+        else k_attend_first<bf16><<<first, 256, 0, stream>>>(F);
+        RP_TRY(rp_op_launched());
+    } else if (half) {
+        k_attend_tops<<<blocks, 256, 0, stream>>>((const i64 *)start, n_samples, T, Hq, norms, tops);
+        RP_TRY(rp_op_launched());
+    }
     const i64 mk = P[0].most, mq = P[1].most;
     if (!window) {
         if (half) return d <= 64 ? launch<__half, 64, false>(M, G[0], G[1], mk, mq, sms, stream) : launch<__half, 128, false>(M, G[0], G[1], mk, mq, sms, stream);
@@ -908,7 +987,7 @@ static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_t
     if (half) RP_TRY((d <= 64 ? launch<__half, 64, true>(M, G[0], G[1], mk, mq, sms, stream) : launch<__half, 128, true>(M, G[0], G[1], mk, mq, sms, stream)));
     else RP_TRY((d <= 64 ? launch<bf16, 64, true>(M, G[0], G[1], mk, mq, sms, stream) : launch<bf16, 128, true>(M, G[0], G[1], mk, mq, sms, stream)));
     if (!more) return RP_OK;
-    const dim3 grid((unsigned)std::min(n_samples, 256), 2 * Hk);
+    const int grid = (int)std::min((i64)n_samples * Hk * 2, (i64)sms * 8);
     if (half)
         k_attend_sinks<<<grid, 256, 0, stream>>>((const i64 *)start, n_samples, T, window, sinks, Hk, d, G[0].parts, (__half *)v_grad->x, (__half *)k_grad->x, v_grad->token,
                                                  v_grad->head, k_grad->token, k_grad->head);

@@ -105,16 +105,6 @@ __device__ __forceinline__ void load_matrices_across(u32 at, u32 *r)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ void multiply(float *c, const u32 *a, const u32 *b, bf16)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
-}
-__device__ __forceinline__ void multiply(float *c, const u32 *a, const u32 *b, __half)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
-}
 // Two weights as a pair of the type and a pair of what that leaves of them: as operands they keep 16 bits and more (bf16 alone keeps 8).
 template <typename X> __device__ __forceinline__ void two_pairs(float a, float b, u32 &high, u32 &low)
 {
@@ -321,8 +311,8 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     u32 b[4];
                     const int r = n * 8 + (lane >> 4) * 8 + (lane & 7), p = 2 * ks + ((lane >> 3) & 1);
                     load_matrices(kt + (p >> 3) * PANEL + r * 128 + (((p & 7) ^ (r & 7)) << 4), b);
-                    multiply(s[n], a, b, X());
-                    multiply(s[n + 1], a, b + 2, X());
+                    rp_multiply(s[n], a, b, X());
+                    rp_multiply(s[n + 1], a, b + 2, X());
                 }
             }
             if (x + KEYS >= it.x1) look(unit + step);        // while this one is finished
@@ -386,9 +376,9 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
                             for (int i = 0; i < 4; ++i) b[i] &= keep[i & 1];
                         }
-                        multiply(o[n], a, b, X());
-                        multiply(o[n + 1], a, b + 2, X());
-                        if (!FEW) { multiply(o[n], rest, b, X()); multiply(o[n + 1], rest, b + 2, X()); }
+                        rp_multiply(o[n], a, b, X());
+                        rp_multiply(o[n + 1], a, b + 2, X());
+                        if (!FEW) { rp_multiply(o[n], rest, b, X()); rp_multiply(o[n + 1], rest, b + 2, X()); }
                     }
                 }
             };
