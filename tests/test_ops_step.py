@@ -252,3 +252,22 @@ def test_waits_that_run_out_leave_nan_and_a_status():
         rp.rp_debug_set_wait_limit()
     again = rp.rp_attend_step(q, k, v, st, status=status[2])
     assert [s.item() for s in status] == [0, -8, 0] and all(torch.isnan(x).all() for x in got) and all((a == b).all() for a, b in zip(again, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("limit", [1, 1500, 4000])
+def test_short_limits_leave_right_rows_or_nan(limit):
+    import torch
+    q, k, v, start = inputs((8, 2, 128, [30000, 1, 0, 200, 9000], 0, 0, 0), "bfloat16")
+    st, status = torch.tensor(start, device="cuda"), torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    want = rp.rp_attend_step(q, k, v, st)
+    rp.rp_debug_set_wait_limit(limit)
+    try:
+        got = rp.rp_attend_step(q, k, v, st, status=status)
+        torch.cuda.synchronize()
+    finally:
+        rp.rp_debug_set_wait_limit()
+    for x, y in zip(got, want):
+        lost = torch.isnan(x)
+        assert (x[~lost] == y[~lost]).all() and (status.item() == -8 or not lost.any())
+    assert status.item() in (0, -8)

@@ -355,3 +355,50 @@ def test_waits_that_run_out_leave_nan_and_a_status():
     again = rp.rp_attend_window(q, k, v, st, **kw)
     assert all((a == b).all() for a, b in zip(again, want))
     assert all((a == b).all() for a, b in zip(rp.rp_attend_window_grad(do, q, k, v, *again, st, **kw), back))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("limit", [1, 2000, 8000, 40000])
+def test_short_limits_leave_right_rows_or_nan(limit):
+    """Whatever wait runs out first: a row is right to the last bit or NaN, and NaN anywhere comes with the status."""
+    import torch
+    shape = (9000, 4, 2, 64, [0, 400, 9000])
+    q, k, v, g = inputs(shape, "bfloat16")
+    st, kw = torch.tensor(shape[4], device="cuda"), dict(window=300, sinks=4)
+    do = torch.randn(9000, 4, 64, generator=g).bfloat16().cuda()
+    want = rp.rp_attend_window(q, k, v, st, **kw)
+    back = rp.rp_attend_window_grad(do, q, k, v, *want, st, **kw)
+    status = [torch.full((1,), 7, dtype=torch.int32, device="cuda") for _ in range(2)]
+    rp.rp_debug_set_wait_limit(limit)
+    try:
+        got = rp.rp_attend_window(q, k, v, st, status=status[0], **kw)
+        grads = rp.rp_attend_window_grad(do, q, k, v, *want, st, status=status[1], **kw)
+        torch.cuda.synchronize()
+    finally:
+        rp.rp_debug_set_wait_limit()
+    for s, a, b in ((status[0], got, want), (status[1], grads, back)):
+        assert s.item() in (0, -8)
+        for x, y in zip(a, b):
+            lost = torch.isnan(x)
+            assert (x[~lost] == y[~lost]).all() and (s.item() == -8 or not lost.any())
+
+
+@pytest.mark.gpu
+def test_rows_without_samples_and_many_short_ones():
+    """No block at all, and more CTAs than blocks: zeros, no wait runs out; thousands of samples of a few tokens."""
+    import torch
+    q, k, v, g = inputs((1300, 2, 1, 64), "bfloat16")
+    do = torch.randn(1300, 2, 64, generator=g).bfloat16().cuda()
+    status = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    for start in ([0, 0], [1300, 1300], [5, 5, 5, 5], [-9, 0], [1200, 100]):
+        st = torch.tensor(start, device="cuda")
+        out, lse = rp.rp_attend_window(q, k, v, st, window=7, sinks=3, status=status)
+        assert (out == 0).all() and (lse == 0).all() and status.item() == 0
+        for x in rp.rp_attend_window_grad(do, q, k, v, out, lse, st, window=7, sinks=3, status=status):
+            assert (x == 0).all() and status.item() == 0
+    x = torch.randn(12000, 4, 64, generator=torch.Generator().manual_seed(9)).half().cuda()
+    st = torch.arange(0, 12001, 3, device="cuda")
+    out, lse = rp.rp_attend_window(x[:, :2], x[:, 2:3], x[:, 3:], st, window=2)
+    want, w_lse = rp.rp_attend(x[:, :2], x[:, 2:3], x[:, 3:], st)
+    two = torch.arange(12000, device="cuda") % 3 < 2                     # (the third token of each sees two of three)
+    assert (out[two] == want[two]).all() and (lse[two] == w_lse[two]).all() and not (out[~two] == want[~two]).all()
