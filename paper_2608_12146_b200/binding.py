@@ -603,7 +603,7 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
             x, w, out, g = (q, k)[i], weights[i], outs[i], grads[i]
             xt, xh = _head_strides(x, x, "input")
             if out is None:
-                out = x.new_empty(x.shape)
+                out = _like(torch, x)
                 yt, yh = x.shape[1] * d, d
             else:
                 yt, yh = _head_strides(out, x, "output")
@@ -710,6 +710,16 @@ def _hand_out(status, space, T, torch):
         status.copy_(space[:4].view(torch.int32)) if T else status.zero_()
 
 
+def _like(torch, x):
+    """A new dense tensor of the shape and type of `x` (the shorter way where it is dense itself)."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
+@functools.lru_cache(maxsize=256)
+def _step_workspace(q_heads, kv_heads, head_dim, kind, scale, *sizes):
+    return lib().rp_attend_step_workspace(_attention(q_heads, kv_heads, head_dim, kind, True, scale)[1], *sizes)
+
+
 def _int32(x, what: str) -> int:
     """A whole number for the C entries, what lies outside 32 bits as the next that does not (a window longer than any row, or one that is refused)."""
     try:
@@ -806,15 +816,16 @@ def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int =
     at, n = _starts(torch, start)
     N, H, d = q.shape
     _need(N == n, "q: a token for each sequence wanted")
-    ref = _attention(H, k.shape[1], d, _kind(q, "q"), True, scale)[1]
+    config = (H, k.shape[1], d, _kind(q, "q"))
+    ref = _attention(*config, True, scale)[1]
     window, sinks, T = _int32(window, "window"), _int32(sinks, "sinks"), k.shape[0]
     _dense(status, torch.int32, (1,), "status")
     with _Queue(torch, q, stream) as queue:
         if out is None:
-            out = q.new_empty(q.shape)
+            out = _like(torch, q)
         if lse is None:
             lse = q.new_empty((N, H), dtype=torch.float32)
-        nbytes = lib().rp_attend_step_workspace(ref, window, sinks, T, n)
+        nbytes = _step_workspace(*config, scale, window, sinks, T, n)
         space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         _check(lib().rp_attend_step(ref, window, sinks, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _dense(length, torch.int64, (n,), "length"),
                                     _view(out, q, "out"), _lse_view(lse, N, H, torch), space.data_ptr(), nbytes, queue.handle), "rp_attend_step")
