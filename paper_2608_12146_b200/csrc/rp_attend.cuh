@@ -92,6 +92,7 @@ static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
 {
     __shared__ int count[PLAN_BUCKETS];
     __shared__ int from[PLAN_BUCKETS], sums[32];
+    const int shift = A.rows == 256 ? 8 : 7, chunk = rp_attend_chunk(A.window);
     for (int x = threadIdx.x; x < PLAN_BUCKETS; x += 1024) count[x] = 0;
     __syncthreads();
     for (int pass = 0; pass < 2; ++pass) {
@@ -101,14 +102,13 @@ static __device__ __noinline__ void rp_attend_plan(const AttendPlan &A)
         for (int i0 = threadIdx.x & ~31; i0 < A.N; i0 += 1024) {
             const int i = i0 + lane;
             const i64 lo = i < A.N ? max(A.start[i], (i64)0) : 0, hi = i < A.N ? min(A.start[i + 1], A.T) : 0;
-            const int blocks = hi > lo ? (int)((hi - lo + A.rows - 1) / A.rows) : 0;
+            const int blocks = hi > lo ? (int)((hi - lo + A.rows - 1) >> shift) : 0;
             // (chunks of a first block behind its first one follow the blocks here, and are listed as -1, -2, ..)
-            const int all = blocks + (A.by_key && A.sinks && blocks ? rp_attend_chunks((int)(hi - lo), A.window) - 1 : 0);
+            const int all = blocks + (A.by_key && A.sinks && blocks > chunk ? (blocks + chunk - 1) / chunk - 1 : 0);
             const auto take = [&](int sample, int n, int b) {
                 int work = !A.causal ? n : A.by_key ? n - b : b + 1;
                 if (A.window) {
-                    const int chunk = rp_attend_chunk(A.window);
-                    if (!A.by_key) work = AttendSteps(b * A.rows, A.window, A.sinks).steps((b + 1) * (A.rows >> 7));
+                    if (!A.by_key) work = AttendSteps(b << shift, A.window, A.sinks).steps((b + 1) * (A.rows >> 7));
                     else if (b >= n) { work = min(chunk, n - (b - n + 1) * chunk); b = n - 1 - b; }
                     else work = b == 0 && A.sinks ? min(n, chunk) : min(n, ((b * 128 + 126 + A.window) >> 7) + 1) - b;
                 }

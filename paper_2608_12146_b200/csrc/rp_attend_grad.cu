@@ -51,17 +51,17 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
     rp_attend_clear(C, keys.start, keys.N, keys.T, b, n);
     if constexpr (Narrow<X>::value)
         for (int i = b * 1024 + threadIdx.x; i < keys.N; i += n * 1024) A.tops[i] = 0;
-    // 64 rows of a CTA: heads of a token, tokens; four steps on their way at a time (all lanes go round as often)
-    constexpr int AHEAD = 4;
+    // 64 rows of a CTA: heads of a token, tokens; two steps are worked on while the next two are on their way (all lanes go round as often)
+    constexpr int AHEAD = 2;
     const i64 T = keys.T;
     const int heads = min(A.H, 64), tokens = 64 / heads, row = threadIdx.x >> 4, dt = row / heads;
     for (int h0 = 0; h0 < A.H; h0 += heads) {
         const int h = h0 + row % heads;
         const bool mine = dt < tokens && h < A.H;
         const X *o = (const X *)A.o + h * A.o_head + lane * 8, *g = (const X *)A.g + h * A.g_head + lane * 8;
-        for (i64 t0 = (i64)b * tokens; t0 < T; t0 += (i64)AHEAD * n * tokens) {
-            Pack8<X> p[AHEAD], q[AHEAD];
-            float l[AHEAD];
+        Pack8<X> p[2][AHEAD], q[2][AHEAD];
+        float l[2][AHEAD];
+        const auto fetch = [&](i64 t0, Pack8<X> *p, Pack8<X> *q, float *l) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const i64 t = t0 + (i64)u * n * tokens + dt;
@@ -69,6 +69,8 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
                 if (mine && t < T && lane * 8 < A.d) { p[u] = rp_load8(o + t * A.o_token); q[u] = rp_load8(g + t * A.g_token); }
                 if (mine && t < T && lane == 0) l[u] = A.lse[t * A.l_token + h * A.l_head];
             }
+        };
+        const auto work = [&](i64 t0, const Pack8<X> *p, const Pack8<X> *q, const float *l) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const i64 t = t0 + (i64)u * n * tokens + dt;
@@ -88,6 +90,14 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
                     if (mine && t < T && lane == 0) A.norms[h * T + t] = norm;
                 }
             }
+        };
+        const i64 step = (i64)AHEAD * n * tokens, from = (i64)b * tokens;
+        fetch(from, p[0], q[0], l[0]);
+        for (i64 t0 = from; t0 < T; t0 += 2 * step) {
+            fetch(t0 + step, p[1], q[1], l[1]);
+            work(t0, p[0], q[0], l[0]);
+            fetch(t0 + 2 * step, p[0], q[0], l[0]);
+            work(t0 + step, p[1], q[1], l[1]);
         }
     }
 }
@@ -113,8 +123,8 @@ __global__ void __launch_bounds__(256) k_attend_tops(const i64 *start, int N, i6
 
 // With a window: delta of each sample's first tokens from its definition, sum_j p_j do v_j.  They see few keys, o is as large as v there, and what its rounding leaves in
 // do o is as much as the rounding of their scores' gradients (samples of 60 tokens: gradients of queries and keys 1.6 times as far off as with their own rounding alone,
-// 1.42 so; from the 33rd token on it is a sixth of that rounding and less).  A warp half of a sample's and a query head's.  Behind `first` such CTAs of eight warps those
-// for float16's largest rows.
+// 1.42 so; from the 33rd token on it is a sixth of that rounding and less).  A warp half of a sample's and a query head's.  Behind `first` such CTAs those for float16's
+// largest rows.
 #define FIRST_TOKENS 32
 struct FirstArgs {
     const i64 *start;
@@ -133,31 +143,33 @@ struct FirstArgs {
 template <typename X>
 __global__ void __launch_bounds__(256) k_attend_first(const FirstArgs A)
 {
+    if ((int)blockIdx.x < A.first && threadIdx.x >= 64) return;              // (two warps a CTA: there are few, and their loads go to many lines)
     if ((int)blockIdx.x >= A.first) { rp_attend_tops(A.start, A.N, A.T, A.H, A.norms, A.tops, blockIdx.x - A.first); return; }
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    for (i64 unit = (i64)blockIdx.x * 8 + (threadIdx.x >> 5); unit < (i64)A.N * A.H * 2; unit += (i64)A.first * 8) {
+    for (i64 unit = (i64)blockIdx.x * 2 + (threadIdx.x >> 5); unit < (i64)A.N * A.H * 2; unit += (i64)A.first * 2) {
         const int i = (int)(unit / (2 * A.H)), h = (int)(unit % (2 * A.H)) >> 1, r0 = 16 * (int)(unit & 1), hk = h / A.share;
         const i64 base = max(A.start[i], (i64)0);
         const int n = (int)min(min(A.start[i + 1], A.T) - base, (i64)FIRST_TOKENS);
         if (r0 >= n) continue;
         // (rows behind the sample's end are read as its last one: nothing comes of them)
         const int r[2] = { min(r0 + g, n - 1), min(r0 + g + 8, n - 1) };
-        const X *q = (const X *)A.q + base * A.q_token + h * A.q_head + 2 * t, *o = (const X *)A.g + base * A.g_token + h * A.g_head + 2 * t;
-        const X *k = (const X *)A.k + base * A.k_token + hk * A.k_head + 2 * t, *v = (const X *)A.v + base * A.v_token + hk * A.v_head + 2 * t;
+        // (a lane's eight elements are places 2t, 2t + 1, 2t + 8, 2t + 9 of one product and of the next: the order of a sum's terms is free)
+        const X *q = (const X *)A.q + base * A.q_token + h * A.q_head + 8 * t, *o = (const X *)A.g + base * A.g_token + h * A.g_head + 8 * t;
+        const X *k = (const X *)A.k + base * A.k_token + hk * A.k_head + 8 * t, *v = (const X *)A.v + base * A.v_token + hk * A.v_head + 8 * t;
         float s[4][4] = { }, dp[4][4] = { };
-#pragma unroll 4
-        for (int c = 0; c < A.d; c += 16) {
-            const bool more = c + 8 < A.d;               // (a head of 8, 24, .. elements ends in the middle of a step)
-            const auto at = [&](const X *x, i64 row) { return *(const u32 *)(x + row + c); };
-            const auto behind = [&](const X *x, i64 row) { return more ? *(const u32 *)(x + row + c + 8) : 0u; };
-            const u32 a[4] = { at(q, r[0] * A.q_token), at(q, r[1] * A.q_token), behind(q, r[0] * A.q_token), behind(q, r[1] * A.q_token) };
-            const u32 b[4] = { at(o, r[0] * A.g_token), at(o, r[1] * A.g_token), behind(o, r[0] * A.g_token), behind(o, r[1] * A.g_token) };
+#pragma unroll 2
+        for (int c = 0; c < A.d; c += 32) {
+            const bool there = c + 8 * t < A.d;
+            const auto at = [&](const X *x, i64 row) { return there ? *(const uint4 *)(x + row + c) : make_uint4(0, 0, 0, 0); };
+            const uint4 q0 = at(q, r[0] * A.q_token), q1 = at(q, r[1] * A.q_token), o0 = at(o, r[0] * A.g_token), o1 = at(o, r[1] * A.g_token);
+            const u32 a[2][4] = { { q0.x, q1.x, q0.y, q1.y }, { q0.z, q1.z, q0.w, q1.w } }, b[2][4] = { { o0.x, o1.x, o0.y, o1.y }, { o0.z, o1.z, o0.w, o1.w } };
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const int j = min(8 * x + g, n - 1);
-                const u32 e[2] = { at(k, j * A.k_token), behind(k, j * A.k_token) }, f[2] = { at(v, j * A.v_token), behind(v, j * A.v_token) };
-                rp_multiply(s[x], a, e, X());
-                rp_multiply(dp[x], b, f, X());
+                const uint4 kk = at(k, j * A.k_token), vv = at(v, j * A.v_token);
+                const u32 e[2][2] = { { kk.x, kk.y }, { kk.z, kk.w } }, f[2][2] = { { vv.x, vv.y }, { vv.z, vv.w } };
+#pragma unroll
+                for (int y = 0; y < 2; ++y) { rp_multiply(s[x], a[y], e[y], X()); rp_multiply(dp[x], b[y], f[y], X()); }
             }
         }
 #pragma unroll
@@ -252,7 +264,7 @@ __device__ __forceinline__ void store_part(u32 at, float *out, int d, bool there
 
 // Where a chunk of a first block's queries leaves the sums for the first tokens.  Chunks of a sample start `chunk` tokens apart and a sample with several is longer than
 // that, so no two of those that start in one stretch of as many tokens are both the first of their sample, and no two both are not.
-__host__ __device__ __forceinline__ i64 part_place(i64 base, int chunk, int tokens) { return 2 * ((base + (i64)chunk * tokens) / tokens) + (chunk > 0); }
+__device__ __forceinline__ i64 part_place(i64 base, int chunk, int tokens) { return 2 * ((int)base / tokens + chunk) + (chunk > 0); }           // (rows: less than 2^30)
 
 // ---------------------------------------------------------------------------------------
 // keys: dk and dv
@@ -871,10 +883,11 @@ __global__ void __launch_bounds__(256) k_attend_sinks(const i64 *start, int N, i
         const i64 len = min(start[i + 1], T) - base;
         if (len <= tokens) continue;
         const int chunks = rp_attend_chunks((int)len, window);
+        const float *const from = parts + ((part_place(base, 0, tokens) * Hk + hk) * 2 + b) * sinks * d;
         for (int x = threadIdx.x; x < sinks * d; x += 256) {
             float sum = 0.0f;
 #pragma unroll 4
-            for (int c = 0; c < chunks; ++c) sum += parts[((part_place(base, c, tokens) * Hk + hk) * 2 + b) * sinks * d + x];
+            for (int c = 0; c < chunks; ++c) sum += from[(i64)(2 * c + (c > 0)) * Hk * 2 * sinks * d + x];
             const int r = x / d, e = x % d;
             if (b) dk[(base + r) * k_token + hk * k_head + e] = rp_round<X>(sum);
             else dv[(base + r) * v_token + hk * v_head + e] = rp_round<X>(sum);
@@ -969,7 +982,7 @@ static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_t
     RP_TRY(rp_op_launched());
     const unsigned blocks = (unsigned)((T + 255) / 256);
     if (window) {
-        const int first = (int)std::min(((i64)n_samples * Hq * 2 + 7) / 8, (i64)sms * 4);
+        const int first = (int)std::min((i64)n_samples * Hq, (i64)sms * 8);
         const FirstArgs F = { (const i64 *)start, T, n_samples, Hq, Hq / Hk, d, window, sinks, a->scale, q->x, k->x, v->x, out_grad->x, q->token, q->head, k->token, k->head,
                               v->token, v->head, out_grad->token, out_grad->head, (const float *)lse->x, lse->token, lse->head, stats, norms, tops, first };
         if (half) k_attend_first<__half><<<first + blocks, 256, 0, stream>>>(F);
