@@ -3,14 +3,14 @@
 //   s = scale q k^T over the tokens of a sample, p = exp(s - m), o = p v / sum p, lse = m + log sum p, m a running maximum
 //
 // A tile of 128 queries and 128 keys is 2 * 128 * 128 * head_dim multiply-adds (1024 cycles of an SM's tensor cores at head_dim 128) and 128 * 128 exponentials (1024
-// cycles of its special function units).  What bounds it are the hand-overs between the warps of a tile: at 4097 tokens the tensor cores are busy for 35 % of the
-// time, the special function units for 41 %.
+// cycles of its special function units).  What bounds it are the hand-overs between the warps of a tile: at 4097 tokens the tensor cores are busy for 34 % of the
+// time, the special function units for 43 %.
 // A CTA takes 256 queries of a head as two tiles of 128, each with four warps of its own for the softmax (a thread has a row, so a row's maximum and sum
 // need no exchange); while one tile's weights are worked out, the tensor cores work on the other's.  One warp copies keys and values into a ring of
 // shared memory, one issues the products.  Scores and outputs live in tensor memory (2 x 128 + 2 x head_dim columns), the weights take the
 // scores' place as the operand of the second product.  Outputs are scaled again only when a row's maximum has grown by more than 2^8.
 // CTAs stay resident and take blocks of queries in the order of falling work.
-// 12289 tokens in two samples, 16 heads on 4, 128 wide, causal: 320 us, 1100 TFLOP/s (368 under the power cap of a long run); 32768 tokens in five 1302 us, 1190 TFLOP/s.  A product of 128 x 128 x 16 takes
+// 12289 tokens in two samples, 16 heads on 4, 128 wide, causal: 327 us, 1080 TFLOP/s (359 under the power cap of a long run); 32768 tokens in five 1304 us, 1190 TFLOP/s.  A product of 128 x 128 x 16 takes
 // 64 cycles, to which each wait and commit of the warp that issues adds 50 to 150.  Tried: two warps that issue, one a tile (449 us for 381 then); a part of the
 // exponentials by a polynomial beside the special function unit (323 to 360 for 322).
 #include <algorithm>

@@ -8,7 +8,10 @@
 // Two kernels: one takes 128 keys and goes through the queries that see them (dk, dv), one takes 128 queries and goes through the keys that they see
 // (dq).  Each output is summed by one CTA in a fixed order: no additions from several CTAs to one place, whose order would change the last bits.  The price is
 // that scores and do v^T are worked out twice, 14 multiply-adds a pair and element in place of 10.  Bound by the hand-overs between the warp that issues products and
-// those of the softmax: at 4096 tokens the tensor cores are busy for 21 % (keys, which also wait for the largest block) and 41 % (queries) of the time.
+// those of the softmax: at 4096 tokens the tensor cores are busy for 22 % (keys, which also wait for the largest block) and 56 % (queries) of the time.
+// With a window (WINDOW) blocks of keys are seen by a few tiles of queries, blocks of queries see a few tiles of keys, and the sample's first block is seen by all of its
+// queries when there are first tokens: it is cut into chunks, whose sums for the first tokens meet in a kernel of their own.  A row of 32768 tokens of one sample, 16 heads on
+// 4, 128 wide: 371 us with a window of 128, 929 with 1024 (1037 with 4 first tokens).
 #include <algorithm>
 
 #include "rp_attend.cuh"
@@ -905,8 +908,8 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
     k_attend_keys<X, D, WINDOW><<<(int)std::min((i64)sms, most_keys * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
     RP_TRY(rp_op_launched());
-    // (8192 tokens in three samples, 16 heads on 4, 128 wide: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 249 us, the
-    // queries' 166; 398 us for the whole call.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
+    // (8192 tokens in three samples, 16 heads on 4, 128 wide: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 268 us, the
+    // queries' 144; 350 us for the whole call, in which they overlap.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
     // sample of 2048 tokens, 5 heads on 1: 193 -> 69 us - but a sample's gradients then depend on what else is in its row.)
     cudaLaunchConfig_t how = {};
     how.gridDim = dim3((unsigned)std::min((i64)sms, most * keys.Hq));

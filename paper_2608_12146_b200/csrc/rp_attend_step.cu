@@ -3,11 +3,14 @@
 //   s = scale q k^T over the keys that the token sees, o = softmax(s) v, lse = log sum exp(s)
 //
 // Bound by HBM: each visible key and value is read once, 4 * head_dim bytes for 4 * share * head_dim operations (share: query heads to a key head).  The products go
-// through the warps' matrix instruction, 16 query heads by 16 keys at a time, of which `share` rows are something: with a few rows to a tile there is nothing that
-// fuller instructions could add.
+// through the warps' matrix instruction, 16 rows by 8 keys at a time, of which `share` are something: with a few rows to a tile there is nothing that fuller
+// instructions could add.
 // The keys that a sequence's token sees are cut into chunks of 128, or of a 128th of them where that is more; a chunk and a key head are a unit of one warp, which takes
-// them 16 keys at a time through a ring of its own in shared memory.  Warps stay resident and take units in turn, and the ring runs on into the next unit; no warp waits
+// them in tiles of 4 KB (16 keys of 128) through a ring of its own in shared memory.  Warps stay resident and take units in turn, and the ring runs on into the next unit; no warp waits
 // for another.  The cut goes by the sequence alone, so that its bits do not depend on the others of the batch.  A second kernel adds up the chunks, in their order.
+// 64 ragged sequences, 16 heads on 4, 128 wide (643 MB): 115 us, 86 % of the measured copy rate; 250 with a window of 1000, 8 heads of 64 (445 MB) 82 us, 83 %; four of up to
+// 6000 keys (52 MB) 18 us, where the tiles of a chunk, one after the other, take as long as the launches.  Chunks of 64 keys: 115, 102 and 21 us; of 256 119, 88 and 22.  A
+// chunk to a CTA, whose warps meet at its end: 284, 193.  Keys and values that stay in L2 like everything else: 125, 85 and 18.
 #include <algorithm>
 
 #include "rp_attend.cuh"
@@ -18,7 +21,7 @@
 #define STEP_CHUNKS 128                  // chunks of a sequence at most
 #define STEP_ROWS 16                     // query heads of a unit at most
 
-#define STEP_TABLE 1024                  // sequences whose places a CTA works out for itself
+#define STEP_TABLE 1024                  // sequences whose places a CTA works out for itself: a launch less (250 sequences 82 us for 86, four 17.8 for 18.6; 64 115 for 112)
 
 struct StepHead { int status, pad[3]; };
 struct StepPlan {
