@@ -394,7 +394,8 @@ int rp_rotate_axes_grad(const rp_rotary *r, int64_t n_tokens, const double *inv_
  *   lse [n_tokens][q_heads] float, any strides; nullable in rp_attend.
  *   workspace: rp_attend_workspace(a, n_tokens, n_samples) bytes, 16-byte aligned.  Its first int32 is 0 when the kernels are done, or RP_ERR_TIMEOUT if one of their
  *     waits ran out (two seconds in which a CTA copied nothing more): outputs that had not been worked out are NaN then.
- * Limits: head_dim <= 128 and a multiple of 8, q_heads a multiple of kv_heads, type RP_F16 or RP_BF16, scale > 0, n_tokens < 2^31 - 512, n_samples <= 2^24. */
+ * Limits: head_dim <= 128 and a multiple of 8, q_heads a multiple of kv_heads, type RP_F16 or RP_BF16, scale > 0, n_tokens < 2^31 - 512, n_samples <= 2^24,
+ * (n_tokens / 64 + n_samples) * q_heads < 2^31. */
 typedef struct {
     int32_t q_heads, kv_heads, head_dim;
     int32_t type;               /* rp_type of all tensors but lse                            */
@@ -436,7 +437,8 @@ int rp_attend_window_grad(const rp_attend_config *a, int32_t window, int32_t sin
  * first `sinks` ones.
  *   o[i][h], lse[i][h] as in rp_attend; weights keep 16 bits or more in their product with v.  A sequence without filled rows gets zeros, and -inf for lse.  What rows
  *   hold that are not seen, infinities and NaN too, does not matter.  A sequence's results do not depend on the others of the call.
- *   a->causal is not used; types, strides and limits as in rp_attend (n_tokens: rows of the cache); any sinks >= 0.  lse nullable.
+ *   a->causal is not used; types, strides and limits as in rp_attend (n_tokens: rows of the cache), and (n_tokens / 64 + 2 n_samples) * q_heads < 2^31; any sinks >= 0.
+ *   lse nullable.
  *   workspace: rp_attend_step_workspace(a, window, sinks, n_tokens, n_samples) bytes, 16-byte aligned; contents need not be set.  Its first int32 is 0 when the kernels
  *     are done, or RP_ERR_TIMEOUT, as in rp_attend. */
 int64_t rp_attend_step_workspace(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, int32_t n_samples);

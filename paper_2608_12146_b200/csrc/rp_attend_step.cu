@@ -224,7 +224,7 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             if (u < each && i0 + u < A.plan.N) {
                 sm.from[i0 + u] = at;
                 sm.place[i0 + u] = place[u];
-                if (blockIdx.x == 0) A.where[i0 + u] = make_int2(at, at + n[u] <= A.plan.most ? n[u] : 0);
+                if (blockIdx.x == 0) A.where[i0 + u] = make_int2(at, at <= A.plan.most - n[u] ? n[u] : 0);
                 at += n[u];
             }
         if (threadIdx.x == STEP_THREADS - 1) sm.from[A.plan.N] = x;
@@ -233,7 +233,7 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     } else if (A.where)
         for (int i = blockIdx.x * STEP_THREADS + threadIdx.x; i < A.plan.N; i += gridDim.x * STEP_THREADS) {
             const int at = table.from[i], n = table.from[i + 1] - at;
-            A.where[i] = make_int2(at, at + n <= A.plan.most ? n : 0);
+            A.where[i] = make_int2(at, at <= A.plan.most - n ? n : 0);
         }
     const int total = min(table.from[A.plan.N], A.plan.most) * A.units, mine = blockIdx.x * STEP_WARPS + warp, step = gridDim.x * STEP_WARPS;
     const float sl = A.scale * RP_LOG2E;
@@ -535,7 +535,8 @@ static StepSpace step_space(const rp_attend_config *a, i64 T, int N, int window,
 static int check_step(const rp_attend_config *a, int window, int sinks, i64 T, int N)
 {
     RP_TRY(rp_attend_check(a, T, N));
-    return window < 0 || sinks < 0 ? RP_ERR_ARG : RP_OK;
+    if (window < 0 || sinks < 0) return RP_ERR_ARG;
+    return (T / 64 + 2ll * N) * a->q_heads >= (1ll << 31) ? RP_ERR_RANGE : RP_OK;             // (units are counted in 32 bits, and step_most() of them are less than T / 128 + 1.25 N)
 }
 
 extern "C" int64_t rp_attend_step_workspace(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, int32_t n_samples)

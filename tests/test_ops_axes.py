@@ -230,6 +230,29 @@ def test_in_place_streamed_and_captured_calls_agree_bit_for_bit():
 
 
 @pytest.mark.gpu
+def test_rows_that_lie_beyond_32_bits():
+    """Elements 2^31 and more from a tensor's first one."""
+    import torch
+    T, h, d, step = 1200, 3, 64, 1 << 21
+    g = torch.Generator().manual_seed(8)
+    x, dy = (torch.randn(T, h, d, generator=g).bfloat16().cuda() for _ in range(2))
+    w = torch.rand(d, generator=g).bfloat16().cuda()
+    inv, axis = 1000.0 ** -torch.arange(0, 1, 2 / d, dtype=torch.float64).cuda(), torch.arange(d // 2, dtype=torch.int32).cuda() % 2
+    position = torch.randint(0, 5000, (2, T), generator=g).cuda()
+
+    def apart(x=None):
+        y = torch.empty(T, step, dtype=torch.bfloat16, device="cuda")[:, :h * d].view(T, h, d)
+        return y if x is None else y.copy_(x)
+    want, _ = rp.rp_rotate_axes(x, None, inv, axis, position, q_weight=w)
+    dx, _, dw, _ = rp.rp_rotate_axes_grad(dy, None, x, None, inv, axis, position, q_weight=w)
+    far = apart(x)
+    got, _ = rp.rp_rotate_axes(far, None, inv, axis, position, q_weight=w, q_out=apart())
+    assert (got == want).all()
+    got, _, dw2, _ = rp.rp_rotate_axes_grad(apart(dy), None, far, None, inv, axis, position, q_weight=w, q_grad=apart())
+    assert (got == dx).all() and (dw2 == dw).all()
+
+
+@pytest.mark.gpu
 def test_no_tokens_and_arguments_in_python():
     import torch
     q, w = torch.zeros(0, 4, 64, device="cuda"), torch.ones(64, device="cuda")

@@ -57,9 +57,10 @@ def test_refusals():
                 dict(length=p + 4), dict(out=None), dict(out=ok), dict(nbytes=16), dict(space=None), dict(space=p + 8), dict(cfg=a(kind=0)), dict(cfg=a(scale=0.0))):
         assert call(**bad) == -1, bad
     assert call(cfg=a(d=136)) == -5 and call(cfg=a(d=60)) == -2 and call(cfg=a(hq=3, hk=2)) == -2
+    assert call(cfg=a(hq=64, hk=64), N=1 << 24) == -5 and lib.rp_attend_step_workspace(a(hq=64, hk=64), 0, 0, 2, 1 << 24) == 0          # more units than 32 bits count
     size = lib.rp_attend_step_workspace
     assert size(None, 0, 0, 1, 1) == 0 and size(a(), -1, 0, 1, 1) == 0 and size(a(), 0, -1, 1, 1) == 0
-    # a chunk of a sequence leaves two sums and the values of each query head; with a window there are fewer, and never more than 64 of a sequence
+    # a chunk of a sequence leaves two sums and the values of each query head; with a window there are fewer, and never more than 128 of a sequence
     assert size(a(), 0, 0, 5000, 1) >= 20 * 2 * (64 + 2) * 4 and size(a(), 300, 0, 5000, 1) < size(a(), 0, 0, 5000, 1)
     assert size(a(), 0, 0, 1 << 24, 1) == size(a(), 0, 0, 1 << 25, 1)
 
@@ -188,6 +189,29 @@ def test_a_sequence_gets_alone_what_it_gets_among_others():
     x = torch.randn(5000, 3, 64, generator=torch.Generator().manual_seed(4)).half().cuda()
     out, lse = rp.rp_attend_step(x[:, :1], x[:, 1:2], x[:, 2:], many)
     assert (out == x[:, 2:]).all()                       # one key each: its values
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("apart", [False, True])
+def test_caches_whose_rows_lie_beyond_32_bits(apart):
+    """Elements 2^31 and more from the cache's first one: a long cache, and a short one with its rows far apart."""
+    import torch
+    T, hk, d, step = (1600, 2, 64, 1 << 21) if apart else (1100000, 8, 128, 2048)
+    n, lengths = (800, [700, 800]) if apart else (6000, [5000, 5990])
+    buf = torch.empty(T, step, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(9)
+    seen = torch.randn(2, n, 2 * hk * d, generator=g).bfloat16().cuda()
+    start = [T - 2 * n, T - n, T]
+    for i in range(2):
+        buf[start[i]:start[i + 1], :2 * hk * d] = seen[i]
+    k, v = buf[:, :hk * d].view(T, hk, d), buf[:, hk * d:2 * hk * d].view(T, hk, d)
+    q = torch.randn(2, 4 * hk, d, generator=g).bfloat16().cuda()
+    length = torch.tensor(lengths, device="cuda")
+    small = seen.view(2 * n, 2, hk, d)
+    for kw in (dict(), dict(window=500, sinks=30)):
+        out, lse = rp.rp_attend_step(q, k, v, torch.tensor(start, device="cuda"), length=length, **kw)
+        o, l = rp.rp_attend_step(q, small[:, 0], small[:, 1], torch.tensor([0, n, 2 * n], device="cuda"), length=length, **kw)
+        assert (out == o).all() and (lse == l).all()
 
 
 @pytest.mark.gpu

@@ -197,6 +197,27 @@ def test_samples_of_a_row_get_what_they_get_alone(window, sinks):
 
 
 @pytest.mark.gpu
+def test_rows_that_lie_beyond_32_bits():
+    """Elements 2^31 and more from a tensor's first one, inputs and outputs of both directions."""
+    import torch
+    T, hq, hk, d, step = 1300, 4, 2, 64, 1 << 21
+    g = torch.Generator().manual_seed(6)
+    start, kw = torch.tensor([0, 900, T], device="cuda"), dict(window=300, sinks=5)
+
+    def apart(heads, x=None):
+        y = torch.empty(T, step, dtype=torch.bfloat16, device="cuda")[:, :heads * d].view(T, heads, d)
+        return y if x is None else y.copy_(x)
+    q, k, v, do = (torch.randn(T, h, d, generator=g).bfloat16().cuda() for h in (hq, hk, hk, hq))
+    out, lse = rp.rp_attend_window(q, k, v, start, **kw)
+    grads = rp.rp_attend_window_grad(do, q, k, v, out, lse, start, **kw)
+    q, k, v, do = apart(hq, q), apart(hk, k), apart(hk, v), apart(hq, do)
+    o, l = rp.rp_attend_window(q, k, v, start, out=apart(hq), **kw)
+    assert (o == out).all() and (l == lse).all()
+    for a, b in zip(rp.rp_attend_window_grad(do, q, k, v, o, l, start, q_grad=apart(hq), k_grad=apart(hk), v_grad=apart(hk), **kw), grads):
+        assert (a == b).all()
+
+
+@pytest.mark.gpu
 def test_other_samples_and_keys_out_of_sight_do_not_matter():
     """Infinities and NaN in the tokens of other samples, in the row's padding, and in keys that no query near them sees."""
     import torch
