@@ -5,23 +5,27 @@
 // Bound by HBM: each visible key and value is read once, 4 * head_dim bytes for 4 * share * head_dim operations (share: query heads to a key head).  The products go
 // through the warps' matrix instruction, 16 rows by 8 keys at a time, of which `share` are something: with a few rows to a tile there is nothing that fuller
 // instructions could add.
-// The keys that a sequence's token sees are cut into chunks of 128, or of a 128th of them where that is more; a chunk and a key head are a unit of one warp, which takes
-// them in tiles of 4 KB (16 keys of 128) through a ring of its own in shared memory.  Warps stay resident and take units in turn, and the ring runs on into the next unit; no warp waits
-// for another.  The cut goes by the sequence alone, so that its bits do not depend on the others of the batch.  A second kernel adds up the chunks, in their order.
-// 64 ragged sequences, 16 heads on 4, 128 wide (643 MB): 115 us, 86 % of the measured copy rate; 250 with a window of 1000, 8 heads of 64 (445 MB) 82 us, 83 %; four of up to
-// 6000 keys (52 MB) 18 us, where the tiles of a chunk, one after the other, take as long as the launches.  Chunks of 64 keys: 115, 102 and 21 us; of 256 119, 88 and 22.  A
-// chunk to a CTA, whose warps meet at its end: 284, 193.  Keys and values that stay in L2 like everything else: 125, 85 and 18.
+// The keys that a sequence's token sees are cut into as many chunks as there are 128s in them, 128 at most; a chunk and a key head are a unit of one warp, which takes them in
+// tiles of 4 KB (16 keys of 128) through a ring of its own in shared memory.  Of n chunks each has every n-th tile, so that warps side by side read what lies side by side
+// (a bare reading kernel with as many warps: 6.2 TB/s where a CTA's rows are 16 at a time, 5.3 where they are 128 in a row).  Warps stay resident and take units in
+// turn, and the ring runs on into the next unit; no warp waits for another.  The cut goes by the sequence alone, so that its bits do not depend on the others of the
+// batch.  A second kernel adds up the chunks, in their order.
+// 64 ragged sequences, 16 heads on 4, 128 wide (643 MB): 110 us, 89 % of the measured copy rate; 250 with a window of 1000, 8 heads of 64 (445 MB) 84 us, 81 %; 1000 of 1000 keys
+// (2 GB) 346 us, 90 %; four of up to 6000 keys (52 MB) 17.7 us, where the tiles of a chunk, one after the other, take as long as the launches.  Cut by 96: 118, 88, 353 and 17.6
+// us; by 256 109, 86, 330 and 22.3.  Chunks in whole pieces, cut by 64: 115, 102 and 21 us; by 128 115, 82 and 18, 392 for the thousand; a chunk to a CTA, whose warps meet at its
+// end: 284, 193.  Keys and values that stay in L2 like everything else: 125 for 115, 85 for 82.
 #include <algorithm>
+#include <climits>
 
 #include "rp_attend.cuh"
 
 #define STEP_WARPS 4
 #define STEP_THREADS (32 * STEP_WARPS)
-#define STEP_CHUNK 128                   // keys of a chunk at least
+#define STEP_CHUNK 128                   // keys of a chunk at least, where there are several
 #define STEP_CHUNKS 128                  // chunks of a sequence at most
 #define STEP_ROWS 16                     // query heads of a unit at most
 
-#define STEP_TABLE 1024                  // sequences whose places a CTA works out for itself: a launch less (250 sequences 82 us for 86, four 17.8 for 18.6; 64 115 for 112)
+#define STEP_TABLE 32                    // sequences whose places a warp works out for itself: a launch less (four sequences 17.5 us for 18.9; by more than a lane each it is slower, 64 of them 115 for 112)
 
 struct StepHead { int status, pad[3]; };
 struct StepPlan {
@@ -38,18 +42,17 @@ __device__ __forceinline__ int2 step_place(const StepPlan &P, int i)
     return make_int2((int)min(from, P.T), (int)(P.length ? min(max(P.length[i], (i64)0), room) : room));          // (rows: less than 2^31)
 }
 struct StepSeen {
-    int ahead, first, seen, size, n;         // n: chunks, of `size` places each
+    int ahead, first, seen, n;               // n: chunks, of which each has every n-th tile
     __device__ __forceinline__ StepSeen(const StepPlan &P, int filled)
     {
         first = P.window ? max(filled - P.window, 0) : 0;
         ahead = min(P.sinks, first);
         seen = ((ahead + P.tile - 1) & -P.tile) + filled - first;
-        size = max(STEP_CHUNK, ((seen + STEP_CHUNKS - 1) / STEP_CHUNKS + 31) & ~31);
-        n = max((seen + size - 1) / size, 1);           // (one without keys as well: it writes the outputs)
+        n = min(max(seen / STEP_CHUNK, 1), STEP_CHUNKS);         // (one without keys as well: it writes the outputs)
     }
 };
 
-// More sequences than a CTA has a table for, or none long enough for the second kernel: counts the chunks before each.
+// More sequences than a warp has lanes for, or none long enough for the second kernel: counts the chunks before each.
 __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P, StepHead *head)
 {
     rp_let_next_launch_start();
@@ -82,7 +85,7 @@ __global__ void __launch_bounds__(1024) k_step_plan(StepPlan P, StepHead *head)
 
 struct StepArgs {
     StepPlan plan;
-    bool table, keys;                        // table: a CTA works out the places for itself; keys: is there a cache at all?
+    bool table, keys;                        // table: a warp works out the places for itself; keys: is there a cache at all?
     int2 *where;                             // [N] first item and number of items, for the second kernel
     int Hq, share, groups, d, units;         // groups: of 16 query heads to a key head; units: of a chunk
     float scale;
@@ -96,7 +99,7 @@ struct StepArgs {
     float *parts;                            // [item][Hq][d] its values
     StepHead *head;
     int *states;                             // of the CTAs: whether a wait ran out
-    int ctas;
+    int ctas, each;                          // each: query heads that a CTA of the second kernel takes at a time
     u64 wait_ns;
 };
 
@@ -123,27 +126,33 @@ template <typename X> __device__ __forceinline__ void two_pairs(float a, float b
     low = rp_pair(a - x, b - y, X());
 }
 
-// Places x0 to x1 of the keys that a token sees.
-struct StepItem { int base, sample, chunks, x0, x1, ahead, first; };
+// Places x0, x0 + stride, .. before x1 of the keys that a token sees, a tile at each.
+struct StepItem { int base, sample, chunks, x0, x1, ahead, first, stride; };
 struct StepTable {
     const int *from;
     const int2 *place;
+    int step, coarse;                        // a 32nd of the sequences to a lane: chunks before its first one
+    int2 own;                                // with one sequence to a lane, its place
     // Chunk c of the call: the last sequence that has none behind it.  By a warp, which looks at 32 sequences at a time.
     __device__ __forceinline__ StepItem item(const StepPlan &P, int c) const
     {
-        const int lane = threadIdx.x & 31;
-        int lo = 0, n = P.N;
-        while (n > 1) {
-            const int step = (n + 31) >> 5;
-            const u32 hit = __ballot_sync(0xffffffffu, lane * step < n && from[lo + lane * step] <= c);
-            const int skip = max(__popc(hit) - 1, 0) * step;       // (0: starts that make no sequences)
-            lo += skip;
-            n = min(step, n - skip);
+        const int lane = threadIdx.x & 31, head = max(__popc(__ballot_sync(0xffffffffu, coarse <= c)) - 1, 0);
+        int lo = head * step, n = min(step, P.N - lo), before = __shfl_sync(0xffffffffu, coarse, head);
+        int2 at = make_int2(__shfl_sync(0xffffffffu, own.x, head), __shfl_sync(0xffffffffu, own.y, head));
+        if (step > 1) {
+            while (n > 1) {
+                const int some = (n + 31) >> 5;
+                const u32 hit = __ballot_sync(0xffffffffu, lane * some < n && from[lo + lane * some] <= c);
+                const int skip = max(__popc(hit) - 1, 0) * some;
+                lo += skip;
+                n = min(some, n - skip);
+            }
+            before = from[lo];
+            at = place[lo];
         }
-        const int2 at = place[lo];
         const StepSeen S(P, at.y);
         StepItem it;
-        it.base = at.x; it.sample = lo; it.chunks = S.n; it.x0 = (c - from[lo]) * S.size; it.x1 = (int)min((i64)it.x0 + S.size, (i64)S.seen);
+        it.base = at.x; it.sample = lo; it.chunks = S.n; it.x0 = (c - before) * P.tile; it.x1 = S.seen; it.stride = S.n * P.tile;
         it.ahead = S.ahead; it.first = S.first;
         return it;
     }
@@ -167,9 +176,6 @@ template <int D> struct StepSmem {
     alignas(1024) unsigned char ring[STEP_WARPS][STAGES][2][TILE];
     u64 full[STEP_WARPS][STAGES];
     Waits waits;
-    int sums[STEP_WARPS];
-    int from[STEP_TABLE + 1];
-    int2 place[STEP_TABLE];
 };
 
 // FEW: eight query heads at most, whose places the instruction's other eight rows give the weights' lower halves.
@@ -194,48 +200,37 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     __syncthreads();
     rp_let_next_launch_start();
     rp_wait_for_launch_before();
-    StepTable table = { A.plan.from, A.plan.place };
+    const int N = A.plan.N;
+    StepTable table = { A.plan.from, A.plan.place, (N + 31) >> 5, INT_MAX, make_int2(0, 0) };
+    int chunks;
     if (A.table) {
-        // a thread up to eight neighbouring sequences
-        constexpr int EACH = STEP_TABLE / STEP_THREADS;
-        const int each = (A.plan.N + STEP_THREADS - 1) / STEP_THREADS, i0 = threadIdx.x * each;
-        int2 place[EACH];
-        int n[EACH], own = 0;
-#pragma unroll
-        for (int u = 0; u < EACH; ++u)
-            if (u < each && i0 + u < A.plan.N) place[u] = step_place(A.plan, i0 + u);
-#pragma unroll
-        for (int u = 0; u < EACH; ++u) {
-            n[u] = u < each && i0 + u < A.plan.N ? StepSeen(A.plan, place[u].y).n : 0;
-            own += n[u];
+        int n = 0;
+        if (lane < N) {
+            table.own = step_place(A.plan, lane);
+            n = StepSeen(A.plan, table.own.y).n;
         }
-        int x = own;
+        int x = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
-        if (lane == 31) sm.sums[warp] = x;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) x += sm.sums[w];
-        int at = x - own;
-#pragma unroll
-        for (int u = 0; u < EACH; ++u)
-            if (u < each && i0 + u < A.plan.N) {
-                sm.from[i0 + u] = at;
-                sm.place[i0 + u] = place[u];
-                if (blockIdx.x == 0) A.where[i0 + u] = make_int2(at, at <= A.plan.most - n[u] ? n[u] : 0);
-                at += n[u];
-            }
-        if (threadIdx.x == STEP_THREADS - 1) sm.from[A.plan.N] = x;
-        __syncthreads();
-        table = { sm.from, sm.place };
-    } else if (A.where)
-        for (int i = blockIdx.x * STEP_THREADS + threadIdx.x; i < A.plan.N; i += gridDim.x * STEP_THREADS) {
-            const int at = table.from[i], n = table.from[i + 1] - at;
-            A.where[i] = make_int2(at, at <= A.plan.most - n ? n : 0);
+        chunks = __shfl_sync(0xffffffffu, x, 31);
+        if (lane < N) {
+            table.coarse = x - n;
+            if (blockIdx.x == 0 && warp == 0) A.where[lane] = make_int2(x - n, x <= A.plan.most ? n : 0);
         }
-    const int total = min(table.from[A.plan.N], A.plan.most) * A.units, mine = blockIdx.x * STEP_WARPS + warp, step = gridDim.x * STEP_WARPS;
+    } else {
+        chunks = table.from[N];
+        if (lane * table.step < N) table.coarse = table.from[lane * table.step];
+        if (table.step == 1 && lane < N) table.own = table.place[lane];
+        if (A.where)
+            for (int i = blockIdx.x * STEP_THREADS + threadIdx.x; i < N; i += gridDim.x * STEP_THREADS) {
+                const int at = table.from[i], n = table.from[i + 1] - at;
+                A.where[i] = make_int2(at, at <= A.plan.most - n ? n : 0);
+            }
+    }
+    const int total = min(chunks, A.plan.most) * A.units, mine = blockIdx.x * STEP_WARPS + warp, step = gridDim.x * STEP_WARPS;
     const float sl = A.scale * RP_LOG2E;
     const u64 policy = passing();
 
@@ -252,6 +247,9 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         }
     };
     open();
+    StepItem it = { }, next = { };
+    const auto item = [&](int unit) { return unit == unit_in ? to : table.item(A.plan, unit / A.units); };          // (mostly the one that is being copied)
+    if (mine < total) it = item(mine);
     auto copy = [&](int stage) {                         // the next tile, if there is one
         if (unit_in >= total || waits->gave_up) return;
         if (lane == 0) {
@@ -264,7 +262,8 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             }
         }
         ++copied;
-        if ((at += KEYS) >= to.x1) { unit_in += step; open(); }
+        if (to.x1 - at <= to.stride) { unit_in += step; open(); }
+        else at += to.stride;
     };
     for (int s = 0; s < STAGES; ++s) copy(s);
 
@@ -281,12 +280,10 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                 q[s][i] = r < rows && c < A.d ? *(const u32 *)(from + r * A.q_head + c) : 0u;
             }
     };
-    StepItem it = {}, next = {};
-    if (mine < total) it = table.item(A.plan, mine / A.units);
     load_q(mine, it.sample);
     auto look = [&](int unit) {                          // the next unit, and its queries
         if (unit >= total) return;
-        next = table.item(A.plan, unit / A.units);
+        next = item(unit);
         load_q(unit, next.sample);
     };
     u32 taken = 0;
@@ -300,9 +297,10 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
         bool ok = true;
-        for (int x = it.x0; x < it.x1; x += KEYS) {
+        for (int x = it.x0, last = it.x0 >= it.x1; !last; x += it.stride) {
             if (!(ok = bar_wait_warp(full + 8 * stage, taken / STAGES & 1, waits))) break;
             ++taken;
+            last = it.x1 - x <= it.stride;
             const u32 kt = ring + stage * 2 * Smem::TILE, vt = kt + Smem::TILE;
             const int there = min(x < whole ? it.ahead - x : it.x1 - x, KEYS);           // keys of the tile; behind them may be anything
             float s[NK][4] = { };
@@ -318,7 +316,7 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     rp_multiply(s[n + 1], a, b + 2, X());
                 }
             }
-            if (x + KEYS >= it.x1) look(unit + step);        // while this one is finished
+            if (last) look(unit + step);        // while this one is finished
             float top[R];
 #pragma unroll
             for (int i = 0; i < R; ++i) {
@@ -433,48 +431,33 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     }
 }
 
-// Sequences of several chunks: a CTA a query head, each warp every fourth chunk, a lane four columns.
-template <typename X>
-__global__ void __launch_bounds__(STEP_THREADS) k_step_join(const StepArgs A)
-{
-    constexpr float LIFT = std::is_same<X, bf16>::value ? 1.0f : 32768.0f;
-    constexpr int MINE = STEP_CHUNKS / STEP_WARPS;       // 32: a lane a chunk of the warp's
-    static_assert(MINE == 32, "a lane for each chunk of a warp");
-    __shared__ float4 part[STEP_WARPS][32];
-    __shared__ float tops[STEP_WARPS], sums[STEP_WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane * 4;
-    rp_wait_for_launch_before();
-    if (blockIdx.x == 0) {
-        int late = 0;
-        for (int i = threadIdx.x; i < A.ctas; i += STEP_THREADS) late |= A.states[i];
-        late = __syncthreads_or(late);
-        if (threadIdx.x == 0) A.head->status = late ? RP_ERR_TIMEOUT : RP_OK;
-    }
-    for (i64 unit = blockIdx.x; unit < (i64)A.plan.N * A.Hq; unit += gridDim.x) {
-        const int sample = (int)(unit / A.Hq), h = (int)(unit % A.Hq);
-        const int2 at = A.where[sample];
-        if (at.y <= 1) continue;
-        const int mine = (at.y - warp + STEP_WARPS - 1) / STEP_WARPS;          // chunks warp, warp + 4, ..
-        const float2 y = lane < mine ? A.tops[(i64)(at.x + warp + STEP_WARPS * lane) * A.Hq + h] : make_float2(-INFINITY, 0.0f);
-        const float *from = A.parts + ((i64)(at.x + warp) * A.Hq + h) * A.d + (e < A.d ? e : 0);
-        const i64 step = (i64)STEP_WARPS * A.Hq * A.d;
+// Sequences of several chunks: up to STEP_FEW of them are added up by a warp, more by a CTA, each warp every fourth one; a lane has four columns.  Which of the two goes by the
+// sequence alone.  (1000 sequences of three chunks, 16 heads: 10 us behind the first kernel, 34 with a CTA for each query head.)
+#define STEP_FEW 16
+// Chunks first, first + every, .. of a sequence and query head (`mine` of them, 32 at most): their sums, with their largest maximum as it was or a larger one.
+struct StepSum {
+    float top, sum;
+    float4 o;
+    template <typename Top>
+    __device__ __forceinline__ StepSum(const StepArgs &A, i64 first, int every, int mine, int h, int lane, const Top &top_of)
+    {
+        const int e = lane * 4;
+        const float2 y = lane < mine ? A.tops[(first + every * lane) * A.Hq + h] : make_float2(-INFINITY, 0.0f);
+        const float *from = A.parts + (first * A.Hq + h) * A.d + (e < A.d ? e : 0);
+        const i64 step = (i64)every * A.Hq * A.d;
         constexpr int AHEAD = 8;
         float4 z[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) z[u] = u < mine ? *(const float4 *)(from + u * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        float top = y.x;
+        top = y.x;
 #pragma unroll
         for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        if (lane == 0) tops[warp] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < STEP_WARPS; ++w) top = fmaxf(top, tops[w]);
+        top = top_of(top);
         const float f = y.x == top ? 1.0f : rp_exp2(y.x - top);
-        float sum = y.y * f;
-        if (lane >= mine) sum = 0.0f;
+        sum = lane < mine ? y.y * f : 0.0f;
 #pragma unroll
         for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         for (int c0 = 0; c0 < mine; c0 += AHEAD) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
@@ -485,23 +468,65 @@ __global__ void __launch_bounds__(STEP_THREADS) k_step_join(const StepArgs A)
             for (int u = 0; u < AHEAD; ++u)
                 if (c0 + AHEAD + u < mine) z[u] = *(const float4 *)(from + (c0 + AHEAD + u) * step);
         }
-        part[warp][lane] = o;
-        if (lane == 0) sums[warp] = sum;
-        __syncthreads();
-        if (warp == 0) {
-            sum = 0.0f;
-            o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int w = 0; w < STEP_WARPS; ++w) {
-                const float4 a = part[w][lane];
-                o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
-                sum += sums[w];
-            }
-            const float g = 1.0f / (sum * LIFT);
-            if (e < A.d) *(uint2 *)((X *)A.out + sample * A.o_token + h * A.o_head + e) = make_uint2(rp_pair(o.x * g, o.y * g, X()), rp_pair(o.z * g, o.w * g, X()));
-            if (lane == 0 && A.lse) A.lse[sample * A.l_token + h * A.l_head] = (top + log2f(sum)) * 0.6931471805599453f;
+    }
+};
+template <typename X>
+__global__ void __launch_bounds__(STEP_THREADS) k_step_join(const StepArgs A)
+{
+    constexpr float LIFT = std::is_same<X, bf16>::value ? 1.0f : 32768.0f;
+    static_assert(STEP_CHUNKS <= 32 * STEP_WARPS && STEP_FEW <= 32, "a lane for each chunk of a warp");
+    __shared__ float4 part[STEP_WARPS][32];
+    __shared__ float tops[STEP_WARPS], sums[STEP_WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane * 4;
+    rp_wait_for_launch_before();
+    if (blockIdx.x == 0) {
+        int late = 0;
+        for (int i = threadIdx.x; i < A.ctas; i += STEP_THREADS) late |= A.states[i];
+        late = __syncthreads_or(late);
+        if (threadIdx.x == 0) A.head->status = late ? RP_ERR_TIMEOUT : RP_OK;
+    }
+    const auto hand_out = [&](int sample, int h, float top, float sum, const float4 &o) {
+        const float g = 1.0f / (sum * LIFT);
+        if (e < A.d) *(uint2 *)((X *)A.out + sample * A.o_token + h * A.o_head + e) = make_uint2(rp_pair(o.x * g, o.y * g, X()), rp_pair(o.z * g, o.w * g, X()));
+        if (lane == 0 && A.lse) A.lse[sample * A.l_token + h * A.l_head] = (top + log2f(sum)) * 0.6931471805599453f;
+    };
+    // `each` query heads (of one sequence or of neighbouring ones) at a time
+    const i64 units = (i64)A.plan.N * A.Hq;
+    for (i64 u0 = (i64)blockIdx.x * A.each; u0 < units; u0 += (i64)gridDim.x * A.each) {
+        const i64 unit = u0 + warp;
+        const int sample = (int)(unit / A.Hq), h = (int)(unit % A.Hq);
+        const int2 at = warp < A.each && unit < units ? A.where[sample] : make_int2(0, 0);
+        if (at.y > 1 && at.y <= STEP_FEW) {
+            const StepSum s(A, at.x, 1, at.y, h, lane, [](float top) { return top; });
+            hand_out(sample, h, s.top, s.sum, s.o);
         }
-        __syncthreads();
+        if (!__syncthreads_or(at.y > STEP_FEW)) continue;
+        for (int v = 0; v < A.each && u0 + v < units; ++v) {
+            const int sample = (int)((u0 + v) / A.Hq), h = (int)((u0 + v) % A.Hq);
+            const int2 at = A.where[sample];
+            if (at.y <= STEP_FEW) continue;
+            const StepSum s(A, at.x + warp, STEP_WARPS, (at.y - warp + STEP_WARPS - 1) / STEP_WARPS, h, lane, [&](float top) {
+                if (lane == 0) tops[warp] = top;
+                __syncthreads();
+                for (int w = 0; w < STEP_WARPS; ++w) top = fmaxf(top, tops[w]);
+                return top;
+            });
+            part[warp][lane] = s.o;
+            if (lane == 0) sums[warp] = s.sum;
+            __syncthreads();
+            if (warp == 0) {
+                float sum = 0.0f;
+                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int w = 0; w < STEP_WARPS; ++w) {
+                    const float4 a = part[w][lane];
+                    o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
+                    sum += sums[w];
+                }
+                hand_out(sample, h, s.top, sum, o);
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -513,10 +538,10 @@ static int step_units(const rp_attend_config *a) { return a->kv_heads * ((a->q_h
 static i64 step_most(i64 T, int N, int window, int sinks)
 {
     i64 each = STEP_CHUNKS;
-    if (window) each = std::min(each, ((i64)window + sinks + 31) / STEP_CHUNK + 1);
+    if (window) each = std::min(each, std::max(((i64)window + sinks + 31) / STEP_CHUNK, (i64)1));
     return std::min((T + 31ll * N) / STEP_CHUNK + N, N * each);
 }
-static bool step_several(i64 T, int window, int sinks) { return T + 31 > STEP_CHUNK && (!window || (i64)window + sinks + 31 > STEP_CHUNK); }
+static bool step_several(i64 T, int window, int sinks) { return T + 31 >= 2 * STEP_CHUNK && (!window || (i64)window + sinks + 31 >= 2 * STEP_CHUNK); }
 #define STEP_MOST_CTAS 512                               // (two on each of 148 SMs)
 static StepSpace step_space(const rp_attend_config *a, i64 T, int N, int window, int sinks)
 {
@@ -562,7 +587,10 @@ static int launch(const CUtensorMap &k, const CUtensorMap &v, StepArgs &A, i64 u
     RP_CUDA(cudaLaunchKernelEx(&how, k_attend_step<X, D, FEW>, k, v, (const StepArgs)A));
     RP_TRY(rp_op_launched());
     if (!A.where) return RP_OK;
-    how.gridDim = dim3((unsigned)std::min((i64)sms * 16, (i64)A.plan.N * A.Hq));
+    // (As many CTAs as there are query heads, while all of them are resident; of more a warp takes one.)
+    const i64 joins = (i64)A.plan.N * A.Hq;
+    A.each = joins > (i64)sms * 16 ? STEP_WARPS : 1;
+    how.gridDim = dim3((unsigned)std::min((i64)sms * 16, (joins + A.each - 1) / A.each));
     how.dynamicSmemBytes = 0;
     how.numAttrs = 1;
     RP_CUDA(cudaLaunchKernelEx(&how, k_step_join<X>, (const StepArgs)A));

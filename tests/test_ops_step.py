@@ -70,6 +70,7 @@ CASES = [
     (1, 1, 64, [1], 0, 0, 0), (4, 2, 128, [1, 2, 15, 16, 17], 3, 0, 0), (8, 1, 128, [255, 256, 257, 0, 64], 1, 0, 0), (16, 1, 64, [600, 3], 0, 100, 0),
     (20, 1, 96, [511, 512, 513, 1], 5, 200, 7), (40, 2, 128, [1000, 30], 2, 256, 300), (5, 5, 80, [700], 9, 1, 0), (3, 3, 8, [300, 299], 0, 1, 1), (33, 1, 64, [90, 270], 4, 64, 64),
     (6, 2, 128, [4097, 100, 0, 2000], 0, 4096, 0), (8, 8, 64, [17000, 12], 11, 0, 0), (2, 2, 120, [20001], 0, 20000, 128), (9, 1, 72, [16384, 16385], 1, 0, 0),
+    (4, 1, 128, [2175, 2176, 2177, 2303, 2304], 0, 0, 0), (3, 3, 64, [3000] + [0, 1, 260] * 13, 2, 2170, 9),
 ]
 
 
@@ -113,6 +114,21 @@ def test_the_last_token_of_each_sample_as_the_packed_row_has_it(window, sinks):
     out, lse = rp.rp_attend_step(q[last], k, v, start, window=window, sinks=sinks)
     # (there the weights are rounded once to 2^-8, and both outputs)
     assert (out.double() - want[last].double()).abs().max() <= 2.0 ** -8 * 5 and (lse - w_lse[last]).abs().max() <= 1e-4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hk", [(5, 1), (6, 3)])
+def test_many_sequences_of_a_few_chunks_and_of_many(hq, hk):
+    """More query heads in all than the joining kernel has CTAs, sequences on both sides of what a warp of it takes; some again alone, bit for bit."""
+    import torch
+    lengths = [[130, 300, 255, 0, 2400, 511, 1, 700, 2175, 2176][i * 7 % 10] for i in range(500)]
+    q, k, v, start = inputs((hq, hk, 64, lengths, 0, 0, 0), "bfloat16")
+    st = torch.tensor(start, device="cuda")
+    out, lse = rp.rp_attend_step(q, k, v, st)
+    check(q, k, v, start, None, 0, 0, 64 ** -0.5, out, lse)
+    for i in (0, 1, 2, 3, 5, 8, 250, 499):
+        o, l = rp.rp_attend_step(q[i:i + 1], k, v, st[i:i + 2].contiguous())
+        assert (o[0] == out[i]).all() and (l[0] == lse[i]).all()
 
 
 @pytest.mark.gpu
