@@ -48,6 +48,7 @@ template <typename X> struct Narrow { static constexpr bool value = !std::is_sam
 template <typename X>
 __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, AttendPlan queries, AttendClears C, StatsArgs A)
 {
+    rp_let_next_launch_start();
     if (blockIdx.x == 0) { rp_attend_plan(keys); return; }
     if (blockIdx.x == 1) { rp_attend_plan(queries); return; }
     const int b = blockIdx.x - 2, n = gridDim.x - 2, lane = threadIdx.x & 15;
@@ -146,14 +147,15 @@ struct FirstArgs {
 template <typename X>
 __global__ void __launch_bounds__(256) k_attend_first(const FirstArgs A)
 {
+    rp_let_next_launch_start();              // (nothing here is over before the launch in front is: the next one need only wait for this)
     if ((int)blockIdx.x < A.first && threadIdx.x >= 64) return;              // (two warps a CTA: there are few, and their loads go to many lines)
-    if ((int)blockIdx.x >= A.first) { rp_attend_tops(A.start, A.N, A.T, A.H, A.norms, A.tops, blockIdx.x - A.first); return; }
+    if ((int)blockIdx.x >= A.first) { rp_wait_for_launch_before(); rp_attend_tops(A.start, A.N, A.T, A.H, A.norms, A.tops, blockIdx.x - A.first); return; }
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     for (i64 unit = (i64)blockIdx.x * 2 + (threadIdx.x >> 5); unit < (i64)A.N * A.H * 2; unit += (i64)A.first * 2) {
         const int i = (int)(unit / (2 * A.H)), h = (int)(unit % (2 * A.H)) >> 1, r0 = 16 * (int)(unit & 1), hk = h / A.share;
         const i64 base = max(A.start[i], (i64)0);
         const int n = (int)min(min(A.start[i + 1], A.T) - base, (i64)FIRST_TOKENS);
-        if (r0 >= n) continue;
+        if (r0 >= n) { rp_wait_for_launch_before(); continue; }
         // (rows behind the sample's end are read as its last one: nothing comes of them)
         const int r[2] = { min(r0 + g, n - 1), min(r0 + g + 8, n - 1) };
         // (a lane's eight elements are places 2t, 2t + 1, 2t + 8, 2t + 9 of one product and of the next: the order of a sum's terms is free)
@@ -190,6 +192,7 @@ __global__ void __launch_bounds__(256) k_attend_first(const FirstArgs A)
                 }
             delta += __shfl_xor_sync(0xffffffffu, delta, 1);
             delta += __shfl_xor_sync(0xffffffffu, delta, 2);
+            rp_wait_for_launch_before();                     // (it writes a delta here, too)
             if (row < n && t == 0) A.stats[(i64)h * A.T + base + row].y = delta;
         }
     }
@@ -326,12 +329,13 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         sm.waits.start(A.wait_ns);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    rp_let_next_launch_start();              // the queries' kernel takes the SMs that run out of work here
     if (warp == ATTEND_COPY_WARP) tmem_alloc(rp_smem(&sm.tmem), 512);
     tmem_before();
     __syncthreads();
     tmem_after();
     const u32 tm = rp_uniform(sm.tmem);
+    rp_wait_for_launch_before();             // the list of blocks and the statistics: nothing of them before this line
+    rp_let_next_launch_start();              // the queries' kernel, which needs these too, takes the SMs that run out of work here
     const int total = rp_uniform(A.head->count * A.Hk);
     Waits *const waits = &sm.waits;
 
@@ -906,20 +910,22 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     const size_t sk = sizeof(KeySmem<D>) + 1024, sq = sizeof(QuerySmem<D>) + 1024;
     RP_CUDA(cudaFuncSetAttribute(k_attend_keys<X, D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sk));
     RP_CUDA(cudaFuncSetAttribute(k_attend_queries<X, D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sq));
-    k_attend_keys<X, D, WINDOW><<<(int)std::min((i64)sms, most_keys * keys.Hk), ATTEND_THREADS, sk, stream>>>(M.q, M.k, M.v, M.g, keys);
-    RP_TRY(rp_op_launched());
-    // (8192 tokens in three samples, 16 heads on 4, 128 wide: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 268 us, the
-    // queries' 144; 350 us for the whole call, in which they overlap.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
-    // sample of 2048 tokens, 5 heads on 1: 193 -> 69 us - but a sample's gradients then depend on what else is in its row.)
-    cudaLaunchConfig_t how = {};
-    how.gridDim = dim3((unsigned)std::min((i64)sms, most * keys.Hq));
+    cudaLaunchConfig_t how = {};                         // (both get their barriers, tensor memory and maps ready beside what runs before them)
+    how.gridDim = dim3((unsigned)std::min((i64)sms, most_keys * keys.Hk));
     how.blockDim = dim3(ATTEND_THREADS);
-    how.dynamicSmemBytes = sq;
+    how.dynamicSmemBytes = sk;
     how.stream = stream;
     cudaLaunchAttribute early = {};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     how.attrs = &early; how.numAttrs = 1;
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_keys<X, D, WINDOW>, M.q, M.k, M.v, M.g, (const GradArgs)keys));
+    RP_TRY(rp_op_launched());
+    // (8192 tokens in three samples, 16 heads on 4, 128 wide: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 268 us, the
+    // queries' 144; 350 us for the whole call, in which they overlap.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
+    // sample of 2048 tokens, 5 heads on 1: 193 -> 69 us - but a sample's gradients then depend on what else is in its row.)
+    how.gridDim = dim3((unsigned)std::min((i64)sms, most * keys.Hq));
+    how.dynamicSmemBytes = sq;
     RP_CUDA(cudaLaunchKernelEx(&how, k_attend_queries<X, D, WINDOW>, M.q, M.k, M.v, M.g, (const GradArgs)queries));
     return rp_op_launched();
 }
@@ -989,8 +995,16 @@ static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_t
         const int first = (int)std::min((i64)n_samples * Hq, (i64)sms * 8);
         const FirstArgs F = { (const i64 *)start, T, n_samples, Hq, Hq / Hk, d, window, sinks, a->scale, q->x, k->x, v->x, out_grad->x, q->token, q->head, k->token, k->head,
                               v->token, v->head, out_grad->token, out_grad->head, (const float *)lse->x, lse->token, lse->head, stats, norms, tops, first };
-        if (half) k_attend_first<__half><<<first + blocks, 256, 0, stream>>>(F);
-        else k_attend_first<bf16><<<first, 256, 0, stream>>>(F);
+        cudaLaunchConfig_t how = {};                     // (while the statistics are worked out)
+        how.gridDim = dim3(half ? first + blocks : first);
+        how.blockDim = dim3(256);
+        how.stream = stream;
+        cudaLaunchAttribute early = {};
+        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        early.val.programmaticStreamSerializationAllowed = 1;
+        how.attrs = &early; how.numAttrs = 1;
+        if (half) RP_CUDA(cudaLaunchKernelEx(&how, k_attend_first<__half>, F));
+        else RP_CUDA(cudaLaunchKernelEx(&how, k_attend_first<bf16>, F));
         RP_TRY(rp_op_launched());
     } else if (half) {
         k_attend_tops<<<blocks, 256, 0, stream>>>((const i64 *)start, n_samples, T, Hq, norms, tops);
