@@ -701,7 +701,7 @@ def _attend_args(torch, q, k, v, start, causal, scale):
     _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.dtype == q.dtype and v.dtype == q.dtype and k.shape[0] == q.shape[0]
           and k.shape[2] == q.shape[2], "q, k and v: [n_tokens, n_heads, head_dim] of one type, as many tokens and one head size wanted")
     at, n = _starts(torch, start)
-    return _attention(q.shape[1], k.shape[1], q.shape[2], _kind(q, "q"), causal, scale)[1], at, n
+    return (q.shape[1], k.shape[1], q.shape[2], _kind(q, "q"), causal, scale), at, n
 
 
 def _hand_out(status, space, T, torch):
@@ -716,8 +716,9 @@ def _like(torch, x):
 
 
 @functools.lru_cache(maxsize=256)
-def _step_workspace(q_heads, kv_heads, head_dim, kind, scale, *sizes):
-    return lib().rp_attend_step_workspace(_attention(q_heads, kv_heads, head_dim, kind, True, scale)[1], *sizes)
+def _attend_space(call: str, config, *sizes):
+    """Bytes of the workspace that a call with these heads and sizes wants."""
+    return getattr(lib(), call + "_workspace")(_attention(*config)[1], *sizes)
 
 
 def _int32(x, what: str) -> int:
@@ -730,15 +731,16 @@ def _int32(x, what: str) -> int:
 
 def _attend(window, q, k, v, start, causal, scale, out, lse, status, stream):
     torch = _torch()
-    ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
+    config, at, n = _attend_args(torch, q, k, v, start, causal, scale)
+    ref = _attention(*config)[1]
     T, H, _ = q.shape
     _dense(status, torch.int32, (1,), "status")
     with _Queue(torch, q, stream) as queue:
         if out is None:
-            out = q.new_empty(q.shape)
+            out = _like(torch, q)
         if lse is None:
             lse = q.new_empty((H, T), dtype=torch.float32).t()      # a head's rows side by side: what the backward pass reads fastest
-        nbytes = lib().rp_attend_workspace(ref, T, n)
+        nbytes = _attend_space("rp_attend", config, T, n)
         space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         if T:
             args = (T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _view(out, q, "out"), _lse_view(lse, T, H, torch), space.data_ptr(), nbytes,
@@ -753,14 +755,15 @@ def _attend(window, q, k, v, start, causal, scale, out, lse, status, stream):
 
 def _attend_grad(window, out_grad, q, k, v, out, lse, start, causal, scale, q_grad, k_grad, v_grad, status, stream):
     torch = _torch()
-    ref, at, n = _attend_args(torch, q, k, v, start, causal, scale)
+    config, at, n = _attend_args(torch, q, k, v, start, causal, scale)
+    ref = _attention(*config)[1]
     T, H, _ = q.shape
     _dense(status, torch.int32, (1,), "status")
     with _Queue(torch, q, stream) as queue:
-        q_grad = q.new_empty(q.shape) if q_grad is None else q_grad
-        k_grad = k.new_empty(k.shape) if k_grad is None else k_grad
-        v_grad = v.new_empty(v.shape) if v_grad is None else v_grad
-        nbytes = lib().rp_attend_grad_workspace(ref, T, n) if window is None else lib().rp_attend_window_grad_workspace(ref, *window, T, n)
+        q_grad = _like(torch, q) if q_grad is None else q_grad
+        k_grad = _like(torch, k) if k_grad is None else k_grad
+        v_grad = _like(torch, v) if v_grad is None else v_grad
+        nbytes = _attend_space("rp_attend_grad", config, T, n) if window is None else _attend_space("rp_attend_window_grad", config, *window, T, n)
         space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         if T:
             args = (T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), _view(out, q, "out"), _lse_view(lse, T, H, torch), _view(out_grad, q, "out_grad"), at, n,
@@ -816,8 +819,8 @@ def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int =
     at, n = _starts(torch, start)
     N, H, d = q.shape
     _need(N == n, "q: a token for each sequence wanted")
-    config = (H, k.shape[1], d, _kind(q, "q"))
-    ref = _attention(*config, True, scale)[1]
+    config = (H, k.shape[1], d, _kind(q, "q"), True, scale)
+    ref = _attention(*config)[1]
     window, sinks, T = _int32(window, "window"), _int32(sinks, "sinks"), k.shape[0]
     _dense(status, torch.int32, (1,), "status")
     with _Queue(torch, q, stream) as queue:
@@ -825,7 +828,7 @@ def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int =
             out = _like(torch, q)
         if lse is None:
             lse = q.new_empty((N, H), dtype=torch.float32)
-        nbytes = _step_workspace(*config, scale, window, sinks, T, n)
+        nbytes = _attend_space("rp_attend_step", config, window, sinks, T, n)
         space = q.new_empty(max(nbytes, 16), dtype=torch.uint8)
         _check(lib().rp_attend_step(ref, window, sinks, T, _view(q, q, "q"), _view(k, k, "k"), _view(v, v, "v"), at, n, _dense(length, torch.int64, (n,), "length"),
                                     _view(out, q, "out"), _lse_view(lse, N, H, torch), space.data_ptr(), nbytes, queue.handle), "rp_attend_step")
