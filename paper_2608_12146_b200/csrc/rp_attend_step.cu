@@ -10,10 +10,11 @@
 // (a bare reading kernel with as many warps: 6.2 TB/s where a CTA's rows are 16 at a time, 5.3 where they are 128 in a row).  Warps stay resident and take units in
 // turn, and the ring runs on into the next unit; no warp waits for another.  The cut goes by the sequence alone, so that its bits do not depend on the others of the
 // batch.  A second kernel adds up the chunks, in their order.
-// 64 ragged sequences, 16 heads on 4, 128 wide (643 MB): 110 us, 89 % of the measured copy rate; 250 with a window of 1000, 8 heads of 64 (445 MB) 84 us, 81 %; 1000 of 1000 keys
-// (2 GB) 346 us, 90 %; four of up to 6000 keys (52 MB) 17.7 us, where the tiles of a chunk, one after the other, take as long as the launches.  Cut by 96: 118, 88, 353 and 17.6
-// us; by 256 109, 86, 330 and 22.3.  Chunks in whole pieces, cut by 64: 115, 102 and 21 us; by 128 115, 82 and 18, 392 for the thousand; a chunk to a CTA, whose warps meet at its
-// end: 284, 193.  Keys and values that stay in L2 like everything else: 125 for 115, 85 for 82.
+// 64 ragged sequences, 16 heads on 4, 128 wide (643 MB): 108 us, 91 % of the measured copy rate; 250 with a window of 1000, 8 heads of 64 (445 MB) 83 us, 81 %; 1000 of 1000 keys
+// (2 GB) 327 us, 96 %; four of up to 6000 keys (52 MB) 16.8 us, where the tiles of a chunk, one after the other, take as long as the launches.  Cut by 192: 110, 81, 318 and 18.6
+// us.  With three tiles under way, cut by 96: 118, 88, 353 and 17.6; by 128 111, 84, 346 and 17.7; by 256 109, 86, 330 and 22.3.  Chunks in whole pieces, cut by 64: 115, 102
+// and 21 us; by 128 115, 82 and 18, 392 for the thousand; a chunk to a CTA, whose warps meet at its end: 284, 193.  Keys and values that stay in L2 like everything else:
+// 125 for 115, 85 for 82.
 #include <algorithm>
 #include <climits>
 
@@ -170,9 +171,10 @@ __device__ __forceinline__ void tma_load3_passing(u32 dst, const CUtensorMap *ma
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy) : "memory");
 }
 
-// A tile is 4 KB of keys and as many of values.
+// A tile is 4 KB of keys and as many of values.  Two of them for a warp, 64 KB a CTA and two CTAs to an SM; more under way make the reads slower (three: 64 sequences 111 us for
+// 108, 1000 of 1000 keys 346 for 327).
 template <int D> struct StepSmem {
-    static constexpr int KEYS = 2048 / D, TILE = 4096, STAGES = 3;       // 96 KB of keys and values: two CTAs to an SM
+    static constexpr int KEYS = 2048 / D, TILE = 4096, STAGES = 2;
     alignas(1024) unsigned char ring[STEP_WARPS][STAGES][2][TILE];
     u64 full[STEP_WARPS][STAGES];
     Waits waits;
