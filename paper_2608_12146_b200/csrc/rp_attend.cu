@@ -10,7 +10,7 @@
 // shared memory, one issues the products.  Scores and outputs live in tensor memory (2 x 128 + 2 x head_dim columns), the weights take the
 // scores' place as the operand of the second product.  Outputs are scaled again only when a row's maximum has grown by more than 2^8.
 // CTAs stay resident and take blocks of queries in the order of falling work.
-// 12289 tokens in two samples, 16 heads on 4, 128 wide, causal: 327 us, 1080 TFLOP/s (359 under the power cap of a long run); 32768 tokens in five 1304 us, 1190 TFLOP/s.  A product of 128 x 128 x 16 takes
+// 12289 tokens in two samples, 16 heads on 4, 128 wide, causal: 322 us, 1100 TFLOP/s (357 under the power cap of a long run); 32768 tokens in five 1284 us, 1206 TFLOP/s.  A product of 128 x 128 x 16 takes
 // 64 cycles, to which each wait and commit of the warp that issues adds 50 to 150.  Tried: two warps that issue, one a tile (449 us for 381 then); a part of the
 // exponentials by a polynomial beside the special function unit (323 to 360 for 322).
 #include <algorithm>

@@ -922,7 +922,7 @@ static int launch(const GradMaps &M, GradArgs &keys, GradArgs &queries, i64 most
     RP_CUDA(cudaLaunchKernelEx(&how, k_attend_keys<X, D, WINDOW>, M.q, M.k, M.v, M.g, (const GradArgs)keys));
     RP_TRY(rp_op_launched());
     // (8192 tokens in three samples, 16 heads on 4, 128 wide: the keys' kernel, whose largest block of keys takes as long as 1.4 times its share of all work, 268 us, the
-    // queries' 144; 350 us for the whole call, in which they overlap.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
+    // queries' 144; 346 us for the whole call, in which they overlap.  A block's query heads dealt out to several CTAs, whose sums meet behind them, make short lists of blocks faster - one
     // sample of 2048 tokens, 5 heads on 1: 193 -> 69 us - but a sample's gradients then depend on what else is in its row.)
     how.gridDim = dim3((unsigned)std::min((i64)sms, most * keys.Hq));
     how.dynamicSmemBytes = sq;
