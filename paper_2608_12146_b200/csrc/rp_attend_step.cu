@@ -253,7 +253,8 @@ k_attend_step(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     const auto item = [&](int unit) { return unit == unit_in ? to : table.item(A.plan, unit / A.units); };          // (mostly the one that is being copied)
     if (mine < total) it = item(mine);
     auto copy = [&](int stage) {                         // the next tile, if there is one
-        if (unit_in >= total || waits->gave_up) return;
+        // (the warp's answer, not each lane's: another warp may give up at any time, and all 32 lanes look for the next unit together)
+        if (unit_in >= total || __any_sync(0xffffffffu, waits->gave_up)) return;
         if (lane == 0) {
             const int whole = (to.ahead + KEYS - 1) & ~(KEYS - 1), row = to.base + (at < whole ? at : to.first + at - whole);
             const u32 dst = ring + stage * 2 * Smem::TILE, bar = full + 8 * stage;

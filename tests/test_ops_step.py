@@ -311,3 +311,29 @@ def test_short_limits_leave_right_rows_or_nan(limit):
         lost = torch.isnan(x)
         assert (x[~lost] == y[~lost]).all() and (status.item() == -8 or not lost.any())
     assert status.item() in (0, -8)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window", [0, 700])
+def test_short_limits_with_more_units_than_warps(window):
+    """Waits that run out while warps of the same CTA look for their next sequence: every call ends, rows are right or NaN, and NaN comes with the status."""
+    import torch
+    lengths = [[30, 900, 0, 3000, 257, 1][i % 6] for i in range(400)]
+    q, k, v, start = inputs((8, 4, 128, lengths, 3, 0, 0), "bfloat16")
+    st, length, kw = torch.tensor(start, device="cuda"), torch.tensor(lengths, device="cuda"), dict(window=window, sinks=4)
+    want = rp.rp_attend_step(q, k, v, st, length=length, **kw)
+    check(q, k, v, start, lengths, window, 4, 128 ** -0.5, *want)
+    for limit in (1, 300, 700, 1000, 1500, 2000, 3000, 5000, 10000):
+        status = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+        rp.rp_debug_set_wait_limit(limit)
+        try:
+            got = rp.rp_attend_step(q, k, v, st, length=length, status=status, **kw)
+            torch.cuda.synchronize()
+        finally:
+            rp.rp_debug_set_wait_limit()
+        assert status.item() in (0, -8)
+        for x, y in zip(got, want):
+            lost = torch.isnan(x)
+            assert (x[~lost] == y[~lost]).all() and (status.item() == -8 or not lost.any())
+    again = rp.rp_attend_step(q, k, v, st, length=length, **kw)
+    assert all((a == b).all() for a, b in zip(again, want))
