@@ -479,9 +479,10 @@ def rp_count_routes(routes, start, n_experts: int, demand=None, stream=None):
 SCORES = dict(softmax=0, sigmoid=1)
 
 
+# Structures are kept for numbers, never for objects: what a caller's tensor or array holds may be another number at the next call.
 @functools.lru_cache(maxsize=256)
 def _router(n_experts, top_k, kind, score, normalise, scale, loss_coef):
-    r = rp_router(n_experts, top_k, kind, SCORES[score], int(normalise), scale, loss_coef)
+    r = rp_router(n_experts, top_k, kind, SCORES[score], normalise, scale, loss_coef)
     return r, C.byref(r)
 
 
@@ -511,7 +512,7 @@ def rp_route(logits, top_k: int, start, *, score: str = "softmax", normalise: bo
     row = _rows(logits, "logits")
     T, E = logits.shape
     at, n = _starts(torch, start)
-    r, ref = _router(E, top_k, _kind(logits, "logits"), score, normalise, scale, loss_coef)
+    r, ref = _router(E, operator.index(top_k), _kind(logits, "logits"), score, int(normalise), float(scale), float(loss_coef))
     with _Queue(torch, logits, stream) as queue:
         if replay is not None:
             routes = replay
@@ -547,7 +548,7 @@ def rp_route_grad(logits, routes, start, counts, *, gates_grad=None, loss_grad=N
     k = routes.shape[1]
     size, step = _route_layout(routes)
     at, n = _starts(torch, start)
-    r, ref = _router(E, k, _kind(logits, "logits"), score, normalise, scale, loss_coef)
+    r, ref = _router(E, k, _kind(logits, "logits"), score, int(normalise), float(scale), float(loss_coef))
     with _Queue(torch, logits, stream) as queue:
         if logits_grad is None:
             logits_grad = logits.new_empty((T, E))
@@ -618,7 +619,7 @@ def _rotate(q, k, inv_freq, start, first_position, weights, eps, layout, mscale,
                                 None if w is None else dws[i].data_ptr())
             sides[i] = C.byref(side)
         freq = None if inv_freq is None else _dense(inv_freq, torch.float64, inv_freq.shape, "inv_freq")
-        r, ref = _rotary(d, 0 if inv_freq is None else 2 * inv_freq.numel(), layout, kind, _TYPES[w_type], eps, mscale)
+        r, ref = _rotary(d, 0 if inv_freq is None else 2 * inv_freq.numel(), layout, kind, _TYPES[w_type], float(eps), float(mscale))
         if axes is None:
             forward, backward, name = lib().rp_rotate, lib().rp_rotate_grad, "rp_rotate"
             args = (ref, T, freq, at, n, _dense(first_position, torch.int64, (n,), "first_position"), *sides)
@@ -682,8 +683,13 @@ def rp_rotate_axes_grad(q_out_grad, k_out_grad, q, k, inv_freq, axis, position, 
 
 @functools.lru_cache(maxsize=256)
 def _attention(q_heads, kv_heads, head_dim, kind, causal, scale):
-    a = rp_attend_config(q_heads, kv_heads, head_dim, kind, int(causal), head_dim ** -0.5 if scale is None else scale)
+    a = rp_attend_config(q_heads, kv_heads, head_dim, kind, causal, head_dim ** -0.5 if scale is None else scale)
     return a, C.byref(a)
+
+
+def _config(q, k, causal, scale):
+    """What a call's heads and numbers are kept by."""
+    return q.shape[1], k.shape[1], q.shape[2], _kind(q, "q"), int(causal), None if scale is None else float(scale)
 
 
 def _view(x, like, what: str):
@@ -701,7 +707,7 @@ def _attend_args(torch, q, k, v, start, causal, scale):
     _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.dtype == q.dtype and v.dtype == q.dtype and k.shape[0] == q.shape[0]
           and k.shape[2] == q.shape[2], "q, k and v: [n_tokens, n_heads, head_dim] of one type, as many tokens and one head size wanted")
     at, n = _starts(torch, start)
-    return (q.shape[1], k.shape[1], q.shape[2], _kind(q, "q"), causal, scale), at, n
+    return _config(q, k, causal, scale), at, n
 
 
 def _hand_out(status, space, T, torch):
@@ -817,9 +823,9 @@ def rp_attend_step(q, k, v, start, *, length=None, window: int = 0, sinks: int =
     _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.dtype == q.dtype and v.dtype == q.dtype and k.shape[2] == q.shape[2],
           "q [n_samples, q_heads, head_dim], k and v [n_tokens, kv_heads, head_dim] of one type and head size wanted")
     at, n = _starts(torch, start)
-    N, H, d = q.shape
+    N, H, _ = q.shape
     _need(N == n, "q: a token for each sequence wanted")
-    config = (H, k.shape[1], d, _kind(q, "q"), True, scale)
+    config = _config(q, k, True, scale)
     ref = _attention(*config)[1]
     window, sinks, T = _int32(window, "window"), _int32(sinks, "sinks"), k.shape[0]
     _dense(status, torch.int32, (1,), "status")
