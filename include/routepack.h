@@ -421,7 +421,8 @@ int rp_attend_grad(const rp_attend_config *a, int64_t n_tokens, const rp_view *q
  * these are; a->causal has to be 1, sinks <= 128, n_tokens < 2^30 - 512.  Infinities and NaN in the values of a token's own sample may reach it from tokens that it does
  * not see, as there.
  *   workspace: rp_attend_workspace(a, n_tokens, n_samples) bytes; the gradient's is rp_attend_window_grad_workspace(a, window, sinks, n_tokens, n_samples).
- *   The sum of out_grad * out of a sample's first 32 tokens is worked out anew from their weights; that of the others comes from `out` as it was rounded.
+ *   The sum of out_grad * out of tokens that see 32 keys at most is worked out anew from their weights: a sample's first 32 tokens, and with window + sinks <= 32 all.  That of
+ *   the others comes from `out` as it was rounded.
  *   The gradients of first tokens in samples longer than max(window + 127, 2048) tokens, give or take a tile, are summed over chunks of the queries, in their order, in 32 bits. */
 int rp_attend_window(const rp_attend_config *a, int32_t window, int32_t sinks, int64_t n_tokens, const rp_view *q, const rp_view *k, const rp_view *v,
                      const int64_t *start, int32_t n_samples, const rp_view *out, const rp_view *lse, void *workspace, int64_t workspace_bytes,

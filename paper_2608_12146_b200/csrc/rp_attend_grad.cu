@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(1024) k_attend_prepare(AttendPlan keys, Attend
     // 64 rows of a CTA: heads of a token, tokens; two steps are worked on while the next two are on their way (all lanes go round as often)
     constexpr int AHEAD = 2;
     const i64 T = keys.T;
-    const int heads = min(A.H, 64), tokens = 64 / heads, row = threadIdx.x >> 4, dt = row / heads;
+    const int heads = max(min(A.H, 64), 1), tokens = 64 / heads, row = threadIdx.x >> 4, dt = row / heads;
     for (int h0 = 0; h0 < A.H; h0 += heads) {
         const int h = h0 + row % heads;
         const bool mine = dt < tokens && h < A.H;
@@ -125,10 +125,11 @@ static __device__ __forceinline__ void rp_attend_tops(const i64 *start, int N, i
 }
 __global__ void __launch_bounds__(256) k_attend_tops(const i64 *start, int N, i64 T, int H, const float *norms, u32 *tops) { rp_attend_tops(start, N, T, H, norms, tops, blockIdx.x); }
 
-// With a window: delta of each sample's first tokens from its definition, sum_j p_j do v_j.  They see few keys, o is as large as v there, and what its rounding leaves in
-// do o is as much as the rounding of their scores' gradients (samples of 60 tokens: gradients of queries and keys 1.6 times as far off as with their own rounding alone,
-// 1.42 so; from the 33rd token on it is a sixth of that rounding and less).  A warp half of a sample's and a query head's.  Behind `first` such CTAs those for float16's
-// largest rows.
+// With a window: delta of the tokens that see few keys (32 at most) from its definition, sum_j p_j do v_j.  o is as large as v there, and what its rounding leaves in do o is
+// as much as the rounding of their scores' gradients (samples of 60 tokens: gradients of queries and keys 1.6 times as far off as with their own rounding alone, 1.42 so;
+// from the 33rd key on it is a sixth of that rounding and less).  Those are each sample's first tokens (k_attend_first), and where the window and the first tokens that stay
+// visible are as few, all of them (k_attend_few).
+// A sample's first tokens: a warp half of a sample's and a query head's.  Behind `first` such CTAs those for float16's largest rows.
 #define FIRST_TOKENS 32
 struct FirstArgs {
     const i64 *start;
@@ -196,6 +197,148 @@ __global__ void __launch_bounds__(256) k_attend_first(const FirstArgs A)
             if (row < n && t == 0) A.stats[(i64)h * A.T + base + row].y = delta;
         }
     }
+}
+// Every token, where none sees more than 32 keys; this takes the place of the statistics that come from o (which, in samples of 1000 tokens, leave gradients of queries and
+// keys 1.53 times as far off with a window of 16 as with their own rounding alone, 1.78 times with 4, 2.26 with 2; 1.41 to 1.42 so).  A CTA takes a block of 128 tokens of a
+// sample and some of a key head's query heads, a warp 16 of the tokens, whose q and do stay in registers.  Their keys are tiles of 8: those of the first tokens, then the window's,
+// from as many before the 16 up to themselves.  All of the block's lie in shared memory, neighbouring rows 64 bytes off each other's banks.  By blocks of the sample, so that its
+// bits do not depend on what else is in the row.
+// 16384 tokens of two samples, 16 heads on 4, 128 wide (q and do: 134 MB): 49 us with a window of 16, 70 with 28 and 4 first tokens; the whole gradient 230 and 305 us, where delta
+// from o takes 211 and 262.  It waits for q and do, which a warp asks for between two pieces of work.
+#define FEW_KEYS 32
+struct FewArgs {
+    FirstArgs of;
+    const AttendHead *head;                  // the blocks of queries
+    const int2 *items;
+    int parts;                               // a key head's query heads are dealt out to as many CTAs
+    int ahead, before, tiles;                // tiles of first tokens, of keys before a warp's tokens, in all: 7 at most
+};
+template <int D> struct FewRow { unsigned char at[2 * D + 64]; };
+__device__ __forceinline__ void copy_piece(void *to, const void *from, bool there)       // 16 bytes, or as many zeros, in the background
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(rp_smem(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void pieces_copied() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// A lane's part of what 16 rows see of some tiles: rows lane / 4 and 8 on, of each tile the keys 2 (lane % 4) and 1 on; sees(tile, key, row) as bits.
+template <typename Sees> __device__ __forceinline__ u32 few_mask(int tiles, const Sees &sees)
+{
+    const int lane = threadIdx.x & 31;
+    u32 mask = 0;
+    for (int i = 0; i < 4 * tiles; ++i) mask |= sees(i >> 2, 2 * (lane & 3) + (i & 1), (lane >> 2) + 8 * (i >> 1 & 1)) ? 1u << i : 0u;
+    return mask;
+}
+template <typename X, int D>
+__global__ void __launch_bounds__(256, 2) k_attend_few(const FewArgs F)
+{
+    extern __shared__ __align__(16) unsigned char raw[];
+    const FirstArgs &A = F.of;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, ahead = F.ahead, before = F.before, tiles = F.tiles, rows = 112 + 8 * tiles;
+    FewRow<D> *const keys = (FewRow<D> *)raw, *const values = keys + rows;
+    rp_let_next_launch_start();
+    rp_wait_for_launch_before();             // the list of blocks; float16's largest rows are 0
+    const int each = A.H / A.share * F.parts;            // units of a block
+    const i64 total = (i64)F.head->count * each;
+    // (behind all first tokens and the window's reach of them, what a place sees is the same everywhere)
+    const u32 mask_far = few_mask(tiles, [&](int x, int e, int row) {
+        const int back = row + 8 * before - 8 * (x - ahead) - e;
+        return x < ahead ? 8 * x + e < A.sinks : back >= 0 && back < A.window;
+    });
+    for (i64 unit = blockIdx.x; unit < total; unit += gridDim.x) {
+        const int item = (int)(unit / each), hk = (int)(unit % each) / F.parts, part = (int)(unit % each) % F.parts;
+        const AttendTile block(F.items, A.start, A.T, item, 128);
+        const X *const k = (const X *)A.k + block.base * A.k_token + hk * A.k_head, *const v = (const X *)A.v + block.base * A.v_token + hk * A.v_head;
+        const int near0 = block.row0 - 8 * before;       // the key behind the first tokens' rows
+        __syncthreads();                                 // (the block before has been read)
+        for (int x = threadIdx.x; x < rows * (D / 8); x += 256) {
+            const int y = x / (D / 8), c = x % (D / 8), j = min(max(y < 8 * ahead ? y : near0 + y - 8 * ahead, 0), block.len - 1);
+            const bool there = 8 * c < A.d;
+            copy_piece(keys[y].at + 16 * c, k + j * A.k_token + (there ? 8 * c : 0), there);
+            copy_piece(values[y].at + 16 * c, v + j * A.v_token + (there ? 8 * c : 0), there);
+        }
+        pieces_copied();
+        __syncthreads();
+        const int w0 = 16 * (threadIdx.x >> 5), r0 = block.row0 + w0, near = r0 - 8 * before;
+        if (r0 >= block.len) continue;
+        const u32 mask = near >= A.sinks ? mask_far : few_mask(tiles, [&](int x, int e, int row) {
+            const int j = x < ahead ? 8 * x + e : near + 8 * (x - ahead) + e, y = r0 + row;
+            return j >= 0 && j <= y && (x >= ahead || j < near) && (y - j < A.window || j < A.sinks);
+        });
+        // (rows behind the sample's end are read as its last one: nothing comes of them)
+        const int r[2] = { min(r0 + g, block.len - 1), min(r0 + g + 8, block.len - 1) };
+        float top = 0.0f;
+        for (int h = hk * A.share + part; h < (hk + 1) * A.share; h += F.parts) {
+            // (a lane's eight elements are places 2t, 2t + 1, 2t + 8, 2t + 9 of one product and of the next: the order of a sum's terms is free)
+            const X *const q = (const X *)A.q + block.base * A.q_token + h * A.q_head + 8 * t, *const o = (const X *)A.g + block.base * A.g_token + h * A.g_head + 8 * t;
+            u32 a[D / 16][4], b[D / 16][4];
+            float delta[2] = { 0.0f, 0.0f }, lse[2], norm[2] = { 0.0f, 0.0f };
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                lse[u] = A.lse[(block.base + r[u]) * A.l_token + h * A.l_head];
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint4 x = make_uint4(0, 0, 0, 0), y = x;
+                    if (32 * c + 8 * t < A.d) { x = *(const uint4 *)(q + r[u] * A.q_token + 32 * c); y = *(const uint4 *)(o + r[u] * A.g_token + 32 * c); }
+                    a[2 * c][u] = x.x; a[2 * c][2 + u] = x.y; a[2 * c + 1][u] = x.z; a[2 * c + 1][2 + u] = x.w;
+                    b[2 * c][u] = y.x; b[2 * c][2 + u] = y.y; b[2 * c + 1][u] = y.z; b[2 * c + 1][2 + u] = y.w;
+                }
+            }
+            if constexpr (Narrow<X>::value) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        Pack8<X> p;
+                        float w[8];
+                        p.w[0] = make_uint4(b[2 * c][u], b[2 * c][2 + u], b[2 * c + 1][u], b[2 * c + 1][2 + u]);
+                        rp_open8(p, w);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) norm[u] = fmaf(w[i], w[i], norm[u]);
+                    }
+            }
+            u32 bits = mask;
+#pragma unroll 1
+            for (int x = 0; x < tiles; ++x, bits >>= 4) {
+                const int y = (x < ahead ? 0 : w0) + 8 * x + g;
+                const unsigned char *const kr = keys[y].at + 16 * t, *const vr = values[y].at + 16 * t;
+                float s[4] = { }, dp[4] = { };
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    const uint4 kk = *(const uint4 *)(kr + 64 * c), vv = *(const uint4 *)(vr + 64 * c);
+                    const u32 e[2][2] = { { kk.x, kk.y }, { kk.z, kk.w } }, f[2][2] = { { vv.x, vv.y }, { vv.z, vv.w } };
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) { rp_multiply(s, a[2 * c + z], e[z], X()); rp_multiply(dp, b[2 * c + z], f[z], X()); }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) delta[i >> 1] += bits & 1u << i ? rp_exp2((s[i] * A.scale - lse[i >> 1]) * RP_LOG2E) * dp[i] : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const auto over_row = [](float x) {
+                    x += __shfl_xor_sync(0xffffffffu, x, 1);
+                    return x + __shfl_xor_sync(0xffffffffu, x, 2);
+                };
+                const int row = r0 + g + 8 * u;
+                const float sum = over_row(delta[u]);
+                if (row < block.len && t == 0) A.stats[(i64)h * A.T + block.base + row] = make_float2(lse[u] * RP_LOG2E, sum);
+                if constexpr (Narrow<X>::value) {
+                    const float n = over_row(norm[u]);
+                    if (row < block.len && n < INFINITY) top = fmaxf(top, n);          // (infinities and NaN, which no factor mends, do not count)
+                }
+            }
+        }
+        if constexpr (Narrow<X>::value) {
+            const u32 bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+            if (lane == 0 && bits) atomicMax(A.tops + F.items[item].x, bits);
+        }
+    }
+}
+template <typename X, int D>
+static int launch_few(const FewArgs &F, cudaLaunchConfig_t &how)
+{
+    how.dynamicSmemBytes = 2 * sizeof(FewRow<D>) * (112 + 8 * F.tiles);
+    RP_CUDA(cudaFuncSetAttribute(k_attend_few<X, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(2 * sizeof(FewRow<D>) * (112 + 8 * 7))));
+    RP_CUDA(cudaLaunchKernelEx(&how, k_attend_few<X, D>, F));
+    return RP_OK;
 }
 // Power of two for the gradients of a sample's scores, from its largest row.
 __device__ __forceinline__ float ds_scale(u32 top)
@@ -983,7 +1126,10 @@ static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_t
     float *const norms = (float *)(stats + T * Hq);
     u32 *const tops = (u32 *)(norms + T * Hq);           // (float16)
     G[0].tops = G[1].tops = tops;
-    const StatsArgs S = { out->x, out_grad->x, (const float *)lse->x, out->token, out->head, out_grad->token, out_grad->head, lse->token, lse->head, Hq, d, stats, norms, tops };
+    // (where all tokens see few keys, nothing comes from the outputs; the window is cut to the row and 256, so a short one is as it was)
+    const bool few = window && window + sinks <= FEW_KEYS;
+    const StatsArgs S = { out->x, out_grad->x, (const float *)lse->x, out->token, out->head, out_grad->token, out_grad->head, lse->token, lse->head, few ? 0 : Hq, d, stats, norms,
+                          tops };
     // (A CTA fills an SM's registers: one round of them.  Two rounds: 508 us for 503 with 16384 tokens, 51.6 for 43.6 with 3001.)
     const int ctas = 2 + (int)std::min((T * Hq + 63) / 64, std::max((i64)sms - 2, (i64)1));
     const bool half = a->type == RP_F16;
@@ -1003,7 +1149,15 @@ static int attend_grad(const rp_attend_config *a, int window, int sinks, i64 n_t
         early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         early.val.programmaticStreamSerializationAllowed = 1;
         how.attrs = &early; how.numAttrs = 1;
-        if (half) RP_CUDA(cudaLaunchKernelEx(&how, k_attend_first<__half>, F));
+        if (few) {
+            // a key head's query heads by one CTA, which reads the keys once, or by several where there are few blocks
+            const i64 units = (i64)P[1].most * Hk, most = (i64)sms * 2;
+            FewArgs E = { F, head[1], P[1].items, (int)std::min((i64)(Hq / Hk), (2 * most + units - 1) / units), (sinks + 7) / 8, (window + 6) / 8, 0 };
+            E.tiles = E.ahead + E.before + 2;
+            how.gridDim = dim3((unsigned)std::min(units * E.parts, most));
+            if (half) RP_TRY((d <= 64 ? launch_few<__half, 64>(E, how) : launch_few<__half, 128>(E, how)));
+            else RP_TRY((d <= 64 ? launch_few<bf16, 64>(E, how) : launch_few<bf16, 128>(E, how)));
+        } else if (half) RP_CUDA(cudaLaunchKernelEx(&how, k_attend_first<__half>, F));
         else RP_CUDA(cudaLaunchKernelEx(&how, k_attend_first<bf16>, F));
         RP_TRY(rp_op_launched());
     } else if (half) {

@@ -423,3 +423,113 @@ def test_rows_without_samples_and_many_short_ones():
     want, w_lse = rp.rp_attend(x[:, :2], x[:, 2:3], x[:, 3:], st)
     two = torch.arange(12000, device="cuda") % 3 < 2                     # (the third token of each sees two of three)
     assert (out[two] == want[two]).all() and (lse[two] == w_lse[two]).all() and not (out[~two] == want[~two]).all()
+
+
+FEW = [
+    # tokens, query heads, key heads, head size, starts, window, first tokens: no token sees more than 32 keys
+    (1, 1, 1, 64, [0, 1], 1, 0), (700, 2, 1, 64, [3, 20, 20, 21, 300, 690], 1, 0), (900, 4, 2, 128, [0, 17, 600, 900], 2, 0), (1000, 2, 2, 64, [-5, 1, 400, 1200], 4, 1),
+    (2500, 3, 1, 96, [0, 2300, 2500], 16, 16), (1300, 2, 1, 8, [0, 129, 1300], 1, 31), (600, 5, 1, 72, [0, 33, 97, 600], 8, 0), (3000, 2, 1, 128, [0, 500, 2999], 32, 0),
+    (640, 8, 2, 64, list(range(0, 641, 32)), 1000, 3), (500, 2, 1, 120, [0] + list(range(2, 500, 31)), 33, 128),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,extra", [("bfloat16", 0), ("float16", 8)])
+@pytest.mark.parametrize("shape", FEW, ids=[f"{s[0]}-{s[1]}-{s[2]}-{s[3]}-w{s[5]}-s{s[6]}" for s in FEW])
+def test_gradient_where_few_keys_are_seen(shape, kind, extra):
+    """As exact as one rounding of each weight, score's gradient and result: what the rounding of `out` would do to the sum of out_grad * out does not come in, nor does `out`."""
+    import torch
+    T, hq, hk, d, start, window, sinks = shape
+    q, k, v, g = inputs(shape, kind, extra)
+    st, scale, share = torch.tensor(start, device="cuda"), 0.2, hq // hk
+    do = torch.randn(hq, T, d + 8, generator=g).to(q.dtype).cuda()[:, :, :d].transpose(0, 1)
+    out, lse = rp.rp_attend_window(q, k, v, st, window=window, sinks=sinks, scale=scale)
+    got = rp.rp_attend_window_grad(do, q, k, v, out, lse, st, window=window, sinks=sinks, scale=scale)
+    half = torch.finfo(q.dtype).eps / 2
+    for lo, hi in samples(start, T):
+        mask = hidden(hi - lo, window, sinks)
+        want, size, slip = [[torch.zeros(hi - lo, n, d, dtype=torch.float64, device="cuda") for n in (hq, hk, hk)] for _ in range(3)]
+        for h in range(hq):
+            a = [x[lo:hi, h // n].double() for x, n in ((q, 1), (k, share), (v, share), (do, 1))]
+            for to, parts in zip((want, size, slip), gradients(*a, scale, mask)):
+                for i, n in enumerate((1, share, share)):
+                    to[i][:, h // n] += parts[i]
+        for x, w, s, e in zip(got, want, size, slip):
+            # each weight (or gradient of a score) and the result rounded once; 32 bits: 1e-5 of the weights and of the products with values, whose difference the
+            # gradient of a score is; float16 numbers of less than 2^-14 are off by 2^-25 at most, in up to T terms of |x| <= 6
+            tol = half * (s + w.abs() + half * s) + 2e-5 * (s + e) + (1e-7 + 2.0 ** -25 * 6 * (hi - lo) * share * (kind == "float16"))
+            assert ((x[lo:hi].double() - w).abs() <= tol).all()
+    nothing = torch.full_like(out, float("nan"))
+    for x, w in zip(rp.rp_attend_window_grad(do, q, k, v, nothing, lse, st, window=window, sinks=sinks, scale=scale), got):
+        assert (x == w).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+def test_first_tokens_do_not_go_by_the_rounded_output(kind):
+    """The first 32 of each sample, with a window in which the others see more: `out` there may be anything; the 33rd goes by it."""
+    import torch
+    shape = (1500, 4, 2, 128, [2, 30, 62, 95, 1490], 200, 5)
+    q, k, v, g = inputs(shape, kind)
+    st, kw = torch.tensor(shape[4], device="cuda"), dict(window=200, sinks=5)
+    do = torch.randn(1500, 4, 128, generator=g).to(q.dtype).cuda()
+    out, lse = rp.rp_attend_window(q, k, v, st, **kw)
+    want = rp.rp_attend_window_grad(do, q, k, v, out, lse, st, **kw)
+    other = out.clone()
+    for lo, hi in samples(shape[4], 1500):
+        other[lo:min(lo + 32, hi)] = float("nan")
+    assert all((x == w).all() for x, w in zip(rp.rp_attend_window_grad(do, q, k, v, other, lse, st, **kw), want))
+    other = out.clone()
+    other[62 + 32] += 1
+    assert (rp.rp_attend_window_grad(do, q, k, v, other, lse, st, **kw)[0] != want[0])[62 + 32].any()
+    # the keys' gradient as the definition has it, where the attention without a window takes the rounded output
+    lo, hi = 62, 95
+    for h in range(2):
+        dk = sum(gradients(*(x[lo:hi, y].double() for x, y in ((q, 2 * h + i), (k, h), (v, h), (do, 2 * h + i))), 128 ** -0.5, hidden(hi - lo, 200, 5))[0][1] for i in range(2))
+        plain = rp.rp_attend_grad(do, q, k, v, *rp.rp_attend(q, k, v, st), st)[1][lo:hi, h].double()
+        assert (want[1][lo:hi, h].double() - dk).norm() < (plain - dk).norm()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+@pytest.mark.parametrize("window,sinks", [(9, 5), (32, 0), (2, 30)])
+def test_few_keys_alone_in_a_row_far_apart_and_captured(window, sinks, kind):
+    """Where no token sees more than 32 keys: a sample's bits are the same alone and among samples of NaN and infinities, with rows 2^31 elements from the first, on another
+    stream and replayed."""
+    import torch
+    T, hq, hk, d, step = 1300, 6, 2, 64, 1 << 21
+    start = [4, 4, 5, 38, 200, 201, 1290]
+    q, k, v, g = inputs((T, hq, hk, d), kind)
+    do = torch.randn(T, hq, d, generator=g).to(q.dtype).cuda()
+    st, kw = torch.tensor(start, device="cuda"), dict(window=window, sinks=sinks)
+    out, lse = rp.rp_attend_window(q, k, v, st, **kw)
+    want = rp.rp_attend_window_grad(do, q, k, v, out, lse, st, **kw)
+    for lo, hi in samples(start, T):
+        one, cut = torch.tensor([0, hi - lo], device="cuda"), slice(lo, hi)
+        for a, b in zip(rp.rp_attend_window_grad(do[cut], q[cut], k[cut], v[cut], out[cut], lse[cut], one, **kw), want):
+            assert (a == b[cut]).all()
+        bad = [x.clone() for x in (do, q, k, v, out, lse)]
+        for x in bad:
+            x[:lo], x[hi:] = float("nan"), float("inf")
+        for a, b in zip(rp.rp_attend_window_grad(*bad, st, **kw), want):
+            assert (a[cut] == b[cut]).all() and (a[:4] == 0).all() and (a[1290:] == 0).all()
+
+    def apart(heads, x=None):
+        y = torch.empty(T, step, dtype=q.dtype, device="cuda")[:, :heads * d].view(T, heads, d)
+        return y if x is None else y.copy_(x)
+    far = [apart(x.shape[1], x) for x in (do, q, k, v)]
+    for a, b in zip(rp.rp_attend_window_grad(*far, out, lse, st, q_grad=apart(hq), k_grad=apart(hk), v_grad=apart(hk), **kw), want):
+        assert (a == b).all()
+    del far
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    results = [rp.rp_attend_window_grad(do, q, k, v, out, lse, st, stream=side, **kw) for _ in range(3)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        results.append(rp.rp_attend_window_grad(do, q, k, v, out, lse, st, **kw))
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for got in results:
+        assert all((a == b).all() for a, b in zip(got, want))
