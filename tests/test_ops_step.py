@@ -337,3 +337,32 @@ def test_short_limits_with_more_units_than_warps(window):
             assert (x[~lost] == y[~lost]).all() and (status.item() == -8 or not lost.any())
     again = rp.rp_attend_step(q, k, v, st, length=length, **kw)
     assert all((a == b).all() for a, b in zip(again, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+@pytest.mark.parametrize("d,keys", [(64, 32), (128, 16)])
+def test_sums_over_a_long_cache(d, keys, kind):
+    """140000 equal or small weights beside a large one, with the sums' roundings counted from the cut: 128 chunks, tiles of 4 KB (`keys` keys), of which a chunk has every 128th."""
+    import torch
+    T, dt = 140000, getattr(torch, kind)
+    tiles = -(-(-(-T // keys)) // 128)
+    q = torch.zeros(1, 1, d, device="cuda", dtype=dt)
+    q[..., 0] = 1
+    k = torch.zeros(T, 1, d, device="cuda", dtype=dt)
+    v = torch.rand(T, 1, d, generator=torch.Generator().manual_seed(5)).cuda().to(dt) + 1
+    st = torch.tensor([0, T], device="cuda")
+    for under in (0.0, 9.0, 12.0, 17.5):
+        k[:, 0, 0] = -under
+        k[77777, 0, 0] = 0.0
+        out, lse = rp.rp_attend_step(q, k, v, st, scale=1.0)
+        s = k[:, 0, 0].double()
+        p, w_lse = torch.softmax(s, 0), torch.logsumexp(s, 0).item()
+        want = p @ v[:, 0].double()
+        # a lane adds a pair of weights for each 8 keys of its tiles, then 3 times with its neighbours, 32 and 3 times over the chunks: half a step of 32 bits each.  A weight by
+        # its exponent's two roundings (as powers of two, of the small ones' part of the sum) and by the power's 2 steps; two of those, the chunk's and its factor
+        small = under * math.log2(math.e) * 2.0 ** -23 * (1 - math.exp(-w_lse)) + 2 * 2.0 ** -22
+        assert abs(lse.item() - w_lse) <= (tiles * keys // 8 * 2 + 38) * 2.0 ** -24 + small + 3 * 2.0 ** -23 * (1 + w_lse)
+        # values: a product of 16 keys is added with what lies under 2^-23 of the sum cut off, of the sum so far and of the product; a weight keeps 2^-17
+        near = tiles * keys // 16 * 2.0 ** -22 + 38 * 2.0 ** -24 + small + 2.0 ** -17 + (tiles * keys // 8 * 2 + 38) * 2.0 ** -24
+        assert ((out[0, 0].double() - want).abs() <= (torch.finfo(dt).eps / 2 * (1 + near) + near) * want).all()
