@@ -41,8 +41,10 @@ struct AttendSteps {
     __device__ __forceinline__ int steps(int tiles) const { return ahead + tiles - lo; }             // of queries that see keys up to tile `tiles`
     __device__ __forceinline__ int tile(int step) const { return step < ahead ? 0 : lo + step - ahead; }
 };
-// The same for two tiles of 128 queries that go through their keys together.  Where the window has left the sample's first token behind, they go from the last key
-// down, the first tokens at the end: so that no row begins with a tile of which it sees nothing, after which its sums would have to be taken up anew.
+// The same for two tiles of 128 queries that go through their keys together.  Where the window has left the sample's first token behind for the block's first query, they go
+// from the last key down, the first tokens at the end: no row begins there with a tile of which it sees nothing, after which its sums have to be taken up anew.  Otherwise they
+// go up.  (Without first tokens the second tile then has rows that begin with nothing, where row0 + 1 < window <= row0 + 128: windows up to 128 in a sample's first block,
+// of 300 in its second.)
 struct AttendOrder {
     bool down, one;                                     // one: there is no second tile
     int high, lo, steps, last[2], hole;                 // tile i takes part in the steps first(i) to last[i], the second one not in step `hole`

@@ -422,7 +422,7 @@ __device__ __forceinline__ i64 part_place(i64 base, int chunk, int tokens) { ret
 // each.  The products come in the order dv(j), s(j + 1), dk(j), do v^T(j + 1): while the weights of a tile are worked out, the tensor cores add up dk of the one
 // before and multiply do v^T of this one; while the gradients of its scores are, dv of this and scores of the next.  Weights and gradients lie as operands where the
 // scores and the products of their group were.  (Tiles of 64 queries, two of them at a time, one for each group: 435 us
-// for what takes 249; see the launch.)
+// for what took 249 then; 268 now, see the launch.)
 template <int D> struct KeySmem {
     static constexpr int TILE = 128 * D * 2, STAGES = 2;
     alignas(1024) unsigned char k[TILE];
@@ -702,7 +702,7 @@ k_attend_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 // ---------------------------------------------------------------------------------------
 // Tiles of 128 keys, 64 columns to each of the two groups of four warps.  q and do, which all tiles of a block share, lie in tensor memory as the operands of their
 // products: from shared memory a product of 128 x 128 x 16 reads all of the 128 bytes that a cycle of it has, with the copies coming in beside (220 us for what
-// takes 166).  They come through the ring that brings keys and values, ahead of these: each lane reads its row there and puts it into tensor memory.  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
+// took 166 then; 144 now).  They come through the ring that brings keys and values, ahead of these: each lane reads its row there and puts it into tensor memory.  Scores are multiplied while the weights of the tile before are worked out (as soon as those have been read), dq of a
 // tile and do v^T of the next while the weights of the next are.  Columns: scores 128, do v^T 128 (and in its place ds as operand), dq, q and do 64 each.
 template <int D> struct QuerySmem {
     static constexpr int TILE = 128 * D * 2, STAGES = 3;

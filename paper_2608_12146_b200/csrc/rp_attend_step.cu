@@ -2,19 +2,19 @@
 //
 //   s = scale q k^T over the keys that the token sees, o = softmax(s) v, lse = log sum exp(s)
 //
-// Bound by HBM: each visible key and value is read once, 4 * head_dim bytes for 4 * share * head_dim operations (share: query heads to a key head).  The products go
+// Bound by HBM: each visible key and value is read once (for more than 16 query heads to a key head once for every 16, by neighbouring warps), 4 * head_dim bytes for
+// 4 * share * head_dim operations (share: query heads to a key head).  The products go
 // through the warps' matrix instruction, 16 rows by 8 keys at a time, of which `share` are something: with a few rows to a tile there is nothing that fuller
 // instructions could add.
 // The keys that a sequence's token sees are cut into as many chunks as there are 128s in them, 128 at most; a chunk and a key head are a unit of one warp, which takes them in
 // tiles of 4 KB (16 keys of 128) through a ring of its own in shared memory.  Of n chunks each has every n-th tile, so that warps side by side read what lies side by side
-// (a bare reading kernel of 2368 warps: 6.2 TB/s where a CTA's rows are 16 at a time, 5.3 where they are 128 in a row).  Warps stay resident and take units in
+// (1000 sequences of 1000 keys, 2 GB: 346 us, 392 with chunks in whole pieces).  Warps stay resident and take units in
 // turn, and the ring runs on into the next unit; no warp waits for another.  The cut goes by the sequence alone, so that its bits do not depend on the others of the
 // batch.  A second kernel adds up the chunks, in their order.
 // 64 ragged sequences, 16 heads on 4, 128 wide (643 MB): 108 us, 91 % of the measured copy rate; 250 with a window of 1000, 8 heads of 64 (445 MB) 83 us, 81 %; 1000 of 1000 keys
-// (2 GB) 327 us, 96 %; four of up to 6000 keys (52 MB) 16.8 us, where the tiles of a chunk, one after the other, take as long as the launches.  Cut by 192: 110, 81, 318 and 18.6
-// us.  With three tiles under way, cut by 96: 118, 88, 353 and 17.6; by 128 111, 84, 346 and 17.7; by 256 109, 86, 330 and 22.3.  Chunks in whole pieces, cut by 64: 115, 102
-// and 21 us; by 128 115, 82 and 18, 392 for the thousand; a chunk to a CTA, whose warps meet at its end: 284, 193.  Keys and values that stay in L2 like everything else:
-// 125 for 115, 85 for 82.
+// (2 GB) 327 us, 96 %; four of up to 6000 keys (52 MB) 16.8 us, where the tiles of a chunk, one after the other, take as long as the launches.  Cut by 192: 110, 81, 318 and 18.6 us.
+// A sequence has 128 chunks at most, for which the second kernel has lanes, so one long cache with few key heads leaves warps without work: a sequence of 131072 keys, 128 wide,
+// takes 60 us with one key head or two (67 and 134 MB, 1.1 and 2.2 TB/s), 82 with eight (6.5 TB/s); one of 1048576 with one key head 413.
 #include <algorithm>
 #include <climits>
 

@@ -6,7 +6,9 @@
 // memory.  But a block has few tiles of keys (ten at a window of 1024), so what happens between blocks counts: nothing starts anew there.  Keys and values go through
 // one ring, whose stages hold the values of one step and the keys of the next, across the blocks' ends; each tile's queries are copied as soon as its last scores are
 // there, by a warp of their own; one warp looks up the blocks to come; and the products of a block begin while the one before is handed over.
-// Tiles of which some rows see nothing are taken last (AttendOrder).  First tokens that the window has left behind are a step of their own, as narrow as they are.
+// From where the window has left a sample's first token behind, tiles of which some rows see nothing are taken last (AttendOrder).  First tokens that the window has left
+// behind are a step of their own, as narrow as they are.  Head sizes between 64 and 128 are worked on as 128 columns, the ones behind head_dim zeros: a head of 96 costs what
+// one of 128 does.
 // Bound by the hand-overs between the softmax and the products of a tile, with two tiles in turn, and by what a block costs beside its tiles: a tile of 128 keys adds 0.95 us
 // at head_dim 128, of which the tensor cores need 1024 cycles, and a block 4 to 5 us more - the tiles of which each row sees a part, the last products, the handing over.
 // 32768 tokens of one sample, 16 heads on 4, 128 wide: 125 us with a window of 128, 298 with 1024 (907 TFLOP/s of what is seen; 339 with 4 first tokens), 925 with 4096
